@@ -231,7 +231,7 @@ def _handles(s):
         if c["op"] == "qkv_bwd":
             h["workspace"] = torch.empty(vb.vsa2_qkv_bwd_workspace_bytes(c["dim"]), dtype=torch.uint8, device="cuda")
         if c["op"] == "matmul":
-            h["workspace"] = vb.fp8_matmul_workspace(c["m"], c["n"], c["k"], s["c"].dtype, "cuda")
+            h["workspace"] = vb.fp8_matmul_workspace(c["m"], c["n"], c["k"], "cuda")
         s["handles"] = h
     return vb, s["handles"]
 
