@@ -317,6 +317,96 @@ size_t vsa2_gate_bwd_workspace_bytes(const vsa2_params* p, int32_t hidden);
 int vsa2_gate_bwd(const vsa2_params* p, int32_t hidden, const void* x, const void* w_g, const float* gate,
                   const float* dgate, float* d_w_g, void* dx, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ---- From a layer's hidden states to its attention (the paper has no counterpart: Sec. 2.2 begins at Q, K, V) ------------------
+ * X -> vsa2_fp8_quantize -> vsa2_fp8_matmul (the projection) -> vsa2_qkv_fwd (norms, positions, heads) -> vsa2_route, vsa2_attn_fwd;
+ * backward: vsa2_attn_bwd -> vsa2_qkv_bwd -> vsa2_fp8_quantize (both forms) -> vsa2_fp8_matmul for dX and for dW.  Each stands alone as well.
+ * Conventions as above; none of these calls allocates or synchronises.  Sizes of zero are valid: outputs that sum over nothing are zero. */
+
+/* Rotary positions with three axes.  Pair p of a head's channels turns by (its axis' position) * (its frequency); the pairs of
+ * axis t come first, then those of h, then w; channels behind the last pair stay as they are. */
+enum { VSA2_ROPE_PAIRS = 0,           /* pair p = channels 2p, 2p + 1 */
+       VSA2_ROPE_HALVES = 1 };        /* pair p = channels p, p + P (P pairs in all; P must be a multiple of 8) */
+#define VSA2_ROPE_MAX_PAIRS 64
+typedef struct vsa2_rope {
+  int32_t head_dim, layout;
+  int32_t axis_pairs[3];              /* pairs that turn with t, h, w; their sum is at most head_dim / 2 */
+  int32_t reserved;
+  uint64_t turn[VSA2_ROPE_MAX_PAIRS]; /* turns per position, in units of 2^-64 (whole turns dropped) */
+} vsa2_rope;
+/* Fills `out`: pair j of axis a (axis_channels[a] / 2 pairs, an even number of channels each) turns by scale[a] * theta[a]^(-2 j / axis_channels[a])
+ * radians per position.  theta > 0; scale finite (a factor on the positions, 1: none).  Pure host arithmetic. */
+int vsa2_rope_plan(int32_t head_dim, int32_t layout, const int32_t axis_channels[3], const double theta[3], const double scale[3],
+                   vsa2_rope* out);
+
+/* Where the tokens of a call lie (host struct). */
+typedef struct vsa2_place {
+  int32_t grid_t, grid_h, grid_w;     /* without `positions`: row r = first + i of the views' token i is raster token r of this grid; rows behind the */
+  int32_t first;                      /* grid (text tokens) do not turn */
+  const int32_t* positions;           /* device int32 [batch, tokens, 3] = (t, h, w) of every token, or NULL; any value, negative too */
+  int64_t positions_batch_stride;     /* elements between batch entries, 0: all have the same positions */
+} vsa2_place;
+
+/* Heads as a strided view [batch, heads, tokens, channels] (host struct); strides in elements, channels contiguous.  `data` and the strides
+ * must be multiples of 16 bytes; outputs must not overlap themselves.  heads = 0: absent (data may be NULL). */
+typedef struct vsa2_heads {
+  void* data;
+  int64_t batch_stride, head_stride, token_stride;
+  int32_t batch, heads, tokens, channels;      /* channels 64 or 128 */
+  int32_t dtype;                               /* VSA2_BF16 or VSA2_F32 */
+  int32_t reserved;
+} vsa2_heads;
+
+/* y = R(position) x, or with `inverse` R(position)^-1 x, which is the gradient.  x and y: views of one shape, each bf16 or fp32; y may be x itself (the
+ * same view). */
+int vsa2_rope_apply(const vsa2_rope* rope, const vsa2_place* place, const vsa2_heads* x, const vsa2_heads* y, int32_t inverse,
+                    void* cuda_stream);
+
+/* Norm of every head of q and k: x / sqrt(mean over the channels of x^2 + eps) * weight.  Weights device fp32 [channels], NULL: ones. */
+typedef struct vsa2_qk_norm {
+  const float* q_weight;
+  const float* k_weight;
+  float eps;                          /* >= 0; with 0 a row of zeros has no norm (NaN) */
+  int32_t reserved;
+} vsa2_qk_norm;
+
+/* The projection's q, k, v (views x[0..2], typically of one packed tensor [batch, tokens, (Hq + 2 Hkv) D]) -> normed, turned q and k and the
+ * copied v (views y[0..2], typically [batch, heads, L + Lt, D]).  norm NULL: none; rope NULL: none (place may be NULL then). */
+int vsa2_qkv_fwd(const vsa2_rope* rope, const vsa2_place* place, const vsa2_qk_norm* norm, const vsa2_heads x[3], const vsa2_heads y[3],
+                 void* cuda_stream);
+
+/* Gradients: dy[0..2] of y -> dx[0..2] of x, and of the norm's weights (device fp32 [channels], NULL: not wanted), summed over all tokens and
+ * heads.  x[0..1]: the forward's inputs q and k (only read with a norm; may be NULL without).  workspace: device, 256-byte aligned, at least
+ * vsa2_qkv_bwd_workspace_bytes; sums run in a fixed order (bitwise reproducible). */
+size_t vsa2_qkv_bwd_workspace_bytes(int32_t channels);
+int vsa2_qkv_bwd(const vsa2_rope* rope, const vsa2_place* place, const vsa2_qk_norm* norm, const vsa2_heads x[2], const vsa2_heads dy[3],
+                 const vsa2_heads dx[3], float* d_q_weight, float* d_k_weight, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* 8-bit form of a matrix [rows, cols]: e4m3 values and a power-of-two scale for each block of 128 along a row (host struct).
+ *   values  device, 16-byte aligned, row stride `ld` >= cols, a multiple of 16 (bytes between cols and ld are neither read nor written)
+ *   scales  device uint8 [ceil(cols / 512)][rows][4], 4-byte aligned: byte [g][r][j] is e + 127 of block 4 g + j of row r
+ * An element is value * 2^e. */
+typedef struct vsa2_fp8 {
+  void* values;
+  uint8_t* scales;
+  int64_t ld;
+} vsa2_fp8;
+
+/* x [rows, cols] (bf16 or fp32, row stride ld elements, any alignment of its type) -> `out`, the form of x, and / or `out_t`, the form of its transpose
+ * [cols, rows] (NULL: not wanted).  e = the least integer with max |x| <= 448 * 2^e over a block's finite values (at least -127); values are
+ * rounded to nearest, ties to even; infinities and NaN become NaN.  squares != 0: one scale for each 128 x 128 values (weights: both forms then hold
+ * the same values). */
+int vsa2_fp8_quantize(const void* x, int32_t x_dtype, int32_t rows, int32_t cols, int64_t ld, int32_t squares, const vsa2_fp8* out,
+                      const vsa2_fp8* out_t, void* cuda_stream);
+
+/* C [m, n] = A B^T with A [m, k] and B [n, k] in 8-bit form; products and sums in the tensor cores' fp32, C in bf16 or fp32 with row stride ldc
+ * elements.  The tile shapes suit B as the operand with many rows (a projection's weights [out, in]) and any m from 1.
+ *   workspace: device, 256-byte aligned, at least vsa2_fp8_matmul_workspace_bytes(m, n, k), zeroed once before its first use (calls leave its counters at
+ *   zero, so one may serve calls of any size that follow one another on a stream); its first word is the status of vsa2_device_status.
+ * Results do not depend on timing: parts of a sum are added in a fixed order. */
+size_t vsa2_fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
+int vsa2_fp8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_fp8* a, const vsa2_fp8* b, void* c, int32_t c_dtype, int64_t ldc,
+                    void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Synchronises `cuda_stream`, reads the status word at the start of `workspace` and stores it in
  * *status_out (host): VSA2_OK, VSA2_ERR_DEVICE_TIMEOUT or VSA2_ERR_MAP_OVERFLOW. */
 int vsa2_device_status(const void* workspace, void* cuda_stream, int32_t* status_out);

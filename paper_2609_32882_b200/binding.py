@@ -24,6 +24,7 @@ FLAG_PRECISE_BWD = 8
 FLAG_BF16_COARSE_FWD = 64
 FLAG_GROUP_ROUTING = 256
 FLAG_SELECT_NO_CLUSTERS = 512
+ROPE_PAIRS, ROPE_HALVES = 0, 1
 
 OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE_TOO_SMALL, ERR_MISALIGNED = -1, -2, -3, -4
@@ -35,7 +36,9 @@ EXPORTS = ("vsa2_query_sizes", "vsa2_route", "vsa2_route_scores", "vsa2_attn_fwd
            "vsa2_gate_fwd", "vsa2_gate_bwd", "vsa2_gate_bwd_workspace_bytes",
            "vsa2_attn_bwd_preferred_workspace_bytes", "vsa2_attn_bwd_scratch", "vsa2_attn_bwd_scratch_bytes",
            "vsa2_route_scratch", "vsa2_route_scratch_bytes", "vsa2_permute_cube_major",
-           "vsa2_selftest_timeout", "vsa2_debug_rescue_capacity", "vsa2_selftest_divmod")
+           "vsa2_selftest_timeout", "vsa2_debug_rescue_capacity", "vsa2_selftest_divmod",
+           "vsa2_rope_plan", "vsa2_rope_apply", "vsa2_qkv_fwd", "vsa2_qkv_bwd", "vsa2_qkv_bwd_workspace_bytes",
+           "vsa2_fp8_quantize", "vsa2_fp8_matmul", "vsa2_fp8_matmul_workspace_bytes")
 
 KERNELS = ("pool", "router_lse", "router_pool", "select", "coarse_fwd", "fine_fwd", "bwd_pre", "coarse_bwd",
            "fine_bwd_dq", "fine_bwd_dkv", "pool_router")
@@ -77,6 +80,30 @@ class Map(C.Structure):
 class Saved(C.Structure):
     _fields_ = [("qc", C.c_void_p), ("kc", C.c_void_p), ("vc", C.c_void_p), ("oc_hat", C.c_void_p),
                 ("lse_c", C.c_void_p), ("o_res", C.c_void_p)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("layout", C.c_int32), ("axis_pairs", C.c_int32 * 3), ("reserved", C.c_int32),
+                ("turn", C.c_uint64 * 64)]
+
+
+class Place(C.Structure):
+    _fields_ = [("grid_t", C.c_int32), ("grid_h", C.c_int32), ("grid_w", C.c_int32), ("first", C.c_int32),
+                ("positions", C.c_void_p), ("positions_batch_stride", C.c_int64)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("batch", C.c_int32), ("heads", C.c_int32), ("tokens", C.c_int32), ("channels", C.c_int32),
+                ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class QkNorm(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class Fp8Matrix(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_int64)]
 
 
 _LIB = None
@@ -122,8 +149,22 @@ def _lib():
         lib.vsa2_launch_count.restype = C.c_int64
         lib.vsa2_selftest_divmod.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         lib.vsa2_selftest_divmod.restype = C.c_int64
+        lib.vsa2_rope_plan.argtypes = [C.c_int32, C.c_int32, vp, vp, vp, C.POINTER(Rope)]
+        lib.vsa2_rope_apply.argtypes = [C.POINTER(Rope), C.POINTER(Place), C.POINTER(Heads), C.POINTER(Heads), C.c_int32, vp]
+        lib.vsa2_qkv_fwd.argtypes = [C.POINTER(Rope), C.POINTER(Place), C.POINTER(QkNorm), C.POINTER(Heads), C.POINTER(Heads), vp]
+        lib.vsa2_qkv_bwd.argtypes = [C.POINTER(Rope), C.POINTER(Place), C.POINTER(QkNorm), C.POINTER(Heads), C.POINTER(Heads),
+                                     C.POINTER(Heads), vp, vp, vp, sz, vp]
+        lib.vsa2_qkv_bwd_workspace_bytes.argtypes = [C.c_int32]
+        lib.vsa2_fp8_quantize.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.POINTER(Fp8Matrix),
+                                          C.POINTER(Fp8Matrix), vp]
+        lib.vsa2_fp8_matmul.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.POINTER(Fp8Matrix), C.POINTER(Fp8Matrix), vp, C.c_int32,
+                                        C.c_int64, vp, sz, vp]
+        lib.vsa2_fp8_matmul_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+        for fn in (lib.vsa2_qkv_bwd_workspace_bytes, lib.vsa2_fp8_matmul_workspace_bytes):
+            fn.restype = C.c_size_t
         for name in EXPORTS:
-            if name not in ("vsa2_strerror", "vsa2_route_scores", "vsa2_launch_count", "vsa2_last_cuda_error", "vsa2_selftest_divmod",
+            if name not in ("vsa2_qkv_bwd_workspace_bytes", "vsa2_fp8_matmul_workspace_bytes",
+                            "vsa2_strerror", "vsa2_route_scores", "vsa2_launch_count", "vsa2_last_cuda_error", "vsa2_selftest_divmod",
                             "vsa2_gate_bwd_workspace_bytes", "vsa2_attn_bwd_preferred_workspace_bytes",
                             "vsa2_attn_bwd_scratch_bytes", "vsa2_route_scratch_bytes"):
                 getattr(lib, name).restype = C.c_int
@@ -267,6 +308,201 @@ def vsa2_attn_bwd_scratch_bytes(p) -> int:
 def vsa2_attn_bwd_preferred_workspace_bytes(p) -> int:
     """Bytes of backward workspace with which vsa2_attn_bwd runs fastest (at least sizes.bwd_workspace_bytes)."""
     return int(_lib().vsa2_attn_bwd_preferred_workspace_bytes(C.byref(p)))
+
+
+# ---------------------------------------------------------------------------------------------
+# between a layer's hidden states and its attention
+# ---------------------------------------------------------------------------------------------
+def vsa2_rope_plan(head_dim, channels, theta=1e4, scale=1.0, layout=ROPE_PAIRS) -> Rope:
+    """Rotary positions on (t, h, w): `channels` of a head turn with each axis, pair j of axis a by scale theta^(-2 j / channels[a])
+    radians per position.  theta, scale: one number, or one for each axis."""
+    three = lambda v: (v, v, v) if isinstance(v, (int, float)) else tuple(v)
+    theta, scale, channels = three(theta), three(scale), tuple(channels)
+    if not len(theta) == len(scale) == len(channels) == 3:
+        raise ValueError("three axes are expected: (t, h, w)")
+    out = Rope()
+    _check(_lib().vsa2_rope_plan(head_dim, layout, (C.c_int32 * 3)(*channels), (C.c_double * 3)(*theta), (C.c_double * 3)(*scale),
+                                 C.byref(out)), "vsa2_rope_plan")
+    return out
+
+
+_DTYPES = None
+
+
+def _dtype(t):
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"expected bf16 or fp32, got {t.dtype}")
+    return code
+
+
+def _heads(t, out=None):
+    """A CUDA tensor [batch, heads, tokens, D], any strides but 1 for the channels, as a view; None: absent (see `_views`)."""
+    v = Heads() if out is None else out
+    if t.dim() != 4 or not t.is_cuda:
+        raise ValueError("expected a CUDA tensor [batch, heads, tokens, channels]")
+    v.batch, v.heads, v.tokens, v.channels = t.shape
+    v.batch_stride, v.head_stride, v.token_stride, last = t.stride()
+    if last != 1:
+        raise ValueError("the channels of a row must be contiguous")
+    v.data, v.dtype = t.data_ptr(), _dtype(t)
+    return v
+
+
+def _views(tensors):
+    """An array of views; a None among them is a view without heads."""
+    a = (Heads * len(tensors))()
+    for i, t in enumerate(tensors):
+        if t is not None:
+            _heads(t, a[i])
+    given = next((v for t, v in zip(tensors, a) if t is not None), None)
+    for t, v in zip(tensors, a):
+        if t is None and given is not None:
+            v.batch, v.tokens, v.channels, v.dtype = given.batch, given.tokens, given.channels, given.dtype
+    return a
+
+
+def _place(grid, first, positions, batch, tokens):
+    p = Place()
+    if positions is not None:
+        import torch
+        if positions.dtype != torch.int32 or not positions.is_cuda or not positions.is_contiguous():
+            raise ValueError("positions must be a contiguous CUDA int32 tensor [batch, tokens, 3] or [tokens, 3]")
+        shape = tuple(positions.shape)
+        if shape not in ((batch, tokens, 3), (1, tokens, 3), (tokens, 3)):
+            raise ValueError(f"positions {shape} do not fit {batch} x {tokens} tokens")
+        p.positions = positions.data_ptr()
+        p.positions_batch_stride = 3 * tokens if shape[0] == batch and len(shape) == 3 and batch > 1 else 0
+    elif grid is not None:
+        p.grid_t, p.grid_h, p.grid_w = grid
+    p.first = first
+    return p
+
+
+def _weight(w, channels, name):
+    if w is None:
+        return None
+    import torch
+    if w.dtype != torch.float32 or w.numel() != channels:
+        raise ValueError(f"{name} must be fp32 with {channels} elements")
+    return _ptr(w)
+
+
+def vsa2_rope_apply(rope, x, y, grid=None, first=0, positions=None, inverse=False, stream=None):
+    """y = R(position) x, or with `inverse` its inverse (the gradient); tensors [batch, heads, tokens, D], bf16 or fp32, any strides; y may be x.
+    Positions: rows first, first + 1, .. of the raster of `grid` (rows behind it do not turn), or int32 [batch or 1, tokens, 3]."""
+    vx, vy = _heads(x), _heads(y)
+    _check(_lib().vsa2_rope_apply(C.byref(rope), C.byref(_place(grid, first, positions, vx.batch, vx.tokens)), C.byref(vx), C.byref(vy),
+                                  1 if inverse else 0, _stream(stream)), "vsa2_rope_apply")
+
+
+def _norm(q_weight, k_weight, eps, channels, norm):
+    if not norm:
+        return None
+    return C.byref(QkNorm(_weight(q_weight, channels, "q_weight"), _weight(k_weight, channels, "k_weight"), eps, 0))
+
+
+def vsa2_qkv_fwd(rope, x, y, q_weight=None, k_weight=None, eps=1e-6, norm=True, grid=None, first=0, positions=None, stream=None):
+    """x = (q, k, v) as the projection leaves them -> y = (q, k, v) of the attention: norm of every head of q and k, weights, rotation (rope None:
+    none), v copied.  All are [batch, heads, tokens, D] views of any strides; a member may be None on both sides."""
+    vx, vy = _views(x), _views(y)
+    place = _place(grid, first, positions, vx[0].batch, vx[0].tokens)
+    _check(_lib().vsa2_qkv_fwd(C.byref(rope) if rope is not None else None, C.byref(place),
+                               _norm(q_weight, k_weight, eps, vx[0].channels, norm), vx, vy, _stream(stream)), "vsa2_qkv_fwd")
+
+
+def vsa2_qkv_bwd_workspace_bytes(channels) -> int:
+    return int(_lib().vsa2_qkv_bwd_workspace_bytes(channels))
+
+
+def vsa2_qkv_bwd(rope, x, dy, dx, q_weight, k_weight, d_q_weight, d_k_weight, workspace, eps=1e-6, norm=True, grid=None, first=0,
+                 positions=None, stream=None):
+    """Backward of vsa2_qkv_fwd: x = its inputs (q, k and, unused, v), dy = gradients of its outputs -> dx, and the weights' gradients (fp32, None: not
+    wanted).  workspace: vsa2_qkv_bwd_workspace_bytes(D) bytes (None without a norm)."""
+    vy, vd = _views(dy), _views(dx)
+    d = vy[0].channels
+    place = _place(grid, first, positions, vy[0].batch, vy[0].tokens)
+    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib().vsa2_qkv_bwd(C.byref(rope) if rope is not None else None, C.byref(place), _norm(q_weight, k_weight, eps, d, norm),
+                               _views(x[:2]) if norm else None, vy, vd, _weight(d_q_weight, d, "d_q_weight"),
+                               _weight(d_k_weight, d, "d_k_weight"), _ptr(workspace), nbytes, _stream(stream)), "vsa2_qkv_bwd")
+
+
+class Fp8:
+    """A matrix [rows, cols] in 8-bit form: `values` float8_e4m3fn [rows, cols] whose rows begin on 16-byte boundaries, `scales` uint8
+    [ceil(cols / 512), rows, 4] (exponents + 127, one for each 128 values of a row)."""
+    __slots__ = ("values", "scales")
+
+    def __init__(self, values, scales):
+        import torch
+        rows, cols = values.shape
+        if values.dtype != torch.float8_e4m3fn or (cols > 1 and values.stride(1) != 1):
+            raise ValueError("values must be float8_e4m3fn [rows, cols] with contiguous rows")
+        if scales.dtype != torch.uint8 or tuple(scales.shape) != (-(-cols // 512), rows, 4):
+            raise ValueError(f"scales must be uint8 {(-(-cols // 512), rows, 4)}, got {tuple(scales.shape)}")
+        self.values, self.scales = values, scales
+
+    @classmethod
+    def empty(cls, rows, cols, device="cuda"):
+        import torch
+        room = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.float8_e4m3fn, device=device)
+        return cls(room[:, :cols], torch.empty(-(-cols // 512), rows, 4, dtype=torch.uint8, device=device))
+
+    @property
+    def shape(self):
+        return tuple(self.values.shape)
+
+    def _struct(self):
+        values = self.values
+        if not values.is_cuda:
+            raise ValueError("expected a CUDA tensor")
+        rows, cols = values.shape
+        return Fp8Matrix(values.data_ptr(), _ptr(self.scales), values.stride(0) if rows > 1 else -(-cols // 16) * 16)
+
+    def dequantize(self):
+        """The matrix in fp32 (torch operations: for inspection and tests)."""
+        import torch
+        rows, cols = self.values.shape
+        e = self.scales.transpose(0, 1).reshape(rows, -1).to(torch.int32) - 127
+        return self.values.float() * torch.ldexp(torch.ones(e.shape, device=e.device), e).repeat_interleave(128, dim=1)[:, :cols]
+
+
+def vsa2_fp8_quantize(x, out=None, out_t=None, squares=False, stream=None):
+    """x [rows, cols] (bf16 or fp32, contiguous rows) -> `out`, its 8-bit form, and / or `out_t`, that of its transpose.  squares: one scale for each
+    128 x 128 values instead of each 128 of a row."""
+    if x.dim() != 2 or not x.is_cuda or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("expected a CUDA matrix with contiguous rows")
+    rows, cols = x.shape
+    if (out is not None and out.shape != (rows, cols)) or (out_t is not None and out_t.shape != (cols, rows)):
+        raise ValueError("outputs do not have the shape of x and of its transpose")
+    a, b = (None if o is None else C.byref(o._struct()) for o in (out, out_t))
+    _check(_lib().vsa2_fp8_quantize(x.data_ptr(), _dtype(x), rows, cols, x.stride(0) if rows > 1 else cols, 1 if squares else 0, a, b,
+                                    _stream(stream)), "vsa2_fp8_quantize")
+
+
+def vsa2_fp8_matmul_workspace_bytes(m, n, k) -> int:
+    return int(_lib().vsa2_fp8_matmul_workspace_bytes(m, n, k))
+
+
+def fp8_matmul_workspace(m, n, k, device="cuda"):
+    """Workspace of vsa2_fp8_matmul for products up to this size that follow one another on a stream."""
+    import torch
+    return torch.zeros(vsa2_fp8_matmul_workspace_bytes(m, n, k), dtype=torch.uint8, device=device)
+
+
+def vsa2_fp8_matmul(a, b, c, workspace, stream=None):
+    """c [m, n] = a b^T of two Fp8 matrices [m, k] and [n, k]; c bf16 or fp32 with contiguous rows."""
+    (m, k), (n, kb) = a.shape, b.shape
+    if k != kb or tuple(c.shape) != (m, n):
+        raise ValueError(f"shapes {a.shape}, {b.shape} and {tuple(c.shape)} do not fit")
+    if not c.is_cuda or (n > 1 and c.stride(1) != 1):
+        raise ValueError("c must be a CUDA matrix with contiguous rows")
+    _check(_lib().vsa2_fp8_matmul(m, n, k, C.byref(a._struct()), C.byref(b._struct()), c.data_ptr(), _dtype(c), c.stride(0) if m > 1 else n,
+                                  _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "vsa2_fp8_matmul")
 
 
 def vsa2_profile_events(kernel_id: int, start_event, stop_event):

@@ -5,6 +5,7 @@
 
 #include <atomic>
 
+#include "heads.cuh"
 #include "pooled_inputs.cuh"
 
 using namespace vsa2;
@@ -329,6 +330,88 @@ cudaError_t g_last_cuda_error = cudaSuccess;
       return VSA2_ERR_CUDA;                          \
     }                                                \
   } while (0)
+
+// ---- views of heads, matrices in 8 bits -----------------------------------------------------------------------------------
+// shape, type and strides of one view; `written`: its elements must be distinct as far as strides of zero show it
+int check_heads(const vsa2_heads& v, bool written) {
+  if (v.batch < 0 || v.heads < 0 || v.tokens < 0 || (v.dtype != VSA2_BF16 && v.dtype != VSA2_F32)) return VSA2_ERR_INVALID_ARG;
+  if (v.channels != 64 && v.channels != 128) return VSA2_ERR_UNSUPPORTED;
+  if (v.batch == 0 || v.heads == 0 || v.tokens == 0) return VSA2_OK;
+  if (v.data == nullptr) return VSA2_ERR_INVALID_ARG;
+  if (written && ((v.batch > 1 && v.batch_stride == 0) || (v.heads > 1 && v.head_stride == 0) || (v.tokens > 1 && v.token_stride == 0)))
+    return VSA2_ERR_INVALID_ARG;
+  const int64_t unit = v.dtype == VSA2_F32 ? 4 : 8;      // elements in 16 bytes
+  if ((v.batch > 1 && v.batch_stride % unit) || (v.heads > 1 && v.head_stride % unit) || (v.tokens > 1 && v.token_stride % unit) ||
+      !aligned16(v.data))
+    return VSA2_ERR_MISALIGNED;
+  return VSA2_OK;
+}
+bool same_shape(const vsa2_heads& a, const vsa2_heads& b) {
+  return a.batch == b.batch && a.heads == b.heads && a.tokens == b.tokens && a.channels == b.channels;
+}
+HeadsArg heads_arg(const vsa2_heads& v) { return HeadsArg{v.data, v.batch_stride, v.head_stride, v.token_stride, v.heads}; }
+
+// `shape`: batch, tokens and channels of the call
+int fill_turn(const vsa2_rope* rope, const vsa2_place* place, const vsa2_heads& shape, bool inverse, TurnArgs* t) {
+  memset(t, 0, sizeof *t);
+  t->sign = inverse ? -1.f : 1.f;
+  t->H = t->W = 1;
+  if (rope == nullptr) return VSA2_OK;
+  if (place == nullptr || rope->head_dim != shape.channels || (rope->layout != VSA2_ROPE_PAIRS && rope->layout != VSA2_ROPE_HALVES))
+    return VSA2_ERR_INVALID_ARG;
+  int64_t pairs = 0;
+  for (int a = 0; a < 3; ++a) {
+    if (rope->axis_pairs[a] < 0) return VSA2_ERR_INVALID_ARG;
+    pairs += rope->axis_pairs[a];
+  }
+  if (pairs > rope->head_dim / 2) return VSA2_ERR_INVALID_ARG;
+  if (rope->layout == VSA2_ROPE_HALVES && pairs % 8) return VSA2_ERR_UNSUPPORTED;
+  memcpy(t->turn, rope->turn, sizeof t->turn);
+  t->pairs = (int)pairs;
+  t->pairs_t = rope->axis_pairs[0];
+  t->pairs_th = rope->axis_pairs[0] + rope->axis_pairs[1];
+  if (place->positions != nullptr) {
+    if (reinterpret_cast<uintptr_t>(place->positions) & 3u) return VSA2_ERR_MISALIGNED;
+    if (place->positions_batch_stride < 0) return VSA2_ERR_INVALID_ARG;
+    t->positions = place->positions;
+    t->positions_sb = place->positions_batch_stride;
+    return VSA2_OK;
+  }
+  if (place->grid_t <= 0 || place->grid_h <= 0 || place->grid_w <= 0 || place->first < 0) return VSA2_ERR_INVALID_ARG;
+  const long long hw = (long long)place->grid_h * place->grid_w;
+  if (hw > 0x7fffffffLL || place->grid_t > 0x7fffffffLL / hw) return VSA2_ERR_UNSUPPORTED;
+  t->H = place->grid_h;
+  t->W = place->grid_w;
+  t->L = place->grid_t * hw;
+  t->first = place->first;
+  return VSA2_OK;
+}
+bool rope_halves(const vsa2_rope* rope) { return rope != nullptr && rope->layout == VSA2_ROPE_HALVES; }
+
+// x -> y of up to three views each: shapes agree, all of a side have one type; *empty: there is nothing to do
+int check_qkv(const vsa2_heads* x, const vsa2_heads* y, int n, bool* empty) {
+  int rc;
+  *empty = true;
+  for (int i = 0; i < n; ++i) {
+    if ((rc = check_heads(x[i], false)) != VSA2_OK || (rc = check_heads(y[i], true)) != VSA2_OK) return rc;
+    if (!same_shape(x[i], y[i]) || x[i].batch != x[0].batch || x[i].tokens != x[0].tokens || x[i].channels != x[0].channels ||
+        x[i].dtype != x[0].dtype || y[i].dtype != y[0].dtype)
+      return VSA2_ERR_INVALID_ARG;
+    if (x[i].heads > 0 && x[i].batch > 0 && x[i].tokens > 0) *empty = false;
+  }
+  if ((int64_t)x[0].batch * ((int64_t)x[0].tokens / 16 + 1) > 0x7fffffffLL || x[0].tokens > 0x7fffffff - 64) return VSA2_ERR_UNSUPPORTED;
+  return VSA2_OK;
+}
+
+int check_fp8(const vsa2_fp8* v, int rows, int cols) {
+  if (rows == 0 || cols == 0) return VSA2_OK;
+  if (v->values == nullptr || v->scales == nullptr || v->ld < cols) return VSA2_ERR_INVALID_ARG;
+  if (!aligned16(v->values) || v->ld % 16 || (reinterpret_cast<uintptr_t>(v->scales) & 3u)) return VSA2_ERR_MISALIGNED;
+  return VSA2_OK;
+}
+Fp8Arg fp8_arg(const vsa2_fp8* v) {
+  return v != nullptr ? Fp8Arg{reinterpret_cast<unsigned char*>(v->values), v->scales, v->ld} : Fp8Arg{nullptr, nullptr, 0};
+}
 
 }  // namespace
 
@@ -906,6 +989,163 @@ int vsa2_gate_bwd(const vsa2_params* p, int32_t hidden, const void* x, const voi
   VSA2_CUDA(launch_gate_bwd(g.batch, g.L, hidden, g.Hq, g.out_f32, reinterpret_cast<const bf16*>(x),
                             reinterpret_cast<const bf16*>(w_g), gate, dgate, d_w_g, dx, workspace,
                             reinterpret_cast<cudaStream_t>(cuda_stream)));
+  return VSA2_OK;
+}
+
+int vsa2_rope_plan(int32_t head_dim, int32_t layout, const int32_t axis_channels[3], const double theta[3], const double scale[3],
+                   vsa2_rope* out) {
+  if (!axis_channels || !theta || !scale || !out) return VSA2_ERR_INVALID_ARG;
+  if (layout != VSA2_ROPE_PAIRS && layout != VSA2_ROPE_HALVES) return VSA2_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return VSA2_ERR_UNSUPPORTED;
+  int64_t channels = 0;
+  for (int a = 0; a < 3; ++a) {
+    if (axis_channels[a] < 0 || axis_channels[a] % 2 || !(theta[a] > 0) || !isfinite(theta[a]) || !isfinite(scale[a])) return VSA2_ERR_INVALID_ARG;
+    channels += axis_channels[a];
+  }
+  if (channels > head_dim) return VSA2_ERR_INVALID_ARG;
+  if (layout == VSA2_ROPE_HALVES && channels % 16) return VSA2_ERR_UNSUPPORTED;
+  memset(out, 0, sizeof *out);
+  out->head_dim = head_dim;
+  out->layout = layout;
+  const long double two_pi = 6.283185307179586476925286766559L;
+  int p = 0;
+  for (int a = 0; a < 3; ++a) {
+    out->axis_pairs[a] = axis_channels[a] / 2;
+    for (int j = 0; j < axis_channels[a] / 2; ++j, ++p) {
+      const long double f = scale[a] * powl((long double)theta[a], -2.0L * j / axis_channels[a]) / two_pi;
+      const long double turn = ldexpl(f - floorl(f), 64);      // [0, 2^64]
+      out->turn[p] = turn < 18446744073709551615.0L ? (uint64_t)turn : 0u;
+    }
+  }
+  return VSA2_OK;
+}
+
+int vsa2_rope_apply(const vsa2_rope* rope, const vsa2_place* place, const vsa2_heads* x, const vsa2_heads* y, int32_t inverse,
+                    void* cuda_stream) {
+  if (!rope || !place || !x || !y) return VSA2_ERR_INVALID_ARG;
+  bool empty = false;
+  int rc = check_qkv(x, y, 1, &empty);
+  if (rc != VSA2_OK) return rc;
+  QkvArgs a = {};
+  if ((rc = fill_turn(rope, place, *x, inverse != 0, &a.turn)) != VSA2_OK) return rc;
+  if (empty) return VSA2_OK;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  a.x[0] = heads_arg(*x);
+  a.y[0] = heads_arg(*y);
+  a.tokens = x->tokens;
+  VSA2_CUDA(launch_qkv_fwd(a, x->channels, x->batch, x->dtype == VSA2_F32, y->dtype == VSA2_F32, rope_halves(rope),
+                           reinterpret_cast<cudaStream_t>(cuda_stream)));
+  return VSA2_OK;
+}
+
+int vsa2_qkv_fwd(const vsa2_rope* rope, const vsa2_place* place, const vsa2_qk_norm* norm, const vsa2_heads x[3], const vsa2_heads y[3],
+                 void* cuda_stream) {
+  if (!x || !y) return VSA2_ERR_INVALID_ARG;
+  bool empty = false;
+  int rc = check_qkv(x, y, 3, &empty);
+  if (rc != VSA2_OK) return rc;
+  QkvArgs a = {};
+  if ((rc = fill_turn(rope, place, x[0], false, &a.turn)) != VSA2_OK) return rc;
+  if (norm != nullptr && !(norm->eps >= 0.f)) return VSA2_ERR_INVALID_ARG;
+  if (empty) return VSA2_OK;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  for (int i = 0; i < 3; ++i) {
+    a.x[i] = heads_arg(x[i]);
+    a.y[i] = heads_arg(y[i]);
+  }
+  a.tokens = x[0].tokens;
+  a.norm = norm != nullptr;
+  if (norm != nullptr) {
+    a.w[0] = norm->q_weight;
+    a.w[1] = norm->k_weight;
+    a.eps = norm->eps;
+  }
+  VSA2_CUDA(launch_qkv_fwd(a, x[0].channels, x[0].batch, x[0].dtype == VSA2_F32, y[0].dtype == VSA2_F32, rope_halves(rope),
+                           reinterpret_cast<cudaStream_t>(cuda_stream)));
+  return VSA2_OK;
+}
+
+size_t vsa2_qkv_bwd_workspace_bytes(int32_t channels) { return channels == 64 || channels == 128 ? qkv_bwd_workspace_bytes(channels) : 0; }
+
+int vsa2_qkv_bwd(const vsa2_rope* rope, const vsa2_place* place, const vsa2_qk_norm* norm, const vsa2_heads x[2], const vsa2_heads dy[3],
+                 const vsa2_heads dx[3], float* d_q_weight, float* d_k_weight, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!dy || !dx || (norm != nullptr && (!x || !workspace))) return VSA2_ERR_INVALID_ARG;
+  bool empty = false;
+  int rc = check_qkv(dy, dx, 3, &empty);
+  if (rc != VSA2_OK) return rc;
+  QkvArgs a = {};
+  if ((rc = fill_turn(rope, place, dy[0], true, &a.turn)) != VSA2_OK) return rc;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  HeadsPair fwd = {};
+  if (norm != nullptr) {
+    if (!(norm->eps >= 0.f)) return VSA2_ERR_INVALID_ARG;
+    for (int i = 0; i < 2; ++i) {
+      if ((rc = check_heads(x[i], false)) != VSA2_OK) return rc;
+      if (!same_shape(x[i], dy[i]) || x[i].dtype != x[0].dtype) return VSA2_ERR_INVALID_ARG;
+      fwd.v[i] = heads_arg(x[i]);
+    }
+    if (!aligned256(workspace)) return VSA2_ERR_MISALIGNED;
+    if (workspace_bytes < qkv_bwd_workspace_bytes(dy[0].channels)) return VSA2_ERR_WORKSPACE_TOO_SMALL;
+    a.w[0] = norm->q_weight;
+    a.w[1] = norm->k_weight;
+    a.eps = norm->eps;
+    a.norm = 1;
+  }
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  if (empty || norm == nullptr) {      // (sums over nothing)
+    if (d_q_weight != nullptr) VSA2_CUDA(cudaMemsetAsync(d_q_weight, 0, dy[0].channels * sizeof(float), st));
+    if (d_k_weight != nullptr) VSA2_CUDA(cudaMemsetAsync(d_k_weight, 0, dy[0].channels * sizeof(float), st));
+    if (empty) return VSA2_OK;
+  }
+  for (int i = 0; i < 3; ++i) {
+    a.x[i] = heads_arg(dy[i]);
+    a.y[i] = heads_arg(dx[i]);
+  }
+  a.tokens = dy[0].tokens;
+  VSA2_CUDA(launch_qkv_bwd(a, fwd, dy[0].channels, dy[0].batch, norm != nullptr && x[0].dtype == VSA2_F32, dy[0].dtype == VSA2_F32,
+                           dx[0].dtype == VSA2_F32, rope_halves(rope), d_q_weight, d_k_weight, reinterpret_cast<float*>(workspace), st));
+  return VSA2_OK;
+}
+
+int vsa2_fp8_quantize(const void* x, int32_t x_dtype, int32_t rows, int32_t cols, int64_t ld, int32_t squares, const vsa2_fp8* out,
+                      const vsa2_fp8* out_t, void* cuda_stream) {
+  if (rows < 0 || cols < 0 || (x_dtype != VSA2_BF16 && x_dtype != VSA2_F32) || (out == nullptr && out_t == nullptr)) return VSA2_ERR_INVALID_ARG;
+  if (rows == 0 || cols == 0) return VSA2_OK;
+  if (x == nullptr || ld < cols) return VSA2_ERR_INVALID_ARG;
+  if (cols > 1 << 22 || rows > 0x7fffffff - 128) return VSA2_ERR_UNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(x) & (x_dtype == VSA2_F32 ? 3u : 1u)) return VSA2_ERR_MISALIGNED;
+  int rc;
+  if (out != nullptr && (rc = check_fp8(out, rows, cols)) != VSA2_OK) return rc;
+  if (out_t != nullptr && (rc = check_fp8(out_t, cols, rows)) != VSA2_OK) return rc;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  VSA2_CUDA(launch_fp8_quantize(x, x_dtype == VSA2_F32, rows, cols, ld, squares != 0, fp8_arg(out), fp8_arg(out_t),
+                                reinterpret_cast<cudaStream_t>(cuda_stream)));
+  return VSA2_OK;
+}
+
+size_t vsa2_fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k) {
+  return m < 0 || n < 0 || k < 0 ? 0 : fp8_matmul_workspace_bytes(m, n, k);
+}
+
+int vsa2_fp8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_fp8* a, const vsa2_fp8* b, void* c, int32_t c_dtype, int64_t ldc,
+                    void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (m < 0 || n < 0 || k < 0 || !a || !b || (c_dtype != VSA2_BF16 && c_dtype != VSA2_F32)) return VSA2_ERR_INVALID_ARG;
+  if (m == 0 || n == 0) return VSA2_OK;
+  if (c == nullptr || workspace == nullptr || ldc < n) return VSA2_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(c) & (c_dtype == VSA2_F32 ? 3u : 1u)) return VSA2_ERR_MISALIGNED;
+  if (m > 1 << 30 || n > 1 << 30 || k > 1 << 30 || ((long long)m / 16 + 1) * ((long long)n / 128 + 1) > 1 << 30) return VSA2_ERR_UNSUPPORTED;
+  int rc;
+  if ((rc = check_fp8(a, m, k)) != VSA2_OK || (rc = check_fp8(b, n, k)) != VSA2_OK) return rc;
+  if (!aligned256(workspace)) return VSA2_ERR_MISALIGNED;
+  if (workspace_bytes < fp8_matmul_workspace_bytes(m, n, k)) return VSA2_ERR_WORKSPACE_TOO_SMALL;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (k == 0) {
+    const size_t size = c_dtype == VSA2_F32 ? 4 : 2;
+    VSA2_CUDA(cudaMemset2DAsync(c, (size_t)ldc * size, 0, (size_t)n * size, (size_t)m, st));
+    return VSA2_OK;
+  }
+  VSA2_CUDA(launch_fp8_matmul(m, n, k, fp8_arg(a), fp8_arg(b), c, c_dtype == VSA2_F32, ldc, workspace, st));
   return VSA2_OK;
 }
 

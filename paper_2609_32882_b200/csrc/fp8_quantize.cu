@@ -1,0 +1,224 @@
+// 8-bit form of a matrix for vsa2_fp8_matmul: e4m3 values with a power-of-two scale for each block of 128 values along the rows, the same of
+// the transpose (blocks along the columns), or both from one reading.
+//   e = the least integer with max|x| <= 448 * 2^e over the block's finite values (448: the largest e4m3 value), at least -127
+//   value = x * 2^-e rounded to e4m3 (to nearest, ties to even); what is not finite becomes NaN
+// A power of two scales without rounding, so the 3 mantissa bits are all that is lost, and it is what the tensor cores multiply by themselves.
+// Both kernels are bound by memory: x read once, each form written once.
+#include "common.cuh"
+#include "heads.cuh"
+
+namespace vsa2 {
+
+namespace {
+
+constexpr int kQzThreads = 256;
+
+// exponent + 127 from the bits of max|x|: 448 = 1.75 * 2^8
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+  const int e = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return (uint32_t)max(e, 0);      // (at most 254 - 8 + 1)
+}
+__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+__device__ __forceinline__ uint32_t magnitude(float x) { return finite_bits(x) ? __float_as_uint(x) & 0x7fffffffu : 0u; }
+// an infinity becomes NaN here (times zero), the conversion alone would make it 448
+__device__ __forceinline__ float scaled(float x, float inv) { return finite_bits(x) ? x * inv : __uint_as_float(0x7fffffffu); }
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) { return e4m3x2(a, b) | e4m3x2(c, d) << 16; }
+
+template <bool F32>
+__device__ __forceinline__ float element(const void* x, size_t i) {
+  return F32 ? reinterpret_cast<const float*>(x)[i] : __bfloat162float(reinterpret_cast<const bf16*>(x)[i]);
+}
+// elements i .. i+7 of a row of `cols` (zeros beyond it); VEC: rows lie on 16-byte boundaries
+template <bool F32, bool VEC>
+__device__ __forceinline__ void load8(const void* x, size_t row_at, int i, int cols, float (&f)[8]) {
+  if (VEC && i + 8 <= cols) {
+    if (F32) {
+      const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(x) + row_at + i);
+      const float4 a = p[0], b = p[1];
+      f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    } else {
+      const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(x) + row_at + i);
+      const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f[2 * j] = __uint_as_float(u[j] << 16);
+        f[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = i + j < cols ? element<F32>(x, row_at + i + j) : 0.f;
+  }
+}
+// bytes i .. i+7 of a row of `cols` values (its start 16-byte aligned, i a multiple of 8)
+__device__ __forceinline__ void put8(unsigned char* row, int i, int cols, uint32_t lo, uint32_t hi) {
+  if (i + 8 <= cols) {
+    *reinterpret_cast<uint2*>(row + i) = make_uint2(lo, hi);
+  } else {
+    for (int j = 0; i + j < cols; ++j) row[i + j] = (unsigned char)((j < 4 ? lo >> 8 * j : hi >> 8 * (j - 4)) & 0xffu);
+  }
+}
+__device__ __forceinline__ uint32_t max_of(const float (&f)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, magnitude(f[j]));
+  return top;
+}
+
+// Rows alone: a team of 16 threads takes 512 columns of a row (four blocks, one word of scales).  grid (word groups, row tiles of 16)
+template <bool F32, bool VEC>
+__global__ void __launch_bounds__(kQzThreads) fp8_rows_kernel(const void* x, int rows, int cols, long long ld, Fp8Arg out) {
+  grid_enter();
+  const int l = threadIdx.x & 15;
+  const long long row = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int c0 = blockIdx.y * 512;
+  const long long r = row < rows ? row : rows - 1;
+  float f[4][8];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) load8<F32, VEC>(x, (size_t)r * ld, c0 + b * 128 + l * 8, cols, f[b]);
+  uint32_t word = 0;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    uint32_t top = max_of(f[b]);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (c0 + b * 128 >= cols) continue;
+    const uint32_t s = scale_byte(top);
+    const float inv = inverse_scale(s);
+    word |= s << 8 * b;
+    if (row < rows) {
+      const uint32_t lo = e4m3x4(scaled(f[b][0], inv), scaled(f[b][1], inv), scaled(f[b][2], inv), scaled(f[b][3], inv));
+      const uint32_t hi = e4m3x4(scaled(f[b][4], inv), scaled(f[b][5], inv), scaled(f[b][6], inv), scaled(f[b][7], inv));
+      put8(out.values + row * out.ld, c0 + b * 128 + l * 8, cols, lo, hi);
+    }
+  }
+  if (l == 0 && row < rows) reinterpret_cast<uint32_t*>(out.scales)[(size_t)blockIdx.y * rows + row] = word;
+}
+
+// scale of block kb of row `row` (of a form with `rows` rows and `blocks` blocks a row); the last block clears what is left of its word
+__device__ __forceinline__ void put_scale(unsigned char* scales, int rows, int row, int kb, int blocks, uint32_t byte) {
+  unsigned char* word = scales + ((size_t)(kb >> 2) * rows + row) * 4;
+  word[kb & 3] = (unsigned char)byte;
+  if (kb == blocks - 1)
+    for (int j = (kb & 3) + 1; j < 4; ++j) word[j] = 0;
+}
+
+// A tile of 128 x 128: both forms, or either.  A team of 16 threads holds 8 rows, 8 columns a thread.  The transpose passes through shared memory
+// as bytes: a thread writes the 8 bytes that its rows give a column; the 8-byte places of a column are exchanged by column group
+// so that neither side meets a bank twice.  grid (column tiles, row tiles)
+template <bool F32, bool VEC>
+__global__ void __launch_bounds__(kQzThreads) fp8_tile_kernel(const void* x, int rows, int cols, long long ld, int squares, Fp8Arg out,
+                                                              Fp8Arg out_t) {
+  grid_enter();
+  __shared__ __align__(16) unsigned char turned[128 * 128];
+  __shared__ uint32_t col_top[16][128];
+  __shared__ uint32_t tops[kQzThreads / 32];
+  const int l = threadIdx.x & 15, team = threadIdx.x >> 4, tid = threadIdx.x;
+  const int c0 = blockIdx.y * 128, r0 = blockIdx.x * 128;
+  float f[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = r0 + team * 8 + i;
+    if (row < rows) load8<F32, VEC>(x, (size_t)row * ld, c0 + l * 8, cols, f[i]);
+    else
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] = 0.f;
+  }
+  const int blocks = (cols + 127) / 128, blocks_t = (rows + 127) / 128;
+  uint32_t top_all = 0;
+  if (squares) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top_all = max(top_all, max_of(f[i]));
+    top_all = __reduce_max_sync(0xffffffffu, top_all);
+    if ((tid & 31) == 0) tops[tid >> 5] = top_all;
+    __syncthreads();
+    for (int i = 0; i < kQzThreads / 32; ++i) top_all = max(top_all, tops[i]);
+  }
+  if (out.values != nullptr) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t top = top_all;
+      if (!squares) {
+        top = max_of(f[i]);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      }
+      const uint32_t s = scale_byte(top);
+      const float inv = inverse_scale(s);
+      const int row = r0 + team * 8 + i;
+      if (row < rows) {
+        const uint32_t lo = e4m3x4(scaled(f[i][0], inv), scaled(f[i][1], inv), scaled(f[i][2], inv), scaled(f[i][3], inv));
+        const uint32_t hi = e4m3x4(scaled(f[i][4], inv), scaled(f[i][5], inv), scaled(f[i][6], inv), scaled(f[i][7], inv));
+        put8(out.values + row * out.ld, c0 + l * 8, cols, lo, hi);
+        if (l == 0) put_scale(out.scales, rows, row, blockIdx.y, blocks, s);
+      }
+    }
+  }
+  if (out_t.values == nullptr) return;
+  if (!squares) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, magnitude(f[i][j]));
+      col_top[team][l * 8 + j] = top;
+    }
+    __syncthreads();
+    if (tid < 128) {
+      uint32_t top = 0;
+      for (int t = 0; t < 16; ++t) top = max(top, col_top[t][tid]);
+      col_top[0][tid] = top;
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float inv = inverse_scale(scale_byte(squares ? top_all : col_top[0][l * 8 + j]));
+    const uint32_t lo = e4m3x4(scaled(f[0][j], inv), scaled(f[1][j], inv), scaled(f[2][j], inv), scaled(f[3][j], inv));
+    const uint32_t hi = e4m3x4(scaled(f[4][j], inv), scaled(f[5][j], inv), scaled(f[6][j], inv), scaled(f[7][j], inv));
+    *reinterpret_cast<uint2*>(turned + (l * 8 + j) * 128 + ((team ^ l) << 3)) = make_uint2(lo, hi);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 128 * 8 / kQzThreads; ++u) {
+    const int e = u * kQzThreads + tid, c = e >> 3, part = (e & 7) * 2, g = c >> 3;      // places part, part + 1 of column c
+    uint4 v = *reinterpret_cast<const uint4*>(turned + c * 128 + (((part ^ g) & ~1) << 3));
+    if (g & 1) v = make_uint4(v.z, v.w, v.x, v.y);
+    if (c0 + c < cols) {
+      unsigned char* row = out_t.values + (long long)(c0 + c) * out_t.ld;
+      const int i = r0 + part * 8;
+      if (i + 16 <= rows) {
+        *reinterpret_cast<uint4*>(row + i) = v;
+      } else {
+        put8(row, i, rows, v.x, v.y);
+        put8(row, i + 8, rows, v.z, v.w);
+      }
+    }
+  }
+  if (tid < 128 && c0 + tid < cols)
+    put_scale(out_t.scales, cols, c0 + tid, blockIdx.x, blocks_t, scale_byte(squares ? top_all : col_top[0][tid]));
+}
+
+}  // namespace
+
+cudaError_t launch_fp8_quantize(const void* x, int x_f32, int rows, int cols, long long ld, bool squares, const Fp8Arg& out,
+                                const Fp8Arg& out_t, cudaStream_t st) {
+  const size_t bytes = x_f32 ? 4 : 2;
+  const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && (size_t)ld * bytes % 16 == 0;
+  auto go = [&](auto rows_kernel, auto tile_kernel) {
+    if (!squares && out_t.values == nullptr)
+      return launch_kernel(rows_kernel, dim3((rows + 15) / 16, (cols + 511) / 512), kQzThreads, 0, st, x, rows, cols, ld, out);
+    return launch_kernel(tile_kernel, dim3((rows + 127) / 128, (cols + 127) / 128), kQzThreads, 0, st, x, rows, cols, ld,
+                         squares ? 1 : 0, out, out_t);
+  };
+  if (x_f32) return vec ? go(fp8_rows_kernel<true, true>, fp8_tile_kernel<true, true>) : go(fp8_rows_kernel<true, false>, fp8_tile_kernel<true, false>);
+  return vec ? go(fp8_rows_kernel<false, true>, fp8_tile_kernel<false, true>) : go(fp8_rows_kernel<false, false>, fp8_tile_kernel<false, false>);
+}
+
+}  // namespace vsa2

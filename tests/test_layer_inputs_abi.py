@@ -1,0 +1,206 @@
+"""CPU-only checks of the entry points between hidden states and attention: the rotation's plan, and what each call refuses before any CUDA call."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+from paper_2609_32882_b200 import binding as vb
+from paper_2609_32882_b200 import build as vbuild
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    vbuild.build_library()
+    return vb._lib()
+
+
+def heads(data=256, batch=2, heads=3, tokens=5, channels=64, dtype=vb.BF16, strides=None):
+    sb, sh, st = strides or (heads * tokens * channels, tokens * channels, channels)
+    return vb.Heads(data, sb, sh, st, batch, heads, tokens, channels, dtype, 0)
+
+
+def place(**kw):
+    p = vb.Place(1, 1, 5, 0, None, 0)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+def test_plan_holds_the_frequencies_as_fractions_of_a_turn():
+    channels, theta, scale = (44, 42, 42), (1e4, 500.0, 1e6), (1.0, 0.5, -2.0)
+    for layout in (vb.ROPE_PAIRS, vb.ROPE_HALVES):
+        plan = vb.vsa2_rope_plan(128, channels, theta=theta, scale=scale, layout=layout)
+        assert list(plan.axis_pairs) == [22, 21, 21] and plan.head_dim == 128 and plan.layout == layout
+        p = 0
+        for a, c in enumerate(channels):
+            for j in range(c // 2):
+                want = scale[a] * theta[a] ** (-2.0 * j / c) / (2 * math.pi) % 1.0
+                assert abs(plan.turn[p] / 2.0 ** 64 - want) <= 2.0 ** -50        # (the check's own 64-bit rounding)
+                p += 1
+        assert p == 64
+
+
+def test_plan_is_exact_where_the_fraction_is_known():
+    """Positions that turn by whole turns: scale 2 pi is not a 64-bit number, but its nearest one is 2^-52 off at most."""
+    plan = vb.vsa2_rope_plan(64, (0, 0, 2), scale=math.pi / 2)
+    assert abs(plan.turn[0] - (1 << 62)) <= 1 << 10
+    assert vb.vsa2_rope_plan(64, (0, 0, 64), scale=0.0).turn[5] == 0
+    assert list(vb.vsa2_rope_plan(64, (0, 0, 0)).axis_pairs) == [0, 0, 0]
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(head_dim=96, channels=(32, 32, 32)), vb.ERR_UNSUPPORTED),
+    (dict(head_dim=64, channels=(16, 24, 23)), vb.ERR_INVALID_ARG),                    # odd
+    (dict(head_dim=64, channels=(16, 26, 24)), vb.ERR_INVALID_ARG),                    # more than the head has
+    (dict(head_dim=64, channels=(-2, 24, 24)), vb.ERR_INVALID_ARG),
+    (dict(head_dim=64, channels=(2, 24, 24), layout=vb.ROPE_HALVES), vb.ERR_UNSUPPORTED),
+    (dict(head_dim=64, channels=(16, 24, 24), layout=2), vb.ERR_INVALID_ARG),
+    (dict(head_dim=64, channels=(16, 24, 24), theta=0.0), vb.ERR_INVALID_ARG),
+    (dict(head_dim=64, channels=(16, 24, 24), theta=float("inf")), vb.ERR_INVALID_ARG),
+    (dict(head_dim=64, channels=(16, 24, 24), scale=(1.0, float("nan"), 1.0)), vb.ERR_INVALID_ARG),
+])
+def test_plan_refusals(kw, code):
+    with pytest.raises(vb.Vsa2Error) as e:
+        vb.vsa2_rope_plan(**kw)
+    assert e.value.code == code
+    with pytest.raises(ValueError):
+        vb.vsa2_rope_plan(64, (32, 32))
+
+
+@pytest.mark.parametrize("x,y,where,code", [
+    (dict(data=None), {}, {}, vb.ERR_INVALID_ARG),
+    (dict(data=264), {}, {}, vb.ERR_MISALIGNED),
+    (dict(strides=(960, 320, 68)), {}, {}, vb.ERR_MISALIGNED),                         # rows not on 16 bytes
+    ({}, dict(strides=(960, 320, 68)), {}, vb.ERR_MISALIGNED),
+    (dict(channels=32), dict(channels=32), {}, vb.ERR_UNSUPPORTED),
+    (dict(channels=128), dict(channels=128), {}, vb.ERR_INVALID_ARG),                  # not the plan's
+    (dict(heads=2), {}, {}, vb.ERR_INVALID_ARG),                                       # shapes differ
+    (dict(tokens=-1), dict(tokens=-1), {}, vb.ERR_INVALID_ARG),
+    (dict(dtype=2), {}, {}, vb.ERR_INVALID_ARG),
+    ({}, dict(strides=(960, 0, 64)), {}, vb.ERR_INVALID_ARG),                          # heads written over one another
+    ({}, {}, dict(grid_w=0), vb.ERR_INVALID_ARG),
+    ({}, {}, dict(first=-1), vb.ERR_INVALID_ARG),
+    ({}, {}, dict(grid_h=1 << 20, grid_w=1 << 20), vb.ERR_UNSUPPORTED),
+    ({}, {}, dict(positions=258), vb.ERR_MISALIGNED),
+    ({}, {}, dict(positions=256, positions_batch_stride=-15), vb.ERR_INVALID_ARG),
+])
+def test_rotation_refusals(lib, x, y, where, code):
+    rope = vb.vsa2_rope_plan(64, (16, 24, 24))
+    assert lib.vsa2_rope_apply(C.byref(rope), C.byref(place(**where)), C.byref(heads(**x)), C.byref(heads(**y)), 0, None) == code
+
+
+def test_null_structs_are_refused(lib):
+    rope, at, v = vb.vsa2_rope_plan(64, (16, 24, 24)), place(), heads()
+    full = [C.byref(rope), C.byref(at), C.byref(v), C.byref(v), 0, None]
+    for i in range(4):
+        args = list(full)
+        args[i] = None
+        assert lib.vsa2_rope_apply(*args) == vb.ERR_INVALID_ARG
+    three = (vb.Heads * 3)(v, v, v)
+    assert lib.vsa2_qkv_fwd(C.byref(rope), C.byref(at), None, None, three, None) == vb.ERR_INVALID_ARG
+    assert lib.vsa2_qkv_fwd(C.byref(rope), None, None, three, three, None) == vb.ERR_INVALID_ARG
+    assert lib.vsa2_fp8_quantize(256, vb.BF16, 1, 1, 1, 0, None, None, None) == vb.ERR_INVALID_ARG
+    assert lib.vsa2_rope_plan(64, 0, None, None, None, None) == vb.ERR_INVALID_ARG
+
+
+def test_damaged_plans_are_refused(lib):
+    v = heads()
+    for change in (dict(layout=3), dict(head_dim=128), dict(axis_pairs=(20, 20, 20)), dict(axis_pairs=(-1, 2, 2))):
+        rope = vb.vsa2_rope_plan(64, (16, 24, 24))
+        for k, val in change.items():
+            setattr(rope, k, (C.c_int32 * 3)(*val) if k == "axis_pairs" else val)
+        assert lib.vsa2_rope_apply(C.byref(rope), C.byref(place()), C.byref(v), C.byref(v), 0, None) == vb.ERR_INVALID_ARG
+
+
+def test_norm_and_gradient_refusals(lib):
+    rope, at = vb.vsa2_rope_plan(64, (16, 24, 24)), place()
+    three, two = (vb.Heads * 3)(heads(), heads(), heads()), (vb.Heads * 2)(heads(), heads())
+    norm = vb.QkNorm(256, 256, 1e-6, 0)
+    need = vb.vsa2_qkv_bwd_workspace_bytes(64)
+    assert need > 0 and vb.vsa2_qkv_bwd_workspace_bytes(96) == 0
+
+    def bwd(norm=norm, x=two, dy=three, dx=three, ws=256, nbytes=need):
+        return lib.vsa2_qkv_bwd(C.byref(rope), C.byref(at), C.byref(norm), x, dy, dx, 256, 256, ws, nbytes, None)
+
+    assert bwd(nbytes=need - 1) == vb.ERR_WORKSPACE_TOO_SMALL
+    assert bwd(ws=128) == vb.ERR_MISALIGNED
+    assert bwd(ws=None) == vb.ERR_INVALID_ARG
+    assert bwd(x=None) == vb.ERR_INVALID_ARG
+    assert bwd(norm=vb.QkNorm(256, 256, -1.0, 0)) == vb.ERR_INVALID_ARG
+    assert bwd(norm=vb.QkNorm(256, 256, float("nan"), 0)) == vb.ERR_INVALID_ARG
+    assert bwd(x=(vb.Heads * 2)(heads(), heads(heads=2))) == vb.ERR_INVALID_ARG
+    assert bwd(dy=(vb.Heads * 3)(heads(), heads(), heads(dtype=vb.F32))) == vb.ERR_INVALID_ARG       # one type for a side
+    assert bwd(dx=(vb.Heads * 3)(heads(), heads(tokens=4), heads())) == vb.ERR_INVALID_ARG
+    assert lib.vsa2_qkv_fwd(C.byref(rope), C.byref(at), C.byref(vb.QkNorm(256, 256, -1.0, 0)), three, three, None) == vb.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(rows=-1), vb.ERR_INVALID_ARG),
+    (dict(x=None), vb.ERR_INVALID_ARG),
+    (dict(x=257), vb.ERR_MISALIGNED),
+    (dict(ld=99), vb.ERR_INVALID_ARG),
+    (dict(dtype=5), vb.ERR_INVALID_ARG),
+    (dict(cols=1 << 23, ld=1 << 23), vb.ERR_UNSUPPORTED),
+    (dict(out=(0, 256, 112)), vb.ERR_INVALID_ARG),
+    (dict(out=(256, 256, 96)), vb.ERR_INVALID_ARG),          # rows shorter than the columns
+    (dict(out=(256, 256, 104)), vb.ERR_MISALIGNED),          # rows not on 16 bytes
+    (dict(out=(264, 256, 112)), vb.ERR_MISALIGNED),
+    (dict(out=(256, 258, 112)), vb.ERR_MISALIGNED),
+])
+def test_quantize_refusals(lib, kw, code):
+    a = dict(x=256, dtype=vb.BF16, rows=10, cols=100, ld=100, out=(256, 256, 112))
+    a.update(kw)
+    out = vb.Fp8Matrix(*a["out"])
+    assert lib.vsa2_fp8_quantize(a["x"], a["dtype"], a["rows"], a["cols"], a["ld"], 0, C.byref(out), None, None) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(m=-1), vb.ERR_INVALID_ARG),
+    (dict(c=None), vb.ERR_INVALID_ARG),
+    (dict(c=257), vb.ERR_MISALIGNED),
+    (dict(ldc=299), vb.ERR_INVALID_ARG),
+    (dict(c_dtype=7), vb.ERR_INVALID_ARG),
+    (dict(a=(256, 256, 128)), vb.ERR_INVALID_ARG),
+    (dict(b=(256, 256, 200)), vb.ERR_MISALIGNED),
+    (dict(b=(8, 256, 208)), vb.ERR_MISALIGNED),
+    (dict(a=(256, 0, 208)), vb.ERR_INVALID_ARG),
+    (dict(ws=None), vb.ERR_INVALID_ARG),
+    (dict(ws=128), vb.ERR_MISALIGNED),
+    (dict(short=1), vb.ERR_WORKSPACE_TOO_SMALL),
+    (dict(m=1 << 30, n=1 << 20, ldc=1 << 20), vb.ERR_UNSUPPORTED),
+])
+def test_product_refusals(lib, kw, code):
+    a = dict(m=20, n=300, k=200, a=(256, 256, 208), b=(256, 256, 208), c=256, c_dtype=vb.BF16, ldc=300, ws=256, short=0)
+    a.update(kw)
+    need = vb.vsa2_fp8_matmul_workspace_bytes(20, 300, 200)
+    assert lib.vsa2_fp8_matmul(a["m"], a["n"], a["k"], C.byref(vb.Fp8Matrix(*a["a"])), C.byref(vb.Fp8Matrix(*a["b"])), a["c"], a["c_dtype"],
+                               a["ldc"], a["ws"], need - a["short"], None) == code
+
+
+def test_sizes_of_zero_need_no_device(lib):
+    rope, at = vb.vsa2_rope_plan(64, (16, 24, 24)), place()
+    for kw in (dict(tokens=0), dict(batch=0), dict(heads=0)):
+        v = heads(data=None, **kw)
+        assert lib.vsa2_rope_apply(C.byref(rope), C.byref(at), C.byref(v), C.byref(v), 0, None) == vb.OK
+    f = vb.Fp8Matrix(256, 256, 208)
+    assert lib.vsa2_fp8_matmul(0, 300, 200, C.byref(f), C.byref(f), 256, vb.BF16, 300, 256, 1 << 30, None) == vb.OK
+    assert lib.vsa2_fp8_quantize(None, vb.BF16, 0, 100, 100, 0, C.byref(f), None, None) == vb.OK
+
+
+def test_binding_refuses_what_it_cannot_marshal():
+    rope = vb.vsa2_rope_plan(64, (16, 24, 24))
+    with pytest.raises(ValueError):
+        vb.vsa2_rope_apply(rope, torch.zeros(1, 1, 4, 64), torch.zeros(1, 1, 4, 64), grid=(1, 1, 4))      # host tensors
+    with pytest.raises(ValueError):
+        vb.Fp8(torch.zeros(4, 4), torch.zeros(1, 4, 4, dtype=torch.uint8))
+    with pytest.raises(ValueError):
+        vb.Fp8(torch.zeros(4, 4).to(torch.float8_e4m3fn), torch.zeros(1, 4, 1, dtype=torch.uint8))
+    f = vb.Fp8.empty(4, 20, device="cpu")
+    assert f.shape == (4, 20) and f.values.stride(0) == 32
+    with pytest.raises(ValueError):
+        f._struct()
+    with pytest.raises(ValueError):
+        vb.vsa2_fp8_quantize(torch.zeros(4, 20), f)
+    with pytest.raises(ValueError):
+        vb.vsa2_fp8_matmul(f, vb.Fp8.empty(4, 21, device="cpu"), torch.zeros(4, 4), None)
