@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libvsa2.so")
@@ -150,15 +151,13 @@ def _lib():
         lib.vsa2_selftest_divmod.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         lib.vsa2_selftest_divmod.restype = C.c_int64
         lib.vsa2_rope_plan.argtypes = [C.c_int32, C.c_int32, vp, vp, vp, C.POINTER(Rope)]
-        lib.vsa2_rope_apply.argtypes = [C.POINTER(Rope), C.POINTER(Place), C.POINTER(Heads), C.POINTER(Heads), C.c_int32, vp]
-        lib.vsa2_qkv_fwd.argtypes = [C.POINTER(Rope), C.POINTER(Place), C.POINTER(QkNorm), C.POINTER(Heads), C.POINTER(Heads), vp]
-        lib.vsa2_qkv_bwd.argtypes = [C.POINTER(Rope), C.POINTER(Place), C.POINTER(QkNorm), C.POINTER(Heads), C.POINTER(Heads),
-                                     C.POINTER(Heads), vp, vp, vp, sz, vp]
+        # (structs come as bytes, or as pointers to the classes above)
+        lib.vsa2_rope_apply.argtypes = [vp, vp, vp, vp, C.c_int32, vp]
+        lib.vsa2_qkv_fwd.argtypes = [vp] * 6
+        lib.vsa2_qkv_bwd.argtypes = [vp] * 9 + [sz, vp]
         lib.vsa2_qkv_bwd_workspace_bytes.argtypes = [C.c_int32]
-        lib.vsa2_fp8_quantize.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.POINTER(Fp8Matrix),
-                                          C.POINTER(Fp8Matrix), vp]
-        lib.vsa2_fp8_matmul.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.POINTER(Fp8Matrix), C.POINTER(Fp8Matrix), vp, C.c_int32,
-                                        C.c_int64, vp, sz, vp]
+        lib.vsa2_fp8_quantize.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int32, vp, vp, vp]
+        lib.vsa2_fp8_matmul.argtypes = [C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, C.c_int32, C.c_int64, vp, sz, vp]
         lib.vsa2_fp8_matmul_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
         for fn in (lib.vsa2_qkv_bwd_workspace_bytes, lib.vsa2_fp8_matmul_workspace_bytes):
             fn.restype = C.c_size_t
@@ -326,68 +325,78 @@ def vsa2_rope_plan(head_dim, channels, theta=1e4, scale=1.0, layout=ROPE_PAIRS) 
     return out
 
 
-_DTYPES = None
+# The structs of these calls are packed into bytes instead of filled field by field: a toy grid's calls wait for the host.
+_HEADS = struct.Struct("=QqqqiiiiiI")                  # vsa2_heads
+_HEADS2, _HEADS3 = struct.Struct("=" + 2 * "QqqqiiiiiI"), struct.Struct("=" + 3 * "QqqqiiiiiI")
+_PLACE = struct.Struct("=iiiiQq")                      # vsa2_place
+_NORM = struct.Struct("=QQfi")                         # vsa2_qk_norm
+_FP8 = struct.Struct("=QQq")                           # vsa2_fp8
+_TORCH, _DTYPES = None, {}
+
+
+def _torch():
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _DTYPES.update({torch.bfloat16: BF16, torch.float32: F32})
+        _TORCH = torch
+    return _TORCH
 
 
 def _dtype(t):
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-        _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
     code = _DTYPES.get(t.dtype)
     if code is None:
-        raise ValueError(f"expected bf16 or fp32, got {t.dtype}")
+        _torch()
+        code = _DTYPES.get(t.dtype)
+        if code is None:
+            raise ValueError(f"expected bf16 or fp32, got {t.dtype}")
     return code
 
 
-def _heads(t, out=None):
-    """A CUDA tensor [batch, heads, tokens, D], any strides but 1 for the channels, as a view; None: absent (see `_views`)."""
-    v = Heads() if out is None else out
-    if t.dim() != 4 or not t.is_cuda:
+def _view(t):
+    """The fields of vsa2_heads of a CUDA tensor [batch, heads, tokens, D], any strides but 1 for the channels."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 4 or not t.is_cuda:
         raise ValueError("expected a CUDA tensor [batch, heads, tokens, channels]")
-    v.batch, v.heads, v.tokens, v.channels = t.shape
-    v.batch_stride, v.head_stride, v.token_stride, last = t.stride()
-    if last != 1:
+    if strides[3] != 1:
         raise ValueError("the channels of a row must be contiguous")
-    v.data, v.dtype = t.data_ptr(), _dtype(t)
-    return v
+    return (t.data_ptr(), strides[0], strides[1], strides[2], *shape, _dtype(t), 0)
 
 
 def _views(tensors):
-    """An array of views; a None among them is a view without heads."""
-    a = (Heads * len(tensors))()
-    for i, t in enumerate(tensors):
-        if t is not None:
-            _heads(t, a[i])
-    given = next((v for t, v in zip(tensors, a) if t is not None), None)
-    for t, v in zip(tensors, a):
-        if t is None and given is not None:
-            v.batch, v.tokens, v.channels, v.dtype = given.batch, given.tokens, given.channels, given.dtype
-    return a
+    """Those of two or three; a None among them is a view without heads."""
+    views = [None if t is None else _view(t) for t in tensors]
+    if None in views:
+        like = next((v for v in views if v is not None), None)
+        if like is None:
+            raise ValueError("no tensor is given")
+        absent = (0, 0, 0, 0, like[4], 0, like[6], like[7], like[8], 0)
+        views = [absent if v is None else v for v in views]
+    return views
+
+
+def _pack(views):
+    if len(views) == 3:
+        return _HEADS3.pack(*views[0], *views[1], *views[2])
+    return _HEADS2.pack(*views[0], *views[1])
 
 
 def _place(grid, first, positions, batch, tokens):
-    p = Place()
-    if positions is not None:
-        import torch
-        if positions.dtype != torch.int32 or not positions.is_cuda or not positions.is_contiguous():
-            raise ValueError("positions must be a contiguous CUDA int32 tensor [batch, tokens, 3] or [tokens, 3]")
-        shape = tuple(positions.shape)
-        if shape not in ((batch, tokens, 3), (1, tokens, 3), (tokens, 3)):
-            raise ValueError(f"positions {shape} do not fit {batch} x {tokens} tokens")
-        p.positions = positions.data_ptr()
-        p.positions_batch_stride = 3 * tokens if shape[0] == batch and len(shape) == 3 and batch > 1 else 0
-    elif grid is not None:
-        p.grid_t, p.grid_h, p.grid_w = grid
-    p.first = first
-    return p
+    if positions is None:
+        t, h, w = grid if grid is not None else (0, 0, 0)
+        return _PLACE.pack(t, h, w, first, 0, 0)
+    if positions.dtype != _torch().int32 or not positions.is_cuda or not positions.is_contiguous():
+        raise ValueError("positions must be a contiguous CUDA int32 tensor [batch, tokens, 3] or [tokens, 3]")
+    shape = tuple(positions.shape)
+    if shape not in ((batch, tokens, 3), (1, tokens, 3), (tokens, 3)):
+        raise ValueError(f"positions {shape} do not fit {batch} x {tokens} tokens")
+    return _PLACE.pack(0, 0, 0, first, positions.data_ptr(), 3 * tokens if len(shape) == 3 and shape[0] > 1 else 0)
 
 
 def _weight(w, channels, name):
     if w is None:
-        return None
-    import torch
-    if w.dtype != torch.float32 or w.numel() != channels:
+        return 0
+    if w.dtype != _torch().float32 or w.numel() != channels:
         raise ValueError(f"{name} must be fp32 with {channels} elements")
     return _ptr(w)
 
@@ -395,24 +404,22 @@ def _weight(w, channels, name):
 def vsa2_rope_apply(rope, x, y, grid=None, first=0, positions=None, inverse=False, stream=None):
     """y = R(position) x, or with `inverse` its inverse (the gradient); tensors [batch, heads, tokens, D], bf16 or fp32, any strides; y may be x.
     Positions: rows first, first + 1, .. of the raster of `grid` (rows behind it do not turn), or int32 [batch or 1, tokens, 3]."""
-    vx, vy = _heads(x), _heads(y)
-    _check(_lib().vsa2_rope_apply(C.byref(rope), C.byref(_place(grid, first, positions, vx.batch, vx.tokens)), C.byref(vx), C.byref(vy),
+    vx, vy = _view(x), _view(y)
+    _check(_lib().vsa2_rope_apply(C.byref(rope), _place(grid, first, positions, vx[4], vx[6]), _HEADS.pack(*vx), _HEADS.pack(*vy),
                                   1 if inverse else 0, _stream(stream)), "vsa2_rope_apply")
 
 
 def _norm(q_weight, k_weight, eps, channels, norm):
-    if not norm:
-        return None
-    return C.byref(QkNorm(_weight(q_weight, channels, "q_weight"), _weight(k_weight, channels, "k_weight"), eps, 0))
+    return _NORM.pack(_weight(q_weight, channels, "q_weight"), _weight(k_weight, channels, "k_weight"), eps, 0) if norm else None
 
 
 def vsa2_qkv_fwd(rope, x, y, q_weight=None, k_weight=None, eps=1e-6, norm=True, grid=None, first=0, positions=None, stream=None):
     """x = (q, k, v) as the projection leaves them -> y = (q, k, v) of the attention: norm of every head of q and k, weights, rotation (rope None:
     none), v copied.  All are [batch, heads, tokens, D] views of any strides; a member may be None on both sides."""
     vx, vy = _views(x), _views(y)
-    place = _place(grid, first, positions, vx[0].batch, vx[0].tokens)
-    _check(_lib().vsa2_qkv_fwd(C.byref(rope) if rope is not None else None, C.byref(place),
-                               _norm(q_weight, k_weight, eps, vx[0].channels, norm), vx, vy, _stream(stream)), "vsa2_qkv_fwd")
+    one = vx[0]
+    _check(_lib().vsa2_qkv_fwd(C.byref(rope) if rope is not None else None, _place(grid, first, positions, one[4], one[6]),
+                               _norm(q_weight, k_weight, eps, one[7], norm), _pack(vx), _pack(vy), _stream(stream)), "vsa2_qkv_fwd")
 
 
 def vsa2_qkv_bwd_workspace_bytes(channels) -> int:
@@ -424,12 +431,13 @@ def vsa2_qkv_bwd(rope, x, dy, dx, q_weight, k_weight, d_q_weight, d_k_weight, wo
     """Backward of vsa2_qkv_fwd: x = its inputs (q, k and, unused, v), dy = gradients of its outputs -> dx, and the weights' gradients (fp32, None: not
     wanted).  workspace: vsa2_qkv_bwd_workspace_bytes(D) bytes (None without a norm)."""
     vy, vd = _views(dy), _views(dx)
-    d = vy[0].channels
-    place = _place(grid, first, positions, vy[0].batch, vy[0].tokens)
+    one = vy[0]
+    d = one[7]
     nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    _check(_lib().vsa2_qkv_bwd(C.byref(rope) if rope is not None else None, C.byref(place), _norm(q_weight, k_weight, eps, d, norm),
-                               _views(x[:2]) if norm else None, vy, vd, _weight(d_q_weight, d, "d_q_weight"),
-                               _weight(d_k_weight, d, "d_k_weight"), _ptr(workspace), nbytes, _stream(stream)), "vsa2_qkv_bwd")
+    _check(_lib().vsa2_qkv_bwd(C.byref(rope) if rope is not None else None, _place(grid, first, positions, one[4], one[6]),
+                               _norm(q_weight, k_weight, eps, d, norm), _pack(_views(x[:2])) if norm else None, _pack(vy), _pack(vd),
+                               _weight(d_q_weight, d, "d_q_weight"), _weight(d_k_weight, d, "d_k_weight"), _ptr(workspace), nbytes,
+                               _stream(stream)), "vsa2_qkv_bwd")
 
 
 class Fp8:
@@ -438,11 +446,11 @@ class Fp8:
     __slots__ = ("values", "scales")
 
     def __init__(self, values, scales):
-        import torch
+        torch = _torch()
         rows, cols = values.shape
         if values.dtype != torch.float8_e4m3fn or (cols > 1 and values.stride(1) != 1):
             raise ValueError("values must be float8_e4m3fn [rows, cols] with contiguous rows")
-        if scales.dtype != torch.uint8 or tuple(scales.shape) != (-(-cols // 512), rows, 4):
+        if scales.dtype != torch.uint8 or scales.shape != (-(-cols // 512), rows, 4):
             raise ValueError(f"scales must be uint8 {(-(-cols // 512), rows, 4)}, got {tuple(scales.shape)}")
         self.values, self.scales = values, scales
 
@@ -456,12 +464,12 @@ class Fp8:
     def shape(self):
         return tuple(self.values.shape)
 
-    def _struct(self):
+    def _pack(self):
         values = self.values
         if not values.is_cuda:
             raise ValueError("expected a CUDA tensor")
         rows, cols = values.shape
-        return Fp8Matrix(values.data_ptr(), _ptr(self.scales), values.stride(0) if rows > 1 else -(-cols // 16) * 16)
+        return _FP8.pack(values.data_ptr(), _ptr(self.scales), values.stride(0) if rows > 1 else -(-cols // 16) * 16)
 
     def dequantize(self):
         """The matrix in fp32 (torch operations: for inspection and tests)."""
@@ -479,7 +487,7 @@ def vsa2_fp8_quantize(x, out=None, out_t=None, squares=False, stream=None):
     rows, cols = x.shape
     if (out is not None and out.shape != (rows, cols)) or (out_t is not None and out_t.shape != (cols, rows)):
         raise ValueError("outputs do not have the shape of x and of its transpose")
-    a, b = (None if o is None else C.byref(o._struct()) for o in (out, out_t))
+    a, b = None if out is None else out._pack(), None if out_t is None else out_t._pack()
     _check(_lib().vsa2_fp8_quantize(x.data_ptr(), _dtype(x), rows, cols, x.stride(0) if rows > 1 else cols, 1 if squares else 0, a, b,
                                     _stream(stream)), "vsa2_fp8_quantize")
 
@@ -501,7 +509,7 @@ def vsa2_fp8_matmul(a, b, c, workspace, stream=None):
         raise ValueError(f"shapes {a.shape}, {b.shape} and {tuple(c.shape)} do not fit")
     if not c.is_cuda or (n > 1 and c.stride(1) != 1):
         raise ValueError("c must be a CUDA matrix with contiguous rows")
-    _check(_lib().vsa2_fp8_matmul(m, n, k, C.byref(a._struct()), C.byref(b._struct()), c.data_ptr(), _dtype(c), c.stride(0) if m > 1 else n,
+    _check(_lib().vsa2_fp8_matmul(m, n, k, a._pack(), b._pack(), c.data_ptr(), _dtype(c), c.stride(0) if m > 1 else n,
                                   _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "vsa2_fp8_matmul")
 
 

@@ -25,68 +25,81 @@ namespace vsa2 {
 namespace {
 
 constexpr int kMmCtas = 148;            // most CTAs (the workspace is laid out for them)
-constexpr int kMmThreads = 256;
-constexpr int kMmScaleSlots = 4;
+constexpr int kMmThreads = 384;
+constexpr int kMmStagesMost = 12;
 constexpr int kMmCounters = 2 * kMmCtas;
+constexpr int kMmChunk = 32;            // blocks of K that an accumulator sums for an fp32 result
+constexpr int kMmBunch = 3;             // HALVES = 2: blocks whose products with one half are issued together at a tile's two ends
 constexpr uint32_t kMmPBytes = 128 * 128;
-constexpr uint32_t kMmScaleBytes = 512 + 1024;       // words of 128 rows of B, of up to 256 rows of A
-constexpr uint32_t kMmTmScales = 480;                // columns of tensor memory: accumulators at 0 and 256, scales here (2 x 16)
 
-template <int NT>
+// NT columns an accumulator; PAIR: CTAs that share a tile (2: a pair of SMs, 256 rows of B, each CTA fetches its rows of B and half the rows
+// of A); HALVES: accumulators side by side (2: a tile of 2 NT columns takes both)
+template <int NT, int PAIR, int HALVES>
 struct MmTile {
-  static constexpr uint32_t STAGE = kMmPBytes + NT * 128;
-  static constexpr uint32_t ROOM = 227 * 1024 - 2048 - kMmScaleSlots * kMmScaleBytes;
-  static constexpr int STAGES = ROOM / STAGE < 12 ? ROOM / STAGE : 12;
-  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + kMmScaleSlots * kMmScaleBytes;
-  static constexpr int SFQ = (NT + 127) / 128;        // 512-byte pieces of A's scales
+  static constexpr int COLS = NT * HALVES;
+  static constexpr uint32_t QBYTES = NT / PAIR * 128;                       // rows of A for one accumulator
+  static constexpr uint32_t STAGE = kMmPBytes + HALVES * QBYTES;
+  static constexpr int SFQ = (NT + 127) / 128;                              // 512-byte pieces of A's scales for one accumulator
+  static constexpr uint32_t SCALES = 512 + HALVES * SFQ * 512;              // words of 128 rows of B, of the rows of A
+  static constexpr int SLOTS = HALVES == 2 ? 2 : 4;
+  static constexpr uint32_t ROOM = 227 * 1024 - 2048 - SLOTS * SCALES;
+  static constexpr int STAGES = ROOM / STAGE < kMmStagesMost ? ROOM / STAGE : kMmStagesMost;
+  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + SLOTS * SCALES;
+  // columns of tensor memory: accumulators at 0 and 256 (of 224 at most), scales of even and odd groups of four blocks behind them
+  __host__ __device__ static constexpr uint32_t scales_at(uint32_t group) { return 224 + (group & 1) * 256; }
 };
 
 struct MmArgs {
   int m, n, k, kb;                   // kb: blocks of K
   int pt, qt, gq;                    // tiles along n, along m; tiles along m that are taken together
-  int whole;                         // tiles that are dealt out whole (a multiple of the CTAs)
-  long long units;                   // blocks of K of the other tiles, all told
+  int chunk;                         // most blocks of K in one accumulator
+  int whole, rest, splits;           // tiles that are dealt out whole; the others, each cut into `splits` ranges of K
   const uint32_t* a_scales;
   const uint32_t* b_scales;
   void* c;
   long long ldc;
-  int c_f32;
   StatusBlock* status;
   int* counters;
   float* partial;
 };
 
 struct MmMisc {
-  uint64_t full[12], empty[12], sc_full[kMmScaleSlots], sc_empty[kMmScaleSlots], d_full[2], d_empty[2], group;
+  uint64_t full[kMmStagesMost], empty[kMmStagesMost], sc_full[4], sc_empty[4], d_full[2], d_empty[2], group[2], written[2];
   uint32_t tmem_base;
   int abort_flag;
-  int last;
+  int last[2];
 };
 
-// A CTA's share: whole tiles first, then its part of the units of the others.
+// The items of a CTA (or pair): every `all`-th, the whole tiles first, then the first ranges of the others, their second ranges, ..: CTAs that run at the
+// same time read the same part of K, so that rows they share come from memory once (shares of equal size, begun anywhere: 2304 x 1536, K = 32760
+// 192 us).  Each item in pieces of at most `chunk` blocks.
 struct MmWalk {
-  int tile, kb0, kb1;                // current segment
-  int next;                          // its number
-  long long u, u1;
-  __device__ __forceinline__ void init(const MmArgs& a) {
-    next = 0;
-    u = a.units * blockIdx.x / gridDim.x;
-    u1 = a.units * (blockIdx.x + 1) / gridDim.x;
+  int tile, kb0, kb1;                // current piece
+  int r0, r1, part;                  // the item's blocks; its place among the parts, -1: a whole tile
+  int item, all;
+  __device__ __forceinline__ void init(int me, int of) {
+    item = me;
+    all = of;
+    kb1 = r1 = 0;
   }
   __device__ __forceinline__ bool advance(const MmArgs& a) {
-    const long long t = (long long)next * gridDim.x + blockIdx.x;
-    if (t < a.whole) {
-      ++next;
-      tile = (int)t; kb0 = 0; kb1 = a.kb;
-      return true;
+    if (kb1 < r1) {
+      kb0 = kb1;
+    } else {
+      if (item >= a.whole + a.rest * a.splits) return false;
+      part = -1;
+      tile = item; r0 = 0; r1 = a.kb;
+      if (item >= a.whole && a.splits > 1) {
+        part = item - a.whole;
+        const int split = part / a.rest;
+        tile = a.whole + part - split * a.rest;
+        r0 = (int)((long long)a.kb * split / a.splits);
+        r1 = (int)((long long)a.kb * (split + 1) / a.splits);
+      }
+      item += all;
+      kb0 = r0;
     }
-    if (u >= u1) return false;
-    ++next;
-    const int r = (int)(u / a.kb);
-    tile = a.whole + r;
-    kb0 = (int)(u - (long long)r * a.kb);
-    kb1 = (int)min((long long)a.kb, kb0 + (u1 - u));
-    u += kb1 - kb0;
+    kb1 = min(r1, kb0 + a.chunk);
     return true;
   }
 };
@@ -96,217 +109,373 @@ __device__ __forceinline__ void mm_place(const MmArgs& a, int tile, int& p, int&
   q = g * a.gq + r - p * w;
 }
 
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-               ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(bar)), "r"(c0), "r"(c1)
-               : "memory");
+// ---- a CTA alone, or a pair whose first CTA issues the products and holds the barriers that both sides arrive at
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t leaders(uint64_t* bar) {      // address of the first CTA's barrier
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(tc::smem_u32(bar)));
+  return r;
+}
+template <int PAIR>
+__device__ __forceinline__ void arrive_leader(uint64_t* bar) {
+  if constexpr (PAIR == 1) tc::mbar_arrive(bar);
+  else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar)) : "memory");
+}
+template <int PAIR>
+__device__ __forceinline__ void tma_load_rows(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1) {
+  if constexpr (PAIR == 1)
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(bar)), "r"(c0), "r"(c1)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(leaders(bar)), "r"(c0), "r"(c1)
+                 : "memory");
 }
 // 32 x 16 bytes of shared memory to four columns of tensor memory, the same in each group of 32 lanes: words (r, j) of row j * 32 + r
+// (a pair: each CTA's own)
+template <int PAIR>
 __device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  if constexpr (PAIR == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
+template <int PAIR>
 __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa, uint32_t sfb, bool accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
-      : "memory");
+  if constexpr (PAIR == 1)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
+        : "memory");
 }
-// e4m3 x e4m3, ue8m0 scales, both operands K-major; `sf`: which byte of the scales' words
-__device__ __forceinline__ constexpr uint32_t idesc_scaled(int n, uint32_t sf) {
-  return (sf << 4) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | (1u << 27) | (sf << 29);
+// arrives at the barrier of this CTA, or of both of the pair, once the products and copies issued so far are done
+template <int PAIR>
+__device__ __forceinline__ void commit_all(uint64_t* bar) {
+  if constexpr (PAIR == 1) tc::mma_commit(bar);
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(tc::smem_u32(bar)), "h"((uint16_t)3)
+                 : "memory");
+}
+template <int PAIR>
+__device__ __forceinline__ void mm_alloc(uint32_t* to) {
+  if constexpr (PAIR == 1) {
+    tc::tmem_alloc(to, 512);
+    tc::tmem_relinquish();
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tc::smem_u32(to)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+}
+template <int PAIR>
+__device__ __forceinline__ void mm_dealloc(uint32_t base) {
+  if constexpr (PAIR == 1) tc::tmem_dealloc(base, 512);
+  else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(base) : "memory");
+}
+// 32 lanes x STEP columns of an accumulator
+template <int STEP>
+__device__ __forceinline__ void load_columns(uint32_t taddr, float (&v)[STEP]) {
+  uint32_t r[STEP];
+  tc::tmem_ld32(taddr, r);
+  tc::tmem_ld_wait();
+#pragma unroll
+  for (int c = 0; c < STEP; ++c) v[c] = __uint_as_float(r[c]);
+}
+// e4m3 x e4m3, ue8m0 scales, both operands K-major, 128 rows a CTA; `sf`: which byte of the scales' words
+template <int NT, int PAIR>
+__device__ __forceinline__ constexpr uint32_t idesc_scaled(uint32_t sf) {
+  return (sf << 4) | ((uint32_t)(NT >> 3) << 17) | (1u << 23) | ((uint32_t)PAIR << 27) | (sf << 29);
 }
 
-template <int NT>
-__global__ void __launch_bounds__(kMmThreads, 1) fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constant__ CUtensorMap tm_q,
-                                                                   const __grid_constant__ MmArgs a) {
-  using T = MmTile<NT>;
+// `count` columns (rows of the result) of an accumulator, `stride` elements apart.  Whole steps are straight code: with a test for each
+// element the loads and stores came one at a time, and the epilogue took longer than the products of 40 blocks.
+__device__ __forceinline__ void put(float* to, float v) { *to = v; }
+__device__ __forceinline__ void put(bf16* to, float v) { *to = __float2bfloat16_rn(v); }
+template <int STEP, typename TO>
+__device__ __forceinline__ void put_columns(TO* to, long long stride, int count, const float (&v)[STEP]) {
+  if (count >= STEP) {
+#pragma unroll
+    for (int c = 0; c < STEP; ++c, to += stride) put(to, v[c]);
+  } else {
+#pragma unroll
+    for (int c = 0; c < STEP; ++c, to += stride)
+      if (c < count) put(to, v[c]);
+  }
+}
+template <int STEP>
+__device__ __forceinline__ void add_columns(const float* from, long long stride, int count, float (&v)[STEP]) {
+  float old[STEP];
+#pragma unroll
+  for (int c = 0; c < STEP; ++c) old[c] = __ldcg(from + min(c, count - 1) * stride);
+#pragma unroll
+  for (int c = 0; c < STEP; ++c) v[c] += old[c];
+}
+
+template <int NT, int PAIR, int HALVES, typename TO>
+__global__ void __cluster_dims__(PAIR, 1, 1) __launch_bounds__(kMmThreads, 1)
+fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ MmArgs a) {
+  using T = MmTile<NT, PAIR, HALVES>;
   extern __shared__ unsigned char mm_smem[];
   __shared__ MmMisc misc_store;
   MmMisc* misc = &misc_store;
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(mm_smem) + 1023) & ~(uintptr_t)1023);
   unsigned char* scales = ring + T::STAGES * T::STAGE;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = PAIR == 1 ? 0 : (int)cluster_rank();
   if (tid == 0) {
     misc->abort_flag = 0;
     for (int s = 0; s < T::STAGES; ++s) {
       tc::mbar_init(&misc->full[s], 1);
       tc::mbar_init(&misc->empty[s], 1);
     }
-    for (int s = 0; s < kMmScaleSlots; ++s) {
-      tc::mbar_init(&misc->sc_full[s], 32);
+    for (int s = 0; s < T::SLOTS; ++s) {
+      tc::mbar_init(&misc->sc_full[s], PAIR);
       tc::mbar_init(&misc->sc_empty[s], 1);
     }
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&misc->d_full[s], 1);
-      tc::mbar_init(&misc->d_empty[s], 128);
+      tc::mbar_init(&misc->d_empty[s], 4 * PAIR);
+      tc::mbar_init(&misc->group[s], 128);
+      tc::mbar_init(&misc->written[s], 128);
     }
-    tc::mbar_init(&misc->group, 128);
     tc::fence_barrier_init();
     tc::prefetch_tmap(&tm_p);
     tc::prefetch_tmap(&tm_q);
   }
-  if (warp == 3) {
-    tc::tmem_alloc(&misc->tmem_base, 512);
-    tc::tmem_relinquish();
-  }
+  if (warp == 3) mm_alloc<PAIR>(&misc->tmem_base);
   tc::tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR == 2) cluster_sync_all();
   tc::tc_fence_after();
   const uint32_t tmem_base = misc->tmem_base;
   grid_enter(false);
   {
     MmWalk w;
-    w.init(a);
+    w.init(blockIdx.x / PAIR, gridDim.x / PAIR);
     if (warp == 0) {
       // ---------------------------------------------------------------- operands
       uint32_t it = 0;
       while (w.advance(a)) {
         int p, q;
         mm_place(a, w.tile, p, q);
+        const int row_p = (p * PAIR + rank) * 128, row_q = q * T::COLS + rank * (NT / PAIR);
         for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
           const uint32_t s = it % T::STAGES;
           int ok = 1;
           if (lane == 0) {
             ok = tc::mbar_wait(&misc->empty[s], ((it / T::STAGES) & 1) ^ 1, &misc->abort_flag);
             if (ok) {
-              tc::mbar_expect_tx(&misc->full[s], T::STAGE);
-              tma_load_2d(ring + s * T::STAGE, &tm_p, &misc->full[s], kb * 128, p * 128);
-              tma_load_2d(ring + s * T::STAGE + kMmPBytes, &tm_q, &misc->full[s], kb * 128, q * NT);
+              unsigned char* to = ring + s * T::STAGE;
+              if (rank == 0) tc::mbar_expect_tx(&misc->full[s], PAIR * T::STAGE);
+              tma_load_rows<PAIR>(to, &tm_p, &misc->full[s], kb * 128, row_p);
+#pragma unroll
+              for (int h = 0; h < HALVES; ++h)
+                tma_load_rows<PAIR>(to + kMmPBytes + h * T::QBYTES, &tm_q, &misc->full[s], kb * 128, row_q + h * NT);
             }
           }
           if (!__shfl_sync(0xffffffffu, ok, 0)) goto done;
         }
       }
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
       // ---------------------------------------------------------------- products (converged warp, one lane issues)
       const uint64_t ring_desc = tc::smem_desc_sw128(tc::smem_u32(ring), 16, 1024);
       const uint64_t scale_desc = tc::smem_desc_plain(tc::smem_u32(scales), 16, 128);
       uint32_t it = 0, sc = 0, seg = 0;
+      // products of block kb (number `at` of all) with half h of the columns, scales of group number `group`
+      auto products = [&](int kb, uint32_t at, uint32_t group, uint32_t buf, int h, bool first) {
+        const uint64_t dp = ring_desc + (uint64_t)(at % T::STAGES * T::STAGE >> 4), dq = dp + (uint64_t)((kMmPBytes + h * T::QBYTES) >> 4);
+        const uint32_t idesc = idesc_scaled<NT, PAIR>(kb & 3), tm_sc = tmem_base + T::scales_at(group);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          mma_scaled<PAIR>(tmem_base + buf * 256, dp + 2 * ks, dq + 2 * ks, idesc, tm_sc, tm_sc + 4 + h * 4 * T::SFQ, ks > 0 || !first);
+      };
       for (; w.advance(a); ++seg) {
-        const uint32_t buf = seg & 1;
-        VSA2_WAIT(&misc->d_empty[buf], ((seg >> 1) & 1) ^ 1);
-        for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
-          const uint32_t s = it % T::STAGES;
-          const bool fresh = kb == w.kb0 || (kb & 3) == 0;
-          if (fresh) {
-            VSA2_WAIT(&misc->sc_full[sc % kMmScaleSlots], (sc / kMmScaleSlots) & 1);
-            ++sc;
-          }
-          VSA2_WAIT(&misc->full[s], (it / T::STAGES) & 1);
-          tc::tc_fence_after();
-          if (tc::elect_one()) {
-            const uint32_t slot = (sc - 1) % kMmScaleSlots, tm_sc = tmem_base + kMmTmScales + ((sc - 1) & 1) * 16;
+        if constexpr (HALVES == 1) VSA2_WAIT(&misc->d_empty[seg & 1], ((seg >> 1) & 1) ^ 1);
+        else VSA2_WAIT(&misc->d_empty[0], (seg & 1) ^ 1);
+        // HALVES = 2: both accumulators are in use all the time.  Of the last blocks of a tile those with the first half come first, so that its epilogue
+        // runs behind those with the second half; of the first blocks likewise, so that the second half's epilogue runs behind those with the first
+        int kb = w.kb0;
+        while (kb < w.kb1) {
+          const int bunch = HALVES == 1 ? 1 : kb == w.kb0 || kb == w.kb1 - kMmBunch ? min(kMmBunch, w.kb1 - kb) : 1;
+          uint32_t first_group = sc;
+          for (int i = 0; i < bunch; ++i) {
+            const uint32_t s = (it + i) % T::STAGES;
+            const bool fresh = kb + i == w.kb0 || ((kb + i) & 3) == 0;
             if (fresh) {
-              const uint64_t d = scale_desc + (uint64_t)(slot * kMmScaleBytes >> 4);
-              copy_scales(tm_sc, d);
-#pragma unroll
-              for (int i = 0; i < T::SFQ; ++i) copy_scales(tm_sc + 4 + 4 * i, d + (uint64_t)((512 + 512 * i) >> 4));
-              tc::mma_commit(&misc->sc_empty[slot]);
+              VSA2_WAIT(&misc->sc_full[sc % T::SLOTS], (sc / T::SLOTS) & 1);
+              if constexpr (PAIR == 2) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+              ++sc;
             }
-            const uint64_t dp = ring_desc + (uint64_t)(s * T::STAGE >> 4), dq = dp + (uint64_t)(kMmPBytes >> 4);
-            const uint32_t idesc = idesc_scaled(NT, kb & 3);
+            if (i == 0) first_group = sc - 1;
+            VSA2_WAIT(&misc->full[s], ((it + i) / T::STAGES) & 1);
+            tc::tc_fence_after();
+            if (tc::elect_one()) {
+              if (fresh) {
+                const uint32_t slot = (sc - 1) % T::SLOTS, tm_sc = tmem_base + T::scales_at(sc - 1);
+                const uint64_t d = scale_desc + (uint64_t)(slot * T::SCALES >> 4);
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-              mma_scaled(tmem_base + buf * 256, dp + 2 * ks, dq + 2 * ks, idesc, tm_sc, tm_sc + 4, ks > 0 || kb > w.kb0);
-            tc::mma_commit(&misc->empty[s]);
-            if (kb == w.kb1 - 1) tc::mma_commit(&misc->d_full[buf]);
+                for (int j = 0; j < 1 + HALVES * T::SFQ; ++j) copy_scales<PAIR>(tm_sc + 4 * j, d + (uint64_t)(512 * j >> 4));
+                commit_all<PAIR>(&misc->sc_empty[slot]);
+              }
+              products(kb + i, it + i, sc - 1, HALVES == 1 ? seg & 1 : 0, 0, kb + i == w.kb0);
+              if (HALVES == 1) commit_all<PAIR>(&misc->empty[s]);
+              if (kb + i == w.kb1 - 1) commit_all<PAIR>(&misc->d_full[HALVES == 1 ? seg & 1 : 0]);
+            }
+            __syncwarp();
           }
-          __syncwarp();
+          if constexpr (HALVES == 2) {
+            if (kb == w.kb0) {
+              VSA2_WAIT(&misc->d_empty[1], (seg & 1) ^ 1);
+              tc::tc_fence_after();
+            }
+            uint32_t group = first_group;
+            for (int i = 0; i < bunch; ++i) {
+              if (i > 0 && ((kb + i) & 3) == 0) ++group;
+              if (tc::elect_one()) {
+                products(kb + i, it + i, group, 1, 1, kb + i == w.kb0);
+                commit_all<PAIR>(&misc->empty[(it + i) % T::STAGES]);
+                if (kb + i == w.kb1 - 1) commit_all<PAIR>(&misc->d_full[1]);
+              }
+              __syncwarp();
+            }
+          }
+          kb += bunch;
+          it += bunch;
         }
       }
     } else if (warp == 2) {
       // ---------------------------------------------------------------- scales: words of rows lane, lane + 32, .. as 16 bytes a lane
-      uint32_t sc = 0;
-      while (w.advance(a)) {
-        int p, q;
-        mm_place(a, w.tile, p, q);
-        for (int g = w.kb0 >> 2; g <= (w.kb1 - 1) >> 2; ++g, ++sc) {
-          const uint32_t slot = sc % kMmScaleSlots;
-          uint32_t v[4 + 4 * T::SFQ];
+      // AHEAD groups of four blocks are on their way from memory at a time: with one, a group's latency bound short rows (one row of A against 15,360 x
+      // 5,120: 26 us)
+      constexpr int NV = 4 + 4 * HALVES * T::SFQ, AHEAD = NV <= 8 ? 6 : NV <= 12 ? 4 : 2;
+      uint32_t v[AHEAD][NV];
+      bool there[AHEAD];
+      int g = 0, g_end = 0, row_p = 0, row_q = 0;
+      auto next = [&](uint32_t (&to)[NV]) {
+        if (g >= g_end) {
+          if (!w.advance(a)) return false;
+          int p, q;
+          mm_place(a, w.tile, p, q);
+          row_p = (p * PAIR + rank) * 128 + lane;
+          row_q = q * T::COLS + lane;
+          g = w.kb0 >> 2;
+          g_end = ((w.kb1 - 1) >> 2) + 1;
+        }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = p * 128 + j * 32 + lane;
-            v[j] = r < a.n ? a.b_scales[(size_t)g * a.n + r] : 0u;
-          }
+        for (int j = 0; j < 4; ++j) to[j] = row_p + j * 32 < a.n ? a.b_scales[(size_t)g * a.n + row_p + j * 32] : 0u;
 #pragma unroll
-          for (int j = 0; j < 4 * T::SFQ; ++j) {
-            const int i = j * 32 + lane, r = q * NT + i;
-            v[4 + j] = i < NT && r < a.m ? a.a_scales[(size_t)g * a.m + r] : 0u;
-          }
-          VSA2_WAIT_PARKED(&misc->sc_empty[slot], ((sc / kMmScaleSlots) & 1) ^ 1);
-          unsigned char* to = scales + slot * kMmScaleBytes + lane * 16;
+        for (int j = 0; j < NV - 4; ++j) {
+          const int h = j / (4 * T::SFQ), i = (j - h * 4 * T::SFQ) * 32, r = row_q + h * NT + i;
+          to[4 + j] = i < NT && r < a.m ? a.a_scales[(size_t)g * a.m + r] : 0u;
+        }
+        ++g;
+        return true;
+      };
 #pragma unroll
-          for (int j = 0; j <= T::SFQ; ++j)
-            *reinterpret_cast<uint4*>(to + j * 512) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+      for (int d = 0; d < AHEAD; ++d) there[d] = (d == 0 || there[d > 0 ? d - 1 : 0]) && next(v[d]);
+      for (uint32_t sc = 0; there[0];) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+          if (!there[d]) continue;      // (then none of those behind it is there either)
+          const uint32_t slot = sc % T::SLOTS;
+          VSA2_WAIT_PARKED(&misc->sc_empty[slot], ((sc / T::SLOTS) & 1) ^ 1);
+          unsigned char* to = scales + slot * T::SCALES + lane * 16;
+#pragma unroll
+          for (int j = 0; j < NV / 4; ++j)
+            *reinterpret_cast<uint4*>(to + j * 512) = make_uint4(v[d][4 * j], v[d][4 * j + 1], v[d][4 * j + 2], v[d][4 * j + 3]);
           tc::fence_proxy_async_smem();
-          tc::mbar_arrive(&misc->sc_full[slot]);
+          __syncwarp();
+          if (lane == 0) arrive_leader<PAIR>(&misc->sc_full[slot]);
+          ++sc;
+          there[d] = next(v[d]);
         }
       }
     } else if (warp >= 4) {
-      // ---------------------------------------------------------------- epilogue
-      const int quad = warp & 3;
-      constexpr int STEP = NT < 32 ? 16 : 32;
-      uint32_t syncs = 0;
+      // ---------------------------------------------------------------- epilogue: four warps for each accumulator
+      const int quad = warp & 3, buf = (warp >> 2) - 1;
+      constexpr int STEP = 32;
+      uint32_t syncs = 0, turn = 0;
       for (uint32_t seg = 0; w.advance(a); ++seg) {
-        const uint32_t buf = seg & 1;
+        if (HALVES == 1 && (int)(seg & 1) != buf) continue;
         int p, q;
         mm_place(a, w.tile, p, q);
-        const int n = p * 128 + quad * 32 + lane, cols = min(NT, a.m - q * NT);
+        const int n = (p * PAIR + rank) * 128 + quad * 32 + lane, m0 = q * T::COLS + (HALVES == 2 ? buf * NT : 0);
+        const int cols = max(0, min(NT, a.m - m0));
         const bool in = n < a.n;
-        VSA2_WAIT_PARKED(&misc->d_full[buf], (seg >> 1) & 1);
+        VSA2_WAIT_PARKED(&misc->d_full[buf], turn & 1);
+        ++turn;
         tc::tc_fence_after();
-        const bool all = w.kb0 == 0 && w.kb1 == a.kb;
-        float* part = nullptr;
-        if (!all) part = a.partial + ((size_t)blockIdx.x * 2 + (w.kb0 == 0 ? 1 : 0)) * (128 * NT) + quad * 32 + lane;
-        const size_t at = (size_t)(q * (long long)NT * a.ldc) + n;
+        const bool adds = w.kb0 > w.r0;
+        // Pieces of one item come to the two groups of warps in turn (HALVES = 1), each adding to what the other has written: one after the other
+        const bool in_turn = HALVES == 1 && a.chunk < a.kb;
+        if (in_turn && seg > 0) VSA2_WAIT_PARKED(&misc->written[buf ^ 1], ((seg - 1) >> 1) & 1);
+        constexpr int WIDE = HALVES == 2 ? 2 : 1;
+        // [part][half][rank][column][row]
+        const size_t of_part = (size_t)WIDE * PAIR * 128 * NT;
+        float* const parts = a.partial + (size_t)((HALVES == 2 ? buf : 0) * PAIR + rank) * (128 * NT) + quad * 32 + lane;
+        TO* const out = reinterpret_cast<TO*>(a.c) + (size_t)((long long)m0 * a.ldc) + n;
 #pragma unroll 1
         for (int c0 = 0; c0 < cols; c0 += STEP) {
-          uint32_t r[STEP];
-          const uint32_t taddr = tmem_base + buf * 256 + c0 + ((uint32_t)(quad * 32) << 16);
-          if constexpr (STEP == 32) tc::tmem_ld32(taddr, r);
-          else tc::tmem_ld16(taddr, r);
-          tc::tmem_ld_wait();
-#pragma unroll
-          for (int c = 0; c < STEP; ++c) {
-            if (!all) __stcg(part + (size_t)(c0 + c) * 128, __uint_as_float(r[c]));
-            else if (in && c0 + c < cols) store_out(a.c, at + (size_t)(c0 + c) * a.ldc, __uint_as_float(r[c]), a.c_f32);
+          float v[STEP];
+          load_columns<STEP>(tmem_base + buf * 256 + c0 + ((uint32_t)(quad * 32) << 16), v);
+          if (w.part >= 0) {
+            float* to = parts + w.part * of_part + (size_t)c0 * 128;
+            if (adds) add_columns<STEP>(to, 128, STEP, v);
+            put_columns<STEP>(to, 128, STEP, v);
+          } else if (in) {
+            TO* to = out + (size_t)c0 * a.ldc;
+            if constexpr (sizeof(TO) == 4)       // (fp32 results: what this thread has written there for the blocks before)
+              if (adds) add_columns<STEP>(to, a.ldc, cols - c0, v);
+            put_columns<STEP>(to, a.ldc, cols - c0, v);
           }
         }
         tc::tc_fence_before();
-        tc::mbar_arrive(&misc->d_empty[buf]);
-        if (!all) {
-          // the tile's parts: those of the CTAs that its units fall to, in their order
-          const long long first = (long long)(w.tile - a.whole) * a.kb;
-          int lo = (int)(first * gridDim.x / a.units), hi = (int)((first + a.kb - 1) * gridDim.x / a.units);
-          while (a.units * (lo + 1) / gridDim.x <= first) ++lo;
-          while (a.units * lo / gridDim.x > first) --lo;
-          while (a.units * (hi + 1) / gridDim.x <= first + a.kb - 1) ++hi;
-          while (a.units * hi / gridDim.x > first + a.kb - 1) --hi;
+        __syncwarp();
+        if (lane == 0) arrive_leader<PAIR>(&misc->d_empty[buf]);
+        if (in_turn) {
           __threadfence();
-          VSA2_GROUP_SYNC(&misc->group, syncs);
+          tc::mbar_arrive(&misc->written[buf]);
+        }
+        if (w.part >= 0 && w.kb1 == w.r1) {
+          __threadfence();
+          VSA2_GROUP_SYNC(&misc->group[buf], syncs);
           if (quad == 0 && lane == 0) {
-            int* counter = a.counters + (w.tile - a.whole);
-            const bool last = atomicAdd(counter, 1) == hi - lo;
+            int* counter = a.counters + ((w.tile - a.whole) * WIDE + (HALVES == 2 ? buf : 0)) * PAIR + rank;
+            const bool last = atomicAdd(counter, 1) == a.splits - 1;
             if (last) *counter = 0;
-            misc->last = last;
+            misc->last[buf] = last;
             __threadfence();
           }
-          VSA2_GROUP_SYNC(&misc->group, syncs);
-          if (misc->last) {
+          VSA2_GROUP_SYNC(&misc->group[buf], syncs);
+          if (misc->last[buf]) {
             __threadfence();
+            const float* const mine = parts + (size_t)(w.tile - a.whole) * of_part;
 #pragma unroll 1
-            for (int c = 0; c < cols; ++c) {
-              float sum = 0.f;
-              for (int cta = lo; cta <= hi; ++cta) {
-                const bool begins = a.units * cta / gridDim.x <= first;       // its part begins with the tile
-                sum += __ldcg(a.partial + ((size_t)cta * 2 + (begins ? 1 : 0)) * (128 * NT) + (size_t)c * 128 + quad * 32 + lane);
-              }
-              if (in) store_out(a.c, at + (size_t)c * a.ldc, sum, a.c_f32);
+            for (int c0 = 0; c0 < cols; c0 += STEP) {
+              float sum[STEP];
+#pragma unroll
+              for (int c = 0; c < STEP; ++c) sum[c] = 0.f;
+#pragma unroll 1
+              for (int o = 0; o < a.splits; ++o) add_columns<STEP>(mine + (size_t)o * a.rest * of_part + (size_t)c0 * 128, 128, STEP, sum);
+              if (in) put_columns<STEP>(out + (size_t)c0 * a.ldc, a.ldc, cols - c0, sum);
             }
           }
-          VSA2_GROUP_SYNC(&misc->group, syncs);       // (misc->last is read before it is written again)
+          VSA2_GROUP_SYNC(&misc->group[buf], syncs);       // (misc->last is read before it is written again)
         }
       }
     }
@@ -325,7 +494,8 @@ done:
     }
     __syncthreads();
   }
-  if (warp == 3) tc::tmem_dealloc(tmem_base, 512);
+  if constexpr (PAIR == 2) cluster_sync_all();        // (neither leaves while the other may still arrive at its barriers or read its operands)
+  if (warp == 3) mm_dealloc<PAIR>(tmem_base);
 }
 
 bool make_row_tmap(CUtensorMap* out, const void* base, int rows, int cols, long long ld, int box_rows) {
@@ -339,16 +509,69 @@ bool make_row_tmap(CUtensorMap* out, const void* base, int rows, int cols, long 
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int mm_width(int m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : m <= 128 ? 128 : 224; }
+// How a product is cut: tiles, and ranges of K for those that do not fill a round of all CTAs (or pairs).  `cycles`: estimate that the choice is made by.
+struct MmPlan {
+  int pt, qt, whole, rest, splits;
+  double cycles;
+};
+// A block takes the tensor cores 2 cycles a column (for 128 rows of an SM).  An SM is fed 36 bytes a cycle from L2 when all of them are, up to 64 when few are
+// (measured: 8192^3 in tiles of 224 columns, 30,720 bytes a block, 855 cycles a block); what is left of the last rounds is cut into 1 .. 8 ranges, with the
+// parts' way through memory at about 2000 cycles and 700 for each.
+MmPlan mm_plan(int m, int n, int kb, int rows, int cols, int stage, int of, int sms_each) {
+  MmPlan best = {};
+  best.pt = (n + rows - 1) / rows;
+  best.qt = (m + cols - 1) / cols;
+  const long long tiles = (long long)best.pt * best.qt;
+  auto block = [&](long long active) {
+    const double feed = 36.0 * 148 / ((active < of ? active : of) * sms_each);
+    const double fed = stage / (feed < 64.0 ? feed : 64.0), mma = 2.0 * cols;
+    return fed > mma ? fed : mma;
+  };
+  best.whole = (int)(tiles / of * of);
+  best.rest = (int)(tiles - best.whole);
+  best.splits = 1;
+  const double rounds = (double)(tiles / of) * kb * block(of);
+  best.cycles = rounds + (best.rest > 0 ? kb * block(best.rest) : 0);
+  for (int s = 2; s <= 8 && s <= kb && best.rest > 0 && s * best.rest <= 2 * of / (cols > 224 ? 2 : 1); ++s) {
+    const long long items = (long long)s * best.rest;
+    const double cut = (double)((items + of - 1) / of) * ((kb + s - 1) / s) * block(items) + 2000 + 700 * s;
+    if (rounds + cut < best.cycles) {
+      best.cycles = rounds + cut;
+      best.splits = s;
+    }
+  }
+  return best;
+}
 
-template <int NT>
-cudaError_t launch_mm(MmArgs a, const Fp8Arg& fa, const Fp8Arg& fb, int ctas, cudaStream_t st) {
+template <int NT, int PAIR, int HALVES, typename TO>
+cudaError_t launch_mm_of(MmArgs a, const MmPlan& plan, const Fp8Arg& fa, const Fp8Arg& fb, int ctas, cudaStream_t st) {
+  using T = MmTile<NT, PAIR, HALVES>;
   CUtensorMap tp, tq;
-  if (!make_row_tmap(&tp, fb.values, a.n, a.k, fb.ld, 128) || !make_row_tmap(&tq, fa.values, a.m, a.k, fa.ld, NT)) return cudaErrorInvalidValue;
+  if (!make_row_tmap(&tp, fb.values, a.n, a.k, fb.ld, 128) || !make_row_tmap(&tq, fa.values, a.m, a.k, fa.ld, NT / PAIR))
+    return cudaErrorInvalidValue;
+  a.pt = plan.pt; a.qt = plan.qt; a.whole = plan.whole; a.rest = plan.rest; a.splits = plan.splits;
+  // tiles along m that share B's rows while they pass through L2
+  a.gq = a.qt < 12 / HALVES ? a.qt : 12 / HALVES;
+  const long long items = a.whole + (long long)a.rest * a.splits;
+  int of = ctas / PAIR;
+  if (items < of) of = (int)items;
   static KernelAttr attr;
   cudaError_t e;
-  if ((e = prepare_kernel((const void*)fp8_matmul_kernel<NT>, attr, MmTile<NT>::SMEM))) return e;
-  return launch_kernel(fp8_matmul_kernel<NT>, ctas, kMmThreads, MmTile<NT>::SMEM, st, tp, tq, a);
+  if ((e = prepare_kernel((const void*)fp8_matmul_kernel<NT, PAIR, HALVES, TO>, attr, T::SMEM))) return e;
+  return launch_kernel(fp8_matmul_kernel<NT, PAIR, HALVES, TO>, of * PAIR, kMmThreads, T::SMEM, st, tp, tq, a);
+}
+template <int NT, int PAIR, int HALVES>
+MmPlan mm_plan_of(const MmArgs& a, int ctas) {
+  using T = MmTile<NT, PAIR, HALVES>;
+  return mm_plan(a.m, a.n, a.kb, 128 * PAIR, T::COLS, (int)T::STAGE, ctas / PAIR, PAIR);
+}
+template <int NT, int PAIR, int HALVES>
+cudaError_t launch_mm(const MmArgs& a, const MmPlan& plan, const Fp8Arg& fa, const Fp8Arg& fb, int ctas, bool f32, cudaStream_t st) {
+  return f32 ? launch_mm_of<NT, PAIR, HALVES, float>(a, plan, fa, fb, ctas, st) : launch_mm_of<NT, PAIR, HALVES, bf16>(a, plan, fa, fb, ctas, st);
+}
+template <int NT, int PAIR>
+cudaError_t launch_mm(const MmArgs& a, const Fp8Arg& fa, const Fp8Arg& fb, int ctas, bool f32, cudaStream_t st) {
+  return launch_mm<NT, PAIR, 1>(a, mm_plan_of<NT, PAIR, 1>(a, ctas), fa, fb, ctas, f32, st);
 }
 
 }  // namespace
@@ -357,7 +580,8 @@ cudaError_t launch_mm(MmArgs a, const Fp8Arg& fa, const Fp8Arg& fb, int ctas, cu
 size_t fp8_matmul_workspace_bytes(int m, int n, int k) {
   (void)n;
   (void)k;
-  return align_up(sizeof(StatusBlock) + kMmCounters * sizeof(int), 256) + (size_t)2 * kMmCtas * 128 * mm_width(m) * sizeof(float);
+  const int columns = m <= 32 ? 32 : m <= 128 ? 128 : 224;      // (the widest accumulator that a product of m rows may take)
+  return align_up(sizeof(StatusBlock) + kMmCounters * sizeof(int), 256) + (size_t)2 * kMmCtas * 128 * columns * sizeof(float);
 }
 
 cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Arg& fb, void* c, int c_f32, long long ldc,
@@ -365,35 +589,31 @@ cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Ar
   int sms = 0;
   cudaError_t e;
   if ((e = sm_count(&sms)) != cudaSuccess) return e;
-  const int nt = mm_width(m);
+  const int ctas = sms < kMmCtas ? sms : kMmCtas;
+  // Pairs wherever B has rows for both (a pair fetches half the rows of A for each SM) and the context has room for one; the narrowest tile that holds A's
+  // rows.
+  bool pair = n > 128 && ctas >= 2;
+  if (pair) {
+    static ClusterRoom room;
+    if ((e = cluster_room((const void*)fp8_matmul_kernel<224, 2, 2, float>, room, 2, kMmThreads, MmTile<224, 2, 2>::SMEM, &pair))) return e;
+  }
   MmArgs a;
   a.m = m; a.n = n; a.k = k;
   a.kb = (k + 127) / 128;
-  a.pt = (n + 127) / 128;
-  a.qt = (m + nt - 1) / nt;
-  a.gq = a.qt < 12 ? a.qt : 12;
-  int ctas = sms < kMmCtas ? sms : kMmCtas;
-  const long long tiles = (long long)a.pt * a.qt, all_units = tiles * a.kb;
-  if (all_units < ctas) ctas = (int)all_units;
-  // whole rounds, but for the last full one, which joins the remainder (parts of about one to two tiles a CTA instead of less than one)
-  long long rounds = tiles / ctas;
-  if (tiles % ctas != 0 && rounds > 0) --rounds;
-  a.whole = (int)(rounds * ctas);
-  a.units = (tiles - a.whole) * a.kb;
+  a.chunk = c_f32 ? kMmChunk : a.kb;
   a.a_scales = reinterpret_cast<const uint32_t*>(fa.scales);
   a.b_scales = reinterpret_cast<const uint32_t*>(fb.scales);
-  a.c = c; a.c_f32 = c_f32; a.ldc = ldc;
+  a.c = c; a.ldc = ldc;
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
   a.status = reinterpret_cast<StatusBlock*>(ws);
   a.counters = reinterpret_cast<int*>(ws + sizeof(StatusBlock));
   a.partial = reinterpret_cast<float*>(ws + align_up(sizeof(StatusBlock) + kMmCounters * sizeof(int), 256));
-  switch (nt) {
-    case 16: return launch_mm<16>(a, fa, fb, ctas, st);
-    case 32: return launch_mm<32>(a, fa, fb, ctas, st);
-    case 64: return launch_mm<64>(a, fa, fb, ctas, st);
-    case 128: return launch_mm<128>(a, fa, fb, ctas, st);
-    default: return launch_mm<224>(a, fa, fb, ctas, st);
-  }
+  if (!pair) return m <= 32 ? launch_mm<32, 1>(a, fa, fb, ctas, c_f32, st) : launch_mm<128, 1>(a, fa, fb, ctas, c_f32, st);
+  if (m <= 32) return launch_mm<32, 2>(a, fa, fb, ctas, c_f32, st);
+  if (m <= 64) return launch_mm<64, 2>(a, fa, fb, ctas, c_f32, st);
+  if (m <= 128) return launch_mm<128, 2>(a, fa, fb, ctas, c_f32, st);
+  const MmPlan one = mm_plan_of<224, 2, 1>(a, ctas), two = mm_plan_of<224, 2, 2>(a, ctas);
+  return one.cycles <= two.cycles ? launch_mm<224, 2, 1>(a, one, fa, fb, ctas, c_f32, st) : launch_mm<224, 2, 2>(a, two, fa, fb, ctas, c_f32, st);
 }
 
 }  // namespace vsa2

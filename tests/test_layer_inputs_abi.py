@@ -199,8 +199,18 @@ def test_binding_refuses_what_it_cannot_marshal():
     f = vb.Fp8.empty(4, 20, device="cpu")
     assert f.shape == (4, 20) and f.values.stride(0) == 32
     with pytest.raises(ValueError):
-        f._struct()
+        f._pack()
     with pytest.raises(ValueError):
         vb.vsa2_fp8_quantize(torch.zeros(4, 20), f)
     with pytest.raises(ValueError):
         vb.vsa2_fp8_matmul(f, vb.Fp8.empty(4, 21, device="cpu"), torch.zeros(4, 4), None)
+
+
+def test_packed_structs_have_the_layout_of_the_header():
+    for packed, cls in ((vb._HEADS, vb.Heads), (vb._PLACE, vb.Place), (vb._NORM, vb.QkNorm), (vb._FP8, vb.Fp8Matrix)):
+        assert packed.size == C.sizeof(cls)
+    v = vb.Heads.from_buffer_copy(vb._HEADS.pack(1 << 40, 2 << 33, 3, 4, 5, 6, 7, 8, 1, 0))
+    assert [getattr(v, f) for f, _ in vb.Heads._fields_] == [1 << 40, 2 << 33, 3, 4, 5, 6, 7, 8, 1, 0]
+    p = vb.Place.from_buffer_copy(vb._place((3, 4, 5), 6, None, 1, 1))
+    assert (p.grid_t, p.grid_h, p.grid_w, p.first, p.positions) == (3, 4, 5, 6, None)
+    assert vb._HEADS2.size == 2 * vb._HEADS.size and vb._HEADS3.size == 3 * vb._HEADS.size
