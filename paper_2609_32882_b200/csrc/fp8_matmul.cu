@@ -123,11 +123,37 @@ __device__ __forceinline__ uint32_t leaders(uint64_t* bar) {      // address of 
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(tc::smem_u32(bar)));
   return r;
 }
-template <int PAIR>
 __device__ __forceinline__ void arrive_leader(uint64_t* bar) {
-  if constexpr (PAIR == 1) tc::mbar_arrive(bar);
-  else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar)) : "memory");
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar)) : "memory");
 }
+// tc::mbar_wait on a barrier that the other CTA of a pair arrives at too
+template <int PAIR>
+__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  if constexpr (PAIR == 1) {
+    return tc::mbar_wait(bar, parity, abort_flag);
+  } else {
+    const uint32_t t0 = tc::timer_lo_ns();
+    for (;;) {
+      uint32_t ok;
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(ok)
+          : "r"(tc::smem_u32(bar)), "r"(parity)
+          : "memory");
+      if (ok != 0) return true;
+      if (*abort_flag || tc::timer_lo_ns() - t0 > tc::kWaitLimitNs) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+}
+#define VSA2_WAIT_PAIR(bar, parity)                                            \
+  do {                                                                         \
+    if (!wait_pair<PAIR>((bar), (parity), &misc->abort_flag)) goto done;       \
+  } while (0)
 template <int PAIR>
 __device__ __forceinline__ void tma_load_rows(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1) {
   if constexpr (PAIR == 1)
@@ -244,12 +270,12 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
       tc::mbar_init(&misc->empty[s], 1);
     }
     for (int s = 0; s < T::SLOTS; ++s) {
-      tc::mbar_init(&misc->sc_full[s], PAIR);
+      tc::mbar_init(&misc->sc_full[s], rank == 0 ? PAIR : 1);
       tc::mbar_init(&misc->sc_empty[s], 1);
     }
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&misc->d_full[s], 1);
-      tc::mbar_init(&misc->d_empty[s], 4 * PAIR);
+      tc::mbar_init(&misc->d_empty[s], rank == 0 ? 3 + PAIR : 4);
       tc::mbar_init(&misc->group[s], 128);
       tc::mbar_init(&misc->written[s], 128);
     }
@@ -268,61 +294,56 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
     MmWalk w;
     w.init(blockIdx.x / PAIR, gridDim.x / PAIR);
     if (warp == 0) {
-      // ---------------------------------------------------------------- operands
-      uint32_t it = 0;
+      // ---------------------------------------------------------------- operands: a lane for B's rows, one for A's rows of each accumulator
+      // (in one warp or two, in copies of 128 rows or of 32: no difference)
+      uint32_t s = 0, parity = 1;
+      const CUtensorMap* tm = lane == 0 ? &tm_p : &tm_q;
+      const uint32_t offset = lane == 0 ? 0 : kMmPBytes + (lane - 1) * T::QBYTES;
       while (w.advance(a)) {
         int p, q;
         mm_place(a, w.tile, p, q);
-        const int row_p = (p * PAIR + rank) * 128, row_q = q * T::COLS + rank * (NT / PAIR);
-        for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
-          const uint32_t s = it % T::STAGES;
-          int ok = 1;
-          if (lane == 0) {
-            ok = tc::mbar_wait(&misc->empty[s], ((it / T::STAGES) & 1) ^ 1, &misc->abort_flag);
-            if (ok) {
-              unsigned char* to = ring + s * T::STAGE;
-              if (rank == 0) tc::mbar_expect_tx(&misc->full[s], PAIR * T::STAGE);
-              tma_load_rows<PAIR>(to, &tm_p, &misc->full[s], kb * 128, row_p);
-#pragma unroll
-              for (int h = 0; h < HALVES; ++h)
-                tma_load_rows<PAIR>(to + kMmPBytes + h * T::QBYTES, &tm_q, &misc->full[s], kb * 128, row_q + h * NT);
-            }
+        const int row = lane == 0 ? (p * PAIR + rank) * 128 : q * T::COLS + (lane - 1) * NT + rank * (NT / PAIR);
+        for (int kb = w.kb0; kb < w.kb1; ++kb) {
+          VSA2_WAIT(&misc->empty[s], parity);
+          if (rank == 0 && lane == 0) tc::mbar_expect_tx(&misc->full[s], PAIR * T::STAGE);
+          if (lane <= HALVES) tma_load_rows<PAIR>(ring + s * T::STAGE + offset, tm, &misc->full[s], kb * 128, row);
+          __syncwarp();
+          if (++s == T::STAGES) {
+            s = 0;
+            parity ^= 1;
           }
-          if (!__shfl_sync(0xffffffffu, ok, 0)) goto done;
         }
       }
     } else if (warp == 1 && rank == 0) {
       // ---------------------------------------------------------------- products (converged warp, one lane issues)
       const uint64_t ring_desc = tc::smem_desc_sw128(tc::smem_u32(ring), 16, 1024);
       const uint64_t scale_desc = tc::smem_desc_plain(tc::smem_u32(scales), 16, 128);
-      uint32_t it = 0, sc = 0, seg = 0;
-      // products of block kb (number `at` of all) with half h of the columns, scales of group number `group`
-      auto products = [&](int kb, uint32_t at, uint32_t group, uint32_t buf, int h, bool first) {
-        const uint64_t dp = ring_desc + (uint64_t)(at % T::STAGES * T::STAGE >> 4), dq = dp + (uint64_t)((kMmPBytes + h * T::QBYTES) >> 4);
+      uint32_t stage = 0, parity = 0, sc = 0, seg = 0;
+      // products of block kb in stage s with half h of the columns, scales of group number `group`
+      auto products = [&](int kb, uint32_t s, uint32_t group, uint32_t buf, int h, bool first) {
+        const uint64_t dp = ring_desc + (uint64_t)(s * T::STAGE >> 4), dq = dp + (uint64_t)((kMmPBytes + h * T::QBYTES) >> 4);
         const uint32_t idesc = idesc_scaled<NT, PAIR>(kb & 3), tm_sc = tmem_base + T::scales_at(group);
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
           mma_scaled<PAIR>(tmem_base + buf * 256, dp + 2 * ks, dq + 2 * ks, idesc, tm_sc, tm_sc + 4 + h * 4 * T::SFQ, ks > 0 || !first);
       };
       for (; w.advance(a); ++seg) {
-        if constexpr (HALVES == 1) VSA2_WAIT(&misc->d_empty[seg & 1], ((seg >> 1) & 1) ^ 1);
-        else VSA2_WAIT(&misc->d_empty[0], (seg & 1) ^ 1);
+        if constexpr (HALVES == 1) VSA2_WAIT_PAIR(&misc->d_empty[seg & 1], ((seg >> 1) & 1) ^ 1);
+        else VSA2_WAIT_PAIR(&misc->d_empty[0], (seg & 1) ^ 1);
         // HALVES = 2: both accumulators are in use all the time.  Of the last blocks of a tile those with the first half come first, so that its epilogue
         // runs behind those with the second half; of the first blocks likewise, so that the second half's epilogue runs behind those with the first
         int kb = w.kb0;
         while (kb < w.kb1) {
           const int bunch = HALVES == 1 ? 1 : kb == w.kb0 || kb == w.kb1 - kMmBunch ? min(kMmBunch, w.kb1 - kb) : 1;
-          uint32_t first_group = sc;
+          uint32_t first_group = sc, s = stage, s_parity = parity;
           for (int i = 0; i < bunch; ++i) {
-            const uint32_t s = (it + i) % T::STAGES;
             const bool fresh = kb + i == w.kb0 || ((kb + i) & 3) == 0;
             if (fresh) {
-              VSA2_WAIT(&misc->sc_full[sc % T::SLOTS], (sc / T::SLOTS) & 1);
-              if constexpr (PAIR == 2) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+              VSA2_WAIT_PAIR(&misc->sc_full[sc % T::SLOTS], (sc / T::SLOTS) & 1);
               ++sc;
             }
             if (i == 0) first_group = sc - 1;
-            VSA2_WAIT(&misc->full[s], ((it + i) / T::STAGES) & 1);
+            VSA2_WAIT(&misc->full[s], s_parity);
             tc::tc_fence_after();
             if (tc::elect_one()) {
               if (fresh) {
@@ -332,30 +353,58 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
                 for (int j = 0; j < 1 + HALVES * T::SFQ; ++j) copy_scales<PAIR>(tm_sc + 4 * j, d + (uint64_t)(512 * j >> 4));
                 commit_all<PAIR>(&misc->sc_empty[slot]);
               }
-              products(kb + i, it + i, sc - 1, HALVES == 1 ? seg & 1 : 0, 0, kb + i == w.kb0);
+              products(kb + i, s, sc - 1, HALVES == 1 ? seg & 1 : 0, 0, kb + i == w.kb0);
               if (HALVES == 1) commit_all<PAIR>(&misc->empty[s]);
               if (kb + i == w.kb1 - 1) commit_all<PAIR>(&misc->d_full[HALVES == 1 ? seg & 1 : 0]);
             }
             __syncwarp();
+            if (++s == T::STAGES) {
+              s = 0;
+              s_parity ^= 1;
+            }
           }
           if constexpr (HALVES == 2) {
             if (kb == w.kb0) {
-              VSA2_WAIT(&misc->d_empty[1], (seg & 1) ^ 1);
+              VSA2_WAIT_PAIR(&misc->d_empty[1], (seg & 1) ^ 1);
               tc::tc_fence_after();
             }
             uint32_t group = first_group;
             for (int i = 0; i < bunch; ++i) {
               if (i > 0 && ((kb + i) & 3) == 0) ++group;
               if (tc::elect_one()) {
-                products(kb + i, it + i, group, 1, 1, kb + i == w.kb0);
-                commit_all<PAIR>(&misc->empty[(it + i) % T::STAGES]);
+                products(kb + i, stage, group, 1, 1, kb + i == w.kb0);
+                commit_all<PAIR>(&misc->empty[stage]);
                 if (kb + i == w.kb1 - 1) commit_all<PAIR>(&misc->d_full[1]);
               }
               __syncwarp();
+              if (++stage == T::STAGES) stage = 0;
             }
           }
+          stage = s;
+          parity = s_parity;
           kb += bunch;
-          it += bunch;
+        }
+      }
+    } else if ((warp == 1 || warp == 3) && rank == 1) {
+      // ---------------------------------------------------------------- tells the first CTA what this one has ready: scales (warp 1), accumulators that have
+      // been read (warp 3).  An arrival at the other CTA waits for all that its warp has under way: by the scales' own warp (loads) or the epilogue's (stores)
+      // it came a memory latency late, 1500 cycles for each four blocks
+      uint32_t sc = 0;
+      for (uint32_t seg = 0; w.advance(a); ++seg) {
+        if (warp == 1) {
+          for (int g = w.kb0 >> 2; g <= (w.kb1 - 1) >> 2; ++g, ++sc) {
+            VSA2_WAIT(&misc->sc_full[sc % T::SLOTS], (sc / T::SLOTS) & 1);
+            if (lane == 0) arrive_leader(&misc->sc_full[sc % T::SLOTS]);
+            __syncwarp();
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < HALVES; ++h) {
+            const uint32_t buf = HALVES == 2 ? h : seg & 1;
+            VSA2_WAIT(&misc->d_empty[buf], (HALVES == 2 ? seg : seg >> 1) & 1);
+            if (lane == 0) arrive_leader(&misc->d_empty[buf]);
+            __syncwarp();
+          }
         }
       }
     } else if (warp == 2) {
@@ -400,7 +449,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
             *reinterpret_cast<uint4*>(to + j * 512) = make_uint4(v[d][4 * j], v[d][4 * j + 1], v[d][4 * j + 2], v[d][4 * j + 3]);
           tc::fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) arrive_leader<PAIR>(&misc->sc_full[slot]);
+          if (lane == 0) tc::mbar_arrive(&misc->sc_full[slot]);
           ++sc;
           there[d] = next(v[d]);
         }
@@ -446,7 +495,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
         }
         tc::tc_fence_before();
         __syncwarp();
-        if (lane == 0) arrive_leader<PAIR>(&misc->d_empty[buf]);
+        if (lane == 0) tc::mbar_arrive(&misc->d_empty[buf]);
         if (in_turn) {
           __threadfence();
           tc::mbar_arrive(&misc->written[buf]);
