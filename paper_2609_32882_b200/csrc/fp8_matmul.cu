@@ -28,13 +28,13 @@ constexpr int kMmCtas = 148;            // most CTAs (the workspace is laid out 
 constexpr int kMmThreads = 384;
 constexpr int kMmStagesMost = 12;
 constexpr int kMmCounters = 2 * kMmCtas;
-constexpr int kMmChunk = 32;            // blocks of K that an accumulator sums for an fp32 result
-constexpr int kMmBunch = 3;             // HALVES = 2: blocks whose products with one half are issued together at a tile's two ends
+constexpr int kMmChunk = 64;            // blocks of K that an accumulator sums for an fp32 result
 constexpr uint32_t kMmPBytes = 128 * 128;
+constexpr uint32_t kMmTileBytes = 32 * 128 * 2;      // 32 rows of C x 128 elements of bf16
 
 // NT columns an accumulator; PAIR: CTAs that share a tile (2: a pair of SMs, 256 rows of B, each CTA fetches its rows of B and half the rows
 // of A); HALVES: accumulators side by side (2: a tile of 2 NT columns takes both)
-template <int NT, int PAIR, int HALVES>
+template <int NT, int PAIR, int HALVES, typename TO>
 struct MmTile {
   static constexpr int COLS = NT * HALVES;
   static constexpr uint32_t QBYTES = NT / PAIR * 128;                       // rows of A for one accumulator
@@ -42,20 +42,25 @@ struct MmTile {
   static constexpr int SFQ = (NT + 127) / 128;                              // 512-byte pieces of A's scales for one accumulator
   static constexpr uint32_t SCALES = 512 + HALVES * SFQ * 512;              // words of 128 rows of B, of the rows of A
   static constexpr int SLOTS = HALVES == 2 ? 2 : 4;
-  static constexpr uint32_t ROOM = 227 * 1024 - 2048 - SLOTS * SCALES;
+  static constexpr uint32_t STAGING = sizeof(TO) == 2 ? 4 * kMmTileBytes : 0;      // two tiles of results for each group of the epilogue
+  static constexpr uint32_t ROOM = 227 * 1024 - 2048 - SLOTS * SCALES - STAGING;
   static constexpr int STAGES = ROOM / STAGE < kMmStagesMost ? ROOM / STAGE : kMmStagesMost;
-  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + SLOTS * SCALES;
+  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + STAGING + SLOTS * SCALES;
+  // HALVES = 2: blocks whose products with one half are issued together at a tile's two ends
+  static constexpr int BUNCH = STAGES > 4 ? 3 : 2;
   // columns of tensor memory: accumulators at 0 and 256 (of 224 at most), scales of even and odd groups of four blocks behind them
   __host__ __device__ static constexpr uint32_t scales_at(uint32_t group) { return 224 + (group & 1) * 256; }
 };
 
+// P: the operand whose rows are the accumulators' lanes, Q: the one whose rows are its columns
 struct MmArgs {
-  int m, n, k, kb;                   // kb: blocks of K
-  int pt, qt, gq;                    // tiles along n, along m; tiles along m that are taken together
+  int p_rows, q_rows, kb;            // kb: blocks of K
+  int pt, qt, gq;                    // tiles along P, along Q; tiles along Q that are taken together
+  int tensor_stores;                 // C lies as tensor copies need it
   int chunk;                         // most blocks of K in one accumulator
   int whole, rest, splits;           // tiles that are dealt out whole; the others, each cut into `splits` ranges of K
-  const uint32_t* a_scales;
-  const uint32_t* b_scales;
+  const uint32_t* p_scales;
+  const uint32_t* q_scales;
   void* c;
   long long ldc;
   StatusBlock* status;
@@ -228,39 +233,73 @@ __device__ __forceinline__ constexpr uint32_t idesc_scaled(uint32_t sf) {
   return (sf << 4) | ((uint32_t)(NT >> 3) << 17) | (1u << 23) | ((uint32_t)PAIR << 27) | (sf << 29);
 }
 
-// `count` columns (rows of the result) of an accumulator, `stride` elements apart.  Whole steps are straight code: with a test for each
-// element the loads and stores came one at a time, and the epilogue took longer than the products of 40 blocks.
+// 32 columns of an accumulator's row, straight code where all of them exist: with a test for each element the loads and stores came one at a time, and
+// the epilogue took longer than the products of 40 blocks.
 __device__ __forceinline__ void put(float* to, float v) { *to = v; }
 __device__ __forceinline__ void put(bf16* to, float v) { *to = __float2bfloat16_rn(v); }
-template <int STEP, typename TO>
-__device__ __forceinline__ void put_columns(TO* to, long long stride, int count, const float (&v)[STEP]) {
-  if (count >= STEP) {
+// elements `stride` apart (a warp's 32 rows lie next to one another in C)
+template <typename TO>
+__device__ __forceinline__ void put_column(TO* to, long long stride, int count, const float (&v)[32]) {
+  if (count >= 32) {
 #pragma unroll
-    for (int c = 0; c < STEP; ++c, to += stride) put(to, v[c]);
+    for (int c = 0; c < 32; ++c, to += stride) put(to, v[c]);
   } else {
 #pragma unroll
-    for (int c = 0; c < STEP; ++c, to += stride)
+    for (int c = 0; c < 32; ++c, to += stride)
       if (c < count) put(to, v[c]);
   }
 }
-template <int STEP>
-__device__ __forceinline__ void add_columns(const float* from, long long stride, int count, float (&v)[STEP]) {
-  float old[STEP];
+__device__ __forceinline__ void add_column(const float* from, long long stride, int count, float (&v)[32]) {
+  float old[32];
 #pragma unroll
-  for (int c = 0; c < STEP; ++c) old[c] = __ldcg(from + min(c, count - 1) * stride);
+  for (int c = 0; c < 32; ++c) {
+    old[c] = __ldcg(from);
+    if (c + 1 < count) from += stride;
+  }
 #pragma unroll
-  for (int c = 0; c < STEP; ++c) v[c] += old[c];
+  for (int c = 0; c < 32; ++c) v[c] += old[c];
+}
+
+// bf16: 32 rows x 32 columns of an accumulator (lanes and columns of `taddr`) as the fragments that stmatrix turns: four 8 x 8 blocks for each 8 columns
+__device__ __forceinline__ void take_tile(uint32_t taddr, uint32_t (&u)[16]) {
+  uint32_t r[2][16];
+  tc::tmem_ld_16x256b_x4(taddr, r[0]);
+  tc::tmem_ld_16x256b_x4(taddr + (16u << 16), r[1]);
+  tc::tmem_ld_wait();
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      u[4 * g + b] = pack_bf16x2(__uint_as_float(r[b >> 1][4 * g + 2 * (b & 1)]), __uint_as_float(r[b >> 1][4 * g + 2 * (b & 1) + 1]));
+}
+// .. to 32 rows of C of 32 elements, in a tile of 32 rows x 128 elements that lies as the tensor copy takes it: two boxes of 64 elements, rows of 128 bytes, 16-byte places
+// exchanged by the row
+__device__ __forceinline__ void stage_tile(unsigned char* tile, const uint32_t (&u)[16], int quad, int lane) {
+  const int row = lane & 7, block = (quad & 1) * 4 + (lane >> 3);      // of C; of 8 elements in the box
+  const uint32_t to = tc::smem_u32(tile) + (quad >> 1) * 4096 + row * 128 + ((block ^ row) << 4);
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                 ::"r"(to + g * 1024), "r"(u[4 * g]), "r"(u[4 * g + 1]), "r"(u[4 * g + 2]), "r"(u[4 * g + 3])
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, const void* from, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(from)), "r"(c0), "r"(c1)
+               : "memory");
 }
 
 template <int NT, int PAIR, int HALVES, typename TO>
 __global__ void __cluster_dims__(PAIR, 1, 1) __launch_bounds__(kMmThreads, 1)
-fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ MmArgs a) {
-  using T = MmTile<NT, PAIR, HALVES>;
+fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_c,
+                  const __grid_constant__ MmArgs a) {
+  using T = MmTile<NT, PAIR, HALVES, TO>;
   extern __shared__ unsigned char mm_smem[];
   __shared__ MmMisc misc_store;
   MmMisc* misc = &misc_store;
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(mm_smem) + 1023) & ~(uintptr_t)1023);
-  unsigned char* scales = ring + T::STAGES * T::STAGE;
+  unsigned char* staging = ring + T::STAGES * T::STAGE;
+  unsigned char* scales = staging + T::STAGING;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = PAIR == 1 ? 0 : (int)cluster_rank();
   if (tid == 0) {
@@ -334,7 +373,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
         // runs behind those with the second half; of the first blocks likewise, so that the second half's epilogue runs behind those with the first
         int kb = w.kb0;
         while (kb < w.kb1) {
-          const int bunch = HALVES == 1 ? 1 : kb == w.kb0 || kb == w.kb1 - kMmBunch ? min(kMmBunch, w.kb1 - kb) : 1;
+          const int bunch = HALVES == 1 ? 1 : kb == w.kb0 || kb == w.kb1 - T::BUNCH ? min(T::BUNCH, w.kb1 - kb) : 1;
           uint32_t first_group = sc, s = stage, s_parity = parity;
           for (int i = 0; i < bunch; ++i) {
             const bool fresh = kb + i == w.kb0 || ((kb + i) & 3) == 0;
@@ -426,11 +465,11 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
           g_end = ((w.kb1 - 1) >> 2) + 1;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) to[j] = row_p + j * 32 < a.n ? a.b_scales[(size_t)g * a.n + row_p + j * 32] : 0u;
+        for (int j = 0; j < 4; ++j) to[j] = row_p + j * 32 < a.p_rows ? a.p_scales[(size_t)g * a.p_rows + row_p + j * 32] : 0u;
 #pragma unroll
         for (int j = 0; j < NV - 4; ++j) {
           const int h = j / (4 * T::SFQ), i = (j - h * 4 * T::SFQ) * 32, r = row_q + h * NT + i;
-          to[4 + j] = i < NT && r < a.m ? a.a_scales[(size_t)g * a.m + r] : 0u;
+          to[4 + j] = i < NT && r < a.q_rows ? a.q_scales[(size_t)g * a.q_rows + r] : 0u;
         }
         ++g;
         return true;
@@ -457,15 +496,14 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
     } else if (warp >= 4) {
       // ---------------------------------------------------------------- epilogue: four warps for each accumulator
       const int quad = warp & 3, buf = (warp >> 2) - 1;
-      constexpr int STEP = 32;
-      uint32_t syncs = 0, turn = 0;
+      uint32_t syncs = 0, turn = 0, tiles = 0;
       for (uint32_t seg = 0; w.advance(a); ++seg) {
         if (HALVES == 1 && (int)(seg & 1) != buf) continue;
         int p, q;
         mm_place(a, w.tile, p, q);
-        const int n = (p * PAIR + rank) * 128 + quad * 32 + lane, m0 = q * T::COLS + (HALVES == 2 ? buf * NT : 0);
-        const int cols = max(0, min(NT, a.m - m0));
-        const bool in = n < a.n;
+        const int row = (p * PAIR + rank) * 128 + quad * 32 + lane, col = q * T::COLS + (HALVES == 2 ? buf * NT : 0);
+        const int cols = min(NT, a.q_rows - col);      // (0 or less: the second half of a tile that ends in the first)
+        const bool in = row < a.p_rows;
         VSA2_WAIT_PARKED(&misc->d_full[buf], turn & 1);
         ++turn;
         tc::tc_fence_after();
@@ -477,25 +515,56 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
         // [part][half][rank][column][row]
         const size_t of_part = (size_t)WIDE * PAIR * 128 * NT;
         float* const parts = a.partial + (size_t)((HALVES == 2 ? buf : 0) * PAIR + rank) * (128 * NT) + quad * 32 + lane;
-        TO* const out = reinterpret_cast<TO*>(a.c) + (size_t)((long long)m0 * a.ldc) + n;
-#pragma unroll 1
-        for (int c0 = 0; c0 < cols; c0 += STEP) {
-          float v[STEP];
-          load_columns<STEP>(tmem_base + buf * 256 + c0 + ((uint32_t)(quad * 32) << 16), v);
-          if (w.part >= 0) {
-            float* to = parts + w.part * of_part + (size_t)c0 * 128;
-            if (adds) add_columns<STEP>(to, 128, STEP, v);
-            put_columns<STEP>(to, 128, STEP, v);
-          } else if (in) {
-            TO* to = out + (size_t)c0 * a.ldc;
-            if constexpr (sizeof(TO) == 4)       // (fp32 results: what this thread has written there for the blocks before)
-              if (adds) add_columns<STEP>(to, a.ldc, cols - c0, v);
-            put_columns<STEP>(to, a.ldc, cols - c0, v);
+        TO* const out = reinterpret_cast<TO*>(a.c) + (long long)col * a.ldc + row;      // (this thread's elements of C lie ldc apart)
+        const uint32_t tmem = tmem_base + buf * 256 + ((uint32_t)(quad * 32) << 16);
+        auto release = [&] {
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&misc->d_empty[buf]);
+        };
+        if (sizeof(TO) == 2 && w.part < 0 && a.tensor_stores) {
+          // bf16: all columns to registers first (the CTAs' stores come at the same time and take 5000 cycles; with both accumulators in one tile the products would
+          // wait for them), then turned in shared memory, 32 rows of C at a time, and stored by tensor copies that drop what lies outside C.  (Stored by the
+          // warps as they hold it, 64 bytes at a time, an accumulator took 13,000 cycles; with the operands' parts exchanged, sectors of 32 rows at a time, 4000.)
+          uint32_t u[NT / 32][16];
+#pragma unroll
+          for (int i = 0; i < NT / 32; ++i) take_tile(tmem + 32 * i, u[i]);
+          release();
+#pragma unroll
+          for (int i = 0; i < NT / 32; ++i) {
+            if (32 * i >= cols) break;
+            unsigned char* tile = staging + (buf * 2 + (tiles & 1)) * kMmTileBytes;
+            stage_tile(tile, u[i], quad, lane);
+            tc::fence_proxy_async_smem();
+            if (quad == 0 && lane == 0) tc::bulk_store_wait_read();      // the tile before has been read: behind the barrier its place is free
+            VSA2_GROUP_SYNC(&misc->group[buf], syncs);
+            if (quad == 0 && lane == 0) {
+              const int first = (p * PAIR + rank) * 128;
+#pragma unroll
+              for (int b = 0; b < 2; ++b)
+                if (first + 64 * b < a.p_rows) tma_store_2d(&tm_c, tile + b * 4096, first + 64 * b, col + 32 * i);
+              tc::bulk_store_commit();
+            }
+            ++tiles;
           }
+        } else {
+#pragma unroll 1
+          for (int c0 = 0; c0 < cols; c0 += 32) {
+            float v[32];
+            load_columns<32>(tmem + c0, v);
+            if (w.part >= 0) {
+              float* to = parts + w.part * of_part + (size_t)c0 * 128;
+              if (adds) add_column(to, 128, 32, v);
+              put_column(to, 128, 32, v);
+            } else if (in) {
+              TO* to = out + (long long)c0 * a.ldc;
+              if constexpr (sizeof(TO) == 4)      // (fp32 results: what has been written there for the blocks before)
+                if (adds) add_column(to, a.ldc, cols - c0, v);
+              put_column(to, a.ldc, cols - c0, v);
+            }
+          }
+          release();
         }
-        tc::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&misc->d_empty[buf]);
         if (in_turn) {
           __threadfence();
           tc::mbar_arrive(&misc->written[buf]);
@@ -515,18 +584,19 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
             __threadfence();
             const float* const mine = parts + (size_t)(w.tile - a.whole) * of_part;
 #pragma unroll 1
-            for (int c0 = 0; c0 < cols; c0 += STEP) {
-              float sum[STEP];
+            for (int c0 = 0; c0 < cols; c0 += 32) {
+              float sum[32];
 #pragma unroll
-              for (int c = 0; c < STEP; ++c) sum[c] = 0.f;
+              for (int c = 0; c < 32; ++c) sum[c] = 0.f;
 #pragma unroll 1
-              for (int o = 0; o < a.splits; ++o) add_columns<STEP>(mine + (size_t)o * a.rest * of_part + (size_t)c0 * 128, 128, STEP, sum);
-              if (in) put_columns<STEP>(out + (size_t)c0 * a.ldc, a.ldc, cols - c0, sum);
+              for (int o = 0; o < a.splits; ++o) add_column(mine + (size_t)o * a.rest * of_part + (size_t)c0 * 128, 128, 32, sum);
+              if (in) put_column(out + (long long)c0 * a.ldc, a.ldc, cols - c0, sum);
             }
           }
           VSA2_GROUP_SYNC(&misc->group[buf], syncs);       // (misc->last is read before it is written again)
         }
       }
+      if (sizeof(TO) == 2 && quad == 0 && lane == 0) tc::bulk_store_wait();
     }
   }
 
@@ -558,32 +628,50 @@ bool make_row_tmap(CUtensorMap* out, const void* base, int rows, int cols, long 
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// C as boxes of 32 rows x 64 elements of bf16
+bool make_result_tmap(CUtensorMap* out, void* base, int rows, int cols, long long ld) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+  cuuint32_t box[2] = {64, 32};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // How a product is cut: tiles, and ranges of K for those that do not fill a round of all CTAs (or pairs).  `cycles`: estimate that the choice is made by.
 struct MmPlan {
   int pt, qt, whole, rest, splits;
   double cycles;
 };
-// A block takes the tensor cores 2 cycles a column (for 128 rows of an SM).  An SM is fed 36 bytes a cycle from L2 when all of them are, up to 64 when few are
-// (measured: 8192^3 in tiles of 224 columns, 30,720 bytes a block, 855 cycles a block); what is left of the last rounds is cut into 1 .. 8 ranges, with the
-// parts' way through memory at about 2000 cycles and 700 for each.
-MmPlan mm_plan(int m, int n, int kb, int rows, int cols, int stage, int of, int sms_each) {
+struct MmShape {
+  int rows, cols, stage, of, sms_each, halves;
+  double epilogue;
+};
+// A block takes the tensor cores 2 cycles a column (128 rows of an SM); the SMs are fed 52 bytes a cycle when all of them are, up to 64 when few are.  An epilogue
+// hides behind the next tile's products; with both accumulators in one tile behind 1300 cycles of them.  Cutting what is left of the last rounds into
+// ranges of K takes the parts through memory.
+MmPlan mm_plan(int p_rows, int q_rows, int kb, const MmShape& t) {
   MmPlan best = {};
-  best.pt = (n + rows - 1) / rows;
-  best.qt = (m + cols - 1) / cols;
+  best.pt = (p_rows + t.rows - 1) / t.rows;
+  best.qt = (q_rows + t.cols - 1) / t.cols;
   const long long tiles = (long long)best.pt * best.qt;
-  auto block = [&](long long active) {
-    const double feed = 36.0 * 148 / ((active < of ? active : of) * sms_each);
-    const double fed = stage / (feed < 64.0 ? feed : 64.0), mma = 2.0 * cols;
-    return fed > mma ? fed : mma;
+  const double epilogue = t.epilogue;
+  auto item = [&](long long active, int blocks, double last) {
+    const double feed = 52.0 * 148 / ((active < t.of ? active : t.of) * t.sms_each);
+    const double fed = t.stage / (feed < 64.0 ? feed : 64.0), mma = 2.0 * t.cols, products = blocks * (fed > mma ? fed : mma);
+    return t.halves == 2 ? products + (last > 1300 ? last - 1300 : 0) : products > last ? products : last;
   };
-  best.whole = (int)(tiles / of * of);
+  best.whole = (int)(tiles / t.of * t.of);
   best.rest = (int)(tiles - best.whole);
   best.splits = 1;
-  const double rounds = (double)(tiles / of) * kb * block(of);
-  best.cycles = rounds + (best.rest > 0 ? kb * block(best.rest) : 0);
-  for (int s = 2; s <= 8 && s <= kb && best.rest > 0 && s * best.rest <= 2 * of / (cols > 224 ? 2 : 1); ++s) {
+  const double rounds = (double)(tiles / t.of) * item(t.of, kb, epilogue);
+  best.cycles = rounds + (best.rest > 0 ? item(best.rest, kb, epilogue) : 0) + epilogue;
+  for (int s = 2; s <= 8 && s <= kb && best.rest > 0 && s * best.rest <= 2 * t.of / t.halves; ++s) {
     const long long items = (long long)s * best.rest;
-    const double cut = (double)((items + of - 1) / of) * ((kb + s - 1) / s) * block(items) + 2000 + 700 * s;
+    const double parts = 3000 + t.cols * (6.0 + 4.0 * s);
+    const double cut = (double)((items + t.of - 1) / t.of) * item(items, (kb + s - 1) / s, 1500) + parts + epilogue;
     if (rounds + cut < best.cycles) {
       best.cycles = rounds + cut;
       best.splits = s;
@@ -592,35 +680,55 @@ MmPlan mm_plan(int m, int n, int kb, int rows, int cols, int stage, int of, int 
   return best;
 }
 
+struct MmCall {
+  int m, n, k, ctas;
+  Fp8Arg fa, fb;
+  cudaStream_t st;
+  MmArgs a;
+};
 template <int NT, int PAIR, int HALVES, typename TO>
-cudaError_t launch_mm_of(MmArgs a, const MmPlan& plan, const Fp8Arg& fa, const Fp8Arg& fb, int ctas, cudaStream_t st) {
-  using T = MmTile<NT, PAIR, HALVES>;
+MmPlan plan_mm(const MmCall& c) {
+  using T = MmTile<NT, PAIR, HALVES, TO>;
+  const double epilogue = (sizeof(TO) == 2 && c.a.tensor_stores ? HALVES == 2 ? 3.0 : 25.0 : 55.0) * NT;      // until an accumulator can be used again
+  return mm_plan(c.n, c.m, c.a.kb, MmShape{128 * PAIR, T::COLS, (int)T::STAGE, c.ctas / PAIR, PAIR, HALVES, epilogue});
+}
+template <int NT, int PAIR, int HALVES, typename TO>
+cudaError_t launch_mm_of(const MmCall& c, const MmPlan& plan) {
+  using T = MmTile<NT, PAIR, HALVES, TO>;
+  MmArgs a = c.a;
+  const Fp8Arg &p = c.fb, &q = c.fa;
+  a.p_rows = c.n;
+  a.q_rows = c.m;
+  a.p_scales = reinterpret_cast<const uint32_t*>(p.scales);
+  a.q_scales = reinterpret_cast<const uint32_t*>(q.scales);
   CUtensorMap tp, tq;
-  if (!make_row_tmap(&tp, fb.values, a.n, a.k, fb.ld, 128) || !make_row_tmap(&tq, fa.values, a.m, a.k, fa.ld, NT / PAIR))
+  if (!make_row_tmap(&tp, p.values, a.p_rows, c.k, p.ld, 128) || !make_row_tmap(&tq, q.values, a.q_rows, c.k, q.ld, NT / PAIR))
     return cudaErrorInvalidValue;
+  CUtensorMap tm_c = tq;      // (no map of C: never used)
+  if (sizeof(TO) == 2 && a.tensor_stores && !make_result_tmap(&tm_c, a.c, c.m, c.n, a.ldc)) return cudaErrorInvalidValue;
   a.pt = plan.pt; a.qt = plan.qt; a.whole = plan.whole; a.rest = plan.rest; a.splits = plan.splits;
-  // tiles along m that share B's rows while they pass through L2
+  // tiles along Q that share P's rows while they pass through L2
   a.gq = a.qt < 12 / HALVES ? a.qt : 12 / HALVES;
   const long long items = a.whole + (long long)a.rest * a.splits;
-  int of = ctas / PAIR;
+  int of = c.ctas / PAIR;
   if (items < of) of = (int)items;
   static KernelAttr attr;
   cudaError_t e;
   if ((e = prepare_kernel((const void*)fp8_matmul_kernel<NT, PAIR, HALVES, TO>, attr, T::SMEM))) return e;
-  return launch_kernel(fp8_matmul_kernel<NT, PAIR, HALVES, TO>, of * PAIR, kMmThreads, T::SMEM, st, tp, tq, a);
+  return launch_kernel(fp8_matmul_kernel<NT, PAIR, HALVES, TO>, of * PAIR, kMmThreads, T::SMEM, c.st, tp, tq, tm_c, a);
 }
-template <int NT, int PAIR, int HALVES>
-MmPlan mm_plan_of(const MmArgs& a, int ctas) {
-  using T = MmTile<NT, PAIR, HALVES>;
-  return mm_plan(a.m, a.n, a.kb, 128 * PAIR, T::COLS, (int)T::STAGE, ctas / PAIR, PAIR);
-}
-template <int NT, int PAIR, int HALVES>
-cudaError_t launch_mm(const MmArgs& a, const MmPlan& plan, const Fp8Arg& fa, const Fp8Arg& fb, int ctas, bool f32, cudaStream_t st) {
-  return f32 ? launch_mm_of<NT, PAIR, HALVES, float>(a, plan, fa, fb, ctas, st) : launch_mm_of<NT, PAIR, HALVES, bf16>(a, plan, fa, fb, ctas, st);
-}
-template <int NT, int PAIR>
-cudaError_t launch_mm(const MmArgs& a, const Fp8Arg& fa, const Fp8Arg& fb, int ctas, bool f32, cudaStream_t st) {
-  return launch_mm<NT, PAIR, 1>(a, mm_plan_of<NT, PAIR, 1>(a, ctas), fa, fb, ctas, f32, st);
+template <int NT, int PAIR, int HALVES, typename TO>
+cudaError_t launch_mm(const MmCall& c) { return launch_mm_of<NT, PAIR, HALVES, TO>(c, plan_mm<NT, PAIR, HALVES, TO>(c)); }
+
+// B's rows are the accumulators' lanes, A's their columns: few rows of A take the narrowest tile that holds them, many by the estimate tiles of 256 x 224 or
+// 256 x 448.
+template <typename TO>
+cudaError_t launch_product(const MmCall& c, bool pair) {
+  if (c.m <= 32) return launch_mm<32, 1, 1, TO>(c);
+  if (!pair) return launch_mm<128, 1, 1, TO>(c);
+  if (c.m <= 128) return launch_mm<128, 2, 1, TO>(c);
+  const MmPlan one = plan_mm<224, 2, 1, TO>(c), two = plan_mm<224, 2, 2, TO>(c);
+  return one.cycles <= two.cycles ? launch_mm_of<224, 2, 1, TO>(c, one) : launch_mm_of<224, 2, 2, TO>(c, two);
 }
 
 }  // namespace
@@ -639,30 +747,27 @@ cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Ar
   cudaError_t e;
   if ((e = sm_count(&sms)) != cudaSuccess) return e;
   const int ctas = sms < kMmCtas ? sms : kMmCtas;
-  // Pairs wherever B has rows for both (a pair fetches half the rows of A for each SM) and the context has room for one; the narrowest tile that holds A's
-  // rows.
+  // Pairs wherever B has rows for both (a pair fetches half a tile's columns for each SM) and the context has room for one
   bool pair = n > 128 && ctas >= 2;
   if (pair) {
     static ClusterRoom room;
-    if ((e = cluster_room((const void*)fp8_matmul_kernel<224, 2, 2, float>, room, 2, kMmThreads, MmTile<224, 2, 2>::SMEM, &pair))) return e;
+    if ((e = cluster_room((const void*)fp8_matmul_kernel<224, 2, 2, float>, room, 2, kMmThreads, MmTile<224, 2, 2, float>::SMEM, &pair))) return e;
   }
-  MmArgs a;
-  a.m = m; a.n = n; a.k = k;
+  MmCall call;
+  call.m = m; call.n = n; call.k = k; call.ctas = ctas;
+  call.fa = fa; call.fb = fb;
+  call.st = st;
+  MmArgs& a = call.a;
+  a = MmArgs{};
   a.kb = (k + 127) / 128;
   a.chunk = c_f32 ? kMmChunk : a.kb;
-  a.a_scales = reinterpret_cast<const uint32_t*>(fa.scales);
-  a.b_scales = reinterpret_cast<const uint32_t*>(fb.scales);
   a.c = c; a.ldc = ldc;
+  a.tensor_stores = !c_f32 && (reinterpret_cast<uintptr_t>(c) & 15u) == 0 && ldc % 8 == 0;
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
   a.status = reinterpret_cast<StatusBlock*>(ws);
   a.counters = reinterpret_cast<int*>(ws + sizeof(StatusBlock));
   a.partial = reinterpret_cast<float*>(ws + align_up(sizeof(StatusBlock) + kMmCounters * sizeof(int), 256));
-  if (!pair) return m <= 32 ? launch_mm<32, 1>(a, fa, fb, ctas, c_f32, st) : launch_mm<128, 1>(a, fa, fb, ctas, c_f32, st);
-  if (m <= 32) return launch_mm<32, 2>(a, fa, fb, ctas, c_f32, st);
-  if (m <= 64) return launch_mm<64, 2>(a, fa, fb, ctas, c_f32, st);
-  if (m <= 128) return launch_mm<128, 2>(a, fa, fb, ctas, c_f32, st);
-  const MmPlan one = mm_plan_of<224, 2, 1>(a, ctas), two = mm_plan_of<224, 2, 2>(a, ctas);
-  return one.cycles <= two.cycles ? launch_mm<224, 2, 1>(a, one, fa, fb, ctas, c_f32, st) : launch_mm<224, 2, 2>(a, two, fa, fb, ctas, c_f32, st);
+  return c_f32 ? launch_product<float>(call, pair) : launch_product<bf16>(call, pair);
 }
 
 }  // namespace vsa2
