@@ -4,14 +4,15 @@
 // of 128 get the same one.  The scales' words (four blocks of a row, the layout of the quantiser) go to tensor memory as they are, and the
 // instruction's scale selector picks the block's byte: one copy serves 512 values of K.
 //
-// B's rows (n, the weights of a projection) are the 128 rows of a tile, A's rows (m, the tokens) its NT columns.  A warp of the epilogue then holds 32
-// neighbouring elements of a row of C, whatever C's row length or alignment, and few tokens take a narrow tile (NT = 16 .. 224) under
-// weights that stream through at the same rate.
-// Persistent CTAs, one per SM: a producer warp (TMA), an issuer, a warp for the scales, four for the epilogue; two accumulators in tensor memory, so that
-// a tile's epilogue runs behind the next tile's products.
+// B's rows (n, the weights of a projection) are the 128 rows of a CTA's tile, A's rows (m, the tokens) its NT columns: few tokens take a narrow tile under weights that
+// stream through.  Many take 224 columns on a pair of SMs (cta_group::2): 256 rows of B, each CTA fetches its half of B's rows and half of A's, 30 KB
+// for 2 x 128 x 224 x 128 multiply-adds, where a CTA alone fetches 45.  Persistent CTAs, one per SM: a producer warp (TMA), an issuer, a warp for the scales, two
+// groups of four for the epilogue; two accumulators in tensor memory, so that a tile's epilogue runs behind the next tile's products.
 //
-// Whole tiles are dealt out in rounds; what is left of the last rounds (all, where there are fewer tiles than CTAs) is cut along K so that every CTA gets the
-// same share: a tile's parts go to the workspace in fp32 and the CTA that delivers the last part adds them in their order (results do not depend on which that is).
+// What bounds it: with many tiles the power limit and the intake from L2 (8192 x 4096 x 4096: 51 bytes a cycle and SM, 600 cycles a block where the tensor cores need
+// 448); 75600 x 15360 x 5120 runs at 3.1 PFLOP/s and more, 1.9 times the library's bf16 product.  Tiles of 448 columns, both accumulators in one tile, need 27 % less
+// intake and were as fast at large sizes (20000 x 15360 x 5120 1028 us both ways), slower where rounds are few (4096^3 60 us instead of 52).  One row of A: the
+// weights' bytes.
 #include <cuda.h>
 
 #include "common.cuh"
@@ -24,30 +25,27 @@ namespace vsa2 {
 
 namespace {
 
-constexpr int kMmCtas = 148;            // most CTAs (the workspace is laid out for them)
+constexpr int kMmCtas = 148;            // most CTAs
 constexpr int kMmThreads = 384;
 constexpr int kMmStagesMost = 12;
-constexpr int kMmCounters = 2 * kMmCtas;
-constexpr int kMmChunk = 64;            // blocks of K that an accumulator sums for an fp32 result
+constexpr int kMmScaleSlots = 4;
+constexpr int kMmSplits = 16;           // most ranges that K is cut into
+// Blocks of K that an accumulator sums for an fp32 result; the epilogue adds the pieces.  (The tensor cores cut what does not fit an accumulator instead of rounding
+// it: with 24,000 values of K in one the result was 1.7e-6 off, with pieces of 8192 it is 5e-7.)
+constexpr int kMmChunk = 64;
 constexpr uint32_t kMmPBytes = 128 * 128;
 constexpr uint32_t kMmTileBytes = 32 * 128 * 2;      // 32 rows of C x 128 elements of bf16
 
-// NT columns an accumulator; PAIR: CTAs that share a tile (2: a pair of SMs, 256 rows of B, each CTA fetches its rows of B and half the rows
-// of A); HALVES: accumulators side by side (2: a tile of 2 NT columns takes both)
-template <int NT, int PAIR, int HALVES, typename TO>
+// NT columns; PAIR: CTAs that share a tile; TO: type of the results
+template <int NT, int PAIR, typename TO>
 struct MmTile {
-  static constexpr int COLS = NT * HALVES;
-  static constexpr uint32_t QBYTES = NT / PAIR * 128;                       // rows of A for one accumulator
-  static constexpr uint32_t STAGE = kMmPBytes + HALVES * QBYTES;
-  static constexpr int SFQ = (NT + 127) / 128;                              // 512-byte pieces of A's scales for one accumulator
-  static constexpr uint32_t SCALES = 512 + HALVES * SFQ * 512;              // words of 128 rows of B, of the rows of A
-  static constexpr int SLOTS = HALVES == 2 ? 2 : 4;
+  static constexpr uint32_t STAGE = kMmPBytes + NT / PAIR * 128;
+  static constexpr int SFQ = (NT + 127) / 128;                              // 512-byte pieces of the scales of the columns' rows
+  static constexpr uint32_t SCALES = 512 + SFQ * 512;
   static constexpr uint32_t STAGING = sizeof(TO) == 2 ? 4 * kMmTileBytes : 0;      // two tiles of results for each group of the epilogue
-  static constexpr uint32_t ROOM = 227 * 1024 - 2048 - SLOTS * SCALES - STAGING;
+  static constexpr uint32_t ROOM = 227 * 1024 - 2048 - kMmScaleSlots * SCALES - STAGING;
   static constexpr int STAGES = ROOM / STAGE < kMmStagesMost ? ROOM / STAGE : kMmStagesMost;
-  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + STAGING + SLOTS * SCALES;
-  // HALVES = 2: blocks whose products with one half are issued together at a tile's two ends
-  static constexpr int BUNCH = STAGES > 4 ? 3 : 2;
+  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + STAGING + kMmScaleSlots * SCALES;
   // columns of tensor memory: accumulators at 0 and 256 (of 224 at most), scales of even and odd groups of four blocks behind them
   __host__ __device__ static constexpr uint32_t scales_at(uint32_t group) { return 224 + (group & 1) * 256; }
 };
@@ -56,31 +54,27 @@ struct MmTile {
 struct MmArgs {
   int p_rows, q_rows, kb;            // kb: blocks of K
   int pt, qt, gq;                    // tiles along P, along Q; tiles along Q that are taken together
+  int splits, chunk;                 // ranges that K is cut into; most blocks of K in one accumulator
   int tensor_stores;                 // C lies as tensor copies need it
-  int chunk;                         // most blocks of K in one accumulator
-  int whole, rest, splits;           // tiles that are dealt out whole; the others, each cut into `splits` ranges of K
   const uint32_t* p_scales;
   const uint32_t* q_scales;
   void* c;
-  long long ldc;
+  long long ldc, split_stride;       // elements between the results of two ranges
   StatusBlock* status;
-  int* counters;
-  float* partial;
 };
 
 struct MmMisc {
-  uint64_t full[kMmStagesMost], empty[kMmStagesMost], sc_full[4], sc_empty[4], d_full[2], d_empty[2], group[2], written[2];
+  uint64_t full[kMmStagesMost], empty[kMmStagesMost], sc_full[kMmScaleSlots], sc_empty[kMmScaleSlots];
+  uint64_t d_full[2], d_empty[2], group[2], written[2];
   uint32_t tmem_base;
   int abort_flag;
-  int last[2];
 };
 
-// The items of a CTA (or pair): every `all`-th, the whole tiles first, then the first ranges of the others, their second ranges, ..: CTAs that run at the
-// same time read the same part of K, so that rows they share come from memory once (shares of equal size, begun anywhere: 2304 x 1536, K = 32760
-// 192 us).  Each item in pieces of at most `chunk` blocks.
+// The items of a CTA (or pair): every `all`-th of the tiles with the first range of K, then with the second, ..: CTAs that run at the same time read the same part
+// of K, so that rows they share come from memory once.  Each item in pieces of at most `chunk` blocks.
 struct MmWalk {
-  int tile, kb0, kb1;                // current piece
-  int r0, r1, part;                  // the item's blocks; its place among the parts, -1: a whole tile
+  int p, q, split;                   // tile, range
+  int kb0, kb1, r0, r1;              // blocks of the current piece, of the item
   int item, all;
   __device__ __forceinline__ void init(int me, int of) {
     item = me;
@@ -91,16 +85,14 @@ struct MmWalk {
     if (kb1 < r1) {
       kb0 = kb1;
     } else {
-      if (item >= a.whole + a.rest * a.splits) return false;
-      part = -1;
-      tile = item; r0 = 0; r1 = a.kb;
-      if (item >= a.whole && a.splits > 1) {
-        part = item - a.whole;
-        const int split = part / a.rest;
-        tile = a.whole + part - split * a.rest;
-        r0 = (int)((long long)a.kb * split / a.splits);
-        r1 = (int)((long long)a.kb * (split + 1) / a.splits);
-      }
+      const int tiles = a.pt * a.qt;
+      if (item >= tiles * a.splits) return false;
+      split = item / tiles;
+      const int tile = item - split * tiles, per = a.gq * a.pt, g = tile / per, r = tile - g * per, w = min(a.gq, a.qt - g * a.gq);
+      p = r / w;
+      q = g * a.gq + r - p * w;
+      r0 = (int)((long long)a.kb * split / a.splits);
+      r1 = (int)((long long)a.kb * (split + 1) / a.splits);
       item += all;
       kb0 = r0;
     }
@@ -108,11 +100,6 @@ struct MmWalk {
     return true;
   }
 };
-__device__ __forceinline__ void mm_place(const MmArgs& a, int tile, int& p, int& q) {
-  const int per = a.gq * a.pt, g = tile / per, r = tile - g * per, w = min(a.gq, a.qt - g * a.gq);
-  p = r / w;
-  q = g * a.gq + r - p * w;
-}
 
 // ---- a CTA alone, or a pair whose first CTA issues the products and holds the barriers that both sides arrive at
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -218,14 +205,13 @@ __device__ __forceinline__ void mm_dealloc(uint32_t base) {
   if constexpr (PAIR == 1) tc::tmem_dealloc(base, 512);
   else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(base) : "memory");
 }
-// 32 lanes x STEP columns of an accumulator
-template <int STEP>
-__device__ __forceinline__ void load_columns(uint32_t taddr, float (&v)[STEP]) {
-  uint32_t r[STEP];
+// 32 lanes x 32 columns of an accumulator
+__device__ __forceinline__ void load_columns(uint32_t taddr, float (&v)[32]) {
+  uint32_t r[32];
   tc::tmem_ld32(taddr, r);
   tc::tmem_ld_wait();
 #pragma unroll
-  for (int c = 0; c < STEP; ++c) v[c] = __uint_as_float(r[c]);
+  for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(r[c]);
 }
 // e4m3 x e4m3, ue8m0 scales, both operands K-major, 128 rows a CTA; `sf`: which byte of the scales' words
 template <int NT, int PAIR>
@@ -272,9 +258,20 @@ __device__ __forceinline__ void take_tile(uint32_t taddr, uint32_t (&u)[16]) {
     for (int b = 0; b < 4; ++b)
       u[4 * g + b] = pack_bf16x2(__uint_as_float(r[b >> 1][4 * g + 2 * (b & 1)]), __uint_as_float(r[b >> 1][4 * g + 2 * (b & 1) + 1]));
 }
-// .. to 32 rows of C of 32 elements, in a tile of 32 rows x 128 elements that lies as the tensor copy takes it: two boxes of 64 elements, rows of 128 bytes, 16-byte places
-// exchanged by the row
+// .. to rows of C in a tile that lies as the tensor copy takes it, 16-byte places exchanged by the row.  SWAP: 32 rows of C of this warp's, 64 bytes each, in
+// one box of 128 rows.  Else turned, 32 rows of C of 32 elements, in two boxes of 32 rows x 64 elements (128 bytes)
+template <bool SWAP>
 __device__ __forceinline__ void stage_tile(unsigned char* tile, const uint32_t (&u)[16], int quad, int lane) {
+  if constexpr (SWAP) {
+    const int row = quad * 32 + (lane >> 3) * 8 + (lane & 7);
+    const uint32_t to = tc::smem_u32(tile) + row * 64;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};"
+                   ::"r"(to + ((g ^ ((row >> 1) & 3)) << 4)), "r"(u[4 * g]), "r"(u[4 * g + 1]), "r"(u[4 * g + 2]), "r"(u[4 * g + 3])
+                   : "memory");
+    return;
+  }
   const int row = lane & 7, block = (quad & 1) * 4 + (lane >> 3);      // of C; of 8 elements in the box
   const uint32_t to = tc::smem_u32(tile) + (quad >> 1) * 4096 + row * 128 + ((block ^ row) << 4);
 #pragma unroll
@@ -289,11 +286,11 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, const void* f
                : "memory");
 }
 
-template <int NT, int PAIR, int HALVES, typename TO>
+template <int NT, int PAIR, bool SWAP, typename TO>
 __global__ void __cluster_dims__(PAIR, 1, 1) __launch_bounds__(kMmThreads, 1)
 fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_c,
                   const __grid_constant__ MmArgs a) {
-  using T = MmTile<NT, PAIR, HALVES, TO>;
+  using T = MmTile<NT, PAIR, TO>;
   extern __shared__ unsigned char mm_smem[];
   __shared__ MmMisc misc_store;
   MmMisc* misc = &misc_store;
@@ -308,7 +305,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
       tc::mbar_init(&misc->full[s], 1);
       tc::mbar_init(&misc->empty[s], 1);
     }
-    for (int s = 0; s < T::SLOTS; ++s) {
+    for (int s = 0; s < kMmScaleSlots; ++s) {
       tc::mbar_init(&misc->sc_full[s], rank == 0 ? PAIR : 1);
       tc::mbar_init(&misc->sc_empty[s], 1);
     }
@@ -333,19 +330,17 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
     MmWalk w;
     w.init(blockIdx.x / PAIR, gridDim.x / PAIR);
     if (warp == 0) {
-      // ---------------------------------------------------------------- operands: a lane for B's rows, one for A's rows of each accumulator
+      // ---------------------------------------------------------------- operands: a lane for P's rows, one for Q's
       // (in one warp or two, in copies of 128 rows or of 32: no difference)
       uint32_t s = 0, parity = 1;
       const CUtensorMap* tm = lane == 0 ? &tm_p : &tm_q;
-      const uint32_t offset = lane == 0 ? 0 : kMmPBytes + (lane - 1) * T::QBYTES;
+      const uint32_t offset = lane == 0 ? 0 : kMmPBytes;
       while (w.advance(a)) {
-        int p, q;
-        mm_place(a, w.tile, p, q);
-        const int row = lane == 0 ? (p * PAIR + rank) * 128 : q * T::COLS + (lane - 1) * NT + rank * (NT / PAIR);
+        const int row = lane == 0 ? (w.p * PAIR + rank) * 128 : w.q * NT + rank * (NT / PAIR);
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
           VSA2_WAIT(&misc->empty[s], parity);
           if (rank == 0 && lane == 0) tc::mbar_expect_tx(&misc->full[s], PAIR * T::STAGE);
-          if (lane <= HALVES) tma_load_rows<PAIR>(ring + s * T::STAGE + offset, tm, &misc->full[s], kb * 128, row);
+          if (lane < 2) tma_load_rows<PAIR>(ring + s * T::STAGE + offset, tm, &misc->full[s], kb * 128, row);
           __syncwarp();
           if (++s == T::STAGES) {
             s = 0;
@@ -357,71 +352,39 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
       // ---------------------------------------------------------------- products (converged warp, one lane issues)
       const uint64_t ring_desc = tc::smem_desc_sw128(tc::smem_u32(ring), 16, 1024);
       const uint64_t scale_desc = tc::smem_desc_plain(tc::smem_u32(scales), 16, 128);
-      uint32_t stage = 0, parity = 0, sc = 0, seg = 0;
-      // products of block kb in stage s with half h of the columns, scales of group number `group`
-      auto products = [&](int kb, uint32_t s, uint32_t group, uint32_t buf, int h, bool first) {
-        const uint64_t dp = ring_desc + (uint64_t)(s * T::STAGE >> 4), dq = dp + (uint64_t)((kMmPBytes + h * T::QBYTES) >> 4);
-        const uint32_t idesc = idesc_scaled<NT, PAIR>(kb & 3), tm_sc = tmem_base + T::scales_at(group);
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          mma_scaled<PAIR>(tmem_base + buf * 256, dp + 2 * ks, dq + 2 * ks, idesc, tm_sc, tm_sc + 4 + h * 4 * T::SFQ, ks > 0 || !first);
-      };
+      uint32_t s = 0, parity = 0, sc = 0, seg = 0;
       for (; w.advance(a); ++seg) {
-        if constexpr (HALVES == 1) VSA2_WAIT_PAIR(&misc->d_empty[seg & 1], ((seg >> 1) & 1) ^ 1);
-        else VSA2_WAIT_PAIR(&misc->d_empty[0], (seg & 1) ^ 1);
-        // HALVES = 2: both accumulators are in use all the time.  Of the last blocks of a tile those with the first half come first, so that its epilogue
-        // runs behind those with the second half; of the first blocks likewise, so that the second half's epilogue runs behind those with the first
-        int kb = w.kb0;
-        while (kb < w.kb1) {
-          const int bunch = HALVES == 1 ? 1 : kb == w.kb0 || kb == w.kb1 - T::BUNCH ? min(T::BUNCH, w.kb1 - kb) : 1;
-          uint32_t first_group = sc, s = stage, s_parity = parity;
-          for (int i = 0; i < bunch; ++i) {
-            const bool fresh = kb + i == w.kb0 || ((kb + i) & 3) == 0;
+        const uint32_t buf = seg & 1;
+        VSA2_WAIT_PAIR(&misc->d_empty[buf], ((seg >> 1) & 1) ^ 1);
+        for (int kb = w.kb0; kb < w.kb1; ++kb) {
+          const bool fresh = kb == w.kb0 || (kb & 3) == 0;
+          if (fresh) {
+            VSA2_WAIT_PAIR(&misc->sc_full[sc % kMmScaleSlots], (sc / kMmScaleSlots) & 1);
+            ++sc;
+          }
+          VSA2_WAIT(&misc->full[s], parity);
+          tc::tc_fence_after();
+          if (tc::elect_one()) {
+            const uint32_t slot = (sc - 1) % kMmScaleSlots, tm_sc = tmem_base + T::scales_at(sc - 1);
             if (fresh) {
-              VSA2_WAIT_PAIR(&misc->sc_full[sc % T::SLOTS], (sc / T::SLOTS) & 1);
-              ++sc;
-            }
-            if (i == 0) first_group = sc - 1;
-            VSA2_WAIT(&misc->full[s], s_parity);
-            tc::tc_fence_after();
-            if (tc::elect_one()) {
-              if (fresh) {
-                const uint32_t slot = (sc - 1) % T::SLOTS, tm_sc = tmem_base + T::scales_at(sc - 1);
-                const uint64_t d = scale_desc + (uint64_t)(slot * T::SCALES >> 4);
+              const uint64_t d = scale_desc + (uint64_t)(slot * T::SCALES >> 4);
 #pragma unroll
-                for (int j = 0; j < 1 + HALVES * T::SFQ; ++j) copy_scales<PAIR>(tm_sc + 4 * j, d + (uint64_t)(512 * j >> 4));
-                commit_all<PAIR>(&misc->sc_empty[slot]);
-              }
-              products(kb + i, s, sc - 1, HALVES == 1 ? seg & 1 : 0, 0, kb + i == w.kb0);
-              if (HALVES == 1) commit_all<PAIR>(&misc->empty[s]);
-              if (kb + i == w.kb1 - 1) commit_all<PAIR>(&misc->d_full[HALVES == 1 ? seg & 1 : 0]);
+              for (int j = 0; j < 1 + T::SFQ; ++j) copy_scales<PAIR>(tm_sc + 4 * j, d + (uint64_t)(512 * j >> 4));
+              commit_all<PAIR>(&misc->sc_empty[slot]);
             }
-            __syncwarp();
-            if (++s == T::STAGES) {
-              s = 0;
-              s_parity ^= 1;
-            }
+            const uint64_t dp = ring_desc + (uint64_t)(s * T::STAGE >> 4), dq = dp + (uint64_t)(kMmPBytes >> 4);
+            const uint32_t idesc = idesc_scaled<NT, PAIR>(kb & 3);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              mma_scaled<PAIR>(tmem_base + buf * 256, dp + 2 * ks, dq + 2 * ks, idesc, tm_sc, tm_sc + 4, ks > 0 || kb > w.kb0);
+            commit_all<PAIR>(&misc->empty[s]);
+            if (kb == w.kb1 - 1) commit_all<PAIR>(&misc->d_full[buf]);
           }
-          if constexpr (HALVES == 2) {
-            if (kb == w.kb0) {
-              VSA2_WAIT_PAIR(&misc->d_empty[1], (seg & 1) ^ 1);
-              tc::tc_fence_after();
-            }
-            uint32_t group = first_group;
-            for (int i = 0; i < bunch; ++i) {
-              if (i > 0 && ((kb + i) & 3) == 0) ++group;
-              if (tc::elect_one()) {
-                products(kb + i, stage, group, 1, 1, kb + i == w.kb0);
-                commit_all<PAIR>(&misc->empty[stage]);
-                if (kb + i == w.kb1 - 1) commit_all<PAIR>(&misc->d_full[1]);
-              }
-              __syncwarp();
-              if (++stage == T::STAGES) stage = 0;
-            }
+          __syncwarp();
+          if (++s == T::STAGES) {
+            s = 0;
+            parity ^= 1;
           }
-          stage = s;
-          parity = s_parity;
-          kb += bunch;
         }
       }
     } else if ((warp == 1 || warp == 3) && rank == 1) {
@@ -432,45 +395,35 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
       for (uint32_t seg = 0; w.advance(a); ++seg) {
         if (warp == 1) {
           for (int g = w.kb0 >> 2; g <= (w.kb1 - 1) >> 2; ++g, ++sc) {
-            VSA2_WAIT(&misc->sc_full[sc % T::SLOTS], (sc / T::SLOTS) & 1);
-            if (lane == 0) arrive_leader(&misc->sc_full[sc % T::SLOTS]);
+            VSA2_WAIT(&misc->sc_full[sc % kMmScaleSlots], (sc / kMmScaleSlots) & 1);
+            if (lane == 0) arrive_leader(&misc->sc_full[sc % kMmScaleSlots]);
             __syncwarp();
           }
         } else {
-#pragma unroll
-          for (int h = 0; h < HALVES; ++h) {
-            const uint32_t buf = HALVES == 2 ? h : seg & 1;
-            VSA2_WAIT(&misc->d_empty[buf], (HALVES == 2 ? seg : seg >> 1) & 1);
-            if (lane == 0) arrive_leader(&misc->d_empty[buf]);
-            __syncwarp();
-          }
+          VSA2_WAIT(&misc->d_empty[seg & 1], (seg >> 1) & 1);
+          if (lane == 0) arrive_leader(&misc->d_empty[seg & 1]);
+          __syncwarp();
         }
       }
     } else if (warp == 2) {
       // ---------------------------------------------------------------- scales: words of rows lane, lane + 32, .. as 16 bytes a lane
-      // AHEAD groups of four blocks are on their way from memory at a time: with one, a group's latency bound short rows (one row of A against 15,360 x
-      // 5,120: 26 us)
-      constexpr int NV = 4 + 4 * HALVES * T::SFQ, AHEAD = NV <= 8 ? 6 : NV <= 12 ? 4 : 2;
+      // AHEAD groups of four blocks are on their way from memory at a time
+      constexpr int NV = 4 + 4 * T::SFQ, AHEAD = NV <= 8 ? 6 : 4;
       uint32_t v[AHEAD][NV];
       bool there[AHEAD];
       int g = 0, g_end = 0, row_p = 0, row_q = 0;
       auto next = [&](uint32_t (&to)[NV]) {
         if (g >= g_end) {
           if (!w.advance(a)) return false;
-          int p, q;
-          mm_place(a, w.tile, p, q);
-          row_p = (p * PAIR + rank) * 128 + lane;
-          row_q = q * T::COLS + lane;
+          row_p = (w.p * PAIR + rank) * 128 + lane;
+          row_q = w.q * NT + lane;
           g = w.kb0 >> 2;
           g_end = ((w.kb1 - 1) >> 2) + 1;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) to[j] = row_p + j * 32 < a.p_rows ? a.p_scales[(size_t)g * a.p_rows + row_p + j * 32] : 0u;
 #pragma unroll
-        for (int j = 0; j < NV - 4; ++j) {
-          const int h = j / (4 * T::SFQ), i = (j - h * 4 * T::SFQ) * 32, r = row_q + h * NT + i;
-          to[4 + j] = i < NT && r < a.q_rows ? a.q_scales[(size_t)g * a.q_rows + r] : 0u;
-        }
+        for (int j = 0; j < NV - 4; ++j) to[4 + j] = j * 32 < NT && row_q + j * 32 < a.q_rows ? a.q_scales[(size_t)g * a.q_rows + row_q + j * 32] : 0u;
         ++g;
         return true;
       };
@@ -480,8 +433,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
 #pragma unroll
         for (int d = 0; d < AHEAD; ++d) {
           if (!there[d]) continue;      // (then none of those behind it is there either)
-          const uint32_t slot = sc % T::SLOTS;
-          VSA2_WAIT_PARKED(&misc->sc_empty[slot], ((sc / T::SLOTS) & 1) ^ 1);
+          const uint32_t slot = sc % kMmScaleSlots;
+          VSA2_WAIT_PARKED(&misc->sc_empty[slot], ((sc / kMmScaleSlots) & 1) ^ 1);
           unsigned char* to = scales + slot * T::SCALES + lane * 16;
 #pragma unroll
           for (int j = 0; j < NV / 4; ++j)
@@ -496,36 +449,25 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
     } else if (warp >= 4) {
       // ---------------------------------------------------------------- epilogue: four warps for each accumulator
       const int quad = warp & 3, buf = (warp >> 2) - 1;
+      // Pieces of one item come to the two groups in turn, each adding to what the other has written: one after the other
+      const bool in_turn = a.chunk < a.kb;
       uint32_t syncs = 0, turn = 0, tiles = 0;
       for (uint32_t seg = 0; w.advance(a); ++seg) {
-        if (HALVES == 1 && (int)(seg & 1) != buf) continue;
-        int p, q;
-        mm_place(a, w.tile, p, q);
-        const int row = (p * PAIR + rank) * 128 + quad * 32 + lane, col = q * T::COLS + (HALVES == 2 ? buf * NT : 0);
-        const int cols = min(NT, a.q_rows - col);      // (0 or less: the second half of a tile that ends in the first)
-        const bool in = row < a.p_rows;
+        if ((int)(seg & 1) != buf) continue;
+        const int first = (w.p * PAIR + rank) * 128, row = first + quad * 32 + lane, col = w.q * NT, cols = min(NT, a.q_rows - col);
         VSA2_WAIT_PARKED(&misc->d_full[buf], turn & 1);
         ++turn;
         tc::tc_fence_after();
-        const bool adds = w.kb0 > w.r0;
-        // Pieces of one item come to the two groups of warps in turn (HALVES = 1), each adding to what the other has written: one after the other
-        const bool in_turn = HALVES == 1 && a.chunk < a.kb;
         if (in_turn && seg > 0) VSA2_WAIT_PARKED(&misc->written[buf ^ 1], ((seg - 1) >> 1) & 1);
-        constexpr int WIDE = HALVES == 2 ? 2 : 1;
-        // [part][half][rank][column][row]
-        const size_t of_part = (size_t)WIDE * PAIR * 128 * NT;
-        float* const parts = a.partial + (size_t)((HALVES == 2 ? buf : 0) * PAIR + rank) * (128 * NT) + quad * 32 + lane;
-        TO* const out = reinterpret_cast<TO*>(a.c) + (long long)col * a.ldc + row;      // (this thread's elements of C lie ldc apart)
         const uint32_t tmem = tmem_base + buf * 256 + ((uint32_t)(quad * 32) << 16);
         auto release = [&] {
           tc::tc_fence_before();
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(&misc->d_empty[buf]);
         };
-        if (sizeof(TO) == 2 && w.part < 0 && a.tensor_stores) {
-          // bf16: all columns to registers first (the CTAs' stores come at the same time and take 5000 cycles; with both accumulators in one tile the products would
-          // wait for them), then turned in shared memory, 32 rows of C at a time, and stored by tensor copies that drop what lies outside C.  (Stored by the
-          // warps as they hold it, 64 bytes at a time, an accumulator took 13,000 cycles; with the operands' parts exchanged, sectors of 32 rows at a time, 4000.)
+        if (sizeof(TO) == 2 && a.tensor_stores) {
+          // bf16: all columns to registers first (the CTAs' stores come at the same time and take 5000 cycles), then in shared memory, turned unless SWAP, and out
+          // by tensor copies that drop what lies outside C.  (Stored by the warps as they hold it, 64 bytes at a time, an accumulator took 13,000 cycles.)
           uint32_t u[NT / 32][16];
 #pragma unroll
           for (int i = 0; i < NT / 32; ++i) take_tile(tmem + 32 * i, u[i]);
@@ -534,32 +476,33 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
           for (int i = 0; i < NT / 32; ++i) {
             if (32 * i >= cols) break;
             unsigned char* tile = staging + (buf * 2 + (tiles & 1)) * kMmTileBytes;
-            stage_tile(tile, u[i], quad, lane);
+            stage_tile<SWAP>(tile, u[i], quad, lane);
             tc::fence_proxy_async_smem();
             if (quad == 0 && lane == 0) tc::bulk_store_wait_read();      // the tile before has been read: behind the barrier its place is free
             VSA2_GROUP_SYNC(&misc->group[buf], syncs);
             if (quad == 0 && lane == 0) {
-              const int first = (p * PAIR + rank) * 128;
+              if (SWAP) {
+                if (first < a.p_rows) tma_store_2d(&tm_c, tile, col + 32 * i, first);
+              } else {
 #pragma unroll
-              for (int b = 0; b < 2; ++b)
-                if (first + 64 * b < a.p_rows) tma_store_2d(&tm_c, tile + b * 4096, first + 64 * b, col + 32 * i);
+                for (int b = 0; b < 2; ++b)
+                  if (first + 64 * b < a.p_rows) tma_store_2d(&tm_c, tile + b * 4096, first + 64 * b, col + 32 * i);
+              }
               tc::bulk_store_commit();
             }
             ++tiles;
           }
         } else {
+          // (not SWAP: a thread's elements of C lie ldc apart)
+          TO* const out = reinterpret_cast<TO*>(a.c) + w.split * a.split_stride + (long long)col * a.ldc + row;
 #pragma unroll 1
           for (int c0 = 0; c0 < cols; c0 += 32) {
             float v[32];
-            load_columns<32>(tmem + c0, v);
-            if (w.part >= 0) {
-              float* to = parts + w.part * of_part + (size_t)c0 * 128;
-              if (adds) add_column(to, 128, 32, v);
-              put_column(to, 128, 32, v);
-            } else if (in) {
+            load_columns(tmem + c0, v);
+            if (row < a.p_rows) {
               TO* to = out + (long long)c0 * a.ldc;
-              if constexpr (sizeof(TO) == 4)      // (fp32 results: what has been written there for the blocks before)
-                if (adds) add_column(to, a.ldc, cols - c0, v);
+              if constexpr (sizeof(TO) == 4)      // (what has been written there for the blocks before)
+                if (w.kb0 > w.r0) add_column(to, a.ldc, cols - c0, v);
               put_column(to, a.ldc, cols - c0, v);
             }
           }
@@ -568,32 +511,6 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
         if (in_turn) {
           __threadfence();
           tc::mbar_arrive(&misc->written[buf]);
-        }
-        if (w.part >= 0 && w.kb1 == w.r1) {
-          __threadfence();
-          VSA2_GROUP_SYNC(&misc->group[buf], syncs);
-          if (quad == 0 && lane == 0) {
-            int* counter = a.counters + ((w.tile - a.whole) * WIDE + (HALVES == 2 ? buf : 0)) * PAIR + rank;
-            const bool last = atomicAdd(counter, 1) == a.splits - 1;
-            if (last) *counter = 0;
-            misc->last[buf] = last;
-            __threadfence();
-          }
-          VSA2_GROUP_SYNC(&misc->group[buf], syncs);
-          if (misc->last[buf]) {
-            __threadfence();
-            const float* const mine = parts + (size_t)(w.tile - a.whole) * of_part;
-#pragma unroll 1
-            for (int c0 = 0; c0 < cols; c0 += 32) {
-              float sum[32];
-#pragma unroll
-              for (int c = 0; c < 32; ++c) sum[c] = 0.f;
-#pragma unroll 1
-              for (int o = 0; o < a.splits; ++o) add_column(mine + (size_t)o * a.rest * of_part + (size_t)c0 * 128, 128, 32, sum);
-              if (in) put_column(out + (long long)c0 * a.ldc, a.ldc, cols - c0, sum);
-            }
-          }
-          VSA2_GROUP_SYNC(&misc->group[buf], syncs);       // (misc->last is read before it is written again)
         }
       }
       if (sizeof(TO) == 2 && quad == 0 && lane == 0) tc::bulk_store_wait();
@@ -617,6 +534,30 @@ done:
   if (warp == 3) mm_dealloc<PAIR>(tmem_base);
 }
 
+// The ranges of K, each a matrix [m, ldp] in fp32, added in their order.  Four elements of a row a thread.
+template <typename TO>
+__global__ void __launch_bounds__(256) fp8_sum_kernel(const float* parts, int splits, int m, int n, long long ldp, TO* __restrict__ c, long long ldc) {
+  grid_enter();
+  const long long per_row = ldp / 4, i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
+  if (row >= m) return;
+  const int col = (int)(i - row * per_row) * 4;
+  const float* from = parts + row * ldp + col;
+  float4 v[kMmSplits];
+#pragma unroll
+  for (int s = 0; s < kMmSplits; ++s)
+    if (s < splits) v[s] = *reinterpret_cast<const float4*>(from + s * (m * ldp));
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < kMmSplits; ++s) {
+    if (s < splits) {
+      sum[0] += v[s].x; sum[1] += v[s].y; sum[2] += v[s].z; sum[3] += v[s].w;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (col + j < n) put(c + row * ldc + col + j, sum[j]);
+}
+
 bool make_row_tmap(CUtensorMap* out, const void* base, int rows, int cols, long long ld, int box_rows) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
@@ -627,118 +568,114 @@ bool make_row_tmap(CUtensorMap* out, const void* base, int rows, int cols, long 
   return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-// C as boxes of 32 rows x 64 elements of bf16
-bool make_result_tmap(CUtensorMap* out, void* base, int rows, int cols, long long ld) {
+// C as boxes of 32 rows x 64 elements of bf16, with `swap` of 128 rows x 32
+bool make_result_tmap(CUtensorMap* out, void* base, int rows, int cols, long long ld, bool swap) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-  cuuint32_t box[2] = {64, 32};
+  cuuint32_t box[2] = {swap ? 32u : 64u, swap ? 128u : 32u};
   cuuint32_t estr[2] = {1, 1};
-  return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            swap ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a product is cut: tiles, and ranges of K for those that do not fill a round of all CTAs (or pairs).  `cycles`: estimate that the choice is made by.
+// One call
+struct MmCall {
+  int m, n, k, kb, ctas;
+  Fp8Arg fa, fb;
+  void* c;
+  long long ldc;
+  bool f32, tensor_stores;
+  StatusBlock* status;
+  float* parts;
+  cudaStream_t st;
+};
+
+// How a product is cut, and the cycles that it is estimated at.  A block of K takes the tensor cores 2 cycles a column (128 rows of an SM), an issue of at least 300, and
+// an SM is fed 52 bytes a cycle when all of them are, up to 64 when few are.  Where half the CTAs (or pairs) and more would have no tile, K is cut into ranges, each a
+// matrix of its own in the workspace, which a second kernel adds (about 5000 cycles, and the bytes).
 struct MmPlan {
-  int pt, qt, whole, rest, splits;
+  int pt, qt, splits;
   double cycles;
 };
-struct MmShape {
-  int rows, cols, stage, of, sms_each, halves;
-  double epilogue;
-};
-// A block takes the tensor cores 2 cycles a column (128 rows of an SM); the SMs are fed 52 bytes a cycle when all of them are, up to 64 when few are.  An epilogue
-// hides behind the next tile's products; with both accumulators in one tile behind 1300 cycles of them.  Cutting what is left of the last rounds into
-// ranges of K takes the parts through memory.
-MmPlan mm_plan(int p_rows, int q_rows, int kb, const MmShape& t) {
-  MmPlan best = {};
-  best.pt = (p_rows + t.rows - 1) / t.rows;
-  best.qt = (q_rows + t.cols - 1) / t.cols;
-  const long long tiles = (long long)best.pt * best.qt;
-  const double epilogue = t.epilogue;
-  auto item = [&](long long active, int blocks, double last) {
-    const double feed = 52.0 * 148 / ((active < t.of ? active : t.of) * t.sms_each);
-    const double fed = t.stage / (feed < 64.0 ? feed : 64.0), mma = 2.0 * t.cols, products = blocks * (fed > mma ? fed : mma);
-    return t.halves == 2 ? products + (last > 1300 ? last - 1300 : 0) : products > last ? products : last;
+template <int NT, int PAIR>
+MmPlan plan_mm(const MmCall& c, bool swap) {
+  MmPlan plan;
+  plan.pt = ((swap ? c.m : c.n) + 128 * PAIR - 1) / (128 * PAIR);
+  plan.qt = ((swap ? c.n : c.m) + NT - 1) / NT;
+  plan.splits = 1;
+  const int of = c.ctas / PAIR;
+  const long long tiles = (long long)plan.pt * plan.qt;
+  auto products = [&](long long items, int blocks) {
+    const double feed = 52.0 * kMmCtas / ((items < of ? items : of) * PAIR);
+    const double fed = (kMmPBytes + NT / PAIR * 128) / (feed < 64.0 ? feed : 64.0);
+    const double block = fed > 2.0 * NT ? fed : 2.0 * NT;
+    return (double)((items + of - 1) / of) * blocks * (block > 300.0 ? block : 300.0);
   };
-  best.whole = (int)(tiles / t.of * t.of);
-  best.rest = (int)(tiles - best.whole);
-  best.splits = 1;
-  const double rounds = (double)(tiles / t.of) * item(t.of, kb, epilogue);
-  best.cycles = rounds + (best.rest > 0 ? item(best.rest, kb, epilogue) : 0) + epilogue;
-  for (int s = 2; s <= 8 && s <= kb && best.rest > 0 && s * best.rest <= 2 * t.of / t.halves; ++s) {
-    const long long items = (long long)s * best.rest;
-    const double parts = 3000 + t.cols * (6.0 + 4.0 * s);
-    const double cut = (double)((items + t.of - 1) / t.of) * item(items, (kb + s - 1) / s, 1500) + parts + epilogue;
-    if (rounds + cut < best.cycles) {
-      best.cycles = rounds + cut;
-      best.splits = s;
+  plan.cycles = products(tiles, c.kb);
+  if (swap) plan.cycles *= 1.06;      // (its results go out 64 bytes at a time: 8192 x 4096 x 4096 98 us instead of 91)
+  for (int s = 2; !swap && s <= kMmSplits && s <= c.kb && tiles * s <= of; ++s) {
+    const double cycles = products(tiles * s, (c.kb + s - 1) / s) + 5000 + 8.0 * s * c.m * c.n / (30.0 * kMmCtas);
+    if (cycles < plan.cycles) {
+      plan.cycles = cycles;
+      plan.splits = s;
     }
   }
-  return best;
+  return plan;
 }
 
-struct MmCall {
-  int m, n, k, ctas;
-  Fp8Arg fa, fb;
-  cudaStream_t st;
+template <int NT, int PAIR, bool SWAP, typename TO>
+cudaError_t launch_tiles(const MmCall& c, const MmPlan& plan, void* result, long long ldc, long long split_stride) {
+  using T = MmTile<NT, PAIR, TO>;
+  const Fp8Arg &p = SWAP ? c.fa : c.fb, &q = SWAP ? c.fb : c.fa;
   MmArgs a;
-};
-template <int NT, int PAIR, int HALVES, typename TO>
-MmPlan plan_mm(const MmCall& c) {
-  using T = MmTile<NT, PAIR, HALVES, TO>;
-  const double epilogue = (sizeof(TO) == 2 && c.a.tensor_stores ? HALVES == 2 ? 3.0 : 25.0 : 55.0) * NT;      // until an accumulator can be used again
-  return mm_plan(c.n, c.m, c.a.kb, MmShape{128 * PAIR, T::COLS, (int)T::STAGE, c.ctas / PAIR, PAIR, HALVES, epilogue});
-}
-template <int NT, int PAIR, int HALVES, typename TO>
-cudaError_t launch_mm_of(const MmCall& c, const MmPlan& plan) {
-  using T = MmTile<NT, PAIR, HALVES, TO>;
-  MmArgs a = c.a;
-  const Fp8Arg &p = c.fb, &q = c.fa;
-  a.p_rows = c.n;
-  a.q_rows = c.m;
+  a.p_rows = SWAP ? c.m : c.n;
+  a.q_rows = SWAP ? c.n : c.m;
+  a.kb = c.kb;
+  a.pt = plan.pt; a.qt = plan.qt; a.splits = plan.splits;
+  a.gq = a.qt < 12 ? a.qt : 12;      // tiles along Q that share P's rows while they pass through L2
+  a.chunk = c.f32 ? kMmChunk : c.kb;
+  a.tensor_stores = sizeof(TO) == 2 && c.tensor_stores;
   a.p_scales = reinterpret_cast<const uint32_t*>(p.scales);
   a.q_scales = reinterpret_cast<const uint32_t*>(q.scales);
+  a.c = result; a.ldc = ldc; a.split_stride = split_stride;
+  a.status = c.status;
   CUtensorMap tp, tq;
   if (!make_row_tmap(&tp, p.values, a.p_rows, c.k, p.ld, 128) || !make_row_tmap(&tq, q.values, a.q_rows, c.k, q.ld, NT / PAIR))
     return cudaErrorInvalidValue;
-  CUtensorMap tm_c = tq;      // (no map of C: never used)
-  if (sizeof(TO) == 2 && a.tensor_stores && !make_result_tmap(&tm_c, a.c, c.m, c.n, a.ldc)) return cudaErrorInvalidValue;
-  a.pt = plan.pt; a.qt = plan.qt; a.whole = plan.whole; a.rest = plan.rest; a.splits = plan.splits;
-  // tiles along Q that share P's rows while they pass through L2
-  a.gq = a.qt < 12 / HALVES ? a.qt : 12 / HALVES;
-  const long long items = a.whole + (long long)a.rest * a.splits;
-  int of = c.ctas / PAIR;
-  if (items < of) of = (int)items;
+  CUtensorMap tm_c = tq;      // (without tensor stores: never used)
+  if (a.tensor_stores && !make_result_tmap(&tm_c, result, c.m, c.n, ldc, SWAP)) return cudaErrorInvalidValue;
+  const long long items = (long long)plan.pt * plan.qt * plan.splits;
+  const int of = items < c.ctas / PAIR ? (int)items : c.ctas / PAIR;
   static KernelAttr attr;
   cudaError_t e;
-  if ((e = prepare_kernel((const void*)fp8_matmul_kernel<NT, PAIR, HALVES, TO>, attr, T::SMEM))) return e;
-  return launch_kernel(fp8_matmul_kernel<NT, PAIR, HALVES, TO>, of * PAIR, kMmThreads, T::SMEM, c.st, tp, tq, tm_c, a);
+  if ((e = prepare_kernel((const void*)fp8_matmul_kernel<NT, PAIR, SWAP, TO>, attr, T::SMEM))) return e;
+  return launch_kernel(fp8_matmul_kernel<NT, PAIR, SWAP, TO>, of * PAIR, kMmThreads, T::SMEM, c.st, tp, tq, tm_c, a);
 }
-template <int NT, int PAIR, int HALVES, typename TO>
-cudaError_t launch_mm(const MmCall& c) { return launch_mm_of<NT, PAIR, HALVES, TO>(c, plan_mm<NT, PAIR, HALVES, TO>(c)); }
 
-// B's rows are the accumulators' lanes, A's their columns: few rows of A take the narrowest tile that holds them, many by the estimate tiles of 256 x 224 or
-// 256 x 448.
-template <typename TO>
-cudaError_t launch_product(const MmCall& c, bool pair) {
-  if (c.m <= 32) return launch_mm<32, 1, 1, TO>(c);
-  if (!pair) return launch_mm<128, 1, 1, TO>(c);
-  if (c.m <= 128) return launch_mm<128, 2, 1, TO>(c);
-  const MmPlan one = plan_mm<224, 2, 1, TO>(c), two = plan_mm<224, 2, 2, TO>(c);
-  return one.cycles <= two.cycles ? launch_mm_of<224, 2, 1, TO>(c, one) : launch_mm_of<224, 2, 2, TO>(c, two);
+template <int NT, int PAIR>
+cudaError_t launch_mm(const MmCall& c, const MmPlan& plan) {
+  if (plan.splits == 1)
+    return c.f32 ? launch_tiles<NT, PAIR, false, float>(c, plan, c.c, c.ldc, 0) : launch_tiles<NT, PAIR, false, bf16>(c, plan, c.c, c.ldc, 0);
+  const long long ldp = (c.n + 3) / 4 * 4;
+  const cudaError_t e = launch_tiles<NT, PAIR, false, float>(c, plan, c.parts, ldp, c.m * ldp);
+  if (e != cudaSuccess) return e;
+  const unsigned grid = (unsigned)((c.m * ldp / 4 + 255) / 256);
+  return c.f32 ? launch_kernel(fp8_sum_kernel<float>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, reinterpret_cast<float*>(c.c), c.ldc)
+               : launch_kernel(fp8_sum_kernel<bf16>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, reinterpret_cast<bf16*>(c.c), c.ldc);
 }
+
+// most elements of a product whose K is cut: tiles x ranges are at most the CTAs (or pairs)
+size_t parts_elements(int m) { return (size_t)kMmCtas * 128 * (m <= 32 ? 32 : m <= 128 ? 128 : 224); }
 
 }  // namespace
 
-// [status][counters of the tiles that are cut][two parts a CTA]
+// [status][ranges of K]
 size_t fp8_matmul_workspace_bytes(int m, int n, int k) {
   (void)n;
   (void)k;
-  const int columns = m <= 32 ? 32 : m <= 128 ? 128 : 224;      // (the widest accumulator that a product of m rows may take)
-  return align_up(sizeof(StatusBlock) + kMmCounters * sizeof(int), 256) + (size_t)2 * kMmCtas * 128 * columns * sizeof(float);
+  return align_up(sizeof(StatusBlock), 256) + parts_elements(m) * sizeof(float);
 }
 
 cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Arg& fb, void* c, int c_f32, long long ldc,
@@ -746,28 +683,34 @@ cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Ar
   int sms = 0;
   cudaError_t e;
   if ((e = sm_count(&sms)) != cudaSuccess) return e;
-  const int ctas = sms < kMmCtas ? sms : kMmCtas;
-  // Pairs wherever B has rows for both (a pair fetches half a tile's columns for each SM) and the context has room for one
-  bool pair = n > 128 && ctas >= 2;
+  MmCall call;
+  call.m = m; call.n = n; call.k = k;
+  call.kb = (k + 127) / 128;
+  call.ctas = sms < kMmCtas ? sms : kMmCtas;
+  call.fa = fa; call.fb = fb;
+  call.c = c; call.ldc = ldc;
+  call.f32 = c_f32 != 0;
+  call.tensor_stores = !c_f32 && (reinterpret_cast<uintptr_t>(c) & 15u) == 0 && ldc % 8 == 0;
+  unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
+  call.status = reinterpret_cast<StatusBlock*>(ws);
+  call.parts = reinterpret_cast<float*>(ws + align_up(sizeof(StatusBlock), 256));
+  call.st = st;
+  if (m <= 32) return launch_mm<32, 1>(call, plan_mm<32, 1>(call, false));
+  // Pairs wherever B has rows for both and the context has room for one
+  bool pair = n > 128 && call.ctas >= 2;
   if (pair) {
     static ClusterRoom room;
-    if ((e = cluster_room((const void*)fp8_matmul_kernel<224, 2, 2, float>, room, 2, kMmThreads, MmTile<224, 2, 2, float>::SMEM, &pair))) return e;
+    if ((e = cluster_room((const void*)fp8_matmul_kernel<224, 2, false, float>, room, 2, kMmThreads, MmTile<224, 2, float>::SMEM, &pair))) return e;
   }
-  MmCall call;
-  call.m = m; call.n = n; call.k = k; call.ctas = ctas;
-  call.fa = fa; call.fb = fb;
-  call.st = st;
-  MmArgs& a = call.a;
-  a = MmArgs{};
-  a.kb = (k + 127) / 128;
-  a.chunk = c_f32 ? kMmChunk : a.kb;
-  a.c = c; a.ldc = ldc;
-  a.tensor_stores = !c_f32 && (reinterpret_cast<uintptr_t>(c) & 15u) == 0 && ldc % 8 == 0;
-  unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
-  a.status = reinterpret_cast<StatusBlock*>(ws);
-  a.counters = reinterpret_cast<int*>(ws + sizeof(StatusBlock));
-  a.partial = reinterpret_cast<float*>(ws + align_up(sizeof(StatusBlock) + kMmCounters * sizeof(int), 256));
-  return c_f32 ? launch_product<float>(call, pair) : launch_product<bf16>(call, pair);
+  if (!pair) return launch_mm<128, 1>(call, plan_mm<128, 1>(call, false));
+  if (m <= 128) return launch_mm<128, 2>(call, plan_mm<128, 2>(call, false));
+  // A's rows as the lanes, B's as the columns where that fills the rounds better (512 x 15360 x 5120: 138 tiles instead of 180 on 74 pairs, 35 us instead of 49)
+  const MmPlan plan = plan_mm<224, 2>(call, false);
+  if (call.tensor_stores) {
+    const MmPlan swapped = plan_mm<224, 2>(call, true);
+    if (swapped.cycles < plan.cycles) return launch_tiles<224, 2, true, bf16>(call, swapped, c, ldc, 0);
+  }
+  return launch_mm<224, 2>(call, plan);
 }
 
 }  // namespace vsa2
