@@ -20,40 +20,90 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
 }
 __device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 __device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-__device__ __forceinline__ uint32_t magnitude(float x) { return finite_bits(x) ? __float_as_uint(x) & 0x7fffffffu : 0u; }
-// an infinity becomes NaN here (times zero), the conversion alone would make it 448
-__device__ __forceinline__ float scaled(float x, float inv) { return finite_bits(x) ? x * inv : __uint_as_float(0x7fffffffu); }
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) { return e4m3x2(a, b) | e4m3x2(c, d) << 16; }
+// Blocks where something is not finite are rare: only they look at every value (CHECK).  (An infinity becomes NaN; the conversion alone would make it 448.)
+template <bool CHECK>
+__device__ __forceinline__ float scaled(float x, float inv) { return !CHECK || finite_bits(x) ? x * inv : __uint_as_float(0x7fffffffu); }
 
+// Eight neighbouring elements of a row as they lie in memory; magnitudes as the bits of fp32 numbers, those of bf16 two in a word
+template <bool F32> struct Oct;
+template <> struct Oct<false> {
+  uint32_t u[4];
+  __device__ __forceinline__ void zero() { u[0] = u[1] = u[2] = u[3] = 0u; }
+  __device__ __forceinline__ void load(const void* x, size_t at) {
+    const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(x) + at);
+    u[0] = v.x; u[1] = v.y; u[2] = v.z; u[3] = v.w;
+  }
+  __device__ __forceinline__ void set(const void* x, size_t at, int j) {
+    u[j / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(x)[at] << 16 * (j & 1);
+  }
+  __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? u[j / 2] & 0xffff0000u : u[j / 2] << 16); }
+  __device__ __forceinline__ uint32_t top() const {
+    const uint32_t t = __vmaxu2(__vmaxu2(u[0] & 0x7fff7fffu, u[1] & 0x7fff7fffu), __vmaxu2(u[2] & 0x7fff7fffu, u[3] & 0x7fff7fffu));
+    return max(t & 0xffff0000u, t << 16);
+  }
+  struct Tops {                      // of the eight columns
+    uint32_t t[4] = {0u, 0u, 0u, 0u};
+    __device__ __forceinline__ uint32_t get(int j) const { return j & 1 ? t[j / 2] & 0xffff0000u : t[j / 2] << 16; }
+  };
+  __device__ __forceinline__ void raise(Tops& o) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o.t[i] = __vmaxu2(o.t[i], u[i] & 0x7fff7fffu);
+  }
+};
+template <> struct Oct<true> {
+  float f[8];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = 0.f;
+  }
+  __device__ __forceinline__ void load(const void* x, size_t at) {
+    const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(x) + at);
+    const float4 a = p[0], b = p[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+  __device__ __forceinline__ void set(const void* x, size_t at, int j) { f[j] = reinterpret_cast<const float*>(x)[at]; }
+  __device__ __forceinline__ float get(int j) const { return f[j]; }
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t t = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t = max(t, __float_as_uint(f[j]) & 0x7fffffffu);
+    return t;
+  }
+  struct Tops {
+    uint32_t t[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+    __device__ __forceinline__ uint32_t get(int j) const { return t[j]; }
+  };
+  __device__ __forceinline__ void raise(Tops& o) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o.t[j] = max(o.t[j], __float_as_uint(f[j]) & 0x7fffffffu);
+  }
+};
+constexpr uint32_t kInf = 0x7f800000u;
+// the largest finite magnitude of eight
 template <bool F32>
-__device__ __forceinline__ float element(const void* x, size_t i) {
-  return F32 ? reinterpret_cast<const float*>(x)[i] : __bfloat162float(reinterpret_cast<const bf16*>(x)[i]);
+__device__ __forceinline__ uint32_t finite_top(const Oct<F32>& o) {
+  uint32_t t = 0u;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (finite_bits(o.get(j))) t = max(t, __float_as_uint(o.get(j)) & 0x7fffffffu);
+  return t;
 }
 // elements i .. i+7 of a row of `cols` (zeros beyond it); VEC: rows lie on 16-byte boundaries
 template <bool F32, bool VEC>
-__device__ __forceinline__ void load8(const void* x, size_t row_at, int i, int cols, float (&f)[8]) {
+__device__ __forceinline__ void load8(const void* x, size_t row_at, int i, int cols, Oct<F32>& o) {
   if (VEC && i + 8 <= cols) {
-    if (F32) {
-      const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(x) + row_at + i);
-      const float4 a = p[0], b = p[1];
-      f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    } else {
-      const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(x) + row_at + i);
-      const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f[2 * j] = __uint_as_float(u[j] << 16);
-        f[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
-      }
-    }
+    o.load(x, row_at + i);
   } else {
+    o.zero();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = i + j < cols ? element<F32>(x, row_at + i + j) : 0.f;
+    for (int j = 0; j < 8; ++j)
+      if (i + j < cols) o.set(x, row_at + i + j, j);
   }
 }
 // bytes i .. i+7 of a row of `cols` values (its start 16-byte aligned, i a multiple of 8)
@@ -64,14 +114,20 @@ __device__ __forceinline__ void put8(unsigned char* row, int i, int cols, uint32
     for (int j = 0; i + j < cols; ++j) row[i + j] = (unsigned char)((j < 4 ? lo >> 8 * j : hi >> 8 * (j - 4)) & 0xffu);
   }
 }
-__device__ __forceinline__ uint32_t max_of(const float (&f)[8]) {
-  uint32_t top = 0;
+template <bool CHECK, bool F32>
+__device__ __forceinline__ void put_oct(unsigned char* row, int i, int cols, const Oct<F32>& o, float inv) {
+  float f[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) top = max(top, magnitude(f[j]));
-  return top;
+  for (int j = 0; j < 8; ++j) f[j] = scaled<CHECK>(o.get(j), inv);
+  put8(row, i, cols, e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
+}
+__device__ __forceinline__ uint32_t team_max(uint32_t t) {      // of 16 threads
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
+  return t;
 }
 
-// Rows alone: a team of 16 threads takes 512 columns of a row (four blocks, one word of scales).  grid (word groups, row tiles of 16)
+// Rows alone: a team of 16 threads takes 512 columns of a row (four blocks, one word of scales).  grid (row tiles of 16, word groups)
 template <bool F32, bool VEC>
 __global__ void __launch_bounds__(kQzThreads) fp8_rows_kernel(const void* x, int rows, int cols, long long ld, Fp8Arg out) {
   grid_enter();
@@ -79,23 +135,22 @@ __global__ void __launch_bounds__(kQzThreads) fp8_rows_kernel(const void* x, int
   const long long row = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
   const int c0 = blockIdx.y * 512;
   const long long r = row < rows ? row : rows - 1;
-  float f[4][8];
+  Oct<F32> o[4];
 #pragma unroll
-  for (int b = 0; b < 4; ++b) load8<F32, VEC>(x, (size_t)r * ld, c0 + b * 128 + l * 8, cols, f[b]);
+  for (int b = 0; b < 4; ++b) load8<F32, VEC>(x, (size_t)r * ld, c0 + b * 128 + l * 8, cols, o[b]);
   uint32_t word = 0;
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
-    uint32_t top = max_of(f[b]);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    uint32_t top = team_max(o[b].top());
+    const bool odd = __any_sync(0xffffffffu, top >= kInf);
+    if (odd) top = team_max(finite_top<F32>(o[b]));
     if (c0 + b * 128 >= cols) continue;
     const uint32_t s = scale_byte(top);
-    const float inv = inverse_scale(s);
     word |= s << 8 * b;
     if (row < rows) {
-      const uint32_t lo = e4m3x4(scaled(f[b][0], inv), scaled(f[b][1], inv), scaled(f[b][2], inv), scaled(f[b][3], inv));
-      const uint32_t hi = e4m3x4(scaled(f[b][4], inv), scaled(f[b][5], inv), scaled(f[b][6], inv), scaled(f[b][7], inv));
-      put8(out.values + row * out.ld, c0 + b * 128 + l * 8, cols, lo, hi);
+      unsigned char* to = out.values + row * out.ld;
+      if (odd) put_oct<true, F32>(to, c0 + b * 128 + l * 8, cols, o[b], inverse_scale(s));
+      else put_oct<false, F32>(to, c0 + b * 128 + l * 8, cols, o[b], inverse_scale(s));
     }
   }
   if (l == 0 && row < rows) reinterpret_cast<uint32_t*>(out.scales)[(size_t)blockIdx.y * rows + row] = word;
@@ -109,86 +164,79 @@ __device__ __forceinline__ void put_scale(unsigned char* scales, int rows, int r
     for (int j = (kb & 3) + 1; j < 4; ++j) word[j] = 0;
 }
 
-// A tile of 128 x 128: both forms, or either.  A team of 16 threads holds 8 rows, 8 columns a thread.  The transpose passes through shared memory
-// as bytes: a thread writes the 8 bytes that its rows give a column; the 8-byte places of a column are exchanged by column group
-// so that neither side meets a bank twice.  grid (column tiles, row tiles)
-template <bool F32, bool VEC>
-__global__ void __launch_bounds__(kQzThreads) fp8_tile_kernel(const void* x, int rows, int cols, long long ld, int squares, Fp8Arg out,
-                                                              Fp8Arg out_t) {
-  grid_enter();
-  __shared__ __align__(16) unsigned char turned[128 * 128];
-  __shared__ uint32_t col_top[16][128];
-  __shared__ uint32_t tops[kQzThreads / 32];
+struct TileShared {
+  unsigned char turned[128 * 128];
+  uint32_t col_top[16][128];
+  uint32_t tops[kQzThreads / 32];
+};
+
+// a tile whose values are in the threads' registers: both forms, or either
+template <bool CHECK, bool F32>
+__device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], TileShared& sh, int rows, int cols, int squares, const Fp8Arg& out, const Fp8Arg& out_t) {
   const int l = threadIdx.x & 15, team = threadIdx.x >> 4, tid = threadIdx.x;
   const int c0 = blockIdx.y * 128, r0 = blockIdx.x * 128;
-  float f[8][8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = r0 + team * 8 + i;
-    if (row < rows) load8<F32, VEC>(x, (size_t)row * ld, c0 + l * 8, cols, f[i]);
-    else
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[i][j] = 0.f;
-  }
   const int blocks = (cols + 127) / 128, blocks_t = (rows + 127) / 128;
+  auto top_of = [](const Oct<F32>& v) { return CHECK ? finite_top<F32>(v) : v.top(); };
   uint32_t top_all = 0;
   if (squares) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top_all = max(top_all, max_of(f[i]));
+    for (int i = 0; i < 8; ++i) top_all = max(top_all, top_of(o[i]));
     top_all = __reduce_max_sync(0xffffffffu, top_all);
-    if ((tid & 31) == 0) tops[tid >> 5] = top_all;
+    if ((tid & 31) == 0) sh.tops[tid >> 5] = top_all;
     __syncthreads();
-    for (int i = 0; i < kQzThreads / 32; ++i) top_all = max(top_all, tops[i]);
+    for (int i = 0; i < kQzThreads / 32; ++i) top_all = max(top_all, sh.tops[i]);
   }
   if (out.values != nullptr) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      uint32_t top = top_all;
-      if (!squares) {
-        top = max_of(f[i]);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      }
-      const uint32_t s = scale_byte(top);
-      const float inv = inverse_scale(s);
+      const uint32_t s = scale_byte(squares ? top_all : team_max(top_of(o[i])));
       const int row = r0 + team * 8 + i;
       if (row < rows) {
-        const uint32_t lo = e4m3x4(scaled(f[i][0], inv), scaled(f[i][1], inv), scaled(f[i][2], inv), scaled(f[i][3], inv));
-        const uint32_t hi = e4m3x4(scaled(f[i][4], inv), scaled(f[i][5], inv), scaled(f[i][6], inv), scaled(f[i][7], inv));
-        put8(out.values + row * out.ld, c0 + l * 8, cols, lo, hi);
+        put_oct<CHECK, F32>(out.values + row * out.ld, c0 + l * 8, cols, o[i], inverse_scale(s));
         if (l == 0) put_scale(out.scales, rows, row, blockIdx.y, blocks, s);
       }
     }
   }
   if (out_t.values == nullptr) return;
   if (!squares) {
+    typename Oct<F32>::Tops t;
+    if (!CHECK) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i].raise(t);
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      uint32_t top = 0;
+      uint32_t top = t.get(j);
+      if (CHECK) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, magnitude(f[i][j]));
-      col_top[team][l * 8 + j] = top;
+        for (int i = 0; i < 8; ++i)
+          if (finite_bits(o[i].get(j))) top = max(top, __float_as_uint(o[i].get(j)) & 0x7fffffffu);
+      }
+      sh.col_top[team][l * 8 + j] = top;
     }
     __syncthreads();
     if (tid < 128) {
       uint32_t top = 0;
-      for (int t = 0; t < 16; ++t) top = max(top, col_top[t][tid]);
-      col_top[0][tid] = top;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = max(top, sh.col_top[r][tid]);
+      sh.col_top[0][tid] = top;
     }
     __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float inv = inverse_scale(scale_byte(squares ? top_all : col_top[0][l * 8 + j]));
-    const uint32_t lo = e4m3x4(scaled(f[0][j], inv), scaled(f[1][j], inv), scaled(f[2][j], inv), scaled(f[3][j], inv));
-    const uint32_t hi = e4m3x4(scaled(f[4][j], inv), scaled(f[5][j], inv), scaled(f[6][j], inv), scaled(f[7][j], inv));
-    *reinterpret_cast<uint2*>(turned + (l * 8 + j) * 128 + ((team ^ l) << 3)) = make_uint2(lo, hi);
+    const float inv = inverse_scale(scale_byte(squares ? top_all : sh.col_top[0][l * 8 + j]));
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = scaled<CHECK>(o[i].get(j), inv);
+    *reinterpret_cast<uint2*>(sh.turned + (l * 8 + j) * 128 + ((team ^ l) << 3)) =
+        make_uint2(e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
   }
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < 128 * 8 / kQzThreads; ++u) {
     const int e = u * kQzThreads + tid, c = e >> 3, part = (e & 7) * 2, g = c >> 3;      // places part, part + 1 of column c
-    uint4 v = *reinterpret_cast<const uint4*>(turned + c * 128 + (((part ^ g) & ~1) << 3));
+    uint4 v = *reinterpret_cast<const uint4*>(sh.turned + c * 128 + (((part ^ g) & ~1) << 3));
     if (g & 1) v = make_uint4(v.z, v.w, v.x, v.y);
     if (c0 + c < cols) {
       unsigned char* row = out_t.values + (long long)(c0 + c) * out_t.ld;
@@ -202,7 +250,30 @@ __global__ void __launch_bounds__(kQzThreads) fp8_tile_kernel(const void* x, int
     }
   }
   if (tid < 128 && c0 + tid < cols)
-    put_scale(out_t.scales, cols, c0 + tid, blockIdx.x, blocks_t, scale_byte(squares ? top_all : col_top[0][tid]));
+    put_scale(out_t.scales, cols, c0 + tid, blockIdx.x, blocks_t, scale_byte(squares ? top_all : sh.col_top[0][tid]));
+}
+
+// A tile of 128 x 128: both forms, or either.  A team of 16 threads holds 8 rows, 8 columns a thread.  The transpose passes through shared memory
+// as bytes: a thread writes the 8 bytes that its rows give a column; the 8-byte places of a column are exchanged by column group
+// so that neither side meets a bank twice.  grid (row tiles, column tiles)
+template <bool F32, bool VEC>
+__global__ void __launch_bounds__(kQzThreads) fp8_tile_kernel(const void* x, int rows, int cols, long long ld, int squares, Fp8Arg out,
+                                                              Fp8Arg out_t) {
+  grid_enter();
+  __shared__ __align__(16) TileShared sh;
+  const int l = threadIdx.x & 15, team = threadIdx.x >> 4;
+  Oct<F32> o[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = blockIdx.x * 128 + team * 8 + i;
+    if (row < rows) load8<F32, VEC>(x, (size_t)row * ld, blockIdx.y * 128 + l * 8, cols, o[i]);
+    else o[i].zero();
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, o[i].top());
+  if (__syncthreads_or(top >= kInf)) quantize_tile<true, F32>(o, sh, rows, cols, squares, out, out_t);
+  else quantize_tile<false, F32>(o, sh, rows, cols, squares, out, out_t);
 }
 
 }  // namespace

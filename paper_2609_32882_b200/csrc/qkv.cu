@@ -213,14 +213,26 @@ __global__ void __launch_bounds__(kQkvThreads) qkv_bwd_kernel(const __grid_const
       float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = norm && a.w[seg & 1] != nullptr ? a.w[seg & 1][l * 8 + i] : 1.f;
+      Raw8<TG> g_next[U];
+      Raw8<TI> x_next[U];
+      auto fetch = [&](int h) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          g_next[u].load(gp + min(h + u, hi - 1) * g.sh);
+          if (norm) x_next[u].load(xp + min(h + u, hi - 1) * x.sh);
+        }
+      };
+      fetch(lo);
       for (int h = lo; h < hi; h += U) {
+        // (the next heads' rows are on their way while these are computed)
         Raw8<TG> gr[U];
         Raw8<TI> xr[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          gr[u].load(gp + min(h + u, hi - 1) * g.sh);
-          if (norm) xr[u].load(xp + min(h + u, hi - 1) * x.sh);
+          gr[u] = g_next[u];
+          xr[u] = x_next[u];
         }
+        if (h + U < hi) fetch(h + U);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           float f[8];
