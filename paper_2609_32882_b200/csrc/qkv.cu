@@ -19,12 +19,14 @@ namespace vsa2 {
 namespace {
 
 constexpr int kQkvThreads = 256;
-constexpr int kQkvParts = 1024;      // most CTAs of the backward, each with its own partial sums of the weights' gradients
+constexpr int kBwdQueue = 12;        // 16-byte pieces that a thread of the backward has in its queue (48 KB a CTA)
+constexpr int kQkvParts = 1024;      // most CTAs of the backward, each with its own partial sums of a weight's gradient
 
 template <typename T> struct Raw8;      // eight channels as they lie in memory
 template <> struct Raw8<bf16> {
   uint4 v;
   __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void load(const uint4* p, int) { v = *p; }      // (pieces `apart` from one another)
   __device__ __forceinline__ void get(float (&f)[8]) const {
     const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -39,6 +41,10 @@ template <> struct Raw8<float> {
   __device__ __forceinline__ void load(const float* p) {
     a = reinterpret_cast<const float4*>(p)[0];
     b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void load(const uint4* p, int apart) {
+    a = *reinterpret_cast<const float4*>(p);
+    b = *reinterpret_cast<const float4*>(p + apart);
   }
   __device__ __forceinline__ void get(float (&f)[8]) const {
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
@@ -179,122 +185,173 @@ __global__ void __launch_bounds__(kQkvThreads) qkv_fwd_kernel(const __grid_const
   }
 }
 
-// grid (CTAs that walk through the token tiles, 1, groups of heads); x = the forward's rows of q and k, dy -> dx
+// A thread's own queue in shared memory: 16-byte pieces that it asks for AHEAD rows before it uses them.  (Registers for that many in flight would cost the CTAs
+// that hide the rest: with the next two heads' rows in registers 480p with text took 211 us.)
+// (Through L1: the second half of an fp32 row's sectors comes from there.)
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+
+// x = the forward's rows of q and k, dy -> dx.  A job is a tile of tokens and a group of heads.  The first CTAs take q's jobs, the others k's, so that a thread sums the
+// gradient of one weight; then all take v's.
+struct BwdJobs { int ctas[2], jobs[2], per[2]; };      // of q, of k: CTAs, jobs, heads in a group
 template <int D, typename TI, typename TG, typename TO, bool HALVES>
-__global__ void __launch_bounds__(kQkvThreads) qkv_bwd_kernel(const __grid_constant__ QkvArgs a, const __grid_constant__ HeadsPair fwd,
-                                                              float* __restrict__ partial) {
-  constexpr int TEAM = D / 8, ROWS = kQkvThreads / TEAM, U = 2;
+__global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(const __grid_constant__ QkvArgs a, const __grid_constant__ HeadsPair fwd,
+                                                                        const __grid_constant__ BwdJobs list, float* __restrict__ partial) {
+  constexpr int TEAM = D / 8, ROWS = kQkvThreads / TEAM;
+  constexpr int GV = sizeof(TG) / 2, XV = sizeof(TI) / 2, AHEAD = kBwdQueue / (GV + XV);      // 16-byte pieces of a row of dy, of x
   grid_enter();
-  __shared__ float red[2][ROWS][D];
+  extern __shared__ __align__(16) unsigned char qkv_smem[];
+  uint4* const queue = reinterpret_cast<uint4*>(qkv_smem) + threadIdx.x;      // [AHEAD][GV + XV][thread]
   const int l = threadIdx.x % TEAM, slot = threadIdx.x / TEAM;
-  const int h_lo = blockIdx.z * a.per_cta, h_hi = h_lo + a.per_cta;
-  float dw[2][8];
+  // batch entry and token of a tile (a row behind the last one repeats it)
+  struct Place { int b, tok; bool valid; };
+  auto place = [&](int at) {
+    const int b = at / a.tiles, row = (at - b * a.tiles) * ROWS + slot;
+    return Place{b, min(row, a.tokens - 1), row < a.tokens};
+  };
+  {
+    const int side = (int)blockIdx.x < list.ctas[0] ? 0 : 1, first = (int)blockIdx.x - (side > 0 ? list.ctas[0] : 0);
+    const int stride = list.ctas[side], per = list.per[side], jobs = list.jobs[side];
+    const HeadsArg g = a.x[side], y = a.y[side], x = fwd.v[side];
+    const bool norm = a.norm;
+    float2 w[4], dw[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) dw[0][i] = dw[1][i] = 0.f;
-  for (int job = blockIdx.x; job < a.jobs; job += gridDim.x) {
-    const int b = job / a.tiles, tile = job - b * a.tiles;
-    const int row = tile * ROWS + slot;
-    const bool valid = row < a.tokens;
-    const int tok = min(row, a.tokens - 1);
-    Turn<D, HALVES> turn;
-    turn.init(a.turn, b, tok, l);
-    int base = 0;
+    for (int i = 0; i < 4; ++i) {
+      dw[i] = make_float2(0.f, 0.f);
+      w[i] = norm && a.w[side] != nullptr ? make_float2(a.w[side][l * 8 + 2 * i], a.w[side][l * 8 + 2 * i + 1]) : make_float2(1.f, 1.f);
+    }
+    // the queue's end: job, head and place of the next row to ask for
+    int ask_job = first, ask_h = 0, ask_hi = 0;
+    const TG* ask_g = nullptr;
+    const TI* ask_x = nullptr;
+    auto ask = [&](int s) {
+      if (ask_h == ask_hi && ask_job < jobs) {
+        const int group = ask_job / a.jobs, lo = group * per;
+        const Place at = place(ask_job - group * a.jobs);
+        ask_job += stride;
+        ask_h = lo;
+        ask_hi = min(lo + per, g.heads);
+        ask_g = reinterpret_cast<const TG*>(g.p) + at.b * g.sb + at.tok * g.st + lo * g.sh + l * 8;
+        if (norm) ask_x = reinterpret_cast<const TI*>(x.p) + at.b * x.sb + at.tok * x.st + lo * x.sh + l * 8;
+      }
+      if (ask_h < ask_hi) {
+        uint4* to = queue + s * (GV + XV) * kQkvThreads;
 #pragma unroll
-    for (int seg = 0; seg < 3; ++seg) {
-      const HeadsArg g = a.x[seg], y = a.y[seg];
-      const int lo = max(h_lo - base, 0), hi = min(h_hi - base, g.heads);
-      base += g.heads;
-      if (lo >= hi) continue;
-      const bool norm = a.norm && seg < 2;
-      const TG* gp = reinterpret_cast<const TG*>(g.p) + b * g.sb + tok * g.st + l * 8;
-      TO* yp = reinterpret_cast<TO*>(y.p) + b * y.sb + tok * y.st + l * 8;
-      const HeadsArg x = fwd.v[seg & 1];
-      const TI* xp = reinterpret_cast<const TI*>(x.p) + b * x.sb + tok * x.st + l * 8;
-      float w[8];
+        for (int v = 0; v < GV; ++v) copy_async(to + v * kQkvThreads, reinterpret_cast<const uint4*>(ask_g) + v);
+        ask_g += g.sh;
+        if (norm) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = norm && a.w[seg & 1] != nullptr ? a.w[seg & 1][l * 8 + i] : 1.f;
-      Raw8<TG> g_next[U];
-      Raw8<TI> x_next[U];
-      auto fetch = [&](int h) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          g_next[u].load(gp + min(h + u, hi - 1) * g.sh);
-          if (norm) x_next[u].load(xp + min(h + u, hi - 1) * x.sh);
+          for (int v = 0; v < XV; ++v) copy_async(to + (GV + v) * kQkvThreads, reinterpret_cast<const uint4*>(ask_x) + v);
+          ask_x += x.sh;
         }
-      };
-      fetch(lo);
-      for (int h = lo; h < hi; h += U) {
-        // (the next heads' rows are on their way while these are computed)
-        Raw8<TG> gr[U];
-        Raw8<TI> xr[U];
+        ++ask_h;
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          gr[u] = g_next[u];
-          xr[u] = x_next[u];
-        }
-        if (h + U < hi) fetch(h + U);
+    for (int s = 0; s < AHEAD - 1; ++s) ask(s);
+    int s = 0;
+    for (int job = first; job < jobs; job += stride) {
+      const int group = job / a.jobs, lo = group * per, hi = min(lo + per, g.heads);
+      const Place at = place(job - group * a.jobs);
+      Turn<D, HALVES> turn;
+      turn.init(a.turn, at.b, at.tok, l);
+      TO* yp = reinterpret_cast<TO*>(y.p) + at.b * y.sb + at.tok * y.st + lo * y.sh + l * 8;
+      for (int h = lo; h < hi; ++h, yp += y.sh) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 2) : "memory");
+        const uint4* from = queue + s * (GV + XV) * kQkvThreads;
+        Raw8<TG> gr;
+        gr.load(from, kQkvThreads);
+        float f[8];
+        gr.get(f);
+        turn.apply(f);
+        if (norm) {
+          Raw8<TI> xr;
+          xr.load(from + GV * kQkvThreads, kQkvThreads);
+          float xf[8];
+          xr.get(xf);
+          // (two channels an instruction: 16 warps' issue slots are the next bound behind memory)
+          float2 ss = make_float2(0.f, 0.f), dot = ss;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          float f[8];
-          gr[u].get(f);
-          if (seg < 2) turn.apply(f);
-          if (norm) {
-            float xf[8], ss = 0.f, dot = 0.f;
-            xr[u].get(xf);
-            const bool counts = valid && h + u < hi;
-            float g0[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              g0[i] = f[i];
-              f[i] *= w[i];
-              ss += xf[i] * xf[i];
-              dot += f[i] * xf[i];
-            }
-            ss = team_sum<TEAM>(ss);
-            dot = team_sum<TEAM>(dot);
-            const float r = rsqrtf(ss * (1.f / D) + a.eps);
-            const float m = dot * (1.f / D) * r * r * r;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              if (counts) dw[seg & 1][i] += g0[i] * (xf[i] * r);
-              f[i] = r * f[i] - xf[i] * m;
-            }
+          for (int i = 0; i < 4; ++i) {
+            const float2 x2 = make_float2(xf[2 * i], xf[2 * i + 1]), f2 = make_float2(f[2 * i], f[2 * i + 1]);
+            ss = __ffma2_rn(x2, x2, ss);
+            dot = __ffma2_rn(__fmul2_rn(f2, w[i]), x2, dot);
           }
-          if (valid && h + u < hi) store8(yp + (h + u) * y.sh, f);
+          float2 sums = make_float2(ss.x + ss.y, dot.x + dot.y);
+#pragma unroll
+          for (int o = TEAM / 2; o > 0; o >>= 1)
+            sums = __fadd2_rn(sums, make_float2(__shfl_xor_sync(0xffffffffu, sums.x, o), __shfl_xor_sync(0xffffffffu, sums.y, o)));
+          const float r = rsqrtf(sums.x * (1.f / D) + a.eps), m = sums.y * (-1.f / D) * r * r * r;
+          const float2 r2 = make_float2(r, r), m2 = make_float2(m, m);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 x2 = make_float2(xf[2 * i], xf[2 * i + 1]), fr = __fmul2_rn(make_float2(f[2 * i], f[2 * i + 1]), r2);
+            if (at.valid) dw[i] = __ffma2_rn(fr, x2, dw[i]);
+            const float2 o = __ffma2_rn(x2, m2, __fmul2_rn(fr, w[i]));
+            f[2 * i] = o.x;
+            f[2 * i + 1] = o.y;
+          }
         }
+        if (at.valid) store8(yp, f);
+        ask(s == 0 ? AHEAD - 1 : s - 1);      // (the place that was read last time)
+        if (++s == AHEAD) s = 0;
+      }
+    }
+    if (norm) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncthreads();
+      float2* red = reinterpret_cast<float2*>(qkv_smem);      // [ROWS][D / 2]
+#pragma unroll
+      for (int i = 0; i < 4; ++i) red[slot * (D / 2) + l * 4 + i] = dw[i];
+      __syncthreads();
+      for (int i = threadIdx.x; i < D; i += kQkvThreads) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) sum += reinterpret_cast<const float*>(red)[r * D + i];
+        partial[(size_t)blockIdx.x * D + i] = sum;
       }
     }
   }
-  if (!a.norm) return;
+  const HeadsArg g = a.x[2], y = a.y[2];
+  if (g.heads == 0) return;
+  for (int job = blockIdx.x; job < a.jobs; job += gridDim.x) {
+    const Place at = place(job);
+    const TG* gp = reinterpret_cast<const TG*>(g.p) + at.b * g.sb + at.tok * g.st + l * 8;
+    TO* yp = reinterpret_cast<TO*>(y.p) + at.b * y.sb + at.tok * y.st + l * 8;
+    for (int h = 0; h < g.heads; h += 4) {
+      Raw8<TG> gr[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    red[0][slot][l * 8 + i] = dw[0][i];
-    red[1][slot][l * 8 + i] = dw[1][i];
-  }
-  __syncthreads();
-  const size_t cta = (size_t)blockIdx.z * gridDim.x + blockIdx.x;
-  for (int i = threadIdx.x; i < 2 * D; i += kQkvThreads) {
-    float sum = 0.f;
-    for (int r = 0; r < ROWS; ++r) sum += red[i / D][r][i % D];
-    partial[cta * (2 * D) + i] = sum;
+      for (int u = 0; u < 4; ++u) gr[u].load(gp + min(h + u, g.heads - 1) * g.sh);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float f[8];
+        gr[u].get(f);
+        if (at.valid && h + u < g.heads) store8(yp + (h + u) * y.sh, f);
+      }
+    }
   }
 }
 
-// Sums of the CTAs' partial sums in a fixed order: 32 columns a CTA, every 32nd part a warp row.
-__global__ void __launch_bounds__(1024) qkv_bwd_reduce_kernel(const float* partial, int parts, int D, float* __restrict__ dwq,
+// Sums of the CTAs' partial sums in a fixed order: 32 columns a CTA, every 32nd part a warp row.  grid (columns / 32, 2: q, k)
+__global__ void __launch_bounds__(1024) qkv_bwd_reduce_kernel(const float* partial, int q_ctas, int qk_ctas, int D, float* __restrict__ dwq,
                                                               float* __restrict__ dwk) {
   grid_enter();
   __shared__ float red[32][33];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), first = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, col = blockIdx.x * 32 + lane, first = threadIdx.x >> 5;
+  const int lo = blockIdx.y == 0 ? 0 : q_ctas, hi = blockIdx.y == 0 ? q_ctas : qk_ctas;
   float sum = 0.f;
-  for (int p = first; p < parts; p += 32) sum += partial[(size_t)p * (2 * D) + col];
-  red[first][threadIdx.x & 31] = sum;
+#pragma unroll 8
+  for (int p = lo + first; p < hi; p += 32) sum += partial[(size_t)p * D + col];
+  red[first][lane] = sum;
   __syncthreads();
   if (first == 0) {
     float total = 0.f;
-    for (int r = 0; r < 32; ++r) total += red[r][threadIdx.x];
-    float* out = col < D ? dwq : dwk;
-    if (out != nullptr) out[col < D ? col : col - D] = total;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) total += red[r][lane];
+    float* out = blockIdx.y == 0 ? dwq : dwk;
+    if (out != nullptr) out[col] = total;
   }
 }
 
@@ -314,7 +371,7 @@ int heads_per_cta(int tiles, int heads, int unit, int sms) {
 
 }  // namespace
 
-size_t qkv_bwd_workspace_bytes(int D) { return (size_t)kQkvParts * 2 * D * sizeof(float); }
+size_t qkv_bwd_workspace_bytes(int D) { return (size_t)kQkvParts * D * sizeof(float); }
 
 cudaError_t launch_qkv_fwd(QkvArgs a, int D, int batch, int in_f32, int out_f32, bool halves, cudaStream_t st) {
   const int rows = kQkvThreads / (D / 8), heads = a.x[0].heads + a.x[1].heads + a.x[2].heads;
@@ -337,29 +394,59 @@ cudaError_t launch_qkv_fwd(QkvArgs a, int D, int batch, int in_f32, int out_f32,
 
 cudaError_t launch_qkv_bwd(QkvArgs a, const HeadsPair& fwd, int D, int batch, int x_f32, int g_f32, int out_f32, bool halves,
                            float* dwq, float* dwk, float* partial, cudaStream_t st) {
-  const int rows = kQkvThreads / (D / 8), heads = a.x[0].heads + a.x[1].heads + a.x[2].heads;
+  const int rows = kQkvThreads / (D / 8);
   int sms = 0;
   cudaError_t e;
   if ((e = sm_count(&sms)) != cudaSuccess) return e;
   a.tiles = (a.tokens + rows - 1) / rows;
   a.jobs = a.tiles * batch;
-  a.per_cta = heads_per_cta(a.jobs, heads, 2, sms);
-  const int groups = (heads + a.per_cta - 1) / a.per_cta;
-  int ctas = a.jobs;
-  if (ctas > kQkvParts / groups) ctas = kQkvParts / groups;
-  const dim3 grid(ctas, 1, groups);
+  // CTAs for q and for k by what a tile of theirs costs: its heads and the sines and cosines of its tokens, about two heads' worth (by the heads alone, 40 q heads on one k
+  // head waited for the k CTAs, 550 us instead of 290).  Heads go in groups where that makes the rounds of jobs even.
+  BwdJobs list = {};
+  const int at_once = (halves ? 3 : 4) * sms, ctas = at_once < kQkvParts ? at_once : kQkvParts;
+  const int nq = a.x[0].heads, nk = a.x[1].heads;
+  int share[2] = {nq == 0 ? 0 : ctas, nk == 0 ? 0 : ctas};
+  if (nq > 0 && nk > 0) {
+    share[0] = (int)((long long)ctas * (nq + 2) / (nq + nk + 4));
+    share[1] = ctas - share[0];
+  }
+  for (int i = 0; i < 2; ++i) {
+    const int n = a.x[i].heads;
+    if (n == 0) continue;
+    long long least = 0;
+    int groups = 1;
+    for (int g = 1; g <= 16 && g <= n; ++g) {
+      const int per = (n + g - 1) / g, of = (n + per - 1) / per;
+      const long long cost = ((long long)a.jobs * of + share[i] - 1) / share[i] * (2 + per);
+      if (g == 1 || cost < least) {
+        least = cost;
+        list.per[i] = per;
+        groups = of;
+      }
+    }
+    const long long jobs = (long long)a.jobs * groups;
+    if (jobs > 0x7fffffff - kQkvParts) return cudaErrorInvalidValue;
+    list.jobs[i] = (int)jobs;
+    list.ctas[i] = jobs < share[i] ? (int)jobs : share[i];
+  }
+  int grid = list.ctas[0] + list.ctas[1];
+  if (grid == 0) {      // (v alone: CTAs whose list is empty)
+    grid = a.jobs < ctas ? a.jobs : ctas;
+    list.ctas[0] = grid;
+  }
+  const size_t smem = (size_t)kBwdQueue * kQkvThreads * 16;
   auto go = [&](auto tx, auto tg, auto to) {
     using TX = decltype(tx);
     using TG = decltype(tg);
     using TO = decltype(to);
-    if (D == 128) return halves ? launch_kernel(qkv_bwd_kernel<128, TX, TG, TO, true>, grid, kQkvThreads, 0, st, a, fwd, partial)
-                                : launch_kernel(qkv_bwd_kernel<128, TX, TG, TO, false>, grid, kQkvThreads, 0, st, a, fwd, partial);
-    return halves ? launch_kernel(qkv_bwd_kernel<64, TX, TG, TO, true>, grid, kQkvThreads, 0, st, a, fwd, partial)
-                  : launch_kernel(qkv_bwd_kernel<64, TX, TG, TO, false>, grid, kQkvThreads, 0, st, a, fwd, partial);
+    if (D == 128) return halves ? launch_kernel(qkv_bwd_kernel<128, TX, TG, TO, true>, grid, kQkvThreads, smem, st, a, fwd, list, partial)
+                                : launch_kernel(qkv_bwd_kernel<128, TX, TG, TO, false>, grid, kQkvThreads, smem, st, a, fwd, list, partial);
+    return halves ? launch_kernel(qkv_bwd_kernel<64, TX, TG, TO, true>, grid, kQkvThreads, smem, st, a, fwd, list, partial)
+                  : launch_kernel(qkv_bwd_kernel<64, TX, TG, TO, false>, grid, kQkvThreads, smem, st, a, fwd, list, partial);
   };
   e = by_types(g_f32, out_f32, [&](auto tg, auto to) { return x_f32 ? go(float(), tg, to) : go(bf16(), tg, to); });
   if (e != cudaSuccess || !a.norm) return e;
-  return launch_kernel(qkv_bwd_reduce_kernel, 2 * D / 32, 1024, 0, st, partial, ctas * groups, D, dwq, dwk);
+  return launch_kernel(qkv_bwd_reduce_kernel, dim3(D / 32, 2), 1024, 0, st, partial, list.ctas[0], list.ctas[0] + list.ctas[1], D, dwq, dwk);
 }
 
 }  // namespace vsa2

@@ -335,3 +335,14 @@ def test_another_stream_and_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(y, want))
+
+
+def test_weights_at_any_fp32_address():
+    p = Problem(1, 3, 3, (2, 3, 4), 0, 128, (44, 42, 42), vb.ROPE_PAIRS, seed=13)
+    want, (dx, dw) = p.forward(), p.backward()
+    room = torch.empty(300, device="cuda")
+    for i, at in enumerate((1, 131)):
+        room[at:at + 128] = p.w[i]
+        p.w[i] = room[at:at + 128]
+    got, (dx2, dw2) = p.forward(), p.backward()
+    assert all(torch.equal(a, b) for a, b in zip((*want, *dx, *dw), (*got, *dx2, *dw2)))
