@@ -13,11 +13,8 @@ namespace {
 
 constexpr int kQzThreads = 256;
 
-// exponent + 127 from the bits of max|x|: 448 = 1.75 * 2^8
-__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
-  const int e = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return (uint32_t)max(e, 0);      // (at most 254 - 8 + 1)
-}
+// exponent + 127 from the bits of max|x|: 448 = 1.75 * 2^8, so a fraction above 0.75 carries (at most 254 - 8 + 1)
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) { return (uint32_t)max((int)((top + 0x1fffffu) >> 23) - 8, 0); }
 __device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 __device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
@@ -171,16 +168,17 @@ struct TileShared {
 };
 
 // a tile whose values are in the threads' registers: both forms, or either
+// (`tops`: largest magnitudes of the thread's rows where all is finite)
 template <bool CHECK, bool F32>
-__device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], TileShared& sh, int rows, int cols, int squares, const Fp8Arg& out, const Fp8Arg& out_t) {
+__device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint32_t (&tops)[8], TileShared& sh, int rows, int cols, int squares, const Fp8Arg& out, const Fp8Arg& out_t) {
   const int l = threadIdx.x & 15, team = threadIdx.x >> 4, tid = threadIdx.x;
   const int c0 = blockIdx.y * 128, r0 = blockIdx.x * 128;
   const int blocks = (cols + 127) / 128, blocks_t = (rows + 127) / 128;
-  auto top_of = [](const Oct<F32>& v) { return CHECK ? finite_top<F32>(v) : v.top(); };
+  auto top_of = [&](int i) { return CHECK ? finite_top<F32>(o[i]) : F32 ? o[i].top() : tops[i]; };      // (fp32: no registers to keep them in)
   uint32_t top_all = 0;
   if (squares) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top_all = max(top_all, top_of(o[i]));
+    for (int i = 0; i < 8; ++i) top_all = max(top_all, top_of(i));
     top_all = __reduce_max_sync(0xffffffffu, top_all);
     if ((tid & 31) == 0) sh.tops[tid >> 5] = top_all;
     __syncthreads();
@@ -189,7 +187,7 @@ __device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], TileShared
   if (out.values != nullptr) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t s = scale_byte(squares ? top_all : team_max(top_of(o[i])));
+      const uint32_t s = scale_byte(squares ? top_all : team_max(top_of(i)));
       const int row = r0 + team * 8 + i;
       if (row < rows) {
         put_oct<CHECK, F32>(out.values + row * out.ld, c0 + l * 8, cols, o[i], inverse_scale(s));
@@ -257,13 +255,13 @@ __device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], TileShared
 // as bytes: a thread writes the 8 bytes that its rows give a column; the 8-byte places of a column are exchanged by column group
 // so that neither side meets a bank twice.  grid (row tiles, column tiles)
 template <bool F32, bool VEC>
-__global__ void __launch_bounds__(kQzThreads) fp8_tile_kernel(const void* x, int rows, int cols, long long ld, int squares, Fp8Arg out,
+__global__ void __launch_bounds__(kQzThreads, F32 ? 2 : 4) fp8_tile_kernel(const void* x, int rows, int cols, long long ld, int squares, Fp8Arg out,
                                                               Fp8Arg out_t) {
   grid_enter();
   __shared__ __align__(16) TileShared sh;
   const int l = threadIdx.x & 15, team = threadIdx.x >> 4;
   Oct<F32> o[8];
-  uint32_t top = 0;
+  uint32_t tops[8], top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int row = blockIdx.x * 128 + team * 8 + i;
@@ -271,9 +269,12 @@ __global__ void __launch_bounds__(kQzThreads) fp8_tile_kernel(const void* x, int
     else o[i].zero();
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, o[i].top());
-  if (__syncthreads_or(top >= kInf)) quantize_tile<true, F32>(o, sh, rows, cols, squares, out, out_t);
-  else quantize_tile<false, F32>(o, sh, rows, cols, squares, out, out_t);
+  for (int i = 0; i < 8; ++i) {
+    tops[i] = o[i].top();
+    top = max(top, tops[i]);
+  }
+  if (__syncthreads_or(top >= kInf)) quantize_tile<true, F32>(o, tops, sh, rows, cols, squares, out, out_t);
+  else quantize_tile<false, F32>(o, tops, sh, rows, cols, squares, out, out_t);
 }
 
 }  // namespace
