@@ -1,0 +1,95 @@
+"""One self-attention layer from its hidden states on: the library's calls in the order a model makes them.
+
+    x [B, L + Lt, C] -> 8-bit projection -> norms of q and k, rotary positions, heads -> router, attention with the gate projected from x -> o
+
+and back to the gradients of x and of all weights.  The projection's three products (forward, dX, dW) run on e4m3 values with a scale for each 128 of
+them: weights are quantised once per update in 128 x 128 blocks (both forms), hidden states and gradients as they come, along the dimension that is
+summed over.  Master weights stay with the caller.  torch is used for memory, and to add the two parts of dX.
+"""
+from __future__ import annotations
+
+from . import binding as vb
+
+
+class Vsa2Layer:
+    """params: the attention's problem (make_params; out_dtype BF16); hidden: channels of x; rope_channels: channels of a head that turn with (t, h, w).
+
+    set_weights takes w_qkv [(Hq + 2 Hkv) D, C] bf16 (rows: q's heads, k's, v's), w_g [C, Hq] bf16 and the norms' weights fp32 [D]; forward keeps what backward
+    needs until the next forward."""
+
+    def __init__(self, params, hidden, rope_channels, theta=1e4, scale=1.0, layout=vb.ROPE_PAIRS, eps=1e-6, device="cuda"):
+        import torch
+        if params.out_dtype != vb.BF16:
+            raise ValueError("the layer's attention gives bf16 (out_dtype BF16)")
+        self.torch, self.p, self.hidden, self.eps, self.device = torch, params, hidden, eps, torch.device(device)
+        p = params
+        self.rope = vb.vsa2_rope_plan(p.head_dim, rope_channels, theta=theta, scale=scale, layout=layout)
+        self.attn = vb.Vsa2Attention(p, device)
+        self.grid, self.tokens = (p.grid_t, p.grid_h, p.grid_w), int(self.attn.sizes.tokens_per_head)
+        self.rows, self.width = p.batch * self.tokens, (p.heads_q + 2 * p.heads_kv) * p.head_dim
+        self.w, self.w_t = vb.Fp8.empty(self.width, hidden, device), vb.Fp8.empty(hidden, self.width, device)
+        need = max(vb.vsa2_fp8_matmul_workspace_bytes(*s) for s in ((self.rows, self.width, hidden), (self.rows, hidden, self.width),
+                                                                    (self.width, hidden, self.rows)))
+        self.ws_matmul = torch.zeros(need, dtype=torch.uint8, device=device)
+        self.ws_qkv = torch.empty(vb.vsa2_qkv_bwd_workspace_bytes(p.head_dim), dtype=torch.uint8, device=device)
+        self.ws_gate = torch.empty(max(256, vb.vsa2_gate_bwd_workspace_bytes(p, hidden)), dtype=torch.uint8, device=device)
+        self.saved = None
+
+    def set_weights(self, w_qkv, w_g, q_weight, k_weight):
+        vb.vsa2_fp8_quantize(w_qkv, self.w, self.w_t, squares=True)
+        self.w_g, self.q_weight, self.k_weight = w_g, q_weight, k_weight
+
+    def _heads(self, packed):
+        """q, k, v as [B, heads, tokens, D] views of the projection's rows."""
+        p = self.p
+        v = packed.view(p.batch, self.tokens, p.heads_q + 2 * p.heads_kv, p.head_dim).transpose(1, 2)
+        return v[:, :p.heads_q], v[:, p.heads_q:p.heads_q + p.heads_kv], v[:, p.heads_q + p.heads_kv:]
+
+    def _empty(self, *shape, dtype=None):
+        return self.torch.empty(*shape, dtype=dtype or self.torch.bfloat16, device=self.device)
+
+    def forward(self, x):
+        """x [B, L + Lt, C] bf16, contiguous -> o [B, Hq, L + Lt, D] bf16."""
+        p, torch = self.p, self.torch
+        if tuple(x.shape) != (p.batch, self.tokens, self.hidden) or not x.is_contiguous():
+            raise ValueError(f"expected contiguous hidden states {(p.batch, self.tokens, self.hidden)}")
+        a = vb.Fp8.empty(self.rows, self.hidden, self.device)
+        vb.vsa2_fp8_quantize(x.view(self.rows, self.hidden), a)
+        packed = self._empty(self.rows, self.width)
+        vb.vsa2_fp8_matmul(a, self.w, packed, self.ws_matmul)
+        q, k, v = (self._empty(p.batch, h, self.tokens, p.head_dim) for h in (p.heads_q, p.heads_kv, p.heads_kv))
+        vb.vsa2_qkv_fwd(self.rope, self._heads(packed), (q, k, v), self.q_weight, self.k_weight, eps=self.eps, grid=self.grid)
+        video = x[:, :self.attn.sizes.seq_len].contiguous()
+        gate = self._empty(p.batch, p.heads_q, self.attn.sizes.seq_len, dtype=torch.float32)
+        vb.vsa2_gate_fwd(p, self.hidden, video, self.w_g, gate)
+        self.attn.route(q, k)
+        o, lse = self.attn.forward(q, k, v, gate)
+        self.saved = (x, video, packed, q, k, v, gate, o, lse)
+        return o
+
+    def backward(self, d_o):
+        """d_o [B, Hq, L + Lt, D] bf16 -> dict of dx [B, L + Lt, C] bf16 and, in fp32, dw_qkv, dw_g, dq_weight, dk_weight."""
+        p, torch = self.p, self.torch
+        x, video, packed, q, k, v, gate, o, lse = self.saved
+        dq, dk, dv, dgate = self.attn.backward(q, k, v, gate, o, lse, d_o)
+        d_packed = torch.empty_like(packed)
+        dqw, dkw = (self._empty(p.head_dim, dtype=torch.float32) for _ in range(2))
+        vb.vsa2_qkv_bwd(self.rope, self._heads(packed), (dq, dk, dv), self._heads(d_packed), self.q_weight, self.k_weight, dqw, dkw, self.ws_qkv,
+                        eps=self.eps, grid=self.grid)
+        g, g_t, x_t = (vb.Fp8.empty(*s, self.device) for s in ((self.rows, self.width), (self.width, self.rows), (self.hidden, self.rows)))
+        vb.vsa2_fp8_quantize(d_packed, g, g_t)
+        vb.vsa2_fp8_quantize(x.view(self.rows, self.hidden), None, x_t)
+        dx = self._empty(p.batch, self.tokens, self.hidden)
+        vb.vsa2_fp8_matmul(g, self.w_t, dx.view(self.rows, self.hidden), self.ws_matmul)
+        dw = self._empty(self.width, self.hidden, dtype=torch.float32)
+        vb.vsa2_fp8_matmul(g_t, x_t, dw, self.ws_matmul)
+        dw_g, dx_gate = self._empty(self.hidden, p.heads_q, dtype=torch.float32), torch.empty_like(video)
+        vb.vsa2_gate_bwd(p, self.hidden, video, self.w_g, gate, dgate, dw_g, dx_gate, self.ws_gate)
+        dx[:, :video.shape[1]] += dx_gate
+        return {"dx": dx, "dw_qkv": dw, "dw_g": dw_g, "dq_weight": dqw, "dk_weight": dkw}
+
+    def check_status(self):
+        self.attn.check_status()
+        code = vb.vsa2_device_status(self.ws_matmul)
+        if code != vb.OK:
+            raise vb.Vsa2Error(code, "device status after the projection")
