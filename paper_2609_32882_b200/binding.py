@@ -355,12 +355,14 @@ def _dtype(t):
 
 def _view(t):
     """The fields of vsa2_heads of a CUDA tensor [batch, heads, tokens, D], any strides but 1 for the channels."""
-    shape, strides = t.shape, t.stride()
-    if len(shape) != 4 or not t.is_cuda:
+    if t.dim() != 4 or not t.is_cuda:
         raise ValueError("expected a CUDA tensor [batch, heads, tokens, channels]")
-    if strides[3] != 1:
+    sb, sh, st, last = t.stride()
+    if last != 1:
         raise ValueError("the channels of a row must be contiguous")
-    return (t.data_ptr(), strides[0], strides[1], strides[2], *shape, _dtype(t), 0)
+    code = _DTYPES.get(t.dtype)
+    b, h, n, c = t.shape
+    return t.data_ptr(), sb, sh, st, b, h, n, c, _dtype(t) if code is None else code, 0
 
 
 def _views(tensors):
@@ -396,7 +398,7 @@ def _place(grid, first, positions, batch, tokens):
 def _weight(w, channels, name):
     if w is None:
         return 0
-    if w.dtype != _torch().float32 or w.numel() != channels:
+    if _DTYPES.get(w.dtype) != F32 and _dtype(w) != F32 or w.numel() != channels:
         raise ValueError(f"{name} must be fp32 with {channels} elements")
     return _ptr(w)
 
@@ -446,11 +448,11 @@ class Fp8:
     __slots__ = ("values", "scales")
 
     def __init__(self, values, scales):
-        torch = _torch()
+        torch = _TORCH or _torch()
         rows, cols = values.shape
-        if values.dtype != torch.float8_e4m3fn or (cols > 1 and values.stride(1) != 1):
+        if values.dtype is not torch.float8_e4m3fn or (cols > 1 and values.stride(1) != 1):
             raise ValueError("values must be float8_e4m3fn [rows, cols] with contiguous rows")
-        if scales.dtype != torch.uint8 or scales.shape != (-(-cols // 512), rows, 4):
+        if scales.dtype is not torch.uint8 or scales.shape != (-(-cols // 512), rows, 4):
             raise ValueError(f"scales must be uint8 {(-(-cols // 512), rows, 4)}, got {tuple(scales.shape)}")
         self.values, self.scales = values, scales
 

@@ -19,7 +19,9 @@ namespace vsa2 {
 namespace {
 
 constexpr int kQkvThreads = 256;
-constexpr int kBwdQueue = 12;        // 16-byte pieces that a thread of the backward has in its queue (48 KB a CTA)
+// Rows of `pieces` times 16 bytes that a thread of the backward has in its queue.  720p, 20 heads: two 558 us, three 487, four 536, six 513; with halves as pairs, whose
+// registers leave room for three CTAs per SM instead of four, 480p, 24 heads: three 276, four 262
+__host__ __device__ constexpr int bwd_ahead(int pieces, bool halves) { return pieces > 2 ? 2 : halves ? 4 : 3; }
 constexpr int kQkvParts = 1024;      // most CTAs of the backward, each with its own partial sums of a weight's gradient
 
 template <typename T> struct Raw8;      // eight channels as they lie in memory
@@ -199,7 +201,7 @@ template <int D, typename TI, typename TG, typename TO, bool HALVES>
 __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(const __grid_constant__ QkvArgs a, const __grid_constant__ HeadsPair fwd,
                                                                         const __grid_constant__ BwdJobs list, float* __restrict__ partial) {
   constexpr int TEAM = D / 8, ROWS = kQkvThreads / TEAM;
-  constexpr int GV = sizeof(TG) / 2, XV = sizeof(TI) / 2, AHEAD = kBwdQueue / (GV + XV);      // 16-byte pieces of a row of dy, of x
+  constexpr int GV = sizeof(TG) / 2, XV = sizeof(TI) / 2, AHEAD = bwd_ahead(GV + XV, HALVES);      // 16-byte pieces of a row of dy, of x
   grid_enter();
   extern __shared__ __align__(16) unsigned char qkv_smem[];
   uint4* const queue = reinterpret_cast<uint4*>(qkv_smem) + threadIdx.x;      // [AHEAD][GV + XV][thread]
@@ -400,14 +402,14 @@ cudaError_t launch_qkv_bwd(QkvArgs a, const HeadsPair& fwd, int D, int batch, in
   if ((e = sm_count(&sms)) != cudaSuccess) return e;
   a.tiles = (a.tokens + rows - 1) / rows;
   a.jobs = a.tiles * batch;
-  // CTAs for q and for k by what a tile of theirs costs: its heads and the sines and cosines of its tokens, about two heads' worth (by the heads alone, 40 q heads on one k
-  // head waited for the k CTAs, 550 us instead of 290).  Heads go in groups where that makes the rounds of jobs even.
+  // CTAs for q and for k by what a tile of theirs costs: its heads and the sines and cosines of its tokens, about three heads' worth (by the heads alone 40 q heads on one k
+  // head waited for the k CTAs, 550 us; one head's worth 315, two 241, three 218).  Heads go in groups where that makes the rounds of jobs even.
   BwdJobs list = {};
   const int at_once = (halves ? 3 : 4) * sms, ctas = at_once < kQkvParts ? at_once : kQkvParts;
   const int nq = a.x[0].heads, nk = a.x[1].heads;
   int share[2] = {nq == 0 ? 0 : ctas, nk == 0 ? 0 : ctas};
   if (nq > 0 && nk > 0) {
-    share[0] = (int)((long long)ctas * (nq + 2) / (nq + nk + 4));
+    share[0] = (int)((long long)ctas * (nq + 3) / (nq + nk + 6));
     share[1] = ctas - share[0];
   }
   for (int i = 0; i < 2; ++i) {
@@ -434,7 +436,9 @@ cudaError_t launch_qkv_bwd(QkvArgs a, const HeadsPair& fwd, int D, int batch, in
     grid = a.jobs < ctas ? a.jobs : ctas;
     list.ctas[0] = grid;
   }
-  const size_t smem = (size_t)kBwdQueue * kQkvThreads * 16;
+  const int pieces = (g_f32 ? 2 : 1) + (x_f32 ? 2 : 1);
+  size_t smem = (size_t)bwd_ahead(pieces, halves) * pieces * kQkvThreads * 16;
+  if (smem < kQkvThreads * 8 * sizeof(float)) smem = kQkvThreads * 8 * sizeof(float);      // (the CTA's sums)
   auto go = [&](auto tx, auto tg, auto to) {
     using TX = decltype(tx);
     using TG = decltype(tg);
