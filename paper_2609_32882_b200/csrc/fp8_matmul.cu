@@ -7,7 +7,7 @@
 // B's rows (n, the weights of a projection) are the 128 rows of a CTA's tile, A's rows (m, the tokens) its NT columns: few tokens take a narrow tile under weights that
 // stream through.  Many take 224 columns on a pair of SMs (cta_group::2): 256 rows of B, each CTA fetches its half of B's rows and half of A's, 30 KB
 // for 2 x 128 x 224 x 128 multiply-adds, where a CTA alone fetches 45.  Persistent CTAs, one per SM: a producer warp (TMA), an issuer, a warp for the scales, two
-// groups of four for the epilogue; two accumulators in tensor memory, so that a tile's epilogue runs behind the next tile's products.
+// groups of four, half the columns each, for the epilogue; two accumulators in tensor memory, so that a tile's epilogue runs behind the next tile's products.
 //
 // What bounds it: with many tiles the power limit and the intake from L2 (8192 x 4096 x 4096: 51 bytes a cycle and SM, 600 cycles a block where the tensor cores need
 // 448); 75600 x 15360 x 5120 runs at 3.1 PFLOP/s and more, 1.9 times the library's bf16 product.  Tiles of 448 columns, both accumulators in one tile, need 27 % less
@@ -65,7 +65,7 @@ struct MmArgs {
 
 struct MmMisc {
   uint64_t full[kMmStagesMost], empty[kMmStagesMost], sc_full[kMmScaleSlots], sc_empty[kMmScaleSlots];
-  uint64_t d_full[2], d_empty[2], group[2], written[2];
+  uint64_t d_full[2], d_empty[2], group[2];
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -311,9 +311,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
     }
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&misc->d_full[s], 1);
-      tc::mbar_init(&misc->d_empty[s], rank == 0 ? 3 + PAIR : 4);
+      tc::mbar_init(&misc->d_empty[s], (NT > 32 ? 8 : 4) + (rank == 0 ? PAIR - 1 : 0));
       tc::mbar_init(&misc->group[s], 128);
-      tc::mbar_init(&misc->written[s], 128);
     }
     tc::fence_barrier_init();
     tc::prefetch_tmap(&tm_p);
@@ -447,19 +446,19 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
         }
       }
     } else if (warp >= 4) {
-      // ---------------------------------------------------------------- epilogue: four warps for each accumulator
-      const int quad = warp & 3, buf = (warp >> 2) - 1;
-      // Pieces of one item come to the two groups in turn, each adding to what the other has written: one after the other
-      const bool in_turn = a.chunk < a.kb;
-      uint32_t syncs = 0, turn = 0, tiles = 0;
+      // ---------------------------------------------------------------- epilogue: two groups of four warps, each half of the columns
+      const int quad = warp & 3, group = (warp >> 2) - 1;
+      constexpr int FIRST = (NT / 32 + 1) / 2, MOST = FIRST;      // pieces of 32 columns that are group 0's
+      const int piece0 = group == 0 ? 0 : FIRST, pieces = group == 0 ? FIRST : NT / 32 - FIRST;
+      uint32_t syncs = 0, tiles = 0;
+      if (pieces == 0) goto done;
       for (uint32_t seg = 0; w.advance(a); ++seg) {
-        if ((int)(seg & 1) != buf) continue;
-        const int first = (w.p * PAIR + rank) * 128, row = first + quad * 32 + lane, col = w.q * NT, cols = min(NT, a.q_rows - col);
-        VSA2_WAIT_PARKED(&misc->d_full[buf], turn & 1);
-        ++turn;
+        const uint32_t buf = seg & 1;
+        const int first = (w.p * PAIR + rank) * 128, row = first + quad * 32 + lane, col = w.q * NT + piece0 * 32;
+        const int cols = min(pieces * 32, a.q_rows - col);      // (0 or less: the tile ends before)
+        VSA2_WAIT_PARKED(&misc->d_full[buf], (seg >> 1) & 1);
         tc::tc_fence_after();
-        if (in_turn && seg > 0) VSA2_WAIT_PARKED(&misc->written[buf ^ 1], ((seg - 1) >> 1) & 1);
-        const uint32_t tmem = tmem_base + buf * 256 + ((uint32_t)(quad * 32) << 16);
+        const uint32_t tmem = tmem_base + buf * 256 + piece0 * 32 + ((uint32_t)(quad * 32) << 16);
         auto release = [&] {
           tc::tc_fence_before();
           __syncwarp();
@@ -468,18 +467,19 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
         if (sizeof(TO) == 2 && a.tensor_stores) {
           // bf16: all columns to registers first (the CTAs' stores come at the same time and take 5000 cycles), then in shared memory, turned unless SWAP, and out
           // by tensor copies that drop what lies outside C.  (Stored by the warps as they hold it, 64 bytes at a time, an accumulator took 13,000 cycles.)
-          uint32_t u[NT / 32][16];
+          uint32_t u[MOST][16];
 #pragma unroll
-          for (int i = 0; i < NT / 32; ++i) take_tile(tmem + 32 * i, u[i]);
+          for (int i = 0; i < MOST; ++i)
+            if (i < pieces) take_tile(tmem + 32 * i, u[i]);
           release();
 #pragma unroll
-          for (int i = 0; i < NT / 32; ++i) {
+          for (int i = 0; i < MOST; ++i) {
             if (32 * i >= cols) break;
-            unsigned char* tile = staging + (buf * 2 + (tiles & 1)) * kMmTileBytes;
+            unsigned char* tile = staging + (group * 2 + (tiles & 1)) * kMmTileBytes;
             stage_tile<SWAP>(tile, u[i], quad, lane);
             tc::fence_proxy_async_smem();
             if (quad == 0 && lane == 0) tc::bulk_store_wait_read();      // the tile before has been read: behind the barrier its place is free
-            VSA2_GROUP_SYNC(&misc->group[buf], syncs);
+            VSA2_GROUP_SYNC(&misc->group[group], syncs);
             if (quad == 0 && lane == 0) {
               if (SWAP) {
                 if (first < a.p_rows) tma_store_2d(&tm_c, tile, col + 32 * i, first);
@@ -501,16 +501,12 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
             load_columns(tmem + c0, v);
             if (row < a.p_rows) {
               TO* to = out + (long long)c0 * a.ldc;
-              if constexpr (sizeof(TO) == 4)      // (what has been written there for the blocks before)
+              if constexpr (sizeof(TO) == 4)      // (what this thread has written there for the blocks before)
                 if (w.kb0 > w.r0) add_column(to, a.ldc, cols - c0, v);
               put_column(to, a.ldc, cols - c0, v);
             }
           }
           release();
-        }
-        if (in_turn) {
-          __threadfence();
-          tc::mbar_arrive(&misc->written[buf]);
         }
       }
       if (sizeof(TO) == 2 && quad == 0 && lane == 0) tc::bulk_store_wait();

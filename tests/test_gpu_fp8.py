@@ -219,3 +219,16 @@ def test_graph_and_another_stream():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(c, want)
+
+
+def test_long_sums_in_pieces_and_in_ranges():
+    """fp32 results of more blocks of K than one accumulator sums, in few tiles (K in ranges) and in many (pieces added in place)."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    for m, n, k in ((300, 515, 20000), (5, 200, 30000), (1400, 2300, 17000), (100, 100, 33000)):
+        a, b = whole_numbers(gen, m, k, 0, 1), whole_numbers(gen, n, k, 0, 1)
+        want = (a.dequantize().double() @ b.dequantize().double().T).float()
+        ws = vb.fp8_matmul_workspace(m, n, k)
+        for dtype in (F, BF):
+            c = torch.full((m, n), float("nan"), dtype=dtype, device="cuda")
+            vb.vsa2_fp8_matmul(a, b, c, ws)
+            assert torch.equal(c, want.to(dtype))
