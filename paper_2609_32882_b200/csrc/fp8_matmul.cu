@@ -9,10 +9,11 @@
 // for 2 x 128 x 224 x 128 multiply-adds, where a CTA alone fetches 45.  Persistent CTAs, one per SM: a producer warp (TMA), an issuer, a warp for the scales, two
 // groups of four, half the columns each, for the epilogue; two accumulators in tensor memory, so that a tile's epilogue runs behind the next tile's products.
 //
-// What bounds it: with many tiles the power limit and the intake from L2 (8192 x 4096 x 4096: 51 bytes a cycle and SM, 600 cycles a block where the tensor cores need
-// 448); 75600 x 15360 x 5120 runs at 3.1 PFLOP/s and more, 1.9 times the library's bf16 product.  Tiles of 448 columns, both accumulators in one tile, need 27 % less
-// intake and were as fast at large sizes (20000 x 15360 x 5120 1028 us both ways), slower where rounds are few (4096^3 60 us instead of 52).  One row of A: the
-// weights' bytes.
+// What bounds it: in long runs the power limit, at which values of normal numbers draw a quarter more than small whole ones (75600 x 15360 x 5120: 4.6 - 4.8 ms, 2.5
+// PFLOP/s, against 3.7 ms and 3.2 PFLOP/s, twice the library's bf16 product); else the intake from L2 (8192 x 4096 x 4096 91 us: 51 bytes a cycle and SM, 600
+// cycles a block where the tensor cores need 448).  Tiles of 448 columns, both accumulators in one tile, need 27 % less intake and were as fast at large sizes (20000 x 15360 x
+// 5120 1028 us both ways), slower where rounds are few (4096^3 60 us instead of 52).  One row of A: the weights' bytes (15360 x 5120 16 us, 4.9 TB/s with the
+// launch); few tiles and short K: the launch, the first block's way from memory and the epilogue, 3 - 5 us.
 #include <cuda.h>
 
 #include "common.cuh"

@@ -3,7 +3,8 @@
 //   e = the least integer with max|x| <= 448 * 2^e over the block's finite values (448: the largest e4m3 value), at least -127
 //   value = x * 2^-e rounded to e4m3 (to nearest, ties to even); what is not finite becomes NaN
 // A power of two scales without rounding, so the 3 mantissa bits are all that is lost, and it is what the tensor cores multiply by themselves.
-// Both kernels are bound by memory: x read once, each form written once.
+// x is read once, each form written once.  Rows alone are bound by memory: 75600 x 5120 193 us (6.0 TB/s), 20000 x 5120 of fp32 77 us (6.6).  Both forms in one
+// reading are bound by instructions, about 70 % of the issue slots (a conversion for every value and form): 20000 x 5120 98 us (4.2 TB/s).
 #include "common.cuh"
 #include "heads.cuh"
 
