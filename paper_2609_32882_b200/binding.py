@@ -1,4 +1,4 @@
-"""ctypes binding of libvsa2.so: argument marshalling only, every step runs in the CUDA library.
+"""Binding of libvsa2.so: argument marshalling only (ctypes, and for the short calls csrc/marshal.c), every step runs in the CUDA library.
 
 The functions ``vsa2_query_sizes``, ``vsa2_route``, ``vsa2_attn_fwd``, ``vsa2_attn_bwd`` and
 ``vsa2_device_status`` mirror the C entry points of ``include/vsa2.h`` and take torch CUDA tensors
@@ -11,7 +11,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libvsa2.so")
@@ -151,7 +150,6 @@ def _lib():
         lib.vsa2_selftest_divmod.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         lib.vsa2_selftest_divmod.restype = C.c_int64
         lib.vsa2_rope_plan.argtypes = [C.c_int32, C.c_int32, vp, vp, vp, C.POINTER(Rope)]
-        # (structs come as bytes, or as pointers to the classes above)
         lib.vsa2_rope_apply.argtypes = [vp, vp, vp, vp, C.c_int32, vp]
         lib.vsa2_qkv_fwd.argtypes = [vp] * 6
         lib.vsa2_qkv_bwd.argtypes = [vp] * 9 + [sz, vp]
@@ -325,103 +323,46 @@ def vsa2_rope_plan(head_dim, channels, theta=1e4, scale=1.0, layout=ROPE_PAIRS) 
     return out
 
 
-# The structs of these calls are packed into bytes instead of filled field by field: a toy grid's calls wait for the host.
-_HEADS = struct.Struct("=QqqqiiiiiI")                  # vsa2_heads
-_HEADS2, _HEADS3 = struct.Struct("=" + 2 * "QqqqiiiiiI"), struct.Struct("=" + 3 * "QqqqiiiiiI")
-_PLACE = struct.Struct("=iiiiQq")                      # vsa2_place
-_NORM = struct.Struct("=QQfi")                         # vsa2_qk_norm
-_FP8 = struct.Struct("=QQq")                           # vsa2_fp8
-_TORCH, _DTYPES = None, {}
+# These calls are marshalled by a small module of C (csrc/marshal.c): a toy grid's calls wait for the host.
+MARSHAL_PATH = os.path.join(HERE, "_marshal.so")
+_MARSHAL = None
 
 
-def _torch():
-    global _TORCH
-    if _TORCH is None:
+def _marshal():
+    """The module (built in-tree with the library); raises if it is missing."""
+    global _MARSHAL
+    if _MARSHAL is None:
+        import importlib.machinery
+        import importlib.util
+
         import torch
-        _DTYPES.update({torch.bfloat16: BF16, torch.float32: F32})
-        _TORCH = torch
-    return _TORCH
-
-
-def _dtype(t):
-    code = _DTYPES.get(t.dtype)
-    if code is None:
-        _torch()
-        code = _DTYPES.get(t.dtype)
-        if code is None:
-            raise ValueError(f"expected bf16 or fp32, got {t.dtype}")
-    return code
-
-
-def _view(t):
-    """The fields of vsa2_heads of a CUDA tensor [batch, heads, tokens, D], any strides but 1 for the channels."""
-    if t.dim() != 4 or not t.is_cuda:
-        raise ValueError("expected a CUDA tensor [batch, heads, tokens, channels]")
-    sb, sh, st, last = t.stride()
-    if last != 1:
-        raise ValueError("the channels of a row must be contiguous")
-    code = _DTYPES.get(t.dtype)
-    b, h, n, c = t.shape
-    return t.data_ptr(), sb, sh, st, b, h, n, c, _dtype(t) if code is None else code, 0
-
-
-def _views(tensors):
-    """Those of two or three; a None among them is a view without heads."""
-    views = [None if t is None else _view(t) for t in tensors]
-    if None in views:
-        like = next((v for v in views if v is not None), None)
-        if like is None:
-            raise ValueError("no tensor is given")
-        absent = (0, 0, 0, 0, like[4], 0, like[6], like[7], like[8], 0)
-        views = [absent if v is None else v for v in views]
-    return views
-
-
-def _pack(views):
-    if len(views) == 3:
-        return _HEADS3.pack(*views[0], *views[1], *views[2])
-    return _HEADS2.pack(*views[0], *views[1])
-
-
-def _place(grid, first, positions, batch, tokens):
-    if positions is None:
-        t, h, w = grid if grid is not None else (0, 0, 0)
-        return _PLACE.pack(t, h, w, first, 0, 0)
-    if positions.dtype != _torch().int32 or not positions.is_cuda or not positions.is_contiguous():
-        raise ValueError("positions must be a contiguous CUDA int32 tensor [batch, tokens, 3] or [tokens, 3]")
-    shape = tuple(positions.shape)
-    if shape not in ((batch, tokens, 3), (1, tokens, 3), (tokens, 3)):
-        raise ValueError(f"positions {shape} do not fit {batch} x {tokens} tokens")
-    return _PLACE.pack(0, 0, 0, first, positions.data_ptr(), 3 * tokens if len(shape) == 3 and shape[0] > 1 else 0)
-
-
-def _weight(w, channels, name):
-    if w is None:
-        return 0
-    if _DTYPES.get(w.dtype) != F32 and _dtype(w) != F32 or w.numel() != channels:
-        raise ValueError(f"{name} must be fp32 with {channels} elements")
-    return _ptr(w)
+        if not os.path.exists(MARSHAL_PATH):
+            raise FileNotFoundError(f"{MARSHAL_PATH} not found: build it with `python -m paper_2609_32882_b200.build`")
+        loader = importlib.machinery.ExtensionFileLoader("_marshal", MARSHAL_PATH)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_marshal", MARSHAL_PATH, loader=loader))
+        loader.exec_module(module)
+        lib = _lib()
+        module.bind((torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn, torch.uint8),
+                    tuple(C.cast(f, C.c_void_p).value for f in (lib.vsa2_rope_apply, lib.vsa2_qkv_fwd, lib.vsa2_qkv_bwd, lib.vsa2_fp8_quantize,
+                                                                lib.vsa2_fp8_matmul)), _stream)
+        _MARSHAL = module
+    return _MARSHAL
 
 
 def vsa2_rope_apply(rope, x, y, grid=None, first=0, positions=None, inverse=False, stream=None):
     """y = R(position) x, or with `inverse` its inverse (the gradient); tensors [batch, heads, tokens, D], bf16 or fp32, any strides; y may be x.
     Positions: rows first, first + 1, .. of the raster of `grid` (rows behind it do not turn), or int32 [batch or 1, tokens, 3]."""
-    vx, vy = _view(x), _view(y)
-    _check(_lib().vsa2_rope_apply(C.byref(rope), _place(grid, first, positions, vx[4], vx[6]), _HEADS.pack(*vx), _HEADS.pack(*vy),
-                                  1 if inverse else 0, _stream(stream)), "vsa2_rope_apply")
-
-
-def _norm(q_weight, k_weight, eps, channels, norm):
-    return _NORM.pack(_weight(q_weight, channels, "q_weight"), _weight(k_weight, channels, "k_weight"), eps, 0) if norm else None
+    code = (_MARSHAL or _marshal()).rope_apply(rope, x, y, grid, first, positions, inverse, stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_rope_apply")
 
 
 def vsa2_qkv_fwd(rope, x, y, q_weight=None, k_weight=None, eps=1e-6, norm=True, grid=None, first=0, positions=None, stream=None):
     """x = (q, k, v) as the projection leaves them -> y = (q, k, v) of the attention: norm of every head of q and k, weights, rotation (rope None:
     none), v copied.  All are [batch, heads, tokens, D] views of any strides; a member may be None on both sides."""
-    vx, vy = _views(x), _views(y)
-    one = vx[0]
-    _check(_lib().vsa2_qkv_fwd(C.byref(rope) if rope is not None else None, _place(grid, first, positions, one[4], one[6]),
-                               _norm(q_weight, k_weight, eps, one[7], norm), _pack(vx), _pack(vy), _stream(stream)), "vsa2_qkv_fwd")
+    code = (_MARSHAL or _marshal()).qkv_fwd(rope, x, y, q_weight, k_weight, eps, norm, grid, first, positions, stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_qkv_fwd")
 
 
 def vsa2_qkv_bwd_workspace_bytes(channels) -> int:
@@ -432,14 +373,10 @@ def vsa2_qkv_bwd(rope, x, dy, dx, q_weight, k_weight, d_q_weight, d_k_weight, wo
                  positions=None, stream=None):
     """Backward of vsa2_qkv_fwd: x = its inputs (q, k and, unused, v), dy = gradients of its outputs -> dx, and the weights' gradients (fp32, None: not
     wanted).  workspace: vsa2_qkv_bwd_workspace_bytes(D) bytes (None without a norm)."""
-    vy, vd = _views(dy), _views(dx)
-    one = vy[0]
-    d = one[7]
-    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    _check(_lib().vsa2_qkv_bwd(C.byref(rope) if rope is not None else None, _place(grid, first, positions, one[4], one[6]),
-                               _norm(q_weight, k_weight, eps, d, norm), _pack(_views(x[:2])) if norm else None, _pack(vy), _pack(vd),
-                               _weight(d_q_weight, d, "d_q_weight"), _weight(d_k_weight, d, "d_k_weight"), _ptr(workspace), nbytes,
-                               _stream(stream)), "vsa2_qkv_bwd")
+    code = (_MARSHAL or _marshal()).qkv_bwd(rope, x, dy, dx, q_weight, k_weight, d_q_weight, d_k_weight, workspace, eps, norm, grid, first, positions,
+                                            stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_qkv_bwd")
 
 
 class Fp8:
@@ -448,12 +385,7 @@ class Fp8:
     __slots__ = ("values", "scales")
 
     def __init__(self, values, scales):
-        torch = _TORCH or _torch()
-        rows, cols = values.shape
-        if values.dtype is not torch.float8_e4m3fn or (cols > 1 and values.stride(1) != 1):
-            raise ValueError("values must be float8_e4m3fn [rows, cols] with contiguous rows")
-        if scales.dtype is not torch.uint8 or scales.shape != (-(-cols // 512), rows, 4):
-            raise ValueError(f"scales must be uint8 {(-(-cols // 512), rows, 4)}, got {tuple(scales.shape)}")
+        (_MARSHAL or _marshal()).check_fp8(values, scales)
         self.values, self.scales = values, scales
 
     @classmethod
@@ -466,13 +398,6 @@ class Fp8:
     def shape(self):
         return tuple(self.values.shape)
 
-    def _pack(self):
-        values = self.values
-        if not values.is_cuda:
-            raise ValueError("expected a CUDA tensor")
-        rows, cols = values.shape
-        return _FP8.pack(values.data_ptr(), _ptr(self.scales), values.stride(0) if rows > 1 else -(-cols // 16) * 16)
-
     def dequantize(self):
         """The matrix in fp32 (torch operations: for inspection and tests)."""
         import torch
@@ -484,14 +409,9 @@ class Fp8:
 def vsa2_fp8_quantize(x, out=None, out_t=None, squares=False, stream=None):
     """x [rows, cols] (bf16 or fp32, contiguous rows) -> `out`, its 8-bit form, and / or `out_t`, that of its transpose.  squares: one scale for each
     128 x 128 values instead of each 128 of a row."""
-    if x.dim() != 2 or not x.is_cuda or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise ValueError("expected a CUDA matrix with contiguous rows")
-    rows, cols = x.shape
-    if (out is not None and out.shape != (rows, cols)) or (out_t is not None and out_t.shape != (cols, rows)):
-        raise ValueError("outputs do not have the shape of x and of its transpose")
-    a, b = None if out is None else out._pack(), None if out_t is None else out_t._pack()
-    _check(_lib().vsa2_fp8_quantize(x.data_ptr(), _dtype(x), rows, cols, x.stride(0) if rows > 1 else cols, 1 if squares else 0, a, b,
-                                    _stream(stream)), "vsa2_fp8_quantize")
+    code = (_MARSHAL or _marshal()).quantize(x, out, out_t, squares, stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_fp8_quantize")
 
 
 def vsa2_fp8_matmul_workspace_bytes(m, n, k) -> int:
@@ -506,13 +426,9 @@ def fp8_matmul_workspace(m, n, k, device="cuda"):
 
 def vsa2_fp8_matmul(a, b, c, workspace, stream=None):
     """c [m, n] = a b^T of two Fp8 matrices [m, k] and [n, k]; c bf16 or fp32 with contiguous rows."""
-    (m, k), (n, kb) = a.shape, b.shape
-    if k != kb or tuple(c.shape) != (m, n):
-        raise ValueError(f"shapes {a.shape}, {b.shape} and {tuple(c.shape)} do not fit")
-    if not c.is_cuda or (n > 1 and c.stride(1) != 1):
-        raise ValueError("c must be a CUDA matrix with contiguous rows")
-    _check(_lib().vsa2_fp8_matmul(m, n, k, a._pack(), b._pack(), c.data_ptr(), _dtype(c), c.stride(0) if m > 1 else n,
-                                  _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "vsa2_fp8_matmul")
+    code = (_MARSHAL or _marshal()).matmul(a, b, c, workspace, stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_fp8_matmul")
 
 
 def vsa2_profile_events(kernel_id: int, start_event, stop_event):

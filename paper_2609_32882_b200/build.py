@@ -5,11 +5,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libvsa2.so")
+MARSHAL_PATH = os.path.join(HERE, "_marshal.so")      # CPython module that hands the binding's short calls to the library
 ARCH_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a"]
 
 
@@ -18,15 +20,15 @@ def sources():
 
 
 def _stale():
-    if not os.path.exists(LIB_PATH):
+    if not os.path.exists(LIB_PATH) or not os.path.exists(MARSHAL_PATH):
         return True
-    t = os.path.getmtime(LIB_PATH)
+    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(MARSHAL_PATH))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "vsa2.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compiles csrc/*.cu into libvsa2.so next to this file and returns its path."""
+    """Compiles csrc/*.cu into libvsa2.so next to this file, and csrc/marshal.c into _marshal.so; returns the library's path."""
     if not force and not _stale():
         return LIB_PATH
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
@@ -52,6 +54,8 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(out.decode())
         if pr.returncode:
             raise RuntimeError(f"nvcc failed on {src}")
+    subprocess.check_call([shutil.which("gcc") or "cc", "-shared", "-fPIC", "-O2", "-I", sysconfig.get_paths()["include"], "-I",
+                           os.path.join(ROOT, "include"), os.path.join(CSRC, "marshal.c"), "-o", MARSHAL_PATH])
     subprocess.check_call([nvcc, "-shared", "-o", LIB_PATH] + objs + ARCH_FLAGS + ["-lcudart_static", "-ldl", "-lrt", "-lpthread"])
     return LIB_PATH
 

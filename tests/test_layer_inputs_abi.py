@@ -199,18 +199,129 @@ def test_binding_refuses_what_it_cannot_marshal():
     f = vb.Fp8.empty(4, 20, device="cpu")
     assert f.shape == (4, 20) and f.values.stride(0) == 32
     with pytest.raises(ValueError):
-        f._pack()
-    with pytest.raises(ValueError):
         vb.vsa2_fp8_quantize(torch.zeros(4, 20), f)
     with pytest.raises(ValueError):
         vb.vsa2_fp8_matmul(f, vb.Fp8.empty(4, 21, device="cpu"), torch.zeros(4, 4), None)
+    with pytest.raises(ValueError):
+        vb.Fp8(torch.zeros(4, 20).to(torch.float8_e4m3fn), torch.zeros(1, 4, 4))
+    with pytest.raises(ValueError):
+        vb.Fp8(torch.zeros(4).to(torch.float8_e4m3fn), torch.zeros(1, 4, 4, dtype=torch.uint8))
+    with pytest.raises(AttributeError):
+        vb.vsa2_rope_apply(rope, "x", "y", grid=(1, 1, 4))
+    with pytest.raises(TypeError):
+        vb._marshal().rope_apply(rope)
+    with pytest.raises(ValueError):
+        vb.vsa2_qkv_fwd(rope, (None, None, None), (None, None, None), grid=(1, 1, 4))
+    with pytest.raises(ValueError):
+        vb.vsa2_qkv_fwd(rope, (None,), (None,), grid=(1, 1, 4))
 
 
-def test_packed_structs_have_the_layout_of_the_header():
-    for packed, cls in ((vb._HEADS, vb.Heads), (vb._PLACE, vb.Place), (vb._NORM, vb.QkNorm), (vb._FP8, vb.Fp8Matrix)):
-        assert packed.size == C.sizeof(cls)
-    v = vb.Heads.from_buffer_copy(vb._HEADS.pack(1 << 40, 2 << 33, 3, 4, 5, 6, 7, 8, 1, 0))
-    assert [getattr(v, f) for f, _ in vb.Heads._fields_] == [1 << 40, 2 << 33, 3, 4, 5, 6, 7, 8, 1, 0]
-    p = vb.Place.from_buffer_copy(vb._place((3, 4, 5), 6, None, 1, 1))
-    assert (p.grid_t, p.grid_h, p.grid_w, p.first, p.positions) == (3, 4, 5, 6, None)
-    assert vb._HEADS2.size == 2 * vb._HEADS.size and vb._HEADS3.size == 3 * vb._HEADS.size
+class FakeTensor:
+    """What the marshalling asks of a CUDA tensor; nothing is ever launched with it."""
+
+    def __init__(self, tensor, is_cuda=True):
+        self._t, self.shape, self.dtype, self.is_cuda, self.nbytes = tensor, tensor.shape, tensor.dtype, is_cuda, tensor.nbytes
+
+    def __getattr__(self, name):
+        return getattr(self._t, name)
+
+
+def test_marshalling_passes_what_the_tensors_say(monkeypatch):
+    """Bound to functions that record their arguments instead of the library's."""
+    seen = {}
+    rope_t = C.CFUNCTYPE(C.c_int, C.POINTER(vb.Rope), C.POINTER(vb.Place), C.POINTER(vb.Heads), C.POINTER(vb.Heads), C.c_int32, C.c_void_p)
+    fwd_t = C.CFUNCTYPE(C.c_int, C.POINTER(vb.Rope), C.POINTER(vb.Place), C.POINTER(vb.QkNorm), C.POINTER(vb.Heads), C.POINTER(vb.Heads), C.c_void_p)
+    bwd_t = C.CFUNCTYPE(C.c_int, C.POINTER(vb.Rope), C.POINTER(vb.Place), C.POINTER(vb.QkNorm), *[C.POINTER(vb.Heads)] * 3, *[C.c_void_p] * 3, C.c_size_t,
+                        C.c_void_p)
+    qz_t = C.CFUNCTYPE(C.c_int, C.c_void_p, *[C.c_int32] * 3, C.c_int64, C.c_int32, C.POINTER(vb.Fp8Matrix), C.POINTER(vb.Fp8Matrix), C.c_void_p)
+    mm_t = C.CFUNCTYPE(C.c_int, *[C.c_int32] * 3, C.POINTER(vb.Fp8Matrix), C.POINTER(vb.Fp8Matrix), C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_size_t,
+                       C.c_void_p)
+    fields = lambda s: {f: (list(getattr(s, f)) if f in ("turn", "axis_pairs") else getattr(s, f)) for f, _ in s._fields_}
+    view = lambda s: tuple(fields(s).values())
+
+    def keep(name, *indices):
+        def f(*a):
+            seen[name] = [x if not isinstance(x, C._Pointer) else [view(x[k]) for k in range(indices[i])] if x else None for i, x in enumerate(a)]
+            return 0
+        return f
+
+    fns = (rope_t(keep("rope", 1, 1, 1, 1, 0, 0)), fwd_t(keep("fwd", 1, 1, 1, 3, 3, 0)), bwd_t(keep("bwd", 1, 1, 1, 2, 3, 3, 0, 0, 0, 0, 0)),
+           qz_t(keep("qz", 0, 0, 0, 0, 0, 0, 1, 1, 0)), mm_t(keep("mm", 0, 0, 0, 1, 1, 0, 0, 0, 0, 0, 0)))
+    types = (torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn, torch.uint8)
+    m = vb._marshal()
+    lib = vb._lib()
+    real = tuple(C.cast(f, C.c_void_p).value for f in (lib.vsa2_rope_apply, lib.vsa2_qkv_fwd, lib.vsa2_qkv_bwd, lib.vsa2_fp8_quantize, lib.vsa2_fp8_matmul))
+    m.bind(types, tuple(C.cast(f, C.c_void_p).value for f in fns), lambda s: 77 if s is None else s)
+    try:
+        rope = vb.vsa2_rope_plan(64, (16, 24, 24))
+        base = torch.zeros(2, 5, 7, 64, dtype=torch.bfloat16)
+        x, y = FakeTensor(base.transpose(1, 2)[:, 2:5]), FakeTensor(torch.zeros(2, 3, 5, 64))
+        pos = FakeTensor(torch.zeros(2, 5, 3, dtype=torch.int32))
+        vb.vsa2_rope_apply(rope, x, y, grid=(1, 2, 3), first=4, inverse=True, stream=9)
+        r, p, vx, vy, inverse, stream = seen["rope"]
+        assert r[0][-1] == list(rope.turn) and p == [(1, 2, 3, 4, None, 0)] and (inverse, stream) == (1, 9)
+        assert vx == [(x.data_ptr(), 5 * 7 * 64, 64, 7 * 64, 2, 3, 5, 64, vb.BF16, 0)]
+        assert vy == [(y.data_ptr(), 3 * 5 * 64, 5 * 64, 64, 2, 3, 5, 64, vb.F32, 0)]
+        vb.vsa2_rope_apply(rope, x, y, positions=pos)
+        assert seen["rope"][1] == [(0, 0, 0, 0, pos.data_ptr(), 15)] and seen["rope"][5] == 77
+        one = FakeTensor(torch.zeros(5, 3, dtype=torch.int32))
+        vb.vsa2_rope_apply(rope, x, y, positions=one)
+        assert seen["rope"][1] == [(0, 0, 0, 0, one.data_ptr(), 0)]
+        for bad in (torch.zeros(2, 4, 3, dtype=torch.int32), torch.zeros(3, 5, 3, dtype=torch.int32), torch.zeros(2, 5, 3, dtype=torch.int64),
+                    torch.zeros(2, 3, 5, dtype=torch.int32).transpose(1, 2)):
+            with pytest.raises(ValueError):
+                vb.vsa2_rope_apply(rope, x, y, positions=FakeTensor(bad))
+        w = [FakeTensor(torch.zeros(64)) for _ in range(4)]
+        vb.vsa2_qkv_fwd(None, (x, None, x), [y, None, y], w[0], None, eps=0.25, grid=[1, 1, 5])
+        r, p, n, vx, vy, _ = seen["fwd"]
+        assert r is None and n == [(w[0].data_ptr(), None, 0.25, 0)] and p == [(1, 1, 5, 0, None, 0)]
+        assert vx[1] == (None, 0, 0, 0, 2, 0, 5, 64, vb.BF16, 0) and vx[0] == vx[2] and vy[1][5] == 0 and vy[1][8] == vb.F32
+        vb.vsa2_qkv_fwd(rope, (x, x, x), (y, y, y), norm=False, grid=(1, 1, 5))
+        assert seen["fwd"][2] is None
+        for bad in (torch.zeros(63), torch.zeros(64, dtype=torch.float64), torch.zeros(128)[::2]):
+            with pytest.raises(ValueError):
+                vb.vsa2_qkv_fwd(rope, (x, x, x), (y, y, y), FakeTensor(bad), grid=(1, 1, 5))
+        ws = FakeTensor(torch.zeros(100, dtype=torch.float32))
+        vb.vsa2_qkv_bwd(rope, (x, x, None), (y, y, y), (x, x, x), w[0], w[1], w[2], None, ws, grid=(1, 1, 5))
+        a = seen["bwd"]
+        assert a[6:9] == [w[2].data_ptr(), None, ws.data_ptr()] and a[9] == 400 and len(a[3]) == 2 and a[4][0][0] == y.data_ptr()
+        vb.vsa2_qkv_bwd(rope, None, (y, y, y), (x, x, x), None, None, None, None, None, norm=False, grid=(1, 1, 5))
+        assert seen["bwd"][2] is None and seen["bwd"][3] is None and seen["bwd"][9] == 0
+        f8 = lambda rows, cols: vb.Fp8(FakeTensor(torch.zeros(rows, -(-cols // 16) * 16).to(torch.float8_e4m3fn)[:, :cols]),
+                                       FakeTensor(torch.zeros(-(-cols // 512), rows, 4, dtype=torch.uint8)))
+        mat, out, out_t = FakeTensor(torch.zeros(6, 50)[:, :40]), f8(6, 40), f8(40, 6)
+        vb.vsa2_fp8_quantize(mat, out, out_t, squares=True)
+        a = seen["qz"]
+        assert a[:6] == [mat.data_ptr(), vb.F32, 6, 40, 50, 1] and a[6] == [(out.values.data_ptr(), out.scales.data_ptr(), 48)]
+        assert a[7] == [(out_t.values.data_ptr(), out_t.scales.data_ptr(), 16)]
+        for bad in ((mat, out_t), (mat, None, out)):
+            with pytest.raises(ValueError):
+                vb.vsa2_fp8_quantize(*bad)
+        c = FakeTensor(torch.zeros(6, 9, dtype=torch.bfloat16)[:, :7])
+        vb.vsa2_fp8_matmul(f8(6, 40), f8(7, 40), c, ws)
+        a = seen["mm"]
+        assert a[:3] == [6, 7, 40] and a[5:10] == [c.data_ptr(), vb.BF16, 9, ws.data_ptr(), 400]
+        for bad in ((f8(6, 40), f8(7, 39), c), (f8(5, 40), f8(7, 40), c), (f8(6, 40), f8(8, 40), c)):
+            with pytest.raises(ValueError):
+                vb.vsa2_fp8_matmul(*bad, ws)
+        with pytest.raises(ValueError):
+            vb.vsa2_fp8_matmul(f8(6, 40), f8(7, 40), FakeTensor(torch.zeros(6, 7, dtype=torch.float16)), ws)
+    finally:
+        m.bind(types, real, vb._stream)
+
+
+def test_marshalling_leaks_no_references():
+    import gc
+    import sys
+    rope, t = vb.vsa2_rope_plan(64, (16, 24, 24)), torch.zeros(1, 1, 4, 64)
+    grid, f = (1, 1, 4), vb.Fp8.empty(4, 20, device="cpu")
+    objects = (rope, t, grid, f, f.values, f.scales, torch.float32, vb._stream)
+    counts = [sys.getrefcount(o) for o in objects]
+    for _ in range(200):
+        for call in (lambda: vb.vsa2_rope_apply(rope, t, t, grid=grid), lambda: vb.vsa2_qkv_fwd(rope, (t, None, t), (t, t, t), grid=grid),
+                     lambda: vb.vsa2_fp8_quantize(t[0, 0], f), lambda: vb.vsa2_fp8_matmul(f, f, t[0, 0], t)):
+            with pytest.raises(ValueError):
+                call()
+        vb.Fp8(f.values, f.scales)
+    gc.collect()
+    assert all(abs(sys.getrefcount(o) - c) <= 2 for o, c in zip(objects, counts))
