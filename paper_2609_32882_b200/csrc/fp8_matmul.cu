@@ -325,7 +325,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
   if constexpr (PAIR == 2) cluster_sync_all();
   tc::tc_fence_after();
   const uint32_t tmem_base = misc->tmem_base;
-  grid_enter(false);
+  grid_enter(a.splits > 1);      // (the kernel that adds the ranges finds room beside this one)
   {
     MmWalk w;
     w.init(blockIdx.x / PAIR, gridDim.x / PAIR);
@@ -610,10 +610,11 @@ MmPlan plan_mm(const MmCall& c, bool swap) {
     const double block = fed > 2.0 * NT ? fed : 2.0 * NT;
     return (double)((items + of - 1) / of) * blocks * (block > 300.0 ? block : 300.0);
   };
-  plan.cycles = products(tiles, c.kb);
+  const double epilogue = 12.0 * NT;      // of the last tile
+  plan.cycles = products(tiles, c.kb) + epilogue;
   if (swap) plan.cycles *= 1.06;      // (its results go out 64 bytes at a time: 8192 x 4096 x 4096 98 us instead of 91)
   for (int s = 2; !swap && s <= kMmSplits && s <= c.kb && tiles * s <= of; ++s) {
-    const double cycles = products(tiles * s, (c.kb + s - 1) / s) + 5000 + 8.0 * s * c.m * c.n / (30.0 * kMmCtas);
+    const double cycles = products(tiles * s, (c.kb + s - 1) / s) + epilogue + 5000 + 8.0 * s * c.m * c.n / (30.0 * kMmCtas);
     if (cycles < plan.cycles) {
       plan.cycles = cycles;
       plan.splits = s;
@@ -705,13 +706,14 @@ cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Ar
   }
   if (!pair) return launch_mm<128, 1>(call, plan_mm<128, 1>(call, false));
   if (m <= 128) return launch_mm<128, 2>(call, plan_mm<128, 2>(call, false));
-  // A's rows as the lanes, B's as the columns where that fills the rounds better (512 x 15360 x 5120: 138 tiles instead of 180 on 74 pairs, 35 us instead of 49)
-  const MmPlan plan = plan_mm<224, 2>(call, false);
+  // The columns that waste least (256 x 4608 x 1536: two tiles of 128 instead of two of 224, 8.8 us instead of 9.9), and A's rows as the lanes, B's as the columns where that
+  // fills the rounds better (512 x 15360 x 5120: 138 tiles instead of 180 on 74 pairs, 35 us instead of 49)
+  const MmPlan wide = plan_mm<224, 2>(call, false), narrow = plan_mm<128, 2>(call, false);
   if (call.tensor_stores) {
     const MmPlan swapped = plan_mm<224, 2>(call, true);
-    if (swapped.cycles < plan.cycles) return launch_tiles<224, 2, true, bf16>(call, swapped, c, ldc, 0);
+    if (swapped.cycles < wide.cycles && swapped.cycles < narrow.cycles) return launch_tiles<224, 2, true, bf16>(call, swapped, c, ldc, 0);
   }
-  return launch_mm<224, 2>(call, plan);
+  return narrow.cycles < wide.cycles ? launch_mm<128, 2>(call, narrow) : launch_mm<224, 2>(call, wide);
 }
 
 }  // namespace vsa2
