@@ -4,7 +4,7 @@
 //   value = x * 2^-e rounded to e4m3 (to nearest, ties to even); what is not finite becomes NaN
 // A power of two scales without rounding, so the 3 mantissa bits are all that is lost, and it is what the tensor cores multiply by themselves.
 // x is read once, each form written once.  Rows alone are bound by memory: 75600 x 5120 193 us (6.0 TB/s), 20000 x 5120 of fp32 77 us (6.6).  Both forms in one
-// reading are bound by instructions, about 70 % of the issue slots (a conversion for every value and form): 20000 x 5120 98 us (4.2 TB/s).
+// reading are bound by instructions (a conversion for every value and form): 20000 x 5120 82 us (5.0 TB/s), blocks of 128 x 128 of 15360 x 5120 54 us (5.8).
 #include "common.cuh"
 #include "heads.cuh"
 
@@ -18,12 +18,15 @@ constexpr int kQzThreads = 256;
 __device__ __forceinline__ uint32_t scale_byte(uint32_t top) { return (uint32_t)max((int)((top + 0x1fffffu) >> 23) - 8, 0); }
 __device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 __device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
+      "mov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
 }
-__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) { return e4m3x2(a, b) | e4m3x2(c, d) << 16; }
 // Blocks where something is not finite are rare: only they look at every value (CHECK).  (An infinity becomes NaN; the conversion alone would make it 448.)
 template <bool CHECK>
 __device__ __forceinline__ float scaled(float x, float inv) { return !CHECK || finite_bits(x) ? x * inv : __uint_as_float(0x7fffffffu); }
@@ -49,9 +52,16 @@ template <> struct Oct<false> {
     uint32_t t[4] = {0u, 0u, 0u, 0u};
     __device__ __forceinline__ uint32_t get(int j) const { return j & 1 ? t[j / 2] & 0xffff0000u : t[j / 2] << 16; }
   };
-  __device__ __forceinline__ void raise(Tops& o) const {
+  // the row's, raising the columns'
+  __device__ __forceinline__ uint32_t sweep(Tops& o) const {
+    uint32_t m[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o.t[i] = __vmaxu2(o.t[i], u[i] & 0x7fff7fffu);
+    for (int i = 0; i < 4; ++i) {
+      m[i] = u[i] & 0x7fff7fffu;
+      o.t[i] = __vmaxu2(o.t[i], m[i]);
+    }
+    const uint32_t t = __vmaxu2(__vmaxu2(m[0], m[1]), __vmaxu2(m[2], m[3]));
+    return max(t & 0xffff0000u, t << 16);
   }
 };
 template <> struct Oct<true> {
@@ -77,9 +87,10 @@ template <> struct Oct<true> {
     uint32_t t[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
     __device__ __forceinline__ uint32_t get(int j) const { return t[j]; }
   };
-  __device__ __forceinline__ void raise(Tops& o) const {
+  __device__ __forceinline__ uint32_t sweep(Tops& o) const {
 #pragma unroll
     for (int j = 0; j < 8; ++j) o.t[j] = max(o.t[j], __float_as_uint(f[j]) & 0x7fffffffu);
+    return top();
   }
 };
 constexpr uint32_t kInf = 0x7f800000u;
@@ -112,12 +123,12 @@ __device__ __forceinline__ void put8(unsigned char* row, int i, int cols, uint32
     for (int j = 0; i + j < cols; ++j) row[i + j] = (unsigned char)((j < 4 ? lo >> 8 * j : hi >> 8 * (j - 4)) & 0xffu);
   }
 }
-template <bool CHECK, bool F32>
+template <bool CHECK, bool FULL, bool F32>
 __device__ __forceinline__ void put_oct(unsigned char* row, int i, int cols, const Oct<F32>& o, float inv) {
   float f[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) f[j] = scaled<CHECK>(o.get(j), inv);
-  put8(row, i, cols, e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
+  put8(row, i, FULL ? i + 8 : cols, e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
 }
 __device__ __forceinline__ uint32_t team_max(uint32_t t) {      // of 16 threads
 #pragma unroll
@@ -147,8 +158,8 @@ __global__ void __launch_bounds__(kQzThreads) fp8_rows_kernel(const void* x, int
     word |= s << 8 * b;
     if (row < rows) {
       unsigned char* to = out.values + row * out.ld;
-      if (odd) put_oct<true, F32>(to, c0 + b * 128 + l * 8, cols, o[b], inverse_scale(s));
-      else put_oct<false, F32>(to, c0 + b * 128 + l * 8, cols, o[b], inverse_scale(s));
+      if (odd) put_oct<true, false, F32>(to, c0 + b * 128 + l * 8, cols, o[b], inverse_scale(s));
+      else put_oct<false, false, F32>(to, c0 + b * 128 + l * 8, cols, o[b], inverse_scale(s));
     }
   }
   if (l == 0 && row < rows) reinterpret_cast<uint32_t*>(out.scales)[(size_t)blockIdx.y * rows + row] = word;
@@ -165,17 +176,19 @@ __device__ __forceinline__ void put_scale(unsigned char* scales, int rows, int r
 struct TileShared {
   unsigned char turned[128 * 128];
   uint32_t col_top[16][128];
+  float col_inv[128];
   uint32_t tops[kQzThreads / 32];
 };
 
-// a tile whose values are in the threads' registers: both forms, or either
-// (`tops`: largest magnitudes of the thread's rows where all is finite)
-template <bool CHECK, bool F32>
-__device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint32_t (&tops)[8], TileShared& sh, int rows, int cols, int squares, const Fp8Arg& out, const Fp8Arg& out_t) {
+// A tile whose values are in the threads' registers: both forms, or either.  `tops`, `cols_top`: largest magnitudes of the thread's rows and columns (of no use with CHECK);
+// FULL: the tile lies inside the matrix
+template <bool CHECK, bool FULL, bool F32>
+__device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint32_t (&tops)[8], const typename Oct<F32>::Tops& cols_top, TileShared& sh,
+                                              int rows, int cols, int squares, const Fp8Arg& out, const Fp8Arg& out_t) {
   const int l = threadIdx.x & 15, team = threadIdx.x >> 4, tid = threadIdx.x;
   const int c0 = blockIdx.y * 128, r0 = blockIdx.x * 128;
   const int blocks = (cols + 127) / 128, blocks_t = (rows + 127) / 128;
-  auto top_of = [&](int i) { return CHECK ? finite_top<F32>(o[i]) : F32 ? o[i].top() : tops[i]; };      // (fp32: no registers to keep them in)
+  auto top_of = [&](int i) { return CHECK ? finite_top<F32>(o[i]) : tops[i]; };
   uint32_t top_all = 0;
   if (squares) {
 #pragma unroll
@@ -183,30 +196,29 @@ __device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint
     top_all = __reduce_max_sync(0xffffffffu, top_all);
     if ((tid & 31) == 0) sh.tops[tid >> 5] = top_all;
     __syncthreads();
+#pragma unroll
     for (int i = 0; i < kQzThreads / 32; ++i) top_all = max(top_all, sh.tops[i]);
   }
   if (out.values != nullptr) {
+    unsigned char* to = out.values + (r0 + team * 8) * out.ld;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i, to += out.ld) {
       const uint32_t s = scale_byte(squares ? top_all : team_max(top_of(i)));
       const int row = r0 + team * 8 + i;
-      if (row < rows) {
-        put_oct<CHECK, F32>(out.values + row * out.ld, c0 + l * 8, cols, o[i], inverse_scale(s));
+      if (FULL || row < rows) {
+        put_oct<CHECK, FULL, F32>(to, c0 + l * 8, cols, o[i], inverse_scale(s));
         if (l == 0) put_scale(out.scales, rows, row, blockIdx.y, blocks, s);
       }
     }
   }
   if (out_t.values == nullptr) return;
+  uint32_t byte = 0;      // of column tid
   if (!squares) {
-    typename Oct<F32>::Tops t;
-    if (!CHECK) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[i].raise(t);
-    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      uint32_t top = t.get(j);
+      uint32_t top = cols_top.get(j);
       if (CHECK) {
+        top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if (finite_bits(o[i].get(j))) top = max(top, __float_as_uint(o[i].get(j)) & 0x7fffffffu);
@@ -214,20 +226,24 @@ __device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint
       sh.col_top[team][l * 8 + j] = top;
     }
     __syncthreads();
-    if (tid < 128) {
-      uint32_t top = 0;
+  }
+  if (tid < 128) {
+    uint32_t top = top_all;
+    if (!squares) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = max(top, sh.col_top[r][tid]);
-      sh.col_top[0][tid] = top;
     }
-    __syncthreads();
+    byte = scale_byte(top);
+    sh.col_inv[tid] = inverse_scale(byte);
   }
+  __syncthreads();
+  const float4 inv0 = reinterpret_cast<const float4*>(sh.col_inv)[2 * l], inv1 = reinterpret_cast<const float4*>(sh.col_inv)[2 * l + 1];
+  const float inv[8] = {inv0.x, inv0.y, inv0.z, inv0.w, inv1.x, inv1.y, inv1.z, inv1.w};
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float inv = inverse_scale(scale_byte(squares ? top_all : sh.col_top[0][l * 8 + j]));
     float f[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = scaled<CHECK>(o[i].get(j), inv);
+    for (int i = 0; i < 8; ++i) f[i] = scaled<CHECK>(o[i].get(j), inv[j]);
     *reinterpret_cast<uint2*>(sh.turned + (l * 8 + j) * 128 + ((team ^ l) << 3)) =
         make_uint2(e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
   }
@@ -237,10 +253,10 @@ __device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint
     const int e = u * kQzThreads + tid, c = e >> 3, part = (e & 7) * 2, g = c >> 3;      // places part, part + 1 of column c
     uint4 v = *reinterpret_cast<const uint4*>(sh.turned + c * 128 + (((part ^ g) & ~1) << 3));
     if (g & 1) v = make_uint4(v.z, v.w, v.x, v.y);
-    if (c0 + c < cols) {
+    if (FULL || c0 + c < cols) {
       unsigned char* row = out_t.values + (long long)(c0 + c) * out_t.ld;
       const int i = r0 + part * 8;
-      if (i + 16 <= rows) {
+      if (FULL || i + 16 <= rows) {
         *reinterpret_cast<uint4*>(row + i) = v;
       } else {
         put8(row, i, rows, v.x, v.y);
@@ -248,8 +264,7 @@ __device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint
       }
     }
   }
-  if (tid < 128 && c0 + tid < cols)
-    put_scale(out_t.scales, cols, c0 + tid, blockIdx.x, blocks_t, scale_byte(squares ? top_all : sh.col_top[0][tid]));
+  if (tid < 128 && c0 + tid < cols) put_scale(out_t.scales, cols, c0 + tid, blockIdx.x, blocks_t, byte);
 }
 
 // A tile of 128 x 128: both forms, or either.  A team of 16 threads holds 8 rows, 8 columns a thread.  The transpose passes through shared memory
@@ -263,19 +278,28 @@ __global__ void __launch_bounds__(kQzThreads, F32 ? 2 : 4) fp8_tile_kernel(const
   const int l = threadIdx.x & 15, team = threadIdx.x >> 4;
   Oct<F32> o[8];
   uint32_t tops[8], top = 0;
+  typename Oct<F32>::Tops cols_top;
+  const bool full = VEC && (blockIdx.x + 1) * 128 <= rows && (blockIdx.y + 1) * 128 <= cols;
+  if (full) {
+    const size_t at = (size_t)(blockIdx.x * 128 + team * 8) * ld + blockIdx.y * 128 + l * 8;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = blockIdx.x * 128 + team * 8 + i;
-    if (row < rows) load8<F32, VEC>(x, (size_t)row * ld, blockIdx.y * 128 + l * 8, cols, o[i]);
-    else o[i].zero();
+    for (int i = 0; i < 8; ++i) o[i].load(x, at + i * ld);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = blockIdx.x * 128 + team * 8 + i;
+      if (row < rows) load8<F32, VEC>(x, (size_t)row * ld, blockIdx.y * 128 + l * 8, cols, o[i]);
+      else o[i].zero();
+    }
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    tops[i] = o[i].top();
+    tops[i] = o[i].sweep(cols_top);
     top = max(top, tops[i]);
   }
-  if (__syncthreads_or(top >= kInf)) quantize_tile<true, F32>(o, tops, sh, rows, cols, squares, out, out_t);
-  else quantize_tile<false, F32>(o, tops, sh, rows, cols, squares, out, out_t);
+  if (__syncthreads_or(top >= kInf)) quantize_tile<true, false, F32>(o, tops, cols_top, sh, rows, cols, squares, out, out_t);
+  else if (full) quantize_tile<false, true, F32>(o, tops, cols_top, sh, rows, cols, squares, out, out_t);
+  else quantize_tile<false, false, F32>(o, tops, cols_top, sh, rows, cols, squares, out, out_t);
 }
 
 }  // namespace
