@@ -87,6 +87,7 @@ class Rope(C.Structure):
                 ("turn", C.c_uint64 * 64)]
 
 
+# (the structs below: for callers of the library's functions themselves; the wrappers go through csrc/marshal.c)
 class Place(C.Structure):
     _fields_ = [("grid_t", C.c_int32), ("grid_h", C.c_int32), ("grid_w", C.c_int32), ("first", C.c_int32),
                 ("positions", C.c_void_p), ("positions_batch_stride", C.c_int64)]

@@ -43,7 +43,7 @@ struct MmTile {
   static constexpr uint32_t STAGE = kMmPBytes + NT / PAIR * 128;
   static constexpr int SFQ = (NT + 127) / 128;                              // 512-byte pieces of the scales of the columns' rows
   static constexpr uint32_t SCALES = 512 + SFQ * 512;
-  static constexpr uint32_t STAGING = sizeof(TO) == 2 ? 4 * kMmTileBytes : 0;      // two tiles of results for each group of the epilogue
+  static constexpr uint32_t STAGING = sizeof(TO) == 2 ? (NT > 32 ? 4 : 2) * kMmTileBytes : 0;      // two tiles of results for each group of the epilogue
   static constexpr uint32_t ROOM = 227 * 1024 - 2048 - kMmScaleSlots * SCALES - STAGING;
   static constexpr int STAGES = ROOM / STAGE < kMmStagesMost ? ROOM / STAGE : kMmStagesMost;
   static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + STAGING + kMmScaleSlots * SCALES;
