@@ -347,7 +347,8 @@ typedef struct vsa2_place {
 } vsa2_place;
 
 /* Heads as a strided view [batch, heads, tokens, channels] (host struct); strides in elements, channels contiguous.  `data` and the strides
- * must be multiples of 16 bytes; outputs must not overlap themselves.  heads = 0: absent (data may be NULL). */
+ * must be multiples of 16 bytes; outputs overlap neither themselves nor, unless a call allows it, an input.  heads = 0: absent (data may be NULL); a
+ * call takes 2^20 heads in all. */
 typedef struct vsa2_heads {
   void* data;
   int64_t batch_stride, head_stride, token_stride;

@@ -332,6 +332,8 @@ cudaError_t g_last_cuda_error = cudaSuccess;
   } while (0)
 
 // ---- views of heads, matrices in 8 bits -----------------------------------------------------------------------------------
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
 // shape, type and strides of one view; `written`: its elements must be distinct as far as strides of zero show it
 int check_heads(const vsa2_heads& v, bool written) {
   if (v.batch < 0 || v.heads < 0 || v.tokens < 0 || (v.dtype != VSA2_BF16 && v.dtype != VSA2_F32)) return VSA2_ERR_INVALID_ARG;
@@ -371,7 +373,7 @@ int fill_turn(const vsa2_rope* rope, const vsa2_place* place, const vsa2_heads& 
   t->pairs_t = rope->axis_pairs[0];
   t->pairs_th = rope->axis_pairs[0] + rope->axis_pairs[1];
   if (place->positions != nullptr) {
-    if (reinterpret_cast<uintptr_t>(place->positions) & 3u) return VSA2_ERR_MISALIGNED;
+    if (!aligned4(place->positions)) return VSA2_ERR_MISALIGNED;
     if (place->positions_batch_stride < 0) return VSA2_ERR_INVALID_ARG;
     t->positions = place->positions;
     t->positions_sb = place->positions_batch_stride;
@@ -391,6 +393,7 @@ bool rope_halves(const vsa2_rope* rope) { return rope != nullptr && rope->layout
 // x -> y of up to three views each: shapes agree, all of a side have one type; *empty: there is nothing to do
 int check_qkv(const vsa2_heads* x, const vsa2_heads* y, int n, bool* empty) {
   int rc;
+  int64_t heads = 0;
   *empty = true;
   for (int i = 0; i < n; ++i) {
     if ((rc = check_heads(x[i], false)) != VSA2_OK || (rc = check_heads(y[i], true)) != VSA2_OK) return rc;
@@ -398,15 +401,23 @@ int check_qkv(const vsa2_heads* x, const vsa2_heads* y, int n, bool* empty) {
         x[i].dtype != x[0].dtype || y[i].dtype != y[0].dtype)
       return VSA2_ERR_INVALID_ARG;
     if (x[i].heads > 0 && x[i].batch > 0 && x[i].tokens > 0) *empty = false;
+    heads += x[i].heads;
   }
+  if (heads > 1 << 20) return VSA2_ERR_UNSUPPORTED;
   if ((int64_t)x[0].batch * ((int64_t)x[0].tokens / 16 + 1) > 0x7fffffffLL || x[0].tokens > 0x7fffffff - 64) return VSA2_ERR_UNSUPPORTED;
   return VSA2_OK;
+}
+
+// a norm and its weights (NULL: ones)
+int check_norm(const vsa2_qk_norm& norm) {
+  if (!(norm.eps >= 0.f)) return VSA2_ERR_INVALID_ARG;
+  return aligned4(norm.q_weight) && aligned4(norm.k_weight) ? VSA2_OK : VSA2_ERR_MISALIGNED;
 }
 
 int check_fp8(const vsa2_fp8* v, int rows, int cols) {
   if (rows == 0 || cols == 0) return VSA2_OK;
   if (v->values == nullptr || v->scales == nullptr || v->ld < cols) return VSA2_ERR_INVALID_ARG;
-  if (!aligned16(v->values) || v->ld % 16 || (reinterpret_cast<uintptr_t>(v->scales) & 3u)) return VSA2_ERR_MISALIGNED;
+  if (!aligned16(v->values) || v->ld % 16 || !aligned4(v->scales)) return VSA2_ERR_MISALIGNED;
   return VSA2_OK;
 }
 Fp8Arg fp8_arg(const vsa2_fp8* v) {
@@ -1046,7 +1057,7 @@ int vsa2_qkv_fwd(const vsa2_rope* rope, const vsa2_place* place, const vsa2_qk_n
   if (rc != VSA2_OK) return rc;
   QkvArgs a = {};
   if ((rc = fill_turn(rope, place, x[0], false, &a.turn)) != VSA2_OK) return rc;
-  if (norm != nullptr && !(norm->eps >= 0.f)) return VSA2_ERR_INVALID_ARG;
+  if (norm != nullptr && (rc = check_norm(*norm)) != VSA2_OK) return rc;
   if (empty) return VSA2_OK;
   if ((rc = check_device()) != VSA2_OK) return rc;
   for (int i = 0; i < 3; ++i) {
@@ -1077,8 +1088,9 @@ int vsa2_qkv_bwd(const vsa2_rope* rope, const vsa2_place* place, const vsa2_qk_n
   if ((rc = fill_turn(rope, place, dy[0], true, &a.turn)) != VSA2_OK) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   HeadsPair fwd = {};
+  if (!aligned4(d_q_weight) || !aligned4(d_k_weight)) return VSA2_ERR_MISALIGNED;
   if (norm != nullptr) {
-    if (!(norm->eps >= 0.f)) return VSA2_ERR_INVALID_ARG;
+    if ((rc = check_norm(*norm)) != VSA2_OK) return rc;
     for (int i = 0; i < 2; ++i) {
       if ((rc = check_heads(x[i], false)) != VSA2_OK) return rc;
       if (!same_shape(x[i], dy[i]) || x[i].dtype != x[0].dtype) return VSA2_ERR_INVALID_ARG;

@@ -412,6 +412,7 @@ cudaError_t launch_qkv_bwd(QkvArgs a, const HeadsPair& fwd, int D, int batch, in
   int share[2] = {nq == 0 ? 0 : ctas, nk == 0 ? 0 : ctas};
   if (nq > 0 && nk > 0) {
     share[0] = (int)((long long)ctas * (nq + 3) / (nq + nk + 6));
+    share[0] = share[0] < 1 ? 1 : share[0] >= ctas ? ctas - 1 : share[0];
     share[1] = ctas - share[0];
   }
   for (int i = 0; i < 2; ++i) {

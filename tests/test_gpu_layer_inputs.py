@@ -346,3 +346,11 @@ def test_weights_at_any_fp32_address():
         p.w[i] = room[at:at + 128]
     got, (dx2, dw2) = p.forward(), p.backward()
     assert all(torch.equal(a, b) for a, b in zip((*want, *dx, *dw), (*got, *dx2, *dw2)))
+
+
+@pytest.mark.parametrize("hq,hk", [(1, 3000), (3000, 1)])
+def test_one_head_beside_thousands(hq, hk):
+    """Each side keeps a CTA of its own."""
+    p = Problem(1, hq, hk, (1, 2, 3), 0, 64, (16, 24, 24), vb.ROPE_PAIRS, seed=14)
+    p.check_forward(p.forward())
+    p.check_backward(*p.backward())

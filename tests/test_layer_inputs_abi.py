@@ -135,6 +135,24 @@ def test_norm_and_gradient_refusals(lib):
     assert lib.vsa2_qkv_fwd(C.byref(rope), C.byref(at), C.byref(vb.QkNorm(256, 256, -1.0, 0)), three, three, None) == vb.ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("q_weight,k_weight,d_q_weight,d_k_weight", [(258, 256, 256, 256), (256, 257, 256, 256), (256, 256, 258, 256), (256, 256, 256, 259)])
+def test_weights_off_their_type_are_refused(lib, q_weight, k_weight, d_q_weight, d_k_weight):
+    rope, at, norm = vb.vsa2_rope_plan(64, (16, 24, 24)), place(), vb.QkNorm(q_weight, k_weight, 1e-6, 0)
+    three, two = (vb.Heads * 3)(heads(), heads(), heads()), (vb.Heads * 2)(heads(), heads())
+    need = vb.vsa2_qkv_bwd_workspace_bytes(64)
+    assert lib.vsa2_qkv_bwd(C.byref(rope), C.byref(at), C.byref(norm), two, three, three, d_q_weight, d_k_weight, 256, need, None) == vb.ERR_MISALIGNED
+    if q_weight % 4 or k_weight % 4:
+        assert lib.vsa2_qkv_fwd(C.byref(rope), C.byref(at), C.byref(norm), three, three, None) == vb.ERR_MISALIGNED
+
+
+def test_more_heads_than_a_call_takes_are_refused(lib):
+    """Three views whose heads together pass 32 bits, and one head more than a call takes."""
+    rope, at = vb.vsa2_rope_plan(64, (16, 24, 24)), place()
+    for n in ((1 << 30,) * 3, (1 << 20, 1, 0)):
+        three = (vb.Heads * 3)(*(heads(batch=1, heads=h, tokens=1) for h in n))
+        assert lib.vsa2_qkv_fwd(C.byref(rope), C.byref(at), None, three, three, None) == vb.ERR_UNSUPPORTED
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(rows=-1), vb.ERR_INVALID_ARG),
     (dict(x=None), vb.ERR_INVALID_ARG),
