@@ -74,6 +74,7 @@ struct Turn {
   static constexpr int N = HALVES ? 8 : 4;
   float c[N], s[N];
   int partner;      // lane of the warp (HALVES)
+  int active;       // pairs of this thread that turn (HALVES: all 8 or none); the other channels stay as they are, infinities among them
 
   __device__ __forceinline__ void init(const TurnArgs& t, int b, int tok, int l) {
     int pos[3] = {0, 0, 0};
@@ -93,6 +94,7 @@ struct Turn {
     }
     const int lane = threadIdx.x & 31;
     partner = lane;
+    active = !turns ? 0 : HALVES ? (l * 4 < t.pairs ? N : 0) : min(max(t.pairs - l * N, 0), N);
     if (HALVES) {
       const int chunk = t.pairs >> 3;
       partner = l < chunk ? lane + chunk : l < 2 * chunk ? lane - chunk : lane;
@@ -121,10 +123,14 @@ struct Turn {
   __device__ __forceinline__ void apply(float (&f)[8]) const {
     if (HALVES) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = f[i] * c[i % N] + __shfl_sync(0xffffffffu, f[i], partner) * s[i % N];
+      for (int i = 0; i < 8; ++i) {
+        const float other = __shfl_sync(0xffffffffu, f[i], partner);
+        if (active > 0) f[i] = f[i] * c[i % N] + other * s[i % N];
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        if (i >= active) continue;
         const float x = f[2 * i], y = f[2 * i + 1];
         f[2 * i] = x * c[i % N] - y * s[i % N];
         f[2 * i + 1] = x * s[i % N] + y * c[i % N];

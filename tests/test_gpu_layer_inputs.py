@@ -354,3 +354,32 @@ def test_one_head_beside_thousands(hq, hk):
     p = Problem(1, hq, hk, (1, 2, 3), 0, 64, (16, 24, 24), vb.ROPE_PAIRS, seed=14)
     p.check_forward(p.forward())
     p.check_backward(*p.backward())
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("dim,channels,layout", [(64, (2, 0, 4), vb.ROPE_PAIRS), (64, (16, 0, 0), vb.ROPE_HALVES), (128, (44, 42, 40), vb.ROPE_PAIRS),
+                                                 (128, (32, 32, 48), vb.ROPE_HALVES), (128, (0, 0, 0), vb.ROPE_PAIRS)])
+def test_what_does_not_turn_stays_as_it_is(dim, channels, layout, dtype):
+    """Channels behind the last pair, and all channels of rows behind the grid: bit for bit, whatever their neighbours hold."""
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    grid, text, total = (2, 2, 3), 5, sum(channels)
+    n = 12 + text
+    x = randn(gen, 2, n, 3, dim, dtype=dtype).transpose(1, 2)
+    odd = torch.tensor([float("inf"), -float("inf"), -0.0, 0.0, 1.0, float("nan"), -3.0], device="cuda", dtype=dtype)
+    room = x[..., total:].numel()
+    x[..., total:] = odd[torch.randint(len(odd), (room,), generator=gen, device="cuda")].view(x[..., total:].shape)
+    x[:, :, 12:] = odd[torch.randint(len(odd), (x[:, :, 12:].numel(),), generator=gen, device="cuda")].view(x[:, :, 12:].shape)
+    rope = vb.vsa2_rope_plan(dim, channels, layout=layout)
+
+    def same(a, b):
+        bits = torch.int16 if dtype == BF else torch.int32
+        return bool((a.isnan() == b.isnan()).all()) and bool(((a.contiguous().view(bits) == b.contiguous().view(bits)) | a.isnan()).all())
+
+    for inverse in (False, True):
+        y = torch.zeros_like(x)
+        vb.vsa2_rope_apply(rope, x, y, grid=grid, inverse=inverse)
+        assert same(y[..., total:], x[..., total:]) and same(y[:, :, 12:], x[:, :, 12:])
+        assert bool(y[:, :, :12, :total].isfinite().all())
+    dx = [torch.zeros_like(x) for _ in range(3)]
+    vb.vsa2_qkv_bwd(rope, (x,) * 2, (x,) * 3, dx, None, None, None, None, None, norm=False, grid=grid)
+    assert same(dx[0], y) and same(dx[1], y) and same(dx[2], x)
