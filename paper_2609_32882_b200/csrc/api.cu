@@ -358,6 +358,7 @@ int fill_turn(const vsa2_rope* rope, const vsa2_place* place, const vsa2_heads& 
   memset(t, 0, sizeof *t);
   t->sign = inverse ? -1.f : 1.f;
   t->H = t->W = 1;
+  t->by_H = t->by_W = divisor(1);
   if (rope == nullptr) return VSA2_OK;
   if (place == nullptr || rope->head_dim != shape.channels || (rope->layout != VSA2_ROPE_PAIRS && rope->layout != VSA2_ROPE_HALVES))
     return VSA2_ERR_INVALID_ARG;
@@ -384,6 +385,8 @@ int fill_turn(const vsa2_rope* rope, const vsa2_place* place, const vsa2_heads& 
   if (hw > 0x7fffffffLL || place->grid_t > 0x7fffffffLL / hw) return VSA2_ERR_UNSUPPORTED;
   t->H = place->grid_h;
   t->W = place->grid_w;
+  t->by_H = divisor(t->H);
+  t->by_W = divisor(t->W);
   t->L = place->grid_t * hw;
   t->first = place->first;
   return VSA2_OK;

@@ -56,6 +56,7 @@ struct MmArgs {
   int p_rows, q_rows, kb;            // kb: blocks of K
   int pt, qt, gq;                    // tiles along P, along Q; tiles along Q that are taken together
   int splits, chunk;                 // ranges that K is cut into; most blocks of K in one accumulator
+  Divisor by_tiles, by_group, by_gq, by_rest, by_splits;      // pt qt; gq pt; gq, and what the last group has of tiles along Q
   int tensor_stores;                 // C lies as tensor copies need it
   const uint32_t* p_scales;
   const uint32_t* q_scales;
@@ -88,12 +89,12 @@ struct MmWalk {
     } else {
       const int tiles = a.pt * a.qt;
       if (item >= tiles * a.splits) return false;
-      split = item / tiles;
-      const int tile = item - split * tiles, per = a.gq * a.pt, g = tile / per, r = tile - g * per, w = min(a.gq, a.qt - g * a.gq);
-      p = r / w;
+      split = divided(item, a.by_tiles);
+      const int tile = item - split * tiles, g = divided(tile, a.by_group), r = tile - g * a.gq * a.pt, w = min(a.gq, a.qt - g * a.gq);
+      p = w == a.gq ? divided(r, a.by_gq) : divided(r, a.by_rest);
       q = g * a.gq + r - p * w;
-      r0 = (int)((long long)a.kb * split / a.splits);
-      r1 = (int)((long long)a.kb * (split + 1) / a.splits);
+      r0 = divided(a.kb * split, a.by_splits);      // (at most 2^23 blocks and 16 ranges)
+      r1 = divided(a.kb * (split + 1), a.by_splits);
       item += all;
       kb0 = r0;
     }
@@ -533,11 +534,11 @@ done:
 
 // The ranges of K, each a matrix [m, ldp] in fp32, added in their order.  Four elements of a row a thread.
 template <typename TO>
-__global__ void __launch_bounds__(256) fp8_sum_kernel(const float* parts, int splits, int m, int n, long long ldp, TO* __restrict__ c, long long ldc) {
+__global__ void __launch_bounds__(256) fp8_sum_kernel(const float* parts, int splits, int m, int n, long long ldp, Divisor by_row, TO* __restrict__ c, long long ldc) {
   grid_enter();
-  const long long per_row = ldp / 4, i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
+  const int i = blockIdx.x * 256 + threadIdx.x, row = divided(i, by_row);      // (the parts have 4.3 million elements at most)
   if (row >= m) return;
-  const int col = (int)(i - row * per_row) * 4;
+  const int col = (i - row * (int)(ldp / 4)) * 4;
   const float* from = parts + row * ldp + col;
   float4 v[kMmSplits];
 #pragma unroll
@@ -637,6 +638,11 @@ cudaError_t launch_tiles(const MmCall& c, const MmPlan& plan, void* result, long
   const long long group = (48LL << 20) / ((long long)NT * c.kb * 128);
   a.gq = (int)(group < 4 ? 4 : group > 37 ? 37 : group);
   if (a.gq > a.qt) a.gq = a.qt;
+  a.by_tiles = divisor((long long)a.pt * a.qt);
+  a.by_group = divisor((long long)a.gq * a.pt);
+  a.by_gq = divisor(a.gq);
+  a.by_rest = divisor(a.qt % a.gq > 0 ? a.qt % a.gq : a.gq);
+  a.by_splits = divisor(a.splits);
   a.chunk = c.f32 ? kMmChunk : c.kb;
   a.tensor_stores = sizeof(TO) == 2 && c.tensor_stores;
   a.p_scales = reinterpret_cast<const uint32_t*>(p.scales);
@@ -664,8 +670,9 @@ cudaError_t launch_mm(const MmCall& c, const MmPlan& plan) {
   const cudaError_t e = launch_tiles<NT, PAIR, false, float>(c, plan, c.parts, ldp, c.m * ldp);
   if (e != cudaSuccess) return e;
   const unsigned grid = (unsigned)((c.m * ldp / 4 + 255) / 256);
-  return c.f32 ? launch_kernel(fp8_sum_kernel<float>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, reinterpret_cast<float*>(c.c), c.ldc)
-               : launch_kernel(fp8_sum_kernel<bf16>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, reinterpret_cast<bf16*>(c.c), c.ldc);
+  const Divisor by_row = divisor(ldp / 4);
+  return c.f32 ? launch_kernel(fp8_sum_kernel<float>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, by_row, reinterpret_cast<float*>(c.c), c.ldc)
+               : launch_kernel(fp8_sum_kernel<bf16>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, by_row, reinterpret_cast<bf16*>(c.c), c.ldc);
 }
 
 // most elements of a product whose K is cut: tiles x ranges are at most the CTAs (or pairs)

@@ -13,10 +13,23 @@ struct HeadsArg {
 };
 struct HeadsPair { HeadsArg v[2]; };
 
+// n / d for 0 <= n < 2^31 and 0 < d < 2^31 by a product and a shift: with l = ceil(log2 d) and m = ceil(2^(31 + l) / d), which has 32 bits, m d is less than 2^l above
+// 2^(31 + l), so n m / 2^(31 + l) lies less than 1 / d above n / d
+struct Divisor {
+  uint32_t m;
+  int l;
+};
+inline Divisor divisor(long long d) {
+  const int l = d > 1 ? 64 - __builtin_clzll((unsigned long long)d - 1) : 0;
+  return Divisor{(uint32_t)(((1ULL << (31 + l)) + (unsigned long long)d - 1) / (unsigned long long)d), l};
+}
+__device__ __forceinline__ int divided(int n, const Divisor& by) { return (int)(__umulhi(2u * (uint32_t)n, by.m) >> by.l); }
+
 struct TurnArgs {
   unsigned long long turn[64];      // 2^-64 turns per position of every pair
   int pairs, pairs_t, pairs_th;     // pairs that turn; those below pairs_t turn with t, below pairs_th with h, the others with w
   int H, W;                         // grid, L = T H W
+  Divisor by_H, by_W;
   long long L;
   int first;                        // row of the views' first token
   float sign;                       // -1: the inverse
@@ -28,7 +41,8 @@ struct QkvArgs {
   const float* w[2];                // norm weights of q and k, null: ones
   float eps;
   int norm, tokens;
-  int tiles, jobs, per_cta;         // (set by the launcher) token tiles of a batch entry and of all, heads per CTA
+  int tiles, jobs, per_cta;         // (set by the launcher, with their divisors) token tiles of a batch entry and of all, heads per CTA
+  Divisor by_tiles, by_jobs;
   TurnArgs turn;
 };
 size_t qkv_bwd_workspace_bytes(int D);

@@ -11,8 +11,8 @@
 // All of it is bound by memory: every element is read once and written once, the few operations hide behind that.  A team of D / 8
 // threads holds one row of one head, 8 channels a thread; it keeps its token and walks through the heads, so that a token's sines and
 // cosines (and the norm weights) are formed once, and the reads of a CTA's tokens are whole rows of the projection.  At 75,600 tokens: rotation of 40
-// heads 240 us (6.4 TB/s), norms, rotation and heads of 3 x 40 heads 755 us (6.2 TB/s), backward of 3 x 20 heads 484 us (6.4 TB/s); a copy reaches 6.45.
-// With few tokens it is the latency of one row (2048 tokens, 3 x 12 heads: 9.7 us; 256 tokens, 3 x 2: 3.9 us).
+// heads 239 us (6.5 TB/s), norms, rotation and heads of 3 x 40 heads 736 us (6.3 TB/s), backward of 3 x 20 heads 484 us (6.4 TB/s); a copy reaches 6.45.
+// With few tokens it is the latency of one row (2048 tokens, 3 x 12 heads: 8.7 us; 256 tokens, 3 x 2: 3.6 us).
 #include "common.cuh"
 #include "heads.cuh"
 
@@ -76,46 +76,47 @@ struct Turn {
   int partner;      // lane of the warp (HALVES)
   int active;       // pairs of this thread that turn (HALVES: all 8 or none); the other channels stay as they are, infinities among them
 
-  __device__ __forceinline__ void init(const TurnArgs& t, int b, int tok, int l) {
+  // `turns`: t.turn, in shared memory
+  __device__ __forceinline__ void init(const TurnArgs& t, const unsigned long long* turns, int b, int tok, int l) {
     int pos[3] = {0, 0, 0};
-    bool turns = t.pairs > 0;
+    active = HALVES ? (l * 4 < t.pairs ? N : 0) : min(max(t.pairs - l * N, 0), N);
     if (t.positions != nullptr) {
       const int* p = t.positions + b * t.positions_sb + (long long)tok * 3;
       pos[0] = p[0]; pos[1] = p[1]; pos[2] = p[2];
     } else {
       const long long r = (long long)t.first + tok;
-      turns = turns && r < t.L;
-      if (turns) {
-        const int rr = (int)r, th = rr / t.W;
+      if (r < t.L) {
+        const int rr = (int)r, th = divided(rr, t.by_W);
         pos[2] = rr - th * t.W;
-        pos[0] = th / t.H;
+        pos[0] = divided(th, t.by_H);
         pos[1] = th - pos[0] * t.H;
+      } else {
+        active = 0;
       }
     }
-    const int lane = threadIdx.x & 31;
-    partner = lane;
-    active = !turns ? 0 : HALVES ? (l * 4 < t.pairs ? N : 0) : min(max(t.pairs - l * N, 0), N);
+    int p0 = l * N;                     // the thread's first pair
+    float sign = t.sign;
     if (HALVES) {
-      const int chunk = t.pairs >> 3;
+      const int lane = threadIdx.x & 31, chunk = t.pairs >> 3;
       partner = l < chunk ? lane + chunk : l < 2 * chunk ? lane - chunk : lane;
+      if (p0 < t.pairs) sign = -sign;   // (the first half: x cos - partner sin)
+      else p0 -= t.pairs;
     }
+    if (active > 0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      int p = HALVES ? l * 8 + i : l * 4 + i;
-      float sign = t.sign;
-      if (HALVES) {
-        if (p < t.pairs) sign = -sign;      // (the first half: x cos - partner sin)
-        else p -= t.pairs;
-      }
-      c[i] = 1.f;
-      s[i] = 0.f;
-      if (turns && p < t.pairs) {
-        const int at = p < t.pairs_t ? pos[0] : p < t.pairs_th ? pos[1] : pos[2];
-        const unsigned long long angle = t.turn[p] * (unsigned long long)(long long)at;
-        float sn, cs;
-        sincospif((float)(int)(angle >> 32) * 0x1p-31f, &sn, &cs);
-        c[i] = cs;
-        s[i] = sign * sn;
+      for (int i = 0; i < N; i += 2) {
+        const ulonglong2 both = *reinterpret_cast<const ulonglong2*>(turns + p0 + i);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const unsigned long long turn = k == 0 ? both.x : both.y;
+          const int p = p0 + i + k, at = p < t.pairs_t ? pos[0] : p < t.pairs_th ? pos[1] : pos[2];
+          // upper half of turn * at modulo 2^64
+          const uint32_t lo = (uint32_t)turn, angle = (uint32_t)(turn >> 32) * (uint32_t)at + __umulhi(lo, (uint32_t)at) - (at < 0 ? lo : 0u);
+          float sn, cs;
+          sincospif((float)(int)angle * 0x1p-31f, &sn, &cs);
+          c[i + k] = cs;
+          s[i + k] = sign * sn;
+        }
       }
     }
   }
@@ -139,6 +140,13 @@ struct Turn {
   }
 };
 
+// t.turn for the CTA's threads.  (A warp that reads the kernel's arguments at 16 places waits for one after the other: 480p, 12 heads on 3, backward 160 us
+// instead of 153, forward of 2048 tokens 10.0 instead of 9.1.  Quotients as products (Divisor) then gave 148.5 and 8.7.)
+__device__ __forceinline__ void share_turns(const TurnArgs& t, unsigned long long* turns) {
+  if (threadIdx.x < 64) turns[threadIdx.x] = t.turn[threadIdx.x];
+  __syncthreads();
+}
+
 template <int TEAM>
 __device__ __forceinline__ float team_sum(float v) {
 #pragma unroll
@@ -150,14 +158,16 @@ __device__ __forceinline__ float team_sum(float v) {
 template <int D, typename TI, typename TO, bool HALVES>
 __global__ void __launch_bounds__(kQkvThreads) qkv_fwd_kernel(const __grid_constant__ QkvArgs a) {
   constexpr int TEAM = D / 8, ROWS = kQkvThreads / TEAM, U = sizeof(TI) == 2 ? 4 : 2;
+  __shared__ __align__(16) unsigned long long turns[64];
+  share_turns(a.turn, turns);
   grid_enter();
   const int l = threadIdx.x % TEAM;
-  const int b = blockIdx.x / a.tiles, tile = blockIdx.x - b * a.tiles;
+  const int b = divided(blockIdx.x, a.by_tiles), tile = blockIdx.x - b * a.tiles;
   const int row = tile * ROWS + threadIdx.x / TEAM;
   const bool valid = row < a.tokens;
   const int tok = min(row, a.tokens - 1);
   Turn<D, HALVES> turn;
-  turn.init(a.turn, b, tok, l);
+  turn.init(a.turn, turns, b, tok, l);
   const int h_lo = blockIdx.z * a.per_cta, h_hi = h_lo + a.per_cta;
   int base = 0;
 #pragma unroll 1
@@ -210,6 +220,8 @@ __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(co
                                                                         const __grid_constant__ BwdJobs list, float* __restrict__ partial) {
   constexpr int TEAM = D / 8, ROWS = kQkvThreads / TEAM;
   constexpr int GV = sizeof(TG) / 2, XV = sizeof(TI) / 2, AHEAD = bwd_ahead(GV + XV, HALVES);      // 16-byte pieces of a row of dy, of x
+  __shared__ __align__(16) unsigned long long turns[64];
+  share_turns(a.turn, turns);
   grid_enter();
   extern __shared__ __align__(16) unsigned char qkv_smem[];
   uint4* const queue = reinterpret_cast<uint4*>(qkv_smem) + threadIdx.x;      // [AHEAD][GV + XV][thread]
@@ -217,7 +229,7 @@ __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(co
   // batch entry and token of a tile (a row behind the last one repeats it)
   struct Place { int b, tok; bool valid; };
   auto place = [&](int at) {
-    const int b = at / a.tiles, row = (at - b * a.tiles) * ROWS + slot;
+    const int b = divided(at, a.by_tiles), row = (at - b * a.tiles) * ROWS + slot;
     return Place{b, min(row, a.tokens - 1), row < a.tokens};
   };
   {
@@ -237,7 +249,7 @@ __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(co
     const TI* ask_x = nullptr;
     auto ask = [&](int s) {
       if (ask_h == ask_hi && ask_job < jobs) {
-        const int group = ask_job / a.jobs, lo = group * per;
+        const int group = divided(ask_job, a.by_jobs), lo = group * per;
         const Place at = place(ask_job - group * a.jobs);
         ask_job += stride;
         ask_h = lo;
@@ -263,10 +275,10 @@ __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(co
     for (int s = 0; s < AHEAD - 1; ++s) ask(s);
     int s = 0;
     for (int job = first; job < jobs; job += stride) {
-      const int group = job / a.jobs, lo = group * per, hi = min(lo + per, g.heads);
+      const int group = divided(job, a.by_jobs), lo = group * per, hi = min(lo + per, g.heads);
       const Place at = place(job - group * a.jobs);
       Turn<D, HALVES> turn;
-      turn.init(a.turn, at.b, at.tok, l);
+      turn.init(a.turn, turns, at.b, at.tok, l);
       TO* yp = reinterpret_cast<TO*>(y.p) + at.b * y.sb + at.tok * y.st + lo * y.sh + l * 8;
       for (int h = lo; h < hi; ++h, yp += y.sh) {
         asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 2) : "memory");
@@ -390,6 +402,8 @@ cudaError_t launch_qkv_fwd(QkvArgs a, int D, int batch, int in_f32, int out_f32,
   if ((e = sm_count(&sms)) != cudaSuccess) return e;
   a.tiles = (a.tokens + rows - 1) / rows;
   a.jobs = a.tiles * batch;
+  a.by_tiles = divisor(a.tiles);
+  a.by_jobs = divisor(a.jobs);
   a.per_cta = heads_per_cta(a.jobs, heads, in_f32 ? 2 : 4, sms);
   const dim3 grid(a.jobs, 1, (heads + a.per_cta - 1) / a.per_cta);
   return by_types(in_f32, out_f32, [&](auto ti, auto to) {
@@ -410,14 +424,16 @@ cudaError_t launch_qkv_bwd(QkvArgs a, const HeadsPair& fwd, int D, int batch, in
   if ((e = sm_count(&sms)) != cudaSuccess) return e;
   a.tiles = (a.tokens + rows - 1) / rows;
   a.jobs = a.tiles * batch;
-  // CTAs for q and for k by what a tile of theirs costs: its heads and the sines and cosines of its tokens, about three heads' worth (by the heads alone 40 q heads on one k
-  // head waited for the k CTAs, 550 us; one head's worth 315, two 241, three 218).  Heads go in groups where that makes the rounds of jobs even.
+  a.by_tiles = divisor(a.tiles);
+  a.by_jobs = divisor(a.jobs);
+  // CTAs for q and for k by what a tile of theirs costs: its heads and the sines and cosines of its tokens, about two heads' worth (40 q heads on one k head: one
+  // head's worth 236 us, two 201, three 203; by the heads alone q waited for the k CTAs, more than twice that).  Heads go in groups where that makes the rounds of jobs even.
   BwdJobs list = {};
   const int at_once = (halves ? 3 : 4) * sms, ctas = at_once < kQkvParts ? at_once : kQkvParts;
   const int nq = a.x[0].heads, nk = a.x[1].heads;
   int share[2] = {nq == 0 ? 0 : ctas, nk == 0 ? 0 : ctas};
   if (nq > 0 && nk > 0) {
-    share[0] = (int)((long long)ctas * (nq + 3) / (nq + nk + 6));
+    share[0] = (int)((long long)ctas * (nq + 2) / (nq + nk + 4));
     share[0] = share[0] < 1 ? 1 : share[0] >= ctas ? ctas - 1 : share[0];
     share[1] = ctas - share[0];
   }

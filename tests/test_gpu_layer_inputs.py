@@ -383,3 +383,20 @@ def test_what_does_not_turn_stays_as_it_is(dim, channels, layout, dtype):
     dx = [torch.zeros_like(x) for _ in range(3)]
     vb.vsa2_qkv_bwd(rope, (x,) * 2, (x,) * 3, dx, None, None, None, None, None, norm=False, grid=grid)
     assert same(dx[0], y) and same(dx[1], y) and same(dx[2], x)
+
+
+@pytest.mark.parametrize("grid", [(1, 46337, 46341), (2147483647, 1, 1), (1, 1, 2147483647), (3, 715827882, 1), (7, 17, 18046080), (65535, 181, 181), (11, 2, 3)])
+def test_places_in_grids_of_any_shape(grid):
+    """Rows at both ends of grids up to 2^31 - 1 tokens, as positions from the grid and as the list of the same positions."""
+    gen = torch.Generator(device="cuda").manual_seed(16)
+    t, h, w = grid
+    rope = vb.vsa2_rope_plan(64, (16, 24, 24))
+    for first in (0, max(0, min(h * w - 7, t * h * w - 37)), t * h * w - 37):
+        x = randn(gen, 1, 1, 37, 64, dtype=F)
+        r = torch.arange(first, first + 37, device="cuda")
+        assert int(r[-1]) < t * h * w
+        pos = torch.stack([r // (h * w), r // w % h, r % w], dim=-1).to(torch.int32)
+        a, b = torch.empty_like(x), torch.empty_like(x)
+        vb.vsa2_rope_apply(rope, x, a, grid=grid, first=first)
+        vb.vsa2_rope_apply(rope, x, b, positions=pos)
+        assert torch.equal(a, b)
