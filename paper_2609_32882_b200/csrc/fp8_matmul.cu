@@ -10,7 +10,7 @@
 // groups of four, half the columns each, for the epilogue; two accumulators in tensor memory, so that a tile's epilogue runs behind the next tile's products.
 //
 // What bounds it: in long runs the power limit, at which values of normal numbers draw a quarter more than small whole ones (75600 x 15360 x 5120: 4.6 - 4.8 ms, 2.5
-// PFLOP/s, against 3.7 ms and 3.2 PFLOP/s, twice the library's bf16 product); else the intake from L2 (8192 x 4096 x 4096 91 us: 51 bytes a cycle and SM, 600
+// PFLOP/s, against 3.7 ms and 3.2 PFLOP/s, twice the library's bf16 product); else the intake from L2 (8192 x 4096 x 4096 90 us: 51 bytes a cycle and SM, 600
 // cycles a block where the tensor cores need 448).  Tiles of 448 columns, both accumulators in one tile, need 27 % less intake and were as fast at large sizes (20000 x 15360 x
 // 5120 1028 us both ways), slower where rounds are few (4096^3 60 us instead of 52).  One row of A: the weights' bytes (15360 x 5120 16 us, 4.9 TB/s with the
 // launch); few tiles and short K: the launch, the first block's way from memory and the epilogue, 3 - 5 us.
@@ -713,8 +713,8 @@ cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Ar
   }
   if (!pair) return launch_mm<128, 1>(call, plan_mm<128, 1>(call, false));
   if (m <= 128) return launch_mm<128, 2>(call, plan_mm<128, 2>(call, false));
-  // The columns that waste least (256 x 4608 x 1536: two tiles of 128 instead of two of 224, 8.8 us instead of 9.9), and A's rows as the lanes, B's as the columns where that
-  // fills the rounds better (512 x 15360 x 5120: 138 tiles instead of 180 on 74 pairs, 35 us instead of 49)
+  // The columns that waste least (256 x 4608 x 1536: two tiles of 128 instead of two of 224, 8.2 us instead of 9.5), and A's rows as the lanes, B's as the columns where that
+  // fills the rounds better (512 x 15360 x 5120: 138 tiles instead of 180 on 74 pairs, 33 us instead of 45)
   const MmPlan wide = plan_mm<224, 2>(call, false), narrow = plan_mm<128, 2>(call, false);
   if (call.tensor_stores) {
     const MmPlan swapped = plan_mm<224, 2>(call, true);
