@@ -356,24 +356,32 @@ __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(co
   }
 }
 
-// Sums of the CTAs' partial sums in a fixed order: 32 columns a CTA, every 32nd part a warp row.  grid (columns / 32, 2: q, k)
+// Sums of the CTAs' partial sums in a fixed order: 8 columns a CTA, 128 parts at a time, so that a thread's few loads are under way together.  grid (columns / 8, 2: q, k)
 __global__ void __launch_bounds__(1024) qkv_bwd_reduce_kernel(const float* partial, int q_ctas, int qk_ctas, int D, float* __restrict__ dwq,
                                                               float* __restrict__ dwk) {
+  constexpr int MOST = kQkvParts / 128;
   grid_enter();
-  __shared__ float red[32][33];
-  const int lane = threadIdx.x & 31, col = blockIdx.x * 32 + lane, first = threadIdx.x >> 5;
-  const int lo = blockIdx.y == 0 ? 0 : q_ctas, hi = blockIdx.y == 0 ? q_ctas : qk_ctas;
+  __shared__ float red[32][8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 8 + (lane & 7);
+  const int lo = blockIdx.y == 0 ? 0 : q_ctas, hi = blockIdx.y == 0 ? q_ctas : qk_ctas, first = lo + warp * 4 + (lane >> 3);
+  float v[MOST];
+#pragma unroll
+  for (int u = 0; u < MOST; ++u) v[u] = first + u * 128 < hi ? partial[(size_t)(first + u * 128) * D + col] : 0.f;
   float sum = 0.f;
-#pragma unroll 8
-  for (int p = lo + first; p < hi; p += 32) sum += partial[(size_t)p * D + col];
-  red[first][lane] = sum;
+#pragma unroll
+  for (int u = 0; u < MOST; ++u) sum += v[u];
+  sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+  sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+  if (lane < 8) red[warp][lane] = sum;
   __syncthreads();
-  if (first == 0) {
+  if (warp == 0) {
     float total = 0.f;
 #pragma unroll
-    for (int r = 0; r < 32; ++r) total += red[r][lane];
+    for (int r = 0; r < 8; ++r) total += red[(lane >> 3) * 8 + r][lane & 7];
+    total += __shfl_xor_sync(0xffffffffu, total, 8);
+    total += __shfl_xor_sync(0xffffffffu, total, 16);
     float* out = blockIdx.y == 0 ? dwq : dwk;
-    if (out != nullptr) out[col] = total;
+    if (lane < 8 && out != nullptr) out[col] = total;
   }
 }
 
@@ -475,7 +483,7 @@ cudaError_t launch_qkv_bwd(QkvArgs a, const HeadsPair& fwd, int D, int batch, in
   };
   e = by_types(g_f32, out_f32, [&](auto tg, auto to) { return x_f32 ? go(float(), tg, to) : go(bf16(), tg, to); });
   if (e != cudaSuccess || !a.norm) return e;
-  return launch_kernel(qkv_bwd_reduce_kernel, dim3(D / 32, 2), 1024, 0, st, partial, list.ctas[0], list.ctas[0] + list.ctas[1], D, dwq, dwk);
+  return launch_kernel(qkv_bwd_reduce_kernel, dim3(D / 8, 2), 1024, 0, st, partial, list.ctas[0], list.ctas[0] + list.ctas[1], D, dwq, dwk);
 }
 
 }  // namespace vsa2
