@@ -43,6 +43,10 @@ template <> struct Oct<false> {
   __device__ __forceinline__ void set(const void* x, size_t at, int j) {
     u[j / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(x)[at] << 16 * (j & 1);
   }
+  __device__ __forceinline__ void keep(int n) {      // the first n of the eight
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = 2 * j + 1 < n ? u[j] : 2 * j < n ? u[j] & 0xffffu : 0u;
+  }
   __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? u[j / 2] & 0xffff0000u : u[j / 2] << 16); }
   __device__ __forceinline__ uint32_t top() const {
     const uint32_t t = __vmaxu2(__vmaxu2(u[0] & 0x7fff7fffu, u[1] & 0x7fff7fffu), __vmaxu2(u[2] & 0x7fff7fffu, u[3] & 0x7fff7fffu));
@@ -76,6 +80,11 @@ template <> struct Oct<true> {
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
   }
   __device__ __forceinline__ void set(const void* x, size_t at, int j) { f[j] = reinterpret_cast<const float*>(x)[at]; }
+  __device__ __forceinline__ void keep(int n) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j >= n) f[j] = 0.f;
+  }
   __device__ __forceinline__ float get(int j) const { return f[j]; }
   __device__ __forceinline__ uint32_t top() const {
     uint32_t t = 0u;
@@ -103,16 +112,77 @@ __device__ __forceinline__ uint32_t finite_top(const Oct<F32>& o) {
     if (finite_bits(o.get(j))) t = max(t, __float_as_uint(o.get(j)) & 0x7fffffffu);
   return t;
 }
-// elements i .. i+7 of a row of `cols` (zeros beyond it); VEC: rows lie on 16-byte boundaries
+// The matrix that is read
+struct Source {
+  const unsigned char* x;
+  int rows, cols;
+  long long ld;
+};
+// words of the pieces from the byte on that the row begins at, `from` (0 .. 15) of the first piece
+__device__ __forceinline__ void set_words(const uint32_t (&w)[8], uint32_t from, Oct<false>& o) {
+  uint32_t a[6], b[5];
+#pragma unroll
+  for (int k = 0; k < 6; ++k) a[k] = from & 8 ? w[k + 2] : w[k];
+#pragma unroll
+  for (int k = 0; k < 5; ++k) b[k] = from & 4 ? a[k + 1] : a[k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o.u[k] = __funnelshift_r(b[k], b[k + 1], (from & 2) * 8);
+}
+__device__ __forceinline__ void set_words(const uint32_t (&w)[12], uint32_t from, Oct<true>& o) {
+  uint32_t a[10];
+#pragma unroll
+  for (int k = 0; k < 10; ++k) a[k] = from & 8 && k + 2 < 12 ? w[k + 2] : w[k];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) o.f[k] = __uint_as_float(from & 4 ? a[k + 1] : a[k]);
+}
+// Elements i .. i+7 of a row (zeros beyond it)
 template <bool F32, bool VEC>
-__device__ __forceinline__ void load8(const void* x, size_t row_at, int i, int cols, Oct<F32>& o) {
-  if (VEC && i + 8 <= cols) {
-    o.load(x, row_at + i);
+__device__ __forceinline__ void load8(const Source& m, size_t row_at, int i, Oct<F32>& o) {
+  if (VEC && i + 8 <= m.cols) {
+    o.load(m.x, row_at + i);
   } else {
     o.zero();
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (i + j < cols) o.set(x, row_at + i + j, j);
+      if (i + j < m.cols) o.set(m.x, row_at + i + j, j);
+  }
+}
+// Rows that do not begin on 16-byte boundaries: N octs, `step` bytes and COLUMNS columns apart, of which `there` exist (zeros for the others).  The aligned pieces that an oct lies in, those of all N asked for before the first is shifted into place, where the matrix has all of these bytes; single elements at
+// its two ends.  (Single elements everywhere: 20001 x 5001 71 us, both forms 143)
+template <bool F32, int N, int COLUMNS>
+__device__ __forceinline__ void load_shifted(const Source& m, long long row, int col, int there, long long step, Oct<F32>* o) {
+  constexpr int SIZE = F32 ? 4 : 2, PIECES = SIZE / 2 + 1;
+  const size_t at = (size_t)row * m.ld + col;
+  const unsigned char* const a = m.x + at * SIZE;
+  const long long before = at * SIZE, behind = ((long long)(m.rows - 1) * m.ld + m.cols) * SIZE - before;      // bytes of the matrix on either side
+  uint32_t w[N][PIECES * 4];
+  bool inside[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const uint32_t from = (uint32_t)reinterpret_cast<uintptr_t>(a + k * step) & 15u;
+    inside[k] = k < there && col + COLUMNS * k < m.cols && before + k * step >= from && behind - k * step >= (int)(PIECES * 16 - from);
+    const uint4* piece = reinterpret_cast<const uint4*>(a + k * step - from);
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (inside[k]) v = piece[p];
+      w[k][4 * p] = v.x; w[k][4 * p + 1] = v.y; w[k][4 * p + 2] = v.z; w[k][4 * p + 3] = v.w;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int left = m.cols - col - COLUMNS * k;
+    set_words(w[k], (uint32_t)reinterpret_cast<uintptr_t>(a + k * step) & 15u, o[k]);
+    if (left < 8 || !inside[k]) {
+      if (inside[k]) {
+        o[k].keep(left);
+      } else if (k < there && left > 0) {
+        o[k].zero();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < left) o[k].set(a + k * step, j, j);
+      }
+    }
   }
 }
 // bytes i .. i+7 of a row of `cols` values (its start 16-byte aligned, i a multiple of 8)
@@ -138,15 +208,20 @@ __device__ __forceinline__ uint32_t team_max(uint32_t t) {      // of 16 threads
 
 // Rows alone: a team of 16 threads takes 512 columns of a row (four blocks, one word of scales).  grid (row tiles of 16, word groups)
 template <bool F32, bool VEC>
-__global__ void __launch_bounds__(kQzThreads) fp8_rows_kernel(const void* x, int rows, int cols, long long ld, Fp8Arg out) {
+__global__ void __launch_bounds__(kQzThreads, F32 ? 4 : 6) fp8_rows_kernel(const __grid_constant__ Source m, Fp8Arg out) {
   grid_enter();
+  const int rows = m.rows, cols = m.cols;
   const int l = threadIdx.x & 15;
   const long long row = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
   const int c0 = blockIdx.y * 512;
   const long long r = row < rows ? row : rows - 1;
   Oct<F32> o[4];
+  if constexpr (VEC) {
 #pragma unroll
-  for (int b = 0; b < 4; ++b) load8<F32, VEC>(x, (size_t)r * ld, c0 + b * 128 + l * 8, cols, o[b]);
+    for (int b = 0; b < 4; ++b) load8<F32, VEC>(m, (size_t)r * m.ld, c0 + b * 128 + l * 8, o[b]);
+  } else {
+    load_shifted<F32, 4, 128>(m, r, c0 + l * 8, 4, 128 * (F32 ? 4 : 2), o);
+  }
   uint32_t word = 0;
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
@@ -271,25 +346,30 @@ __device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint
 // as bytes: a thread writes the 8 bytes that its rows give a column; the 8-byte places of a column are exchanged by column group
 // so that neither side meets a bank twice.  grid (row tiles, column tiles)
 template <bool F32, bool VEC>
-__global__ void __launch_bounds__(kQzThreads, F32 ? 2 : 4) fp8_tile_kernel(const void* x, int rows, int cols, long long ld, int squares, Fp8Arg out,
-                                                              Fp8Arg out_t) {
+__global__ void __launch_bounds__(kQzThreads, F32 ? 2 : 4) fp8_tile_kernel(const __grid_constant__ Source m, int squares, Fp8Arg out, Fp8Arg out_t) {
   grid_enter();
   __shared__ __align__(16) TileShared sh;
+  const int rows = m.rows, cols = m.cols;
   const int l = threadIdx.x & 15, team = threadIdx.x >> 4;
   Oct<F32> o[8];
   uint32_t tops[8], top = 0;
   typename Oct<F32>::Tops cols_top;
-  const bool full = VEC && (blockIdx.x + 1) * 128 <= rows && (blockIdx.y + 1) * 128 <= cols;
-  if (full) {
-    const size_t at = (size_t)(blockIdx.x * 128 + team * 8) * ld + blockIdx.y * 128 + l * 8;
+  const bool full = (blockIdx.x + 1) * 128 <= rows && (blockIdx.y + 1) * 128 <= cols;
+  if (VEC && full) {
+    const size_t at = (size_t)(blockIdx.x * 128 + team * 8) * m.ld + blockIdx.y * 128 + l * 8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i].load(x, at + i * ld);
+    for (int i = 0; i < 8; ++i) o[i].load(m.x, at + i * m.ld);
   } else {
+    const int row = blockIdx.x * 128 + team * 8, col = blockIdx.y * 128 + l * 8;
+    if constexpr (VEC) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = blockIdx.x * 128 + team * 8 + i;
-      if (row < rows) load8<F32, VEC>(x, (size_t)row * ld, blockIdx.y * 128 + l * 8, cols, o[i]);
-      else o[i].zero();
+      for (int i = 0; i < 8; ++i) {
+        if (row + i < rows) load8<F32, VEC>(m, (size_t)(row + i) * m.ld, col, o[i]);
+        else o[i].zero();
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) load_shifted<F32, 4, 0>(m, row + i, col, rows - row - i, m.ld * (F32 ? 4 : 2), o + i);
     }
   }
 #pragma unroll
@@ -307,12 +387,12 @@ __global__ void __launch_bounds__(kQzThreads, F32 ? 2 : 4) fp8_tile_kernel(const
 cudaError_t launch_fp8_quantize(const void* x, int x_f32, int rows, int cols, long long ld, bool squares, const Fp8Arg& out,
                                 const Fp8Arg& out_t, cudaStream_t st) {
   const size_t bytes = x_f32 ? 4 : 2;
+  const Source m{reinterpret_cast<const unsigned char*>(x), rows, cols, ld};
   const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && (size_t)ld * bytes % 16 == 0;
   auto go = [&](auto rows_kernel, auto tile_kernel) {
     if (!squares && out_t.values == nullptr)
-      return launch_kernel(rows_kernel, dim3((rows + 15) / 16, (cols + 511) / 512), kQzThreads, 0, st, x, rows, cols, ld, out);
-    return launch_kernel(tile_kernel, dim3((rows + 127) / 128, (cols + 127) / 128), kQzThreads, 0, st, x, rows, cols, ld,
-                         squares ? 1 : 0, out, out_t);
+      return launch_kernel(rows_kernel, dim3((rows + 15) / 16, (cols + 511) / 512), kQzThreads, 0, st, m, out);
+    return launch_kernel(tile_kernel, dim3((rows + 127) / 128, (cols + 127) / 128), kQzThreads, 0, st, m, squares ? 1 : 0, out, out_t);
   };
   if (x_f32) return vec ? go(fp8_rows_kernel<true, true>, fp8_tile_kernel<true, true>) : go(fp8_rows_kernel<true, false>, fp8_tile_kernel<true, false>);
   return vec ? go(fp8_rows_kernel<false, true>, fp8_tile_kernel<false, true>) : go(fp8_rows_kernel<false, false>, fp8_tile_kernel<false, false>);

@@ -232,3 +232,27 @@ def test_long_sums_in_pieces_and_in_ranges():
             c = torch.full((m, n), float("nan"), dtype=dtype, device="cuda")
             vb.vsa2_fp8_matmul(a, b, c, ws)
             assert torch.equal(c, want.to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols,ld", [(1, 1, 1), (3, 9, 9), (130, 131, 133), (17, 520, 527), (129, 127, 1001), (5, 513, 513)])
+def test_rows_at_any_address(rows, cols, ld, dtype):
+    """A matrix whose rows begin at any multiple of its type, with NaN all around it, as one on 16-byte boundaries."""
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    x = (torch.randn(rows, cols, generator=gen, device="cuda") * 3).to(dtype)
+    even = torch.zeros(rows, -(-cols // 8) * 8, dtype=dtype, device="cuda")[:, :cols]
+    even.copy_(x)
+    want = [vb.Fp8.empty(rows, cols), vb.Fp8.empty(cols, rows)]
+    vb.vsa2_fp8_quantize(even, *want)
+    alone = vb.Fp8.empty(rows, cols)
+    vb.vsa2_fp8_quantize(even, alone)
+    for shift in range(9):
+        room = torch.full((shift + rows * ld + 16,), float("nan"), dtype=dtype, device="cuda")
+        view = room[shift:shift + rows * ld].view(rows, ld)[:, :cols]
+        view.copy_(x)
+        got = [vb.Fp8.empty(rows, cols), vb.Fp8.empty(cols, rows)]
+        vb.vsa2_fp8_quantize(view, *got)
+        single = vb.Fp8.empty(rows, cols)
+        vb.vsa2_fp8_quantize(view, single)
+        for a, b in zip((*got, single), (*want, alone)):
+            assert torch.equal(a.values.view(torch.uint8), b.values.view(torch.uint8)) and torch.equal(a.scales, b.scales)
