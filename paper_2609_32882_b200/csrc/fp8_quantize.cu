@@ -118,22 +118,17 @@ struct Source {
   int rows, cols;
   long long ld;
 };
-// words of the pieces from the byte on that the row begins at, `from` (0 .. 15) of the first piece
-__device__ __forceinline__ void set_words(const uint32_t (&w)[8], uint32_t from, Oct<false>& o) {
-  uint32_t a[6], b[5];
+// the oct that begins at byte `from` (0 .. 7) of some words
+__device__ __forceinline__ void set_words(const uint32_t (&w)[6], uint32_t from, Oct<false>& o) {
+  uint32_t a[5];
 #pragma unroll
-  for (int k = 0; k < 6; ++k) a[k] = from & 8 ? w[k + 2] : w[k];
+  for (int k = 0; k < 5; ++k) a[k] = from & 4 ? w[k + 1] : w[k];
 #pragma unroll
-  for (int k = 0; k < 5; ++k) b[k] = from & 4 ? a[k + 1] : a[k];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) o.u[k] = __funnelshift_r(b[k], b[k + 1], (from & 2) * 8);
+  for (int k = 0; k < 4; ++k) o.u[k] = __funnelshift_r(a[k], a[k + 1], (from & 2) * 8);
 }
-__device__ __forceinline__ void set_words(const uint32_t (&w)[12], uint32_t from, Oct<true>& o) {
-  uint32_t a[10];
+__device__ __forceinline__ void set_words(const uint32_t (&w)[10], uint32_t from, Oct<true>& o) {
 #pragma unroll
-  for (int k = 0; k < 10; ++k) a[k] = from & 8 && k + 2 < 12 ? w[k + 2] : w[k];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) o.f[k] = __uint_as_float(from & 4 ? a[k + 1] : a[k]);
+  for (int k = 0; k < 8; ++k) o.f[k] = __uint_as_float(from & 4 ? w[k + 1] : w[k]);
 }
 // Elements i .. i+7 of a row (zeros beyond it)
 template <bool F32, bool VEC>
@@ -147,32 +142,34 @@ __device__ __forceinline__ void load8(const Source& m, size_t row_at, int i, Oct
       if (i + j < m.cols) o.set(m.x, row_at + i + j, j);
   }
 }
-// Rows that do not begin on 16-byte boundaries: N octs, `step` bytes and COLUMNS columns apart, of which `there` exist (zeros for the others).  The aligned pieces that an oct lies in, those of all N asked for before the first is shifted into place, where the matrix has all of these bytes; single elements at
-// its two ends.  (Single elements everywhere: 20001 x 5001 71 us, both forms 143)
+// Rows that do not begin on 16-byte boundaries: N octs, `step` bytes and COLUMNS columns apart, of which `there` exist (zeros for the others).  The aligned pieces that an oct
+// lies in, those of all N asked for before the first is shifted into place, where the matrix has all of these bytes; single elements at its two ends.
+// 20001 x 5001, single elements everywhere, pieces of 16 bytes (two stages of selection instead of one), of 8: bf16 71, 68, 66 us, both forms 143, 119, 108; fp32 102, 83, 86,
+// both forms 214, 158, 162.  With each oct's loads behind the one's before bf16 took 92.
 template <bool F32, int N, int COLUMNS>
 __device__ __forceinline__ void load_shifted(const Source& m, long long row, int col, int there, long long step, Oct<F32>* o) {
-  constexpr int SIZE = F32 ? 4 : 2, PIECES = SIZE / 2 + 1;
+  constexpr int SIZE = F32 ? 4 : 2, PIECES = SIZE + 1;      // of 8 bytes
   const size_t at = (size_t)row * m.ld + col;
   const unsigned char* const a = m.x + at * SIZE;
   const long long before = at * SIZE, behind = ((long long)(m.rows - 1) * m.ld + m.cols) * SIZE - before;      // bytes of the matrix on either side
-  uint32_t w[N][PIECES * 4];
+  uint32_t w[N][PIECES * 2];
   bool inside[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    const uint32_t from = (uint32_t)reinterpret_cast<uintptr_t>(a + k * step) & 15u;
-    inside[k] = k < there && col + COLUMNS * k < m.cols && before + k * step >= from && behind - k * step >= (int)(PIECES * 16 - from);
-    const uint4* piece = reinterpret_cast<const uint4*>(a + k * step - from);
+    const uint32_t from = (uint32_t)reinterpret_cast<uintptr_t>(a + k * step) & 7u;
+    inside[k] = k < there && col + COLUMNS * k < m.cols && before + k * step >= from && behind - k * step >= (int)(PIECES * 8 - from);
+    const uint2* piece = reinterpret_cast<const uint2*>(a + k * step - from);
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      uint2 v = make_uint2(0u, 0u);
       if (inside[k]) v = piece[p];
-      w[k][4 * p] = v.x; w[k][4 * p + 1] = v.y; w[k][4 * p + 2] = v.z; w[k][4 * p + 3] = v.w;
+      w[k][2 * p] = v.x; w[k][2 * p + 1] = v.y;
     }
   }
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const int left = m.cols - col - COLUMNS * k;
-    set_words(w[k], (uint32_t)reinterpret_cast<uintptr_t>(a + k * step) & 15u, o[k]);
+    set_words(w[k], (uint32_t)reinterpret_cast<uintptr_t>(a + k * step) & 7u, o[k]);
     if (left < 8 || !inside[k]) {
       if (inside[k]) {
         o[k].keep(left);
