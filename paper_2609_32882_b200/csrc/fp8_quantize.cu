@@ -17,6 +17,7 @@ constexpr int kQzThreads = 256;
 // exponent + 127 from the bits of max|x|: 448 = 1.75 * 2^8, so a fraction above 0.75 carries (at most 254 - 8 + 1)
 __device__ __forceinline__ uint32_t scale_byte(uint32_t top) { return (uint32_t)max((int)((top + 0x1fffffu) >> 23) - 8, 0); }
 __device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ uint32_t scale_of(float inverse) { return 254u - (__float_as_uint(inverse) >> 23); }
 __device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   uint32_t r;
@@ -53,8 +54,11 @@ template <> struct Oct<false> {
     return max(t & 0xffff0000u, t << 16);
   }
   struct Tops {                      // of the eight columns
+    static constexpr int PER = 2;      // columns in a word
     uint32_t t[4] = {0u, 0u, 0u, 0u};
-    __device__ __forceinline__ uint32_t get(int j) const { return j & 1 ? t[j / 2] & 0xffff0000u : t[j / 2] << 16; }
+    __device__ __forceinline__ void set(int j, uint32_t top) { t[j / 2] |= j & 1 ? top : top >> 16; }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return __vmaxu2(a, b); }
+    static __device__ __forceinline__ uint32_t get(uint32_t word, int j) { return j & 1 ? word & 0xffff0000u : word << 16; }
   };
   // the row's, raising the columns'
   __device__ __forceinline__ uint32_t sweep(Tops& o) const {
@@ -93,8 +97,11 @@ template <> struct Oct<true> {
     return t;
   }
   struct Tops {
+    static constexpr int PER = 1;
     uint32_t t[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-    __device__ __forceinline__ uint32_t get(int j) const { return t[j]; }
+    __device__ __forceinline__ void set(int j, uint32_t top) { t[j] = top; }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
+    static __device__ __forceinline__ uint32_t get(uint32_t word, int) { return word; }
   };
   __device__ __forceinline__ uint32_t sweep(Tops& o) const {
 #pragma unroll
@@ -197,15 +204,29 @@ __device__ __forceinline__ void put_oct(unsigned char* row, int i, int cols, con
   for (int j = 0; j < 8; ++j) f[j] = scaled<CHECK>(o.get(j), inv);
   put8(row, i, FULL ? i + 8 : cols, e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
 }
-__device__ __forceinline__ uint32_t team_max(uint32_t t) {      // of 16 threads
+// The largest of each of N values over a team's 16 threads, value l / (16 / N) in thread l: halves of the values change sides at each step, N shuffles in all and a few for
+// what is left instead of 4 N one behind the other
+template <int N>
+__device__ __forceinline__ uint32_t team_tops(uint32_t (&t)[N], int l) {
+  int o = 8;
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
-  return t;
+  for (int n = N / 2; n > 0; n >>= 1, o >>= 1) {
+    const bool upper = l & o;
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, upper ? t[k] : t[k + n], o);
+      t[k] = max(upper ? t[k + n] : t[k], other);
+    }
+  }
+#pragma unroll
+  for (; o > 0; o >>= 1) t[0] = max(t[0], __shfl_xor_sync(0xffffffffu, t[0], o));
+  return t[0];
 }
 
 // Rows alone: a team of 16 threads takes 512 columns of a row (four blocks, one word of scales).  grid (row tiles of 16, word groups)
 template <bool F32, bool VEC>
-__global__ void __launch_bounds__(kQzThreads, F32 ? 4 : 6) fp8_rows_kernel(const __grid_constant__ Source m, Fp8Arg out) {
+__global__ void __launch_bounds__(kQzThreads, F32 ? 5 : 6) fp8_rows_kernel(const __grid_constant__ Source m, Fp8Arg out) {
+  constexpr int G = F32 ? 2 : 4;      // blocks whose scales are found together: as many as the registers of five or six CTAs hold (fp32 in fours spilled, 85 us; in pairs 76)
   grid_enter();
   const int rows = m.rows, cols = m.cols;
   const int l = threadIdx.x & 15;
@@ -221,17 +242,29 @@ __global__ void __launch_bounds__(kQzThreads, F32 ? 4 : 6) fp8_rows_kernel(const
   }
   uint32_t word = 0;
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    uint32_t top = team_max(o[b].top());
-    const bool odd = __any_sync(0xffffffffu, top >= kInf);
-    if (odd) top = team_max(finite_top<F32>(o[b]));
-    if (c0 + b * 128 >= cols) continue;
-    const uint32_t s = scale_byte(top);
-    word |= s << 8 * b;
-    if (row < rows) {
-      unsigned char* to = out.values + row * out.ld;
-      if (odd) put_oct<true, false, F32>(to, c0 + b * 128 + l * 8, cols, o[b], inverse_scale(s));
-      else put_oct<false, false, F32>(to, c0 + b * 128 + l * 8, cols, o[b], inverse_scale(s));
+  for (int b0 = 0; b0 < 4; b0 += G) {
+    uint32_t tops[G];
+#pragma unroll
+    for (int b = 0; b < G; ++b) tops[b] = o[b0 + b].top();
+    uint32_t byte = team_tops(tops, l);
+    const bool odd = __any_sync(0xffffffffu, byte >= kInf);
+    if (odd) {
+#pragma unroll
+      for (int b = 0; b < G; ++b) tops[b] = finite_top<F32>(o[b0 + b]);
+      byte = team_tops(tops, l);
+    }
+    byte = scale_byte(byte);
+#pragma unroll
+    for (int b = 0; b < G; ++b) {
+      const uint32_t s = __shfl_sync(0xffffffffu, byte, 16 / G * b, 16);
+      const int col = c0 + (b0 + b) * 128;
+      if (col >= cols) continue;
+      word |= s << 8 * (b0 + b);
+      if (row < rows) {
+        unsigned char* to = out.values + row * out.ld;
+        if (odd) put_oct<true, false, F32>(to, col + l * 8, cols, o[b0 + b], inverse_scale(s));
+        else put_oct<false, false, F32>(to, col + l * 8, cols, o[b0 + b], inverse_scale(s));
+      }
     }
   }
   if (l == 0 && row < rows) reinterpret_cast<uint32_t*>(out.scales)[(size_t)blockIdx.y * rows + row] = word;
@@ -255,16 +288,19 @@ struct TileShared {
 // A tile whose values are in the threads' registers: both forms, or either.  `tops`, `cols_top`: largest magnitudes of the thread's rows and columns (of no use with CHECK);
 // FULL: the tile lies inside the matrix
 template <bool CHECK, bool FULL, bool F32>
-__device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint32_t (&tops)[8], const typename Oct<F32>::Tops& cols_top, TileShared& sh,
+__device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], uint32_t (&tops)[8], const typename Oct<F32>::Tops& cols_top, TileShared& sh,
                                               int rows, int cols, int squares, const Fp8Arg& out, const Fp8Arg& out_t) {
   const int l = threadIdx.x & 15, team = threadIdx.x >> 4, tid = threadIdx.x;
   const int c0 = blockIdx.y * 128, r0 = blockIdx.x * 128;
   const int blocks = (cols + 127) / 128, blocks_t = (rows + 127) / 128;
-  auto top_of = [&](int i) { return CHECK ? finite_top<F32>(o[i]) : tops[i]; };
+  if (CHECK) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) tops[i] = finite_top<F32>(o[i]);
+  }
   uint32_t top_all = 0;
   if (squares) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top_all = max(top_all, top_of(i));
+    for (int i = 0; i < 8; ++i) top_all = max(top_all, tops[i]);
     top_all = __reduce_max_sync(0xffffffffu, top_all);
     if ((tid & 31) == 0) sh.tops[tid >> 5] = top_all;
     __syncthreads();
@@ -273,40 +309,43 @@ __device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint
   }
   if (out.values != nullptr) {
     unsigned char* to = out.values + (r0 + team * 8) * out.ld;
+    const uint32_t mine = scale_byte(squares ? top_all : team_tops(tops, l));      // of row l / 2
+    const int row = r0 + team * 8 + l / 2;
+    if ((l & 1) == 0 && (FULL || row < rows)) put_scale(out.scales, rows, row, blockIdx.y, blocks, mine);
 #pragma unroll
     for (int i = 0; i < 8; ++i, to += out.ld) {
-      const uint32_t s = scale_byte(squares ? top_all : team_max(top_of(i)));
-      const int row = r0 + team * 8 + i;
-      if (FULL || row < rows) {
-        put_oct<CHECK, FULL, F32>(to, c0 + l * 8, cols, o[i], inverse_scale(s));
-        if (l == 0) put_scale(out.scales, rows, row, blockIdx.y, blocks, s);
-      }
+      const uint32_t s = __shfl_sync(0xffffffffu, mine, 2 * i, 16);
+      if (FULL || r0 + team * 8 + i < rows) put_oct<CHECK, FULL, F32>(to, c0 + l * 8, cols, o[i], inverse_scale(s));
     }
   }
   if (out_t.values == nullptr) return;
-  uint32_t byte = 0;      // of column tid
-  if (!squares) {
+  using Tops = typename Oct<F32>::Tops;
+  if (squares) {
+    if (tid < 128) sh.col_inv[tid] = inverse_scale(scale_byte(top_all));
+  } else {
+    Tops mine = cols_top;
+    if (CHECK) {
+      mine = Tops();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      uint32_t top = cols_top.get(j);
-      if (CHECK) {
-        top = 0;
+      for (int j = 0; j < 8; ++j) {
+        uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if (finite_bits(o[i].get(j))) top = max(top, __float_as_uint(o[i].get(j)) & 0x7fffffffu);
+        mine.set(j, top);
       }
-      sh.col_top[team][l * 8 + j] = top;
     }
-    __syncthreads();
-  }
-  if (tid < 128) {
-    uint32_t top = top_all;
-    if (!squares) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) top = max(top, sh.col_top[r][tid]);
+    for (int k = 0; k < 8 / Tops::PER; k += 4)
+      *reinterpret_cast<uint4*>(&sh.col_top[team][l * (8 / Tops::PER) + k]) = make_uint4(mine.t[k], mine.t[k + 1], mine.t[k + 2], mine.t[k + 3]);
+    __syncthreads();
+    if (tid < 128 / Tops::PER) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = Tops::larger(top, sh.col_top[r][tid]);
+#pragma unroll
+      for (int j = 0; j < Tops::PER; ++j) sh.col_inv[tid * Tops::PER + j] = inverse_scale(scale_byte(Tops::get(top, j)));
     }
-    byte = scale_byte(top);
-    sh.col_inv[tid] = inverse_scale(byte);
   }
   __syncthreads();
   const float4 inv0 = reinterpret_cast<const float4*>(sh.col_inv)[2 * l], inv1 = reinterpret_cast<const float4*>(sh.col_inv)[2 * l + 1];
@@ -336,7 +375,7 @@ __device__ __forceinline__ void quantize_tile(const Oct<F32> (&o)[8], const uint
       }
     }
   }
-  if (tid < 128 && c0 + tid < cols) put_scale(out_t.scales, cols, c0 + tid, blockIdx.x, blocks_t, byte);
+  if (tid < 128 && c0 + tid < cols) put_scale(out_t.scales, cols, c0 + tid, blockIdx.x, blocks_t, scale_of(sh.col_inv[tid]));
 }
 
 // A tile of 128 x 128: both forms, or either.  A team of 16 threads holds 8 rows, 8 columns a thread.  The transpose passes through shared memory
