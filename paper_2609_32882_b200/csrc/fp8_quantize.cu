@@ -3,8 +3,8 @@
 //   e = the least integer with max|x| <= 448 * 2^e over the block's finite values (448: the largest e4m3 value), at least -127
 //   value = x * 2^-e rounded to e4m3 (to nearest, ties to even); what is not finite becomes NaN
 // A power of two scales without rounding, so the 3 mantissa bits are all that is lost, and it is what the tensor cores multiply by themselves.
-// x is read once, each form written once.  Rows alone are bound by memory: 75600 x 5120 193 us (6.0 TB/s), 20000 x 5120 of fp32 77 us (6.6).  Both forms in one
-// reading are bound by instructions (a conversion for every value and form): 20000 x 5120 82 us (5.0 TB/s), blocks of 128 x 128 of 15360 x 5120 54 us (5.8).
+// x is read once, each form written once; bound by memory.  Rows: 75600 x 5120 184 us (6.3 TB/s), 20000 x 5120 47 us (6.5), of fp32 76 us (6.7).  Both forms in one reading: 20000 x 5120
+// 69 us (6.0), of fp32 98 us (6.3), blocks of 128 x 128 of 15360 x 5120 53 us (5.9); 2025 x 4600, one wave of CTAs, 11.4 us.
 #include "common.cuh"
 #include "heads.cuh"
 
@@ -151,8 +151,8 @@ __device__ __forceinline__ void load8(const Source& m, size_t row_at, int i, Oct
 }
 // Rows that do not begin on 16-byte boundaries: N octs, `step` bytes and COLUMNS columns apart, of which `there` exist (zeros for the others).  The aligned pieces that an oct
 // lies in, those of all N asked for before the first is shifted into place, where the matrix has all of these bytes; single elements at its two ends.
-// 20001 x 5001, single elements everywhere, pieces of 16 bytes (two stages of selection instead of one), of 8: bf16 71, 68, 66 us, both forms 143, 119, 108; fp32 102, 83, 86,
-// both forms 214, 158, 162.  With each oct's loads behind the one's before bf16 took 92.
+// 20001 x 5001: single elements everywhere, pieces of 16 bytes (two stages of selection instead of one), of 8: bf16 71, 68, 66 us, both forms 143, 119, 108; fp32 102, 83, 86,
+// both forms 214, 158, 162 (with the reductions of then; now 63, 95, 84, 140, and 50, 80, 78, 104 on 16-byte boundaries).  With each oct's loads behind the one's before bf16 took 92.
 template <bool F32, int N, int COLUMNS>
 __device__ __forceinline__ void load_shifted(const Source& m, long long row, int col, int there, long long step, Oct<F32>* o) {
   constexpr int SIZE = F32 ? 4 : 2, PIECES = SIZE + 1;      // of 8 bytes
@@ -205,7 +205,7 @@ __device__ __forceinline__ void put_oct(unsigned char* row, int i, int cols, con
   put8(row, i, FULL ? i + 8 : cols, e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
 }
 // The largest of each of N values over a team's 16 threads, value l / (16 / N) in thread l: halves of the values change sides at each step, N shuffles in all and a few for
-// what is left instead of 4 N one behind the other
+// what is left instead of 4 N (20000 x 5120: both forms 82 -> 69 us, of fp32 131 -> 98)
 template <int N>
 __device__ __forceinline__ uint32_t team_tops(uint32_t (&t)[N], int l) {
   int o = 8;

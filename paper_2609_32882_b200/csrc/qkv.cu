@@ -147,11 +147,23 @@ __device__ __forceinline__ void share_turns(const TurnArgs& t, unsigned long lon
   __syncthreads();
 }
 
-template <int TEAM>
-__device__ __forceinline__ float team_sum(float v) {
+// Sums of each of N values over a team's threads, value l / (TEAM / N) in thread l: halves of the values change sides at each step
+// (four rows of the forward: 480p, 24 heads, halves as pairs 209 -> 195 us; the backward's two sums: no faster, and one step more behind the other, clip 15.0 -> 15.8)
+template <int TEAM, int N>
+__device__ __forceinline__ float team_sums(float (&t)[N], int l) {
+  int o = TEAM / 2;
 #pragma unroll
-  for (int o = TEAM / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
+  for (int n = N / 2; n > 0; n >>= 1, o >>= 1) {
+    const bool upper = l & o;
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+      const float other = __shfl_xor_sync(0xffffffffu, upper ? t[k] : t[k + n], o);
+      t[k] = (upper ? t[k + n] : t[k]) + other;
+    }
+  }
+#pragma unroll
+  for (; o > 0; o >>= 1) t[0] += __shfl_xor_sync(0xffffffffu, t[0], o);
+  return t[0];
 }
 
 // grid (token tiles of all batch entries, 1, groups of heads)
@@ -186,17 +198,27 @@ __global__ void __launch_bounds__(kQkvThreads) qkv_fwd_kernel(const __grid_const
       Raw8<TI> raw[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) raw[u].load(xp + min(h + u, hi - 1) * x.sh);
+      float r = 1.f;      // of row l / (TEAM / U)
+      if (norm) {
+        float ss[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float f[8];
+          raw[u].get(f);
+          ss[u] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) ss[u] += f[i] * f[i];
+        }
+        r = rsqrtf(team_sums<TEAM>(ss, l) * (1.f / D) + a.eps);
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         float f[8];
         raw[u].get(f);
         if (norm) {
-          float ss = 0.f;
+          const float ru = __shfl_sync(0xffffffffu, r, TEAM / U * u, TEAM);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) ss += f[i] * f[i];
-          const float r = rsqrtf(team_sum<TEAM>(ss) * (1.f / D) + a.eps);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) f[i] *= r * w[i];
+          for (int i = 0; i < 8; ++i) f[i] *= ru * w[i];
         }
         if (rotate) turn.apply(f);
         if (valid && h + u < hi) store8(yp + (h + u) * y.sh, f);
