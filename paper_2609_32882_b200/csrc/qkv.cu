@@ -11,7 +11,7 @@
 // All of it is bound by memory: every element is read once and written once, the few operations hide behind that.  A team of D / 8
 // threads holds one row of one head, 8 channels a thread; it keeps its token and walks through the heads, so that a token's sines and
 // cosines (and the norm weights) are formed once, and the reads of a CTA's tokens are whole rows of the projection.  At 75,600 tokens: rotation of 40
-// heads 239 us (6.5 TB/s), norms, rotation and heads of 3 x 40 heads 736 us (6.3 TB/s), backward of 3 x 20 heads 484 us (6.4 TB/s); a copy reaches 6.45.
+// heads 239 us (6.5 TB/s), norms, rotation and heads of 3 x 40 heads 736 us (6.3 TB/s), backward of 3 x 20 heads 485 - 494 us (6.3 TB/s); a copy reaches 6.45.
 // With few tokens it is the latency of one row (2048 tokens, 3 x 12 heads: 8.7 us; 256 tokens, 3 x 2: 3.6 us).
 #include "common.cuh"
 #include "heads.cuh"
