@@ -14,7 +14,7 @@ from . import binding as vb
 class Vsa2Layer:
     """params: the attention's problem (make_params; out_dtype BF16); hidden: channels of x; rope_channels: channels of a head that turn with (t, h, w).
 
-    set_weights takes w_qkv [(Hq + 2 Hkv) D, C] bf16 (rows: q's heads, k's, v's), w_g [C, Hq] bf16 and the norms' weights fp32 [D]; forward keeps what backward
+    set_weights takes w_qkv [(Hq + 2 Hkv) D, C] bf16 or fp32 (rows: q's heads, k's, v's), w_g [C, Hq] bf16 and the norms' weights fp32 [D] (None: ones); forward keeps what backward
     needs until the next forward."""
 
     def __init__(self, params, hidden, rope_channels, theta=1e4, scale=1.0, layout=vb.ROPE_PAIRS, eps=1e-6, device="cuda"):
@@ -35,7 +35,16 @@ class Vsa2Layer:
         self.ws_gate = torch.empty(max(256, vb.vsa2_gate_bwd_workspace_bytes(p, hidden)), dtype=torch.uint8, device=device)
         self.saved = None
 
+    def _expect(self, t, what, shape, dtype):
+        """The attention and the gate get plain addresses; sizes and types are the layer's."""
+        if tuple(t.shape) != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"expected {what} as a contiguous CUDA tensor {shape} in {dtype}, not {tuple(t.shape)} in {t.dtype}")
+
     def set_weights(self, w_qkv, w_g, q_weight, k_weight):
+        self._expect(w_g, "the gate's weights", (self.hidden, self.p.heads_q), self.torch.bfloat16)
+        for w in (q_weight, k_weight):
+            if w is not None:
+                self._expect(w, "a norm's weights", (self.p.head_dim,), self.torch.float32)
         vb.vsa2_fp8_quantize(w_qkv, self.w, self.w_t, squares=True)
         self.w_g, self.q_weight, self.k_weight = w_g, q_weight, k_weight
 
@@ -51,8 +60,7 @@ class Vsa2Layer:
     def forward(self, x):
         """x [B, L + Lt, C] bf16, contiguous -> o [B, Hq, L + Lt, D] bf16."""
         p, torch = self.p, self.torch
-        if tuple(x.shape) != (p.batch, self.tokens, self.hidden) or not x.is_contiguous():
-            raise ValueError(f"expected contiguous hidden states {(p.batch, self.tokens, self.hidden)}")
+        self._expect(x, "hidden states", (p.batch, self.tokens, self.hidden), torch.bfloat16)
         a = vb.Fp8.empty(self.rows, self.hidden, self.device)
         vb.vsa2_fp8_quantize(x.view(self.rows, self.hidden), a)
         packed = self._empty(self.rows, self.width)
@@ -71,6 +79,7 @@ class Vsa2Layer:
         """d_o [B, Hq, L + Lt, D] bf16 -> dict of dx [B, L + Lt, C] bf16 and, in fp32, dw_qkv, dw_g, dq_weight, dk_weight."""
         p, torch = self.p, self.torch
         x, video, packed, q, k, v, gate, o, lse = self.saved
+        self._expect(d_o, "the output's gradient", tuple(o.shape), torch.bfloat16)
         dq, dk, dv, dgate = self.attn.backward(q, k, v, gate, o, lse, d_o)
         d_packed = torch.empty_like(packed)
         dqw, dkw = (self._empty(p.head_dim, dtype=torch.float32) for _ in range(2))
