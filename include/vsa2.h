@@ -316,6 +316,10 @@ int vsa2_gate_fwd(const vsa2_params* p, int32_t hidden, const void* x, const voi
 size_t vsa2_gate_bwd_workspace_bytes(const vsa2_params* p, int32_t hidden);
 int vsa2_gate_bwd(const vsa2_params* p, int32_t hidden, const void* x, const void* w_g, const float* gate,
                   const float* dgate, float* d_w_g, void* dx, void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* The same with dx added to what it holds (the gradient of the same hidden states through the projection), rounded once; the batch entries of dx lie dx_batch_stride
+ * elements apart (at least L * hidden, a multiple of 16 bytes; of no use with one), so that rows behind a video's tokens (text) stay as they are. */
+int vsa2_gate_bwd_add(const vsa2_params* p, int32_t hidden, const void* x, const void* w_g, const float* gate, const float* dgate, float* d_w_g, void* dx,
+                      int64_t dx_batch_stride, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* ---- From a layer's hidden states to its attention (the paper has no counterpart: Sec. 2.2 begins at Q, K, V) ------------------
  * X -> vsa2_fp8_quantize -> vsa2_fp8_matmul (the projection) -> vsa2_qkv_fwd (norms, positions, heads) -> vsa2_route, vsa2_attn_fwd;

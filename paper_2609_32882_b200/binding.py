@@ -33,7 +33,7 @@ ERR_STATIC_SCRATCH = -8
 
 EXPORTS = ("vsa2_query_sizes", "vsa2_route", "vsa2_route_scores", "vsa2_attn_fwd", "vsa2_attn_bwd",
            "vsa2_device_status", "vsa2_strerror", "vsa2_profile_events", "vsa2_launch_count", "vsa2_selftest_umma", "vsa2_route_noalloc", "vsa2_last_cuda_error",
-           "vsa2_gate_fwd", "vsa2_gate_bwd", "vsa2_gate_bwd_workspace_bytes",
+           "vsa2_gate_fwd", "vsa2_gate_bwd", "vsa2_gate_bwd_add", "vsa2_gate_bwd_workspace_bytes",
            "vsa2_attn_bwd_preferred_workspace_bytes", "vsa2_attn_bwd_scratch", "vsa2_attn_bwd_scratch_bytes",
            "vsa2_route_scratch", "vsa2_route_scratch_bytes", "vsa2_permute_cube_major",
            "vsa2_selftest_timeout", "vsa2_debug_rescue_capacity", "vsa2_selftest_divmod",
@@ -150,6 +150,7 @@ def _lib():
         lib.vsa2_launch_count.restype = C.c_int64
         lib.vsa2_selftest_divmod.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         lib.vsa2_selftest_divmod.restype = C.c_int64
+        lib.vsa2_gate_bwd_add.argtypes = [vp, C.c_int32] + [vp] * 6 + [C.c_int64, vp, sz, vp]
         lib.vsa2_rope_plan.argtypes = [C.c_int32, C.c_int32, vp, vp, vp, C.POINTER(Rope)]
         lib.vsa2_rope_apply.argtypes = [vp, vp, vp, vp, C.c_int32, vp]
         lib.vsa2_qkv_fwd.argtypes = [vp] * 6
@@ -272,6 +273,18 @@ def vsa2_gate_bwd(p, hidden, x, w_g, gate, dgate, d_w_g, dx, workspace, stream=N
     nbytes = workspace.numel() * workspace.element_size()
     _check(_lib().vsa2_gate_bwd(C.byref(p), hidden, _ptr(x), _ptr(w_g), _ptr(gate), _ptr(dgate), _ptr(d_w_g), _ptr(dx),
                                 _ptr(workspace), nbytes, _stream(stream)), "vsa2_gate_bwd")
+
+
+def vsa2_gate_bwd_add(p, hidden, x, w_g, gate, dgate, d_w_g, dx, workspace, stream=None):
+    """vsa2_gate_bwd with its dx added to what `dx` holds: [B, L or more rows, hidden], contiguous but for its batch entries' distance; rows from L on stay."""
+    sizes = vsa2_query_sizes(p)
+    dtype = {BF16: "torch.bfloat16", F32: "torch.float32"}[p.out_dtype]
+    rows_ok = dx.dim() == 3 and dx.shape[0] == p.batch and dx.shape[1] >= sizes.seq_len and dx.shape[2] == hidden
+    if not rows_ok or not dx.is_cuda or str(dx.dtype) != dtype or not dx[0].is_contiguous():
+        raise ValueError(f"expected dx as a CUDA tensor [{p.batch}, {sizes.seq_len} or more, {hidden}] in {dtype} with contiguous batch entries")
+    nbytes = workspace.numel() * workspace.element_size()
+    _check(_lib().vsa2_gate_bwd_add(C.byref(p), hidden, _ptr(x), _ptr(w_g), _ptr(gate), _ptr(dgate), _ptr(d_w_g), dx.data_ptr(), dx.stride(0), _ptr(workspace),
+                                    nbytes, _stream(stream)), "vsa2_gate_bwd_add")
 
 
 def vsa2_route_scores(p, workspace) -> int:

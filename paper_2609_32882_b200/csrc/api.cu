@@ -331,6 +331,27 @@ cudaError_t g_last_cuda_error = cudaSuccess;
     }                                                \
   } while (0)
 
+// vsa2_gate_bwd, or vsa2_gate_bwd_add
+int gate_bwd(const vsa2_params* p, int32_t hidden, const void* x, const void* w_g, const float* gate, const float* dgate, float* d_w_g, void* dx, bool add,
+             int64_t dx_batch_stride, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  Geo g;
+  int rc = fill_geo(p, &g);
+  if (rc != VSA2_OK) return rc;
+  if (!x || !w_g || !gate || !dgate || !d_w_g || !dx || !workspace) return VSA2_ERR_INVALID_ARG;
+  if (!gate_supported(hidden, g.Hq)) return VSA2_ERR_UNSUPPORTED;
+  if (!aligned16(x) || !aligned16(dx) || !aligned256(workspace)) return VSA2_ERR_MISALIGNED;
+  const int64_t whole = (int64_t)g.L * hidden;
+  if (!add || g.batch == 1) dx_batch_stride = whole;
+  if (dx_batch_stride < whole) return VSA2_ERR_INVALID_ARG;
+  if (dx_batch_stride % (g.out_f32 ? 4 : 8)) return VSA2_ERR_MISALIGNED;
+  if (workspace_bytes < gate_bwd_workspace_bytes(g.batch, g.L, hidden, g.Hq)) return VSA2_ERR_WORKSPACE_TOO_SMALL;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  VSA2_CUDA(launch_gate_bwd(g.batch, g.L, hidden, g.Hq, g.out_f32, reinterpret_cast<const bf16*>(x),
+                            reinterpret_cast<const bf16*>(w_g), gate, dgate, d_w_g, dx, add, dx_batch_stride, workspace,
+                            reinterpret_cast<cudaStream_t>(cuda_stream)));
+  return VSA2_OK;
+}
+
 // ---- views of heads, matrices in 8 bits -----------------------------------------------------------------------------------
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -992,18 +1013,12 @@ size_t vsa2_gate_bwd_workspace_bytes(const vsa2_params* p, int32_t hidden) {
 
 int vsa2_gate_bwd(const vsa2_params* p, int32_t hidden, const void* x, const void* w_g, const float* gate,
                   const float* dgate, float* d_w_g, void* dx, void* workspace, size_t workspace_bytes, void* cuda_stream) {
-  Geo g;
-  int rc = fill_geo(p, &g);
-  if (rc != VSA2_OK) return rc;
-  if (!x || !w_g || !gate || !dgate || !d_w_g || !dx || !workspace) return VSA2_ERR_INVALID_ARG;
-  if (!gate_supported(hidden, g.Hq)) return VSA2_ERR_UNSUPPORTED;
-  if (!aligned16(x) || !aligned16(dx) || !aligned256(workspace)) return VSA2_ERR_MISALIGNED;
-  if (workspace_bytes < gate_bwd_workspace_bytes(g.batch, g.L, hidden, g.Hq)) return VSA2_ERR_WORKSPACE_TOO_SMALL;
-  if ((rc = check_device()) != VSA2_OK) return rc;
-  VSA2_CUDA(launch_gate_bwd(g.batch, g.L, hidden, g.Hq, g.out_f32, reinterpret_cast<const bf16*>(x),
-                            reinterpret_cast<const bf16*>(w_g), gate, dgate, d_w_g, dx, workspace,
-                            reinterpret_cast<cudaStream_t>(cuda_stream)));
-  return VSA2_OK;
+  return gate_bwd(p, hidden, x, w_g, gate, dgate, d_w_g, dx, false, 0, workspace, workspace_bytes, cuda_stream);
+}
+
+int vsa2_gate_bwd_add(const vsa2_params* p, int32_t hidden, const void* x, const void* w_g, const float* gate, const float* dgate, float* d_w_g, void* dx,
+                      int64_t dx_batch_stride, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return gate_bwd(p, hidden, x, w_g, gate, dgate, d_w_g, dx, true, dx_batch_stride, workspace, workspace_bytes, cuda_stream);
 }
 
 int vsa2_rope_plan(int32_t head_dim, int32_t layout, const int32_t axis_channels[3], const double theta[3], const double scale[3],

@@ -217,11 +217,12 @@ __global__ void __launch_bounds__(kGtThreads, MW != 4 ? 0 : NT == 4 ? 4 : NT == 
 // ---------------------------------------------------------------------------------------------- dX
 // grid (ceil(L / 64), batch, channel slices); KT = head tiles of 16 (the contraction).  Four column tiles of a group of 32
 // channels are interleaved (column n of tile u is channel 8 (n / 2) + 2 u + n % 2), so that a thread's accumulators of the four
-// are 8 neighbouring channels of a token and go to memory as one 16-byte store; no tile is staged for coalescing.
-template <int KT>
+// are 8 neighbouring channels of a token and go to memory as one 16-byte store; no tile is staged for coalescing.  ADD: to what dx holds (the layer's other
+// gradient of the same hidden states), read ahead of the products.  dx_batch: elements between dx's batch entries.
+template <int KT, bool ADD>
 __global__ void __launch_bounds__(kGtThreads) gate_bwd_dx_kernel(const bf16* w, const bf16* dz_tm,
                                                                  int L, int Lp, int C, int Hq, int per_slice, int out_f32,
-                                                                 void* __restrict__ dx) {
+                                                                 void* dx, long long dx_batch) {
   grid_enter();
   constexpr int LDZ = KT * 16 + 8;
   __shared__ __align__(16) bf16 az[kGtTok * LDZ];            // dz^T: [token][head]
@@ -269,6 +270,21 @@ __global__ void __launch_bounds__(kGtThreads) gate_bwd_dx_kernel(const bf16* w, 
 #pragma unroll 2
     for (int q = 0; q < kDxCh / 32; ++q) {
       float acc[4][4];
+      const int c = c0 + q * 32 + t * 8;                       // (C is a multiple of 8)
+      uint4 old[2][2];                                         // of both rows
+      if (ADD) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int l = half ? lb : la;
+          if (c < c_end && l < L) {
+            const size_t idx = b * dx_batch + (size_t)l * C + c;
+            const uint4* from = out_f32 ? reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(dx) + idx)
+                                        : reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(dx) + idx);
+            old[half][0] = from[0];
+            if (out_f32) old[half][1] = from[1];
+          }
+        }
+      }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         acc[u][0] = acc[u][1] = acc[u][2] = acc[u][3] = 0.f;
@@ -276,13 +292,20 @@ __global__ void __launch_bounds__(kGtThreads) gate_bwd_dx_kernel(const bf16* w, 
 #pragma unroll
         for (int ks = 0; ks < KT; ++ks) mma_bf16(acc[u], a[ks], lds32(wr + ks * 16), lds32(wr + ks * 16 + 8));
       }
-      const int c = c0 + q * 32 + t * 8;                       // (C is a multiple of 8)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int l = half ? lb : la;
-        const size_t idx = ((size_t)b * L + l) * C + c;
-        const float* v[4] = {acc[0] + 2 * half, acc[1] + 2 * half, acc[2] + 2 * half, acc[3] + 2 * half};
+        const size_t idx = b * dx_batch + (size_t)l * C + c;
+        float* v[4] = {acc[0] + 2 * half, acc[1] + 2 * half, acc[2] + 2 * half, acc[3] + 2 * half};
         if (c < c_end && l < L) {
+          if (ADD) {
+            const uint32_t o[8] = {old[half][0].x, old[half][0].y, old[half][0].z, old[half][0].w, old[half][1].x, old[half][1].y, old[half][1].z, old[half][1].w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              v[u][0] += __uint_as_float(out_f32 ? o[2 * u] : o[u] << 16);
+              v[u][1] += __uint_as_float(out_f32 ? o[2 * u + 1] : o[u] & 0xffff0000u);
+            }
+          }
           if (out_f32) {
             float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(dx) + idx);
             dst[0] = make_float4(v[0][0], v[0][1], v[1][0], v[1][1]);
@@ -438,7 +461,7 @@ cudaError_t launch_gate_fwd(int batch, int L, int C, int Hq, const bf16* x, cons
 }
 
 cudaError_t launch_gate_bwd(int batch, int L, int C, int Hq, int out_f32, const bf16* x, const bf16* w, const float* gate,
-                            const float* dgate, float* d_w, void* dx, void* workspace, cudaStream_t st) {
+                            const float* dgate, float* d_w, void* dx, bool add, long long dx_batch, void* workspace, cudaStream_t st) {
   const int HP = padded_heads(Hq), Lp = padded_tokens(L);
   float* partial = reinterpret_cast<float*>(workspace);
   unsigned char* wsb = reinterpret_cast<unsigned char*>(workspace);
@@ -457,7 +480,9 @@ cudaError_t launch_gate_bwd(int batch, int L, int C, int Hq, int out_f32, const 
     const int per_slice = (chunks + slices - 1) / slices * kDxCh;
     dim3 grid((L + kGtTok - 1) / kGtTok, batch, (C + per_slice - 1) / per_slice);
     const int kt = (Hq + 15) / 16;
-#define VSA2_GATE_DX(KT_) launch_kernel(gate_bwd_dx_kernel<KT_>, grid, kGtThreads, 0, st, w, dz_tm, L, Lp, C, Hq, per_slice, out_f32, dx)
+#define VSA2_GATE_DX(KT_)                                                                                                                        \
+  launch_kernel(add ? gate_bwd_dx_kernel<KT_, true> : gate_bwd_dx_kernel<KT_, false>, grid, kGtThreads, 0, st, w, dz_tm, L, Lp, C, Hq, per_slice, out_f32, \
+                dx, dx_batch)
     if (kt <= 1) VSA2_GATE_DX(1);
     else if (kt <= 2) VSA2_GATE_DX(2);
     else if (kt <= 3) VSA2_GATE_DX(3);

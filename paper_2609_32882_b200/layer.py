@@ -4,7 +4,8 @@
 
 and back to the gradients of x and of all weights.  The projection's three products (forward, dX, dW) run on e4m3 values with a scale for each 128 of
 them: weights are quantised once per update in 128 x 128 blocks (both forms), hidden states and gradients as they come, along the dimension that is
-summed over.  Master weights stay with the caller.  torch is used for memory, and to add the two parts of dX.
+summed over.  Master weights stay with the caller.  torch is used for memory, and with text behind the videos of a batch to copy
+the video rows next to one another, as the gate's calls take them.
 """
 from __future__ import annotations
 
@@ -92,9 +93,8 @@ class Vsa2Layer:
         vb.vsa2_fp8_matmul(g, self.w_t, dx.view(self.rows, self.hidden), self.ws_matmul)
         dw = self._empty(self.width, self.hidden, dtype=torch.float32)
         vb.vsa2_fp8_matmul(g_t, x_t, dw, self.ws_matmul)
-        dw_g, dx_gate = self._empty(self.hidden, p.heads_q, dtype=torch.float32), torch.empty_like(video)
-        vb.vsa2_gate_bwd(p, self.hidden, video, self.w_g, gate, dgate, dw_g, dx_gate, self.ws_gate)
-        dx[:, :video.shape[1]] += dx_gate
+        dw_g = self._empty(self.hidden, p.heads_q, dtype=torch.float32)
+        vb.vsa2_gate_bwd_add(p, self.hidden, video, self.w_g, gate, dgate, dw_g, dx, self.ws_gate)
         return {"dx": dx, "dw_qkv": dw, "dw_g": dw_g, "dq_weight": dqw, "dk_weight": dkw}
 
     def check_status(self):

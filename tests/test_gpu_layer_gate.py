@@ -1,4 +1,4 @@
-"""The gate's share of the layer: output and all gradients against the layer with its gated coarse branch in 64 bits.
+"""The gate's share of the layer: output and all gradients against the layer with its gated coarse branch in 64 bits, and how the two parts of dX come together.
 
 Bounds as for the layer without a gate (outputs 1 %; gradients that pass the 8-bit products 6 %).  dW_g and the norm weights' gradients pass none: the gate's dz is rounded to bf16 (2^-9 at
 most), and what it is made of is the attention's output, 1 % off at most."""
@@ -84,3 +84,63 @@ def test_layer_with_a_gate_against_autograd(batch, hq, hk, dim, grid, text, hidd
     assert off(got["dw_qkv"], W.grad) <= 0.06
     assert off(got["dw_g"], WG.grad) <= 0.02
     assert off(got["dq_weight"], QW.grad) <= 0.02 and off(got["dk_weight"], KW.grad) <= 0.02
+
+
+@pytest.mark.parametrize("batch,grid,text", [(1, (4, 8, 8), 0), (2, (3, 5, 9), 21)])
+def test_parts_of_dx(batch, grid, text, monkeypatch):
+    """dX = the product's result + sum_h dz_h w_g, and in text rows the product's alone.  With the layer's own product and dz (as it rounds them, to bf16) the sum is known to
+    2^-20, and one rounding to bf16 is left: its squares average a twelfth of the unit's."""
+    hidden = 256
+    layer, _, x, w_g, _, _, d_o = problem(batch, 4, 2, 64, grid, text, hidden, 4.0)
+    video = grid[0] * grid[1] * grid[2]
+    products, dgates = [], []
+    matmul, attn_backward = vb.vsa2_fp8_matmul, layer.attn.backward
+
+    def recorded(a, b, c, *rest, **kw):
+        matmul(a, b, c, *rest, **kw)
+        products.append(c.clone())
+
+    def recorded_backward(*a, **kw):
+        out = attn_backward(*a, **kw)
+        dgates.append(out[3].clone())
+        return out
+
+    layer.forward(x)
+    gate = layer.saved[6].clone()
+    monkeypatch.setattr(vb, "vsa2_fp8_matmul", recorded)
+    monkeypatch.setattr(layer.attn, "backward", recorded_backward)
+    dx = layer.backward(d_o)["dx"]
+    product = next(c for c in products if c.shape == (layer.rows, hidden) and c.dtype == BF).view(dx.shape)
+    dz = (dgates[0] * (1 - gate * gate)).to(BF).double()
+    gates_part = dz.transpose(1, 2) @ w_g.double().T
+    want = product.double()
+    assert torch.equal(dx[:, video:], product[:, video:])
+    want[:, :video] += gates_part
+    unit = torch.ldexp(torch.ones_like(want), torch.frexp(want)[1] - 8)[:, :video]
+    assert float(gates_part.norm()) >= 2 * float(product[:, :video].norm())      # (whose own rounding would show)
+    err = (dx.double() - want)[:, :video]
+    assert float((err ** 2).sum()) <= 1.2 * float((unit ** 2).sum()) / 12
+
+
+@pytest.mark.parametrize("out_dtype", [vb.BF16, vb.F32])
+@pytest.mark.parametrize("batch,heads,grid,hidden,rows", [(1, 5, (3, 5, 7), 72, 105), (2, 40, (4, 8, 16), 264, 600), (3, 64, (2, 9, 11), 136, 198), (2, 17, (1, 1, 3), 8, 4)])
+def test_gate_backward_onto_a_gradient(batch, heads, grid, hidden, rows, out_dtype):
+    """vsa2_gate_bwd_add against vsa2_gate_bwd in fp32: the same products, added to what is there and rounded once; rows behind the video's and dW_g as they are without."""
+    gen = torch.Generator(device="cuda").manual_seed(heads)
+    randn = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    n = grid[0] * grid[1] * grid[2]
+    make = lambda dtype: vb.make_params(batch, heads, heads, 64, grid, topk=1, out_dtype=dtype)
+    p = make(out_dtype)
+    x, w, gate, dgate = randn(batch, n, hidden).to(BF), randn(hidden, heads).to(BF), torch.tanh(randn(batch, heads, n)), randn(batch, heads, n)
+    ws = torch.empty(vb.vsa2_gate_bwd_workspace_bytes(p, hidden), dtype=torch.uint8, device="cuda")
+    dw, part = [torch.empty(hidden, heads, device="cuda") for _ in range(2)], torch.empty(batch, n, hidden, device="cuda")
+    vb.vsa2_gate_bwd(make(vb.F32), hidden, x, w, gate, dgate, dw[0], part, ws)
+    before = randn(batch, rows, hidden).to(torch.float32 if out_dtype == vb.F32 else BF)
+    dx = before.clone()
+    vb.vsa2_gate_bwd_add(p, hidden, x, w, gate, dgate, dw[1], dx, ws)
+    want = before.clone()
+    want[:, :n] = (before[:, :n].float() + part).to(before.dtype)
+    assert torch.equal(dx, want) and torch.equal(dw[0], dw[1])
+    for bad in (dx.half(), dx[:, :n - 1], dx[..., :-1], dx.transpose(1, 2), dx[:1, :, :].expand(batch + 1, rows, hidden)):
+        with pytest.raises(ValueError):
+            vb.vsa2_gate_bwd_add(p, hidden, x, w, gate, dgate, dw[1], bad, ws)
