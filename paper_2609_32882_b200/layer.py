@@ -15,8 +15,9 @@ from . import binding as vb
 class Vsa2Layer:
     """params: the attention's problem (make_params; out_dtype BF16); hidden: channels of x; rope_channels: channels of a head that turn with (t, h, w).
 
-    set_weights takes w_qkv [(Hq + 2 Hkv) D, C] bf16 or fp32 (rows: q's heads, k's, v's), w_g [C, Hq] bf16 and the norms' weights fp32 [D] (None: ones); forward keeps what backward
-    needs until the next forward."""
+    set_weights takes w_qkv [(Hq + 2 Hkv) D, C] bf16 or fp32 (rows: q's heads, k's, v's), w_g [C, Hq] bf16 and the norms' weights fp32 [D] (None: ones); forward keeps what
+    backward needs until the next forward.  x, o and the weights of the gate and of the norms are kept as they are, not copied: they, and the weights that were set, have to stay until
+    backward returns.  It refuses where torch or set_weights has changed one of them since (what other kernels write into them it cannot see)."""
 
     def __init__(self, params, hidden, rope_channels, theta=1e4, scale=1.0, layout=vb.ROPE_PAIRS, eps=1e-6, device="cuda"):
         import torch
@@ -34,7 +35,8 @@ class Vsa2Layer:
         self.ws_matmul = torch.zeros(need, dtype=torch.uint8, device=device)
         self.ws_qkv = torch.empty(vb.vsa2_qkv_bwd_workspace_bytes(p.head_dim), dtype=torch.uint8, device=device)
         self.ws_gate = torch.empty(max(256, vb.vsa2_gate_bwd_workspace_bytes(p, hidden)), dtype=torch.uint8, device=device)
-        self.saved = None
+        self.w_g = self.q_weight = self.k_weight = None
+        self.saved, self.kept, self.updates = None, {}, 0
 
     def _expect(self, t, what, shape, dtype):
         """The attention and the gate get plain addresses; sizes and types are the layer's."""
@@ -46,6 +48,7 @@ class Vsa2Layer:
         for w in (q_weight, k_weight):
             if w is not None:
                 self._expect(w, "a norm's weights", (self.p.head_dim,), self.torch.float32)
+        self.updates += 1
         vb.vsa2_fp8_quantize(w_qkv, self.w, self.w_t, squares=True)
         self.w_g, self.q_weight, self.k_weight = w_g, q_weight, k_weight
 
@@ -62,6 +65,8 @@ class Vsa2Layer:
         """x [B, L + Lt, C] bf16, contiguous -> o [B, Hq, L + Lt, D] bf16."""
         p, torch = self.p, self.torch
         self._expect(x, "hidden states", (p.batch, self.tokens, self.hidden), torch.bfloat16)
+        if self.updates == 0:
+            raise RuntimeError("forward before set_weights")
         a = vb.Fp8.empty(self.rows, self.hidden, self.device)
         vb.vsa2_fp8_quantize(x.view(self.rows, self.hidden), a)
         packed = self._empty(self.rows, self.width)
@@ -74,12 +79,23 @@ class Vsa2Layer:
         self.attn.route(q, k)
         o, lse = self.attn.forward(q, k, v, gate)
         self.saved = (x, video, packed, q, k, v, gate, o, lse)
+        self.kept = self._versions(x, o)
         return o
+
+    def _versions(self, x, o):
+        """What backward needs unchanged, as it is now: torch's counters of changes in place, and the number of updates."""
+        tensors = {"x": x, "o": o, "w_g": self.w_g, "q_weight": self.q_weight, "k_weight": self.k_weight}
+        return {"the weights (set_weights)": self.updates, **{k: None if t is None or t.is_inference() else t._version for k, t in tensors.items()}}
 
     def backward(self, d_o):
         """d_o [B, Hq, L + Lt, D] bf16 -> dict of dx [B, L + Lt, C] bf16 and, in fp32, dw_qkv, dw_g, dq_weight, dk_weight."""
         p, torch = self.p, self.torch
+        if self.saved is None:
+            raise RuntimeError("backward without a forward before it")
         x, video, packed, q, k, v, gate, o, lse = self.saved
+        changed = [name for name, version in self._versions(x, o).items() if version != self.kept[name]]
+        if changed:
+            raise RuntimeError(f"changed between forward and backward: {', '.join(changed)}")
         self._expect(d_o, "the output's gradient", tuple(o.shape), torch.bfloat16)
         dq, dk, dv, dgate = self.attn.backward(q, k, v, gate, o, lse, d_o)
         d_packed = torch.empty_like(packed)

@@ -55,3 +55,38 @@ def test_master_weights_in_fp32_and_norms_without_weights():
     room[:, 3:131] = w[0]
     layer.set_weights(room[:, 3:131], w[1], None, None)            # (rows of a larger matrix)
     assert torch.equal(layer.forward(x), want)
+
+
+@pytest.mark.parametrize("change", ["x", "o", "w_g", "q_weight", "k_weight", "set_weights"])
+def test_backward_of_a_forward_whose_tensors_have_changed(change):
+    """Gradients would be of a mixture of two states: x is quantised again for dW, the weights are read again."""
+    layer, w, x, d_o = problem()
+    layer.set_weights(*w)
+    o = layer.forward(x)
+    want = layer.backward(d_o)
+    if change == "set_weights":
+        layer.set_weights(*w)
+    else:
+        {"x": x, "o": o, "w_g": w[1], "q_weight": w[2], "k_weight": w[3]}[change].mul_(1)
+    with pytest.raises(RuntimeError, match=change):
+        layer.backward(d_o)
+    layer.forward(x)
+    again = layer.backward(d_o)
+    assert all(torch.equal(want[k], again[k]) for k in want)
+
+
+def test_calls_before_those_they_need():
+    layer, w, x, d_o = problem()
+    with pytest.raises(RuntimeError, match="set_weights"):
+        layer.forward(x)
+    layer.set_weights(*w)
+    with pytest.raises(RuntimeError, match="forward"):
+        layer.backward(d_o)
+
+
+def test_tensors_of_inference_mode():
+    with torch.inference_mode():
+        layer, w, x, d_o = problem()
+        layer.set_weights(*w)
+        layer.forward(x)
+        layer.backward(d_o)
