@@ -216,14 +216,27 @@ static int get_norm(PyObject* on, PyObject* eps, PyObject* qw, PyObject* kw, int
   *out = norm;
   return 0;
 }
-/* an Fp8 object; its shape */
+/* values and scales of a matrix in 8-bit form, on any device: its shape and strides */
+static int fp8_form(PyObject* values, PyObject* scales, int64_t* shape, int64_t* stride) {
+  int64_t of[3];
+  int rank, typed = is_type(values, t_e4m3);
+  if (typed < 0 || (rank = integers(PyObject_GetAttr(values, n_shape), shape, 2)) < 0) return -1;
+  if (rank == 2 && integers(PyObject_CallMethodNoArgs(values, n_stride), stride, 2) != 2) return -1;
+  if (!typed || rank != 2 || (shape[1] > 1 && stride[1] != 1)) return refuse("values must be float8_e4m3fn [rows, cols] with contiguous rows");
+  typed = is_type(scales, t_u8);
+  if (typed < 0 || (rank = integers(PyObject_GetAttr(scales, n_shape), of, 3)) < 0) return -1;
+  if (!typed || rank != 3 || of[0] != (shape[1] + 511) / 512 || of[1] != shape[0] || of[2] != 4)
+    return refuse("scales must be uint8 [ceil(cols / 512), rows, 4]");
+  return 0;
+}
+/* an Fp8 object; its shape.  (Its members may have been assigned, or resized, since it was made: they are looked at again at every call, 0.1 us.) */
 static int get_fp8(PyObject* o, vsa2_fp8* v, int64_t* shape) {
   int bad = -1;
   int64_t stride[2];
   void* scales;
   PyObject *values = PyObject_GetAttr(o, n_values), *s = values != NULL ? PyObject_GetAttr(o, n_scales) : NULL;
-  if (s == NULL || on_gpu(values, "expected a CUDA tensor") || integers(PyObject_GetAttr(values, n_shape), shape, 2) != 2 || fits_int(shape, 2) ||
-      integers(PyObject_CallMethodNoArgs(values, n_stride), stride, 2) != 2 || address(values, &v->values) || get_memory(s, &scales, NULL))
+  if (s == NULL || on_gpu(values, "expected a CUDA tensor") || fp8_form(values, s, shape, stride) || fits_int(shape, 2) || address(values, &v->values) ||
+      get_memory(s, &scales, NULL))
     goto out;
   v->scales = (uint8_t*)scales;
   v->ld = shape[0] > 1 ? stride[0] : (shape[1] + 15) / 16 * 16;
@@ -231,7 +244,6 @@ static int get_fp8(PyObject* o, vsa2_fp8* v, int64_t* shape) {
 out:
   Py_XDECREF(values);
   Py_XDECREF(s);
-  if (bad && !PyErr_Occurred()) refuse("values must be a matrix");
   return bad;
 }
 /* a CUDA matrix with contiguous rows */
@@ -339,23 +351,8 @@ static PyObject* matmul(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 /* (values, scales): whether they are a matrix in 8-bit form */
 static PyObject* check_fp8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  int64_t shape[2], stride[2], of[3];
-  int r;
-  if (arguments(n, 2)) return NULL;
-  r = is_type(a[0], t_e4m3);
-  if (r < 0) return NULL;
-  int rank = integers(PyObject_GetAttr(a[0], n_shape), shape, 2);
-  if (rank < 0 || (rank == 2 && integers(PyObject_CallMethodNoArgs(a[0], n_stride), stride, 2) != 2)) return NULL;
-  if (!r || rank != 2 || (shape[1] > 1 && stride[1] != 1)) {
-    refuse("values must be float8_e4m3fn [rows, cols] with contiguous rows");
-    return NULL;
-  }
-  r = is_type(a[1], t_u8);
-  if (r < 0 || (rank = integers(PyObject_GetAttr(a[1], n_shape), of, 3)) < 0) return NULL;
-  if (!r || rank != 3 || of[0] != (shape[1] + 511) / 512 || of[1] != shape[0] || of[2] != 4) {
-    refuse("scales must be uint8 [ceil(cols / 512), rows, 4]");
-    return NULL;
-  }
+  int64_t shape[2], stride[2];
+  if (arguments(n, 2) || fp8_form(a[0], a[1], shape, stride)) return NULL;
   Py_RETURN_NONE;
 }
 
