@@ -265,6 +265,14 @@ static int get_stream(PyObject* s, void** out) { /* None, a handle, or a stream 
   Py_DECREF(v);
   return *out == NULL && PyErr_Occurred() ? -1 : 0;
 }
+/* The library's answer, called without the interpreter's lock as ctypes does it: a launch can wait (full queue, first load of a kernel), and a host function on that
+ * stream that needs the lock would then never run.  (The caller holds the arguments.) */
+#define CALLED(call)                                        \
+  do {                                                      \
+    int code_;                                              \
+    Py_BEGIN_ALLOW_THREADS code_ = (call);                  \
+    Py_END_ALLOW_THREADS return PyLong_FromLong(code_);     \
+  } while (0)
 static int arguments(Py_ssize_t n, Py_ssize_t want) {
   if (n == want) return 0;
   PyErr_Format(PyExc_TypeError, "%zd arguments are expected, not %zd", want, n);
@@ -283,7 +291,7 @@ static PyObject* rope_apply(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   if (arguments(n, 8) || get_rope(a[0], &store, &rope) || get_view(a[1], &x) || get_view(a[2], &y) || get_place(a[3], a[4], a[5], &x, &place) ||
       (inverse = PyObject_IsTrue(a[6])) < 0 || get_stream(a[7], &stream))
     return NULL;
-  return PyLong_FromLong(f_rope_apply(rope, &place, &x, &y, inverse, stream));
+  CALLED(f_rope_apply(rope, &place, &x, &y, inverse, stream));
 }
 /* (rope, x, y, q_weight, k_weight, eps, norm, grid, first, positions, stream) */
 static PyObject* qkv_fwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -297,7 +305,7 @@ static PyObject* qkv_fwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   if (arguments(n, 11) || get_rope(a[0], &store, &rope) || get_views(a[1], x, 3) || get_views(a[2], y, 3) ||
       get_norm(a[6], a[5], a[3], a[4], x[0].channels, &norm, &with) || get_place(a[7], a[8], a[9], &x[0], &place) || get_stream(a[10], &stream))
     return NULL;
-  return PyLong_FromLong(f_qkv_fwd(rope, &place, with, x, y, stream));
+  CALLED(f_qkv_fwd(rope, &place, with, x, y, stream));
 }
 /* (rope, x, dy, dx, q_weight, k_weight, d_q_weight, d_k_weight, workspace, eps, norm, grid, first, positions, stream) */
 static PyObject* qkv_bwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -314,7 +322,7 @@ static PyObject* qkv_bwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
       get_weight(a[6], dy[0].channels, &dq) || get_weight(a[7], dy[0].channels, &dk) || get_memory(a[8], &workspace, &bytes) ||
       get_place(a[11], a[12], a[13], &dy[0], &place) || get_stream(a[14], &stream))
     return NULL;
-  return PyLong_FromLong(f_qkv_bwd(rope, &place, with, with != NULL ? x : NULL, dy, dx, (float*)dq, (float*)dk, workspace, bytes, stream));
+  CALLED(f_qkv_bwd(rope, &place, with, with != NULL ? x : NULL, dy, dx, (float*)dq, (float*)dk, workspace, bytes, stream));
 }
 /* (x, out, out_t, squares, stream) */
 static PyObject* quantize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -330,7 +338,7 @@ static PyObject* quantize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     refuse("outputs do not have the shape of x and of its transpose");
     return NULL;
   }
-  return PyLong_FromLong(f_quantize(x, type, (int32_t)shape[0], (int32_t)shape[1], ld, squares, a[1] != Py_None ? &out : NULL,
+  CALLED(f_quantize(x, type, (int32_t)shape[0], (int32_t)shape[1], ld, squares, a[1] != Py_None ? &out : NULL,
                                     a[2] != Py_None ? &out_t : NULL, stream));
 }
 /* (a, b, c, workspace, stream) */
@@ -347,7 +355,7 @@ static PyObject* matmul(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     refuse("the shapes of a, b and c do not fit");
     return NULL;
   }
-  return PyLong_FromLong(f_matmul((int32_t)of_a[0], (int32_t)of_b[0], (int32_t)of_a[1], &va, &vb, c, type, ld, workspace, bytes, stream));
+  CALLED(f_matmul((int32_t)of_a[0], (int32_t)of_b[0], (int32_t)of_a[1], &va, &vb, c, type, ld, workspace, bytes, stream));
 }
 /* (values, scales): whether they are a matrix in 8-bit form */
 static PyObject* check_fp8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
