@@ -19,18 +19,43 @@ def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
 
 
+def _older(path, *deps):
+    """Whether `path` is missing or older than one of `deps`."""
+    return not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in deps)
+
+
+def _header():
+    return os.path.join(ROOT, "include", "vsa2.h")
+
+
 def _stale():
-    if not os.path.exists(LIB_PATH) or not os.path.exists(MARSHAL_PATH):
-        return True
-    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(MARSHAL_PATH))
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "vsa2.h")]
-    return any(os.path.getmtime(d) > t for d in deps)
+    return _older(LIB_PATH, *(os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".c")), _header())
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compiles csrc/*.cu into libvsa2.so next to this file, and csrc/marshal.c into _marshal.so; returns the library's path."""
-    if not force and not _stale():
-        return LIB_PATH
+    """Compiles csrc/*.cu into libvsa2.so next to this file, and csrc/marshal.c into _marshal.so; returns the library's path.
+
+    The library stands without the module (attention, gate, router go through ctypes): where the module cannot be compiled, say without Python's
+    headers, that is said on stderr and the calls that need it fail (binding._marshal)."""
+    if force or _stale():
+        _build_cuda(force, verbose)
+    if force or _older(MARSHAL_PATH, os.path.join(CSRC, "marshal.c"), _header()):
+        _build_marshal()
+    return LIB_PATH
+
+
+def _build_marshal():
+    if os.path.exists(MARSHAL_PATH):
+        os.remove(MARSHAL_PATH)      # (of another header's structs)
+    try:
+        subprocess.run([shutil.which("gcc") or "cc", "-shared", "-fPIC", "-O2", "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
+                        os.path.join(CSRC, "marshal.c"), "-o", MARSHAL_PATH], check=True, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    except (OSError, subprocess.CalledProcessError) as e:
+        said = (getattr(e, "output", None) or b"").decode(errors="replace")
+        sys.stderr.write(f"{said}{os.path.basename(MARSHAL_PATH)} was not built ({e}): the calls between hidden states and attention will fail\n")
+
+
+def _build_cuda(force, verbose):
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     objs = []
     obj_dir = os.path.join(HERE, "build")
@@ -54,10 +79,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(out.decode())
         if pr.returncode:
             raise RuntimeError(f"nvcc failed on {src}")
-    subprocess.check_call([shutil.which("gcc") or "cc", "-shared", "-fPIC", "-O2", "-I", sysconfig.get_paths()["include"], "-I",
-                           os.path.join(ROOT, "include"), os.path.join(CSRC, "marshal.c"), "-o", MARSHAL_PATH])
     subprocess.check_call([nvcc, "-shared", "-o", LIB_PATH] + objs + ARCH_FLAGS + ["-lcudart_static", "-ldl", "-lrt", "-lpthread"])
-    return LIB_PATH
 
 
 if __name__ == "__main__":
