@@ -38,7 +38,7 @@ EXPORTS = ("vsa2_query_sizes", "vsa2_route", "vsa2_route_scores", "vsa2_attn_fwd
            "vsa2_route_scratch", "vsa2_route_scratch_bytes", "vsa2_permute_cube_major",
            "vsa2_selftest_timeout", "vsa2_debug_rescue_capacity", "vsa2_selftest_divmod",
            "vsa2_rope_plan", "vsa2_rope_apply", "vsa2_qkv_fwd", "vsa2_qkv_bwd", "vsa2_qkv_bwd_workspace_bytes",
-           "vsa2_fp8_quantize", "vsa2_fp8_matmul", "vsa2_fp8_matmul_workspace_bytes")
+           "vsa2_fp8_quantize", "vsa2_fp8_matmul", "vsa2_fp8_matmul_workspace_bytes", "vsa2_debug_fp8_matmul_plan")
 
 KERNELS = ("pool", "router_lse", "router_pool", "select", "coarse_fwd", "fine_fwd", "bwd_pre", "coarse_bwd",
            "fine_bwd_dq", "fine_bwd_dkv", "pool_router")
@@ -159,6 +159,7 @@ def _lib():
         lib.vsa2_fp8_quantize.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int32, vp, vp, vp]
         lib.vsa2_fp8_matmul.argtypes = [C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, C.c_int32, C.c_int64, vp, sz, vp]
         lib.vsa2_fp8_matmul_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+        lib.vsa2_debug_fp8_matmul_plan.argtypes = [C.c_int32] * 7 + [vp]
         for fn in (lib.vsa2_qkv_bwd_workspace_bytes, lib.vsa2_fp8_matmul_workspace_bytes):
             fn.restype = C.c_size_t
         for name in EXPORTS:
@@ -443,6 +444,13 @@ def vsa2_fp8_matmul(a, b, c, workspace, stream=None):
     code = (_MARSHAL or _marshal()).matmul(a, b, c, workspace, stream)
     if code != OK:
         raise Vsa2Error(code, "vsa2_fp8_matmul")
+
+
+def vsa2_debug_fp8_matmul_plan(m, n, k, c_dtype=BF16, c_aligned=True, sms=148, pairs=True):
+    """(columns of a tile, CTAs that share one, whether A's rows are its lanes, ranges of K, tiles along the columns' operand, tiles taken together); host arithmetic."""
+    out = (C.c_int32 * 6)()
+    _check(_lib().vsa2_debug_fp8_matmul_plan(m, n, k, c_dtype, c_aligned, sms, pairs, out), "vsa2_debug_fp8_matmul_plan")
+    return tuple(out)
 
 
 def vsa2_profile_events(kernel_id: int, start_event, stop_event):

@@ -1179,6 +1179,12 @@ int vsa2_fp8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_fp8* a, const vs
   return VSA2_OK;
 }
 
+int vsa2_debug_fp8_matmul_plan(int32_t m, int32_t n, int32_t k, int32_t c_dtype, int32_t c_aligned, int32_t sms, int32_t pairs, int32_t out[6]) {
+  if (m <= 0 || n <= 0 || k <= 0 || sms <= 0 || (c_dtype != VSA2_BF16 && c_dtype != VSA2_F32) || out == nullptr) return VSA2_ERR_INVALID_ARG;
+  fp8_matmul_plan(m, n, k, c_dtype == VSA2_F32, c_aligned != 0, sms, pairs != 0, out);
+  return VSA2_OK;
+}
+
 int vsa2_device_status(const void* workspace, void* cuda_stream, int32_t* status_out) {
   if (workspace == nullptr || status_out == nullptr) return VSA2_ERR_INVALID_ARG;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);

@@ -625,6 +625,14 @@ MmPlan plan_mm(const MmCall& c, bool swap) {
   return plan;
 }
 
+// Tiles along Q that are taken together, under all of P's rows one after the other: half a round of pairs, as far as their rows lie in L2 (48 MB).
+// 75600 x 15360 x 5120, us: 6 tiles 4910, 12 4630, 24 4640, 37 4540, 74 5370
+int tiles_together(int columns, int kb, int qt) {
+  const long long group = (48LL << 20) / ((long long)columns * kb * 128);
+  const int together = (int)(group < 4 ? 4 : group > 37 ? 37 : group);
+  return together < qt ? together : qt;
+}
+
 template <int NT, int PAIR, bool SWAP, typename TO>
 cudaError_t launch_tiles(const MmCall& c, const MmPlan& plan, void* result, long long ldc, long long split_stride) {
   using T = MmTile<NT, PAIR, TO>;
@@ -634,11 +642,7 @@ cudaError_t launch_tiles(const MmCall& c, const MmPlan& plan, void* result, long
   a.q_rows = SWAP ? c.n : c.m;
   a.kb = c.kb;
   a.pt = plan.pt; a.qt = plan.qt; a.splits = plan.splits;
-  // Tiles along Q that are taken together, under all of P's rows one after the other: half a round of pairs, as far as their rows lie in L2 (48 MB).
-  // 75600 x 15360 x 5120, us: 6 tiles 4910, 12 4630, 24 4640, 37 4540, 74 5370
-  const long long group = (48LL << 20) / ((long long)NT * c.kb * 128);
-  a.gq = (int)(group < 4 ? 4 : group > 37 ? 37 : group);
-  if (a.gq > a.qt) a.gq = a.qt;
+  a.gq = tiles_together(NT, c.kb, a.qt);
   a.by_tiles = divisor((long long)a.pt * a.qt);
   a.by_group = divisor((long long)a.gq * a.pt);
   a.by_gq = divisor(a.gq);
@@ -676,6 +680,28 @@ cudaError_t launch_mm(const MmCall& c, const MmPlan& plan) {
                : launch_kernel(fp8_sum_kernel<bf16>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, by_row, reinterpret_cast<bf16*>(c.c), c.ldc);
 }
 
+// The kernel of a call: columns of a tile, CTAs that share one, which operand's rows are its lanes.  `pairs`: takes_pairs, and the context has room for one
+struct MmChoice {
+  int columns, pair;
+  bool swap;
+  MmPlan plan;
+};
+bool takes_pairs(const MmCall& call) { return call.m > 32 && call.n > 128 && call.ctas >= 2; }      // (wherever B has rows for both)
+MmChoice choose_mm(const MmCall& call, bool pairs) {
+  if (call.m <= 32) return {32, 1, false, plan_mm<32, 1>(call, false)};
+  if (!pairs) return {128, 1, false, plan_mm<128, 1>(call, false)};
+  const MmPlan narrow = plan_mm<128, 2>(call, false);
+  if (call.m <= 128) return {128, 2, false, narrow};
+  // The columns that waste least (256 x 4608 x 1536: two tiles of 128 instead of two of 224, 8.2 us instead of 9.5), and A's rows as the lanes, B's as the columns where that
+  // fills the rounds better (512 x 15360 x 5120: 138 tiles instead of 180 on 74 pairs, 33 us instead of 45)
+  const MmPlan wide = plan_mm<224, 2>(call, false);
+  if (call.tensor_stores) {
+    const MmPlan swapped = plan_mm<224, 2>(call, true);
+    if (swapped.cycles < wide.cycles && swapped.cycles < narrow.cycles) return {224, 2, true, swapped};
+  }
+  return narrow.cycles < wide.cycles ? MmChoice{128, 2, false, narrow} : MmChoice{224, 2, false, wide};
+}
+
 // most elements of a product whose K is cut: tiles x ranges are at most the CTAs (or pairs)
 size_t parts_elements(int m) { return (size_t)kMmCtas * 128 * (m <= 32 ? 32 : m <= 128 ? 128 : 224); }
 
@@ -705,23 +731,28 @@ cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Ar
   call.status = reinterpret_cast<StatusBlock*>(ws);
   call.parts = reinterpret_cast<float*>(ws + align_up(sizeof(StatusBlock), 256));
   call.st = st;
-  if (m <= 32) return launch_mm<32, 1>(call, plan_mm<32, 1>(call, false));
-  // Pairs wherever B has rows for both and the context has room for one
-  bool pair = n > 128 && call.ctas >= 2;
-  if (pair) {
+  bool pairs = takes_pairs(call);
+  if (pairs) {
     static ClusterRoom room;
-    if ((e = cluster_room((const void*)fp8_matmul_kernel<224, 2, false, float>, room, 2, kMmThreads, MmTile<224, 2, float>::SMEM, &pair))) return e;
+    if ((e = cluster_room((const void*)fp8_matmul_kernel<224, 2, false, float>, room, 2, kMmThreads, MmTile<224, 2, float>::SMEM, &pairs))) return e;
   }
-  if (!pair) return launch_mm<128, 1>(call, plan_mm<128, 1>(call, false));
-  if (m <= 128) return launch_mm<128, 2>(call, plan_mm<128, 2>(call, false));
-  // The columns that waste least (256 x 4608 x 1536: two tiles of 128 instead of two of 224, 8.2 us instead of 9.5), and A's rows as the lanes, B's as the columns where that
-  // fills the rounds better (512 x 15360 x 5120: 138 tiles instead of 180 on 74 pairs, 33 us instead of 45)
-  const MmPlan wide = plan_mm<224, 2>(call, false), narrow = plan_mm<128, 2>(call, false);
-  if (call.tensor_stores) {
-    const MmPlan swapped = plan_mm<224, 2>(call, true);
-    if (swapped.cycles < wide.cycles && swapped.cycles < narrow.cycles) return launch_tiles<224, 2, true, bf16>(call, swapped, c, ldc, 0);
-  }
-  return narrow.cycles < wide.cycles ? launch_mm<128, 2>(call, narrow) : launch_mm<224, 2>(call, wide);
+  const MmChoice choice = choose_mm(call, pairs);
+  if (choice.swap) return launch_tiles<224, 2, true, bf16>(call, choice.plan, c, ldc, 0);
+  if (choice.columns == 32) return launch_mm<32, 1>(call, choice.plan);
+  if (choice.pair == 1) return launch_mm<128, 1>(call, choice.plan);
+  return choice.columns == 128 ? launch_mm<128, 2>(call, choice.plan) : launch_mm<224, 2>(call, choice.plan);
+}
+
+void fp8_matmul_plan(int m, int n, int k, int c_f32, bool tensor_stores, int sms, bool pairs, int32_t* out) {
+  MmCall call = {};
+  call.m = m; call.n = n; call.k = k;
+  call.kb = (k + 127) / 128;
+  call.ctas = sms < kMmCtas ? sms : kMmCtas;
+  call.f32 = c_f32 != 0;
+  call.tensor_stores = !c_f32 && tensor_stores;
+  const MmChoice choice = choose_mm(call, pairs && takes_pairs(call));
+  out[0] = choice.columns; out[1] = choice.pair; out[2] = choice.swap;
+  out[3] = choice.plan.splits; out[4] = choice.plan.qt; out[5] = tiles_together(choice.columns, call.kb, choice.plan.qt);
 }
 
 }  // namespace vsa2

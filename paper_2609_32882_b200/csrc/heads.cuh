@@ -60,6 +60,8 @@ cudaError_t launch_fp8_quantize(const void* x, int x_f32, int rows, int cols, lo
                                 const Fp8Arg& out_t, cudaStream_t st);
 
 size_t fp8_matmul_workspace_bytes(int m, int n, int k);
+// vsa2_debug_fp8_matmul_plan
+void fp8_matmul_plan(int m, int n, int k, int c_f32, bool tensor_stores, int sms, bool pairs, int32_t* out);
 cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& a, const Fp8Arg& b, void* c, int c_f32, long long ldc,
                               void* workspace, cudaStream_t st);
 
