@@ -405,8 +405,8 @@ int vsa2_fp8_quantize(const void* x, int32_t x_dtype, int32_t rows, int32_t cols
 
 /* C [m, n] = A B^T with A [m, k] and B [n, k] in 8-bit form; products and sums in the tensor cores' fp32, C in bf16 or fp32 with row stride ldc
  * elements.  The tile shapes suit B as the operand with many rows (a projection's weights [out, in]) and any m from 1.
- *   workspace: device, 256-byte aligned, at least vsa2_fp8_matmul_workspace_bytes(m, n, k); one may serve all calls up to that size that follow one
- *   another on a stream.  Its first word is the status of vsa2_device_status (the caller zeroes the first 256 bytes once); the rest need not be set.
+ *   workspace: device, 256-byte aligned, at least vsa2_fp8_matmul_workspace_bytes(m, n, k); one may serve all calls with an m, n and k of at most
+ *   those that follow one another on a stream.  Its first word is the status of vsa2_device_status (the caller zeroes the first 256 bytes once); the rest need not be set.
  * Results do not depend on timing: the parts of a sum are added in a fixed order. */
 size_t vsa2_fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
 int vsa2_fp8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_fp8* a, const vsa2_fp8* b, void* c, int32_t c_dtype, int64_t ldc,

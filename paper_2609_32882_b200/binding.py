@@ -436,7 +436,9 @@ def vsa2_fp8_matmul_workspace_bytes(m, n, k) -> int:
 def fp8_matmul_workspace(m, n, k, device="cuda"):
     """Workspace of vsa2_fp8_matmul for products up to this size that follow one another on a stream."""
     import torch
-    return torch.zeros(vsa2_fp8_matmul_workspace_bytes(m, n, k), dtype=torch.uint8, device=device)
+    workspace = torch.empty(vsa2_fp8_matmul_workspace_bytes(m, n, k), dtype=torch.uint8, device=device)
+    workspace[:256].zero_()          # status block
+    return workspace
 
 
 def vsa2_fp8_matmul(a, b, c, workspace, stream=None):

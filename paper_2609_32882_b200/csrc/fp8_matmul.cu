@@ -702,17 +702,19 @@ MmChoice choose_mm(const MmCall& call, bool pairs) {
   return narrow.cycles < wide.cycles ? MmChoice{128, 2, false, narrow} : MmChoice{224, 2, false, wide};
 }
 
-// most elements of a product whose K is cut: tiles x ranges are at most the CTAs (or pairs)
-size_t parts_elements(int m) { return (size_t)kMmCtas * 128 * (m <= 32 ? 32 : m <= 128 ? 128 : 224); }
+// Most elements of the ranges of a product of up to m, n and k: tiles x ranges are at most the CTAs (or pairs), ranges at most the blocks of K.  (Grows with each of the three,
+// so that one workspace serves smaller products, which are cut where a large one is not.)
+size_t parts_elements(int m, int n, int k) {
+  const size_t all = (size_t)kMmCtas * 128 * (m <= 32 ? 32 : m <= 128 ? 128 : 224), one = (size_t)m * (((size_t)n + 3) / 4 * 4);
+  const int kb = (int)(((long long)k + 127) / 128), most = kb < kMmSplits ? kb : kMmSplits;
+  if (most < 2) return 0;
+  return one < all / most ? one * most : all;
+}
 
 }  // namespace
 
 // [status][ranges of K]
-size_t fp8_matmul_workspace_bytes(int m, int n, int k) {
-  (void)n;
-  (void)k;
-  return align_up(sizeof(StatusBlock), 256) + parts_elements(m) * sizeof(float);
-}
+size_t fp8_matmul_workspace_bytes(int m, int n, int k) { return align_up(sizeof(StatusBlock), 256) + parts_elements(m, n, k) * sizeof(float); }
 
 cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Arg& fb, void* c, int c_f32, long long ldc,
                               void* workspace, cudaStream_t st) {

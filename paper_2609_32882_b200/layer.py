@@ -32,7 +32,8 @@ class Vsa2Layer:
         self.w, self.w_t = vb.Fp8.empty(self.width, hidden, device), vb.Fp8.empty(hidden, self.width, device)
         need = max(vb.vsa2_fp8_matmul_workspace_bytes(*s) for s in ((self.rows, self.width, hidden), (self.rows, hidden, self.width),
                                                                     (self.width, hidden, self.rows)))
-        self.ws_matmul = torch.zeros(need, dtype=torch.uint8, device=device)
+        self.ws_matmul = torch.empty(need, dtype=torch.uint8, device=device)
+        self.ws_matmul[:256].zero_()      # status block
         self.ws_qkv = torch.empty(vb.vsa2_qkv_bwd_workspace_bytes(p.head_dim), dtype=torch.uint8, device=device)
         self.ws_gate = torch.empty(max(256, vb.vsa2_gate_bwd_workspace_bytes(p, hidden)), dtype=torch.uint8, device=device)
         self.w_g = self.q_weight = self.k_weight = None
