@@ -366,7 +366,8 @@ typedef struct vsa2_heads {
 int vsa2_rope_apply(const vsa2_rope* rope, const vsa2_place* place, const vsa2_heads* x, const vsa2_heads* y, int32_t inverse,
                     void* cuda_stream);
 
-/* Norm of every head of q and k: x / sqrt(mean over the channels of x^2 + eps) * weight.  Weights device fp32 [channels], NULL: ones. */
+/* Norm of every head of q and k: x / sqrt(mean over the channels of x^2 + eps) * weight, for rows of any finite size (their squares may lie beyond fp32's range).  Weights device
+ * fp32 [channels], NULL: ones. */
 typedef struct vsa2_qk_norm {
   const float* q_weight;
   const float* k_weight;

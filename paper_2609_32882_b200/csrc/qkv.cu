@@ -166,6 +166,73 @@ __device__ __forceinline__ float team_sums(float (&t)[N], int l) {
   return t[0];
 }
 
+// Rows whose mean square lies outside are normed with their channels scaled by a power of two: their squares, or the backward's r^3, could vanish or pass fp32's range (a channel of 2e19
+// made a whole head zero).  Inside, nothing is near either end, whatever the gradients; with the usual eps no row is below.
+constexpr float kPlainLeast = 0x1p-40f, kPlainMost = 0x1p40f;
+// Positive numbers in the order of their bits, those below kPlainLeast and what is not a number behind all others
+__device__ __forceinline__ uint32_t beyond_least(float mean_square) { return __float_as_uint(mean_square) - __float_as_uint(kPlainLeast); }
+__device__ __forceinline__ bool plain_row(float mean_square) { return beyond_least(mean_square) <= beyond_least(kPlainMost); }
+// 1 / sqrt of a plain row's: the instruction alone, without the steps for numbers below the normal ones
+__device__ __forceinline__ float rsqrt_plain(float t) {
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+  return r;
+}
+// The power of two that brings the larger of a row's largest magnitude and sqrt(eps) to about one; one where that is zero or not finite.  (By the threads of a team together)
+template <int TEAM>
+__device__ __forceinline__ float row_scale(const float (&f)[8], float eps) {
+  float top = sqrtf(eps);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
+#pragma unroll
+  for (int o = TEAM / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const int e = __float_as_int(top) >> 23;
+  return top == 0.f || e == 255 ? 1.f : __int_as_float(max(254 - e, 1) << 23);
+}
+
+// The rows of a warp that are not plain, once more on scaled channels.  Rare, and a function of its own: as a branch among the rows 480p, 24 heads, halves as pairs took 199.5 us, without
+// the look at them 197.5, 197.7 so.
+template <int D, typename TI, typename TO, bool HALVES>
+__device__ __noinline__ void scaled_rows_fwd(const QkvArgs& a, const unsigned long long* turns) {
+  constexpr int TEAM = D / 8, ROWS = kQkvThreads / TEAM;
+  const int l = threadIdx.x % TEAM;
+  const int b = divided(blockIdx.x, a.by_tiles), row = ((int)blockIdx.x - b * a.tiles) * ROWS + threadIdx.x / TEAM, tok = min(row, a.tokens - 1);
+  Turn<D, HALVES> turn;
+  turn.init(a.turn, turns, b, tok, l);
+  const int h_lo = blockIdx.z * a.per_cta, h_hi = h_lo + a.per_cta;
+  int base = 0;
+#pragma unroll 1
+  for (int seg = 0; seg < 2; ++seg) {
+    const HeadsArg x = a.x[seg], y = a.y[seg];
+    const int lo = max(h_lo - base, 0), hi = min(h_hi - base, x.heads);
+    base += x.heads;
+    const TI* xp = reinterpret_cast<const TI*>(x.p) + b * x.sb + tok * x.st + l * 8;
+    TO* yp = reinterpret_cast<TO*>(y.p) + b * y.sb + tok * y.st + l * 8;
+#pragma unroll 1
+    for (int h = lo; h < hi; ++h) {
+      Raw8<TI> raw;
+      raw.load(xp + h * x.sh);
+      float f[8];
+      raw.get(f);
+      float ss[1] = {0.f};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss[0] += f[i] * f[i];
+      const bool plain = plain_row(team_sums<TEAM>(ss, l) * (1.f / D) + a.eps);      // (one on the edge may come out either way: both ways are right there)
+      const float s = row_scale<TEAM>(f, a.eps);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] *= s;
+      float scaled[1] = {0.f};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) scaled[0] += f[i] * f[i];
+      const float r = rsqrtf(team_sums<TEAM>(scaled, l) * (1.f / D) + a.eps * s * s);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] *= r * (a.w[seg] != nullptr ? a.w[seg][l * 8 + i] : 1.f);
+      turn.apply(f);
+      if (row < a.tokens && !plain) store8(yp + h * y.sh, f);
+    }
+  }
+}
+
 // grid (token tiles of all batch entries, 1, groups of heads)
 template <int D, typename TI, typename TO, bool HALVES>
 __global__ void __launch_bounds__(kQkvThreads) qkv_fwd_kernel(const __grid_constant__ QkvArgs a) {
@@ -181,6 +248,7 @@ __global__ void __launch_bounds__(kQkvThreads) qkv_fwd_kernel(const __grid_const
   Turn<D, HALVES> turn;
   turn.init(a.turn, turns, b, tok, l);
   const int h_lo = blockIdx.z * a.per_cta, h_hi = h_lo + a.per_cta;
+  uint32_t farthest = 0u;      // of the rows' mean squares
   int base = 0;
 #pragma unroll 1
   for (int seg = 0; seg < 3; ++seg) {
@@ -209,7 +277,9 @@ __global__ void __launch_bounds__(kQkvThreads) qkv_fwd_kernel(const __grid_const
 #pragma unroll
           for (int i = 0; i < 8; ++i) ss[u] += f[i] * f[i];
         }
-        r = rsqrtf(team_sums<TEAM>(ss, l) * (1.f / D) + a.eps);
+        const float t = team_sums<TEAM>(ss, l) * (1.f / D) + a.eps;
+        farthest = max(farthest, beyond_least(t));
+        r = rsqrt_plain(t);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -225,6 +295,7 @@ __global__ void __launch_bounds__(kQkvThreads) qkv_fwd_kernel(const __grid_const
       }
     }
   }
+  if (__any_sync(0xffffffffu, farthest > beyond_least(kPlainMost))) scaled_rows_fwd<D, TI, TO, HALVES>(a, turns);
 }
 
 // A thread's own queue in shared memory: 16-byte pieces that it asks for AHEAD rows before it uses them.  (Registers for that many in flight would cost the CTAs
@@ -234,9 +305,95 @@ __device__ __forceinline__ void copy_async(void* to, const void* from) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
 
+// A row's sums over its team: x^2, and the weighted gradient along x.  (Two channels an instruction: 16 warps' issue slots are the next bound behind memory)
+template <int TEAM>
+__device__ __forceinline__ float2 row_sums(const float (&x)[8], const float (&g)[8], const float2 (&w)[4]) {
+  float2 ss = make_float2(0.f, 0.f), dot = ss;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x2 = make_float2(x[2 * i], x[2 * i + 1]), g2 = make_float2(g[2 * i], g[2 * i + 1]);
+    ss = __ffma2_rn(x2, x2, ss);
+    dot = __ffma2_rn(__fmul2_rn(g2, w[i]), x2, dot);
+  }
+  float2 sums = make_float2(ss.x + ss.y, dot.x + dot.y);
+#pragma unroll
+  for (int o = TEAM / 2; o > 0; o >>= 1)
+    sums = __fadd2_rn(sums, make_float2(__shfl_xor_sync(0xffffffffu, sums.x, o), __shfl_xor_sync(0xffffffffu, sums.y, o)));
+  return sums;
+}
+// g -> dx = r (w g) + m x; the weight's gradient gets g r x
+__device__ __forceinline__ void dx_row(float (&g)[8], const float (&x)[8], const float2 (&w)[4], float2 (&dw)[4], float r, float m, bool counts) {
+  const float2 r2 = make_float2(r, r), m2 = make_float2(m, m);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x2 = make_float2(x[2 * i], x[2 * i + 1]), gr = __fmul2_rn(make_float2(g[2 * i], g[2 * i + 1]), r2);
+    if (counts) dw[i] = __ffma2_rn(gr, x2, dw[i]);
+    const float2 o = __ffma2_rn(x2, m2, __fmul2_rn(gr, w[i]));
+    g[2 * i] = o.x;
+    g[2 * i + 1] = o.y;
+  }
+}
+
+struct BwdJobs { int ctas[2], jobs[2], per[2]; };      // of q, of k: CTAs, jobs, heads in a group
+// The rows of a warp among which one is not plain, once more: such a row on scaled channels (x r does not change, dx is the scale's multiple), and the weight's gradient summed anew.
+// Rare, and a function of its own so that the plain rows keep their registers: 480p with text 156.3 us without the look at the rows, 167 with a branch at each row, 160 with this in the
+// kernel, 157.5 so.
+template <int D, typename TI, typename TG, typename TO, bool HALVES>
+__device__ __noinline__ void scaled_rows(const QkvArgs& a, const HeadsPair& fwd, const BwdJobs& list, const unsigned long long* turns, float2* anew) {
+  constexpr int TEAM = D / 8, ROWS = kQkvThreads / TEAM;
+  const int l = threadIdx.x % TEAM, slot = threadIdx.x / TEAM;
+  const int side = (int)blockIdx.x < list.ctas[0] ? 0 : 1, first = (int)blockIdx.x - (side > 0 ? list.ctas[0] : 0);
+  const HeadsArg g = a.x[side], y = a.y[side], x = fwd.v[side];
+  float2 w[4], dw[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    dw[i] = make_float2(0.f, 0.f);
+    w[i] = a.w[side] != nullptr ? make_float2(a.w[side][l * 8 + 2 * i], a.w[side][l * 8 + 2 * i + 1]) : make_float2(1.f, 1.f);
+  }
+#pragma unroll 1
+  for (int job = first; job < list.jobs[side]; job += list.ctas[side]) {
+    const int group = divided(job, a.by_jobs), lo = group * list.per[side], hi = min(lo + list.per[side], g.heads);
+    const int at = job - group * a.jobs, b = divided(at, a.by_tiles), row = (at - b * a.tiles) * ROWS + slot, tok = min(row, a.tokens - 1);
+    const bool valid = row < a.tokens;
+    const TG* gp = reinterpret_cast<const TG*>(g.p) + b * g.sb + tok * g.st + l * 8;
+    const TI* xp = reinterpret_cast<const TI*>(x.p) + b * x.sb + tok * x.st + l * 8;
+    TO* yp = reinterpret_cast<TO*>(y.p) + b * y.sb + tok * y.st + l * 8;
+    Turn<D, HALVES> turn;
+    turn.init(a.turn, turns, b, tok, l);
+#pragma unroll 1
+    for (int h = lo; h < hi; ++h) {
+      Raw8<TG> gr;
+      Raw8<TI> xr;
+      gr.load(gp + h * g.sh);
+      xr.load(xp + h * x.sh);
+      float f[8], xf[8];
+      gr.get(f);
+      xr.get(xf);
+      turn.apply(f);
+      float2 sums = row_sums<TEAM>(xf, f, w);
+      float t = __fmaf_rn(sums.x, 1.f / D, a.eps);
+      const bool plain = plain_row(t);
+      const float scale = row_scale<TEAM>(xf, a.eps), s = plain ? 1.f : scale;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) xf[i] *= s;
+      const float2 scaled = row_sums<TEAM>(xf, f, w);
+      if (!plain) {
+        sums = scaled;
+        t = sums.x * (1.f / D) + a.eps * s * s;
+      }
+      const float r = rsqrtf(t);
+      dx_row(f, xf, w, dw, r, sums.y * (-1.f / D) * r * r * r, valid);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] *= s;
+      if (valid && !plain) store8(yp + h * y.sh, f);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) anew[i] = dw[i];
+}
+
 // x = the forward's rows of q and k, dy -> dx.  A job is a tile of tokens and a group of heads.  The first CTAs take q's jobs, the others k's, so that a thread sums the
 // gradient of one weight; then all take v's.
-struct BwdJobs { int ctas[2], jobs[2], per[2]; };      // of q, of k: CTAs, jobs, heads in a group
 template <int D, typename TI, typename TG, typename TO, bool HALVES>
 __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(const __grid_constant__ QkvArgs a, const __grid_constant__ HeadsPair fwd,
                                                                         const __grid_constant__ BwdJobs list, float* __restrict__ partial) {
@@ -260,6 +417,7 @@ __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(co
     const HeadsArg g = a.x[side], y = a.y[side], x = fwd.v[side];
     const bool norm = a.norm;
     float2 w[4], dw[4];
+    uint32_t farthest = 0u;      // of the rows' mean squares
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       dw[i] = make_float2(0.f, 0.f);
@@ -315,28 +473,11 @@ __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(co
           xr.load(from + GV * kQkvThreads, kQkvThreads);
           float xf[8];
           xr.get(xf);
-          // (two channels an instruction: 16 warps' issue slots are the next bound behind memory)
-          float2 ss = make_float2(0.f, 0.f), dot = ss;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 x2 = make_float2(xf[2 * i], xf[2 * i + 1]), f2 = make_float2(f[2 * i], f[2 * i + 1]);
-            ss = __ffma2_rn(x2, x2, ss);
-            dot = __ffma2_rn(__fmul2_rn(f2, w[i]), x2, dot);
-          }
-          float2 sums = make_float2(ss.x + ss.y, dot.x + dot.y);
-#pragma unroll
-          for (int o = TEAM / 2; o > 0; o >>= 1)
-            sums = __fadd2_rn(sums, make_float2(__shfl_xor_sync(0xffffffffu, sums.x, o), __shfl_xor_sync(0xffffffffu, sums.y, o)));
-          const float r = rsqrtf(sums.x * (1.f / D) + a.eps), m = sums.y * (-1.f / D) * r * r * r;
-          const float2 r2 = make_float2(r, r), m2 = make_float2(m, m);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 x2 = make_float2(xf[2 * i], xf[2 * i + 1]), fr = __fmul2_rn(make_float2(f[2 * i], f[2 * i + 1]), r2);
-            if (at.valid) dw[i] = __ffma2_rn(fr, x2, dw[i]);
-            const float2 o = __ffma2_rn(x2, m2, __fmul2_rn(fr, w[i]));
-            f[2 * i] = o.x;
-            f[2 * i + 1] = o.y;
-          }
+          const float2 sums = row_sums<TEAM>(xf, f, w);
+          const float t = __fmaf_rn(sums.x, 1.f / D, a.eps);
+          farthest = max(farthest, beyond_least(t));
+          const float r = rsqrt_plain(t), m = sums.y * (-1.f / D) * r * r * r;
+          dx_row(f, xf, w, dw, r, m, at.valid);
         }
         if (at.valid) store8(yp, f);
         ask(s == 0 ? AHEAD - 1 : s - 1);      // (the place that was read last time)
@@ -345,6 +486,12 @@ __global__ void __launch_bounds__(kQkvThreads, HALVES ? 3 : 4) qkv_bwd_kernel(co
     }
     if (norm) {
       asm volatile("cp.async.wait_all;" ::: "memory");
+      if (__any_sync(0xffffffffu, farthest > beyond_least(kPlainMost))) {
+        float2 anew[4];
+        scaled_rows<D, TI, TG, TO, HALVES>(a, fwd, list, turns, anew);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dw[i] = anew[i];
+      }
       __syncthreads();
       float2* red = reinterpret_cast<float2*>(qkv_smem);      // [ROWS][D / 2]
 #pragma unroll
