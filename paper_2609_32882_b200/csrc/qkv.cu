@@ -4,9 +4,10 @@
 //   backward: g = R(position)^-1 dy;  dw = sum g x r;  dx = r (w g) - x r^3 mean((w g) x)
 // R turns pair p of a head's channels by (position on the pair's axis) * (its frequency); the inverse turns back, and is R's gradient too.
 //
-// Angles.  A frequency is held as a fraction of a turn in 64 bits (2^-64 turns per position).  The product with an integer position,
-// modulo 2^64, is the angle modulo a turn without any rounding, however far the position; its upper half, 2^-32 turns, goes to sincospi.
-// (In fp32, position * frequency alone is 2^-24 of the angle off: 4e-3 at position 65,536.)
+// Angles.  A frequency is held as a fraction of a turn in 64 bits (2^-64 turns per position).  The product with an integer position, modulo 2^64, is the angle modulo a turn: the
+// product itself is exact however far the position, so what is off is the frequency's own rounding times the position (2^-33 turns at 2^31) and what goes to sincospi, the upper half
+// (2^-32 turns) rounded to fp32's 24 bits: 2^-26 turns at most (9.4e-8 rad, near half a turn), as an fp32 angle of that size is.  (In fp32, position * frequency alone is 2^-24 of the
+// angle off: 4e-3 at position 65,536.)
 //
 // All of it is bound by memory: every element is read once and written once, the few operations hide behind that.  A team of D / 8
 // threads holds one row of one head, 8 channels a thread; it keeps its token and walks through the heads, so that a token's sines and
