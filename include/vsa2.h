@@ -408,7 +408,9 @@ int vsa2_fp8_quantize(const void* x, int32_t x_dtype, int32_t rows, int32_t cols
  * elements.  The tile shapes suit B as the operand with many rows (a projection's weights [out, in]) and any m from 1.
  *   workspace: device, 256-byte aligned, at least vsa2_fp8_matmul_workspace_bytes(m, n, k); one may serve all calls with an m, n and k of at most
  *   those that follow one another on a stream.  Its first word is the status of vsa2_device_status (the caller zeroes the first 256 bytes once); the rest need not be set.
- * Results do not depend on timing: the parts of a sum are added in a fixed order. */
+ * Results do not depend on timing: the parts of a sum are added in a fixed order.  They do depend, in the last bits, on m, n and k (unlike the gate and the coarse branch): these
+ * choose the tiles and the ranges of K, so a row of A alone and among others need not give the same bits.  An accumulator sums up to 5120 values of K of an fp32 result, all of a range
+ * of a bf16 one, and cuts what does not fit instead of rounding it (2^-23 of its magnitude at most for each 32 values). */
 size_t vsa2_fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
 int vsa2_fp8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_fp8* a, const vsa2_fp8* b, void* c, int32_t c_dtype, int64_t ldc,
                     void* workspace, size_t workspace_bytes, void* cuda_stream);
