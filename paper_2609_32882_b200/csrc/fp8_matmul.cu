@@ -32,8 +32,8 @@ constexpr int kMmStagesMost = 12;
 constexpr int kMmScaleSlots = 4;
 constexpr int kMmSplits = 16;           // most ranges that K is cut into
 // Blocks of K that an accumulator sums for an fp32 result; the epilogue adds the pieces.  (The tensor cores cut what does not fit an accumulator instead of rounding
-// it: with 24,000 values of K in one the result was 1.7e-6 off.  2304 x 1536 x 32760, where fp32 torch is 3.0e-7 off: pieces of 32 blocks 2.2e-7 and 124.8 us, of 40 2.7e-7 and
-// 121.9, of 48 3.3e-7 and 120.8, of 64 4.8e-7 and 117.4.)
+// it: with 24,000 values of K in one the result was 1.7e-6 off.  2304 x 1536 x 32760, where fp32 torch is 3.0e-7 off: pieces of 16 blocks 1.3e-7 and 109.2 us, of 32 2.2e-7 and
+// 108.5, of 40 2.7e-7 and 108.3, of 64 4.8e-7.)
 constexpr int kMmChunk = 40;
 constexpr uint32_t kMmPBytes = 128 * 128;
 constexpr uint32_t kMmTileBytes = 32 * 128 * 2;      // 32 rows of C x 128 elements of bf16
@@ -59,6 +59,7 @@ struct MmArgs {
   int splits, chunk;                 // ranges that K is cut into; most blocks of K in one accumulator
   Divisor by_tiles, by_group, by_gq, by_rest, by_splits;      // pt qt; gq pt; gq, and what the last group has of tiles along Q
   int tensor_stores;                 // C lies as tensor copies need it
+  int in_pieces;                     // some range has more blocks than one accumulator sums
   const uint32_t* p_scales;
   const uint32_t* q_scales;
   void* c;
@@ -208,13 +209,15 @@ __device__ __forceinline__ void mm_dealloc(uint32_t base) {
   if constexpr (PAIR == 1) tc::tmem_dealloc(base, 512);
   else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(base) : "memory");
 }
-// 32 lanes x 32 columns of an accumulator
-__device__ __forceinline__ void load_columns(uint32_t taddr, float (&v)[32]) {
-  uint32_t r[32];
-  tc::tmem_ld32(taddr, r);
+// 32 lanes x 32 columns, or 16, of an accumulator
+template <int N>
+__device__ __forceinline__ void load_columns(uint32_t taddr, float (&v)[N]) {
+  uint32_t r[N];
+  if constexpr (N == 32) tc::tmem_ld32(taddr, r);
+  else tc::tmem_ld16(taddr, r);
   tc::tmem_ld_wait();
 #pragma unroll
-  for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(r[c]);
+  for (int c = 0; c < N; ++c) v[c] = __uint_as_float(r[c]);
 }
 // e4m3 x e4m3, ue8m0 scales, both operands K-major, 128 rows a CTA; `sf`: which byte of the scales' words
 template <int NT, int PAIR>
@@ -222,31 +225,27 @@ __device__ __forceinline__ constexpr uint32_t idesc_scaled(uint32_t sf) {
   return (sf << 4) | ((uint32_t)(NT >> 3) << 17) | (1u << 23) | ((uint32_t)PAIR << 27) | (sf << 29);
 }
 
-// 32 columns of an accumulator's row, straight code where all of them exist: with a test for each element the loads and stores came one at a time, and
+// Columns of an accumulator's row, straight code where all of them exist: with a test for each element the loads and stores came one at a time, and
 // the epilogue took longer than the products of 40 blocks.
 __device__ __forceinline__ void put(float* to, float v) { *to = v; }
 __device__ __forceinline__ void put(bf16* to, float v) { *to = __float2bfloat16_rn(v); }
 // elements `stride` apart (a warp's 32 rows lie next to one another in C)
-template <typename TO>
-__device__ __forceinline__ void put_column(TO* to, long long stride, int count, const float (&v)[32]) {
-  if (count >= 32) {
+template <typename TO, int N>
+__device__ __forceinline__ void put_columns(TO* to, long long stride, int count, const float (&v)[N]) {
+  const bool all = count >= N;
 #pragma unroll
-    for (int c = 0; c < 32; ++c, to += stride) put(to, v[c]);
-  } else {
+  for (int c0 = 0; c0 < N; c0 += 8) {
+    asm volatile("" : "+l"(to));      // (eight addresses at a time: all of them at once are more registers than there are)
+    if (all) {
 #pragma unroll
-    for (int c = 0; c < 32; ++c, to += stride)
-      if (c < count) put(to, v[c]);
+      for (int c = 0; c < 8; ++c) put(to + c * stride, v[c0 + c]);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (c0 + c < count) put(to + c * stride, v[c0 + c]);
+    }
+    to += 8 * stride;
   }
-}
-__device__ __forceinline__ void add_column(const float* from, long long stride, int count, float (&v)[32]) {
-  float old[32];
-#pragma unroll
-  for (int c = 0; c < 32; ++c) {
-    old[c] = __ldcg(from);
-    if (c + 1 < count) from += stride;
-  }
-#pragma unroll
-  for (int c = 0; c < 32; ++c) v[c] += old[c];
 }
 
 // bf16: 32 rows x 32 columns of an accumulator (lanes and columns of `taddr`) as the fragments that stmatrix turns: four 8 x 8 blocks for each 8 columns
@@ -448,6 +447,44 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
           there[d] = next(v[d]);
         }
       }
+    } else if (sizeof(TO) == 4 && warp >= 4 && a.in_pieces) {
+      // ---------------------------------------------------------------- epilogue of fp32 results in pieces: two groups of four warps, each half of the columns.  A thread keeps the
+      // sums of its row's columns over the pieces in registers.  (Added up in C, through L2, they took a share of the products' intake: 2304 x 1536 x 32760 119.4 us in pieces of 40
+      // blocks, 108.3 so.  It is long code, which a product of a single piece would have to fetch: 300 x 500 x 4000 8.8 us instead of 8.5)
+      const int quad = warp & 3, group = (warp >> 2) - 1;
+      constexpr int MINE = NT > 32 ? NT / 2 : NT, STEP = MINE % 32 == 0 ? 32 : 16;      // columns at a time
+      if (group * MINE >= NT) goto done;
+      float sum[MINE];
+#pragma unroll
+      for (int c = 0; c < MINE; ++c) sum[c] = 0.f;
+      for (uint32_t seg = 0; w.advance(a); ++seg) {
+        const uint32_t buf = seg & 1;
+        VSA2_WAIT_PARKED(&misc->d_full[buf], (seg >> 1) & 1);
+        tc::tc_fence_after();
+        const uint32_t tmem = tmem_base + buf * 256 + group * MINE + ((uint32_t)(quad * 32) << 16);
+        const int row = (w.p * PAIR + rank) * 128 + quad * 32 + lane, col = w.q * NT + group * MINE;
+        const bool last = w.kb1 == w.r1;
+        const int cols = row < a.p_rows ? a.q_rows - col : 0;      // columns that exist (or more)
+        float* to = reinterpret_cast<float*>(a.c) + w.split * a.split_stride + (long long)col * a.ldc + row;
+#pragma unroll
+        for (int c0 = 0; c0 < MINE; c0 += STEP) {
+          float v[STEP];
+          load_columns(tmem + c0, v);
+#pragma unroll
+          for (int c = 0; c < STEP; ++c) {
+            v[c] += sum[c0 + c];
+            sum[c0 + c] = last ? 0.f : v[c];
+          }
+          if (last) {
+            put_columns(to, a.ldc, cols - c0, v);
+            to += STEP * a.ldc;
+            __syncwarp();
+          }
+        }
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&misc->d_empty[buf]);
+      }
     } else if (warp >= 4) {
       // ---------------------------------------------------------------- epilogue: two groups of four warps, each half of the columns
       const int quad = warp & 3, group = (warp >> 2) - 1;
@@ -502,12 +539,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constan
           for (int c0 = 0; c0 < cols; c0 += 32) {
             float v[32];
             load_columns(tmem + c0, v);
-            if (row < a.p_rows) {
-              TO* to = out + (long long)c0 * a.ldc;
-              if constexpr (sizeof(TO) == 4)      // (what this thread has written there for the blocks before)
-                if (w.kb0 > w.r0) add_column(to, a.ldc, cols - c0, v);
-              put_column(to, a.ldc, cols - c0, v);
-            }
+            if (row < a.p_rows) put_columns(out + (long long)c0 * a.ldc, a.ldc, cols - c0, v);
           }
           release();
         }
@@ -649,6 +681,7 @@ cudaError_t launch_tiles(const MmCall& c, const MmPlan& plan, void* result, long
   a.by_rest = divisor(a.qt % a.gq > 0 ? a.qt % a.gq : a.gq);
   a.by_splits = divisor(a.splits);
   a.chunk = c.f32 ? kMmChunk : c.kb;
+  a.in_pieces = (a.kb + a.splits - 1) / a.splits > a.chunk;
   a.tensor_stores = sizeof(TO) == 2 && c.tensor_stores;
   a.p_scales = reinterpret_cast<const uint32_t*>(p.scales);
   a.q_scales = reinterpret_cast<const uint32_t*>(q.scales);
