@@ -9,8 +9,8 @@
 // for 2 x 128 x 224 x 128 multiply-adds, where a CTA alone fetches 45.  Persistent CTAs, one per SM: a producer warp (TMA), an issuer, a warp for the scales, two
 // groups of four, half the columns each, for the epilogue; two accumulators in tensor memory, so that a tile's epilogue runs behind the next tile's products.
 //
-// What bounds it: in long runs the power limit, at which values of normal numbers draw a quarter more than small whole ones (75600 x 15360 x 5120: 4.6 - 4.8 ms, 2.5
-// PFLOP/s, against 3.7 ms and 3.2 PFLOP/s, twice the library's bf16 product); else the intake from L2 (8192 x 4096 x 4096 90 us: 51 bytes a cycle and SM, 600
+// What bounds it: in long runs the power limit, at which values of normal numbers draw a quarter more than small whole ones (75600 x 15360 x 5120: 4.5 - 5.0 ms from box to box,
+// 2.4 - 2.6 PFLOP/s, against 3.7 ms and 3.2 PFLOP/s, twice the library's bf16 product); else the intake from L2 (8192 x 4096 x 4096 90 us: 51 bytes a cycle and SM, 600
 // cycles a block where the tensor cores need 448).  Tiles of 448 columns, both accumulators in one tile, need 27 % less intake and were as fast at large sizes (20000 x 15360 x
 // 5120 1028 us both ways), slower where rounds are few (4096^3 60 us instead of 52).  One row of A: the weights' bytes (15360 x 5120 16 us, 4.9 TB/s with the
 // launch); few tiles and short K: the launch, the first block's way from memory and the epilogue, 3 - 5 us.
@@ -230,21 +230,21 @@ __device__ __forceinline__ constexpr uint32_t idesc_scaled(uint32_t sf) {
 __device__ __forceinline__ void put(float* to, float v) { *to = v; }
 __device__ __forceinline__ void put(bf16* to, float v) { *to = __float2bfloat16_rn(v); }
 // elements `stride` apart (a warp's 32 rows lie next to one another in C)
+// (in the pieces' epilogue eight addresses at a time: all of them at once are more registers than there are)
 template <typename TO, int N>
 __device__ __forceinline__ void put_columns(TO* to, long long stride, int count, const float (&v)[N]) {
-  const bool all = count >= N;
+  constexpr int AT = N < 32 ? 8 : N;
 #pragma unroll
-  for (int c0 = 0; c0 < N; c0 += 8) {
-    asm volatile("" : "+l"(to));      // (eight addresses at a time: all of them at once are more registers than there are)
-    if (all) {
+  for (int c0 = 0; c0 < N; c0 += AT) {
+    if (AT < N) asm volatile("" : "+l"(to));
+    if (count >= N) {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) put(to + c * stride, v[c0 + c]);
+      for (int c = 0; c < AT; ++c, to += stride) put(to, v[c0 + c]);
     } else {
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
-        if (c0 + c < count) put(to + c * stride, v[c0 + c]);
+      for (int c = 0; c < AT; ++c, to += stride)
+        if (c0 + c < count) put(to, v[c0 + c]);
     }
-    to += 8 * stride;
   }
 }
 
