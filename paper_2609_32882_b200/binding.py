@@ -278,13 +278,13 @@ def vsa2_gate_bwd(p, hidden, x, w_g, gate, dgate, d_w_g, dx, workspace, stream=N
 
 def vsa2_gate_bwd_add(p, hidden, x, w_g, gate, dgate, d_w_g, dx, workspace, stream=None):
     """vsa2_gate_bwd with its dx added to what `dx` holds: [B, L or more rows, hidden], contiguous but for its batch entries' distance; rows from L on stay."""
-    sizes = vsa2_query_sizes(p)
-    dtype = {BF16: "torch.bfloat16", F32: "torch.float32"}[p.out_dtype]
-    rows_ok = dx.dim() == 3 and dx.shape[0] == p.batch and dx.shape[1] >= sizes.seq_len and dx.shape[2] == hidden
-    if not rows_ok or not dx.is_cuda or str(dx.dtype) != dtype or not dx[0].is_contiguous():
-        raise ValueError(f"expected dx as a CUDA tensor [{p.batch}, {sizes.seq_len} or more, {hidden}] in {dtype} with contiguous batch entries")
+    import torch
+    video, dtype, shape, strides = p.grid_t * p.grid_h * p.grid_w, torch.float32 if p.out_dtype == F32 else torch.bfloat16, dx.shape, dx.stride()
+    if not (len(shape) == 3 and shape[0] == p.batch and shape[1] >= video and shape[2] == hidden and (shape[1] == 1 or strides[1] == hidden) and strides[2] == 1 and
+            dx.is_cuda and dx.dtype == dtype):
+        raise ValueError(f"expected dx as a CUDA tensor [{p.batch}, {video} or more, {hidden}] in {dtype} with contiguous batch entries")
     nbytes = workspace.numel() * workspace.element_size()
-    _check(_lib().vsa2_gate_bwd_add(C.byref(p), hidden, _ptr(x), _ptr(w_g), _ptr(gate), _ptr(dgate), _ptr(d_w_g), dx.data_ptr(), dx.stride(0), _ptr(workspace),
+    _check(_lib().vsa2_gate_bwd_add(C.byref(p), hidden, _ptr(x), _ptr(w_g), _ptr(gate), _ptr(dgate), _ptr(d_w_g), dx.data_ptr(), strides[0], _ptr(workspace),
                                     nbytes, _stream(stream)), "vsa2_gate_bwd_add")
 
 

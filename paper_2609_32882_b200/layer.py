@@ -37,7 +37,7 @@ class Vsa2Layer:
         self.ws_qkv = torch.empty(vb.vsa2_qkv_bwd_workspace_bytes(p.head_dim), dtype=torch.uint8, device=device)
         self.ws_gate = torch.empty(max(256, vb.vsa2_gate_bwd_workspace_bytes(p, hidden)), dtype=torch.uint8, device=device)
         self.w_g = self.q_weight = self.k_weight = None
-        self.saved, self.kept, self.updates = None, {}, 0
+        self.saved, self.kept, self.updates = None, (), 0
 
     def _expect(self, t, what, shape, dtype):
         """The attention and the gate get plain addresses; sizes and types are the layer's."""
@@ -84,9 +84,8 @@ class Vsa2Layer:
         return o
 
     def _versions(self, x, o):
-        """What backward needs unchanged, as it is now: torch's counters of changes in place, and the number of updates."""
-        tensors = {"x": x, "o": o, "w_g": self.w_g, "q_weight": self.q_weight, "k_weight": self.k_weight}
-        return {"the weights (set_weights)": self.updates, **{k: None if t is None or t.is_inference() else t._version for k, t in tensors.items()}}
+        """What backward needs unchanged, as it is now: the number of updates, and torch's counters of changes in place."""
+        return (self.updates, *(None if t is None or t.is_inference() else t._version for t in (x, o, self.w_g, self.q_weight, self.k_weight)))
 
     def backward(self, d_o):
         """d_o [B, Hq, L + Lt, D] bf16 -> dict of dx [B, L + Lt, C] bf16 and, in fp32, dw_qkv, dw_g, dq_weight, dk_weight."""
@@ -94,9 +93,10 @@ class Vsa2Layer:
         if self.saved is None:
             raise RuntimeError("backward without a forward before it")
         x, video, packed, q, k, v, gate, o, lse = self.saved
-        changed = [name for name, version in self._versions(x, o).items() if version != self.kept[name]]
-        if changed:
-            raise RuntimeError(f"changed between forward and backward: {', '.join(changed)}")
+        now = self._versions(x, o)
+        if now != self.kept:
+            names = ("the weights (set_weights)", "x", "o", "w_g", "q_weight", "k_weight")
+            raise RuntimeError(f"changed between forward and backward: {', '.join(n for n, a, b in zip(names, now, self.kept) if a != b)}")
         self._expect(d_o, "the output's gradient", tuple(o.shape), torch.bfloat16)
         dq, dk, dv, dgate = self.attn.backward(q, k, v, gate, o, lse, d_o)
         d_packed = torch.empty_like(packed)
