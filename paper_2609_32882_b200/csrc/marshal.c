@@ -100,9 +100,10 @@ static int get_view(PyObject* t, vsa2_heads* v) {
   v->reserved = 0;
   return 0;
 }
-/* the first n members of a sequence; a None among them is a view without heads */
-static int get_views(PyObject* sequence, vsa2_heads* v, int n) {
-  int like = -1, result = -1;
+/* the first n members of a sequence; a None among them is a view without heads, of the others' shape (of `otherwise`'s where all are None; may be null) */
+static int get_views(PyObject* sequence, vsa2_heads* v, int n, const vsa2_heads* otherwise) {
+  int given = 0, result = -1;
+  vsa2_heads like;
   PyObject* fast = PySequence_Fast(sequence, "a sequence of tensors is expected");
   if (fast == NULL) return -1;
   if (PySequence_Fast_GET_SIZE(fast) < n) {
@@ -113,16 +114,20 @@ static int get_views(PyObject* sequence, vsa2_heads* v, int n) {
     PyObject* t = PySequence_Fast_GET_ITEM(fast, i);
     if (t == Py_None) continue;
     if (get_view(t, &v[i])) goto out;
-    if (like < 0) like = i;
+    if (!given) like = v[i];
+    given = 1;
   }
-  if (like < 0) {
-    refuse("no tensor is given");
-    goto out;
+  if (!given) {
+    if (otherwise == NULL) {
+      refuse("no tensor is given");
+      goto out;
+    }
+    like = *otherwise;
   }
   for (int i = 0; i < n; ++i) {
     if (PySequence_Fast_GET_ITEM(fast, i) != Py_None) continue;
     memset(&v[i], 0, sizeof v[i]);
-    v[i].batch = v[like].batch; v[i].tokens = v[like].tokens; v[i].channels = v[like].channels; v[i].dtype = v[like].dtype;
+    v[i].batch = like.batch; v[i].tokens = like.tokens; v[i].channels = like.channels; v[i].dtype = like.dtype;
   }
   result = 0;
 out:
@@ -302,7 +307,7 @@ static PyObject* qkv_fwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   vsa2_qk_norm norm;
   const vsa2_qk_norm* with;
   void* stream;
-  if (arguments(n, 11) || get_rope(a[0], &store, &rope) || get_views(a[1], x, 3) || get_views(a[2], y, 3) ||
+  if (arguments(n, 11) || get_rope(a[0], &store, &rope) || get_views(a[1], x, 3, NULL) || get_views(a[2], y, 3, NULL) ||
       get_norm(a[6], a[5], a[3], a[4], x[0].channels, &norm, &with) || get_place(a[7], a[8], a[9], &x[0], &place) || get_stream(a[10], &stream))
     return NULL;
   CALLED(f_qkv_fwd(rope, &place, with, x, y, stream));
@@ -317,8 +322,8 @@ static PyObject* qkv_bwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   const vsa2_qk_norm* with;
   void *stream, *dq, *dk, *workspace;
   size_t bytes;
-  if (arguments(n, 15) || get_rope(a[0], &store, &rope) || get_views(a[2], dy, 3) || get_views(a[3], dx, 3) ||
-      get_norm(a[10], a[9], a[4], a[5], dy[0].channels, &norm, &with) || (with != NULL && get_views(a[1], x, 2)) ||
+  if (arguments(n, 15) || get_rope(a[0], &store, &rope) || get_views(a[2], dy, 3, NULL) || get_views(a[3], dx, 3, NULL) ||
+      get_norm(a[10], a[9], a[4], a[5], dy[0].channels, &norm, &with) || (with != NULL && get_views(a[1], x, 2, &dy[0])) ||
       get_weight(a[6], dy[0].channels, &dq) || get_weight(a[7], dy[0].channels, &dk) || get_memory(a[8], &workspace, &bytes) ||
       get_place(a[11], a[12], a[13], &dy[0], &place) || get_stream(a[14], &stream))
     return NULL;
