@@ -417,7 +417,7 @@ class Fp8:
         """The matrix in fp32 (torch operations: for inspection and tests)."""
         import torch
         rows, cols = self.values.shape
-        e = self.scales.transpose(0, 1).reshape(rows, -1).to(torch.int32) - 127
+        e = self.scales.transpose(0, 1).reshape(rows, 4 * self.scales.shape[0]).to(torch.int32) - 127
         return self.values.float() * torch.ldexp(torch.ones(e.shape, device=e.device), e).repeat_interleave(128, dim=1)[:, :cols]
 
 

@@ -51,3 +51,12 @@ def test_changed_members_are_refused(change, monkeypatch):
         assert len(called) == 2
     finally:
         m.bind(types, real, vb._stream)
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 8), (8, 0), (0, 0), (1, 1), (3, 600)])
+def test_dequantized_shapes(rows, cols):
+    f = vb.Fp8.empty(rows, cols, device="cpu")
+    f.values.copy_(torch.full((rows, cols), 1.5).to(torch.float8_e4m3fn))
+    f.scales.fill_(128)
+    x = f.dequantize()
+    assert x.shape == (rows, cols) and (x == 3.0).all()
