@@ -477,7 +477,7 @@ int64_t vsa2_selftest_divmod(int32_t n_max, int32_t d_min, int32_t d_exhaustive,
 int32_t vsa2_debug_rescue_capacity(int32_t capacity);
 
 /* Host-only diagnostic (no GPU, no CUDA call): how vsa2_fp8_matmul cuts a product on a device of `sms` SMs whose context has room for pairs of CTAs (`pairs`),
- * with C's rows on 16-byte boundaries (`c_aligned`) or not.  out: columns of a tile (32, 128, 224); CTAs that share one (1, 2); 1 where A's rows are the
+ * with C's rows on 16-byte boundaries (`c_aligned`; of no use with an n that is no multiple of 8) or not.  out: columns of a tile (32, 128, 224); CTAs that share one (1, 2); 1 where A's rows are the
  * accumulators' lanes instead of B's; ranges that K is cut into; tiles along the columns' operand; of those, how many are taken together. */
 int vsa2_debug_fp8_matmul_plan(int32_t m, int32_t n, int32_t k, int32_t c_dtype, int32_t c_aligned, int32_t sms, int32_t pairs, int32_t out[6]);
 

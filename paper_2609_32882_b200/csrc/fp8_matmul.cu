@@ -58,7 +58,7 @@ struct MmArgs {
   int pt, qt, gq;                    // tiles along P, along Q; tiles along Q that are taken together
   int splits, chunk;                 // ranges that K is cut into; most blocks of K in one accumulator
   Divisor by_tiles, by_group, by_gq, by_rest, by_splits;      // pt qt; gq pt; gq, and what the last group has of tiles along Q
-  int tensor_stores;                 // C lies as tensor copies need it
+  int tensor_stores;                 // C lies as tensor copies need it, and ends where they end
   int in_pieces;                     // some range has more blocks than one accumulator sums
   const uint32_t* p_scales;
   const uint32_t* q_scales;
@@ -713,6 +713,9 @@ cudaError_t launch_mm(const MmCall& c, const MmPlan& plan) {
                : launch_kernel(fp8_sum_kernel<bf16>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, by_row, reinterpret_cast<bf16*>(c.c), c.ldc);
 }
 
+// Tensor copies write whole units of 16 bytes: with an n that is no multiple of 8 they put zeros behind C's last column (into what else lies in its rows).  Such results take plain stores.
+bool whole_units(int n) { return n % 8 == 0; }
+
 // The kernel of a call: columns of a tile, CTAs that share one, which operand's rows are its lanes.  `pairs`: takes_pairs, and the context has room for one
 struct MmChoice {
   int columns, pair;
@@ -761,7 +764,7 @@ cudaError_t launch_fp8_matmul(int m, int n, int k, const Fp8Arg& fa, const Fp8Ar
   call.fa = fa; call.fb = fb;
   call.c = c; call.ldc = ldc;
   call.f32 = c_f32 != 0;
-  call.tensor_stores = !c_f32 && (reinterpret_cast<uintptr_t>(c) & 15u) == 0 && ldc % 8 == 0;
+  call.tensor_stores = !c_f32 && (reinterpret_cast<uintptr_t>(c) & 15u) == 0 && ldc % 8 == 0 && whole_units(n);
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
   call.status = reinterpret_cast<StatusBlock*>(ws);
   call.parts = reinterpret_cast<float*>(ws + align_up(sizeof(StatusBlock), 256));
@@ -784,7 +787,7 @@ void fp8_matmul_plan(int m, int n, int k, int c_f32, bool tensor_stores, int sms
   call.kb = (k + 127) / 128;
   call.ctas = sms < kMmCtas ? sms : kMmCtas;
   call.f32 = c_f32 != 0;
-  call.tensor_stores = !c_f32 && tensor_stores;
+  call.tensor_stores = !c_f32 && tensor_stores && whole_units(n);
   const MmChoice choice = choose_mm(call, pairs && takes_pairs(call));
   out[0] = choice.columns; out[1] = choice.pair; out[2] = choice.swap;
   out[3] = choice.plan.splits; out[4] = choice.plan.qt; out[5] = tiles_together(choice.columns, call.kb, choice.plan.qt);
