@@ -415,6 +415,74 @@ size_t vsa2_fp8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
 int vsa2_fp8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_fp8* a, const vsa2_fp8* b, void* c, int32_t c_dtype, int64_t ldc,
                     void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ---- The residual stream around a layer (no counterpart in the paper) ---------------------------------------------------------
+ * A branch (attention's output projection, a feed-forward part) is added to the stream, with dropout, and the next layer's hidden states are the norm of what comes out:
+ * vsa2_residual_norm_fwd -> vsa2_fp8_matmul or vsa2_int8_matmul; backward: vsa2_residual_norm_bwd.  Each stands alone as well.
+ * Conventions as above; none of these calls allocates or synchronises, sums run in a fixed order (bitwise reproducible on a device), and sizes of zero are valid. */
+
+/* A matrix [rows, cols] of a call (host struct): contiguous rows, `ld` >= cols elements apart (of no use with one row); any alignment of its type, rows on 16-byte boundaries are
+ * faster.  An output may be an input itself (the same data, ld and dtype); otherwise outputs overlap neither inputs nor one another. */
+typedef struct vsa2_rows {
+  void* data;
+  int64_t ld;
+  int32_t dtype;                      /* VSA2_BF16 or VSA2_F32 */
+  int32_t reserved;
+} vsa2_rows;
+
+/* Dropout with probability p (host struct).  The mask is never stored: element (row, col) has 16 bits of the counter-based generator Philox 4x32-10 with the key `seed` and the
+ * counter (col / 8, row, offset) -- bits 16 (col % 2) of word (col % 8) / 2 -- and is kept, times 65536 / (65536 - t), where they are at least t = p * 65536 rounded.  Dropped elements
+ * are zero whatever they were.  The same seed and offset give the same mask at any size, stride and type. */
+typedef struct vsa2_drop {
+  const uint64_t* rng;                /* device [2] = {seed, offset}, 8-byte aligned, read when the kernel runs: a captured call draws anew when they are changed between replays, and */
+                                      /* backward needs what forward had.  May be NULL with p = 0 */
+  double p;                           /* 0 <= p < 1; at most 65535 / 65536 is applied */
+} vsa2_drop;
+
+/* 8-bit form of a matrix [rows, cols] with a scale for each row (host struct).
+ *   values  device int8, 16-byte aligned, row stride `ld` >= cols, a multiple of 16 (bytes between cols and ld are neither read nor written)
+ *   scales  device fp32 [rows]
+ * An element is value * scale. */
+typedef struct vsa2_int8 {
+  void* values;
+  float* scales;
+  int64_t ld;
+} vsa2_int8;
+
+/* h = residual + drop(x) (residual NULL: drop(x); drop NULL: no dropout), rounded to h's type, and the norm of every row of it: y = h / sqrt(mean(h^2) + eps) * weight, for rows of any
+ * finite size (their squares may lie beyond fp32's range).  weight: device fp32 [cols], NULL: ones.  eps >= 0; with 0 a row of zeros has no norm (NaN).  Outputs, each NULL where it
+ * is not wanted, one at least:
+ *   h       of the residual's type (without one of x's); the norm is that of the rounded h also where h is not stored
+ *   y       bf16 or fp32
+ *   y_fp8   as vsa2_fp8_quantize makes it of the unrounded y
+ *   y_int8  with v = h * weight in fp32, m = max(max |v| of the row, 2^-100): values v * (127 / m), each operation rounded once, to the nearest whole number (ties to even); scale m / 127
+ *           times the row's 1 / sqrt (rows whose mean square + eps is outside 2^-40 .. 2^40: of h times a power of two).  A row that holds something that is not finite: zeros with the scale NaN
+ * x and residual: bf16 or fp32, each on its own.  cols up to 2^22. */
+int vsa2_residual_norm_fwd(int32_t rows, int32_t cols, const vsa2_rows* x, const vsa2_rows* residual, const vsa2_drop* drop, const float* weight, float eps,
+                           const vsa2_rows* h, const vsa2_rows* y, const vsa2_fp8* y_fp8, const vsa2_int8* y_int8, void* cuda_stream);
+
+/* Gradients.  h: the forward's (its type the stream's), dy: of y (bf16 or fp32), dh: of h from what else reads it, of h's type (NULL: none) -> d_residual: of h, in h's type; dx: of x,
+ * d_residual through the dropout, before it is rounded (bf16 or fp32); d_weight: device fp32 [cols]; each NULL where it is not wanted, one at least.  Without a dropout, and in one type,
+ * d_residual is the branch's gradient too.  workspace: device, 256-byte aligned, at least vsa2_residual_norm_bwd_workspace_bytes (grows with each of the two; may be NULL without
+ * d_weight). */
+size_t vsa2_residual_norm_bwd_workspace_bytes(int32_t rows, int32_t cols);
+int vsa2_residual_norm_bwd(int32_t rows, int32_t cols, const vsa2_rows* h, const vsa2_rows* dy, const vsa2_rows* dh, const vsa2_drop* drop, const float* weight,
+                           float eps, const vsa2_rows* d_residual, const vsa2_rows* dx, float* d_weight, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* y = drop(x), or residual + drop(x) (of y's type; NULL: none).  Its own backward: dx = drop(dy) with the same rng and p. */
+int vsa2_dropout(int32_t rows, int32_t cols, const vsa2_rows* x, const vsa2_rows* residual, const vsa2_drop* drop, const vsa2_rows* y, void* cuda_stream);
+
+/* x [rows, cols] (bf16 or fp32) -> its 8-bit form with a scale for each row, as y_int8 above with v = x: m / 127 is the scale.  cols up to 2^22. */
+int vsa2_int8_quantize(int32_t rows, int32_t cols, const vsa2_rows* x, const vsa2_int8* out, void* cuda_stream);
+
+/* C [m, n] = A B^T with A [m, k] and B [n, k] in int8 form: C[i, j] = a.scales[i] * b.scales[j] * sum + bias[j].  The sum is exact (32-bit whole numbers: k is at most 131071) and so
+ * depends on nothing but the values; the scales multiply it in fp32 (a's, then b's), C is bf16 or fp32 with row stride ldc elements.  bias: device fp32 [n], NULL: none.  The tile shapes suit B as the
+ * operand with many rows (a projection's weights [out, in]) and any m from 1.
+ *   workspace: device, 256-byte aligned, at least vsa2_int8_matmul_workspace_bytes(m, n, k); one may serve all calls with an m, n and k of at most those that follow one another on a
+ *   stream.  Its first word is the status of vsa2_device_status (the caller zeroes the first 256 bytes once); the rest need not be set. */
+size_t vsa2_int8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
+int vsa2_int8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_int8* a, const vsa2_int8* b, const float* bias, void* c, int32_t c_dtype, int64_t ldc,
+                     void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Synchronises `cuda_stream`, reads the status word at the start of `workspace` and stores it in
  * *status_out (host): VSA2_OK, VSA2_ERR_DEVICE_TIMEOUT or VSA2_ERR_MAP_OVERFLOW. */
 int vsa2_device_status(const void* workspace, void* cuda_stream, int32_t* status_out);

@@ -38,7 +38,9 @@ EXPORTS = ("vsa2_query_sizes", "vsa2_route", "vsa2_route_scores", "vsa2_attn_fwd
            "vsa2_route_scratch", "vsa2_route_scratch_bytes", "vsa2_permute_cube_major",
            "vsa2_selftest_timeout", "vsa2_debug_rescue_capacity", "vsa2_selftest_divmod",
            "vsa2_rope_plan", "vsa2_rope_apply", "vsa2_qkv_fwd", "vsa2_qkv_bwd", "vsa2_qkv_bwd_workspace_bytes",
-           "vsa2_fp8_quantize", "vsa2_fp8_matmul", "vsa2_fp8_matmul_workspace_bytes", "vsa2_debug_fp8_matmul_plan")
+           "vsa2_fp8_quantize", "vsa2_fp8_matmul", "vsa2_fp8_matmul_workspace_bytes", "vsa2_debug_fp8_matmul_plan",
+           "vsa2_residual_norm_fwd", "vsa2_residual_norm_bwd", "vsa2_residual_norm_bwd_workspace_bytes", "vsa2_dropout",
+           "vsa2_int8_quantize", "vsa2_int8_matmul", "vsa2_int8_matmul_workspace_bytes")
 
 KERNELS = ("pool", "router_lse", "router_pool", "select", "coarse_fwd", "fine_fwd", "bwd_pre", "coarse_bwd",
            "fine_bwd_dq", "fine_bwd_dkv", "pool_router")
@@ -107,6 +109,18 @@ class Fp8Matrix(C.Structure):
     _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_int64)]
 
 
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class Drop(C.Structure):
+    _fields_ = [("rng", C.c_void_p), ("p", C.c_double)]
+
+
+class Int8Matrix(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_int64)]
+
+
 _LIB = None
 
 
@@ -160,10 +174,19 @@ def _lib():
         lib.vsa2_fp8_matmul.argtypes = [C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, C.c_int32, C.c_int64, vp, sz, vp]
         lib.vsa2_fp8_matmul_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
         lib.vsa2_debug_fp8_matmul_plan.argtypes = [C.c_int32] * 7 + [vp]
-        for fn in (lib.vsa2_qkv_bwd_workspace_bytes, lib.vsa2_fp8_matmul_workspace_bytes):
+        lib.vsa2_residual_norm_fwd.argtypes = [C.c_int32] * 2 + [vp] * 4 + [C.c_float] + [vp] * 5
+        lib.vsa2_residual_norm_bwd.argtypes = [C.c_int32] * 2 + [vp] * 5 + [C.c_float] + [vp] * 4 + [sz, vp]
+        lib.vsa2_residual_norm_bwd_workspace_bytes.argtypes = [C.c_int32] * 2
+        lib.vsa2_dropout.argtypes = [C.c_int32] * 2 + [vp] * 5
+        lib.vsa2_int8_quantize.argtypes = [C.c_int32] * 2 + [vp] * 3
+        lib.vsa2_int8_matmul.argtypes = [C.c_int32] * 3 + [vp] * 4 + [C.c_int32, C.c_int64, vp, sz, vp]
+        lib.vsa2_int8_matmul_workspace_bytes.argtypes = [C.c_int32] * 3
+        for fn in (lib.vsa2_qkv_bwd_workspace_bytes, lib.vsa2_fp8_matmul_workspace_bytes, lib.vsa2_residual_norm_bwd_workspace_bytes,
+                   lib.vsa2_int8_matmul_workspace_bytes):
             fn.restype = C.c_size_t
         for name in EXPORTS:
-            if name not in ("vsa2_qkv_bwd_workspace_bytes", "vsa2_fp8_matmul_workspace_bytes",
+            if name not in ("vsa2_qkv_bwd_workspace_bytes", "vsa2_fp8_matmul_workspace_bytes", "vsa2_residual_norm_bwd_workspace_bytes",
+                            "vsa2_int8_matmul_workspace_bytes",
                             "vsa2_strerror", "vsa2_route_scores", "vsa2_launch_count", "vsa2_last_cuda_error", "vsa2_selftest_divmod",
                             "vsa2_gate_bwd_workspace_bytes", "vsa2_attn_bwd_preferred_workspace_bytes",
                             "vsa2_attn_bwd_scratch_bytes", "vsa2_route_scratch_bytes"):
@@ -357,9 +380,11 @@ def _marshal():
         module = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_marshal", MARSHAL_PATH, loader=loader))
         loader.exec_module(module)
         lib = _lib()
+        at = lambda *functions: tuple(C.cast(f, C.c_void_p).value for f in functions)
         module.bind((torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn, torch.uint8),
-                    tuple(C.cast(f, C.c_void_p).value for f in (lib.vsa2_rope_apply, lib.vsa2_qkv_fwd, lib.vsa2_qkv_bwd, lib.vsa2_fp8_quantize,
-                                                                lib.vsa2_fp8_matmul)), _stream)
+                    at(lib.vsa2_rope_apply, lib.vsa2_qkv_fwd, lib.vsa2_qkv_bwd, lib.vsa2_fp8_quantize, lib.vsa2_fp8_matmul), _stream)
+        module.bind_rows((torch.int8, torch.int64), at(lib.vsa2_residual_norm_fwd, lib.vsa2_residual_norm_bwd, lib.vsa2_dropout, lib.vsa2_int8_quantize,
+                                                       lib.vsa2_int8_matmul), getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device)
         _MARSHAL = module
     return _MARSHAL
 
@@ -453,6 +478,87 @@ def vsa2_debug_fp8_matmul_plan(m, n, k, c_dtype=BF16, c_aligned=True, sms=148, p
     out = (C.c_int32 * 6)()
     _check(_lib().vsa2_debug_fp8_matmul_plan(m, n, k, c_dtype, c_aligned, sms, pairs, out), "vsa2_debug_fp8_matmul_plan")
     return tuple(out)
+
+
+# ---------------------------------------------------------------------------------------------
+# the residual stream around a layer
+# ---------------------------------------------------------------------------------------------
+class Int8:
+    """A matrix [rows, cols] in 8-bit whole numbers: `values` int8 [rows, cols] whose rows begin on 16-byte boundaries, `scales` fp32 [rows]."""
+    __slots__ = ("values", "scales")
+
+    def __init__(self, values, scales):
+        (_MARSHAL or _marshal()).check_int8(values, scales)
+        self.values, self.scales = values, scales
+
+    @classmethod
+    def empty(cls, rows, cols, device="cuda"):
+        import torch
+        room = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.int8, device=device)
+        return cls(room[:, :cols], torch.empty(rows, dtype=torch.float32, device=device))
+
+    @property
+    def shape(self):
+        return tuple(self.values.shape)
+
+    def dequantize(self):
+        """The matrix in fp32 (torch operations: for inspection and tests)."""
+        return self.values.float() * self.scales.unsqueeze(1)
+
+
+def vsa2_residual_norm_fwd(x, residual=None, weight=None, eps=1e-6, h=None, y=None, y_fp8=None, y_int8=None, p=0.0, rng=None, stream=None):
+    """h = residual + dropout(x), y = h / sqrt(mean over the row of h^2 + eps) * weight, of matrices [rows, cols] (bf16 or fp32, contiguous rows).  Written are the
+    outputs that are given: h (of the residual's type, without one of x's), y (bf16 or fp32), y_fp8 (Fp8), y_int8 (Int8).  h may be x or residual itself.  weight: fp32 [cols], None:
+    ones.  p, rng: as vsa2_dropout."""
+    code = (_MARSHAL or _marshal()).norm_fwd(x, residual, weight, eps, h, y, y_fp8, y_int8, p, rng, stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_residual_norm_fwd")
+
+
+def vsa2_residual_norm_bwd_workspace_bytes(rows, cols) -> int:
+    return int(_lib().vsa2_residual_norm_bwd_workspace_bytes(rows, cols))
+
+
+def vsa2_residual_norm_bwd(h, dy, dh=None, weight=None, eps=1e-6, d_residual=None, dx=None, d_weight=None, workspace=None, p=0.0, rng=None, stream=None):
+    """Backward of vsa2_residual_norm_fwd: h, the gradient dy of y and dh of h (None: none; of h's type) -> what is given of d_residual (h's type), dx (through the dropout; without
+    one, and in h's type, d_residual is x's gradient too) and d_weight (fp32 [cols]).  workspace: vsa2_residual_norm_bwd_workspace_bytes(rows, cols) bytes (None without d_weight)."""
+    code = (_MARSHAL or _marshal()).norm_bwd(h, dy, dh, weight, eps, d_residual, dx, d_weight, workspace, p, rng, stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_residual_norm_bwd")
+
+
+def vsa2_dropout(x, y, p, rng, residual=None, stream=None):
+    """y = x / (1 - p) where an element is kept, else zero, plus the residual (of y's type) where one is given; y may be x or residual itself.  The mask follows from rng (int64 [2] on the
+    device: seed, offset) and an element's place; the backward is the same call on the gradient.  rng is read when the kernel runs: a captured graph draws anew when it changes."""
+    code = (_MARSHAL or _marshal()).dropout(x, y, p, rng, residual, stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_dropout")
+
+
+def vsa2_int8_quantize(x, out, stream=None):
+    """x [rows, cols] (bf16 or fp32, contiguous rows) -> `out` (Int8): each row's values times 127 over its largest magnitude, rounded to nearest."""
+    code = (_MARSHAL or _marshal()).int8_quantize(x, out, stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_int8_quantize")
+
+
+def vsa2_int8_matmul_workspace_bytes(m, n, k) -> int:
+    return int(_lib().vsa2_int8_matmul_workspace_bytes(m, n, k))
+
+
+def int8_matmul_workspace(m, n, k, device="cuda"):
+    """Workspace of vsa2_int8_matmul for products up to this size that follow one another on a stream."""
+    import torch
+    workspace = torch.empty(vsa2_int8_matmul_workspace_bytes(m, n, k), dtype=torch.uint8, device=device)
+    workspace[:256].zero_()          # status block
+    return workspace
+
+
+def vsa2_int8_matmul(a, b, c, workspace, bias=None, stream=None):
+    """c [m, n] = a b^T of two Int8 matrices [m, k] and [n, k], plus bias (fp32 [n]); c bf16 or fp32 with contiguous rows."""
+    code = (_MARSHAL or _marshal()).int8_matmul(a, b, c, workspace, bias, stream)
+    if code != OK:
+        raise Vsa2Error(code, "vsa2_int8_matmul")
 
 
 def vsa2_profile_events(kernel_id: int, start_event, stop_event):

@@ -6,6 +6,7 @@
 #include <atomic>
 
 #include "heads.cuh"
+#include "rows.cuh"
 #include "pooled_inputs.cuh"
 
 using namespace vsa2;
@@ -447,6 +448,46 @@ int check_fp8(const vsa2_fp8* v, int rows, int cols) {
 Fp8Arg fp8_arg(const vsa2_fp8* v) {
   return v != nullptr ? Fp8Arg{reinterpret_cast<unsigned char*>(v->values), v->scales, v->ld} : Fp8Arg{nullptr, nullptr, 0};
 }
+
+// ---- matrices of the residual stream ---------------------------------------------------------------------------------------
+// m [rows, cols] of a call that has elements; NULL: absent
+int check_rows(const vsa2_rows* m, int rows, int cols) {
+  if (m == nullptr) return VSA2_OK;
+  if (m->dtype != VSA2_BF16 && m->dtype != VSA2_F32) return VSA2_ERR_INVALID_ARG;
+  if (rows == 0 || cols == 0) return VSA2_OK;
+  if (m->data == nullptr || (rows > 1 && m->ld < cols)) return VSA2_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(m->data) & (m->dtype == VSA2_F32 ? 3u : 1u)) return VSA2_ERR_MISALIGNED;
+  return VSA2_OK;
+}
+// (the stride of a single row is of no use, but the kernels' choice of loads looks at it)
+RowsArg rows_arg(const vsa2_rows* m, int rows) { return m != nullptr ? RowsArg{m->data, rows > 1 ? m->ld : 0} : RowsArg{nullptr, 0}; }
+bool is_f32(const vsa2_rows* m) { return m != nullptr && m->dtype == VSA2_F32; }
+// whether two matrices begin at the same address (outputs do not)
+bool same_place(const vsa2_rows* a, const vsa2_rows* b) { return a != nullptr && b != nullptr && a->data == b->data; }
+int check_int8(const vsa2_int8* v, int rows, int cols) {
+  if (rows == 0 || cols == 0) return VSA2_OK;
+  if (v->values == nullptr || v->scales == nullptr || v->ld < cols) return VSA2_ERR_INVALID_ARG;
+  if (!aligned16(v->values) || v->ld % 16 || !aligned4(v->scales)) return VSA2_ERR_MISALIGNED;
+  return VSA2_OK;
+}
+Int8Arg int8_arg(const vsa2_int8* v) {
+  return v != nullptr ? Int8Arg{reinterpret_cast<signed char*>(v->values), v->scales, v->ld} : Int8Arg{nullptr, nullptr, 0};
+}
+int fill_drop(const vsa2_drop* drop, DropArg* out) {
+  *out = DropArg{nullptr, 0u, 1.f};
+  if (drop == nullptr) return VSA2_OK;
+  if (!(drop->p >= 0.0 && drop->p < 1.0)) return VSA2_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(drop->rng) & 7u) return VSA2_ERR_MISALIGNED;
+  if (drop->p == 0.0) return VSA2_OK;
+  if (drop->rng == nullptr) return VSA2_ERR_INVALID_ARG;
+  const int t = (int)(drop->p * 65536.0 + 0.5);
+  out->rng = reinterpret_cast<const unsigned long long*>(drop->rng);
+  out->threshold = t < 65535 ? t : 65535;
+  out->scale = (float)(65536.0 / (65536 - (int)out->threshold));
+  return VSA2_OK;
+}
+// rows and columns that the kernels' indices hold
+int check_extent(int rows, int cols) { return cols > 1 << 22 || rows > 0x7fffffff - (1 << 16) ? VSA2_ERR_UNSUPPORTED : VSA2_OK; }
 
 }  // namespace
 
@@ -1182,6 +1223,117 @@ int vsa2_fp8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_fp8* a, const vs
 int vsa2_debug_fp8_matmul_plan(int32_t m, int32_t n, int32_t k, int32_t c_dtype, int32_t c_aligned, int32_t sms, int32_t pairs, int32_t out[6]) {
   if (m <= 0 || n <= 0 || k <= 0 || sms <= 0 || (c_dtype != VSA2_BF16 && c_dtype != VSA2_F32) || out == nullptr) return VSA2_ERR_INVALID_ARG;
   fp8_matmul_plan(m, n, k, c_dtype == VSA2_F32, c_aligned != 0, sms, pairs != 0, out);
+  return VSA2_OK;
+}
+
+int vsa2_residual_norm_fwd(int32_t rows, int32_t cols, const vsa2_rows* x, const vsa2_rows* residual, const vsa2_drop* drop, const float* weight, float eps,
+                           const vsa2_rows* h, const vsa2_rows* y, const vsa2_fp8* y_fp8, const vsa2_int8* y_int8, void* cuda_stream) {
+  if (rows < 0 || cols < 0 || x == nullptr || !(eps >= 0.f)) return VSA2_ERR_INVALID_ARG;
+  if (h == nullptr && y == nullptr && y_fp8 == nullptr && y_int8 == nullptr) return VSA2_ERR_INVALID_ARG;
+  int rc;
+  for (const vsa2_rows* m : {x, residual, h, y})
+    if ((rc = check_rows(m, rows, cols)) != VSA2_OK) return rc;
+  const vsa2_rows* stream = residual != nullptr ? residual : x;
+  if ((h != nullptr && h->dtype != stream->dtype) || (rows > 0 && cols > 0 && same_place(h, y))) return VSA2_ERR_INVALID_ARG;
+  if ((y_fp8 != nullptr && (rc = check_fp8(y_fp8, rows, cols)) != VSA2_OK) || (y_int8 != nullptr && (rc = check_int8(y_int8, rows, cols)) != VSA2_OK)) return rc;
+  NormFwdArgs a = {};
+  if ((rc = fill_drop(drop, &a.drop)) != VSA2_OK) return rc;
+  if (!aligned4(weight)) return VSA2_ERR_MISALIGNED;
+  if ((rc = check_extent(rows, cols)) != VSA2_OK) return rc;
+  if (rows == 0 || cols == 0) return VSA2_OK;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  a.x = rows_arg(x, rows); a.r = rows_arg(residual, rows); a.h = rows_arg(h, rows); a.y = rows_arg(y, rows);
+  a.y_f32 = is_f32(y);
+  a.fp8 = fp8_arg(y_fp8); a.int8 = int8_arg(y_int8);
+  a.w = weight; a.eps = eps;
+  a.rows = rows; a.cols = cols;
+  VSA2_CUDA(launch_norm_fwd(a, is_f32(x), is_f32(stream), reinterpret_cast<cudaStream_t>(cuda_stream)));
+  return VSA2_OK;
+}
+
+size_t vsa2_residual_norm_bwd_workspace_bytes(int32_t rows, int32_t cols) { return rows < 0 || cols < 0 ? 0 : norm_bwd_workspace_bytes(rows, cols); }
+
+int vsa2_residual_norm_bwd(int32_t rows, int32_t cols, const vsa2_rows* h, const vsa2_rows* dy, const vsa2_rows* dh, const vsa2_drop* drop, const float* weight,
+                           float eps, const vsa2_rows* d_residual, const vsa2_rows* dx, float* d_weight, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (rows < 0 || cols < 0 || h == nullptr || dy == nullptr || !(eps >= 0.f)) return VSA2_ERR_INVALID_ARG;
+  if (d_residual == nullptr && dx == nullptr && d_weight == nullptr) return VSA2_ERR_INVALID_ARG;
+  int rc;
+  for (const vsa2_rows* m : {h, dy, dh, d_residual, dx})
+    if ((rc = check_rows(m, rows, cols)) != VSA2_OK) return rc;
+  if ((dh != nullptr && dh->dtype != h->dtype) || (d_residual != nullptr && d_residual->dtype != h->dtype)) return VSA2_ERR_INVALID_ARG;
+  if (rows > 0 && cols > 0 && same_place(d_residual, dx)) return VSA2_ERR_INVALID_ARG;
+  NormBwdArgs a = {};
+  if ((rc = fill_drop(drop, &a.drop)) != VSA2_OK) return rc;
+  if (!aligned4(weight) || !aligned4(d_weight)) return VSA2_ERR_MISALIGNED;
+  if ((rc = check_extent(rows, cols)) != VSA2_OK) return rc;
+  if (d_weight != nullptr && rows > 0 && cols > 0) {
+    if (workspace == nullptr) return VSA2_ERR_INVALID_ARG;
+    if (!aligned256(workspace)) return VSA2_ERR_MISALIGNED;
+    if (workspace_bytes < norm_bwd_workspace_bytes(rows, cols)) return VSA2_ERR_WORKSPACE_TOO_SMALL;
+  }
+  if (cols == 0 || (rows == 0 && d_weight == nullptr)) return VSA2_OK;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (rows == 0) {      // (a sum over nothing)
+    VSA2_CUDA(cudaMemsetAsync(d_weight, 0, cols * sizeof(float), st));
+    return VSA2_OK;
+  }
+  a.h = rows_arg(h, rows); a.dy = rows_arg(dy, rows); a.dh = rows_arg(dh, rows); a.dr = rows_arg(d_residual, rows); a.dx = rows_arg(dx, rows);
+  a.dx_f32 = is_f32(dx);
+  a.w = weight; a.eps = eps;
+  a.rows = rows; a.cols = cols;
+  VSA2_CUDA(launch_norm_bwd(a, is_f32(h), is_f32(dy), d_weight, reinterpret_cast<float*>(workspace), st));
+  return VSA2_OK;
+}
+
+int vsa2_dropout(int32_t rows, int32_t cols, const vsa2_rows* x, const vsa2_rows* residual, const vsa2_drop* drop, const vsa2_rows* y, void* cuda_stream) {
+  if (rows < 0 || cols < 0 || x == nullptr || y == nullptr || drop == nullptr) return VSA2_ERR_INVALID_ARG;
+  int rc;
+  for (const vsa2_rows* m : {x, residual, y})
+    if ((rc = check_rows(m, rows, cols)) != VSA2_OK) return rc;
+  if (residual != nullptr && residual->dtype != y->dtype) return VSA2_ERR_INVALID_ARG;
+  DropoutArgs a = {};
+  if ((rc = fill_drop(drop, &a.drop)) != VSA2_OK || (rc = check_extent(rows, cols)) != VSA2_OK) return rc;
+  if ((int64_t)rows * (cols / 8 + 1) > 1LL << 40) return VSA2_ERR_UNSUPPORTED;      // (more CTAs than a launch has)
+  if (rows == 0 || cols == 0) return VSA2_OK;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  a.x = rows_arg(x, rows); a.r = rows_arg(residual, rows); a.y = rows_arg(y, rows);
+  a.rows = rows; a.cols = cols;
+  VSA2_CUDA(launch_dropout(a, is_f32(x), is_f32(y), reinterpret_cast<cudaStream_t>(cuda_stream)));
+  return VSA2_OK;
+}
+
+int vsa2_int8_quantize(int32_t rows, int32_t cols, const vsa2_rows* x, const vsa2_int8* out, void* cuda_stream) {
+  if (rows < 0 || cols < 0 || x == nullptr || out == nullptr) return VSA2_ERR_INVALID_ARG;
+  int rc;
+  if ((rc = check_rows(x, rows, cols)) != VSA2_OK || (rc = check_int8(out, rows, cols)) != VSA2_OK || (rc = check_extent(rows, cols)) != VSA2_OK) return rc;
+  if (rows == 0 || cols == 0) return VSA2_OK;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  VSA2_CUDA(launch_int8_quantize(rows_arg(x, rows), is_f32(x), rows, cols, int8_arg(out), reinterpret_cast<cudaStream_t>(cuda_stream)));
+  return VSA2_OK;
+}
+
+size_t vsa2_int8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k) {
+  return m < 0 || n < 0 || k < 0 ? 0 : int8_matmul_workspace_bytes(m, n, k);
+}
+
+int vsa2_int8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_int8* a, const vsa2_int8* b, const float* bias, void* c, int32_t c_dtype, int64_t ldc,
+                     void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (m < 0 || n < 0 || k < 0 || !a || !b || (c_dtype != VSA2_BF16 && c_dtype != VSA2_F32)) return VSA2_ERR_INVALID_ARG;
+  if (m == 0 || n == 0) return VSA2_OK;
+  if (c == nullptr || workspace == nullptr || (m > 1 && ldc < n)) return VSA2_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(c) & (c_dtype == VSA2_F32 ? 3u : 1u) || !aligned4(bias)) return VSA2_ERR_MISALIGNED;
+  // (131071 products of 128 x 128 at most fit 32 bits)
+  if (m > 1 << 30 || n > 1 << 30 || k > 131071 || ((long long)m / 16 + 1) * ((long long)n / 128 + 1) > 1 << 30) return VSA2_ERR_UNSUPPORTED;
+  int rc;
+  if ((rc = check_int8(a, m, k)) != VSA2_OK || (rc = check_int8(b, n, k)) != VSA2_OK) return rc;
+  if (!aligned256(workspace)) return VSA2_ERR_MISALIGNED;
+  if (workspace_bytes < int8_matmul_workspace_bytes(m, n, k)) return VSA2_ERR_WORKSPACE_TOO_SMALL;
+  if ((rc = check_device()) != VSA2_OK) return rc;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (m == 1) ldc = n;
+  if (k == 0) VSA2_CUDA(launch_bias_rows(m, n, bias, c, c_dtype == VSA2_F32, ldc, st));
+  else VSA2_CUDA(launch_int8_matmul(m, n, k, int8_arg(a), int8_arg(b), bias, c, c_dtype == VSA2_F32, ldc, workspace, st));
   return VSA2_OK;
 }
 

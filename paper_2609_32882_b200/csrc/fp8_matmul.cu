@@ -14,29 +14,18 @@
 // cycles a block where the tensor cores need 448).  Tiles of 448 columns, both accumulators in one tile, need 27 % less intake and were as fast at large sizes (20000 x 15360 x
 // 5120 1028 us both ways), slower where rounds are few (4096^3 60 us instead of 52).  One row of A: the weights' bytes (15360 x 5120 16 us, 4.9 TB/s with the
 // launch); few tiles and short K: the launch, the first block's way from memory and the epilogue, 3 - 5 us.
-#include <cuda.h>
-
-#include "common.cuh"
-#include "heads.cuh"
-#include "tc05.cuh"
-#include "tc_attn.cuh"
-#include "tmap.cuh"
+#include "mm_tiles.cuh"
 
 namespace vsa2 {
 
 namespace {
 
-constexpr int kMmCtas = 148;            // most CTAs
-constexpr int kMmThreads = 384;
 constexpr int kMmStagesMost = 12;
 constexpr int kMmScaleSlots = 4;
-constexpr int kMmSplits = 16;           // most ranges that K is cut into
 // Blocks of K that an accumulator sums for an fp32 result; the epilogue adds the pieces.  (The tensor cores cut what does not fit an accumulator instead of rounding
 // it: with 24,000 values of K in one the result was 1.7e-6 off.  2304 x 1536 x 32760, where fp32 torch is 3.0e-7 off: pieces of 16 blocks 1.3e-7 and 109.2 us, of 32 2.2e-7 and
 // 108.5, of 40 2.7e-7 and 108.3, of 64 4.8e-7.)
 constexpr int kMmChunk = 40;
-constexpr uint32_t kMmPBytes = 128 * 128;
-constexpr uint32_t kMmTileBytes = 32 * 128 * 2;      // 32 rows of C x 128 elements of bf16
 
 // NT columns; PAIR: CTAs that share a tile; TO: type of the results
 template <int NT, int PAIR, typename TO>
@@ -52,12 +41,7 @@ struct MmTile {
   __host__ __device__ static constexpr uint32_t scales_at(uint32_t group) { return 224 + (group & 1) * 256; }
 };
 
-// P: the operand whose rows are the accumulators' lanes, Q: the one whose rows are its columns
-struct MmArgs {
-  int p_rows, q_rows, kb;            // kb: blocks of K
-  int pt, qt, gq;                    // tiles along P, along Q; tiles along Q that are taken together
-  int splits, chunk;                 // ranges that K is cut into; most blocks of K in one accumulator
-  Divisor by_tiles, by_group, by_gq, by_rest, by_splits;      // pt qt; gq pt; gq, and what the last group has of tiles along Q
+struct MmArgs : MmCut {
   int tensor_stores;                 // C lies as tensor copies need it, and ends where they end
   int in_pieces;                     // some range has more blocks than one accumulator sums
   const uint32_t* p_scales;
@@ -74,93 +58,6 @@ struct MmMisc {
   int abort_flag;
 };
 
-// The items of a CTA (or pair): every `all`-th of the tiles with the first range of K, then with the second, ..: CTAs that run at the same time read the same part
-// of K, so that rows they share come from memory once.  Each item in pieces of at most `chunk` blocks.
-struct MmWalk {
-  int p, q, split;                   // tile, range
-  int kb0, kb1, r0, r1;              // blocks of the current piece, of the item
-  int item, all;
-  __device__ __forceinline__ void init(int me, int of) {
-    item = me;
-    all = of;
-    kb1 = r1 = 0;
-  }
-  __device__ __forceinline__ bool advance(const MmArgs& a) {
-    if (kb1 < r1) {
-      kb0 = kb1;
-    } else {
-      const int tiles = a.pt * a.qt;
-      if (item >= tiles * a.splits) return false;
-      split = divided(item, a.by_tiles);
-      const int tile = item - split * tiles, g = divided(tile, a.by_group), r = tile - g * a.gq * a.pt, w = min(a.gq, a.qt - g * a.gq);
-      p = w == a.gq ? divided(r, a.by_gq) : divided(r, a.by_rest);
-      q = g * a.gq + r - p * w;
-      r0 = divided(a.kb * split, a.by_splits);      // (at most 2^23 blocks and 16 ranges)
-      r1 = divided(a.kb * (split + 1), a.by_splits);
-      item += all;
-      kb0 = r0;
-    }
-    kb1 = min(r1, kb0 + a.chunk);
-    return true;
-  }
-};
-
-// ---- a CTA alone, or a pair whose first CTA issues the products and holds the barriers that both sides arrive at
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t leaders(uint64_t* bar) {      // address of the first CTA's barrier
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(tc::smem_u32(bar)));
-  return r;
-}
-__device__ __forceinline__ void arrive_leader(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar)) : "memory");
-}
-// tc::mbar_wait on a barrier that the other CTA of a pair arrives at too
-template <int PAIR>
-__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  if constexpr (PAIR == 1) {
-    return tc::mbar_wait(bar, parity, abort_flag);
-  } else {
-    const uint32_t t0 = tc::timer_lo_ns();
-    for (;;) {
-      uint32_t ok;
-      asm volatile(
-          "{\n\t.reg .pred p;\n\t"
-          "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-          "selp.u32 %0, 1, 0, p;\n\t}"
-          : "=r"(ok)
-          : "r"(tc::smem_u32(bar)), "r"(parity)
-          : "memory");
-      if (ok != 0) return true;
-      if (*abort_flag || tc::timer_lo_ns() - t0 > tc::kWaitLimitNs) {
-        *abort_flag = 1;
-        return false;
-      }
-    }
-  }
-}
-#define VSA2_WAIT_PAIR(bar, parity)                                            \
-  do {                                                                         \
-    if (!wait_pair<PAIR>((bar), (parity), &misc->abort_flag)) goto done;       \
-  } while (0)
-template <int PAIR>
-__device__ __forceinline__ void tma_load_rows(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1) {
-  if constexpr (PAIR == 1)
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(bar)), "r"(c0), "r"(c1)
-                 : "memory");
-  else
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(leaders(bar)), "r"(c0), "r"(c1)
-                 : "memory");
-}
 // 32 x 16 bytes of shared memory to four columns of tensor memory, the same in each group of 32 lanes: words (r, j) of row j * 32 + r
 // (a pair: each CTA's own)
 template <int PAIR>
@@ -185,30 +82,6 @@ __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a_desc, uint64_t
         ::"r"(d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
         : "memory");
 }
-// arrives at the barrier of this CTA, or of both of the pair, once the products and copies issued so far are done
-template <int PAIR>
-__device__ __forceinline__ void commit_all(uint64_t* bar) {
-  if constexpr (PAIR == 1) tc::mma_commit(bar);
-  else
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(tc::smem_u32(bar)), "h"((uint16_t)3)
-                 : "memory");
-}
-template <int PAIR>
-__device__ __forceinline__ void mm_alloc(uint32_t* to) {
-  if constexpr (PAIR == 1) {
-    tc::tmem_alloc(to, 512);
-    tc::tmem_relinquish();
-  } else {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tc::smem_u32(to)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-  }
-}
-template <int PAIR>
-__device__ __forceinline__ void mm_dealloc(uint32_t base) {
-  if constexpr (PAIR == 1) tc::tmem_dealloc(base, 512);
-  else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(base) : "memory");
-}
 // 32 lanes x 32 columns, or 16, of an accumulator
 template <int N>
 __device__ __forceinline__ void load_columns(uint32_t taddr, float (&v)[N]) {
@@ -225,29 +98,6 @@ __device__ __forceinline__ constexpr uint32_t idesc_scaled(uint32_t sf) {
   return (sf << 4) | ((uint32_t)(NT >> 3) << 17) | (1u << 23) | ((uint32_t)PAIR << 27) | (sf << 29);
 }
 
-// Columns of an accumulator's row, straight code where all of them exist: with a test for each element the loads and stores came one at a time, and
-// the epilogue took longer than the products of 40 blocks.
-__device__ __forceinline__ void put(float* to, float v) { *to = v; }
-__device__ __forceinline__ void put(bf16* to, float v) { *to = __float2bfloat16_rn(v); }
-// elements `stride` apart (a warp's 32 rows lie next to one another in C)
-// (in the pieces' epilogue eight addresses at a time: all of them at once are more registers than there are)
-template <typename TO, int N>
-__device__ __forceinline__ void put_columns(TO* to, long long stride, int count, const float (&v)[N]) {
-  constexpr int AT = N < 32 ? 8 : N;
-#pragma unroll
-  for (int c0 = 0; c0 < N; c0 += AT) {
-    if (AT < N) asm volatile("" : "+l"(to));
-    if (count >= N) {
-#pragma unroll
-      for (int c = 0; c < AT; ++c, to += stride) put(to, v[c0 + c]);
-    } else {
-#pragma unroll
-      for (int c = 0; c < AT; ++c, to += stride)
-        if (c0 + c < count) put(to, v[c0 + c]);
-    }
-  }
-}
-
 // bf16: 32 rows x 32 columns of an accumulator (lanes and columns of `taddr`) as the fragments that stmatrix turns: four 8 x 8 blocks for each 8 columns
 __device__ __forceinline__ void take_tile(uint32_t taddr, uint32_t (&u)[16]) {
   uint32_t r[2][16];
@@ -260,34 +110,6 @@ __device__ __forceinline__ void take_tile(uint32_t taddr, uint32_t (&u)[16]) {
     for (int b = 0; b < 4; ++b)
       u[4 * g + b] = pack_bf16x2(__uint_as_float(r[b >> 1][4 * g + 2 * (b & 1)]), __uint_as_float(r[b >> 1][4 * g + 2 * (b & 1) + 1]));
 }
-// .. to rows of C in a tile that lies as the tensor copy takes it, 16-byte places exchanged by the row.  SWAP: 32 rows of C of this warp's, 64 bytes each, in
-// one box of 128 rows.  Else turned, 32 rows of C of 32 elements, in two boxes of 32 rows x 64 elements (128 bytes)
-template <bool SWAP>
-__device__ __forceinline__ void stage_tile(unsigned char* tile, const uint32_t (&u)[16], int quad, int lane) {
-  if constexpr (SWAP) {
-    const int row = quad * 32 + (lane >> 3) * 8 + (lane & 7);
-    const uint32_t to = tc::smem_u32(tile) + row * 64;
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};"
-                   ::"r"(to + ((g ^ ((row >> 1) & 3)) << 4)), "r"(u[4 * g]), "r"(u[4 * g + 1]), "r"(u[4 * g + 2]), "r"(u[4 * g + 3])
-                   : "memory");
-    return;
-  }
-  const int row = lane & 7, block = (quad & 1) * 4 + (lane >> 3);      // of C; of 8 elements in the box
-  const uint32_t to = tc::smem_u32(tile) + (quad >> 1) * 4096 + row * 128 + ((block ^ row) << 4);
-#pragma unroll
-  for (int g = 0; g < 4; ++g)
-    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
-                 ::"r"(to + g * 1024), "r"(u[4 * g]), "r"(u[4 * g + 1]), "r"(u[4 * g + 2]), "r"(u[4 * g + 3])
-                 : "memory");
-}
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, const void* from, int c0, int c1) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
-               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(from)), "r"(c0), "r"(c1)
-               : "memory");
-}
-
 template <int NT, int PAIR, bool SWAP, typename TO>
 __global__ void __cluster_dims__(PAIR, 1, 1) __launch_bounds__(kMmThreads, 1)
 fp8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_c,
@@ -589,28 +411,6 @@ __global__ void __launch_bounds__(256) fp8_sum_kernel(const float* parts, int sp
     if (col + j < n) put(c + row * ldc + col + j, sum[j]);
 }
 
-bool make_row_tmap(CUtensorMap* out, const void* base, int rows, int cols, long long ld, int box_rows) {
-  EncodeTiledFn fn = encode_tiled_fn();
-  if (fn == nullptr) return false;
-  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {(cuuint64_t)ld};
-  cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
-  cuuint32_t estr[2] = {1, 1};
-  return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-// C as boxes of 32 rows x 64 elements of bf16, with `swap` of 128 rows x 32
-bool make_result_tmap(CUtensorMap* out, void* base, int rows, int cols, long long ld, bool swap) {
-  EncodeTiledFn fn = encode_tiled_fn();
-  if (fn == nullptr) return false;
-  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-  cuuint32_t box[2] = {swap ? 32u : 64u, swap ? 128u : 32u};
-  cuuint32_t estr[2] = {1, 1};
-  return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            swap ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // One call
 struct MmCall {
   int m, n, k, kb, ctas;
@@ -657,30 +457,12 @@ MmPlan plan_mm(const MmCall& c, bool swap) {
   return plan;
 }
 
-// Tiles along Q that are taken together, under all of P's rows one after the other: half a round of pairs, as far as their rows lie in L2 (48 MB).
-// 75600 x 15360 x 5120, us: 6 tiles 4910, 12 4630, 24 4640, 37 4540, 74 5370
-int tiles_together(int columns, int kb, int qt) {
-  const long long group = (48LL << 20) / ((long long)columns * kb * 128);
-  const int together = (int)(group < 4 ? 4 : group > 37 ? 37 : group);
-  return together < qt ? together : qt;
-}
-
 template <int NT, int PAIR, bool SWAP, typename TO>
 cudaError_t launch_tiles(const MmCall& c, const MmPlan& plan, void* result, long long ldc, long long split_stride) {
   using T = MmTile<NT, PAIR, TO>;
   const Fp8Arg &p = SWAP ? c.fa : c.fb, &q = SWAP ? c.fb : c.fa;
   MmArgs a;
-  a.p_rows = SWAP ? c.m : c.n;
-  a.q_rows = SWAP ? c.n : c.m;
-  a.kb = c.kb;
-  a.pt = plan.pt; a.qt = plan.qt; a.splits = plan.splits;
-  a.gq = tiles_together(NT, c.kb, a.qt);
-  a.by_tiles = divisor((long long)a.pt * a.qt);
-  a.by_group = divisor((long long)a.gq * a.pt);
-  a.by_gq = divisor(a.gq);
-  a.by_rest = divisor(a.qt % a.gq > 0 ? a.qt % a.gq : a.gq);
-  a.by_splits = divisor(a.splits);
-  a.chunk = c.f32 ? kMmChunk : c.kb;
+  fill_cut(a, SWAP ? c.m : c.n, SWAP ? c.n : c.m, c.kb, plan.pt, plan.qt, plan.splits, tiles_together(NT, c.kb, plan.qt), c.f32 ? kMmChunk : c.kb);
   a.in_pieces = (a.kb + a.splits - 1) / a.splits > a.chunk;
   a.tensor_stores = sizeof(TO) == 2 && c.tensor_stores;
   a.p_scales = reinterpret_cast<const uint32_t*>(p.scales);
@@ -712,9 +494,6 @@ cudaError_t launch_mm(const MmCall& c, const MmPlan& plan) {
   return c.f32 ? launch_kernel(fp8_sum_kernel<float>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, by_row, reinterpret_cast<float*>(c.c), c.ldc)
                : launch_kernel(fp8_sum_kernel<bf16>, grid, 256, 0, c.st, c.parts, plan.splits, c.m, c.n, ldp, by_row, reinterpret_cast<bf16*>(c.c), c.ldc);
 }
-
-// Tensor copies write whole units of 16 bytes: with an n that is no multiple of 8 they put zeros behind C's last column (into what else lies in its rows).  Such results take plain stores.
-bool whole_units(int n) { return n % 8 == 0; }
 
 // The kernel of a call: columns of a tile, CTAs that share one, which operand's rows are its lanes.  `pairs`: takes_pairs, and the context has room for one
 struct MmChoice {

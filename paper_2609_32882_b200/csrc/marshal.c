@@ -1,4 +1,4 @@
-/* Argument marshalling of the calls between hidden states and attention, as a CPython module: tensors to the structs of vsa2.h and the library's function called,
+/* Argument marshalling of the calls between hidden states and attention, and of those of the residual stream, as a CPython module: tensors to the structs of vsa2.h and the library's function called,
  * nothing else.  A toy grid's calls wait for the host, and a view of a tensor costs the interpreter 0.6 us (norms and rotation: six of them), ctypes another
  * 0.7 us a call.  Tensors are used through their Python attributes, so the module needs no header of torch's.
  *
@@ -10,14 +10,21 @@
 #include "vsa2.h"
 
 /* names, torch's types (bind), the library's functions (bind) */
-static PyObject *n_shape, *n_stride, *n_dtype, *n_is_cuda, *n_data_ptr, *n_is_contiguous, *n_numel, *n_nbytes, *n_values, *n_scales;
-static PyObject *t_bf16, *t_f32, *t_i32, *t_e4m3, *t_u8, *stream_of;
+static PyObject *n_shape, *n_stride, *n_dtype, *n_is_cuda, *n_data_ptr, *n_is_contiguous, *n_numel, *n_nbytes, *n_values, *n_scales, *n_get_device;
+static PyObject *t_bf16, *t_f32, *t_i32, *t_e4m3, *t_u8, *t_i8, *t_i64, *stream_of, *device_of;
 static int (*f_rope_apply)(const vsa2_rope*, const vsa2_place*, const vsa2_heads*, const vsa2_heads*, int32_t, void*);
 static int (*f_qkv_fwd)(const vsa2_rope*, const vsa2_place*, const vsa2_qk_norm*, const vsa2_heads*, const vsa2_heads*, void*);
 static int (*f_qkv_bwd)(const vsa2_rope*, const vsa2_place*, const vsa2_qk_norm*, const vsa2_heads*, const vsa2_heads*, const vsa2_heads*, float*, float*, void*,
                         size_t, void*);
 static int (*f_quantize)(const void*, int32_t, int32_t, int32_t, int64_t, int32_t, const vsa2_fp8*, const vsa2_fp8*, void*);
 static int (*f_matmul)(int32_t, int32_t, int32_t, const vsa2_fp8*, const vsa2_fp8*, void*, int32_t, int64_t, void*, size_t, void*);
+static int (*f_norm_fwd)(int32_t, int32_t, const vsa2_rows*, const vsa2_rows*, const vsa2_drop*, const float*, float, const vsa2_rows*, const vsa2_rows*,
+                         const vsa2_fp8*, const vsa2_int8*, void*);
+static int (*f_norm_bwd)(int32_t, int32_t, const vsa2_rows*, const vsa2_rows*, const vsa2_rows*, const vsa2_drop*, const float*, float, const vsa2_rows*,
+                         const vsa2_rows*, float*, void*, size_t, void*);
+static int (*f_dropout)(int32_t, int32_t, const vsa2_rows*, const vsa2_rows*, const vsa2_drop*, const vsa2_rows*, void*);
+static int (*f_int8_quantize)(int32_t, int32_t, const vsa2_rows*, const vsa2_int8*, void*);
+static int (*f_int8_matmul)(int32_t, int32_t, int32_t, const vsa2_int8*, const vsa2_int8*, const float*, void*, int32_t, int64_t, void*, size_t, void*);
 
 static int refuse(const char* what) {
   PyErr_SetString(PyExc_ValueError, what);
@@ -369,22 +376,200 @@ static PyObject* check_fp8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-/* ((bf16, fp32, int32, e4m3, uint8), (addresses of the five functions), function that gives a stream's handle) */
+/* ---- the residual stream.  Its calls look at every tensor's device: the library runs on the current one, where another's addresses mean nothing */
+static int here(PyObject* t, int64_t* device) { /* of a CUDA tensor; *device: the current one, -1 before it was asked for */
+  int64_t of;
+  if ((*device < 0 && number(PyObject_CallNoArgs(device_of), device)) || number(PyObject_CallMethodNoArgs(t, n_get_device), &of)) return -1;
+  return of == *device ? 0 : refuse("tensors must be on the current CUDA device");
+}
+/* a matrix of the call's shape (the first sets it: rows < 0), None: absent */
+static int get_rows(PyObject* t, int64_t* device, int64_t* shape, vsa2_rows* r, const vsa2_rows** out) {
+  int64_t of[2];
+  *out = NULL;
+  if (t == Py_None) return 0;
+  if (get_matrix(t, of, &r->ld, &r->dtype, &r->data) || here(t, device)) return -1;
+  if (shape[0] >= 0 && (of[0] != shape[0] || of[1] != shape[1])) return refuse("the matrices of a call must have one shape");
+  shape[0] = of[0]; shape[1] = of[1];
+  r->reserved = 0;
+  *out = r;
+  return 0;
+}
+/* rng: int64 [2] on the device, or None */
+static int get_drop(PyObject* p, PyObject* rng, int64_t* device, vsa2_drop* d, const vsa2_drop** out) {
+  void* at = NULL;
+  d->p = PyFloat_AsDouble(p);
+  if (d->p == -1.0 && PyErr_Occurred()) return -1;
+  if (rng != Py_None) {
+    int64_t n;
+    const int typed = is_type(rng, t_i64);
+    if (typed < 0 || number(PyObject_CallMethodNoArgs(rng, n_numel), &n)) return -1;
+    if (!typed || n != 2) return refuse("rng must be a contiguous CUDA int64 tensor of two elements: seed and offset");
+    if (get_memory(rng, &at, NULL) || here(rng, device)) return -1;
+  }
+  d->rng = (const uint64_t*)at;
+  *out = d;
+  return 0;
+}
+static int get_weights(PyObject* t, int64_t* device, int64_t cols, float** out) { /* fp32 [cols], None: null */
+  void* at;
+  if (get_weight(t, (int)cols, &at) || (t != Py_None && here(t, device))) return -1;
+  *out = (float*)at;
+  return 0;
+}
+/* values and scales of a matrix in int8 form, on any device */
+static int int8_form(PyObject* values, PyObject* scales, int64_t* shape, int64_t* stride) {
+  int64_t of[1];
+  int rank, typed = is_type(values, t_i8);
+  if (typed < 0 || (rank = integers(PyObject_GetAttr(values, n_shape), shape, 2)) < 0) return -1;
+  if (rank == 2 && integers(PyObject_CallMethodNoArgs(values, n_stride), stride, 2) != 2) return -1;
+  if (!typed || rank != 2 || (shape[1] > 1 && stride[1] != 1)) return refuse("values must be int8 [rows, cols] with contiguous rows");
+  typed = is_type(scales, t_f32);
+  if (typed < 0 || (rank = integers(PyObject_GetAttr(scales, n_shape), of, 1)) < 0) return -1;
+  if (!typed || rank != 1 || of[0] != shape[0]) return refuse("scales must be fp32 [rows]");
+  return 0;
+}
+static int get_int8(PyObject* o, int64_t* device, vsa2_int8* v, int64_t* shape) { /* an Int8 object; its shape */
+  int bad = -1;
+  int64_t stride[2];
+  void* scales;
+  PyObject *values = PyObject_GetAttr(o, n_values), *s = values != NULL ? PyObject_GetAttr(o, n_scales) : NULL;
+  if (s == NULL || on_gpu(values, "expected a CUDA tensor") || int8_form(values, s, shape, stride) || fits_int(shape, 2) || address(values, &v->values) ||
+      get_memory(s, &scales, NULL) || here(values, device) || here(s, device))
+    goto out;
+  v->scales = (float*)scales;
+  v->ld = shape[0] > 1 ? stride[0] : (shape[1] + 15) / 16 * 16;
+  bad = 0;
+out:
+  Py_XDECREF(values);
+  Py_XDECREF(s);
+  return bad;
+}
+static int fp8_here(PyObject* o, int64_t* device) {
+  PyObject *values = PyObject_GetAttr(o, n_values), *s = values != NULL ? PyObject_GetAttr(o, n_scales) : NULL;
+  const int bad = s == NULL || here(values, device) || here(s, device);
+  Py_XDECREF(values);
+  Py_XDECREF(s);
+  return bad ? -1 : 0;
+}
+static int one_shape(const int64_t* a, const int64_t* b) {
+  return a[0] == b[0] && a[1] == b[1] ? 0 : refuse("the matrices of a call must have one shape");
+}
+/* (x, residual, weight, eps, h, y, y_fp8, y_int8, p, rng, stream) */
+static PyObject* norm_fwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t shape[2] = {-1, -1}, of[2], device = -1;
+  vsa2_rows m[4];
+  const vsa2_rows *x, *r, *h, *y;
+  vsa2_fp8 fp8;
+  vsa2_int8 int8;
+  vsa2_drop store;
+  const vsa2_drop* drop;
+  float* w;
+  void* stream;
+  if (arguments(n, 11) || get_rows(a[0], &device, shape, &m[0], &x) || get_rows(a[1], &device, shape, &m[1], &r) ||
+      get_rows(a[4], &device, shape, &m[2], &h) || get_rows(a[5], &device, shape, &m[3], &y))
+    return NULL;
+  if (x == NULL) {
+    refuse("x is missing");
+    return NULL;
+  }
+  if ((a[6] != Py_None && (get_fp8(a[6], &fp8, of) || fp8_here(a[6], &device) || one_shape(of, shape))) ||
+      (a[7] != Py_None && (get_int8(a[7], &device, &int8, of) || one_shape(of, shape))) || get_weights(a[2], &device, shape[1], &w) ||
+      get_drop(a[8], a[9], &device, &store, &drop))
+    return NULL;
+  const double eps = PyFloat_AsDouble(a[3]);
+  if ((eps == -1.0 && PyErr_Occurred()) || get_stream(a[10], &stream)) return NULL;
+  CALLED(f_norm_fwd((int32_t)shape[0], (int32_t)shape[1], x, r, drop, w, (float)eps, h, y, a[6] != Py_None ? &fp8 : NULL, a[7] != Py_None ? &int8 : NULL,
+                    stream));
+}
+/* (h, dy, dh, weight, eps, d_residual, dx, d_weight, workspace, p, rng, stream) */
+static PyObject* norm_bwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t shape[2] = {-1, -1}, device = -1;
+  vsa2_rows m[5];
+  const vsa2_rows *h, *dy, *dh, *dr, *dx;
+  vsa2_drop store;
+  const vsa2_drop* drop;
+  float *w, *dw;
+  void *workspace, *stream;
+  size_t bytes;
+  if (arguments(n, 12) || get_rows(a[0], &device, shape, &m[0], &h) || get_rows(a[1], &device, shape, &m[1], &dy) ||
+      get_rows(a[2], &device, shape, &m[2], &dh) || get_rows(a[5], &device, shape, &m[3], &dr) || get_rows(a[6], &device, shape, &m[4], &dx))
+    return NULL;
+  if (h == NULL || dy == NULL) {
+    refuse("h or dy is missing");
+    return NULL;
+  }
+  if (get_weights(a[3], &device, shape[1], &w) || get_weights(a[7], &device, shape[1], &dw) || get_memory(a[8], &workspace, &bytes) ||
+      (a[8] != Py_None && here(a[8], &device)) || get_drop(a[9], a[10], &device, &store, &drop))
+    return NULL;
+  const double eps = PyFloat_AsDouble(a[4]);
+  if ((eps == -1.0 && PyErr_Occurred()) || get_stream(a[11], &stream)) return NULL;
+  CALLED(f_norm_bwd((int32_t)shape[0], (int32_t)shape[1], h, dy, dh, drop, w, (float)eps, dr, dx, dw, workspace, bytes, stream));
+}
+/* (x, y, p, rng, residual, stream) */
+static PyObject* dropout(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t shape[2] = {-1, -1}, device = -1;
+  vsa2_rows m[3];
+  const vsa2_rows *x, *y, *r;
+  vsa2_drop store;
+  const vsa2_drop* drop;
+  void* stream;
+  if (arguments(n, 6) || get_rows(a[0], &device, shape, &m[0], &x) || get_rows(a[1], &device, shape, &m[1], &y) ||
+      get_rows(a[4], &device, shape, &m[2], &r) || get_drop(a[2], a[3], &device, &store, &drop) || get_stream(a[5], &stream))
+    return NULL;
+  CALLED(f_dropout((int32_t)shape[0], (int32_t)shape[1], x, r, drop, y, stream));
+}
+/* (x, out, stream) */
+static PyObject* int8_quantize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t shape[2] = {-1, -1}, of[2], device = -1;
+  vsa2_rows m;
+  const vsa2_rows* x;
+  vsa2_int8 out;
+  void* stream;
+  if (arguments(n, 3) || get_rows(a[0], &device, shape, &m, &x) || get_int8(a[1], &device, &out, of) || one_shape(of, shape) ||
+      get_stream(a[2], &stream))
+    return NULL;
+  CALLED(f_int8_quantize((int32_t)shape[0], (int32_t)shape[1], x, &out, stream));
+}
+/* (a, b, c, workspace, bias, stream) */
+static PyObject* int8_matmul(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t of_a[2], of_b[2], of_c[2], ld, device = -1;
+  int32_t type;
+  void *c, *workspace, *stream;
+  size_t bytes;
+  vsa2_int8 va, vb;
+  float* bias;
+  if (arguments(n, 6) || get_int8(a[0], &device, &va, of_a) || get_int8(a[1], &device, &vb, of_b) ||
+      get_matrix(a[2], of_c, &ld, &type, &c) || here(a[2], &device) || get_memory(a[3], &workspace, &bytes) || (a[3] != Py_None && here(a[3], &device)))
+    return NULL;
+  if (of_a[1] != of_b[1] || of_c[0] != of_a[0] || of_c[1] != of_b[0]) {
+    refuse("the shapes of a, b and c do not fit");
+    return NULL;
+  }
+  if (get_weights(a[4], &device, of_b[0], &bias) || get_stream(a[5], &stream)) return NULL;
+  CALLED(f_int8_matmul((int32_t)of_a[0], (int32_t)of_b[0], (int32_t)of_a[1], &va, &vb, bias, c, type, ld, workspace, bytes, stream));
+}
+/* (values, scales): whether they are a matrix in int8 form */
+static PyObject* check_int8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t shape[2], stride[2];
+  if (arguments(n, 2) || int8_form(a[0], a[1], shape, stride)) return NULL;
+  Py_RETURN_NONE;
+}
+
+/* n objects of a tuple, borrowed, and n addresses of another */
+static int bound(PyObject* types, PyObject* calls, int n_types, int n_calls, void** f) {
+  if (!PyTuple_Check(types) || !PyTuple_Check(calls) || PyTuple_GET_SIZE(types) != n_types || PyTuple_GET_SIZE(calls) != n_calls)
+    return refuse("a tuple of types and a tuple of addresses are expected");
+  for (int i = 0; i < n_calls; ++i) {
+    f[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(calls, i));
+    if (f[i] == NULL) return PyErr_Occurred() ? -1 : refuse("a function's address is missing");
+  }
+  return 0;
+}
+/* ((bf16, fp32, int32, e4m3, uint8), (addresses of the five functions between hidden states and attention), function that gives a stream's handle) */
 static PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   PyObject** const types[5] = {&t_bf16, &t_f32, &t_i32, &t_e4m3, &t_u8};
   void* f[5];
-  if (arguments(n, 3)) return NULL;
-  if (!PyTuple_Check(a[0]) || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[0]) != 5 || PyTuple_GET_SIZE(a[1]) != 5) {
-    refuse("two tuples of five are expected");
-    return NULL;
-  }
-  for (int i = 0; i < 5; ++i) {
-    f[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(a[1], i));
-    if (f[i] == NULL) {
-      if (!PyErr_Occurred()) refuse("a function's address is missing");
-      return NULL;
-    }
-  }
+  if (arguments(n, 3) || bound(a[0], a[1], 5, 5, f)) return NULL;
   for (int i = 0; i < 5; ++i) Py_XSETREF(*types[i], Py_NewRef(PyTuple_GET_ITEM(a[0], i)));
   Py_XSETREF(stream_of, Py_NewRef(a[2]));
   memcpy(&f_rope_apply, &f[0], sizeof f[0]);
@@ -394,15 +579,31 @@ static PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   memcpy(&f_matmul, &f[4], sizeof f[0]);
   Py_RETURN_NONE;
 }
+/* ((int8, int64), (addresses of the five functions of the residual stream), function that gives the current device); behind bind */
+static PyObject* bind_rows(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* f[5];
+  if (arguments(n, 3) || bound(a[0], a[1], 2, 5, f)) return NULL;
+  Py_XSETREF(t_i8, Py_NewRef(PyTuple_GET_ITEM(a[0], 0)));
+  Py_XSETREF(t_i64, Py_NewRef(PyTuple_GET_ITEM(a[0], 1)));
+  Py_XSETREF(device_of, Py_NewRef(a[2]));
+  memcpy(&f_norm_fwd, &f[0], sizeof f[0]);
+  memcpy(&f_norm_bwd, &f[1], sizeof f[0]);
+  memcpy(&f_dropout, &f[2], sizeof f[0]);
+  memcpy(&f_int8_quantize, &f[3], sizeof f[0]);
+  memcpy(&f_int8_matmul, &f[4], sizeof f[0]);
+  Py_RETURN_NONE;
+}
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
-static PyMethodDef methods[] = {ENTRY(bind), ENTRY(check_fp8), ENTRY(rope_apply), ENTRY(qkv_fwd), ENTRY(qkv_bwd), ENTRY(quantize), ENTRY(matmul), {NULL, NULL, 0, NULL}};
+static PyMethodDef methods[] = {ENTRY(bind), ENTRY(bind_rows), ENTRY(check_fp8), ENTRY(rope_apply), ENTRY(qkv_fwd), ENTRY(qkv_bwd), ENTRY(quantize), ENTRY(matmul),
+                                ENTRY(check_int8), ENTRY(norm_fwd), ENTRY(norm_bwd), ENTRY(dropout), ENTRY(int8_quantize), ENTRY(int8_matmul), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, .m_name = "_marshal", .m_size = -1, .m_methods = methods};
 
 PyMODINIT_FUNC PyInit__marshal(void) {
   static const struct { PyObject** at; const char* name; } names[] = {
       {&n_shape, "shape"}, {&n_stride, "stride"}, {&n_dtype, "dtype"}, {&n_is_cuda, "is_cuda"}, {&n_data_ptr, "data_ptr"},
-      {&n_is_contiguous, "is_contiguous"}, {&n_numel, "numel"}, {&n_nbytes, "nbytes"}, {&n_values, "values"}, {&n_scales, "scales"}};
+      {&n_is_contiguous, "is_contiguous"}, {&n_numel, "numel"}, {&n_nbytes, "nbytes"}, {&n_values, "values"}, {&n_scales, "scales"},
+      {&n_get_device, "get_device"}};
   for (size_t i = 0; i < sizeof names / sizeof names[0]; ++i)
     if ((*names[i].at = PyUnicode_InternFromString(names[i].name)) == NULL) return NULL;
   return PyModule_Create(&module);

@@ -1,0 +1,171 @@
+// Matrices whose rows are tokens, taken in pieces of eight neighbouring elements, and the dropout that falls on them: what the kernels of the
+// residual stream (residual_norm.cu, dropout.cu) share, and their arguments.
+#pragma once
+#include "common.cuh"
+#include "heads.cuh"
+
+namespace vsa2 {
+
+// [rows, cols] with contiguous rows `ld` elements apart; null: absent
+struct RowsArg {
+  void* p;
+  long long ld;
+};
+// int8 values [rows, ld] and a scale a row
+struct Int8Arg {
+  signed char* values;
+  float* scales;
+  long long ld;
+};
+// rng: seed and offset, on the device; an element is kept where its 16 bits are at least `threshold` (0: no dropout)
+struct DropArg {
+  const unsigned long long* rng;
+  uint32_t threshold;
+  float scale;
+};
+struct NormFwdArgs {
+  RowsArg x, r, h, y;
+  Fp8Arg fp8;
+  Int8Arg int8;
+  const float* w;
+  float eps, inv_cols;
+  int rows, cols, octs, y_f32;
+  DropArg drop;
+};
+struct NormBwdArgs {
+  RowsArg h, dy, dh, dr, dx;
+  const float* w;
+  float* parts;      // null: the weight's gradient is not wanted
+  float eps, inv_cols;
+  int rows, cols, octs, dx_f32;
+  DropArg drop;
+};
+struct DropoutArgs {
+  RowsArg x, r, y;
+  int rows, cols, octs;
+  Divisor by_octs;
+  DropArg drop;
+};
+cudaError_t launch_norm_fwd(NormFwdArgs a, bool x_f32, bool h_f32, cudaStream_t st);
+cudaError_t launch_int8_quantize(const RowsArg& x, bool x_f32, int rows, int cols, const Int8Arg& out, cudaStream_t st);
+size_t norm_bwd_workspace_bytes(int rows, int cols);
+cudaError_t launch_norm_bwd(NormBwdArgs a, bool h_f32, bool dy_f32, float* dw, float* parts, cudaStream_t st);
+cudaError_t launch_dropout(DropoutArgs a, bool x_f32, bool y_f32, cudaStream_t st);
+size_t int8_matmul_workspace_bytes(int m, int n, int k);
+cudaError_t launch_int8_matmul(int m, int n, int k, const Int8Arg& a, const Int8Arg& b, const float* bias, void* c, int c_f32, long long ldc, void* workspace,
+                               cudaStream_t st);
+// k = 0: the bias, or nothing
+cudaError_t launch_bias_rows(int m, int n, const float* bias, void* c, int c_f32, long long ldc, cudaStream_t st);
+
+// whether every row of a matrix of elements of `size` bytes begins on a 16-byte boundary
+inline bool rows_aligned(const RowsArg& m, size_t size) {
+  return m.p == nullptr || ((reinterpret_cast<uintptr_t>(m.p) & 15u) == 0 && m.ld * (long long)size % 16 == 0);
+}
+
+// Eight neighbouring elements as they lie in memory
+template <typename T> struct Eight;
+template <> struct Eight<bf16> {
+  uint32_t u[4];
+  __device__ __forceinline__ void zero() { u[0] = u[1] = u[2] = u[3] = 0u; }
+  __device__ __forceinline__ void load(const bf16* p) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    u[0] = v.x; u[1] = v.y; u[2] = v.z; u[3] = v.w;
+  }
+  __device__ __forceinline__ void set(int j, const bf16* p) { u[j / 2] |= (uint32_t)*reinterpret_cast<const unsigned short*>(p) << 16 * (j & 1); }
+  __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? u[j / 2] & 0xffff0000u : u[j / 2] << 16); }
+  __device__ __forceinline__ void round(const float (&f)[8]) {      // to the type
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+  }
+  __device__ __forceinline__ void store(bf16* p) const { *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]); }
+  __device__ __forceinline__ void store(bf16* p, int j) const { *reinterpret_cast<unsigned short*>(p) = (unsigned short)(u[j / 2] >> 16 * (j & 1)); }
+};
+template <> struct Eight<float> {
+  float f[8];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = 0.f;
+  }
+  __device__ __forceinline__ void load(const float* p) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+  __device__ __forceinline__ void set(int j, const float* p) { f[j] = *p; }
+  __device__ __forceinline__ float get(int j) const { return f[j]; }
+  __device__ __forceinline__ void round(const float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = v[j];
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  }
+  __device__ __forceinline__ void store(float* p, int j) const { *p = f[j]; }
+};
+// Elements i .. i+7 of a row (zeros behind it, and for i beyond it); VEC: rows begin on 16-byte boundaries
+template <bool VEC, typename T>
+__device__ __forceinline__ void load_eight(Eight<T>& e, const T* row, int i, int cols) {
+  if (VEC && i + 8 <= cols) {
+    e.load(row + i);
+  } else {
+    e.zero();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i + j < cols) e.set(j, row + i + j);
+  }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_eight(const Eight<T>& e, T* row, int i, int cols) {
+  if (VEC && i + 8 <= cols) {
+    e.store(row + i);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i + j < cols) e.store(row + i + j, j);
+  }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_floats(const float (&f)[8], T* row, int i, int cols) {
+  Eight<T> e;
+  e.round(f);
+  store_eight<VEC>(e, row, i, cols);
+}
+
+// Which elements are kept.  The counter-based generator Philox 4x32 with ten rounds (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): its
+// key is the seed, its counter (column / 8, row, offset), and its 128 bits are 16 for each of eight neighbours.  So the mask follows from seed, offset and an element's place alone: no
+// shape of a launch, alignment or stride changes it, and a backward pass forms it again.  (32 bits an element would take twice the multiplications, and ten rounds for four
+// elements run at the pace of memory.)
+struct DropMask {
+  uint32_t k0, k1, o0, o1, limit;
+  float scale;
+  __device__ __forceinline__ void init(const DropArg& d) {
+    const unsigned long long seed = d.threshold ? d.rng[0] : 0, offset = d.threshold ? d.rng[1] : 0;
+    k0 = (uint32_t)seed; k1 = (uint32_t)(seed >> 32);
+    o0 = (uint32_t)offset; o1 = (uint32_t)(offset >> 32);
+    limit = d.threshold << 16;
+    scale = d.scale;
+  }
+  // Eight elements: zero, or times the scale.  (A product of its own, not part of a fused one: what the library computes does not depend on what is added behind it.)
+  __device__ __forceinline__ void apply(float (&f)[8], uint32_t row, uint32_t oct) const {
+    if (limit == 0) return;
+    uint32_t a = oct, b = row, c = o0, d = o1, p = k0, q = k1;
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+      const unsigned long long u = (unsigned long long)a * 0xD2511F53u, v = (unsigned long long)c * 0xCD9E8D57u;
+      a = (uint32_t)(v >> 32) ^ b ^ p;
+      b = (uint32_t)v;
+      c = (uint32_t)(u >> 32) ^ d ^ q;
+      d = (uint32_t)u;
+      p += 0x9E3779B9u;
+      q += 0xBB67AE85u;
+    }
+    const uint32_t w[4] = {a, b, c, d};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t bits = j & 1 ? w[j / 2] : w[j / 2] << 16;      // (of the odd ones the lower half decides nothing)
+      f[j] = bits >= limit ? __fmul_rn(f[j], scale) : 0.f;
+    }
+  }
+};
+
+}  // namespace vsa2
