@@ -15,7 +15,8 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const __grid_cons
   DropMask mask;
   mask.init(a.drop);
   // pieces in the order of the rows; the first of this CTA's in 64 bits, the others from there
-  const long long first = (long long)blockIdx.x * (kDropThreads * kDropOcts), row0 = first / a.octs;
+  // (less than 2^40 pieces in all, 2^20 in a row: the product with 2^64 / octs is exact)
+  const long long first = (long long)blockIdx.x * (kDropThreads * kDropOcts), row0 = a.octs == 1 ? first : (long long)__umul64hi(first, a.per_octs);
   const int skip = (int)(first - row0 * a.octs) + threadIdx.x;
   Eight<X> x[kDropOcts];
   Eight<Y> r[kDropOcts];
@@ -41,10 +42,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const __grid_cons
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = x[u].get(j);
     mask.apply(f, row[u], oct[u]);
-    if (a.r.p != nullptr) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = __fadd_rn(r[u].get(j), f[j]);
-    }
+    if (a.r.p != nullptr) add_eight(f, r[u]);
     if (row[u] < a.rows) store_floats<VEC>(f, reinterpret_cast<Y*>(a.y.p) + row[u] * a.y.ld, oct[u] * 8, a.cols);
   }
 }
@@ -54,10 +52,11 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const __grid_cons
 cudaError_t launch_dropout(DropoutArgs a, bool x_f32, bool y_f32, cudaStream_t st) {
   a.octs = (a.cols + 7) / 8;
   a.by_octs = divisor(a.octs);
+  a.per_octs = ~0ULL / a.octs + 1;
   const long long octs = (long long)a.rows * a.octs, per = kDropThreads * kDropOcts;
   const unsigned grid = (unsigned)((octs + per - 1) / per);
   const size_t size = y_f32 ? 4 : 2;
-  const bool vec = rows_aligned(a.x, x_f32 ? 4 : 2) && rows_aligned(a.r, size) && rows_aligned(a.y, size);
+  const bool vec = a.cols % 8 == 0 && rows_aligned(a.x, x_f32 ? 4 : 2) && rows_aligned(a.r, size) && rows_aligned(a.y, size);
   auto go = [&](auto aligned, auto any) { return launch_kernel(vec ? aligned : any, grid, kDropThreads, 0, st, a); };
   if (x_f32) return y_f32 ? go(dropout_kernel<float, float, true>, dropout_kernel<float, float, false>) : go(dropout_kernel<float, bf16, true>, dropout_kernel<float, bf16, false>);
   return y_f32 ? go(dropout_kernel<bf16, float, true>, dropout_kernel<bf16, float, false>) : go(dropout_kernel<bf16, bf16, true>, dropout_kernel<bf16, bf16, false>);

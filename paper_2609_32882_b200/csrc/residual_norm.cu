@@ -4,8 +4,9 @@
 //   backward: with r = 1 / sqrt(mean(h^2) + eps), g = w dy:  dh' = dh + r g - h r^3 mean(g h);  dx = dropout's part of dh';  dw = sum over the rows of dy h r
 //   int8    : v = h w (for vsa2_int8_quantize a matrix' own values), s = max |v| / 127, value = v * (127 / max |v|) rounded to nearest, ties to even; the row's r is part of its
 //             scale alone, so a value does not depend on how the sum of squares was rounded
-// A CTA takes a row at a time, eight neighbouring elements in each of a thread's V pieces: the row is read once, stays in registers while its sums pass through one barrier, and
-// leaves.  Bound by memory.  Rows of more than 8192 elements (MANY) are read twice, the second time from L2, in a loop over the pieces.
+// A CTA takes a row at a time, eight neighbouring elements in each of a thread's pieces.  Rows on 16-byte boundaries of up to 8192 elements (the ring kernels): each thread asks for its own
+// pieces of the next rows ahead of time, in places of shared memory that are its own, so that memory is kept busy while a row's sums pass through the CTA's one barrier.
+// Other rows come as they are needed: of up to 8192 elements they stay in registers, longer ones (MANY) are read twice, the second time from L2.  Bound by memory.
 #include "fp8_values.cuh"
 #include "rows.cuh"
 
@@ -15,6 +16,8 @@ namespace {
 
 constexpr int kNormMost = 512;       // threads of a CTA at most
 constexpr int kNormParts = 1184;     // most CTAs of the backward, each with its own partial sums of the weight's gradient (eight for each of 148 SMs)
+constexpr int kAhead = 2;            // rows that a thread of the ring kernels has asked for beyond the one it works on
+constexpr int kRingCols = 8192;      // their longest rows
 constexpr float kInt8Least = 0x1p-100f;      // least max |v|: below it 127 / max |v| would leave fp32's range
 
 // Rows whose mean square lies outside are taken again times a power of two: their squares could vanish or pass fp32's range
@@ -29,7 +32,18 @@ __device__ __forceinline__ float power_for(uint32_t top_bits, float eps) {
 struct RowSums {      // double-buffered by the row's parity: one barrier a row
   float2 of[2][kNormMost / 32];
 };
-// Sum of `sum` and of `other` (MAX: the largest of its bits as an unsigned number) over the CTA, the same bits in every thread
+// the larger magnitude; NaN where one is
+__device__ __forceinline__ float larger(float top, float a, float b) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(top), "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float warp_largest(float v) {
+  float r;
+  asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+// Sum of `sum` and of `other` (MAX: the largest magnitude) over the CTA, the same bits in every thread
 template <bool MAX>
 __device__ __forceinline__ float2 row_total(float sum, float other, RowSums& sh, uint32_t parity) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -38,7 +52,7 @@ __device__ __forceinline__ float2 row_total(float sum, float other, RowSums& sh,
     sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (!MAX) other += __shfl_xor_sync(0xffffffffu, other, o);
   }
-  if (MAX) other = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(other)));
+  if (MAX) other = warp_largest(other);
   if (warps == 1) return make_float2(sum, other);
   float2* of = sh.of[parity & 1];
   if (lane == 0) of[warp] = make_float2(sum, other);
@@ -52,177 +66,334 @@ __device__ __forceinline__ float2 row_total(float sum, float other, RowSums& sh,
     if (!MAX) other += __shfl_xor_sync(0xffffffffu, other, o);
   }
   sum = __shfl_sync(0xffffffffu, sum, 0);
-  if (MAX) other = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(other)));
+  if (MAX) other = warp_largest(other);
   else other = __shfl_sync(0xffffffffu, other, 0);
   return make_float2(sum, other);
 }
 
-__device__ __forceinline__ void load_weight(float (&w)[8], const float* from, int i, int cols) {
-  // (weights may lie at any fp32's address)
-#pragma unroll
-  for (int j = 0; j < 8; ++j) w[j] = from == nullptr ? 1.f : i + j < cols ? from[i + j] : 0.f;
-}
-// (aligned, whole pieces)
-__device__ __forceinline__ void load_weight(float (&w)[8], const float4* from) {
-  const float4 a = from[0], b = from[1];
-  w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-}
+// Weights of elements i .. i+7 (null: ones), zeros behind the row.  VEC: whole pieces on 16-byte boundaries
 template <bool VEC>
-__device__ __forceinline__ void weight_of(float (&w)[8], const float* from, int i, int cols) {
-  if (VEC && from != nullptr && i + 8 <= cols) load_weight(w, reinterpret_cast<const float4*>(from + i));
-  else load_weight(w, from, i, cols);
+__device__ __forceinline__ void weight_of(float2 (&w)[4], const float* from, int i, int cols) {
+  if (VEC && from != nullptr && i < cols) {
+    const float4 a = reinterpret_cast<const float4*>(from + i)[0], b = reinterpret_cast<const float4*>(from + i)[1];
+    w[0] = make_float2(a.x, a.y); w[1] = make_float2(a.z, a.w);
+    w[2] = make_float2(b.x, b.y); w[3] = make_float2(b.z, b.w);
+  } else {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = from == nullptr ? 1.f : !VEC && i + j < cols ? from[i + j] : 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = make_float2(v[2 * j], v[2 * j + 1]);
+  }
+}
+// times a power of two
+template <typename S>
+__device__ __forceinline__ void rescale(Eight<S>& e, float s) {
+  float f[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = e.get(j) * s;
+  e.round(f);
+}
+template <typename S>
+__device__ __forceinline__ float largest_of(const Eight<S>& e, float top) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = larger(top, e.pair(i).x, e.pair(i).y);
+  return top;
+}
+// the row's sum of squares (two sums) and its largest |h w|
+template <bool NORM, bool INT8, typename S>
+__device__ __forceinline__ void add_sums(const Eight<S>& h, const float2 (&w)[4], float2& ss, float& top) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 p = h.pair(i);
+    if (NORM) ss = __ffma2_rn(p, p, ss);
+    if (INT8) {
+      const float2 v = NORM ? __fmul2_rn(p, w[i]) : p;
+      top = larger(top, v.x, v.y);
+    }
+  }
 }
 
 // ---- the forms that y leaves in
 // e4m3: the 16 threads of a block of 128 find its scale together.  (By whole warps; pieces behind the row are zeros.)
-__device__ __forceinline__ void put_fp8(const float (&v)[8], float r, const NormFwdArgs& a, int row, int oct) {
-  float f[8];
-  uint32_t top = 0;
+__device__ __forceinline__ void put_fp8(const float2 (&y)[4], const NormFwdArgs& a, int row, int oct) {
+  float top = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    f[j] = v[j] * r;
-    top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
+  for (int i = 0; i < 4; ++i) top = larger(top, y[i].x, y[i].y);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    const float other = __shfl_xor_sync(0xffffffffu, top, o);
+    top = larger(top, other, other);
   }
+  uint32_t bits = __float_as_uint(top);
+  const bool odd = __any_sync(0xffffffffu, bits >= kInf);
+  if (odd) {      // (rare) the largest of what is finite
+    bits = 0u;
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  const bool odd = __any_sync(0xffffffffu, top >= kInf);
-  if (odd) {
-    top = 0;
+    for (int i = 0; i < 4; ++i) {
+      if (finite_bits(y[i].x)) bits = max(bits, __float_as_uint(y[i].x) & 0x7fffffffu);
+      if (finite_bits(y[i].y)) bits = max(bits, __float_as_uint(y[i].y) & 0x7fffffffu);
+    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (finite_bits(f[j])) top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int o = 8; o > 0; o >>= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, o));
   }
   if (oct >= a.octs) return;
-  const uint32_t byte = scale_byte(top);
+  const uint32_t byte = scale_byte(bits);
   const float inv = inverse_scale(byte);
+  float f[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = odd ? scaled<true>(f[j], inv) : f[j] * inv;
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = __fmul2_rn(y[i], make_float2(inv, inv));
+    f[2 * i] = !odd || finite_bits(y[i].x) ? v.x : __uint_as_float(0x7fffffffu);
+    f[2 * i + 1] = !odd || finite_bits(y[i].y) ? v.y : __uint_as_float(0x7fffffffu);
+  }
   put8(a.fp8.values + row * a.fp8.ld, oct * 8, a.cols, e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
   if ((oct & 15) == 0) put_scale(a.fp8.scales, a.rows, row, oct >> 4, (a.octs + 15) >> 4, byte);
 }
-// int8: the product is rounded once, then to a whole number by an addition whose last bit is one (1.5 * 2^23; |product| is 127 and a little at most)
-__device__ __forceinline__ uint32_t int8x4(float a, float b, float c, float d, float inv) {
-  const uint32_t i = __float_as_uint(__fadd_rn(__fmul_rn(a, inv), 12582912.f)), j = __float_as_uint(__fadd_rn(__fmul_rn(b, inv), 12582912.f)),
-                 k = __float_as_uint(__fadd_rn(__fmul_rn(c, inv), 12582912.f)), l = __float_as_uint(__fadd_rn(__fmul_rn(d, inv), 12582912.f));
-  return __byte_perm(__byte_perm(i, j, 0x0040), __byte_perm(k, l, 0x0040), 0x5410);
+// int8: the product is rounded once, then to a whole number by an addition whose last bit is one (1.5 * 2^23; |product| is 127 and a little at most).  (One at a time: the assembler makes
+// one operation of a packed product and a packed sum behind it, also of mul.rn and add.rn, which rounds once, and numbers half way between two come out on the other side.)
+__device__ __forceinline__ uint32_t int8_bits(float v, float factor) { return __float_as_uint(__fadd_rn(__fmul_rn(v, factor), 12582912.f)); }
+__device__ __forceinline__ uint32_t int8x4(float2 a, float2 b, float factor) {
+  return __byte_perm(__byte_perm(int8_bits(a.x, factor), int8_bits(a.y, factor), 0x0040), __byte_perm(int8_bits(b.x, factor), int8_bits(b.y, factor), 0x0040), 0x5410);
 }
-// top: bits of the row's max |v|.  A row that holds something that is not finite has no scale: zeros, and a scale that makes its products NaN
-__device__ __forceinline__ void put_int8(const float (&v)[8], uint32_t top, const Int8Arg& out, int row, int oct, int cols) {
-  const float inv = __fdiv_rn(127.f, fmaxf(__uint_as_float(top), kInt8Least));
-  const bool fine = top < kInf;
-  put8(reinterpret_cast<unsigned char*>(out.values) + row * out.ld, oct * 8, cols, fine ? int8x4(v[0], v[1], v[2], v[3], inv) : 0u,
-       fine ? int8x4(v[4], v[5], v[6], v[7], inv) : 0u);
+// What a row's max |v| stands for: what its values are multiplied by, and its scale.  A row that holds something that is not finite has no scale: zeros (times zero, plus a zero
+// in place of the value), and a scale that makes its products NaN
+__device__ __forceinline__ float int8_factor(float top) { return __fdiv_rn(127.f, fmaxf(top, kInt8Least)); }
+__device__ __forceinline__ float int8_scale(float top, float r) {
+  return __float_as_uint(top) < kInf ? __fdiv_rn(fmaxf(top, kInt8Least), 127.f) * r : __uint_as_float(0x7fffffffu);
 }
-__device__ __forceinline__ float int8_scale(uint32_t top, float r) {
-  return top < kInf ? __fdiv_rn(fmaxf(__uint_as_float(top), kInt8Least), 127.f) * r : __uint_as_float(0x7fffffffu);
+// A piece of a row in every form that is wanted: h (or x), its weights, 1 / sqrt, the row's max |v| and what it is multiplied by
+template <bool NORM, bool VEC, typename S>
+__device__ __forceinline__ void put_piece(const Eight<S>& h, const float2 (&w)[4], float r, float top, float factor, bool int8, const NormFwdArgs& a, int row, int oct) {
+  float2 v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = NORM ? __fmul2_rn(h.pair(i), w[i]) : h.pair(i);
+  if (int8 && oct < a.octs) {
+    const bool fine = __float_as_uint(top) < kInf;
+    put8(reinterpret_cast<unsigned char*>(a.int8.values) + row * a.int8.ld, oct * 8, a.cols, fine ? int8x4(v[0], v[1], factor) : 0u, fine ? int8x4(v[2], v[3], factor) : 0u);
+  }
+  if (!NORM) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __fmul2_rn(v[i], make_float2(r, r));
+  if (a.fp8.values != nullptr) put_fp8(v, a, row, oct);
+  if (a.y.p != nullptr) {
+    const float f[8] = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
+    if (a.y_f32) store_floats<VEC>(f, reinterpret_cast<float*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
+    else store_floats<VEC>(f, reinterpret_cast<bf16*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
+  }
+}
+// h of a piece: x through the dropout, plus the residual, rounded to the stream's type
+template <typename X, typename S>
+__device__ __forceinline__ void combine(Eight<S>& h, const Eight<X>& x, const Eight<S>& r, bool residual, const DropMask& mask, int row, int oct) {
+  float f[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = x.get(j);
+  mask.apply(f, row, oct);
+  if (residual) add_eight(f, r);
+  h.round(f);
 }
 
-// V: pieces of eight elements a thread (MANY: as many as it takes, in a loop); NORM: else the int8 form of x as it is
+// ---- rows on 16-byte boundaries: pieces on their way, each in 16-byte places `threads` apart that one thread writes and reads
+__device__ __forceinline__ void ask(uint32_t to, const void* from, bool there) {      // (not there: zeros)
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void ask_eight(uint32_t to, uint32_t apart, const T* row, int oct, bool there) {
+  const T* from = row + (there ? oct * 8 : 0);
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) ask(to + i * apart, reinterpret_cast<const char*>(from) + 16 * i, there);
+}
+__device__ __forceinline__ void asked() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void take(Eight<bf16>& e, const unsigned char* from, uint32_t) {
+  const uint4 v = *reinterpret_cast<const uint4*>(from);
+  e.u[0] = v.x; e.u[1] = v.y; e.u[2] = v.z; e.u[3] = v.w;
+}
+__device__ __forceinline__ void take(Eight<float>& e, const unsigned char* from, uint32_t apart) {
+  const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + apart);
+  e.f[0] = a.x; e.f[1] = a.y; e.f[2] = a.z; e.f[3] = a.w; e.f[4] = b.x; e.f[5] = b.y; e.f[6] = b.z; e.f[7] = b.w;
+}
+
+template <int V, typename X, typename S, bool NORM, bool INT8>
+__global__ void __launch_bounds__(kNormMost, 2) norm_fwd_ring_kernel(const __grid_constant__ NormFwdArgs a) {
+  extern __shared__ __align__(16) unsigned char ring[];
+  __shared__ RowSums sh;
+  constexpr int XP = sizeof(X) / 2, SP = sizeof(S) / 2;      // 16-byte places of a piece
+  grid_enter();
+  const int t = threadIdx.x, T = blockDim.x;
+  const uint32_t apart = T * 16, slot = V * (XP + SP) * apart;
+  unsigned char* const mine = ring + t * 16;
+  const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine);
+  const bool residual = a.r.p != nullptr;
+  auto ask_row = [&](int row, int s) {
+    if (row < a.rows) {
+      const X* xp = reinterpret_cast<const X*>(a.x.p) + row * a.x.ld;
+      const S* rp = reinterpret_cast<const S*>(a.r.p) + row * a.r.ld;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int oct = v * T + t;
+        ask_eight(to + s * slot + v * XP * apart, apart, xp, oct, oct < a.octs);
+        if (residual) ask_eight(to + s * slot + (V * XP + v * SP) * apart, apart, rp, oct, oct < a.octs);
+      }
+    }
+    asked();
+  };
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s) ask_row(blockIdx.x + s * gridDim.x, s);
+  DropMask mask;
+  mask.init(a.drop);
+  float2 w[V][4];
+  if (NORM) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) weight_of<true>(w[v], a.w, (v * T + t) * 8, a.cols);
+  }
+  uint32_t turn = 0;
+  int s = 0;
+  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    // (the place behind the others is free: this thread has read it, and only it does)
+    ask_row(row + kAhead * gridDim.x, s == 0 ? kAhead : s - 1);
+    arrived<kAhead>();
+    Eight<S> h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const unsigned char* from = mine + s * slot;
+      Eight<X> x;
+      Eight<S> r;
+      take(x, from + v * XP * apart, apart);
+      if (residual) take(r, from + (V * XP + v * SP) * apart, apart);
+      combine(h[v], x, r, residual, mask, row, v * T + t);
+    }
+    s = s == kAhead ? 0 : s + 1;
+    if (NORM && a.h.p != nullptr) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) store_eight<true>(h[v], reinterpret_cast<S*>(a.h.p) + row * a.h.ld, (v * T + t) * 8, a.cols);
+    }
+    float r = 1.f, top = 0.f, eps = a.eps;
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+      float2 ss = make_float2(0.f, 0.f);
+      top = 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) add_sums<NORM, INT8>(h[v], w[v], ss, top);
+      const float2 of = row_total<true>(ss.x + ss.y, top, sh, turn++);
+      top = of.y;
+      if constexpr (NORM) {
+        const float ms = of.x * a.inv_cols + eps;
+        r = rsqrtf(ms);
+        if (in_range(ms) || again) break;
+        float size = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) size = largest_of(h[v], size);
+        const float power = power_for(__float_as_uint(row_total<true>(0.f, size, sh, turn++).y), eps);
+#pragma unroll
+        for (int v = 0; v < V; ++v) rescale(h[v], power);
+        eps = eps * power * power;
+      } else {
+        break;
+      }
+    }
+    const float factor = INT8 ? int8_factor(top) : 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) put_piece<NORM, true>(h[v], w[v], r, top, factor, INT8, a, row, v * T + t);
+    if (INT8 && t == 0) a.int8.scales[row] = int8_scale(top, r);
+  }
+  arrived<0>();
+}
+
+// Any rows.  V: pieces of eight elements a thread (MANY: as many as it takes, in a loop); NORM: else the int8 form of x as it is
 template <int V, bool MANY, typename X, typename S, bool NORM, bool VEC>
-__global__ void __launch_bounds__(kNormMost) norm_fwd_kernel(const __grid_constant__ NormFwdArgs a) {
+__global__ void __launch_bounds__(kNormMost, 1) norm_fwd_kernel(const __grid_constant__ NormFwdArgs a) {
   __shared__ RowSums sh;
   grid_enter();
   const int t = threadIdx.x, T = blockDim.x;
   DropMask mask;
   mask.init(a.drop);
   const int rounds = MANY ? (a.octs + T * V - 1) / (T * V) : 1;
-  const bool want_int8 = a.int8.values != nullptr;
+  const bool int8 = a.int8.values != nullptr;
   uint32_t turn = 0;
   for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const X* const xp = reinterpret_cast<const X*>(a.x.p) + row * a.x.ld;
-    const S* const rp = a.r.p != nullptr ? reinterpret_cast<const S*>(a.r.p) + row * a.r.ld : nullptr;
+    const S* const rp = reinterpret_cast<const S*>(a.r.p) + row * a.r.ld;
     Eight<S> h[V];
+    float power = 1.f;
     auto fetch = [&](int first) {      // h of the pieces first + t, first + t + T, ..
       Eight<X> x[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) load_eight<VEC>(x[v], xp, (first + v * T + t) * 8, a.cols);
-      if (rp != nullptr) {
+      if (a.r.p != nullptr) {
 #pragma unroll
         for (int v = 0; v < V; ++v) load_eight<VEC>(h[v], rp, (first + v * T + t) * 8, a.cols);
       }
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float f[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = x[v].get(j);
-        mask.apply(f, row, first + v * T + t);
-        if (rp != nullptr) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = __fadd_rn(h[v].get(j), f[j]);
-        }
-        h[v].round(f);
-      }
+      for (int v = 0; v < V; ++v) combine(h[v], x[v], h[v], a.r.p != nullptr, mask, row, first + v * T + t);
     };
     auto keep = [&](int first) {
-      if (a.h.p == nullptr) return;
+      if (!NORM || a.h.p == nullptr) return;
 #pragma unroll
       for (int v = 0; v < V; ++v) store_eight<VEC>(h[v], reinterpret_cast<S*>(a.h.p) + row * a.h.ld, (first + v * T + t) * 8, a.cols);
     };
-    // sum of squares and the largest |h w|, of h times s; `largest`: of |h|
-    auto sums = [&](int first, float s, bool weighted, float& ss, uint32_t& top) {
+    auto apply_power = [&] {
+      if (power == 1.f) return;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float w[8];
-        if (NORM && weighted && want_int8) weight_of<VEC>(w, a.w, (first + v * T + t) * 8, a.cols);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float f = h[v].get(j) * s;
-          if (NORM) ss += f * f;
-          if (!weighted || want_int8) top = max(top, __float_as_uint(NORM && weighted ? __fmul_rn(f, w[j]) : f) & 0x7fffffffu);
-        }
-      }
-    };
-    auto total = [&](float s, bool weighted) {
-      float ss = 0.f;
-      uint32_t top = 0;
-      for (int i = 0; i < rounds; ++i) {
-        if (MANY) fetch(i * T * V);
-        sums(i * T * V, s, weighted, ss, top);
-      }
-      return row_total<true>(ss, __uint_as_float(top), sh, turn++);
+      for (int v = 0; v < V; ++v) rescale(h[v], power);
     };
     if (!MANY) {
       fetch(0);
       keep(0);
     }
-    float2 of = total(1.f, true);
-    float r = 1.f, s = 1.f;
-    if (NORM) {
-      float ms = of.x * a.inv_cols + a.eps;
-      if (!in_range(ms)) {
-        s = power_for(__float_as_uint(total(1.f, false).y), a.eps);
-        of = total(s, true);
-        ms = of.x * a.inv_cols + a.eps * s * s;
+    float r = 1.f, top = 0.f, eps = a.eps;
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+      float2 ss = make_float2(0.f, 0.f);
+      float size = 0.f;
+      top = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < rounds; ++i) {
+        const int first = i * T * V;
+        if (MANY) {
+          fetch(first);
+          apply_power();
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          float2 w[4];
+          if (NORM) weight_of<VEC>(w, a.w, (first + v * T + t) * 8, a.cols);
+          if (int8) add_sums<NORM, true>(h[v], w, ss, top);
+          else add_sums<NORM, false>(h[v], w, ss, top);
+          if (NORM) size = largest_of(h[v], size);
+        }
       }
-      r = rsqrtf(ms);
+      const float2 of = row_total<true>(ss.x + ss.y, top, sh, turn++);
+      top = of.y;
+      if constexpr (NORM) {
+        const float ms = of.x * a.inv_cols + eps;
+        r = rsqrtf(ms);
+        if (in_range(ms) || again) break;
+        power = power_for(__float_as_uint(row_total<true>(0.f, size, sh, turn++).y), eps);
+        if (!MANY) apply_power();
+        eps = eps * power * power;
+      } else {
+        break;
+      }
     }
-    const uint32_t top = __float_as_uint(of.y);
+    const float factor = int8 ? int8_factor(top) : 0.f;
+#pragma unroll 1
     for (int i = 0; i < rounds; ++i) {
       const int first = i * T * V;
       if (MANY) {
         fetch(first);
         keep(first);
+        apply_power();
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int oct = first + v * T + t;
-        float f[8], w[8];
-        if (NORM) weight_of<VEC>(w, a.w, oct * 8, a.cols);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = NORM ? __fmul_rn(h[v].get(j) * s, w[j]) : h[v].get(j);
-        if (NORM && a.fp8.values != nullptr) put_fp8(f, r, a, row, oct);
-        if (want_int8 && oct < a.octs) put_int8(f, top, a.int8, row, oct, a.cols);
-        if (NORM && a.y.p != nullptr) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] *= r;
-          if (a.y_f32) store_floats<VEC>(f, reinterpret_cast<float*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
-          else store_floats<VEC>(f, reinterpret_cast<bf16*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
-        }
+        float2 w[4];
+        if (NORM) weight_of<VEC>(w, a.w, (first + v * T + t) * 8, a.cols);
+        put_piece<NORM, VEC>(h[v], w, r, top, factor, int8, a, row, first + v * T + t);
       }
     }
-    if (want_int8 && t == 0) a.int8.scales[row] = int8_scale(top, r);
+    if (int8 && t == 0) a.int8.scales[row] = int8_scale(top, r);
   }
 }
 
@@ -262,13 +433,13 @@ __global__ void __launch_bounds__(kNormMost) norm_bwd_kernel(const __grid_consta
         if (MANY) fetch(i * T * V, false);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          float w[8];
+          float2 w[4];
           weight_of<VEC>(w, a.w, (i * T * V + v * T + t) * 8, a.cols);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const float f = h[v].get(j) * s;
             ss += f * f;
-            dot += dy[v].get(j) * w[j] * f;
+            dot += dy[v].get(j) * (j & 1 ? w[j / 2].y : w[j / 2].x) * f;
           }
         }
       }
@@ -278,15 +449,13 @@ __global__ void __launch_bounds__(kNormMost) norm_bwd_kernel(const __grid_consta
     float2 of = total(1.f);
     float s = 1.f, ms = of.x * a.inv_cols + a.eps;
     if (!in_range(ms)) {
-      uint32_t top = 0;
+      float top = 0.f;
       for (int i = 0; i < rounds; ++i) {
         if (MANY) fetch(i * T * V, false);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(h[v].get(j)) & 0x7fffffffu);
+        for (int v = 0; v < V; ++v) top = largest_of(h[v], top);
       }
-      s = power_for(__float_as_uint(row_total<true>(0.f, __uint_as_float(top), sh, turn++).y), a.eps);
+      s = power_for(__float_as_uint(row_total<true>(0.f, top, sh, turn++).y), a.eps);
       of = total(s);
       ms = of.x * a.inv_cols + a.eps * s * s;
     }
@@ -298,12 +467,13 @@ __global__ void __launch_bounds__(kNormMost) norm_bwd_kernel(const __grid_consta
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int oct = first + v * T + t;
-        float f[8], w[8];
+        float f[8];
+        float2 w[4];
         weight_of<VEC>(w, a.w, oct * 8, a.cols);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float hat = h[v].get(j) * s * r, g = dy[v].get(j);
-          f[j] = out * (g * w[j] - hat * along);
+          f[j] = out * (g * (j & 1 ? w[j / 2].y : w[j / 2].x) - hat * along);
           if (a.dh.p != nullptr) f[j] += dh[v].get(j);
           dw[v][j] += g * hat;
         }
@@ -359,17 +529,19 @@ __global__ void __launch_bounds__(256) norm_weight_kernel(const float* parts, in
   }
 }
 
-// CTAs of a kernel that an SM holds, asked once for each number of warps, device and context
+// CTAs of a kernel that the device holds, asked once for each number of warps and device (with the same shared memory each time); it is allowed its shared memory first
 struct Residents {
+  KernelAttr attr;
   std::atomic<int> known[kMaxDevices][kNormMost / 32 + 1] = {};
 };
-cudaError_t resident_ctas(const void* kernel, Residents& r, int threads, int* ctas) {
+cudaError_t resident_ctas(const void* kernel, Residents& r, int threads, size_t smem, int* ctas) {
   int dev = 0, sms = 0, n = 0;
   cudaError_t e;
   if ((e = cudaGetDevice(&dev)) != cudaSuccess || (e = sm_count(&sms)) != cudaSuccess) return e;
+  if (smem > 0 && (e = prepare_kernel(kernel, r.attr, smem)) != cudaSuccess) return e;
   if (dev < kMaxDevices) n = r.known[dev][threads / 32].load(std::memory_order_relaxed);
   if (n == 0) {
-    if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0)) != cudaSuccess) return e;
+    if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem)) != cudaSuccess) return e;
     if (n < 1) n = 1;
     if (dev < kMaxDevices) r.known[dev][threads / 32].store(n, std::memory_order_relaxed);
   }
@@ -383,21 +555,33 @@ int threads_for(int octs, int v) {
   return t < 32 ? 32 : t > kNormMost ? kNormMost : t;
 }
 
+template <int V, typename X, typename S, bool NORM, bool INT8>
+cudaError_t go_fwd_ring(const NormFwdArgs& a, cudaStream_t st) {
+  static Residents residents;
+  const int threads = threads_for(a.octs, V);
+  const size_t smem = (size_t)(kAhead + 1) * V * threads * 8 * (sizeof(X) + sizeof(S));
+  int ctas = 0;
+  const cudaError_t e = resident_ctas((const void*)norm_fwd_ring_kernel<V, X, S, NORM, INT8>, residents, threads, smem, &ctas);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(norm_fwd_ring_kernel<V, X, S, NORM, INT8>, a.rows < ctas ? a.rows : ctas, threads, smem, st, a);
+}
 template <int V, bool MANY, typename X, typename S, bool NORM, bool VEC>
 cudaError_t go_fwd(const NormFwdArgs& a, cudaStream_t st) {
   static Residents residents;
   const int threads = threads_for(a.octs, V);
   int ctas = 0;
-  const cudaError_t e = resident_ctas((const void*)norm_fwd_kernel<V, MANY, X, S, NORM, VEC>, residents, threads, &ctas);
+  const cudaError_t e = resident_ctas((const void*)norm_fwd_kernel<V, MANY, X, S, NORM, VEC>, residents, threads, 0, &ctas);
   if (e != cudaSuccess) return e;
   return launch_kernel(norm_fwd_kernel<V, MANY, X, S, NORM, VEC>, a.rows < ctas ? a.rows : ctas, threads, 0, st, a);
 }
-template <typename X, typename S, bool NORM, bool VEC>
-cudaError_t size_fwd(const NormFwdArgs& a, cudaStream_t st) {
-  if (a.octs <= 128) return go_fwd<1, false, X, S, NORM, VEC>(a, st);
-  if (a.octs <= 512) return go_fwd<2, false, X, S, NORM, VEC>(a, st);
-  if (a.octs <= 4 * kNormMost) return go_fwd<4, false, X, S, NORM, VEC>(a, st);
-  return go_fwd<2, true, X, S, NORM, VEC>(a, st);
+template <typename X, typename S, bool NORM>
+cudaError_t size_fwd(const NormFwdArgs& a, bool vec, cudaStream_t st) {
+  const bool many = a.cols > 2 * 8 * kNormMost;
+  if (!vec) return many ? go_fwd<2, true, X, S, NORM, false>(a, st) : go_fwd<2, false, X, S, NORM, false>(a, st);
+  if (a.cols > kRingCols) return go_fwd<2, true, X, S, NORM, true>(a, st);
+  if (!NORM) return a.octs <= 128 ? go_fwd_ring<1, X, S, NORM, true>(a, st) : go_fwd_ring<2, X, S, NORM, true>(a, st);
+  if (a.int8.values != nullptr) return a.octs <= 128 ? go_fwd_ring<1, X, S, true, true>(a, st) : go_fwd_ring<2, X, S, true, true>(a, st);
+  return a.octs <= 128 ? go_fwd_ring<1, X, S, true, false>(a, st) : go_fwd_ring<2, X, S, true, false>(a, st);
 }
 
 template <int V, bool MANY, typename S, typename G, bool VEC>
@@ -405,7 +589,7 @@ cudaError_t go_bwd(const NormBwdArgs& a, float* dw, cudaStream_t st) {
   static Residents residents;
   const int threads = threads_for(a.octs, V);
   int ctas = 0;
-  cudaError_t e = resident_ctas((const void*)norm_bwd_kernel<V, MANY, S, G, VEC>, residents, threads, &ctas);
+  cudaError_t e = resident_ctas((const void*)norm_bwd_kernel<V, MANY, S, G, VEC>, residents, threads, 0, &ctas);
   if (e != cudaSuccess) return e;
   if (ctas > kNormParts) ctas = kNormParts;
   if (ctas > a.rows) ctas = a.rows;
@@ -425,11 +609,10 @@ cudaError_t launch_norm_fwd(NormFwdArgs a, bool x_f32, bool h_f32, cudaStream_t 
   a.octs = (a.cols + 7) / 8;
   a.inv_cols = 1.f / a.cols;
   const size_t size = h_f32 ? 4 : 2;
-  const bool vec = rows_aligned(a.x, x_f32 ? 4 : 2) && rows_aligned(a.r, size) && rows_aligned(a.h, size) && rows_aligned(a.y, a.y_f32 ? 4 : 2) &&
-                   (reinterpret_cast<uintptr_t>(a.w) & 15u) == 0;
-  auto go = [&](auto aligned, auto any) { return vec ? aligned(a, st) : any(a, st); };
-  if (x_f32) return h_f32 ? go(size_fwd<float, float, true, true>, size_fwd<float, float, true, false>) : go(size_fwd<float, bf16, true, true>, size_fwd<float, bf16, true, false>);
-  return h_f32 ? go(size_fwd<bf16, float, true, true>, size_fwd<bf16, float, true, false>) : go(size_fwd<bf16, bf16, true, true>, size_fwd<bf16, bf16, true, false>);
+  const bool vec = a.cols % 8 == 0 && rows_aligned(a.x, x_f32 ? 4 : 2) && rows_aligned(a.r, size) && rows_aligned(a.h, size) &&
+                   rows_aligned(a.y, a.y_f32 ? 4 : 2) && (reinterpret_cast<uintptr_t>(a.w) & 15u) == 0;
+  if (x_f32) return h_f32 ? size_fwd<float, float, true>(a, vec, st) : size_fwd<float, bf16, true>(a, vec, st);
+  return h_f32 ? size_fwd<bf16, float, true>(a, vec, st) : size_fwd<bf16, bf16, true>(a, vec, st);
 }
 
 cudaError_t launch_int8_quantize(const RowsArg& x, bool x_f32, int rows, int cols, const Int8Arg& out, cudaStream_t st) {
@@ -438,9 +621,8 @@ cudaError_t launch_int8_quantize(const RowsArg& x, bool x_f32, int rows, int col
   a.int8 = out;
   a.rows = rows; a.cols = cols;
   a.octs = (cols + 7) / 8;
-  const bool vec = rows_aligned(x, x_f32 ? 4 : 2);
-  if (x_f32) return vec ? size_fwd<float, float, false, true>(a, st) : size_fwd<float, float, false, false>(a, st);
-  return vec ? size_fwd<bf16, bf16, false, true>(a, st) : size_fwd<bf16, bf16, false, false>(a, st);
+  const bool vec = cols % 8 == 0 && rows_aligned(x, x_f32 ? 4 : 2);
+  return x_f32 ? size_fwd<float, float, false>(a, vec, st) : size_fwd<bf16, bf16, false>(a, vec, st);
 }
 
 // a row of sums for each CTA
@@ -453,7 +635,7 @@ cudaError_t launch_norm_bwd(NormBwdArgs a, bool h_f32, bool dy_f32, float* dw, f
   a.inv_cols = 1.f / a.cols;
   a.parts = dw != nullptr ? parts : nullptr;
   const size_t size = h_f32 ? 4 : 2;
-  const bool vec = rows_aligned(a.h, size) && rows_aligned(a.dy, dy_f32 ? 4 : 2) && rows_aligned(a.dh, size) && rows_aligned(a.dr, size) &&
+  const bool vec = a.cols % 8 == 0 && rows_aligned(a.h, size) && rows_aligned(a.dy, dy_f32 ? 4 : 2) && rows_aligned(a.dh, size) && rows_aligned(a.dr, size) &&
                    rows_aligned(a.dx, a.dx_f32 ? 4 : 2) && (reinterpret_cast<uintptr_t>(a.w) & 15u) == 0;
   auto go = [&](auto aligned, auto any) { return vec ? aligned(a, dw, st) : any(a, dw, st); };
   if (h_f32) return dy_f32 ? go(size_bwd<float, float, true>, size_bwd<float, float, false>) : go(size_bwd<float, bf16, true>, size_bwd<float, bf16, false>);

@@ -44,6 +44,7 @@ struct DropoutArgs {
   RowsArg x, r, y;
   int rows, cols, octs;
   Divisor by_octs;
+  unsigned long long per_octs;      // 2^64 / octs, rounded up
   DropArg drop;
 };
 cudaError_t launch_norm_fwd(NormFwdArgs a, bool x_f32, bool h_f32, cudaStream_t st);
@@ -73,6 +74,7 @@ template <> struct Eight<bf16> {
   }
   __device__ __forceinline__ void set(int j, const bf16* p) { u[j / 2] |= (uint32_t)*reinterpret_cast<const unsigned short*>(p) << 16 * (j & 1); }
   __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? u[j / 2] & 0xffff0000u : u[j / 2] << 16); }
+  __device__ __forceinline__ float2 pair(int i) const { return make_float2(get(2 * i), get(2 * i + 1)); }
   __device__ __forceinline__ void round(const float (&f)[8]) {      // to the type
 #pragma unroll
     for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
@@ -92,6 +94,7 @@ template <> struct Eight<float> {
   }
   __device__ __forceinline__ void set(int j, const float* p) { f[j] = *p; }
   __device__ __forceinline__ float get(int j) const { return f[j]; }
+  __device__ __forceinline__ float2 pair(int i) const { return make_float2(f[2 * i], f[2 * i + 1]); }
   __device__ __forceinline__ void round(const float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = v[j];
@@ -102,11 +105,12 @@ template <> struct Eight<float> {
   }
   __device__ __forceinline__ void store(float* p, int j) const { *p = f[j]; }
 };
-// Elements i .. i+7 of a row (zeros behind it, and for i beyond it); VEC: rows begin on 16-byte boundaries
+// Elements i .. i+7 of a row (zeros behind it, and for i beyond it); VEC: rows begin on 16-byte boundaries and are whole pieces of eight
 template <bool VEC, typename T>
 __device__ __forceinline__ void load_eight(Eight<T>& e, const T* row, int i, int cols) {
-  if (VEC && i + 8 <= cols) {
-    e.load(row + i);
+  if (VEC) {
+    if (i < cols) e.load(row + i);
+    else e.zero();
   } else {
     e.zero();
 #pragma unroll
@@ -116,8 +120,8 @@ __device__ __forceinline__ void load_eight(Eight<T>& e, const T* row, int i, int
 }
 template <bool VEC, typename T>
 __device__ __forceinline__ void store_eight(const Eight<T>& e, T* row, int i, int cols) {
-  if (VEC && i + 8 <= cols) {
-    e.store(row + i);
+  if (VEC) {
+    if (i < cols) e.store(row + i);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -129,6 +133,17 @@ __device__ __forceinline__ void store_floats(const float (&f)[8], T* row, int i,
   Eight<T> e;
   e.round(f);
   store_eight<VEC>(e, row, i, cols);
+}
+
+// f plus e, each sum rounded
+template <typename T>
+__device__ __forceinline__ void add_eight(float (&f)[8], const Eight<T>& e) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = __fadd2_rn(e.pair(i), make_float2(f[2 * i], f[2 * i + 1]));
+    f[2 * i] = v.x;
+    f[2 * i + 1] = v.y;
+  }
 }
 
 // Which elements are kept.  The counter-based generator Philox 4x32 with ten rounds (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): its
@@ -161,9 +176,10 @@ struct DropMask {
     }
     const uint32_t w[4] = {a, b, c, d};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t bits = j & 1 ? w[j / 2] : w[j / 2] << 16;      // (of the odd ones the lower half decides nothing)
-      f[j] = bits >= limit ? __fmul_rn(f[j], scale) : 0.f;
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = __fmul2_rn(make_float2(f[2 * i], f[2 * i + 1]), make_float2(scale, scale));
+      f[2 * i] = w[i] << 16 >= limit ? v.x : 0.f;
+      f[2 * i + 1] = w[i] >= limit ? v.y : 0.f;      // (the lower half decides nothing)
     }
   }
 };
