@@ -9,7 +9,7 @@ namespace {
 constexpr int kDropThreads = 256;
 constexpr int kDropOcts = 4;      // pieces of eight elements a thread, all asked for before the first is used
 
-template <typename X, typename Y, bool VEC>
+template <typename X, typename Y, int LIE>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const __grid_constant__ DropoutArgs a) {
   grid_enter();
   DropMask mask;
@@ -26,13 +26,13 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const __grid_cons
     const int at = skip + u * kDropThreads, down = divided(at, a.by_octs);
     row[u] = (int)min((long long)a.rows, row0 + down);
     oct[u] = at - down * a.octs;
-    if (row[u] < a.rows) load_eight<VEC>(x[u], reinterpret_cast<const X*>(a.x.p) + row[u] * a.x.ld, oct[u] * 8, a.cols);
+    if (row[u] < a.rows) load_eight<LIE>(x[u], reinterpret_cast<const X*>(a.x.p) + row[u] * a.x.ld, oct[u] * 8, a.cols);
     else x[u].zero();
   }
   if (a.r.p != nullptr) {
 #pragma unroll
     for (int u = 0; u < kDropOcts; ++u) {
-      if (row[u] < a.rows) load_eight<VEC>(r[u], reinterpret_cast<const Y*>(a.r.p) + row[u] * a.r.ld, oct[u] * 8, a.cols);
+      if (row[u] < a.rows) load_eight<LIE>(r[u], reinterpret_cast<const Y*>(a.r.p) + row[u] * a.r.ld, oct[u] * 8, a.cols);
       else r[u].zero();
     }
   }
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const __grid_cons
     for (int j = 0; j < 8; ++j) f[j] = x[u].get(j);
     mask.apply(f, row[u], oct[u]);
     if (a.r.p != nullptr) add_eight(f, r[u]);
-    if (row[u] < a.rows) store_floats<VEC>(f, reinterpret_cast<Y*>(a.y.p) + row[u] * a.y.ld, oct[u] * 8, a.cols);
+    if (row[u] < a.rows) store_floats<LIE>(f, reinterpret_cast<Y*>(a.y.p) + row[u] * a.y.ld, oct[u] * 8, a.cols);
   }
 }
 
@@ -58,8 +58,8 @@ cudaError_t launch_dropout(DropoutArgs a, bool x_f32, bool y_f32, cudaStream_t s
   const size_t size = y_f32 ? 4 : 2;
   const bool vec = a.cols % 8 == 0 && rows_aligned(a.x, x_f32 ? 4 : 2) && rows_aligned(a.r, size) && rows_aligned(a.y, size);
   auto go = [&](auto aligned, auto any) { return launch_kernel(vec ? aligned : any, grid, kDropThreads, 0, st, a); };
-  if (x_f32) return y_f32 ? go(dropout_kernel<float, float, true>, dropout_kernel<float, float, false>) : go(dropout_kernel<float, bf16, true>, dropout_kernel<float, bf16, false>);
-  return y_f32 ? go(dropout_kernel<bf16, float, true>, dropout_kernel<bf16, float, false>) : go(dropout_kernel<bf16, bf16, true>, dropout_kernel<bf16, bf16, false>);
+  if (x_f32) return y_f32 ? go(dropout_kernel<float, float, ROWS_ALIGNED>, dropout_kernel<float, float, ROWS_ANY>) : go(dropout_kernel<float, bf16, ROWS_ALIGNED>, dropout_kernel<float, bf16, ROWS_ANY>);
+  return y_f32 ? go(dropout_kernel<bf16, float, ROWS_ALIGNED>, dropout_kernel<bf16, float, ROWS_ANY>) : go(dropout_kernel<bf16, bf16, ROWS_ALIGNED>, dropout_kernel<bf16, bf16, ROWS_ANY>);
 }
 
 }  // namespace vsa2

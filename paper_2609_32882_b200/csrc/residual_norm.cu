@@ -4,9 +4,9 @@
 //   backward: with r = 1 / sqrt(mean(h^2) + eps), g = w dy:  dh' = dh + r g - h r^3 mean(g h);  dx = dropout's part of dh';  dw = sum over the rows of dy h r
 //   int8    : v = h w (for vsa2_int8_quantize a matrix' own values), s = max |v| / 127, value = v * (127 / max |v|) rounded to nearest, ties to even; the row's r is part of its
 //             scale alone, so a value does not depend on how the sum of squares was rounded
-// A CTA takes a row at a time, eight neighbouring elements in each of a thread's pieces.  Rows on 16-byte boundaries of up to 8192 elements (the ring kernels): each thread asks for its own
-// pieces of the next rows ahead of time, in places of shared memory that are its own, so that memory is kept busy while a row's sums pass through the CTA's one barrier.
-// Other rows come as they are needed: of up to 8192 elements they stay in registers, longer ones (MANY) are read twice, the second time from L2.  Bound by memory.
+// A CTA takes a row at a time, eight neighbouring elements in each of a thread's pieces.  Rows on 16-byte boundaries whose pieces fit shared memory (the ring kernels): each thread asks
+// for its own pieces of the next row ahead of time, in places that are its own, so that memory is kept busy while a row's sums pass through the CTA's one barrier.  Other rows come as
+// they are needed: of up to 8192 elements they stay in registers, longer ones (MANY) are read twice, the second time from L2.  Bound by memory and, close behind, by issue slots.
 #include "fp8_values.cuh"
 #include "rows.cuh"
 
@@ -16,8 +16,6 @@ namespace {
 
 constexpr int kNormMost = 512;       // threads of a CTA at most
 constexpr int kNormParts = 1184;     // most CTAs of the backward, each with its own partial sums of the weight's gradient (eight for each of 148 SMs)
-constexpr int kAhead = 2;            // rows that a thread of the ring kernels has asked for beyond the one it works on
-constexpr int kRingCols = 8192;      // their longest rows
 constexpr float kInt8Least = 0x1p-100f;      // least max |v|: below it 127 / max |v| would leave fp32's range
 
 // Rows whose mean square lies outside are taken again times a power of two: their squares could vanish or pass fp32's range
@@ -29,8 +27,12 @@ __device__ __forceinline__ float power_for(uint32_t top_bits, float eps) {
   return e == 0 || e == 255 ? (e == 0 && top_bits != 0 ? 0x1p126f : 1.f) : __int_as_float(max(254 - e, 1) << 23);
 }
 
-struct RowSums {      // double-buffered by the row's parity: one barrier a row
-  float2 of[2][kNormMost / 32];
+struct RowSums {      // double-buffered by the row's parity: one barrier a row.  Zeros behind the CTA's warps
+  float sum[2][kNormMost / 32], other[2][kNormMost / 32];
+  __device__ __forceinline__ void init() {
+    if (threadIdx.x < 32) sum[threadIdx.x >> 4][threadIdx.x & 15] = other[threadIdx.x >> 4][threadIdx.x & 15] = 0.f;
+    __syncthreads();
+  }
 };
 // the larger magnitude; NaN where one is
 __device__ __forceinline__ float larger(float top, float a, float b) {
@@ -43,45 +45,63 @@ __device__ __forceinline__ float warp_largest(float v) {
   asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
-// Sum of `sum` and of `other` (MAX: the largest magnitude) over the CTA, the same bits in every thread
-template <bool MAX>
+// Over the CTA, the same bits in every thread: the sum of `sum`, where it is wanted (SUM), and of `other` the largest magnitude (MAX: 1), the sum (2) or nothing (0)
+template <bool SUM, int MAX>
 __device__ __forceinline__ float2 row_total(float sum, float other, RowSums& sh, uint32_t parity) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  parity &= 1;
+  if constexpr (SUM && MAX == 2) {
+    // (the lower half of the warp goes on with one sum, the upper half with the other)
+    const bool upper = lane & 16;
+    float mine = upper ? other : sum;
+    mine += __shfl_xor_sync(0xffffffffu, upper ? sum : other, 16);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (!MAX) other += __shfl_xor_sync(0xffffffffu, other, o);
+    for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (warps == 1) return make_float2(__shfl_sync(0xffffffffu, mine, 0), __shfl_sync(0xffffffffu, mine, 16));
+    if ((lane & 15) == 0) (upper ? sh.other : sh.sum)[parity][warp] = mine;
+  } else {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      if (SUM) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (MAX == 1) other = warp_largest(other);
+    if (warps == 1) return make_float2(sum, other);
+    if (lane == 0) {
+      if (SUM) sh.sum[parity][warp] = sum;
+      if (MAX) sh.other[parity][warp] = other;
+    }
   }
-  if (MAX) other = warp_largest(other);
-  if (warps == 1) return make_float2(sum, other);
-  float2* of = sh.of[parity & 1];
-  if (lane == 0) of[warp] = make_float2(sum, other);
   __syncthreads();
-  const float2 v = lane < warps ? of[lane] : make_float2(0.f, 0.f);
-  sum = v.x;
-  other = v.y;
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) {      // (16 warps at most)
-    sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (!MAX) other += __shfl_xor_sync(0xffffffffu, other, o);
+  sum = other = 0.f;
+#pragma unroll 1
+  for (int i = 0; i < warps; i += 4) {
+    if (SUM) {
+      const float4 v = *reinterpret_cast<const float4*>(&sh.sum[parity][i]);
+      sum += (v.x + v.y) + (v.z + v.w);
+    }
+    if (MAX) {
+      const float4 v = *reinterpret_cast<const float4*>(&sh.other[parity][i]);
+      if (MAX == 1) other = larger(larger(other, v.x, v.y), v.z, v.w);
+      else other += (v.x + v.y) + (v.z + v.w);
+    }
   }
-  sum = __shfl_sync(0xffffffffu, sum, 0);
-  if (MAX) other = warp_largest(other);
-  else other = __shfl_sync(0xffffffffu, other, 0);
   return make_float2(sum, other);
 }
 
-// Weights of elements i .. i+7 (null: ones), zeros behind the row.  VEC: whole pieces on 16-byte boundaries
-template <bool VEC>
+// Weights of elements i .. i+7 (null: ones); any behind the row, where all else is zero
+__device__ __forceinline__ void weights_at(float2 (&w)[4], const float* p) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  w[0] = make_float2(a.x, a.y); w[1] = make_float2(a.z, a.w);
+  w[2] = make_float2(b.x, b.y); w[3] = make_float2(b.z, b.w);
+}
+__device__ const float kOnes[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+template <int LIE>
 __device__ __forceinline__ void weight_of(float2 (&w)[4], const float* from, int i, int cols) {
-  if (VEC && from != nullptr && i < cols) {
-    const float4 a = reinterpret_cast<const float4*>(from + i)[0], b = reinterpret_cast<const float4*>(from + i)[1];
-    w[0] = make_float2(a.x, a.y); w[1] = make_float2(a.z, a.w);
-    w[2] = make_float2(b.x, b.y); w[3] = make_float2(b.z, b.w);
+  if (LIE != ROWS_ANY) {
+    weights_at(w, element(from != nullptr ? from : kOnes, from != nullptr && (LIE == ROWS_WHOLE || i < cols) ? i : 0));
   } else {
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = from == nullptr ? 1.f : !VEC && i + j < cols ? from[i + j] : 0.f;
+    for (int j = 0; j < 8; ++j) v[j] = from != nullptr && i + j < cols ? from[i + j] : 1.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = make_float2(v[2 * j], v[2 * j + 1]);
   }
@@ -113,42 +133,73 @@ __device__ __forceinline__ void add_sums(const Eight<S>& h, const float2 (&w)[4]
     }
   }
 }
+// .. and, backward, the sum of the weighted gradient along h
+template <typename S, typename G>
+__device__ __forceinline__ void add_dots(const Eight<S>& h, const Eight<G>& dy, const float2 (&w)[4], float2& ss, float2& dot) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 p = h.pair(i);
+    ss = __ffma2_rn(p, p, ss);
+    dot = __ffma2_rn(__fmul2_rn(dy.pair(i), w[i]), p, dot);
+  }
+}
+// A piece's gradient: out (w dy - hat along) (+ dh) with hat = h r, and out = r but for a row that was taken times a power of two; the weight's gets dy hat
+template <typename S, typename G>
+__device__ __forceinline__ void gradient_piece(float (&f)[8], const Eight<S>& h, const Eight<G>& dy, const Eight<S>& dh, bool stream, const float2 (&w)[4], float2 (&dw)[4], float r,
+                                               float out, float along) {
+  const float2 out2 = make_float2(out, out), by = make_float2(-along * r * out, -along * r * out);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 p = h.pair(i), g = dy.pair(i), t = __fmul2_rn(g, out2);
+    const float2 v = __ffma2_rn(t, w[i], stream ? __ffma2_rn(p, by, dh.pair(i)) : __fmul2_rn(p, by));
+    if (out == r) dw[i] = __ffma2_rn(t, p, dw[i]);
+    else dw[i] = __ffma2_rn(g, __fmul2_rn(p, make_float2(r, r)), dw[i]);
+    f[2 * i] = v.x;
+    f[2 * i + 1] = v.y;
+  }
+}
 
 // ---- the forms that y leaves in
-// e4m3: the 16 threads of a block of 128 find its scale together.  (By whole warps; pieces behind the row are zeros.)
-__device__ __forceinline__ void put_fp8(const float2 (&y)[4], const NormFwdArgs& a, int row, int oct) {
+// e4m3: the 16 threads of a block of 128 find its scale together (whole warps; pieces behind the row are zeros): of v times r, whose largest magnitude is the largest |v| times r, as
+// rounding keeps the order, and whose product with a power of two is that of v with r times the power.
+__device__ __forceinline__ uint2 fp8_piece(const float2 (&v)[4], float r, uint32_t& byte) {
   float top = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) top = larger(top, y[i].x, y[i].y);
+  for (int i = 0; i < 4; ++i) top = larger(top, v[i].x, v[i].y);
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) {
     const float other = __shfl_xor_sync(0xffffffffu, top, o);
     top = larger(top, other, other);
   }
-  uint32_t bits = __float_as_uint(top);
-  const bool odd = __any_sync(0xffffffffu, bits >= kInf);
-  if (odd) {      // (rare) the largest of what is finite
-    bits = 0u;
+  byte = scale_byte(__float_as_uint(top * r) & 0x7fffffffu);
+  // (what is not finite, and scales whose product with r could leave fp32's range, zeros among them: rare)
+  const bool odd = __any_sync(0xffffffffu, byte - 32u > 168u);
+  float f[8];
+  if (odd) {      // the largest of what is finite
+    uint32_t bits = 0u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (finite_bits(y[i].x)) bits = max(bits, __float_as_uint(y[i].x) & 0x7fffffffu);
-      if (finite_bits(y[i].y)) bits = max(bits, __float_as_uint(y[i].y) & 0x7fffffffu);
+      if (finite_bits(v[i].x * r)) bits = max(bits, __float_as_uint(v[i].x * r) & 0x7fffffffu);
+      if (finite_bits(v[i].y * r)) bits = max(bits, __float_as_uint(v[i].y * r) & 0x7fffffffu);
     }
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, o));
-  }
-  if (oct >= a.octs) return;
-  const uint32_t byte = scale_byte(bits);
-  const float inv = inverse_scale(byte);
-  float f[8];
+    byte = scale_byte(bits);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 v = __fmul2_rn(y[i], make_float2(inv, inv));
-    f[2 * i] = !odd || finite_bits(y[i].x) ? v.x : __uint_as_float(0x7fffffffu);
-    f[2 * i + 1] = !odd || finite_bits(y[i].y) ? v.y : __uint_as_float(0x7fffffffu);
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = scaled<true>(v[i].x * r, inverse_scale(byte));
+      f[2 * i + 1] = scaled<true>(v[i].y * r, inverse_scale(byte));
+    }
+  } else {
+    const float by = inverse_scale(byte) * r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 p = __fmul2_rn(v[i], make_float2(by, by));
+      f[2 * i] = p.x;
+      f[2 * i + 1] = p.y;
+    }
   }
-  put8(a.fp8.values + row * a.fp8.ld, oct * 8, a.cols, e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
-  if ((oct & 15) == 0) put_scale(a.fp8.scales, a.rows, row, oct >> 4, (a.octs + 15) >> 4, byte);
+  return make_uint2(e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
 }
 // int8: the product is rounded once, then to a whole number by an addition whose last bit is one (1.5 * 2^23; |product| is 127 and a little at most).  (One at a time: the assembler makes
 // one operation of a packed product and a packed sum behind it, also of mul.rn and add.rn, which rounds once, and numbers half way between two come out on the other side.)
@@ -156,157 +207,48 @@ __device__ __forceinline__ uint32_t int8_bits(float v, float factor) { return __
 __device__ __forceinline__ uint32_t int8x4(float2 a, float2 b, float factor) {
   return __byte_perm(__byte_perm(int8_bits(a.x, factor), int8_bits(a.y, factor), 0x0040), __byte_perm(int8_bits(b.x, factor), int8_bits(b.y, factor), 0x0040), 0x5410);
 }
-// What a row's max |v| stands for: what its values are multiplied by, and its scale.  A row that holds something that is not finite has no scale: zeros (times zero, plus a zero
-// in place of the value), and a scale that makes its products NaN
+// What a row's max |v| stands for: what its values are multiplied by, and its scale.  A row that holds something that is not finite has no scale: zeros, and a scale that makes its
+// products NaN
 __device__ __forceinline__ float int8_factor(float top) { return __fdiv_rn(127.f, fmaxf(top, kInt8Least)); }
 __device__ __forceinline__ float int8_scale(float top, float r) {
   return __float_as_uint(top) < kInf ? __fdiv_rn(fmaxf(top, kInt8Least), 127.f) * r : __uint_as_float(0x7fffffffu);
 }
-// A piece of a row in every form that is wanted: h (or x), its weights, 1 / sqrt, the row's max |v| and what it is multiplied by
-template <bool NORM, bool VEC, typename S>
-__device__ __forceinline__ void put_piece(const Eight<S>& h, const float2 (&w)[4], float r, float top, float factor, bool int8, const NormFwdArgs& a, int row, int oct) {
-  float2 v[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = NORM ? __fmul2_rn(h.pair(i), w[i]) : h.pair(i);
-  if (int8 && oct < a.octs) {
-    const bool fine = __float_as_uint(top) < kInf;
-    put8(reinterpret_cast<unsigned char*>(a.int8.values) + row * a.int8.ld, oct * 8, a.cols, fine ? int8x4(v[0], v[1], factor) : 0u, fine ? int8x4(v[2], v[3], factor) : 0u);
-  }
-  if (!NORM) return;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = __fmul2_rn(v[i], make_float2(r, r));
-  if (a.fp8.values != nullptr) put_fp8(v, a, row, oct);
-  if (a.y.p != nullptr) {
-    const float f[8] = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
-    if (a.y_f32) store_floats<VEC>(f, reinterpret_cast<float*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
-    else store_floats<VEC>(f, reinterpret_cast<bf16*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
-  }
+__device__ __forceinline__ uint2 int8_piece(const float2 (&v)[4], float top, float factor) {
+  const bool fine = __float_as_uint(top) < kInf;
+  return make_uint2(fine ? int8x4(v[0], v[1], factor) : 0u, fine ? int8x4(v[2], v[3], factor) : 0u);
 }
-// h of a piece: x through the dropout, plus the residual, rounded to the stream's type
+// eight bytes of a row of `cols`, at place i
+template <int LIE>
+__device__ __forceinline__ void put_bytes(uint2 q, unsigned char* row, int i, int cols) {
+  if (LIE == ROWS_WHOLE) *reinterpret_cast<uint2*>(element(row, i)) = q;
+  else if (i < cols) put8(row, i, cols, q.x, q.y);
+}
+// h of a piece: x through the dropout, plus the residual (in h), rounded to the stream's type
 template <typename X, typename S>
-__device__ __forceinline__ void combine(Eight<S>& h, const Eight<X>& x, const Eight<S>& r, bool residual, const DropMask& mask, int row, int oct) {
+__device__ __forceinline__ void combine(Eight<S>& h, const Eight<X>& x, bool residual, const DropMask& mask, int row, int oct) {
   float f[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) f[j] = x.get(j);
   mask.apply(f, row, oct);
-  if (residual) add_eight(f, r);
+  if (residual) add_eight(f, h);
   h.round(f);
 }
-
-// ---- rows on 16-byte boundaries: pieces on their way, each in 16-byte places `threads` apart that one thread writes and reads
-__device__ __forceinline__ void ask(uint32_t to, const void* from, bool there) {      // (not there: zeros)
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
-template <typename T>
-__device__ __forceinline__ void ask_eight(uint32_t to, uint32_t apart, const T* row, int oct, bool there) {
-  const T* from = row + (there ? oct * 8 : 0);
+// A sum of two bf16 numbers rounded once is their fp32 sum rounded: where that is not exact the smaller one is less than 2^-16 of the other, far from half a step
+__device__ __forceinline__ void combine_bf16(Eight<bf16>& h, const Eight<bf16>& x) {
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) ask(to + i * apart, reinterpret_cast<const char*>(from) + 16 * i, there);
-}
-__device__ __forceinline__ void asked() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT>
-__device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
-__device__ __forceinline__ void take(Eight<bf16>& e, const unsigned char* from, uint32_t) {
-  const uint4 v = *reinterpret_cast<const uint4*>(from);
-  e.u[0] = v.x; e.u[1] = v.y; e.u[2] = v.z; e.u[3] = v.w;
-}
-__device__ __forceinline__ void take(Eight<float>& e, const unsigned char* from, uint32_t apart) {
-  const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + apart);
-  e.f[0] = a.x; e.f[1] = a.y; e.f[2] = a.z; e.f[3] = a.w; e.f[4] = b.x; e.f[5] = b.y; e.f[6] = b.z; e.f[7] = b.w;
-}
-
-template <int V, typename X, typename S, bool NORM, bool INT8>
-__global__ void __launch_bounds__(kNormMost, 2) norm_fwd_ring_kernel(const __grid_constant__ NormFwdArgs a) {
-  extern __shared__ __align__(16) unsigned char ring[];
-  __shared__ RowSums sh;
-  constexpr int XP = sizeof(X) / 2, SP = sizeof(S) / 2;      // 16-byte places of a piece
-  grid_enter();
-  const int t = threadIdx.x, T = blockDim.x;
-  const uint32_t apart = T * 16, slot = V * (XP + SP) * apart;
-  unsigned char* const mine = ring + t * 16;
-  const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine);
-  const bool residual = a.r.p != nullptr;
-  auto ask_row = [&](int row, int s) {
-    if (row < a.rows) {
-      const X* xp = reinterpret_cast<const X*>(a.x.p) + row * a.x.ld;
-      const S* rp = reinterpret_cast<const S*>(a.r.p) + row * a.r.ld;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int oct = v * T + t;
-        ask_eight(to + s * slot + v * XP * apart, apart, xp, oct, oct < a.octs);
-        if (residual) ask_eight(to + s * slot + (V * XP + v * SP) * apart, apart, rp, oct, oct < a.octs);
-      }
-    }
-    asked();
-  };
-#pragma unroll
-  for (int s = 0; s < kAhead; ++s) ask_row(blockIdx.x + s * gridDim.x, s);
-  DropMask mask;
-  mask.init(a.drop);
-  float2 w[V][4];
-  if (NORM) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) weight_of<true>(w[v], a.w, (v * T + t) * 8, a.cols);
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 sum = __hadd2_rn(*reinterpret_cast<const __nv_bfloat162*>(&h.u[i]), *reinterpret_cast<const __nv_bfloat162*>(&x.u[i]));
+    h.u[i] = *reinterpret_cast<const uint32_t*>(&sum);
   }
-  uint32_t turn = 0;
-  int s = 0;
-  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    // (the place behind the others is free: this thread has read it, and only it does)
-    ask_row(row + kAhead * gridDim.x, s == 0 ? kAhead : s - 1);
-    arrived<kAhead>();
-    Eight<S> h[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const unsigned char* from = mine + s * slot;
-      Eight<X> x;
-      Eight<S> r;
-      take(x, from + v * XP * apart, apart);
-      if (residual) take(r, from + (V * XP + v * SP) * apart, apart);
-      combine(h[v], x, r, residual, mask, row, v * T + t);
-    }
-    s = s == kAhead ? 0 : s + 1;
-    if (NORM && a.h.p != nullptr) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) store_eight<true>(h[v], reinterpret_cast<S*>(a.h.p) + row * a.h.ld, (v * T + t) * 8, a.cols);
-    }
-    float r = 1.f, top = 0.f, eps = a.eps;
-#pragma unroll 1
-    for (bool again = false;; again = true) {
-      float2 ss = make_float2(0.f, 0.f);
-      top = 0.f;
-#pragma unroll
-      for (int v = 0; v < V; ++v) add_sums<NORM, INT8>(h[v], w[v], ss, top);
-      const float2 of = row_total<true>(ss.x + ss.y, top, sh, turn++);
-      top = of.y;
-      if constexpr (NORM) {
-        const float ms = of.x * a.inv_cols + eps;
-        r = rsqrtf(ms);
-        if (in_range(ms) || again) break;
-        float size = 0.f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) size = largest_of(h[v], size);
-        const float power = power_for(__float_as_uint(row_total<true>(0.f, size, sh, turn++).y), eps);
-#pragma unroll
-        for (int v = 0; v < V; ++v) rescale(h[v], power);
-        eps = eps * power * power;
-      } else {
-        break;
-      }
-    }
-    const float factor = INT8 ? int8_factor(top) : 0.f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) put_piece<NORM, true>(h[v], w[v], r, top, factor, INT8, a, row, v * T + t);
-    if (INT8 && t == 0) a.int8.scales[row] = int8_scale(top, r);
-  }
-  arrived<0>();
 }
 
-// Any rows.  V: pieces of eight elements a thread (MANY: as many as it takes, in a loop); NORM: else the int8 form of x as it is
-template <int V, bool MANY, typename X, typename S, bool NORM, bool VEC>
-__global__ void __launch_bounds__(kNormMost, 1) norm_fwd_kernel(const __grid_constant__ NormFwdArgs a) {
-  __shared__ RowSums sh;
+// V: pieces of eight elements a thread, two or four (MANY: as many as it takes, in a loop); NORM: else the int8 form of x as it is
+template <int V, bool MANY, typename X, typename S, bool NORM, int LIE>
+__global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_constant__ NormFwdArgs a) {
+  __shared__ __align__(16) RowSums sh;
+  sh.init();
   grid_enter();
-  const int t = threadIdx.x, T = blockDim.x;
+  const int t = threadIdx.x, T = blockDim.x, mine = (t >> 5) * (32 * V) + (t & 31);      // pieces mine, mine + 32, ..: a warp's lie next to one another
   DropMask mask;
   mask.init(a.drop);
   const int rounds = MANY ? (a.octs + T * V - 1) / (T * V) : 1;
@@ -317,21 +259,29 @@ __global__ void __launch_bounds__(kNormMost, 1) norm_fwd_kernel(const __grid_con
     const S* const rp = reinterpret_cast<const S*>(a.r.p) + row * a.r.ld;
     Eight<S> h[V];
     float power = 1.f;
-    auto fetch = [&](int first) {      // h of the pieces first + t, first + t + T, ..
+    auto fetch = [&](int first) {      // h of the pieces from `first` on
       Eight<X> x[V];
 #pragma unroll
-      for (int v = 0; v < V; ++v) load_eight<VEC>(x[v], xp, (first + v * T + t) * 8, a.cols);
+      for (int v = 0; v < V; ++v) load_eight<LIE>(x[v], xp, (first + mine + 32 * v) * 8, a.cols);
       if (a.r.p != nullptr) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) load_eight<VEC>(h[v], rp, (first + v * T + t) * 8, a.cols);
+        for (int v = 0; v < V; ++v) load_eight<LIE>(h[v], rp, (first + mine + 32 * v) * 8, a.cols);
       }
 #pragma unroll
-      for (int v = 0; v < V; ++v) combine(h[v], x[v], h[v], a.r.p != nullptr, mask, row, first + v * T + t);
+      for (int v = 0; v < V; ++v) {
+        if constexpr (sizeof(X) == 2 && sizeof(S) == 2) {
+          if (mask.limit != 0) combine(h[v], x[v], a.r.p != nullptr, mask, row, first + mine + 32 * v);
+          else if (a.r.p != nullptr) combine_bf16(h[v], x[v]);
+          else h[v] = x[v];
+        } else {
+          combine(h[v], x[v], a.r.p != nullptr, mask, row, first + mine + 32 * v);
+        }
+      }
     };
     auto keep = [&](int first) {
       if (!NORM || a.h.p == nullptr) return;
 #pragma unroll
-      for (int v = 0; v < V; ++v) store_eight<VEC>(h[v], reinterpret_cast<S*>(a.h.p) + row * a.h.ld, (first + v * T + t) * 8, a.cols);
+      for (int v = 0; v < V; ++v) store_eight<LIE>(h[v], reinterpret_cast<S*>(a.h.p) + row * a.h.ld, (first + mine + 32 * v) * 8, a.cols);
     };
     auto apply_power = [&] {
       if (power == 1.f) return;
@@ -343,10 +293,10 @@ __global__ void __launch_bounds__(kNormMost, 1) norm_fwd_kernel(const __grid_con
       keep(0);
     }
     float r = 1.f, top = 0.f, eps = a.eps;
+    bool again = false;
 #pragma unroll 1
-    for (bool again = false;; again = true) {
+    for (;;) {
       float2 ss = make_float2(0.f, 0.f);
-      float size = 0.f;
       top = 0.f;
 #pragma unroll 1
       for (int i = 0; i < rounds; ++i) {
@@ -358,26 +308,32 @@ __global__ void __launch_bounds__(kNormMost, 1) norm_fwd_kernel(const __grid_con
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           float2 w[4];
-          if (NORM) weight_of<VEC>(w, a.w, (first + v * T + t) * 8, a.cols);
+          if (NORM) weight_of<LIE>(w, a.w, (first + mine + 32 * v) * 8, a.cols);
           if (int8) add_sums<NORM, true>(h[v], w, ss, top);
           else add_sums<NORM, false>(h[v], w, ss, top);
-          if (NORM) size = largest_of(h[v], size);
         }
       }
-      const float2 of = row_total<true>(ss.x + ss.y, top, sh, turn++);
+      const float2 of = row_total<NORM, 1>(ss.x + ss.y, top, sh, turn++);
       top = of.y;
+      const float ms = NORM ? of.x * a.inv_cols + eps : 1.f;
+      r = NORM ? rsqrtf(ms) : 1.f;
+      if (in_range(ms) || again) break;
       if constexpr (NORM) {
-        const float ms = of.x * a.inv_cols + eps;
-        r = rsqrtf(ms);
-        if (in_range(ms) || again) break;
-        power = power_for(__float_as_uint(row_total<true>(0.f, size, sh, turn++).y), eps);
+        again = true;
+        float size = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < rounds; ++i) {
+          if (MANY) fetch(i * T * V);
+#pragma unroll
+          for (int v = 0; v < V; ++v) size = largest_of(h[v], size);
+        }
+        power = power_for(__float_as_uint(row_total<false, 1>(0.f, size, sh, turn++).y), eps);
         if (!MANY) apply_power();
         eps = eps * power * power;
-      } else {
-        break;
       }
     }
     const float factor = int8 ? int8_factor(top) : 0.f;
+    uint32_t scales = 0u;
 #pragma unroll 1
     for (int i = 0; i < rounds; ++i) {
       const int first = i * T * V;
@@ -388,112 +344,160 @@ __global__ void __launch_bounds__(kNormMost, 1) norm_fwd_kernel(const __grid_con
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float2 w[4];
-        if (NORM) weight_of<VEC>(w, a.w, (first + v * T + t) * 8, a.cols);
-        put_piece<NORM, VEC>(h[v], w, r, top, factor, int8, a, row, first + v * T + t);
+        const int oct = first + mine + 32 * v;
+        float2 w[4], f[4];
+        if (NORM) weight_of<LIE>(w, a.w, oct * 8, a.cols);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = NORM ? __fmul2_rn(h[v].pair(j), w[j]) : h[v].pair(j);
+        if (int8) {
+          put_bytes<LIE>(int8_piece(f, top, factor), reinterpret_cast<unsigned char*>(a.int8.values) + row * a.int8.ld, oct * 8, a.cols);
+        }
+        if (NORM && a.fp8.values != nullptr) {
+          uint32_t byte;
+          const uint2 q = fp8_piece(f, r, byte);
+          put_bytes<LIE>(q, a.fp8.values + row * a.fp8.ld, oct * 8, a.cols);
+          // four blocks, one word of scales, are in two pieces of a warp, two blocks each (zero for those behind the row)
+          scales = v & 1 ? scales | byte << 16 : byte;
+          if (v & 1) {
+            const uint32_t others = __shfl_down_sync(0xffffffffu, scales, 16);
+            if ((t & 31) == 0 && oct - 32 < a.octs) reinterpret_cast<uint32_t*>(a.fp8.scales)[(size_t)(oct >> 6) * a.rows + row] = scales | others << 8;
+          }
+        }
+        if (NORM && a.y.p != nullptr) {
+          float g[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            g[2 * j] = f[j].x * r;
+            g[2 * j + 1] = f[j].y * r;
+          }
+          if (a.y_f32) store_floats<LIE>(g, reinterpret_cast<float*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
+          else store_floats<LIE>(g, reinterpret_cast<bf16*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
+        }
       }
     }
     if (int8 && t == 0) a.int8.scales[row] = int8_scale(top, r);
   }
 }
 
-// MANY: the sums of the weight's gradient are kept in the CTA's row of `parts`, where a thread finds its own again; else in registers
-template <int V, bool MANY, typename S, typename G, bool VEC>
-__global__ void __launch_bounds__(kNormMost) norm_bwd_kernel(const __grid_constant__ NormBwdArgs a) {
-  __shared__ RowSums sh;
+// Any rows.  MANY: the sums of the weight's gradient are kept in the CTA's row of `parts`, where a thread finds its own again; else in registers
+// V: pieces of a thread, one where they suffice: each has its sums of the weight's gradient in registers, and with two there is room for half the warps (65972 x 1536 in fp32 254 us, with two
+// 284 in the same registers).  Two take 96 registers, with which an SM holds two CTAs of 320 threads (75600 x 5120 572 us, in 104 registers 889).
+template <int V, bool MANY, typename S, typename G, int LIE>
+__global__ void __maxnreg__(V == 1 ? 64 : 96) norm_bwd_kernel(const __grid_constant__ NormBwdArgs a) {
+  __shared__ __align__(16) RowSums sh;
+  sh.init();
   grid_enter();
-  const int t = threadIdx.x, T = blockDim.x;
+  const int t = threadIdx.x, T = blockDim.x, mine = (t >> 5) * (32 * V) + (t & 31);      // pieces mine, mine + 32, ..: a warp's lie next to one another
   DropMask mask;
   mask.init(a.drop);
   const int rounds = MANY ? (a.octs + T * V - 1) / (T * V) : 1;
-  float dw[V][8];
+  const bool stream = a.dh.p != nullptr;
+  float2 dw[V][4];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dw[v][j] = 0.f;
+    for (int i = 0; i < 4; ++i) dw[v][i] = make_float2(0.f, 0.f);
   float* const part = a.parts != nullptr ? a.parts + (size_t)blockIdx.x * a.octs * 8 : nullptr;
+  auto sum_of = [&](int v) {
+    Eight<float> e;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      e.f[2 * i] = dw[v][i].x;
+      e.f[2 * i + 1] = dw[v][i].y;
+    }
+    return e;
+  };
   uint32_t turn = 0;
   for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
     Eight<S> h[V], dh[V];
     Eight<G> dy[V];
+    float power = 1.f;
+    auto apply_power = [&] {
+      if (power == 1.f) return;
+#pragma unroll
+      for (int v = 0; v < V; ++v) rescale(h[v], power);
+    };
     auto fetch = [&](int first, bool both) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) load_eight<VEC>(h[v], reinterpret_cast<const S*>(a.h.p) + row * a.h.ld, (first + v * T + t) * 8, a.cols);
+      for (int v = 0; v < V; ++v) load_eight<LIE>(h[v], reinterpret_cast<const S*>(a.h.p) + row * a.h.ld, (first + mine + 32 * v) * 8, a.cols);
 #pragma unroll
-      for (int v = 0; v < V; ++v) load_eight<VEC>(dy[v], reinterpret_cast<const G*>(a.dy.p) + row * a.dy.ld, (first + v * T + t) * 8, a.cols);
-      if (both && a.dh.p != nullptr) {
+      for (int v = 0; v < V; ++v) load_eight<LIE>(dy[v], reinterpret_cast<const G*>(a.dy.p) + row * a.dy.ld, (first + mine + 32 * v) * 8, a.cols);
+      if (both && stream) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) load_eight<VEC>(dh[v], reinterpret_cast<const S*>(a.dh.p) + row * a.dh.ld, (first + v * T + t) * 8, a.cols);
+        for (int v = 0; v < V; ++v) load_eight<LIE>(dh[v], reinterpret_cast<const S*>(a.dh.p) + row * a.dh.ld, (first + mine + 32 * v) * 8, a.cols);
       }
     };
-    // of h times s: sum of squares, and of the weighted gradient along it
-    auto total = [&](float s) {
-      float ss = 0.f, dot = 0.f;
+    if (!MANY) fetch(0, true);
+    float r, eps = a.eps, along;
+    bool again = false;
+#pragma unroll 1
+    for (;;) {
+      float2 ss = make_float2(0.f, 0.f), dot = ss;
+#pragma unroll 1
       for (int i = 0; i < rounds; ++i) {
-        if (MANY) fetch(i * T * V, false);
+        const int first = i * T * V;
+        if (MANY) {
+          fetch(first, false);
+          apply_power();
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           float2 w[4];
-          weight_of<VEC>(w, a.w, (i * T * V + v * T + t) * 8, a.cols);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float f = h[v].get(j) * s;
-            ss += f * f;
-            dot += dy[v].get(j) * (j & 1 ? w[j / 2].y : w[j / 2].x) * f;
-          }
+          weight_of<LIE>(w, a.w, (first + mine + 32 * v) * 8, a.cols);
+          add_dots(h[v], dy[v], w, ss, dot);
         }
       }
-      return row_total<false>(ss, dot, sh, turn++);
-    };
-    if (!MANY) fetch(0, true);
-    float2 of = total(1.f);
-    float s = 1.f, ms = of.x * a.inv_cols + a.eps;
-    if (!in_range(ms)) {
-      float top = 0.f;
+      const float2 of = row_total<true, 2>(ss.x + ss.y, dot.x + dot.y, sh, turn++);
+      const float ms = of.x * a.inv_cols + eps;
+      r = rsqrtf(ms);
+      along = of.y * r * a.inv_cols;
+      if (in_range(ms) || again) break;
+      again = true;
+      float size = 0.f;
+#pragma unroll 1
       for (int i = 0; i < rounds; ++i) {
         if (MANY) fetch(i * T * V, false);
 #pragma unroll
-        for (int v = 0; v < V; ++v) top = largest_of(h[v], top);
+        for (int v = 0; v < V; ++v) size = largest_of(h[v], size);
       }
-      s = power_for(__float_as_uint(row_total<true>(0.f, top, sh, turn++).y), a.eps);
-      of = total(s);
-      ms = of.x * a.inv_cols + a.eps * s * s;
+      power = power_for(__float_as_uint(row_total<false, 1>(0.f, size, sh, turn++).y), eps);
+      eps = eps * power * power;
+      if (!MANY) apply_power();
     }
-    // (h times s) r is the normed row, and r s what its gradient is multiplied by
-    const float r = rsqrtf(ms), out = r * s, along = of.y * r * a.inv_cols;
+    const float out = r * power;
+#pragma unroll 1
     for (int i = 0; i < rounds; ++i) {
       const int first = i * T * V;
-      if (MANY) fetch(first, true);
+      if (MANY) {
+        fetch(first, true);
+        apply_power();
+      }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int oct = first + v * T + t;
+        const int oct = first + mine + 32 * v;
         float f[8];
         float2 w[4];
-        weight_of<VEC>(w, a.w, oct * 8, a.cols);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float hat = h[v].get(j) * s * r, g = dy[v].get(j);
-          f[j] = out * (g * (j & 1 ? w[j / 2].y : w[j / 2].x) - hat * along);
-          if (a.dh.p != nullptr) f[j] += dh[v].get(j);
-          dw[v][j] += g * hat;
-        }
-        if (a.dr.p != nullptr) store_floats<VEC>(f, reinterpret_cast<S*>(a.dr.p) + row * a.dr.ld, oct * 8, a.cols);
+        weight_of<LIE>(w, a.w, oct * 8, a.cols);
+        gradient_piece(f, h[v], dy[v], dh[v], stream, w, dw[v], r, out, along);
+        if (a.dr.p != nullptr) store_floats<LIE>(f, reinterpret_cast<S*>(a.dr.p) + row * a.dr.ld, oct * 8, a.cols);
         if (a.dx.p != nullptr) {
           mask.apply(f, row, oct);
-          if (a.dx_f32) store_floats<VEC>(f, reinterpret_cast<float*>(a.dx.p) + row * a.dx.ld, oct * 8, a.cols);
-          else store_floats<VEC>(f, reinterpret_cast<bf16*>(a.dx.p) + row * a.dx.ld, oct * 8, a.cols);
+          if (a.dx_f32) store_floats<LIE>(f, reinterpret_cast<float*>(a.dx.p) + row * a.dx.ld, oct * 8, a.cols);
+          else store_floats<LIE>(f, reinterpret_cast<bf16*>(a.dx.p) + row * a.dx.ld, oct * 8, a.cols);
         }
         if (MANY) {
           if (part != nullptr && oct < a.octs) {
-            Eight<float> sum;
-            if (row == (int)blockIdx.x) sum.zero();
-            else sum.load(part + oct * 8);
+            Eight<float> sum = sum_of(v);
+            if (row != (int)blockIdx.x) {
+              Eight<float> before;
+              before.load(part + oct * 8);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum.f[j] += dw[v][j];
+              for (int j = 0; j < 8; ++j) sum.f[j] += before.f[j];
+            }
             sum.store(part + oct * 8);
           }
 #pragma unroll
-          for (int j = 0; j < 8; ++j) dw[v][j] = 0.f;
+          for (int j = 0; j < 4; ++j) dw[v][j] = make_float2(0.f, 0.f);
         }
       }
     }
@@ -501,49 +505,46 @@ __global__ void __launch_bounds__(kNormMost) norm_bwd_kernel(const __grid_consta
   if (!MANY && part != nullptr) {
 #pragma unroll
     for (int v = 0; v < V; ++v)
-      if (v * T + t < a.octs) {
-        Eight<float> sum;
-        sum.round(dw[v]);
-        sum.store(part + (v * T + t) * 8);
-      }
+      if (mine + 32 * v < a.octs) sum_of(v).store(part + (mine + 32 * v) * 8);
   }
 }
 
-// The weight's gradient: the CTAs' parts, each of `width` columns, added in a fixed order.  32 columns a CTA, eight ranges of the parts.
-__global__ void __launch_bounds__(256) norm_weight_kernel(const float* parts, int count, int cols, int width, float* __restrict__ dw) {
-  __shared__ float sh[8][32];
+// The weight's gradient: the CTAs' parts, each of `width` columns, added in a fixed order.  32 columns a CTA, 32 ranges of the parts, eight loads of a thread under way.
+__global__ void __launch_bounds__(1024) norm_weight_kernel(const float* parts, int count, int cols, int width, float* __restrict__ dw) {
+  __shared__ float sh[32][33];
   grid_enter();
   const int lane = threadIdx.x & 31, range = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
   float sum = 0.f;
   if (col < cols) {
     const float* from = parts + col;
 #pragma unroll 8
-    for (int i = range; i < count; i += 8) sum += from[(size_t)i * width];
+    for (int i = range; i < count; i += 32) sum += from[(size_t)i * width];
   }
   sh[range][lane] = sum;
   __syncthreads();
-  if (range == 0 && col < cols) {
+  sum = sh[lane][range];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) sum += sh[i][lane];
-    dw[col] = sum;
-  }
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0 && blockIdx.x * 32 + range < cols) dw[blockIdx.x * 32 + range] = sum;
 }
 
-// CTAs of a kernel that the device holds, asked once for each number of warps and device (with the same shared memory each time); it is allowed its shared memory first
+// CTAs of a kernel that the device holds: the last answer for each number of warps and device, with the shared memory that it was asked for; the kernel is allowed its shared memory first
 struct Residents {
   KernelAttr attr;
-  std::atomic<int> known[kMaxDevices][kNormMost / 32 + 1] = {};
+  std::atomic<unsigned long long> known[kMaxDevices][kNormMost / 32 + 1] = {};      // bytes << 8 | CTAs of an SM
 };
 cudaError_t resident_ctas(const void* kernel, Residents& r, int threads, size_t smem, int* ctas) {
   int dev = 0, sms = 0, n = 0;
   cudaError_t e;
   if ((e = cudaGetDevice(&dev)) != cudaSuccess || (e = sm_count(&sms)) != cudaSuccess) return e;
   if (smem > 0 && (e = prepare_kernel(kernel, r.attr, smem)) != cudaSuccess) return e;
-  if (dev < kMaxDevices) n = r.known[dev][threads / 32].load(std::memory_order_relaxed);
-  if (n == 0) {
+  const unsigned long long last = dev < kMaxDevices ? r.known[dev][threads / 32].load(std::memory_order_relaxed) : 0;
+  if (last != 0 && last >> 8 == smem) {
+    n = (int)(last & 255);
+  } else {
     if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem)) != cudaSuccess) return e;
     if (n < 1) n = 1;
-    if (dev < kMaxDevices) r.known[dev][threads / 32].store(n, std::memory_order_relaxed);
+    if (dev < kMaxDevices) r.known[dev][threads / 32].store((unsigned long long)smem << 8 | (unsigned)n, std::memory_order_relaxed);
   }
   *ctas = n * sms;
   return cudaSuccess;
@@ -554,53 +555,60 @@ int threads_for(int octs, int v) {
   const int t = (octs + v * 32 - 1) / (v * 32) * 32;
   return t < 32 ? 32 : t > kNormMost ? kNormMost : t;
 }
+// Pieces of a thread.  Forward: four share a row's fixed steps (its sums, the barrier, two divisions), two leave more warps whose latencies overlap.  Rows of bf16 of more than 4096
+// elements take four (75600 x 5120 to e4m3 440 us, with two 500; 10000 x 8192 94, 110), shorter ones two (75600 x 1536 to e4m3 130 us, with four 185; 2048 x 1536 5.5, 7.6), and so
+// do rows with fp32, of which four pieces do not fit the registers (65972 x 1536 219 us, with four 319).  0: as many as it takes
+int pieces_fwd(int octs, bool narrow) { return octs <= (narrow ? kNormMost : 2 * kNormMost) ? 2 : octs <= 4 * kNormMost ? 4 : 0; }
 
-template <int V, typename X, typename S, bool NORM, bool INT8>
-cudaError_t go_fwd_ring(const NormFwdArgs& a, cudaStream_t st) {
-  static Residents residents;
-  const int threads = threads_for(a.octs, V);
-  const size_t smem = (size_t)(kAhead + 1) * V * threads * 8 * (sizeof(X) + sizeof(S));
-  int ctas = 0;
-  const cudaError_t e = resident_ctas((const void*)norm_fwd_ring_kernel<V, X, S, NORM, INT8>, residents, threads, smem, &ctas);
-  if (e != cudaSuccess) return e;
-  return launch_kernel(norm_fwd_ring_kernel<V, X, S, NORM, INT8>, a.rows < ctas ? a.rows : ctas, threads, smem, st, a);
-}
-template <int V, bool MANY, typename X, typename S, bool NORM, bool VEC>
+template <int V, bool MANY, typename X, typename S, bool NORM, int LIE>
 cudaError_t go_fwd(const NormFwdArgs& a, cudaStream_t st) {
   static Residents residents;
   const int threads = threads_for(a.octs, V);
   int ctas = 0;
-  const cudaError_t e = resident_ctas((const void*)norm_fwd_kernel<V, MANY, X, S, NORM, VEC>, residents, threads, 0, &ctas);
+  const cudaError_t e = resident_ctas((const void*)norm_fwd_kernel<V, MANY, X, S, NORM, LIE>, residents, threads, 0, &ctas);
   if (e != cudaSuccess) return e;
-  return launch_kernel(norm_fwd_kernel<V, MANY, X, S, NORM, VEC>, a.rows < ctas ? a.rows : ctas, threads, 0, st, a);
+  return launch_kernel(norm_fwd_kernel<V, MANY, X, S, NORM, LIE>, a.rows < ctas ? a.rows : ctas, threads, 0, st, a);
+}
+template <int V, typename X, typename S, bool NORM>
+cudaError_t lie_fwd(const NormFwdArgs& a, cudaStream_t st) {
+  return a.octs % (V * 32) == 0 && threads_for(a.octs, V) * V == a.octs ? go_fwd<V, false, X, S, NORM, ROWS_WHOLE>(a, st) : go_fwd<V, false, X, S, NORM, ROWS_ALIGNED>(a, st);
 }
 template <typename X, typename S, bool NORM>
 cudaError_t size_fwd(const NormFwdArgs& a, bool vec, cudaStream_t st) {
-  const bool many = a.cols > 2 * 8 * kNormMost;
-  if (!vec) return many ? go_fwd<2, true, X, S, NORM, false>(a, st) : go_fwd<2, false, X, S, NORM, false>(a, st);
-  if (a.cols > kRingCols) return go_fwd<2, true, X, S, NORM, true>(a, st);
-  if (!NORM) return a.octs <= 128 ? go_fwd_ring<1, X, S, NORM, true>(a, st) : go_fwd_ring<2, X, S, NORM, true>(a, st);
-  if (a.int8.values != nullptr) return a.octs <= 128 ? go_fwd_ring<1, X, S, true, true>(a, st) : go_fwd_ring<2, X, S, true, true>(a, st);
-  return a.octs <= 128 ? go_fwd_ring<1, X, S, true, false>(a, st) : go_fwd_ring<2, X, S, true, false>(a, st);
+  if (!vec) return a.octs > 2 * kNormMost ? go_fwd<2, true, X, S, NORM, ROWS_ANY>(a, st) : go_fwd<2, false, X, S, NORM, ROWS_ANY>(a, st);
+  switch (pieces_fwd(a.octs, sizeof(X) + sizeof(S) == 4)) {
+    case 2: return lie_fwd<2, X, S, NORM>(a, st);
+    case 4: return lie_fwd<4, X, S, NORM>(a, st);
+    default: return go_fwd<2, true, X, S, NORM, ROWS_ALIGNED>(a, st);
+  }
 }
 
-template <int V, bool MANY, typename S, typename G, bool VEC>
+cudaError_t sum_parts(const NormBwdArgs& a, int ctas, float* dw, cudaStream_t st) {
+  if (dw == nullptr) return cudaSuccess;
+  return launch_kernel(norm_weight_kernel, (a.cols + 31) / 32, 1024, 0, st, a.parts, ctas, a.cols, a.octs * 8, dw);
+}
+template <int V, bool MANY, typename S, typename G, int LIE>
 cudaError_t go_bwd(const NormBwdArgs& a, float* dw, cudaStream_t st) {
   static Residents residents;
   const int threads = threads_for(a.octs, V);
   int ctas = 0;
-  cudaError_t e = resident_ctas((const void*)norm_bwd_kernel<V, MANY, S, G, VEC>, residents, threads, 0, &ctas);
+  cudaError_t e = resident_ctas((const void*)norm_bwd_kernel<V, MANY, S, G, LIE>, residents, threads, 0, &ctas);
   if (e != cudaSuccess) return e;
   if (ctas > kNormParts) ctas = kNormParts;
-  if (ctas > a.rows) ctas = a.rows;
-  if ((e = launch_kernel(norm_bwd_kernel<V, MANY, S, G, VEC>, ctas, threads, 0, st, a)) != cudaSuccess || dw == nullptr) return e;
-  return launch_kernel(norm_weight_kernel, (a.cols + 31) / 32, 256, 0, st, a.parts, ctas, a.cols, a.octs * 8, dw);
+  const int each = (a.rows + ctas - 1) / ctas;      // rows of a CTA: no more CTAs, and parts, than take the same time with as many each
+  ctas = (a.rows + each - 1) / each;
+  e = launch_kernel(norm_bwd_kernel<V, MANY, S, G, LIE>, ctas, threads, 0, st, a);
+  return e != cudaSuccess ? e : sum_parts(a, ctas, dw, st);
 }
-template <typename S, typename G, bool VEC>
-cudaError_t size_bwd(const NormBwdArgs& a, float* dw, cudaStream_t st) {
-  if (a.octs <= 128) return go_bwd<1, false, S, G, VEC>(a, dw, st);
-  if (a.octs <= 2 * kNormMost) return go_bwd<2, false, S, G, VEC>(a, dw, st);
-  return go_bwd<1, true, S, G, VEC>(a, dw, st);
+template <int V, typename S, typename G>
+cudaError_t lie_bwd(const NormBwdArgs& a, float* dw, cudaStream_t st) {
+  return threads_for(a.octs, V) * V == a.octs ? go_bwd<V, false, S, G, ROWS_WHOLE>(a, dw, st) : go_bwd<V, false, S, G, ROWS_ALIGNED>(a, dw, st);
+}
+template <typename S, typename G>
+cudaError_t size_bwd(const NormBwdArgs& a, bool vec, float* dw, cudaStream_t st) {
+  if (!vec) return a.octs <= 2 * kNormMost ? go_bwd<2, false, S, G, ROWS_ANY>(a, dw, st) : go_bwd<1, true, S, G, ROWS_ANY>(a, dw, st);
+  if (a.octs <= kNormMost) return lie_bwd<1, S, G>(a, dw, st);
+  return a.octs <= 2 * kNormMost ? lie_bwd<2, S, G>(a, dw, st) : go_bwd<1, true, S, G, ROWS_ALIGNED>(a, dw, st);
 }
 
 }  // namespace
@@ -637,9 +645,8 @@ cudaError_t launch_norm_bwd(NormBwdArgs a, bool h_f32, bool dy_f32, float* dw, f
   const size_t size = h_f32 ? 4 : 2;
   const bool vec = a.cols % 8 == 0 && rows_aligned(a.h, size) && rows_aligned(a.dy, dy_f32 ? 4 : 2) && rows_aligned(a.dh, size) && rows_aligned(a.dr, size) &&
                    rows_aligned(a.dx, a.dx_f32 ? 4 : 2) && (reinterpret_cast<uintptr_t>(a.w) & 15u) == 0;
-  auto go = [&](auto aligned, auto any) { return vec ? aligned(a, dw, st) : any(a, dw, st); };
-  if (h_f32) return dy_f32 ? go(size_bwd<float, float, true>, size_bwd<float, float, false>) : go(size_bwd<float, bf16, true>, size_bwd<float, bf16, false>);
-  return dy_f32 ? go(size_bwd<bf16, float, true>, size_bwd<bf16, float, false>) : go(size_bwd<bf16, bf16, true>, size_bwd<bf16, bf16, false>);
+  if (h_f32) return dy_f32 ? size_bwd<float, float>(a, vec, dw, st) : size_bwd<float, bf16>(a, vec, dw, st);
+  return dy_f32 ? size_bwd<bf16, float>(a, vec, dw, st) : size_bwd<bf16, bf16>(a, vec, dw, st);
 }
 
 }  // namespace vsa2

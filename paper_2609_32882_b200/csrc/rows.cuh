@@ -105,11 +105,18 @@ template <> struct Eight<float> {
   }
   __device__ __forceinline__ void store(float* p, int j) const { *p = f[j]; }
 };
-// Elements i .. i+7 of a row (zeros behind it, and for i beyond it); VEC: rows begin on 16-byte boundaries and are whole pieces of eight
-template <bool VEC, typename T>
+// How the rows of a call lie: anywhere; on 16-byte boundaries and in whole pieces of eight elements; so, and as many pieces as the kernel's threads take
+enum { ROWS_ANY = 0, ROWS_ALIGNED = 1, ROWS_WHOLE = 2 };
+// element i of a row that is the same for all threads: a base of 64 bits and a thread's offset of 32 (2^22 elements at most), which a load adds by itself
+template <typename T>
+__device__ __forceinline__ T* element(T* row, int i) { return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + (uint32_t)i * (uint32_t)sizeof(T)); }
+// Elements i .. i+7 of a row (zeros behind it, and for i beyond it)
+template <int LIE, typename T>
 __device__ __forceinline__ void load_eight(Eight<T>& e, const T* row, int i, int cols) {
-  if (VEC) {
-    if (i < cols) e.load(row + i);
+  if (LIE == ROWS_WHOLE) {
+    e.load(element(row, i));
+  } else if (LIE == ROWS_ALIGNED) {
+    if (i < cols) e.load(element(row, i));
     else e.zero();
   } else {
     e.zero();
@@ -118,21 +125,21 @@ __device__ __forceinline__ void load_eight(Eight<T>& e, const T* row, int i, int
       if (i + j < cols) e.set(j, row + i + j);
   }
 }
-template <bool VEC, typename T>
+template <int LIE, typename T>
 __device__ __forceinline__ void store_eight(const Eight<T>& e, T* row, int i, int cols) {
-  if (VEC) {
-    if (i < cols) e.store(row + i);
+  if (LIE != ROWS_ANY) {
+    if (LIE == ROWS_WHOLE || i < cols) e.store(element(row, i));
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (i + j < cols) e.store(row + i + j, j);
   }
 }
-template <bool VEC, typename T>
+template <int LIE, typename T>
 __device__ __forceinline__ void store_floats(const float (&f)[8], T* row, int i, int cols) {
   Eight<T> e;
   e.round(f);
-  store_eight<VEC>(e, row, i, cols);
+  store_eight<LIE>(e, row, i, cols);
 }
 
 // f plus e, each sum rounded
@@ -166,7 +173,9 @@ struct DropMask {
     uint32_t a = oct, b = row, c = o0, d = o1, p = k0, q = k1;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
-      const unsigned long long u = (unsigned long long)a * 0xD2511F53u, v = (unsigned long long)c * 0xCD9E8D57u;
+      unsigned long long u, v;
+      asm("mul.wide.u32 %0, %1, %2;" : "=l"(u) : "r"(a), "r"(0xD2511F53u));
+      asm("mul.wide.u32 %0, %1, %2;" : "=l"(v) : "r"(c), "r"(0xCD9E8D57u));
       a = (uint32_t)(v >> 32) ^ b ^ p;
       b = (uint32_t)v;
       c = (uint32_t)(u >> 32) ^ d ^ q;
