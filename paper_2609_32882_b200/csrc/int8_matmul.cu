@@ -3,7 +3,7 @@
 // On the tensor cores: tcgen05.mma kind::i8 adds products of whole numbers in 32 bits, exactly, so ranges of K are added in any order and a result is the same however the product is
 // cut.  The scales and the bias come in the epilogue: one of the two vectors is a lane's own, the other one lies in shared memory.
 //
-// Tiles and roles as in the product of e4m3 matrices (fp8_matmul.cu): B's rows are the 128 rows of a CTA's tile, A's rows its NT columns; pairs of SMs share a tile of 256 x 256
+// Up to eight rows of A take a kernel of their own (int8_few_kernel).  Otherwise tiles and roles are as in the product of e4m3 matrices (fp8_matmul.cu): B's rows are the 128 rows of a CTA's tile, A's rows its NT columns; pairs of SMs share a tile of 256 x 256
 // where there are rows for it.  No scales go to tensor memory, so the two accumulators have all of it.
 #include "mm_tiles.cuh"
 #include "rows.cuh"
@@ -329,6 +329,78 @@ __global__ void __launch_bounds__(256) int8_bias_kernel(int m, int n, const floa
   for (int row = blockIdx.y; row < m; row += gridDim.y) put(c + row * ldc + col, v);
 }
 
+// Few rows of A: every byte of B is read once and meets little work, and what counts is how many bytes are on their way.  The eight warps of a CTA share 16 rows of B; each has five
+// neighbouring pieces of 64 bytes of them under way (four: 15.2 us instead of 14.3 for 1 x 15360 x 5120; pieces of a warp 512 bytes apart: 18.4).  The products are those of the warp-wide
+// instruction on 16 x 8 x 32 values: memory is the bound (5.5 TB/s with the launch), and tensor memory and its pipeline are set up longer than a small product takes (1 x 4608 x 1536
+// 2.6 us, on tiles of 32 columns 5.9; 8 x 15360 x 5120 15.1, 16.1).  Sums of four bytes at once by the integer units (dp4a) cost 12 cycles each: 14.4 us for one row, 56 for eight.
+// The order in which the values of K are taken is of no account as long as it is the same for both: a lane's 16 neighbouring bytes are four of each quarter of two such products.
+constexpr int kI8Few = 8, kI8FewThreads = 256;
+// bytes at .. k - 1 of a row, less than 16, and zeros (bytes behind a row are not read)
+__device__ __forceinline__ uint4 bytes16(const signed char* row, int at, int k) {
+  uint32_t v[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 16; ++j)
+    if (at + j < k) v[j / 4] |= (uint32_t)(unsigned char)row[at + j] << 8 * (j & 3);
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+// sum += rows g and g + 8 (values lo and hi, 32 of K) times columns g
+__device__ __forceinline__ void mma_16x8x32(int (&sum)[4], uint32_t lo0, uint32_t hi0, uint32_t lo1, uint32_t hi1, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+r"(sum[0]), "+r"(sum[1]), "+r"(sum[2]), "+r"(sum[3]) : "r"(lo0), "r"(hi0), "r"(lo1), "r"(hi1), "r"(b0), "r"(b1));
+}
+template <typename TO>
+__global__ void __launch_bounds__(kI8FewThreads, 4) int8_few_kernel(int m, int n, int k, const __grid_constant__ Int8Arg a, const __grid_constant__ Int8Arg b, const float* n_bias,
+                                                                 TO* __restrict__ c, long long ldc) {
+  constexpr int AHEAD = 5, WARPS = kI8FewThreads / 32;      // pieces of 64 bytes of a row under way
+  __shared__ __align__(16) int part[WARPS][128];
+  grid_enter();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, row = blockIdx.x * 16 + g;
+  const signed char* const lo = b.values + min(row, n - 1) * b.ld;
+  const signed char* const hi = b.values + min(row + 8, n - 1) * b.ld;
+  const signed char* const x = a.values + min(g, m - 1) * a.ld;      // (columns behind m: not stored)
+  int sum[4] = {0, 0, 0, 0};
+  auto add = [&](const uint4& u, const uint4& v, const uint4& y) {
+    mma_16x8x32(sum, u.x, v.x, u.y, v.y, y.x, y.y);
+    mma_16x8x32(sum, u.z, v.z, u.w, v.w, y.z, y.w);
+  };
+  // rounds of `per` pieces a warp, next to one another in a row
+  const int pieces = (k + 63) / 64, per = min(AHEAD, (pieces + WARPS - 1) / WARPS), in = (lane & 3) * 16;
+#pragma unroll 1
+  for (int first = warp * per; first < pieces; first += WARPS * per) {
+    uint4 u[AHEAD], v[AHEAD];
+    const int at = first * 64 + in;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const bool there = i < per && at + i * 64 + 16 <= k;
+      u[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (there) {
+        u[i] = *reinterpret_cast<const uint4*>(lo + at + i * 64);
+        v[i] = *reinterpret_cast<const uint4*>(hi + at + i * 64);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      uint4 y = make_uint4(0u, 0u, 0u, 0u);
+      if (i < per && at + i * 64 + 16 <= k) y = *reinterpret_cast<const uint4*>(x + at + i * 64);
+      if (i < per) add(u[i], v[i], y);
+    }
+  }
+  if (warp == WARPS - 1 && k % 16 != 0) {      // what is behind the last whole 16
+    const int at = in == 0 ? k / 16 * 16 : k;
+    add(bytes16(lo, at, k), bytes16(hi, at, k), bytes16(x, at, k));
+  }
+  // the warps' parts: row g (+ 8), columns 2 (lane % 4), + 1
+  *reinterpret_cast<int2*>(&part[warp][g * 8 + (lane & 3) * 2]) = make_int2(sum[0], sum[1]);
+  *reinterpret_cast<int2*>(&part[warp][(g + 8) * 8 + (lane & 3) * 2]) = make_int2(sum[2], sum[3]);
+  __syncthreads();
+  const int i = threadIdx.x >> 4, col = blockIdx.x * 16 + (threadIdx.x & 15);      // (16 neighbouring results of a row of C)
+  if (i >= m || i >= kI8Few || col >= n) return;
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) total += part[w][(threadIdx.x & 15) * 8 + i];
+  put(c + i * ldc + col, finished(total, a.scales[i], b.scales[col], n_bias != nullptr ? n_bias[col] : 0.f));
+}
+
 // One call
 struct I8Call {
   int m, n, k, kb, ctas;
@@ -413,6 +485,11 @@ cudaError_t launch_i8(const I8Call& c, const I8Plan& plan) {
                                reinterpret_cast<bf16*>(c.c), c.ldc);
 }
 
+template <typename TO>
+cudaError_t launch_few(const I8Call& c) {
+  return launch_kernel(int8_few_kernel<TO>, (c.n + 15) / 16, kI8FewThreads, 0, c.st, c.m, c.n, c.k, c.a, c.b, c.bias, reinterpret_cast<TO*>(c.c), c.ldc);
+}
+
 // The kernel of a call: columns of a tile, CTAs that share one, which operand's rows are its lanes.  `pairs`: takes_pairs, and the context has room for one
 struct I8Choice {
   int columns, pair;
@@ -471,6 +548,7 @@ cudaError_t launch_int8_matmul(int m, int n, int k, const Int8Arg& a, const Int8
   call.status = reinterpret_cast<StatusBlock*>(ws);
   call.parts = reinterpret_cast<int*>(ws + align_up(sizeof(StatusBlock), 256));
   call.st = st;
+  if (m <= kI8Few) return call.f32 ? launch_few<float>(call) : launch_few<bf16>(call);
   bool pairs = takes_pairs(call);
   if (pairs) {
     static ClusterRoom room;

@@ -101,6 +101,23 @@ def test_products(m, n, k, dtype):
     assert vb.vsa2_device_status(ws) == vb.OK
 
 
+@pytest.mark.parametrize("m", [1, 2, 3, 4, 7, 8, 9])
+@pytest.mark.parametrize("n", [1, 15, 16, 17, 1000])
+@pytest.mark.parametrize("k", [1, 15, 16, 17, 63, 64, 65, 500, 512, 2561, 5120])
+def test_few_rows(m, n, k):
+    gen = torch.Generator(device="cuda").manual_seed(m + 3 * n + 7 * k)
+    a, b = operand(gen, m, k), operand(gen, n, k)
+    bias = torch.randn(n, generator=gen, device="cuda")
+    room = torch.full((m, n + 3), 7.0, device="cuda")
+    ws = vb.int8_matmul_workspace(m, n, k)
+    vb.vsa2_int8_matmul(a, b, room[:, 1:1 + n], ws)
+    assert torch.equal(room[:, 1:1 + n], expected(a, b, None, F)) and (room[:, 0] == 7).all() and (room[:, 1 + n:] == 7).all()
+    c = torch.empty(m, n, dtype=BF, device="cuda")
+    vb.vsa2_int8_matmul(a, b, c, ws, bias=bias)
+    want = expected(a, b, bias, BF)
+    assert ((c.double() - want.double()).abs() <= 2.0 ** -7 * want.double().abs()).all()
+
+
 @pytest.mark.parametrize("m,n,k", [(3, 200, 131071), (300, 600, 131071)])
 def test_the_largest_sums(m, n, k):
     gen = torch.Generator(device="cuda").manual_seed(1)
