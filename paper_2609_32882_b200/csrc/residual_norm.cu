@@ -93,15 +93,17 @@ __device__ __forceinline__ void weights_at(float2 (&w)[4], const float* p) {
   w[0] = make_float2(a.x, a.y); w[1] = make_float2(a.z, a.w);
   w[2] = make_float2(b.x, b.y); w[3] = make_float2(b.z, b.w);
 }
-__device__ const float kOnes[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+__device__ const __align__(16) float kOnes[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
 template <int LIE>
 __device__ __forceinline__ void weight_of(float2 (&w)[4], const float* from, int i, int cols) {
   if (LIE != ROWS_ANY) {
     weights_at(w, element(from != nullptr ? from : kOnes, from != nullptr && (LIE == ROWS_WHOLE || i < cols) ? i : 0));
+  } else if (from == nullptr || i >= cols || (i + 8 <= cols && (reinterpret_cast<uintptr_t>(from) & 15u) == 0)) {
+    weights_at(w, from == nullptr || i >= cols ? kOnes : element(from, i));
   } else {
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = from != nullptr && i + j < cols ? from[i + j] : 1.f;
+    for (int j = 0; j < 8; ++j) v[j] = i + j < cols ? from[i + j] : 1.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = make_float2(v[2 * j], v[2 * j + 1]);
   }
@@ -223,6 +225,18 @@ __device__ __forceinline__ void put_bytes(uint2 q, unsigned char* row, int i, in
   if (LIE == ROWS_WHOLE) *reinterpret_cast<uint2*>(element(row, i)) = q;
   else if (i < cols) put8(row, i, cols, q.x, q.y);
 }
+// Pieces of fp32 numbers on their way to a row of another type, one after the other
+template <typename T>
+struct Outgoing {
+  Eight<T> before;
+  template <int LIE, int V>
+  __device__ __forceinline__ void store(const float (&f)[8], int v, T* row, int i, int cols) {
+    Eight<T> e;
+    e.round(f);
+    store_eight<LIE, V>(e, v > 0 ? before : e, v, row, i, cols);
+    if (LIE == ROWS_ANY) before = e;
+  }
+};
 // h of a piece: x through the dropout, plus the residual (in h), rounded to the stream's type
 template <typename X, typename S>
 __device__ __forceinline__ void combine(Eight<S>& h, const Eight<X>& x, bool residual, const DropMask& mask, int row, int oct) {
@@ -281,7 +295,7 @@ __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_con
     auto keep = [&](int first) {
       if (!NORM || a.h.p == nullptr) return;
 #pragma unroll
-      for (int v = 0; v < V; ++v) store_eight<LIE>(h[v], reinterpret_cast<S*>(a.h.p) + row * a.h.ld, (first + mine + 32 * v) * 8, a.cols);
+      for (int v = 0; v < V; ++v) store_eight<LIE, V>(h[v], h[v > 0 ? v - 1 : 0], v, reinterpret_cast<S*>(a.h.p) + row * a.h.ld, (first + mine + 32 * v) * 8, a.cols);
     };
     auto apply_power = [&] {
       if (power == 1.f) return;
@@ -334,6 +348,8 @@ __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_con
     }
     const float factor = int8 ? int8_factor(top) : 0.f;
     uint32_t scales = 0u;
+    Outgoing<float> y_wide;
+    Outgoing<bf16> y_narrow;
 #pragma unroll 1
     for (int i = 0; i < rounds; ++i) {
       const int first = i * T * V;
@@ -370,8 +386,8 @@ __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_con
             g[2 * j] = f[j].x * r;
             g[2 * j + 1] = f[j].y * r;
           }
-          if (a.y_f32) store_floats<LIE>(g, reinterpret_cast<float*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
-          else store_floats<LIE>(g, reinterpret_cast<bf16*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
+          if (a.y_f32) y_wide.store<LIE, V>(g, v, reinterpret_cast<float*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
+          else y_narrow.store<LIE, V>(g, v, reinterpret_cast<bf16*>(a.y.p) + row * a.y.ld, oct * 8, a.cols);
         }
       }
     }
@@ -465,6 +481,9 @@ __global__ void __maxnreg__(V == 1 ? 64 : 96) norm_bwd_kernel(const __grid_const
       if (!MANY) apply_power();
     }
     const float out = r * power;
+    Outgoing<S> dr;
+    Outgoing<float> dx_wide;
+    Outgoing<bf16> dx_narrow;
 #pragma unroll 1
     for (int i = 0; i < rounds; ++i) {
       const int first = i * T * V;
@@ -479,11 +498,11 @@ __global__ void __maxnreg__(V == 1 ? 64 : 96) norm_bwd_kernel(const __grid_const
         float2 w[4];
         weight_of<LIE>(w, a.w, oct * 8, a.cols);
         gradient_piece(f, h[v], dy[v], dh[v], stream, w, dw[v], r, out, along);
-        if (a.dr.p != nullptr) store_floats<LIE>(f, reinterpret_cast<S*>(a.dr.p) + row * a.dr.ld, oct * 8, a.cols);
+        if (a.dr.p != nullptr) dr.template store<LIE, V>(f, v, reinterpret_cast<S*>(a.dr.p) + row * a.dr.ld, oct * 8, a.cols);
         if (a.dx.p != nullptr) {
           mask.apply(f, row, oct);
-          if (a.dx_f32) store_floats<LIE>(f, reinterpret_cast<float*>(a.dx.p) + row * a.dx.ld, oct * 8, a.cols);
-          else store_floats<LIE>(f, reinterpret_cast<bf16*>(a.dx.p) + row * a.dx.ld, oct * 8, a.cols);
+          if (a.dx_f32) dx_wide.store<LIE, V>(f, v, reinterpret_cast<float*>(a.dx.p) + row * a.dx.ld, oct * 8, a.cols);
+          else dx_narrow.store<LIE, V>(f, v, reinterpret_cast<bf16*>(a.dx.p) + row * a.dx.ld, oct * 8, a.cols);
         }
         if (MANY) {
           if (part != nullptr && oct < a.octs) {
@@ -606,7 +625,9 @@ cudaError_t lie_bwd(const NormBwdArgs& a, float* dw, cudaStream_t st) {
 }
 template <typename S, typename G>
 cudaError_t size_bwd(const NormBwdArgs& a, bool vec, float* dw, cudaStream_t st) {
-  if (!vec) return a.octs <= 2 * kNormMost ? go_bwd<2, false, S, G, ROWS_ANY>(a, dw, st) : go_bwd<1, true, S, G, ROWS_ANY>(a, dw, st);
+  if (!vec)
+    return a.octs <= kNormMost ? go_bwd<1, false, S, G, ROWS_ANY>(a, dw, st) : a.octs <= 2 * kNormMost ? go_bwd<2, false, S, G, ROWS_ANY>(a, dw, st)
+                                                                                                       : go_bwd<1, true, S, G, ROWS_ANY>(a, dw, st);
   if (a.octs <= kNormMost) return lie_bwd<1, S, G>(a, dw, st);
   return a.octs <= 2 * kNormMost ? lie_bwd<2, S, G>(a, dw, st) : go_bwd<1, true, S, G, ROWS_ALIGNED>(a, dw, st);
 }

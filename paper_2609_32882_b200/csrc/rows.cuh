@@ -110,7 +110,28 @@ enum { ROWS_ANY = 0, ROWS_ALIGNED = 1, ROWS_WHOLE = 2 };
 // element i of a row that is the same for all threads: a base of 64 bits and a thread's offset of 32 (2^22 elements at most), which a load adds by itself
 template <typename T>
 __device__ __forceinline__ T* element(T* row, int i) { return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + (uint32_t)i * (uint32_t)sizeof(T)); }
-// Elements i .. i+7 of a row (zeros behind it, and for i beyond it)
+// 16 bytes (bf16), or 32, that begin `shift` bytes (even, up to 16) into some words, of which those beyond the first 16 (32) matter only up to there
+__device__ __forceinline__ void shifted(Eight<bf16>& e, const uint32_t (&w)[8], uint32_t shift) {
+  uint32_t a[6], b[5];
+#pragma unroll
+  for (int k = 0; k < 6; ++k) a[k] = shift & 8 ? w[k + 2] : w[k];
+#pragma unroll
+  for (int k = 0; k < 5; ++k) b[k] = shift & 4 ? a[k + 1] : a[k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) e.u[k] = shift & 16 ? w[k + 4] : __funnelshift_r(b[k], b[k + 1], (shift & 2) * 8);
+}
+__device__ __forceinline__ void shifted(Eight<float>& e, const uint32_t (&w)[12], uint32_t shift) {      // (a multiple of four)
+  uint32_t a[10];
+#pragma unroll
+  for (int k = 0; k < 10; ++k) a[k] = shift & 8 ? w[k + 2] : w[k];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) e.f[k] = __uint_as_float(shift & 16 ? w[k + 4] : shift & 4 ? a[k + 1] : a[k]);
+}
+__device__ __forceinline__ uint32_t word_of(const Eight<bf16>& e, int k) { return e.u[k]; }
+__device__ __forceinline__ uint32_t word_of(const Eight<float>& e, int k) { return __float_as_uint(e.f[k]); }
+
+// Elements i .. i+7 of a row (zeros behind it, and for i beyond it).  Rows that lie anywhere: the aligned 16-byte places that the piece lies in, where the row has all of them, shifted into
+// place; single elements at a row's two ends
 template <int LIE, typename T>
 __device__ __forceinline__ void load_eight(Eight<T>& e, const T* row, int i, int cols) {
   if (LIE == ROWS_WHOLE) {
@@ -119,27 +140,60 @@ __device__ __forceinline__ void load_eight(Eight<T>& e, const T* row, int i, int
     if (i < cols) e.load(element(row, i));
     else e.zero();
   } else {
-    e.zero();
+    constexpr int SIZE = sizeof(T), PLACES = SIZE / 2;      // of 16 bytes in a piece
+    const T* const at = element(row, i);
+    const int s = (int)(reinterpret_cast<uintptr_t>(at) & 15u), left = cols - i;
+    if (i * SIZE >= s && left * SIZE + s >= 16 * (PLACES + 1)) {
+      const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(at) - s);
+      uint32_t w[4 * PLACES + 4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (i + j < cols) e.set(j, row + i + j);
+      for (int k = 0; k <= PLACES; ++k) {
+        const uint4 v = from[k];
+        w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
+      }
+      shifted(e, w, (uint32_t)s);      // (whole: more than eight elements are left)
+    } else {
+      e.zero();
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < left) e.set(j, at + j);
+    }
   }
 }
-template <int LIE, typename T>
-__device__ __forceinline__ void store_eight(const Eight<T>& e, T* row, int i, int cols) {
+// .. back to a row.  By whole warps: a warp's pieces lie next to one another, 32 of number v and then those of number v + 1 (`before`: this thread's of number v - 1).  Rows that lie anywhere:
+// a thread stores the aligned places that end in its piece, with what it is told of the piece before, where the row has all of them; single elements at the ends of a row and of a
+// warp's pieces
+template <int LIE, int V, typename T>
+__device__ __forceinline__ void store_eight(const Eight<T>& e, const Eight<T>& before, int v, T* row, int i, int cols) {
   if (LIE != ROWS_ANY) {
     if (LIE == ROWS_WHOLE || i < cols) e.store(element(row, i));
   } else {
+    constexpr int SIZE = sizeof(T), PLACES = SIZE / 2, WORDS = 4 * PLACES;
+    const int lane = threadIdx.x & 31;
+    T* const at = element(row, i);
+    const int s = (int)(reinterpret_cast<uintptr_t>(at) & 15u);      // (the same for the whole row)
+    uint32_t w[WORDS + 4];      // the 16 bytes in front of the piece, and it
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (i + j < cols) e.store(row + i + j, j);
+    for (int k = 0; k < 4; ++k) w[k] = __shfl_sync(0xffffffffu, lane == 31 && v > 0 ? word_of(before, WORDS - 4 + k) : word_of(e, WORDS - 4 + k), (lane + 31) & 31);
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k) w[4 + k] = word_of(e, k);
+    Eight<T> out;
+    shifted(out, w, 16u - s);
+    const int first = i - s / SIZE;      // element that it begins with
+    const bool told = s == 0 || v > 0 || lane > 0;
+    if (told && first >= 0 && first + 8 <= cols) {
+      out.store(reinterpret_cast<T*>(reinterpret_cast<char*>(at) - s));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (first + j >= 0 && first + j < cols && (told || j * SIZE >= s)) out.store(at - s / SIZE + j, j);
+    }
+    if (v == V - 1 && lane == 31) {      // what the places leave of the warp's last piece
+#pragma unroll
+      for (int j = 1; j < 8; ++j)
+        if ((8 - j) * SIZE <= s && i + j < cols) e.store(at + j, j);
+    }
   }
-}
-template <int LIE, typename T>
-__device__ __forceinline__ void store_floats(const float (&f)[8], T* row, int i, int cols) {
-  Eight<T> e;
-  e.round(f);
-  store_eight<LIE>(e, row, i, cols);
 }
 
 // f plus e, each sum rounded

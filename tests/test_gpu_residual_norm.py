@@ -213,3 +213,46 @@ def test_sizes_of_zero():
         ws = torch.empty(vb.vsa2_residual_norm_bwd_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
         vb.vsa2_residual_norm_bwd(x, x, d_residual=torch.empty_like(x), d_weight=dw, workspace=ws)
         assert (dw == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("cols", [1, 7, 9, 250, 255, 511, 1024, 2041, 2047, 2049, 4100, 8191, 8200, 9000])
+def test_rows_at_every_address(dtype, cols):
+    """Matrices of one odd stride whose rows begin at every offset from a 16-byte boundary; what lies around the rows stays, also in place."""
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    rows, ld = 17, cols + 5 + cols % 2
+    rooms = [make(rows + 1, ld, dtype, gen) for _ in range(3)]
+    view = lambda room, skip: torch.as_strided(room, (rows, cols), (ld, 1), skip)
+    for skip in (0, 1, 3):
+        x, r = view(rooms[0], skip), view(rooms[1], (skip + 2) % 5)
+        out = torch.full_like(rooms[2], 7.0)
+        y = view(out, (skip + 1) % 4)
+        keep = out.clone()
+        h = torch.empty(rows, cols, dtype=dtype, device="cuda")
+        vb.vsa2_residual_norm_fwd(x, r, None, h=h, y=y, p=0.25, rng=rng_of(skip, 1))
+        want_h = ref.stream(x, r, ref.factors(skip, 1, rows, cols, 0.25))
+        assert torch.equal(h, want_h)
+        want, _ = ref.normed(want_h, None, 1e-6)
+        assert ((y.double() - want).abs() <= (FINE + half_step(dtype)) * want.abs() + 1e-37).all()
+        y.copy_(view(keep, (skip + 1) % 4))
+        assert torch.equal(out, keep)                             # nothing else was written
+        again = rooms[1].clone()
+        stream = view(again, (skip + 2) % 5)
+        vb.vsa2_residual_norm_fwd(x, stream, None, h=stream, p=0.25, rng=rng_of(skip, 1))
+        assert torch.equal(stream, want_h)
+        stream.copy_(r)
+        assert torch.equal(again, rooms[1])
+        dr = view(out, (skip + 1) % 4)
+        vb.vsa2_residual_norm_bwd(h, x, r, d_residual=dr)
+        grad, _, size, _ = ref.gradients(h, x, r, None, 1e-6)
+        assert ((dr.double() - grad).abs() <= 2 * FINE * size + half_step(dtype) * grad.abs() + 1e-37).all()
+        dr.copy_(view(keep, (skip + 1) % 4))
+        assert torch.equal(out, keep)
+        d = view(out, (skip + 3) % 6)
+        vb.vsa2_dropout(x, d, 0.5, rng_of(skip, 2), residual=r)
+        assert torch.equal(d, (r.float() + ref.dropped(x, ref.factors(skip, 2, rows, cols, 0.5))).to(dtype))
+        d.copy_(view(keep, (skip + 3) % 6))
+        assert torch.equal(out, keep)
+        q = vb.Int8.empty(rows, cols)
+        vb.vsa2_int8_quantize(x, q)
+        assert torch.equal(q.values, ref.int8_of(x.float())[0])
