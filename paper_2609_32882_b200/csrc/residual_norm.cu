@@ -396,10 +396,12 @@ __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_con
 }
 
 // Any rows.  MANY: the sums of the weight's gradient are kept in the CTA's row of `parts`, where a thread finds its own again; else in registers
-// V: pieces of a thread, one where they suffice: each has its sums of the weight's gradient in registers, and with two there is room for half the warps (65972 x 1536 in fp32 254 us, with two
-// 284 in the same registers).  Two take 96 registers, with which an SM holds two CTAs of 320 threads (75600 x 5120 572 us, in 104 registers 889).
+// V: pieces of a thread, one up to 2048 elements of bf16 and 4096 of fp32, where it is faster or as fast: each has its sums of the weight's gradient in registers, which leave room for
+// fewer warps (30000 x 1536 bf16 67.9 us, with two 72.2; in fp32 116.8, 126.5; 20000 x 4096 bf16 141.5, 135.7).  Two take 96 registers, with which an SM holds two CTAs of 320 threads
+// (75600 x 5120 572 us, in 104 registers 889).  One piece of bf16 takes 80, and has the next row under way (without it, in 64 registers: 30000 x 1536 77.6 us instead of 67.9, 60000 x 640 87.7
+// instead of 69.5); in fp32 that has no room (65972 x 1536 281 us, without 255).
 template <int V, bool MANY, typename S, typename G, int LIE>
-__global__ void __maxnreg__(V == 1 ? 64 : 96) norm_bwd_kernel(const __grid_constant__ NormBwdArgs a) {
+__global__ void __maxnreg__(V == 2 ? 96 : sizeof(S) == 2 ? 80 : 64) norm_bwd_kernel(const __grid_constant__ NormBwdArgs a) {
   __shared__ __align__(16) RowSums sh;
   sh.init();
   grid_enter();
@@ -423,27 +425,38 @@ __global__ void __maxnreg__(V == 1 ? 64 : 96) norm_bwd_kernel(const __grid_const
     }
     return e;
   };
+  constexpr bool AHEAD = V == 1 && !MANY && sizeof(S) == 2;      // the next row is asked for before this one is looked at
+  Eight<S> h[V], dh[V];
+  Eight<G> dy[V];
+  auto fetch = [&](Eight<S> (&to_h)[V], Eight<G> (&to_dy)[V], Eight<S> (&to_dh)[V], int row, int first, bool both) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) load_eight<LIE>(to_h[v], reinterpret_cast<const S*>(a.h.p) + row * a.h.ld, (first + mine + 32 * v) * 8, a.cols);
+#pragma unroll
+    for (int v = 0; v < V; ++v) load_eight<LIE>(to_dy[v], reinterpret_cast<const G*>(a.dy.p) + row * a.dy.ld, (first + mine + 32 * v) * 8, a.cols);
+    if (both && stream) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) load_eight<LIE>(to_dh[v], reinterpret_cast<const S*>(a.dh.p) + row * a.dh.ld, (first + mine + 32 * v) * 8, a.cols);
+    }
+  };
+  Eight<S> next_h[V], next_dh[V];
+  Eight<G> next_dy[V];
+  if (AHEAD) fetch(next_h, next_dy, next_dh, blockIdx.x, 0, true);
   uint32_t turn = 0;
   for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    Eight<S> h[V], dh[V];
-    Eight<G> dy[V];
     float power = 1.f;
     auto apply_power = [&] {
       if (power == 1.f) return;
 #pragma unroll
       for (int v = 0; v < V; ++v) rescale(h[v], power);
     };
-    auto fetch = [&](int first, bool both) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) load_eight<LIE>(h[v], reinterpret_cast<const S*>(a.h.p) + row * a.h.ld, (first + mine + 32 * v) * 8, a.cols);
-#pragma unroll
-      for (int v = 0; v < V; ++v) load_eight<LIE>(dy[v], reinterpret_cast<const G*>(a.dy.p) + row * a.dy.ld, (first + mine + 32 * v) * 8, a.cols);
-      if (both && stream) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) load_eight<LIE>(dh[v], reinterpret_cast<const S*>(a.dh.p) + row * a.dh.ld, (first + mine + 32 * v) * 8, a.cols);
-      }
-    };
-    if (!MANY) fetch(0, true);
+    if (AHEAD) {
+      h[0] = next_h[0];
+      dy[0] = next_dy[0];
+      dh[0] = next_dh[0];
+      if (row + (int)gridDim.x < a.rows) fetch(next_h, next_dy, next_dh, row + gridDim.x, 0, true);
+    } else if (!MANY) {
+      fetch(h, dy, dh, row, 0, true);
+    }
     float r, eps = a.eps, along;
     bool again = false;
 #pragma unroll 1
@@ -453,7 +466,7 @@ __global__ void __maxnreg__(V == 1 ? 64 : 96) norm_bwd_kernel(const __grid_const
       for (int i = 0; i < rounds; ++i) {
         const int first = i * T * V;
         if (MANY) {
-          fetch(first, false);
+          fetch(h, dy, dh, row, first, false);
           apply_power();
         }
 #pragma unroll
@@ -472,7 +485,7 @@ __global__ void __maxnreg__(V == 1 ? 64 : 96) norm_bwd_kernel(const __grid_const
       float size = 0.f;
 #pragma unroll 1
       for (int i = 0; i < rounds; ++i) {
-        if (MANY) fetch(i * T * V, false);
+        if (MANY) fetch(h, dy, dh, row, i * T * V, false);
 #pragma unroll
         for (int v = 0; v < V; ++v) size = largest_of(h[v], size);
       }
@@ -488,7 +501,7 @@ __global__ void __maxnreg__(V == 1 ? 64 : 96) norm_bwd_kernel(const __grid_const
     for (int i = 0; i < rounds; ++i) {
       const int first = i * T * V;
       if (MANY) {
-        fetch(first, true);
+        fetch(h, dy, dh, row, first, true);
         apply_power();
       }
 #pragma unroll
@@ -628,7 +641,7 @@ cudaError_t size_bwd(const NormBwdArgs& a, bool vec, float* dw, cudaStream_t st)
   if (!vec)
     return a.octs <= kNormMost ? go_bwd<1, false, S, G, ROWS_ANY>(a, dw, st) : a.octs <= 2 * kNormMost ? go_bwd<2, false, S, G, ROWS_ANY>(a, dw, st)
                                                                                                        : go_bwd<1, true, S, G, ROWS_ANY>(a, dw, st);
-  if (a.octs <= kNormMost) return lie_bwd<1, S, G>(a, dw, st);
+  if (a.octs <= (sizeof(S) == 2 ? kNormMost / 2 : kNormMost)) return lie_bwd<1, S, G>(a, dw, st);
   return a.octs <= 2 * kNormMost ? lie_bwd<2, S, G>(a, dw, st) : go_bwd<1, true, S, G, ROWS_ALIGNED>(a, dw, st);
 }
 
