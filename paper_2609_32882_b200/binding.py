@@ -384,7 +384,8 @@ def _marshal():
         module.bind((torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn, torch.uint8),
                     at(lib.vsa2_rope_apply, lib.vsa2_qkv_fwd, lib.vsa2_qkv_bwd, lib.vsa2_fp8_quantize, lib.vsa2_fp8_matmul), _stream)
         module.bind_rows((torch.int8, torch.int64), at(lib.vsa2_residual_norm_fwd, lib.vsa2_residual_norm_bwd, lib.vsa2_dropout, lib.vsa2_int8_quantize,
-                                                       lib.vsa2_int8_matmul), getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device)
+                                                       lib.vsa2_int8_matmul),
+                         getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream", None))
         _MARSHAL = module
     return _MARSHAL
 

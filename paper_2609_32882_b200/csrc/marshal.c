@@ -11,7 +11,7 @@
 
 /* names, torch's types (bind), the library's functions (bind) */
 static PyObject *n_shape, *n_stride, *n_dtype, *n_is_cuda, *n_data_ptr, *n_is_contiguous, *n_numel, *n_nbytes, *n_values, *n_scales, *n_get_device;
-static PyObject *t_bf16, *t_f32, *t_i32, *t_e4m3, *t_u8, *t_i8, *t_i64, *stream_of, *device_of;
+static PyObject *t_bf16, *t_f32, *t_i32, *t_e4m3, *t_u8, *t_i8, *t_i64, *stream_of, *device_of, *raw_stream;
 static int (*f_rope_apply)(const vsa2_rope*, const vsa2_place*, const vsa2_heads*, const vsa2_heads*, int32_t, void*);
 static int (*f_qkv_fwd)(const vsa2_rope*, const vsa2_place*, const vsa2_qk_norm*, const vsa2_heads*, const vsa2_heads*, void*);
 static int (*f_qkv_bwd)(const vsa2_rope*, const vsa2_place*, const vsa2_qk_norm*, const vsa2_heads*, const vsa2_heads*, const vsa2_heads*, float*, float*, void*,
@@ -377,20 +377,39 @@ static PyObject* check_fp8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 
 /* ---- the residual stream.  Its calls look at every tensor's device: the library runs on the current one, where another's addresses mean nothing */
-static int here(PyObject* t, int64_t* device) { /* of a CUDA tensor; *device: the current one, -1 before it was asked for */
-  int64_t of;
-  if ((*device < 0 && number(PyObject_CallNoArgs(device_of), device)) || number(PyObject_CallMethodNoArgs(t, n_get_device), &of)) return -1;
+static int here(PyObject* t, int64_t* device) { /* *device: the current one, -1 before it was asked for */
+  int64_t of; /* -1: not a CUDA tensor's */
+  if (number(PyObject_CallMethodNoArgs(t, n_get_device), &of)) return -1;
+  if (of < 0) return refuse("expected a CUDA tensor");
+  if (*device < 0 && number(PyObject_CallNoArgs(device_of), device)) return -1;
   return of == *device ? 0 : refuse("tensors must be on the current CUDA device");
+}
+/* the stream of a call whose tensors were looked at: None is the device's current one, without the detour through the binding's function (0.7 us) */
+static int stream_here(PyObject* s, int64_t device, void** out) {
+  if (s != Py_None || raw_stream == Py_None || device < 0) return get_stream(s, out);
+  PyObject *d = PyLong_FromLongLong(device), *v = d != NULL ? PyObject_CallOneArg(raw_stream, d) : NULL;
+  Py_XDECREF(d);
+  if (v == NULL) return -1;
+  *out = PyLong_AsVoidPtr(v);
+  Py_DECREF(v);
+  return *out == NULL && PyErr_Occurred() ? -1 : 0;
 }
 /* a matrix of the call's shape (the first sets it: rows < 0), None: absent */
 static int get_rows(PyObject* t, int64_t* device, int64_t* shape, vsa2_rows* r, const vsa2_rows** out) {
-  int64_t of[2];
+  static const char* const what = "expected a CUDA matrix with contiguous rows";
+  int64_t of[2], stride[2];
   *out = NULL;
   if (t == Py_None) return 0;
-  if (get_matrix(t, of, &r->ld, &r->dtype, &r->data) || here(t, device)) return -1;
+  const int n = integers(PyObject_GetAttr(t, n_shape), of, 2);
+  if (n < 0) return -1;
+  if (n != 2) return refuse(what);
+  if (here(t, device) || integers(PyObject_CallMethodNoArgs(t, n_stride), stride, 2) != 2) return -1;
+  if (of[1] > 1 && stride[1] != 1) return refuse(what);
   if (shape[0] >= 0 && (of[0] != shape[0] || of[1] != shape[1])) return refuse("the matrices of a call must have one shape");
-  shape[0] = of[0]; shape[1] = of[1];
+  if (fits_int(of, 2) || float_type(t, &r->dtype) || address(t, &r->data)) return -1;
+  r->ld = of[0] > 1 ? stride[0] : of[1];
   r->reserved = 0;
+  shape[0] = of[0]; shape[1] = of[1];
   *out = r;
   return 0;
 }
@@ -433,8 +452,8 @@ static int get_int8(PyObject* o, int64_t* device, vsa2_int8* v, int64_t* shape) 
   int64_t stride[2];
   void* scales;
   PyObject *values = PyObject_GetAttr(o, n_values), *s = values != NULL ? PyObject_GetAttr(o, n_scales) : NULL;
-  if (s == NULL || on_gpu(values, "expected a CUDA tensor") || int8_form(values, s, shape, stride) || fits_int(shape, 2) || address(values, &v->values) ||
-      get_memory(s, &scales, NULL) || here(values, device) || here(s, device))
+  if (s == NULL || here(values, device) || here(s, device) || int8_form(values, s, shape, stride) || fits_int(shape, 2) || address(values, &v->values) ||
+      get_memory(s, &scales, NULL))
     goto out;
   v->scales = (float*)scales;
   v->ld = shape[0] > 1 ? stride[0] : (shape[1] + 15) / 16 * 16;
@@ -477,7 +496,7 @@ static PyObject* norm_fwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
       get_drop(a[8], a[9], &device, &store, &drop))
     return NULL;
   const double eps = PyFloat_AsDouble(a[3]);
-  if ((eps == -1.0 && PyErr_Occurred()) || get_stream(a[10], &stream)) return NULL;
+  if ((eps == -1.0 && PyErr_Occurred()) || stream_here(a[10], device, &stream)) return NULL;
   CALLED(f_norm_fwd((int32_t)shape[0], (int32_t)shape[1], x, r, drop, w, (float)eps, h, y, a[6] != Py_None ? &fp8 : NULL, a[7] != Py_None ? &int8 : NULL,
                     stream));
 }
@@ -502,7 +521,7 @@ static PyObject* norm_bwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
       (a[8] != Py_None && here(a[8], &device)) || get_drop(a[9], a[10], &device, &store, &drop))
     return NULL;
   const double eps = PyFloat_AsDouble(a[4]);
-  if ((eps == -1.0 && PyErr_Occurred()) || get_stream(a[11], &stream)) return NULL;
+  if ((eps == -1.0 && PyErr_Occurred()) || stream_here(a[11], device, &stream)) return NULL;
   CALLED(f_norm_bwd((int32_t)shape[0], (int32_t)shape[1], h, dy, dh, drop, w, (float)eps, dr, dx, dw, workspace, bytes, stream));
 }
 /* (x, y, p, rng, residual, stream) */
@@ -514,7 +533,7 @@ static PyObject* dropout(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   const vsa2_drop* drop;
   void* stream;
   if (arguments(n, 6) || get_rows(a[0], &device, shape, &m[0], &x) || get_rows(a[1], &device, shape, &m[1], &y) ||
-      get_rows(a[4], &device, shape, &m[2], &r) || get_drop(a[2], a[3], &device, &store, &drop) || get_stream(a[5], &stream))
+      get_rows(a[4], &device, shape, &m[2], &r) || get_drop(a[2], a[3], &device, &store, &drop) || stream_here(a[5], device, &stream))
     return NULL;
   CALLED(f_dropout((int32_t)shape[0], (int32_t)shape[1], x, r, drop, y, stream));
 }
@@ -526,7 +545,7 @@ static PyObject* int8_quantize(PyObject* self, PyObject* const* a, Py_ssize_t n)
   vsa2_int8 out;
   void* stream;
   if (arguments(n, 3) || get_rows(a[0], &device, shape, &m, &x) || get_int8(a[1], &device, &out, of) || one_shape(of, shape) ||
-      get_stream(a[2], &stream))
+      stream_here(a[2], device, &stream))
     return NULL;
   CALLED(f_int8_quantize((int32_t)shape[0], (int32_t)shape[1], x, &out, stream));
 }
@@ -545,7 +564,7 @@ static PyObject* int8_matmul(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     refuse("the shapes of a, b and c do not fit");
     return NULL;
   }
-  if (get_weights(a[4], &device, of_b[0], &bias) || get_stream(a[5], &stream)) return NULL;
+  if (get_weights(a[4], &device, of_b[0], &bias) || stream_here(a[5], device, &stream)) return NULL;
   CALLED(f_int8_matmul((int32_t)of_a[0], (int32_t)of_b[0], (int32_t)of_a[1], &va, &vb, bias, c, type, ld, workspace, bytes, stream));
 }
 /* (values, scales): whether they are a matrix in int8 form */
@@ -579,13 +598,14 @@ static PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   memcpy(&f_matmul, &f[4], sizeof f[0]);
   Py_RETURN_NONE;
 }
-/* ((int8, int64), (addresses of the five functions of the residual stream), function that gives the current device); behind bind */
+/* ((int8, int64), (addresses of the five functions of the residual stream), function that gives the current device, one that gives a device's current stream or None); behind bind */
 static PyObject* bind_rows(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   void* f[5];
-  if (arguments(n, 3) || bound(a[0], a[1], 2, 5, f)) return NULL;
+  if (arguments(n, 4) || bound(a[0], a[1], 2, 5, f)) return NULL;
   Py_XSETREF(t_i8, Py_NewRef(PyTuple_GET_ITEM(a[0], 0)));
   Py_XSETREF(t_i64, Py_NewRef(PyTuple_GET_ITEM(a[0], 1)));
   Py_XSETREF(device_of, Py_NewRef(a[2]));
+  Py_XSETREF(raw_stream, Py_NewRef(a[3]));
   memcpy(&f_norm_fwd, &f[0], sizeof f[0]);
   memcpy(&f_norm_bwd, &f[1], sizeof f[0]);
   memcpy(&f_dropout, &f[2], sizeof f[0]);
