@@ -5,6 +5,10 @@
 //
 // Up to eight rows of A take a kernel of their own (int8_few_kernel).  Otherwise tiles and roles are as in the product of e4m3 matrices (fp8_matmul.cu): B's rows are the 128 rows of a CTA's tile, A's rows its NT columns; pairs of SMs share a tile of 256 x 256
 // where there are rows for it.  No scales go to tensor memory, so the two accumulators have all of it.
+//
+// What bounds it: in long runs the power limit (75600 x 15360 x 5120 4.15 - 4.29 ms, 2.8 PFLOP/s; 18900 rows of it alone 866 us, 3.4 PFLOP/s, tensor pipe busy 93 % of the time);
+// else the intake from L2 (8192 x 4096 x 4096 87 us, 4096^3 48); few tiles and short K: the launch, the first block's way from memory and the last tile's way out (2048 x 4608 x 1536
+// 14.7 us, of which the products need 7).  Asking for the next tile's scales ahead of time, or staging all of a tile's results at once in the place of a stage: no faster, or slower.
 #include "mm_tiles.cuh"
 #include "rows.cuh"
 

@@ -4,9 +4,10 @@
 //   backward: with r = 1 / sqrt(mean(h^2) + eps), g = w dy:  dh' = dh + r g - h r^3 mean(g h);  dx = dropout's part of dh';  dw = sum over the rows of dy h r
 //   int8    : v = h w (for vsa2_int8_quantize a matrix' own values), s = max |v| / 127, value = v * (127 / max |v|) rounded to nearest, ties to even; the row's r is part of its
 //             scale alone, so a value does not depend on how the sum of squares was rounded
-// A CTA takes a row at a time, eight neighbouring elements in each of a thread's pieces.  Rows on 16-byte boundaries whose pieces fit shared memory (the ring kernels): each thread asks
-// for its own pieces of the next row ahead of time, in places that are its own, so that memory is kept busy while a row's sums pass through the CTA's one barrier.  Other rows come as
-// they are needed: of up to 8192 elements they stay in registers, longer ones (MANY) are read twice, the second time from L2.  Bound by memory and, close behind, by issue slots.
+// A CTA takes a row at a time, eight neighbouring elements in each of a thread's pieces; the row is read once and stays in registers while its sums pass through the CTA's one barrier.
+// (Rows of more than 16,384 elements forward and 8192 backward, MANY, are read twice, the second time from L2.)  Bound by memory, and close behind by the issue slots: 75600 x 5120 with
+// residual to e4m3 448 us (6.0 TB/s), 65972 x 1536 fp32 with dropout to bf16 and e4m3 219 us (6.0), its backward 255 - 275 us (5.9 - 6.4), int8 of 15360 x 5120 42 us (5.6).  With few rows
+// it is the latency of one: a token to int8 2.6 us, 2048 x 1536 backward 12.8 us in two kernels.
 #include "fp8_values.cuh"
 #include "rows.cuh"
 
