@@ -238,13 +238,13 @@ struct Outgoing {
     if (LIE == ROWS_ANY) before = e;
   }
 };
-// h of a piece: x through the dropout, plus the residual (in h), rounded to the stream's type
+// h of a piece: x through the dropout (`words`: the generator's, where there is one), plus the residual (in h), rounded to the stream's type
 template <typename X, typename S>
-__device__ __forceinline__ void combine(Eight<S>& h, const Eight<X>& x, bool residual, const DropMask& mask, int row, int oct) {
+__device__ __forceinline__ void combine(Eight<S>& h, const Eight<X>& x, bool residual, const DropMask& mask, const uint32_t (&words)[4]) {
   float f[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) f[j] = x.get(j);
-  mask.apply(f, row, oct);
+  if (mask.limit != 0) mask.keep(f, words);
   if (residual) add_eight(f, h);
   h.round(f);
 }
@@ -282,14 +282,29 @@ __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_con
 #pragma unroll
         for (int v = 0; v < V; ++v) load_eight<LIE>(h[v], rp, (first + mine + 32 * v) * 8, a.cols);
       }
+      // (the generator's rounds of all pieces together, where the registers have room: 75600 x 5120 bf16 with dropout 541 us instead of 570, 65972 x 1536 fp32 215 instead of 209)
+      constexpr bool TOGETHER = sizeof(X) + sizeof(S) == 4;
+      uint32_t words[V][4];
+      if (TOGETHER && mask.limit != 0) {
+        uint32_t rows[V], octs[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          rows[v] = row;
+          octs[v] = first + mine + 32 * v;
+        }
+        mask.words(words, rows, octs);
+      }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         if constexpr (sizeof(X) == 2 && sizeof(S) == 2) {
-          if (mask.limit != 0) combine(h[v], x[v], a.r.p != nullptr, mask, row, first + mine + 32 * v);
+          if (mask.limit != 0) combine(h[v], x[v], a.r.p != nullptr, mask, words[v]);
           else if (a.r.p != nullptr) combine_bf16(h[v], x[v]);
           else h[v] = x[v];
         } else {
-          combine(h[v], x[v], a.r.p != nullptr, mask, row, first + mine + 32 * v);
+          uint32_t own[1][4];
+          const uint32_t rows[1] = {(uint32_t)row}, octs[1] = {(uint32_t)(first + mine + 32 * v)};
+          if (mask.limit != 0) mask.words(own, rows, octs);
+          combine(h[v], x[v], a.r.p != nullptr, mask, own[0]);
         }
       }
     };

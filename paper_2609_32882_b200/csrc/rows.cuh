@@ -221,29 +221,46 @@ struct DropMask {
     limit = d.threshold << 16;
     scale = d.scale;
   }
-  // Eight elements: zero, or times the scale.  (A product of its own, not part of a fused one: what the library computes does not depend on what is added behind it.)
-  __device__ __forceinline__ void apply(float (&f)[8], uint32_t row, uint32_t oct) const {
-    if (limit == 0) return;
-    uint32_t a = oct, b = row, c = o0, d = o1, p = k0, q = k1;
+  // The generator's four words for each of N pieces, round by round, so that a round's key is formed once
+  template <int N>
+  __device__ __forceinline__ void words(uint32_t (&w)[N][4], const uint32_t (&row)[N], const uint32_t (&oct)[N]) const {
+    uint32_t p = k0, q = k1;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      w[n][0] = oct[n]; w[n][1] = row[n];
+      w[n][2] = o0; w[n][3] = o1;
+    }
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
-      unsigned long long u, v;
-      asm("mul.wide.u32 %0, %1, %2;" : "=l"(u) : "r"(a), "r"(0xD2511F53u));
-      asm("mul.wide.u32 %0, %1, %2;" : "=l"(v) : "r"(c), "r"(0xCD9E8D57u));
-      a = (uint32_t)(v >> 32) ^ b ^ p;
-      b = (uint32_t)v;
-      c = (uint32_t)(u >> 32) ^ d ^ q;
-      d = (uint32_t)u;
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        unsigned long long u, v;
+        asm("mul.wide.u32 %0, %1, %2;" : "=l"(u) : "r"(w[n][0]), "r"(0xD2511F53u));
+        asm("mul.wide.u32 %0, %1, %2;" : "=l"(v) : "r"(w[n][2]), "r"(0xCD9E8D57u));
+        w[n][0] = (uint32_t)(v >> 32) ^ w[n][1] ^ p;
+        w[n][1] = (uint32_t)v;
+        w[n][2] = (uint32_t)(u >> 32) ^ w[n][3] ^ q;
+        w[n][3] = (uint32_t)u;
+      }
       p += 0x9E3779B9u;
       q += 0xBB67AE85u;
     }
-    const uint32_t w[4] = {a, b, c, d};
+  }
+  // Eight elements: zero, or times the scale.  (A product of its own, not part of a fused one: what the library computes does not depend on what is added behind it.)
+  __device__ __forceinline__ void keep(float (&f)[8], const uint32_t (&w)[4]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float2 v = __fmul2_rn(make_float2(f[2 * i], f[2 * i + 1]), make_float2(scale, scale));
       f[2 * i] = w[i] << 16 >= limit ? v.x : 0.f;
       f[2 * i + 1] = w[i] >= limit ? v.y : 0.f;      // (the lower half decides nothing)
     }
+  }
+  __device__ __forceinline__ void apply(float (&f)[8], uint32_t row, uint32_t oct) const {
+    if (limit == 0) return;
+    uint32_t w[1][4];
+    const uint32_t rows[1] = {row}, octs[1] = {oct};
+    words(w, rows, octs);
+    keep(f, w[0]);
   }
 };
 
