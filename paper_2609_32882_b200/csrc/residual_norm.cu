@@ -258,14 +258,15 @@ __device__ __forceinline__ void combine_bf16(Eight<bf16>& h, const Eight<bf16>& 
 }
 
 // V: pieces of eight elements a thread, two or four (MANY: as many as it takes, in a loop); NORM: else the int8 form of x as it is
-template <int V, bool MANY, typename X, typename S, bool NORM, int LIE>
+template <int V, bool MANY, typename X, typename S, bool NORM, int LIE, bool DROP>
 __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_constant__ NormFwdArgs a) {
   __shared__ __align__(16) RowSums sh;
   sh.init();
   grid_enter();
   const int t = threadIdx.x, T = blockDim.x, mine = (t >> 5) * (32 * V) + (t & 31);      // pieces mine, mine + 32, ..: a warp's lie next to one another
   DropMask mask;
-  mask.init(a.drop);
+  if (DROP) mask.init(a.drop);
+  else mask.limit = 0;
   const int rounds = MANY ? (a.octs + T * V - 1) / (T * V) : 1;
   const bool int8 = a.int8.values != nullptr;
   uint32_t turn = 0;
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_con
       // (the generator's rounds of all pieces together, where the registers have room: 75600 x 5120 bf16 with dropout 541 us instead of 570, 65972 x 1536 fp32 215 instead of 209)
       constexpr bool TOGETHER = sizeof(X) + sizeof(S) == 4;
       uint32_t words[V][4];
-      if (TOGETHER && mask.limit != 0) {
+      if (TOGETHER && DROP && mask.limit != 0) {
         uint32_t rows[V], octs[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -297,7 +298,7 @@ __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_con
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         if constexpr (sizeof(X) == 2 && sizeof(S) == 2) {
-          if (mask.limit != 0) combine(h[v], x[v], a.r.p != nullptr, mask, words[v]);
+          if (DROP && mask.limit != 0) combine(h[v], x[v], a.r.p != nullptr, mask, words[v]);
           else if (a.r.p != nullptr) combine_bf16(h[v], x[v]);
           else h[v] = x[v];
         } else {
@@ -610,28 +611,35 @@ int threads_for(int octs, int v) {
 // do rows with fp32, of which four pieces do not fit the registers (65972 x 1536 219 us, with four 319).  0: as many as it takes
 int pieces_fwd(int octs, bool narrow) { return octs <= (narrow ? kNormMost : 2 * kNormMost) ? 2 : octs <= 4 * kNormMost ? 4 : 0; }
 
-template <int V, bool MANY, typename X, typename S, bool NORM, int LIE>
+template <int V, bool MANY, typename X, typename S, bool NORM, int LIE, bool DROP = NORM>
 cudaError_t go_fwd(const NormFwdArgs& a, cudaStream_t st) {
   static Residents residents;
   const int threads = threads_for(a.octs, V);
   int ctas = 0;
-  const cudaError_t e = resident_ctas((const void*)norm_fwd_kernel<V, MANY, X, S, NORM, LIE>, residents, threads, 0, &ctas);
+  const cudaError_t e = resident_ctas((const void*)norm_fwd_kernel<V, MANY, X, S, NORM, LIE, DROP>, residents, threads, 0, &ctas);
   if (e != cudaSuccess) return e;
   // four rows a CTA, or as many as it takes: CTAs that end at different times keep memory busy (75600 x 5120 to e4m3 412 us, with CTAs that stay 429, of one row each 417; int8 of
   // 15360 x 5120 42, 42, 47)
   const int fours = (a.rows + 3) / 4;
-  return launch_kernel(norm_fwd_kernel<V, MANY, X, S, NORM, LIE>, fours > ctas ? fours : a.rows < ctas ? a.rows : ctas, threads, 0, st, a);
+  return launch_kernel(norm_fwd_kernel<V, MANY, X, S, NORM, LIE, DROP>, fours > ctas ? fours : a.rows < ctas ? a.rows : ctas, threads, 0, st, a);
+}
+template <int V, typename X, typename S, bool NORM, bool DROP>
+cudaError_t lie_fwd(const NormFwdArgs& a, cudaStream_t st) {
+  return a.octs % (V * 32) == 0 && threads_for(a.octs, V) * V == a.octs ? go_fwd<V, false, X, S, NORM, ROWS_WHOLE, DROP>(a, st)
+                                                                        : go_fwd<V, false, X, S, NORM, ROWS_ALIGNED, DROP>(a, st);
 }
 template <int V, typename X, typename S, bool NORM>
-cudaError_t lie_fwd(const NormFwdArgs& a, cudaStream_t st) {
-  return a.octs % (V * 32) == 0 && threads_for(a.octs, V) * V == a.octs ? go_fwd<V, false, X, S, NORM, ROWS_WHOLE>(a, st) : go_fwd<V, false, X, S, NORM, ROWS_ALIGNED>(a, st);
+cudaError_t drop_fwd(const NormFwdArgs& a, cudaStream_t st) {
+  // (rows of bf16, whose kernels are the ones that are short of registers, have kernels without a dropout)
+  if constexpr (NORM && sizeof(X) + sizeof(S) == 4) return a.drop.threshold ? lie_fwd<V, X, S, NORM, true>(a, st) : lie_fwd<V, X, S, NORM, false>(a, st);
+  else return lie_fwd<V, X, S, NORM, NORM>(a, st);
 }
 template <typename X, typename S, bool NORM>
 cudaError_t size_fwd(const NormFwdArgs& a, bool vec, cudaStream_t st) {
   if (!vec) return a.octs > 2 * kNormMost ? go_fwd<2, true, X, S, NORM, ROWS_ANY>(a, st) : go_fwd<2, false, X, S, NORM, ROWS_ANY>(a, st);
   switch (pieces_fwd(a.octs, sizeof(X) + sizeof(S) == 4)) {
-    case 2: return lie_fwd<2, X, S, NORM>(a, st);
-    case 4: return lie_fwd<4, X, S, NORM>(a, st);
+    case 2: return drop_fwd<2, X, S, NORM>(a, st);
+    case 4: return drop_fwd<4, X, S, NORM>(a, st);
     default: return go_fwd<2, true, X, S, NORM, ROWS_ALIGNED>(a, st);
   }
 }
