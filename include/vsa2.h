@@ -548,6 +548,9 @@ int32_t vsa2_debug_rescue_capacity(int32_t capacity);
  * with C's rows on 16-byte boundaries (`c_aligned`; of no use with an n that is no multiple of 8) or not.  out: columns of a tile (32, 128, 224); CTAs that share one (1, 2); 1 where A's rows are the
  * accumulators' lanes instead of B's; ranges that K is cut into; tiles along the columns' operand; of those, how many are taken together. */
 int vsa2_debug_fp8_matmul_plan(int32_t m, int32_t n, int32_t k, int32_t c_dtype, int32_t c_aligned, int32_t sms, int32_t pairs, int32_t out[6]);
+/* The same of vsa2_int8_matmul: out = columns of a tile (8: the kernel of few rows of A, without tiles), CTAs that share one, ranges of K, tiles along A, tiles along A that are taken
+ * together. */
+int vsa2_debug_int8_matmul_plan(int32_t m, int32_t n, int32_t k, int32_t sms, int32_t pairs, int32_t out[5]);
 
 /* Text of the CUDA error behind the most recent VSA2_ERR_CUDA returned in this process ("no error" if none). */
 const char* vsa2_last_cuda_error(void);

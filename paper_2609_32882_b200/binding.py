@@ -40,7 +40,7 @@ EXPORTS = ("vsa2_query_sizes", "vsa2_route", "vsa2_route_scores", "vsa2_attn_fwd
            "vsa2_rope_plan", "vsa2_rope_apply", "vsa2_qkv_fwd", "vsa2_qkv_bwd", "vsa2_qkv_bwd_workspace_bytes",
            "vsa2_fp8_quantize", "vsa2_fp8_matmul", "vsa2_fp8_matmul_workspace_bytes", "vsa2_debug_fp8_matmul_plan",
            "vsa2_residual_norm_fwd", "vsa2_residual_norm_bwd", "vsa2_residual_norm_bwd_workspace_bytes", "vsa2_dropout",
-           "vsa2_int8_quantize", "vsa2_int8_matmul", "vsa2_int8_matmul_workspace_bytes")
+           "vsa2_int8_quantize", "vsa2_int8_matmul", "vsa2_int8_matmul_workspace_bytes", "vsa2_debug_int8_matmul_plan")
 
 KERNELS = ("pool", "router_lse", "router_pool", "select", "coarse_fwd", "fine_fwd", "bwd_pre", "coarse_bwd",
            "fine_bwd_dq", "fine_bwd_dkv", "pool_router")
@@ -181,6 +181,7 @@ def _lib():
         lib.vsa2_int8_quantize.argtypes = [C.c_int32] * 2 + [vp] * 3
         lib.vsa2_int8_matmul.argtypes = [C.c_int32] * 3 + [vp] * 4 + [C.c_int32, C.c_int64, vp, sz, vp]
         lib.vsa2_int8_matmul_workspace_bytes.argtypes = [C.c_int32] * 3
+        lib.vsa2_debug_int8_matmul_plan.argtypes = [C.c_int32] * 5 + [vp]
         for fn in (lib.vsa2_qkv_bwd_workspace_bytes, lib.vsa2_fp8_matmul_workspace_bytes, lib.vsa2_residual_norm_bwd_workspace_bytes,
                    lib.vsa2_int8_matmul_workspace_bytes):
             fn.restype = C.c_size_t
@@ -560,6 +561,13 @@ def vsa2_int8_matmul(a, b, c, workspace, bias=None, stream=None):
     code = (_MARSHAL or _marshal()).int8_matmul(a, b, c, workspace, bias, stream)
     if code != OK:
         raise Vsa2Error(code, "vsa2_int8_matmul")
+
+
+def vsa2_debug_int8_matmul_plan(m, n, k, sms=148, pairs=True):
+    """(columns of a tile, 8: the kernel of few rows of a; CTAs that share one; ranges of K; tiles along a, and those taken together); host arithmetic."""
+    out = (C.c_int32 * 5)()
+    _check(_lib().vsa2_debug_int8_matmul_plan(m, n, k, sms, pairs, out), "vsa2_debug_int8_matmul_plan")
+    return tuple(out)
 
 
 def vsa2_profile_events(kernel_id: int, start_event, stop_event):

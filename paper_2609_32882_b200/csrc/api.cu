@@ -1337,6 +1337,12 @@ int vsa2_int8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_int8* a, const 
   return VSA2_OK;
 }
 
+int vsa2_debug_int8_matmul_plan(int32_t m, int32_t n, int32_t k, int32_t sms, int32_t pairs, int32_t out[5]) {
+  if (m <= 0 || n <= 0 || k <= 0 || sms <= 0 || out == nullptr) return VSA2_ERR_INVALID_ARG;
+  int8_matmul_plan(m, n, k, sms, pairs != 0, out);
+  return VSA2_OK;
+}
+
 int vsa2_device_status(const void* workspace, void* cuda_stream, int32_t* status_out) {
   if (workspace == nullptr || status_out == nullptr) return VSA2_ERR_INVALID_ARG;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);

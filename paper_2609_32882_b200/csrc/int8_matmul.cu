@@ -33,8 +33,7 @@ struct I8Args : MmCut {
   int tensor_stores;                 // C lies as tensor copies need it, and ends where they end
   const float* p_scales;
   const float* q_scales;
-  const float* p_bias;               // (of n: that of the operand whose rows are B's; the other one null)
-  const float* q_bias;
+  const float* p_bias;               // null: none
   void* c;
   long long ldc, split_stride;       // elements between the results of two ranges
   StatusBlock* status;
@@ -45,7 +44,7 @@ struct I8Misc {
   uint64_t d_full[2], d_empty[2], group[2];
   uint32_t tmem_base;
   int abort_flag;
-  float2 of_column[2][2][128];       // scale and bias of the columns, of even and odd items, of each group
+  __align__(16) float of_column[2][2][128];      // scales of the columns, of even and odd items, of each group (read two at a time)
 };
 
 template <int PAIR>
@@ -76,7 +75,7 @@ __device__ __forceinline__ float finished(int sum, float a_scale, float b_scale,
   return __fmaf_rn(__fmul_rn(__int2float_rn(sum), a_scale), b_scale, bias);
 }
 
-template <int NT, int PAIR, bool SWAP, typename TO>
+template <int NT, int PAIR, typename TO>
 __global__ void __cluster_dims__(PAIR, 1, 1) __launch_bounds__(kMmThreads, 1)
 int8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_c,
                    const __grid_constant__ I8Args a) {
@@ -175,7 +174,7 @@ int8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_consta
         const int first = (w.p * PAIR + rank) * 128, row = first + quad * 32 + lane, col = w.q * NT + group * T::MINE;
         const int cols = min(T::MINE, a.q_rows - col);      // (0 or less: the tile ends before)
         const uint32_t tmem = tmem_base + buf * 256 + group * T::MINE + ((uint32_t)(quad * 32) << 16);
-        const float2* const of_column = misc->of_column[group][buf];
+        const float* const of_column = misc->of_column[group][buf];
         auto release = [&] {
           tc::tc_fence_before();
           __syncwarp();
@@ -197,15 +196,11 @@ int8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_consta
           }
           release();
         } else {
-          // the columns' vectors, while the products run.  (The other item's place may still be read: a warp that writes here has seen all four arrive behind the item before that one.)
+          // the columns' scales, while the products run.  (The other item's place may still be read: a warp that writes here has seen all four arrive behind the item before that one.)
           const int mine = quad * 32 + lane;
-          if (mine < T::MINE) {
-            float2 v = make_float2(0.f, 0.f);
-            if (mine < cols) v = make_float2(a.q_scales[col + mine], a.q_bias != nullptr ? a.q_bias[col + mine] : 0.f);
-            misc->of_column[group][buf][mine] = v;
-          }
+          if (mine < T::MINE) misc->of_column[group][buf][mine] = mine < cols ? a.q_scales[col + mine] : 0.f;
           if (sizeof(TO) == 2 && a.tensor_stores) {
-            // bf16: through registers and shared memory, turned unless SWAP, and out by tensor copies that drop what lies outside C.  A thread's fragments are of four rows
+            // bf16: through registers and shared memory, turned, and out by tensor copies that drop what lies outside C.  A thread's fragments are of four rows
             float scale[4], bias[4];
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
@@ -225,12 +220,11 @@ int8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_consta
               tc::tmem_ld_wait();
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
-                const float4 of = *reinterpret_cast<const float4*>(of_column + 32 * i + 8 * g + 2 * (lane & 3));      // of two columns
+                const float2 of = *reinterpret_cast<const float2*>(of_column + 32 * i + 8 * g + 2 * (lane & 3));      // of two columns
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                   const int lo = (int)r[b >> 1][4 * g + 2 * (b & 1)], hi = (int)r[b >> 1][4 * g + 2 * (b & 1) + 1];
-                  u[i][4 * g + b] = SWAP ? pack_bf16x2(finished(lo, scale[b], of.x, of.y), finished(hi, scale[b], of.z, of.w))
-                                         : pack_bf16x2(finished(lo, of.x, scale[b], bias[b]), finished(hi, of.z, scale[b], bias[b]));
+                  u[i][4 * g + b] = pack_bf16x2(finished(lo, of.x, scale[b], bias[b]), finished(hi, of.y, scale[b], bias[b]));
                 }
               }
             }
@@ -239,24 +233,20 @@ int8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_consta
             for (int i = 0; i < PIECES; ++i) {
               if (32 * i >= cols) break;
               unsigned char* tile = staging + (group * 2 + (tiles & 1)) * kMmTileBytes;
-              stage_tile<SWAP>(tile, u[i], quad, lane);
+              stage_tile<false>(tile, u[i], quad, lane);
               tc::fence_proxy_async_smem();
               if (quad == 0 && lane == 0) tc::bulk_store_wait_read();      // the tile before has been read: behind the barrier its place is free
               VSA2_GROUP_SYNC(&misc->group[group], syncs);
               if (quad == 0 && lane == 0) {
-                if (SWAP) {
-                  if (first < a.p_rows) tma_store_2d(&tm_c, tile, col + 32 * i, first);
-                } else {
 #pragma unroll
-                  for (int b = 0; b < 2; ++b)
-                    if (first + 64 * b < a.p_rows) tma_store_2d(&tm_c, tile + b * 4096, first + 64 * b, col + 32 * i);
-                }
+                for (int b = 0; b < 2; ++b)
+                  if (first + 64 * b < a.p_rows) tma_store_2d(&tm_c, tile + b * 4096, first + 64 * b, col + 32 * i);
                 tc::bulk_store_commit();
               }
               ++tiles;
             }
           } else {
-            // (not SWAP: a thread's elements of C lie ldc apart)
+            // (a thread's elements of C lie ldc apart)
             const float scale = row < a.p_rows ? a.p_scales[row] : 0.f, bias = row < a.p_rows && a.p_bias != nullptr ? a.p_bias[row] : 0.f;
             VSA2_GROUP_SYNC(&misc->group[group], syncs);
             VSA2_WAIT_PARKED(&misc->d_full[buf], (seg >> 1) & 1);
@@ -269,7 +259,7 @@ int8_matmul_kernel(const __grid_constant__ CUtensorMap tm_p, const __grid_consta
               tc::tmem_ld_wait();
               float v[32];
 #pragma unroll
-              for (int c = 0; c < 32; ++c) v[c] = finished((int)r[c], of_column[c0 + c].x, scale, bias);
+              for (int c = 0; c < 32; ++c) v[c] = finished((int)r[c], of_column[c0 + c], scale, bias);
               if (row < a.p_rows) put_columns(out + (long long)c0 * a.ldc, a.ldc, cols - c0, v);
             }
             release();
@@ -425,10 +415,10 @@ struct I8Plan {
   double cycles;
 };
 template <int NT, int PAIR>
-I8Plan plan_i8(const I8Call& c, bool swap) {
+I8Plan plan_i8(const I8Call& c) {
   I8Plan plan;
-  plan.pt = ((swap ? c.m : c.n) + 128 * PAIR - 1) / (128 * PAIR);
-  plan.qt = ((swap ? c.n : c.m) + NT - 1) / NT;
+  plan.pt = (c.n + 128 * PAIR - 1) / (128 * PAIR);
+  plan.qt = (c.m + NT - 1) / NT;
   plan.splits = 1;
   const int of = c.ctas / PAIR;
   const long long tiles = (long long)plan.pt * plan.qt;
@@ -440,8 +430,7 @@ I8Plan plan_i8(const I8Call& c, bool swap) {
   };
   const double epilogue = 12.0 * NT;      // of the last tile
   plan.cycles = products(tiles, c.kb) + epilogue;
-  if (swap) plan.cycles *= 1.06;
-  for (int s = 2; !swap && s <= kMmSplits && s <= c.kb && tiles * s <= of; ++s) {
+  for (int s = 2; s <= kMmSplits && s <= c.kb && tiles * s <= of; ++s) {
     const double cycles = products(tiles * s, (c.kb + s - 1) / s) + epilogue + 5000 + 8.0 * s * c.m * c.n / (30.0 * kMmCtas);
     if (cycles < plan.cycles) {
       plan.cycles = cycles;
@@ -451,35 +440,35 @@ I8Plan plan_i8(const I8Call& c, bool swap) {
   return plan;
 }
 
-template <int NT, int PAIR, bool SWAP, typename TO>
+template <int NT, int PAIR, typename TO>
 cudaError_t launch_i8_tiles(const I8Call& c, const I8Plan& plan, void* result, long long ldc, long long split_stride) {
   using T = I8Tile<NT, PAIR, TO>;
-  const Int8Arg &p = SWAP ? c.a : c.b, &q = SWAP ? c.b : c.a;
+  const Int8Arg &p = c.b, &q = c.a;
   I8Args a;
-  fill_cut(a, SWAP ? c.m : c.n, SWAP ? c.n : c.m, c.kb, plan.pt, plan.qt, plan.splits, tiles_together(NT, c.kb, plan.qt), c.kb);
+  fill_cut(a, c.n, c.m, c.kb, plan.pt, plan.qt, plan.splits, tiles_together(NT, c.kb, plan.qt), c.kb);
   a.tensor_stores = sizeof(TO) == 2 && c.tensor_stores;
   a.p_scales = p.scales; a.q_scales = q.scales;
-  a.p_bias = SWAP ? nullptr : c.bias; a.q_bias = SWAP ? c.bias : nullptr;
+  a.p_bias = c.bias;
   a.c = result; a.ldc = ldc; a.split_stride = split_stride;
   a.status = c.status;
   CUtensorMap tp, tq;
   if (!make_row_tmap(&tp, p.values, a.p_rows, c.k, p.ld, 128) || !make_row_tmap(&tq, q.values, a.q_rows, c.k, q.ld, NT / PAIR)) return cudaErrorInvalidValue;
   CUtensorMap tm_c = tq;      // (without tensor stores: never used)
-  if (a.tensor_stores && !make_result_tmap(&tm_c, result, c.m, c.n, ldc, SWAP)) return cudaErrorInvalidValue;
+  if (a.tensor_stores && !make_result_tmap(&tm_c, result, c.m, c.n, ldc, false)) return cudaErrorInvalidValue;
   const long long items = (long long)plan.pt * plan.qt * plan.splits;
   const int of = items < c.ctas / PAIR ? (int)items : c.ctas / PAIR;
   static KernelAttr attr;
   cudaError_t e;
-  if ((e = prepare_kernel((const void*)int8_matmul_kernel<NT, PAIR, SWAP, TO>, attr, T::SMEM))) return e;
-  return launch_kernel(int8_matmul_kernel<NT, PAIR, SWAP, TO>, of * PAIR, kMmThreads, T::SMEM, c.st, tp, tq, tm_c, a);
+  if ((e = prepare_kernel((const void*)int8_matmul_kernel<NT, PAIR, TO>, attr, T::SMEM))) return e;
+  return launch_kernel(int8_matmul_kernel<NT, PAIR, TO>, of * PAIR, kMmThreads, T::SMEM, c.st, tp, tq, tm_c, a);
 }
 
 template <int NT, int PAIR>
 cudaError_t launch_i8(const I8Call& c, const I8Plan& plan) {
   if (plan.splits == 1)
-    return c.f32 ? launch_i8_tiles<NT, PAIR, false, float>(c, plan, c.c, c.ldc, 0) : launch_i8_tiles<NT, PAIR, false, bf16>(c, plan, c.c, c.ldc, 0);
+    return c.f32 ? launch_i8_tiles<NT, PAIR, float>(c, plan, c.c, c.ldc, 0) : launch_i8_tiles<NT, PAIR, bf16>(c, plan, c.c, c.ldc, 0);
   const long long ldp = (c.n + 3) / 4 * 4;
-  const cudaError_t e = launch_i8_tiles<NT, PAIR, false, int>(c, plan, c.parts, ldp, c.m * ldp);
+  const cudaError_t e = launch_i8_tiles<NT, PAIR, int>(c, plan, c.parts, ldp, c.m * ldp);
   if (e != cudaSuccess) return e;
   const unsigned grid = (unsigned)((c.m * ldp / 4 + 255) / 256);
   const Divisor by_row = divisor(ldp / 4);
@@ -494,24 +483,20 @@ cudaError_t launch_few(const I8Call& c) {
   return launch_kernel(int8_few_kernel<TO>, (c.n + 15) / 16, kI8FewThreads, 0, c.st, c.m, c.n, c.k, c.a, c.b, c.bias, reinterpret_cast<TO*>(c.c), c.ldc);
 }
 
-// The kernel of a call: columns of a tile, CTAs that share one, which operand's rows are its lanes.  `pairs`: takes_pairs, and the context has room for one
+// The kernel of a call: columns of a tile, CTAs that share one.  `pairs`: takes_pairs, and the context has room for one.  (A's rows as lanes and B's as columns, which fills the rounds
+// of e4m3 products on tiles of 256 x 224 better, is the same on square ones.)
 struct I8Choice {
   int columns, pair;
-  bool swap;
   I8Plan plan;
 };
 bool takes_pairs(const I8Call& call) { return call.m > 32 && call.n > 128 && call.ctas >= 2; }      // (wherever B has rows for both)
 I8Choice choose_i8(const I8Call& call, bool pairs) {
-  if (call.m <= 32) return {32, 1, false, plan_i8<32, 1>(call, false)};
-  if (!pairs) return {128, 1, false, plan_i8<128, 1>(call, false)};
-  const I8Plan narrow = plan_i8<128, 2>(call, false);
-  if (call.m <= 128) return {128, 2, false, narrow};
-  const I8Plan wide = plan_i8<256, 2>(call, false);
-  if (call.tensor_stores) {
-    const I8Plan swapped = plan_i8<256, 2>(call, true);
-    if (swapped.cycles < wide.cycles && swapped.cycles < narrow.cycles) return {256, 2, true, swapped};
-  }
-  return narrow.cycles < wide.cycles ? I8Choice{128, 2, false, narrow} : I8Choice{256, 2, false, wide};
+  if (call.m <= 32) return {32, 1, plan_i8<32, 1>(call)};
+  if (!pairs) return {128, 1, plan_i8<128, 1>(call)};
+  const I8Plan narrow = plan_i8<128, 2>(call);
+  if (call.m <= 128) return {128, 2, narrow};
+  const I8Plan wide = plan_i8<256, 2>(call);
+  return narrow.cycles < wide.cycles ? I8Choice{128, 2, narrow} : I8Choice{256, 2, wide};
 }
 
 // Most elements of the ranges of a product of up to m, n and k: tiles x ranges are at most the CTAs (or pairs), ranges at most the blocks of K.  (Grows with each of the three,
@@ -556,13 +541,27 @@ cudaError_t launch_int8_matmul(int m, int n, int k, const Int8Arg& a, const Int8
   bool pairs = takes_pairs(call);
   if (pairs) {
     static ClusterRoom room;
-    if ((e = cluster_room((const void*)int8_matmul_kernel<256, 2, false, float>, room, 2, kMmThreads, I8Tile<256, 2, float>::SMEM, &pairs))) return e;
+    if ((e = cluster_room((const void*)int8_matmul_kernel<256, 2, float>, room, 2, kMmThreads, I8Tile<256, 2, float>::SMEM, &pairs))) return e;
   }
   const I8Choice choice = choose_i8(call, pairs);
-  if (choice.swap) return launch_i8_tiles<256, 2, true, bf16>(call, choice.plan, c, ldc, 0);
   if (choice.columns == 32) return launch_i8<32, 1>(call, choice.plan);
   if (choice.pair == 1) return launch_i8<128, 1>(call, choice.plan);
   return choice.columns == 128 ? launch_i8<128, 2>(call, choice.plan) : launch_i8<256, 2>(call, choice.plan);
+}
+
+void int8_matmul_plan(int m, int n, int k, int sms, bool pairs, int32_t* out) {
+  I8Call call = {};
+  call.m = m; call.n = n; call.k = k;
+  call.kb = (k + 127) / 128;
+  call.ctas = sms < kMmCtas ? sms : kMmCtas;
+  if (m <= kI8Few) {
+    out[0] = kI8Few;
+    out[1] = out[2] = out[3] = out[4] = 1;
+    return;
+  }
+  const I8Choice choice = choose_i8(call, pairs && takes_pairs(call));
+  out[0] = choice.columns; out[1] = choice.pair;
+  out[2] = choice.plan.splits; out[3] = choice.plan.qt; out[4] = tiles_together(choice.columns, call.kb, choice.plan.qt);
 }
 
 }  // namespace vsa2

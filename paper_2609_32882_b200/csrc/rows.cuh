@@ -55,6 +55,8 @@ cudaError_t launch_dropout(DropoutArgs a, bool x_f32, bool y_f32, cudaStream_t s
 size_t int8_matmul_workspace_bytes(int m, int n, int k);
 cudaError_t launch_int8_matmul(int m, int n, int k, const Int8Arg& a, const Int8Arg& b, const float* bias, void* c, int c_f32, long long ldc, void* workspace,
                                cudaStream_t st);
+// vsa2_debug_int8_matmul_plan
+void int8_matmul_plan(int m, int n, int k, int sms, bool pairs, int32_t* out);
 // k = 0: the bias, or nothing
 cudaError_t launch_bias_rows(int m, int n, const float* bias, void* c, int c_f32, long long ldc, cudaStream_t st);
 

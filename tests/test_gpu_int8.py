@@ -78,6 +78,9 @@ SHAPES = [
     (129, 256, 200), (1000, 264, 3000), (300, 8192, 512), (4096, 4608, 640), (4093, 4616, 136), (1536, 640, 20000), (2978, 488, 17078),
     (20000, 4608, 128), (8400, 2304, 100), (256, 9680, 512), (512, 15360, 640), (511, 15352, 640), (509, 6240, 648), (505, 6248, 1200), (250, 16576, 1000),
     (130, 257, 640), (225, 300, 75), (300, 515, 1153), (449, 2304, 512),
+    # more of tiles of 32 and 128 columns: all ranges of K in one, ragged and on the edge, results on 16-byte boundaries and off them; groups of tiles and a shorter last one
+    (9, 4608, 100), (32, 19200, 1536), (31, 4603, 128), (17, 40, 640), (33, 96, 128), (700, 64, 100), (9000, 128, 256), (64, 4608, 1536), (128, 15360, 640), (100, 9000, 512),
+    (20000, 264, 128), (40000, 520, 64), (2025, 4603, 1530), (3000, 1536, 1536), (200, 71, 100), (4000, 125, 256),
 ]
 
 
@@ -99,6 +102,20 @@ def test_products(m, n, k, dtype):
     step = 2.0 ** -23 if dtype == F else 2.0 ** -7      # (one step where the two roundings of the expectation fall badly)
     assert ((c.double() - want.double()).abs() <= step * want.double().abs()).all() and (c != want).double().mean() < 1e-4
     assert vb.vsa2_device_status(ws) == vb.OK
+
+
+@pytest.mark.parametrize("m,n,k", [(9, 4608, 100), (100, 264, 3000), (33, 96, 128), (700, 64, 100), (300, 8192, 512), (1536, 640, 20000), (5, 4608, 1536)])
+@pytest.mark.parametrize("skip", [0, 1])
+def test_every_kernel_with_results_on_and_off_boundaries(m, n, k, skip):
+    """bf16 with rows of 16-byte units: tensor copies, and plain stores where the first result is off; nothing else is written."""
+    gen = torch.Generator(device="cuda").manual_seed(m + n)
+    a, b, bias = operand(gen, m, k), operand(gen, n, k), torch.randn(n, generator=gen, device="cuda")
+    room = torch.full((m, n + 16), 7.0, dtype=BF, device="cuda")
+    vb.vsa2_int8_matmul(a, b, room[:, skip:skip + n], vb.int8_matmul_workspace(m, n, k), bias=bias)
+    want = expected(a, b, bias, BF)
+    got = room[:, skip:skip + n]
+    assert ((got.double() - want.double()).abs() <= 2.0 ** -7 * want.double().abs()).all() and (got != want).double().mean() < 1e-4
+    assert (room[:, :skip] == 7).all() and (room[:, skip + n:] == 7).all()
 
 
 @pytest.mark.parametrize("m", [1, 2, 3, 4, 7, 8, 9])
