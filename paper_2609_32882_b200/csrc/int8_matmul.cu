@@ -409,7 +409,7 @@ struct I8Call {
 };
 
 // How a product is cut, and the cycles that it is estimated at: as for e4m3 (fp8_matmul.cu), whose products run at the same pace.  Ranges of K are matrices of whole numbers in the
-// workspace, which a second kernel adds (about 5000 cycles, and the bytes).
+// workspace, which a second kernel adds (about 2000 cycles, and the bytes).
 struct I8Plan {
   int pt, qt, splits;
   double cycles;
@@ -426,12 +426,12 @@ I8Plan plan_i8(const I8Call& c) {
     const double feed = 52.0 * kMmCtas / ((items < of ? items : of) * PAIR);
     const double fed = (kMmPBytes + NT / PAIR * 128) / (feed < 64.0 ? feed : 64.0);
     const double block = fed > 2.0 * NT ? fed : 2.0 * NT;
-    return (double)((items + of - 1) / of) * blocks * (block > 300.0 ? block : 300.0);
+    return (double)((items + of - 1) / of) * blocks * (block > 400.0 ? block : 400.0);
   };
-  const double epilogue = 12.0 * NT;      // of the last tile
+  const double epilogue = 12.0 * NT + (PAIR == 2 ? 1500.0 : 0.0);      // of the last tile; a pair's start and end (103 x 893 x 150: 5.3 us, on CTAs alone 4.3)
   plan.cycles = products(tiles, c.kb) + epilogue;
   for (int s = 2; s <= kMmSplits && s <= c.kb && tiles * s <= of; ++s) {
-    const double cycles = products(tiles * s, (c.kb + s - 1) / s) + epilogue + 5000 + 8.0 * s * c.m * c.n / (30.0 * kMmCtas);
+    const double cycles = products(tiles * s, (c.kb + s - 1) / s) + epilogue + 2000 + 8.0 * s * c.m * c.n / (30.0 * kMmCtas);
     if (cycles < plan.cycles) {
       plan.cycles = cycles;
       plan.splits = s;
@@ -483,20 +483,25 @@ cudaError_t launch_few(const I8Call& c) {
   return launch_kernel(int8_few_kernel<TO>, (c.n + 15) / 16, kI8FewThreads, 0, c.st, c.m, c.n, c.k, c.a, c.b, c.bias, reinterpret_cast<TO*>(c.c), c.ldc);
 }
 
-// The kernel of a call: columns of a tile, CTAs that share one.  `pairs`: takes_pairs, and the context has room for one.  (A's rows as lanes and B's as columns, which fills the rounds
-// of e4m3 products on tiles of 256 x 224 better, is the same on square ones.)
+// The kernel of a call: columns of a tile, CTAs that share one, by the estimated cycles: over 110 random products of 9 to 20000 rows 1 % above the fastest cut on the average (pairs
+// wherever they fit and 5000 cycles for ranges: 9 %; 64 x 4608 x 1536 6.7 us on a pair, 5.9 on tiles of 32 columns; 955 x 216 x 1744 9.2 us whole, 7.6 in 4 ranges).  `pairs`: takes_pairs, and the context has room for one.  (A's rows as lanes and B's as columns,
+// which fills the rounds of e4m3 products on tiles of 256 x 224 better, is the same on square ones.)
 struct I8Choice {
   int columns, pair;
   I8Plan plan;
 };
 bool takes_pairs(const I8Call& call) { return call.m > 32 && call.n > 128 && call.ctas >= 2; }      // (wherever B has rows for both)
 I8Choice choose_i8(const I8Call& call, bool pairs) {
-  if (call.m <= 32) return {32, 1, plan_i8<32, 1>(call)};
-  if (!pairs) return {128, 1, plan_i8<128, 1>(call)};
-  const I8Plan narrow = plan_i8<128, 2>(call);
-  if (call.m <= 128) return {128, 2, narrow};
-  const I8Plan wide = plan_i8<256, 2>(call);
-  return narrow.cycles < wide.cycles ? I8Choice{128, 2, narrow} : I8Choice{256, 2, wide};
+  I8Choice best = {128, 1, plan_i8<128, 1>(call)};
+  auto consider = [&](int columns, int pair, const I8Plan& plan) {
+    if (plan.cycles < best.plan.cycles) best = I8Choice{columns, pair, plan};
+  };
+  if (call.m <= 64) consider(32, 1, plan_i8<32, 1>(call));      // (more rows: several tiles that read the same weights)
+  if (pairs) {
+    consider(128, 2, plan_i8<128, 2>(call));
+    if (call.m > 128) consider(256, 2, plan_i8<256, 2>(call));
+  }
+  return best;
 }
 
 // Most elements of the ranges of a product of up to m, n and k: tiles x ranges are at most the CTAs (or pairs), ranges at most the blocks of K.  (Grows with each of the three,

@@ -81,6 +81,8 @@ SHAPES = [
     # more of tiles of 32 and 128 columns: all ranges of K in one, ragged and on the edge, results on 16-byte boundaries and off them; groups of tiles and a shorter last one
     (9, 4608, 100), (32, 19200, 1536), (31, 4603, 128), (17, 40, 640), (33, 96, 128), (700, 64, 100), (9000, 128, 256), (64, 4608, 1536), (128, 15360, 640), (100, 9000, 512),
     (20000, 264, 128), (40000, 520, 64), (2025, 4603, 1530), (3000, 1536, 1536), (200, 71, 100), (4000, 125, 256),
+    # pairs on tiles of 128 columns, whole and in ranges of K
+    (892, 1328, 6331), (3965, 259, 7192), (1214, 512, 6515), (155, 2025, 8135), (2810, 248, 7641),
 ]
 
 
