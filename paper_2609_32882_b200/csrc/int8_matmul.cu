@@ -484,8 +484,9 @@ cudaError_t launch_few(const I8Call& c) {
 }
 
 // The kernel of a call: columns of a tile, CTAs that share one, by the estimated cycles: over 110 random products of 9 to 20000 rows 1 % above the fastest cut on the average (pairs
-// wherever they fit and 5000 cycles for ranges: 9 %; 64 x 4608 x 1536 6.7 us on a pair, 5.9 on tiles of 32 columns; 955 x 216 x 1744 9.2 us whole, 7.6 in 4 ranges).  `pairs`: takes_pairs, and the context has room for one.  (A's rows as lanes and B's as columns,
-// which fills the rounds of e4m3 products on tiles of 256 x 224 better, is the same on square ones.)
+// wherever they fit, and 5000 cycles for ranges: 9 %; 64 x 4608 x 1536 6.7 us on a pair, 5.9 on tiles of 32 columns; 955 x 216 x 1744 9.2 us whole, 7.6 in 4 ranges).
+// `pairs`: takes_pairs, and the context has room for one.  (A's rows as lanes and B's as columns, which fills the rounds of e4m3 products on tiles of 256 x 224 better, is the same
+// on square ones.)
 struct I8Choice {
   int columns, pair;
   I8Plan plan;

@@ -5,9 +5,10 @@
 //   int8    : v = h w (for vsa2_int8_quantize a matrix' own values), s = max |v| / 127, value = v * (127 / max |v|) rounded to nearest, ties to even; the row's r is part of its
 //             scale alone, so a value does not depend on how the sum of squares was rounded
 // A CTA takes a row at a time, eight neighbouring elements in each of a thread's pieces; the row is read once and stays in registers while its sums pass through the CTA's one barrier.
-// (Rows of more than 16,384 elements forward and 8192 backward, MANY, are read twice, the second time from L2.)  Bound by memory, and close behind by the issue slots: 75600 x 5120 with
-// residual to e4m3 448 us (6.0 TB/s), 65972 x 1536 fp32 with dropout to bf16 and e4m3 219 us (6.0), its backward 255 - 275 us (5.9 - 6.4), int8 of 15360 x 5120 42 us (5.6).  With few rows
-// it is the latency of one: a token to int8 2.6 us, 2048 x 1536 backward 12.8 us in two kernels.
+// (Rows of more than 16,384 elements forward and 8192 backward, MANY, are read twice, the second time from L2.)  Bound by memory, and in runs of seconds by the power limit beside it:
+// 75600 x 5120 with residual to e4m3 424 - 440 us (6.2 - 6.4 TB/s; 412 in short runs), 65972 x 1536 fp32 with dropout to bf16 and e4m3 207 - 213 us (6.2 - 6.4), its backward 255 - 275 us
+// (5.9 - 6.4), int8 of 15360 x 5120 38 us (6.2).  With few rows it is the latency of one: a token to int8 2.6 us, 2048 x 1536 backward 12.8 us in two kernels.  Rows of few elements leave
+// a warp to a CTA, of which an SM takes 32: 62500 x 64 bf16 25 us forward (5 of memory), 54 backward.
 #include "fp8_values.cuh"
 #include "rows.cuh"
 
