@@ -1,6 +1,6 @@
 // y = (residual +) x / (1 - p) where an element is kept, zero (or the residual) elsewhere; its own backward.  The mask is formed from a counter
 // (rows.cuh), never stored.  Bound by memory: x, the residual and y once each; 75600 x 5120 bf16 with residual 329 - 360 us (6.5 - 7.1 TB/s, passes that follow one another
-// included), with ten rounds of the generator for eight elements in the issue slots beside it (71 %).
+// included), with ten rounds of the generator for eight elements in the issue slots beside it (52 %).
 #include "rows.cuh"
 
 namespace vsa2 {
