@@ -551,6 +551,8 @@ int vsa2_debug_fp8_matmul_plan(int32_t m, int32_t n, int32_t k, int32_t c_dtype,
 /* The same of vsa2_int8_matmul: out = columns of a tile (8: the kernel of few rows of A, without tiles), CTAs that share one, ranges of K, tiles along A, tiles along A that are taken
  * together. */
 int vsa2_debug_int8_matmul_plan(int32_t m, int32_t n, int32_t k, int32_t sms, int32_t pairs, int32_t out[5]);
+/* What a CTA of vsa2_residual_norm_fwd and vsa2_int8_quantize takes of `rows` rows on a device that holds `resident` CTAs: out = CTAs, rows of this one, the last of them. */
+int vsa2_debug_residual_norm_rows(int32_t rows, int32_t resident, int32_t cta, int64_t out[3]);
 
 /* Text of the CUDA error behind the most recent VSA2_ERR_CUDA returned in this process ("no error" if none). */
 const char* vsa2_last_cuda_error(void);

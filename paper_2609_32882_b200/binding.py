@@ -40,7 +40,8 @@ EXPORTS = ("vsa2_query_sizes", "vsa2_route", "vsa2_route_scores", "vsa2_attn_fwd
            "vsa2_rope_plan", "vsa2_rope_apply", "vsa2_qkv_fwd", "vsa2_qkv_bwd", "vsa2_qkv_bwd_workspace_bytes",
            "vsa2_fp8_quantize", "vsa2_fp8_matmul", "vsa2_fp8_matmul_workspace_bytes", "vsa2_debug_fp8_matmul_plan",
            "vsa2_residual_norm_fwd", "vsa2_residual_norm_bwd", "vsa2_residual_norm_bwd_workspace_bytes", "vsa2_dropout",
-           "vsa2_int8_quantize", "vsa2_int8_matmul", "vsa2_int8_matmul_workspace_bytes", "vsa2_debug_int8_matmul_plan")
+           "vsa2_int8_quantize", "vsa2_int8_matmul", "vsa2_int8_matmul_workspace_bytes", "vsa2_debug_int8_matmul_plan",
+           "vsa2_debug_residual_norm_rows")
 
 KERNELS = ("pool", "router_lse", "router_pool", "select", "coarse_fwd", "fine_fwd", "bwd_pre", "coarse_bwd",
            "fine_bwd_dq", "fine_bwd_dkv", "pool_router")
@@ -182,6 +183,7 @@ def _lib():
         lib.vsa2_int8_matmul.argtypes = [C.c_int32] * 3 + [vp] * 4 + [C.c_int32, C.c_int64, vp, sz, vp]
         lib.vsa2_int8_matmul_workspace_bytes.argtypes = [C.c_int32] * 3
         lib.vsa2_debug_int8_matmul_plan.argtypes = [C.c_int32] * 5 + [vp]
+        lib.vsa2_debug_residual_norm_rows.argtypes = [C.c_int32] * 3 + [vp]
         for fn in (lib.vsa2_qkv_bwd_workspace_bytes, lib.vsa2_fp8_matmul_workspace_bytes, lib.vsa2_residual_norm_bwd_workspace_bytes,
                    lib.vsa2_int8_matmul_workspace_bytes):
             fn.restype = C.c_size_t
@@ -567,6 +569,13 @@ def vsa2_debug_int8_matmul_plan(m, n, k, sms=148, pairs=True):
     """(columns of a tile, 8: the kernel of few rows of a; CTAs that share one; ranges of K; tiles along a, and those taken together); host arithmetic."""
     out = (C.c_int32 * 5)()
     _check(_lib().vsa2_debug_int8_matmul_plan(m, n, k, sms, pairs, out), "vsa2_debug_int8_matmul_plan")
+    return tuple(out)
+
+
+def vsa2_debug_residual_norm_rows(rows, resident, cta):
+    """(CTAs of vsa2_residual_norm_fwd and vsa2_int8_quantize on a device that holds `resident`, rows of CTA `cta`, the last of them); host arithmetic."""
+    out = (C.c_int64 * 3)()
+    _check(_lib().vsa2_debug_residual_norm_rows(rows, resident, cta, out), "vsa2_debug_residual_norm_rows")
     return tuple(out)
 
 

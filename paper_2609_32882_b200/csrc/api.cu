@@ -1343,6 +1343,19 @@ int vsa2_debug_int8_matmul_plan(int32_t m, int32_t n, int32_t k, int32_t sms, in
   return VSA2_OK;
 }
 
+int vsa2_debug_residual_norm_rows(int32_t rows, int32_t resident, int32_t cta, int64_t out[3]) {
+  if (rows <= 0 || check_extent(rows, 1) != VSA2_OK || resident <= 0 || cta < 0 || out == nullptr) return VSA2_ERR_INVALID_ARG;
+  const int ctas = norm_fwd_ctas(rows, resident);
+  if (cta >= ctas) return VSA2_ERR_INVALID_ARG;
+  out[0] = ctas;
+  out[1] = 0;
+  for (RowWalk walk{(uint32_t)cta, (uint32_t)rows, (uint32_t)ctas}; walk.here(); walk.next()) {
+    ++out[1];
+    out[2] = (int)walk.row;
+  }
+  return VSA2_OK;
+}
+
 int vsa2_device_status(const void* workspace, void* cuda_stream, int32_t* status_out) {
   if (workspace == nullptr || status_out == nullptr) return VSA2_ERR_INVALID_ARG;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);

@@ -271,7 +271,8 @@ __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_con
   const int rounds = MANY ? (a.octs + T * V - 1) / (T * V) : 1;
   const bool int8 = a.int8.values != nullptr;
   uint32_t turn = 0;
-  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+  for (RowWalk walk{blockIdx.x, (uint32_t)a.rows, gridDim.x}; walk.here(); walk.next()) {
+    const int row = (int)walk.row;
     const X* const xp = reinterpret_cast<const X*>(a.x.p) + row * a.x.ld;
     const S* const rp = reinterpret_cast<const S*>(a.r.p) + row * a.r.ld;
     Eight<S> h[V];
@@ -619,10 +620,7 @@ cudaError_t go_fwd(const NormFwdArgs& a, cudaStream_t st) {
   int ctas = 0;
   const cudaError_t e = resident_ctas((const void*)norm_fwd_kernel<V, MANY, X, S, NORM, LIE, DROP>, residents, threads, 0, &ctas);
   if (e != cudaSuccess) return e;
-  // four rows a CTA, or as many as it takes: CTAs that end at different times keep memory busy (75600 x 5120 to e4m3 412 us, with CTAs that stay 429, of one row each 417; int8 of
-  // 15360 x 5120 42, 42, 47)
-  const int fours = (a.rows + 3) / 4;
-  return launch_kernel(norm_fwd_kernel<V, MANY, X, S, NORM, LIE, DROP>, fours > ctas ? fours : a.rows < ctas ? a.rows : ctas, threads, 0, st, a);
+  return launch_kernel(norm_fwd_kernel<V, MANY, X, S, NORM, LIE, DROP>, norm_fwd_ctas(a.rows, ctas), threads, 0, st, a);
 }
 template <int V, typename X, typename S, bool NORM, bool DROP>
 cudaError_t lie_fwd(const NormFwdArgs& a, cudaStream_t st) {

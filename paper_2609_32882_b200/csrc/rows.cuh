@@ -47,6 +47,19 @@ struct DropoutArgs {
   unsigned long long per_octs;      // 2^64 / octs, rounded up
   DropArg drop;
 };
+// The rows of a CTA of the norm forward (and of the int8 quantisation): every ctas-th from its own number on.  Counted without a sign: what is formed behind its last row is less than
+// rows + ctas, and with a CTA for each four rows that passes 2^31 from 1,717,986,917 rows on (2^31 + 2^29 at most)
+struct RowWalk {
+  uint32_t row, rows, ctas;
+  __host__ __device__ __forceinline__ bool here() const { return row < rows; }
+  __host__ __device__ __forceinline__ void next() { row += ctas; }
+};
+// CTAs for `rows` rows, where the device holds `resident` at a time.  Four rows a CTA, or as many as it takes: CTAs that end at different times keep memory busy (75600 x 5120 to e4m3
+// 412 us, with CTAs that stay 429, of one row each 417; int8 of 15360 x 5120 42, 42, 47)
+inline int norm_fwd_ctas(int rows, int resident) {
+  const int fours = (rows + 3) / 4;
+  return fours > resident ? fours : rows < resident ? rows : resident;
+}
 cudaError_t launch_norm_fwd(NormFwdArgs a, bool x_f32, bool h_f32, cudaStream_t st);
 cudaError_t launch_int8_quantize(const RowsArg& x, bool x_f32, int rows, int cols, const Int8Arg& out, cudaStream_t st);
 size_t norm_bwd_workspace_bytes(int rows, int cols);
