@@ -23,7 +23,8 @@ class Vsa2ResidualNorm:
     Vsa2Layer's.
 
     forward gives the stream h, its norm x in bf16, and x's 8-bit form; it keeps what backward needs until the next forward.  h and the weight are kept as they are, not copied: backward
-    refuses where torch has changed one of them since.  rng (int64 [2] on the device: seed, offset) is counted on by every forward that drops: a captured step draws anew at each replay."""
+    refuses where torch has changed one of them since.  rng (int64 [2] on the device: seed, offset) is counted on by every forward that drops: a captured step draws anew at each replay.
+    backward forms the mask again from what its own forward drew with, whatever rng has become."""
 
     def __init__(self, rows, hidden, p=0.0, eps=1e-6, seed=0, projection="fp8", device="cuda"):
         import torch
@@ -34,6 +35,7 @@ class Vsa2ResidualNorm:
         self.torch, self.rows, self.hidden, self.p, self.eps, self.device = torch, rows, hidden, p, eps, torch.device(device)
         self.form = vb.Int8 if projection == "int8" else vb.Fp8
         self.rng = torch.tensor([seed, 0], dtype=torch.int64, device=device)
+        self.next = torch.tensor([0, 1], dtype=torch.int64, device=device)
         self.ws = torch.empty(max(256, vb.vsa2_residual_norm_bwd_workspace_bytes(rows, hidden)), dtype=torch.uint8, device=device)
         self.weight = None
         self.saved, self.kept = None, ()
@@ -54,14 +56,16 @@ class Vsa2ResidualNorm:
         """branch, residual [.., hidden], each bf16 or fp32 -> (h of residual's type, x in bf16, both of residual's shape, x's 8-bit form [rows, hidden])."""
         torch = self.torch
         drops = self.p if training else 0.0
+        rng = None
         if drops:
-            self.rng[1] += 1
+            rng = self.rng + self.next      # (a copy of this forward's own)
+            self.rng.copy_(rng)
         h = torch.empty_like(residual)
         x = torch.empty(residual.shape, dtype=torch.bfloat16, device=self.device)
         x8 = self.form.empty(self.rows, self.hidden, self.device)
         vb.vsa2_residual_norm_fwd(self._rows(branch, "the branch"), self._rows(residual, "the residual"), self.weight, eps=self.eps, h=h.view(self.rows, -1), y=x.view(self.rows, -1),
-                                  **{"y_int8" if self.form is vb.Int8 else "y_fp8": x8}, p=drops, rng=self.rng)
-        self.saved, self.kept = (h, branch.dtype, drops), self._versions(h)
+                                  **{"y_int8" if self.form is vb.Int8 else "y_fp8": x8}, p=drops, rng=rng)
+        self.saved, self.kept = (h, branch.dtype, drops, rng), self._versions(h)
         return h, x, x8
 
     def _versions(self, h):
@@ -71,7 +75,7 @@ class Vsa2ResidualNorm:
         """Gradients of x (bf16 or fp32) and, where something else reads the stream, of h -> dict of d_residual, d_branch (each of its input's shape and type) and, in fp32, d_weight."""
         if self.saved is None:
             raise RuntimeError("backward without a forward before it")
-        h, branch_type, drops = self.saved
+        h, branch_type, drops, rng = self.saved
         if self._versions(h) != self.kept:
             raise RuntimeError("changed between forward and backward: the stream, or the norm's weights")
         torch = self.torch
@@ -79,7 +83,7 @@ class Vsa2ResidualNorm:
         d_branch = torch.empty(h.shape, dtype=branch_type, device=self.device) if drops or branch_type != h.dtype else None
         vb.vsa2_residual_norm_bwd(h.view(self.rows, -1), self._rows(dx, "the gradient of x"), None if dh is None else self._rows(dh, "the gradient of h"), self.weight, eps=self.eps,
                                   d_residual=d_residual.view(self.rows, -1), dx=None if d_branch is None else d_branch.view(self.rows, -1), d_weight=d_weight, workspace=self.ws,
-                                  p=drops, rng=self.rng)
+                                  p=drops, rng=rng)
         return {"d_residual": d_residual, "d_branch": d_residual if d_branch is None else d_branch, "d_weight": d_weight}
 
 

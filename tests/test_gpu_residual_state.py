@@ -1,0 +1,68 @@
+"""What the residual stream's norm keeps between forward and backward: the generator's state of its own forward, whatever the shared one has become."""
+import pytest
+import torch
+
+import residual_reference as ref
+from paper_2609_32882_b200.layer import Vsa2ResidualNorm
+
+pytestmark = pytest.mark.gpu
+BF, F = torch.bfloat16, torch.float32
+ROWS, COLS, P = 60, 264, 0.3
+
+
+def made(seed=5):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    branch, residual, dx = (torch.randn(ROWS, COLS, generator=gen, device="cuda") for _ in range(3))
+    return Vsa2ResidualNorm(ROWS, COLS, p=P, seed=seed), branch, residual, dx
+
+
+def check(stream, h, dx, offset):
+    """Gradients through the mask of this offset.  (fp32 throughout: the norm's 2^-17 of the terms, a product with the mask's factor.)"""
+    got = stream.backward(dx)
+    factor = ref.factors(5, offset, ROWS, COLS, P).cuda()
+    d, dw, size, size_w = ref.gradients(h, dx, None, None, 1e-6)
+    assert ((got["d_branch"].double() == 0) == ((factor == 0) | (got["d_residual"] == 0))).all()
+    assert ((got["d_branch"].double() - d * factor).abs() <= (2.0 ** -17 * size + 2.0 ** -23 * d.abs()) * factor).all()
+    assert ((got["d_residual"].double() - d).abs() <= 2.0 ** -17 * size + 2.0 ** -24 * d.abs()).all()
+
+
+def test_backward_after_the_generator_was_set_anew():
+    stream, branch, residual, dx = made()
+    h, _, _ = stream.forward(branch, residual)
+    stream.rng.copy_(torch.tensor([9, 70], device="cuda"))
+    check(stream, h, dx, 1)
+    assert stream.rng.tolist() == [9, 70]
+    h, _, _ = stream.forward(branch, residual)
+    assert torch.equal(h, ref.stream(branch, residual, ref.factors(9, 71, ROWS, COLS, P)))
+
+
+def test_backward_after_a_forward_that_was_refused():
+    stream, branch, residual, dx = made()
+    h, _, _ = stream.forward(branch, residual)
+    for bad in (branch[:-1], branch.half(), branch.cpu()):
+        with pytest.raises(ValueError):
+            stream.forward(bad, residual)
+    check(stream, h, dx, 1)
+
+
+def test_backward_after_a_captured_step_was_replayed():
+    """The captured step counts on the device, which nothing on the host sees."""
+    stream, branch, residual, dx = made()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        stream.forward(branch, residual)
+        stream.backward(dx)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            captured_h, _, _ = stream.forward(branch, residual)
+            captured = stream.backward(dx)
+    torch.cuda.synchronize()
+    h, _, _ = stream.forward(branch, residual)      # the second that has run
+    for _ in range(3):
+        graph.replay()                              # .. up to the fifth
+    check(stream, h, dx, 2)
+    assert stream.rng.tolist() == [5, 5]
+    factor = ref.factors(5, 5, ROWS, COLS, P)
+    assert torch.equal(captured_h, ref.stream(branch, residual, factor))
+    assert ((captured["d_branch"] == 0) == ((factor.cuda() == 0) | (captured["d_residual"] == 0))).all()
