@@ -56,15 +56,14 @@ class Vsa2ResidualNorm:
         """branch, residual [.., hidden], each bf16 or fp32 -> (h of residual's type, x in bf16, both of residual's shape, x's 8-bit form [rows, hidden])."""
         torch = self.torch
         drops = self.p if training else 0.0
-        rng = None
-        if drops:
-            rng = self.rng + self.next      # (a copy of this forward's own)
-            self.rng.copy_(rng)
+        rng = self.rng + self.next if drops else None      # (a copy of this forward's own)
         h = torch.empty_like(residual)
         x = torch.empty(residual.shape, dtype=torch.bfloat16, device=self.device)
         x8 = self.form.empty(self.rows, self.hidden, self.device)
         vb.vsa2_residual_norm_fwd(self._rows(branch, "the branch"), self._rows(residual, "the residual"), self.weight, eps=self.eps, h=h.view(self.rows, -1), y=x.view(self.rows, -1),
                                   **{"y_int8" if self.form is vb.Int8 else "y_fp8": x8}, p=drops, rng=rng)
+        if drops:
+            self.rng.copy_(rng)      # (a call that was refused has not counted)
         self.saved, self.kept = (h, branch.dtype, drops, rng), self._versions(h)
         return h, x, x8
 

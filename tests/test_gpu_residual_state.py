@@ -66,3 +66,13 @@ def test_backward_after_a_captured_step_was_replayed():
     factor = ref.factors(5, 5, ROWS, COLS, P)
     assert torch.equal(captured_h, ref.stream(branch, residual, factor))
     assert ((captured["d_branch"] == 0) == ((factor.cuda() == 0) | (captured["d_residual"] == 0))).all()
+
+
+def test_a_forward_that_was_refused_has_not_counted():
+    stream, branch, residual, _ = made()
+    for bad in ((branch[:-1], residual), (branch.half(), residual), (branch, residual[:, :-1]), (branch.cpu(), residual), (branch, residual.double())):
+        with pytest.raises(ValueError):
+            stream.forward(*bad)
+    assert stream.rng.tolist() == [5, 0]
+    h, _, _ = stream.forward(branch, residual)
+    assert torch.equal(h, ref.stream(branch, residual, ref.factors(5, 1, ROWS, COLS, P))) and stream.rng.tolist() == [5, 1]
