@@ -64,18 +64,19 @@ class Vsa2ResidualNorm:
                                   **{"y_int8" if self.form is vb.Int8 else "y_fp8": x8}, p=drops, rng=rng)
         if drops:
             self.rng.copy_(rng)      # (a call that was refused has not counted)
-        self.saved, self.kept = (h, branch.dtype, drops, rng), self._versions(h)
+        self.saved, self.kept = (h, branch.dtype, drops, rng, self.weight), self._versions(h)
         return h, x, x8
 
     def _versions(self, h):
-        return tuple(None if t is None or t.is_inference() else (id(t), t._version) for t in (h, self.weight))
+        """torch's counters of changes in place."""
+        return tuple(None if t is None or t.is_inference() else t._version for t in (h, self.weight))
 
     def backward(self, dx, dh=None):
         """Gradients of x (bf16 or fp32) and, where something else reads the stream, of h -> dict of d_residual, d_branch (each of its input's shape and type) and, in fp32, d_weight."""
         if self.saved is None:
             raise RuntimeError("backward without a forward before it")
-        h, branch_type, drops, rng = self.saved
-        if self._versions(h) != self.kept:
+        h, branch_type, drops, rng, weight = self.saved
+        if weight is not self.weight or self._versions(h) != self.kept:
             raise RuntimeError("changed between forward and backward: the stream, or the norm's weights")
         torch = self.torch
         d_residual, d_weight = torch.empty_like(h), torch.empty(self.hidden, dtype=torch.float32, device=self.device)

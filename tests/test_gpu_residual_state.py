@@ -76,3 +76,23 @@ def test_a_forward_that_was_refused_has_not_counted():
     assert stream.rng.tolist() == [5, 0]
     h, _, _ = stream.forward(branch, residual)
     assert torch.equal(h, ref.stream(branch, residual, ref.factors(5, 1, ROWS, COLS, P))) and stream.rng.tolist() == [5, 1]
+
+
+def test_other_weights_are_refused_also_where_they_lie_in_the_old_ones_place():
+    """The first weights are let go of between forward and backward, and another tensor comes to have their identity and their address."""
+    stream, branch, residual, dx = made()
+    weight = torch.full((COLS,), 2.0, device="cuda")
+    name = id(weight)
+    stream.set_weights(weight)
+    stream.forward(branch, residual)
+    stream.set_weights(None)
+    del weight
+    others = []
+    for _ in range(1000):
+        others.append(torch.full((COLS,), 3.0, device="cuda"))
+        if id(others[-1]) == name:
+            break
+    for other in (others[-1], None, others[0]):
+        stream.set_weights(other)
+        with pytest.raises(RuntimeError, match="changed between"):
+            stream.backward(dx)
