@@ -64,7 +64,7 @@ class Vsa2ResidualNorm:
                                   **{"y_int8" if self.form is vb.Int8 else "y_fp8": x8}, p=drops, rng=rng)
         if drops:
             self.rng.copy_(rng)      # (a call that was refused has not counted)
-        self.saved, self.kept = (h, branch.dtype, drops, rng, self.weight), self._versions(h)
+        self.saved, self.kept = (h, branch.shape, branch.dtype, drops, rng, self.weight), self._versions(h)
         return h, x, x8
 
     def _versions(self, h):
@@ -75,16 +75,18 @@ class Vsa2ResidualNorm:
         """Gradients of x (bf16 or fp32) and, where something else reads the stream, of h -> dict of d_residual, d_branch (each of its input's shape and type) and, in fp32, d_weight."""
         if self.saved is None:
             raise RuntimeError("backward without a forward before it")
-        h, branch_type, drops, rng, weight = self.saved
+        h, branch_shape, branch_type, drops, rng, weight = self.saved
         if weight is not self.weight or self._versions(h) != self.kept:
             raise RuntimeError("changed between forward and backward: the stream, or the norm's weights")
         torch = self.torch
         d_residual, d_weight = torch.empty_like(h), torch.empty(self.hidden, dtype=torch.float32, device=self.device)
-        d_branch = torch.empty(h.shape, dtype=branch_type, device=self.device) if drops or branch_type != h.dtype else None
+        d_branch = torch.empty(branch_shape, dtype=branch_type, device=self.device) if drops or branch_type != h.dtype else None
         vb.vsa2_residual_norm_bwd(h.view(self.rows, -1), self._rows(dx, "the gradient of x"), None if dh is None else self._rows(dh, "the gradient of h"), self.weight, eps=self.eps,
                                   d_residual=d_residual.view(self.rows, -1), dx=None if d_branch is None else d_branch.view(self.rows, -1), d_weight=d_weight, workspace=self.ws,
                                   p=drops, rng=rng)
-        return {"d_residual": d_residual, "d_branch": d_residual if d_branch is None else d_branch, "d_weight": d_weight}
+        if d_branch is None:
+            d_branch = d_residual if branch_shape == h.shape else d_residual.view(branch_shape)
+        return {"d_residual": d_residual, "d_branch": d_branch, "d_weight": d_weight}
 
 
 class Vsa2Layer:

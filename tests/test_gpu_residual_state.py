@@ -96,3 +96,19 @@ def test_other_weights_are_refused_also_where_they_lie_in_the_old_ones_place():
         stream.set_weights(other)
         with pytest.raises(RuntimeError, match="changed between"):
             stream.backward(dx)
+
+
+@pytest.mark.parametrize("branch_type,p", [(F, 0.0), (F, P), (BF, 0.0), (BF, P)])
+def test_each_gradient_has_its_input_s_shape(branch_type, p):
+    """Rows as they lie; a branch [tokens, hidden] beside a stream [batch, tokens, hidden], and the other way round."""
+    _, branch, residual, dx = made()
+    stream = Vsa2ResidualNorm(ROWS, COLS, p=p, seed=5)
+    h, _, _ = stream.forward(branch.to(branch_type), residual)
+    want = stream.backward(dx)
+    for of_branch, of_residual in (((ROWS, COLS), (2, ROWS // 2, COLS)), ((1, ROWS, COLS), (ROWS, COLS)), ((ROWS, 1, COLS), (3, 4, 5, COLS))):
+        other = Vsa2ResidualNorm(ROWS, COLS, p=p, seed=5)
+        assert torch.equal(other.forward(branch.to(branch_type).view(of_branch), residual.view(of_residual))[0], h.view(of_residual))
+        got = other.backward(dx)
+        assert got["d_branch"].shape == of_branch and got["d_residual"].shape == of_residual
+        assert got["d_branch"].dtype == branch_type and torch.equal(got["d_branch"].view(ROWS, COLS), want["d_branch"])
+        assert torch.equal(got["d_residual"].view(ROWS, COLS), want["d_residual"])
