@@ -60,7 +60,7 @@ class Vsa2ResidualNorm:
         h = torch.empty_like(residual)
         x = torch.empty(residual.shape, dtype=torch.bfloat16, device=self.device)
         x8 = self.form.empty(self.rows, self.hidden, self.device)
-        vb.vsa2_residual_norm_fwd(self._rows(branch, "the branch"), self._rows(residual, "the residual"), self.weight, eps=self.eps, h=h.view(self.rows, -1), y=x.view(self.rows, -1),
+        vb.vsa2_residual_norm_fwd(self._rows(branch, "the branch"), self._rows(residual, "the residual"), self.weight, eps=self.eps, h=h.view(self.rows, self.hidden), y=x.view(self.rows, self.hidden),
                                   **{"y_int8" if self.form is vb.Int8 else "y_fp8": x8}, p=drops, rng=rng)
         if drops:
             self.rng.copy_(rng)      # (a call that was refused has not counted)
@@ -81,8 +81,8 @@ class Vsa2ResidualNorm:
         torch = self.torch
         d_residual, d_weight = torch.empty_like(h), torch.empty(self.hidden, dtype=torch.float32, device=self.device)
         d_branch = torch.empty(branch_shape, dtype=branch_type, device=self.device) if drops or branch_type != h.dtype else None
-        vb.vsa2_residual_norm_bwd(h.view(self.rows, -1), self._rows(dx, "the gradient of x"), None if dh is None else self._rows(dh, "the gradient of h"), self.weight, eps=self.eps,
-                                  d_residual=d_residual.view(self.rows, -1), dx=None if d_branch is None else d_branch.view(self.rows, -1), d_weight=d_weight, workspace=self.ws,
+        vb.vsa2_residual_norm_bwd(h.view(self.rows, self.hidden), self._rows(dx, "the gradient of x"), None if dh is None else self._rows(dh, "the gradient of h"), self.weight, eps=self.eps,
+                                  d_residual=d_residual.view(self.rows, self.hidden), dx=None if d_branch is None else d_branch.view(self.rows, self.hidden), d_weight=d_weight, workspace=self.ws,
                                   p=drops, rng=rng)
         if d_branch is None:
             d_branch = d_residual if branch_shape == h.shape else d_residual.view(branch_shape)

@@ -112,3 +112,14 @@ def test_each_gradient_has_its_input_s_shape(branch_type, p):
         assert got["d_branch"].shape == of_branch and got["d_residual"].shape == of_residual
         assert got["d_branch"].dtype == branch_type and torch.equal(got["d_branch"].view(ROWS, COLS), want["d_branch"])
         assert torch.equal(got["d_residual"].view(ROWS, COLS), want["d_residual"])
+
+
+@pytest.mark.parametrize("projection", ["fp8", "int8"])
+def test_no_rows(projection):
+    stream = Vsa2ResidualNorm(0, COLS, p=P, projection=projection)
+    branch, residual = torch.empty(2, 0, COLS, dtype=BF, device="cuda"), torch.empty(0, COLS, device="cuda")
+    h, x, x8 = stream.forward(branch, residual)
+    assert h.shape == x.shape == x8.shape == (0, COLS) and (h.dtype, x.dtype) == (F, BF)
+    got = stream.backward(torch.empty(0, COLS, device="cuda"), torch.empty(0, COLS, device="cuda"))
+    assert got["d_branch"].shape == (2, 0, COLS) and got["d_residual"].shape == (0, COLS)
+    assert got["d_weight"].shape == (COLS,) and not got["d_weight"].any()
