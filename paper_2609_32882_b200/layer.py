@@ -170,8 +170,9 @@ class Vsa2Layer:
         vb.vsa2_gate_fwd(p, self.hidden, video, self.w_g, gate)
         self.attn.route(q, k)
         o, lse = self.attn.forward(q, k, v, gate)
-        self.saved = (x, video, packed, q, k, v, gate, o, lse)
-        self.kept = self._versions(x, o)
+        if not self.int8:      # (no backward: nothing to keep)
+            self.saved = (x, video, packed, q, k, v, gate, o, lse)
+            self.kept = self._versions(x, o)
         return o
 
     def _versions(self, x, o):
