@@ -421,7 +421,7 @@ int vsa2_fp8_matmul(int32_t m, int32_t n, int32_t k, const vsa2_fp8* a, const vs
  * Conventions as above; none of these calls allocates or synchronises, sums run in a fixed order (bitwise reproducible on a device), and sizes of zero are valid. */
 
 /* A matrix [rows, cols] of a call (host struct): contiguous rows, `ld` >= cols elements apart (of no use with one row); any alignment of its type, rows on 16-byte boundaries are
- * faster.  An output may be an input itself (the same data, ld and dtype); otherwise outputs overlap neither inputs nor one another. */
+ * faster.  An output may be an input itself (the same data, ld and dtype); otherwise outputs overlap neither inputs nor one another (what begins at one address is refused). */
 typedef struct vsa2_rows {
   void* data;
   int64_t ld;

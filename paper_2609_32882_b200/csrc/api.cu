@@ -462,8 +462,14 @@ int check_rows(const vsa2_rows* m, int rows, int cols) {
 // (the stride of a single row is of no use, but the kernels' choice of loads looks at it)
 RowsArg rows_arg(const vsa2_rows* m, int rows) { return m != nullptr ? RowsArg{m->data, rows > 1 ? m->ld : 0} : RowsArg{nullptr, 0}; }
 bool is_f32(const vsa2_rows* m) { return m != nullptr && m->dtype == VSA2_F32; }
-// whether two matrices begin at the same address (outputs do not)
+// Whether two matrices of elements begin at the same address (two outputs do not), and whether an output that begins where an input does lies or reads otherwise: its threads would write
+// over what others have still to read
 bool same_place(const vsa2_rows* a, const vsa2_rows* b) { return a != nullptr && b != nullptr && a->data == b->data; }
+bool over_another(const vsa2_rows* out, const vsa2_rows* in, int rows) {
+  return same_place(out, in) && (out->dtype != in->dtype || (rows > 1 && out->ld != in->ld));
+}
+// .. or whether an output in 8 bits begins where any other matrix of the call does
+bool over_another(const void* values, const vsa2_rows* m) { return m != nullptr && m->data == values; }
 int check_int8(const vsa2_int8* v, int rows, int cols) {
   if (rows == 0 || cols == 0) return VSA2_OK;
   if (v->values == nullptr || v->scales == nullptr || v->ld < cols) return VSA2_ERR_INVALID_ARG;
@@ -1236,6 +1242,13 @@ int vsa2_residual_norm_fwd(int32_t rows, int32_t cols, const vsa2_rows* x, const
   const vsa2_rows* stream = residual != nullptr ? residual : x;
   if ((h != nullptr && h->dtype != stream->dtype) || (rows > 0 && cols > 0 && same_place(h, y))) return VSA2_ERR_INVALID_ARG;
   if ((y_fp8 != nullptr && (rc = check_fp8(y_fp8, rows, cols)) != VSA2_OK) || (y_int8 != nullptr && (rc = check_int8(y_int8, rows, cols)) != VSA2_OK)) return rc;
+  if (rows > 0 && cols > 0) {
+    for (const vsa2_rows* in : {x, residual})
+      if (over_another(h, in, rows) || over_another(y, in, rows)) return VSA2_ERR_INVALID_ARG;
+    for (const vsa2_rows* m : {x, residual, h, y})
+      if ((y_fp8 != nullptr && over_another(y_fp8->values, m)) || (y_int8 != nullptr && over_another(y_int8->values, m))) return VSA2_ERR_INVALID_ARG;
+    if (y_fp8 != nullptr && y_int8 != nullptr && y_fp8->values == y_int8->values) return VSA2_ERR_INVALID_ARG;
+  }
   NormFwdArgs a = {};
   if ((rc = fill_drop(drop, &a.drop)) != VSA2_OK) return rc;
   if (!aligned4(weight)) return VSA2_ERR_MISALIGNED;
@@ -1261,7 +1274,11 @@ int vsa2_residual_norm_bwd(int32_t rows, int32_t cols, const vsa2_rows* h, const
   for (const vsa2_rows* m : {h, dy, dh, d_residual, dx})
     if ((rc = check_rows(m, rows, cols)) != VSA2_OK) return rc;
   if ((dh != nullptr && dh->dtype != h->dtype) || (d_residual != nullptr && d_residual->dtype != h->dtype)) return VSA2_ERR_INVALID_ARG;
-  if (rows > 0 && cols > 0 && same_place(d_residual, dx)) return VSA2_ERR_INVALID_ARG;
+  if (rows > 0 && cols > 0) {
+    if (same_place(d_residual, dx)) return VSA2_ERR_INVALID_ARG;
+    for (const vsa2_rows* in : {h, dy, dh})
+      if (over_another(d_residual, in, rows) || over_another(dx, in, rows)) return VSA2_ERR_INVALID_ARG;
+  }
   NormBwdArgs a = {};
   if ((rc = fill_drop(drop, &a.drop)) != VSA2_OK) return rc;
   if (!aligned4(weight) || !aligned4(d_weight)) return VSA2_ERR_MISALIGNED;
@@ -1292,6 +1309,7 @@ int vsa2_dropout(int32_t rows, int32_t cols, const vsa2_rows* x, const vsa2_rows
   for (const vsa2_rows* m : {x, residual, y})
     if ((rc = check_rows(m, rows, cols)) != VSA2_OK) return rc;
   if (residual != nullptr && residual->dtype != y->dtype) return VSA2_ERR_INVALID_ARG;
+  if (rows > 0 && cols > 0 && (over_another(y, x, rows) || over_another(y, residual, rows))) return VSA2_ERR_INVALID_ARG;
   DropoutArgs a = {};
   if ((rc = fill_drop(drop, &a.drop)) != VSA2_OK || (rc = check_extent(rows, cols)) != VSA2_OK) return rc;
   if ((int64_t)rows * (cols / 8 + 1) > 1LL << 40) return VSA2_ERR_UNSUPPORTED;      // (more CTAs than a launch has)
@@ -1308,6 +1326,7 @@ int vsa2_int8_quantize(int32_t rows, int32_t cols, const vsa2_rows* x, const vsa
   int rc;
   if ((rc = check_rows(x, rows, cols)) != VSA2_OK || (rc = check_int8(out, rows, cols)) != VSA2_OK || (rc = check_extent(rows, cols)) != VSA2_OK) return rc;
   if (rows == 0 || cols == 0) return VSA2_OK;
+  if (over_another(out->values, x)) return VSA2_ERR_INVALID_ARG;
   if ((rc = check_device()) != VSA2_OK) return rc;
   VSA2_CUDA(launch_int8_quantize(rows_arg(x, rows), is_f32(x), rows, cols, int8_arg(out), reinterpret_cast<cudaStream_t>(cuda_stream)));
   return VSA2_OK;
