@@ -581,23 +581,19 @@ __global__ void __launch_bounds__(1024) norm_weight_kernel(const float* parts, i
   if (lane == 0 && blockIdx.x * 32 + range < cols) dw[blockIdx.x * 32 + range] = sum;
 }
 
-// CTAs of a kernel that the device holds: the last answer for each number of warps and device, with the shared memory that it was asked for; the kernel is allowed its shared memory first
+// CTAs of a kernel that the device holds at a time; asked for once for each number of warps and device
 struct Residents {
-  KernelAttr attr;
-  std::atomic<unsigned long long> known[kMaxDevices][kNormMost / 32 + 1] = {};      // bytes << 8 | CTAs of an SM
+  std::atomic<int> known[kMaxDevices][kNormMost / 32 + 1] = {};      // of an SM
 };
-cudaError_t resident_ctas(const void* kernel, Residents& r, int threads, size_t smem, int* ctas) {
-  int dev = 0, sms = 0, n = 0;
+cudaError_t resident_ctas(const void* kernel, Residents& r, int threads, int* ctas) {
+  int dev = 0, sms = 0;
   cudaError_t e;
   if ((e = cudaGetDevice(&dev)) != cudaSuccess || (e = sm_count(&sms)) != cudaSuccess) return e;
-  if (smem > 0 && (e = prepare_kernel(kernel, r.attr, smem)) != cudaSuccess) return e;
-  const unsigned long long last = dev < kMaxDevices ? r.known[dev][threads / 32].load(std::memory_order_relaxed) : 0;
-  if (last != 0 && last >> 8 == smem) {
-    n = (int)(last & 255);
-  } else {
-    if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem)) != cudaSuccess) return e;
+  int n = dev < kMaxDevices ? r.known[dev][threads / 32].load(std::memory_order_relaxed) : 0;
+  if (n == 0) {
+    if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0)) != cudaSuccess) return e;
     if (n < 1) n = 1;
-    if (dev < kMaxDevices) r.known[dev][threads / 32].store((unsigned long long)smem << 8 | (unsigned)n, std::memory_order_relaxed);
+    if (dev < kMaxDevices) r.known[dev][threads / 32].store(n, std::memory_order_relaxed);
   }
   *ctas = n * sms;
   return cudaSuccess;
@@ -618,7 +614,7 @@ cudaError_t go_fwd(const NormFwdArgs& a, cudaStream_t st) {
   static Residents residents;
   const int threads = threads_for(a.octs, V);
   int ctas = 0;
-  const cudaError_t e = resident_ctas((const void*)norm_fwd_kernel<V, MANY, X, S, NORM, LIE, DROP>, residents, threads, 0, &ctas);
+  const cudaError_t e = resident_ctas((const void*)norm_fwd_kernel<V, MANY, X, S, NORM, LIE, DROP>, residents, threads, &ctas);
   if (e != cudaSuccess) return e;
   return launch_kernel(norm_fwd_kernel<V, MANY, X, S, NORM, LIE, DROP>, norm_fwd_ctas(a.rows, ctas), threads, 0, st, a);
 }
@@ -652,7 +648,7 @@ cudaError_t go_bwd(const NormBwdArgs& a, float* dw, cudaStream_t st) {
   static Residents residents;
   const int threads = threads_for(a.octs, V);
   int ctas = 0;
-  cudaError_t e = resident_ctas((const void*)norm_bwd_kernel<V, MANY, S, G, LIE>, residents, threads, 0, &ctas);
+  cudaError_t e = resident_ctas((const void*)norm_bwd_kernel<V, MANY, S, G, LIE>, residents, threads, &ctas);
   if (e != cudaSuccess) return e;
   if (ctas > kNormParts) ctas = kNormParts;
   const int each = (a.rows + ctas - 1) / ctas;      // rows of a CTA: no more CTAs, and parts, than take the same time with as many each
