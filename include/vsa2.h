@@ -431,7 +431,7 @@ typedef struct vsa2_rows {
 
 /* Dropout with probability p (host struct).  The mask is never stored: element (row, col) has 16 bits of the counter-based generator Philox 4x32-10 with the key `seed` and the
  * counter (col / 8, row, offset) -- bits 16 (col % 2) of word (col % 8) / 2 -- and is kept, times 65536 / (65536 - t), where they are at least t = p * 65536 rounded.  Dropped elements
- * are zero whatever they were.  The same seed and offset give the same mask at any size, stride and type. */
+ * are zero whatever they were.  The same seed and offset give the same mask at any size, stride and type: layers of a model, and replicas that see other data, need a seed each. */
 typedef struct vsa2_drop {
   const uint64_t* rng;                /* device [2] = {seed, offset}, 8-byte aligned, read when the kernel runs: a captured call draws anew when they are changed between replays, and */
                                       /* backward needs what forward had.  May be NULL with p = 0 */

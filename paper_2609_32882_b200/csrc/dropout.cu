@@ -9,7 +9,8 @@ namespace {
 
 constexpr int kDropThreads = 256;
 constexpr int kAnyOcts = 2;       // .. of rows that lie anywhere
-// pieces of eight elements a thread, all asked for before the first is used: as many as 64 registers hold (four CTAs an SM: 75600 x 5120 with residual 361 us, three of 68 registers 382)
+// pieces of eight elements a thread, all asked for before the first is used: as many as 64 registers nearly hold (bf16 to bf16 puts 4 bytes a thread aside, 36 where
+// rows are strided; four CTAs an SM: 75600 x 5120 with residual 361 us, three of 68 registers 382)
 template <typename X, typename Y> constexpr int kDropOcts = sizeof(X) + sizeof(Y) == 4 ? 4 : 2;
 
 // pieces of x through the dropout, plus r where there is one (y may be r)

@@ -8,7 +8,8 @@
 //
 // What bounds it: in long runs the power limit (75600 x 15360 x 5120 4.15 - 4.29 ms, 2.8 PFLOP/s; 18900 rows of it alone 866 us, 3.4 PFLOP/s, tensor pipe busy 93 % of the time);
 // else the intake from L2 (8192 x 4096 x 4096 87 us, 4096^3 48); few tiles and short K: the launch, the first block's way from memory and the last tile's way out (2048 x 4608 x 1536
-// 14.7 us, of which the products need 7).  Asking for the next tile's scales ahead of time, or staging all of a tile's results at once in the place of a stage: no faster, or slower.
+// 13.9 - 14.7 us, of which the products need 7); short K: each tile's way out of bf16 (30428 x 9048 x 171 214 us, K = 640 196, as fp32 219, the e4m3 product 175; pairs of 256 columns keep 64
+// packed results a thread, and 44 bytes aside).  Asking for the next tile's scales ahead of time, or staging all of a tile's results at once in the place of a stage: no faster, or slower.
 #include "mm_tiles.cuh"
 #include "rows.cuh"
 

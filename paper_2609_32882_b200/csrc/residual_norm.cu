@@ -5,9 +5,9 @@
 //   int8    : v = h w (for vsa2_int8_quantize a matrix' own values), s = max |v| / 127, value = v * (127 / max |v|) rounded to nearest, ties to even; the row's r is part of its
 //             scale alone, so a value does not depend on how the sum of squares was rounded
 // A CTA takes a row at a time, eight neighbouring elements in each of a thread's pieces; the row is read once and stays in registers while its sums pass through the CTA's one barrier.
-// (Rows of more than 16,384 elements forward and 8192 backward, MANY, are read twice, the second time from L2.)  Bound by memory, and in runs of seconds by the power limit beside it:
+// (Rows of more than 16,384 elements forward, 8192 backward and where they lie anywhere, MANY, are read twice, the second time from L2.)  Bound by memory, and in runs of seconds by the power limit beside it:
 // 75600 x 5120 with residual to e4m3 424 - 440 us (6.2 - 6.4 TB/s; 412 in short runs), 65972 x 1536 fp32 with dropout to bf16 and e4m3 207 - 213 us (6.2 - 6.4), its backward 255 - 275 us
-// (5.9 - 6.4), int8 of 15360 x 5120 38 us (6.2).  With few rows it is the latency of one: a token to int8 2.6 us, 2048 x 1536 backward 12.8 us in two kernels.  Rows of few elements leave
+// (5.9 - 6.4), int8 of 15360 x 5120 38 us (6.2).  With few rows it is the latency of one: a token to int8 3.5 us, 2048 x 1536 backward 11.8 - 12.8 us in two kernels.  Rows of few elements leave
 // a warp to a CTA, of which an SM takes 32: 62500 x 64 bf16 25 us forward (5 of memory), 54 backward.
 #include "fp8_values.cuh"
 #include "rows.cuh"
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(kNormMost, 2) norm_fwd_kernel(const __grid_con
 // Any rows.  MANY: the sums of the weight's gradient are kept in the CTA's row of `parts`, where a thread finds its own again; else in registers
 // V: pieces of a thread, one up to 2048 elements of bf16 and 4096 of fp32, where it is faster or as fast: each has its sums of the weight's gradient in registers, which leave room for
 // fewer warps (30000 x 1536 bf16 67.9 us, with two 72.2; in fp32 116.8, 126.5; 20000 x 4096 bf16 141.5, 135.7).  Two take 96 registers, with which an SM holds two CTAs of 320 threads
-// (75600 x 5120 572 us, in 104 registers 889).  One piece of bf16 takes 80, and has the next row under way (without it, in 64 registers: 30000 x 1536 77.6 us instead of 67.9, 60000 x 640 87.7
+// (75600 x 5120 572 us, in 104 registers 889); up to 56 bytes a thread are put aside for it, up to 148 where rows lie anywhere.  One piece of bf16 takes 80, and has the next row under way (without it, in 64 registers: 30000 x 1536 77.6 us instead of 67.9, 60000 x 640 87.7
 // instead of 69.5); in fp32 that has no room (65972 x 1536 281 us, without 255).
 template <int V, bool MANY, typename S, typename G, int LIE>
 __global__ void __maxnreg__(V == 2 ? 96 : sizeof(S) == 2 ? 80 : 64) norm_bwd_kernel(const __grid_constant__ NormBwdArgs a) {
@@ -606,7 +606,9 @@ int threads_for(int octs, int v) {
 }
 // Pieces of a thread.  Forward: four share a row's fixed steps (its sums, the barrier, two divisions), two leave more warps whose latencies overlap.  Rows of bf16 of more than 4096
 // elements take four (75600 x 5120 to e4m3 440 us, with two 500; 10000 x 8192 94, 110), shorter ones two (75600 x 1536 to e4m3 130 us, with four 185; 2048 x 1536 5.5, 7.6), and so
-// do rows with fp32, of which four pieces do not fit the registers (65972 x 1536 219 us, with four 319).  0: as many as it takes
+// do rows with fp32, of which four pieces do not fit the registers (65972 x 1536 219 us, with four 319).  Rows with fp32 of more than 8192 elements take four all the same, though up to
+// 430 bytes a thread are put aside: 0, as many as it takes, reads them twice (10000 x 8200 fp32 to bf16 222 us, the loop 268; 12288 297, 333; 16384 387, 394; of int8 66, 101 .. 117, 145;
+// only fp32 with a dropout is faster in the loop from 12,288 on: 405, 403; 16384 541, 457)
 int pieces_fwd(int octs, bool narrow) { return octs <= (narrow ? kNormMost : 2 * kNormMost) ? 2 : octs <= 4 * kNormMost ? 4 : 0; }
 
 template <int V, bool MANY, typename X, typename S, bool NORM, int LIE, bool DROP = NORM>

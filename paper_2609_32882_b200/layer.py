@@ -19,8 +19,8 @@ from . import binding as vb
 
 
 class Vsa2ResidualNorm:
-    """rows: tokens of a call, batch and all; hidden: channels; p: share of the branch's elements that a training forward drops; projection: what the 8-bit form of the hidden states is for, as
-    Vsa2Layer's.
+    """rows: tokens of a call, batch and all; hidden: channels; p: share of the branch's elements that a training forward drops; seed: of the masks (norms
+    with one seed drop the same elements: the norms of a model, and its replicas on other data, need one each); projection: what the 8-bit form of the hidden states is for, as Vsa2Layer's.
 
     forward gives the stream h, its norm x in bf16, and x's 8-bit form; it keeps what backward needs until the next forward.  h and the weight are kept as they are, not copied: backward
     refuses where torch has changed one of them since.  rng (int64 [2] on the device: seed, offset) is counted on by every forward that drops: a captured step draws anew at each replay.
@@ -93,7 +93,7 @@ class Vsa2Layer:
     """params: the attention's problem (make_params; out_dtype BF16); hidden: channels of x; rope_channels: channels of a head that turn with (t, h, w).
 
     set_weights takes w_qkv [(Hq + 2 Hkv) D, C] bf16 or fp32 (rows: q's heads, k's, v's), w_g [C, Hq] bf16 and the norms' weights fp32 [D] (None: ones); forward keeps what
-    backward needs until the next forward.  x, o and the weights of the gate and of the norms are kept as they are, not copied: they, and the weights that were set, have to stay until
+    backward needs until the next forward (with an int8 projection, which has none, nothing).  x, o and the weights of the gate and of the norms are kept as they are, not copied: they, and the weights that were set, have to stay until
     backward returns.  It refuses where torch or set_weights has changed one of them since (what other kernels write into them it cannot see)."""
 
     def __init__(self, params, hidden, rope_channels, theta=1e4, scale=1.0, layout=vb.ROPE_PAIRS, eps=1e-6, device="cuda", projection="fp8"):
